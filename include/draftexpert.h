@@ -78,7 +78,8 @@ enum {
   DX_DEV_BAD_EXPERT_ID = 1,     /* a routed expert has no weight blob attached */
   DX_DEV_WAIT_EXPIRED = 2,      /* a bounded wait inside a kernel gave up */
   DX_DEV_WORKLIST_OVERFLOW = 3,
-  DX_DEV_BOUNDS = 4             /* checked build only (-DDX_CHECKED): an index left its range; the access was skipped */
+  DX_DEV_BOUNDS = 4,            /* checked build only (-DDX_CHECKED): an index left its range; the access was skipped */
+  DX_DEV_BAD_TOKEN = 5          /* a token id outside the vocabulary (spec_token_logprobs, spec_distill_topk) */
 };
 
 typedef struct dx_ctx dx_ctx;
@@ -387,6 +388,78 @@ dx_status moe_draft_expert_term(dx_layer* layer, const float* h, int32_t K, floa
 dx_status moe_router_agreement(dx_layer* layer, const float* h_star, const float* h_draft, int32_t K, float* kl,
                                int32_t* agree, void* stream);
 dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t n, float* out, void* stream);
+
+/* ---- whole batches of tokens: scoring, distillation, routing --------------------------------------------------------
+ * What a drafter is scored, trained and routed with outside the decode step: any number of rows N >= 0 (N = 0 does
+ * nothing), one launch per call (moe_route_tokens: two for large batches), no device memory besides the context's
+ * scratch, the same results on every run, safe to capture into CUDA graphs.  The context's GPU need not be the
+ * current device.  Logits and their gradients are fp32 or bf16 (dtype: DX_DTYPE_FP32 / DX_DTYPE_BF16), rows `ld`
+ * elements apart (ld >= the row's length, any value; columns behind the row are neither read nor written), their
+ * address a multiple of the element size; 16-byte aligned rows are fastest.  Everything else is fp32 / int32, dense.
+ * Arithmetic is fp32 (per-row scalars of the loss: fp64); a bf16 gradient is rounded once.
+ *
+ * spec_token_logprobs: for each row t, with p = softmax(logits[t] / temperature):
+ *     logprob[t] = log p[tokens[t]];  tokens[t] = -1 (no token, padding) gives 0, any other id outside [0, V) gives NaN
+ *     and DX_DEV_BAD_TOKEN.  entropy[t] = -sum_v p_v log p_v.  top_ids / top_logprobs [N, n_top]: the n_top largest
+ *     logits in descending order (ties: lower id first) and their log probabilities -- with n_top and temperature as the
+ *     teacher's, the input of spec_distill_topk.
+ *   A logit of -inf is a masked word: no mass, last in the order.  A row of nothing but -inf has log probabilities
+ *   -inf and entropy 0.  A row with a NaN or +inf has NaN log probabilities and entropy; in the order of its
+ *   alternatives NaN comes last.  tokens and logprob may both be NULL, entropy may be NULL; n_top <= 32, n_top <= V
+ *   (0: top_ids / top_logprobs are not looked at); temperature in [1e-4, 1e4].
+ *
+ * spec_distill_topk: distillation from a teacher's top log probabilities (the logit distillation loss of Sec. 3.3,
+ *   Eq. 8, with the teacher cut to a list of k <= 128 words per row).  teacher_ids / teacher_logprobs [N, k]; an id of -1
+ *   is an unused entry, an id listed twice in a row counts once (its first entry), any other id outside [0, V) is left
+ *   out and reported as DX_DEV_BAD_TOKEN.  With q = softmax(logits[t] / temperature) and p_j = exp(teacher_logprobs):
+ *     tail = 0: p renormalised over the listed words, L_t = sum_j p_j (log p_j - log q_j)  (a list without mass: 0);
+ *     tail = 1: p as given, and the rest r = max(0, 1 - sum_j p_j) in one bucket against the student's mass R on all
+ *               unlisted words: L_t = sum_j p_j (log p_j - log q_j) + r (log r - log R).
+ *   loss [N] = L_t.  dlogits (pitch ld_d) = row_weight[t] * dL_t / dlogits, zeros and loss 0 for rows whose weight is 0
+ *   or that list no word (their logits are not looked at).  row_weight NULL: all 1.  loss or dlogits may be NULL.
+ *   dlogits may be the logits buffer itself (same pitch); it must not overlap it otherwise (DX_ERR_INVALID_ARG).
+ *   A listed word that the student gives no mass makes the loss +inf (its gradient stays finite); a row of nothing but
+ *   -inf has loss +inf and gradient 0.  A row must fit the shared memory of 16 SMs (about 1.8 million bf16 logits;
+ *   DX_ERR_UNSUPPORTED beyond).
+ *
+ * moe_route_tokens: the router of Eq. 4 from its logits [N, E], for a batch, with the forms larger MoE models use:
+ *     r = softmax or sigmoid (score_fn);  selection by r_e + select_bias[e] (the bias -- the one load balancing adjusts
+ *     -- takes part in the selection only; NULL: by the logits, whose order is that of the scores);  n_groups groups of
+ *     E / n_groups consecutive experts, ranked by their largest selection value (group_score DX_GROUP_MAX) or the sum
+ *     of their two largest (DX_GROUP_TOP2; without a bias both rank the scores), of which the topk_groups best stay;
+ *     the top_k best experts of those.  Ties go to the lower id; the selection is that of exact arithmetic.
+ *     topk_ids [N, k], topk_w [N, k] = routed_scale * r_e, or routed_scale * r_e / sum of the selected (norm_topk).
+ *     offsets [E+1] and perm [N*k] as in moe_verify_block (both or neither may be NULL).
+ *   A logit of -inf is a masked expert: selected only where too few others are left, with gate weight 0 (so is a whole
+ *   row of them), whatever its bias; a NaN is selected like a masked expert.  E <= 256, k <= 8, n_groups <= 32,
+ *   N * k < 2^31.
+ * moe_route_tokens_backward: d_logits [N, E] (pitch ld_d, type of the logits, written whole) from the gradient of topk_w,
+ *   for the selection in topk_ids (which has no gradient).  An id outside [0, E) is left out and reported as
+ *   DX_DEV_BAD_EXPERT_ID; an expert listed twice gets both gradients.  d_logits must not overlap the logits. */
+enum { DX_GROUP_MAX = 0, DX_GROUP_TOP2 = 1 };
+typedef struct {
+  int32_t n_experts;     /* E */
+  int32_t top_k;         /* k */
+  int32_t score_fn;      /* DX_SCORE_* */
+  int32_t norm_topk;     /* 1: gate weights renormalised over the selected k */
+  int32_t n_groups;      /* 1 = no groups; a divisor of E */
+  int32_t topk_groups;   /* groups that stay, 1 .. n_groups, with at least k experts in them */
+  int32_t group_score;   /* DX_GROUP_* */
+  float routed_scale;
+} dx_route_desc;
+dx_status spec_token_logprobs(dx_ctx* ctx, const void* logits, int32_t dtype, int32_t N, int32_t V, int64_t ld,
+                              const int32_t* tokens, float temperature, int32_t n_top, float* logprob, float* entropy,
+                              int32_t* top_ids, float* top_logprobs, void* stream);
+dx_status spec_distill_topk(dx_ctx* ctx, const void* logits, int32_t dtype, int32_t N, int32_t V, int64_t ld,
+                            const int32_t* teacher_ids, const float* teacher_logprobs, int32_t k, int32_t tail,
+                            float temperature, const float* row_weight, float* loss, void* dlogits, int64_t ld_d,
+                            void* stream);
+dx_status moe_route_tokens(dx_ctx* ctx, const dx_route_desc* desc, const void* logits, int32_t dtype, int32_t N,
+                           int64_t ld, const float* select_bias, int32_t* topk_ids, float* topk_w, int32_t* offsets,
+                           int32_t* perm, void* stream);
+dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, const void* logits, int32_t dtype, int32_t N,
+                                    int64_t ld, const int32_t* topk_ids, const float* d_topk_w, void* d_logits,
+                                    int64_t ld_d, void* stream);
 
 /* ---- greedy verification without any allocation ----------------------------------------------------------------
  * (No counterpart in the paper: an addition for callers of this library that cannot allocate device memory --

@@ -38,6 +38,12 @@ class LayerDesc(C.Structure):
                 ("routed_scale", C.c_float), ("draft_gamma", C.c_float)]
 
 
+class RouteDesc(C.Structure):
+    _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("score_fn", C.c_int32), ("norm_topk", C.c_int32),
+                ("n_groups", C.c_int32), ("topk_groups", C.c_int32), ("group_score", C.c_int32),
+                ("routed_scale", C.c_float)]
+
+
 class CacheStats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("lookups", "hits", "on_demand", "prefetch_issued", "prefetch_used",
                                          "prefetch_wasted", "evictions", "bytes_h2d", "waited_copies", "stall_ns",
@@ -103,6 +109,10 @@ SIGNATURES = {
     "moe_draft_expert_term": (_I, [_P, _P, _I, _P, _P]),
     "moe_router_agreement": (_I, [_P, _P, _P, _I, _P, _P, _P]),
     "dx_squared_error": (_I, [_P, _P, _P, C.c_int64, _P, _P]),
+    "spec_token_logprobs": (_I, [_P, _P, _I, _I, _I, C.c_int64, _P, C.c_float, _I, _P, _P, _P, _P, _P]),
+    "spec_distill_topk": (_I, [_P, _P, _I, _I, _I, C.c_int64, _P, _P, _I, _I, C.c_float, _P, _P, _P, C.c_int64, _P]),
+    "moe_route_tokens": (_I, [_P, C.POINTER(RouteDesc), _P, _I, _I, C.c_int64, _P, _P, _P, _P, _P, _P]),
+    "moe_route_tokens_backward": (_I, [_P, C.POINTER(RouteDesc), _P, _I, _I, C.c_int64, _P, _P, _P, C.c_int64, _P]),
     "expert_cache_create": (_I, [_P, _I, _I, _I, C.c_size_t, C.POINTER(_P)]),
     "expert_cache_set_q4": (_I, [_P, C.POINTER(LayerDesc), _I]),
     "expert_cache_destroy": (_I, [_P]),
@@ -681,6 +691,133 @@ def squared_error(ctx: Context, a: torch.Tensor, b: torch.Tensor) -> torch.Tenso
     """sum (a - b)^2 (with moe_draft_expert_term and moe_missing_residual: one layer's term of Eq. 7)."""
     out = torch.empty((1,), dtype=torch.float32, device=a.device)
     _check(ctx.lib.dx_squared_error(ctx.handle, _ptr(a), _ptr(b), a.numel(), _ptr(out), _stream()), "dx_squared_error")
+    return out
+
+
+# ---- whole batches of tokens: scoring, distillation, routing (the library takes raw pointers, so what a pointer cannot
+# show -- type, device, layout -- is checked here) -----------------------------------------------------------------------
+def _matrix(ctx: Context, t: torch.Tensor, name: str) -> Tuple[int, int]:
+    """dtype code and row pitch of a [rows, cols] matrix of logits on the context's GPU."""
+    if t.dim() != 2 or t.device.type != "cuda" or t.device.index != ctx.device:
+        raise ValueError(f"{name}: a 2-d tensor on cuda:{ctx.device} is expected")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name}: float32 or bfloat16 is expected, not {t.dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    return (1 if t.dtype == torch.bfloat16 else 0), (int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1]))
+
+
+def _dense(ctx: Context, t: Optional[torch.Tensor], name: str, shape: Sequence[int], dtype: torch.dtype) -> None:
+    if t is None:
+        return
+    if t.device.type != "cuda" or t.device.index != ctx.device or t.dtype != dtype or tuple(t.shape) != tuple(shape) \
+            or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on cuda:{ctx.device} is expected")
+
+
+def _ctx_stream(ctx: Context) -> int:
+    return torch.cuda.current_stream(ctx.device).cuda_stream
+
+
+def spec_token_logprobs(ctx: Context, logits: torch.Tensor, tokens: Optional[torch.Tensor], top_n: int = 0,
+                        temperature: float = 1.0, out: Optional[Dict[str, torch.Tensor]] = None
+                        ) -> Dict[str, torch.Tensor]:
+    """For rows of logits [N, V] (float32 / bfloat16, any row pitch): ``logprob`` [N] of the given tokens (int32, -1 =
+    none), ``entropy`` [N] and, with ``top_n`` > 0, ``top_ids`` / ``top_logprobs`` [N, top_n]."""
+    dt, ld = _matrix(ctx, logits, "logits")
+    N, V = logits.shape
+    if out is None:
+        f32 = dict(dtype=torch.float32, device=logits.device)
+        out = {} if tokens is None else {"logprob": torch.empty((N,), **f32)}
+        out["entropy"] = torch.empty((N,), **f32)
+        if top_n > 0:
+            out["top_ids"] = torch.empty((N, top_n), dtype=torch.int32, device=logits.device)
+            out["top_logprobs"] = torch.empty((N, top_n), **f32)
+    _dense(ctx, tokens, "tokens", (N,), torch.int32)
+    _dense(ctx, out.get("logprob"), "logprob", (N,), torch.float32)
+    _dense(ctx, out.get("entropy"), "entropy", (N,), torch.float32)
+    _dense(ctx, out.get("top_ids"), "top_ids", (N, top_n), torch.int32)
+    _dense(ctx, out.get("top_logprobs"), "top_logprobs", (N, top_n), torch.float32)
+    _check(ctx.lib.spec_token_logprobs(ctx.handle, _ptr(logits), dt, N, V, ld, _ptr(tokens), float(temperature), top_n,
+                                       _ptr(out.get("logprob")), _ptr(out.get("entropy")), _ptr(out.get("top_ids")),
+                                       _ptr(out.get("top_logprobs")), _ctx_stream(ctx)), "spec_token_logprobs")
+    return out
+
+
+def spec_distill_topk(ctx: Context, logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logprobs: torch.Tensor,
+                      tail: bool = False, temperature: float = 1.0, row_weight: Optional[torch.Tensor] = None,
+                      grad: bool = True, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """Distillation from a teacher's top log probabilities: ``loss`` [N] and, with ``grad``, ``dlogits`` [N, V] =
+    row_weight * dloss / dlogits (pass ``out={"loss": ..., "dlogits": logits}`` to overwrite the logits)."""
+    dt, ld = _matrix(ctx, logits, "logits")
+    N, V = logits.shape
+    if teacher_ids.dim() != 2:
+        raise ValueError("teacher_ids: [N, k] is expected")
+    k = int(teacher_ids.shape[1])
+    if out is None:
+        out = {"loss": torch.empty((N,), dtype=torch.float32, device=logits.device)}
+        if grad:
+            out["dlogits"] = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+    _dense(ctx, teacher_ids, "teacher_ids", (N, k), torch.int32)
+    _dense(ctx, teacher_logprobs, "teacher_logprobs", (N, k), torch.float32)
+    _dense(ctx, row_weight, "row_weight", (N,), torch.float32)
+    _dense(ctx, out.get("loss"), "loss", (N,), torch.float32)
+    d, ld_d = out.get("dlogits") if grad else None, V
+    if d is not None:
+        if d.dtype != logits.dtype or tuple(d.shape) != (N, V):
+            raise ValueError("dlogits: the logits' shape and type are expected")
+        ld_d = _matrix(ctx, d, "dlogits")[1]
+    _check(ctx.lib.spec_distill_topk(ctx.handle, _ptr(logits), dt, N, V, ld, _ptr(teacher_ids), _ptr(teacher_logprobs),
+                                     k, 1 if tail else 0, float(temperature), _ptr(row_weight), _ptr(out.get("loss")),
+                                     _ptr(d), ld_d, _ctx_stream(ctx)), "spec_distill_topk")
+    return out
+
+
+def moe_route_tokens(ctx: Context, logits: torch.Tensor, top_k: int, score_fn: int = 0, norm_topk: int = 1,
+                     routed_scale: float = 1.0, select_bias: Optional[torch.Tensor] = None, n_groups: int = 1,
+                     topk_groups: int = 1, group_score: int = 0, out: Optional[Dict[str, torch.Tensor]] = None
+                     ) -> Dict[str, torch.Tensor]:
+    """Expert selection for a batch of router logits [N, E]: ``topk_ids`` / ``topk_w`` [N, k], ``offsets`` [E+1] and
+    ``perm`` [N*k] (token-expert pairs by expert).  ``group_score``: 0 largest value, 1 sum of the two largest."""
+    dt, ld = _matrix(ctx, logits, "logits")
+    N, E = logits.shape
+    if out is None:
+        i32 = dict(dtype=torch.int32, device=logits.device)
+        out = {"topk_ids": torch.empty((N, top_k), **i32),
+               "topk_w": torch.empty((N, top_k), dtype=torch.float32, device=logits.device),
+               "offsets": torch.empty((E + 1,), **i32), "perm": torch.empty((N * top_k,), **i32)}
+    _dense(ctx, select_bias, "select_bias", (E,), torch.float32)
+    _dense(ctx, out["topk_ids"], "topk_ids", (N, top_k), torch.int32)
+    _dense(ctx, out["topk_w"], "topk_w", (N, top_k), torch.float32)
+    _dense(ctx, out.get("offsets"), "offsets", (E + 1,), torch.int32)
+    _dense(ctx, out.get("perm"), "perm", (N * top_k,), torch.int32)
+    d = RouteDesc(E, top_k, score_fn, norm_topk, n_groups, topk_groups, group_score, float(routed_scale))
+    _check(ctx.lib.moe_route_tokens(ctx.handle, C.byref(d), _ptr(logits), dt, N, ld, _ptr(select_bias),
+                                    _ptr(out["topk_ids"]), _ptr(out["topk_w"]), _ptr(out.get("offsets")),
+                                    _ptr(out.get("perm")), _ctx_stream(ctx)), "moe_route_tokens")
+    return out
+
+
+def moe_route_tokens_backward(ctx: Context, logits: torch.Tensor, topk_ids: torch.Tensor, d_topk_w: torch.Tensor,
+                              score_fn: int = 0, norm_topk: int = 1, routed_scale: float = 1.0,
+                              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of ``topk_w`` (``d_topk_w`` [N, k]) with respect to the router logits, for the selection ``topk_ids``."""
+    dt, ld = _matrix(ctx, logits, "logits")
+    N, E = logits.shape
+    if topk_ids.dim() != 2:
+        raise ValueError("topk_ids: [N, k] is expected")
+    k = int(topk_ids.shape[1])
+    _dense(ctx, topk_ids, "topk_ids", (N, k), torch.int32)
+    _dense(ctx, d_topk_w, "d_topk_w", (N, k), torch.float32)
+    if out is None:
+        out = torch.empty((N, E), dtype=logits.dtype, device=logits.device)
+    if out.dtype != logits.dtype or tuple(out.shape) != (N, E):
+        raise ValueError("out: the logits' shape and type are expected")
+    ld_d = _matrix(ctx, out, "out")[1]
+    d = RouteDesc(E, k, score_fn, norm_topk, 1, 1, 0, float(routed_scale))
+    _check(ctx.lib.moe_route_tokens_backward(ctx.handle, C.byref(d), _ptr(logits), dt, N, ld, _ptr(topk_ids),
+                                             _ptr(d_topk_w), _ptr(out), ld_d, _ctx_stream(ctx)),
+           "moe_route_tokens_backward")
     return out
 
 

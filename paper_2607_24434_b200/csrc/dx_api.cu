@@ -46,6 +46,9 @@ extern "C" dx_status dx_create(int device, dx_ctx** out) {
   if (e == cudaSuccess) e = cudaMalloc(&ctx->handover, 4 * sizeof(unsigned int));
   if (e == cudaSuccess) e = cudaMemset(ctx->handover, 0, 4 * sizeof(unsigned int));
   if (e == cudaSuccess) e = cudaMalloc(&ctx->conf_part, sizeof(float2) * 8 * ctx->sm_count * DX_MAX_M);
+  if (e == cudaSuccess) e = cudaMalloc(&ctx->route_counts, sizeof(int32_t) * 2 * ctx->sm_count * DX_MAX_E);
+  if (e == cudaSuccess) e = dx_logprobs_prepare();
+  if (e == cudaSuccess) e = dx_distill_prepare(ctx);
   if (e == cudaSuccess) e = cudaMalloc(&ctx->scratch_i32, sizeof(int32_t) * 2);
   if (e == cudaSuccess) e = cudaMalloc(&ctx->union_dev, sizeof(int32_t) * (DX_MAX_E + 1 + DX_MAX_TOPK));
   if (e == cudaSuccess) e = cudaHostAlloc((void**)&ctx->union_host, sizeof(int32_t) * (DX_MAX_E + 1 + DX_MAX_TOPK),
@@ -72,6 +75,7 @@ extern "C" dx_status dx_destroy(dx_ctx* ctx) {
   cudaFree(ctx->dev_status);
   cudaFree(ctx->handover);
   cudaFree(ctx->conf_part);
+  cudaFree(ctx->route_counts);
   cudaFree(ctx->scratch_i32);
   cudaFree(ctx->union_dev);
   if (ctx->union_host) cudaFreeHost(ctx->union_host);
@@ -800,6 +804,149 @@ extern "C" dx_status spec_draft_token(dx_ctx* ctx, const float* h, int32_t M, co
   if (w_dtype == DX_DTYPE_BF16 && (size_t)((M + 7) / 8) * H * 32 > (size_t)ctx->smem_optin) return DX_ERR_UNSUPPORTED;
   DX_CUDA(ctx, dx_launch_accept(ctx, h, M, W_lm, V, H, w_dtype, nullptr, 0, rms_norm, token, ctx->scratch_i32,
                                 ctx->scratch_i32 + 1, confidence, (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+// ---- whole batches of tokens ------------------------------------------------------------------------------------
+namespace {
+
+// the context's GPU for the length of a call
+struct DeviceScope {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceScope(int device) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != device) err = cudaSetDevice(device);
+    if (err == cudaSuccess && before == device) before = -1;
+  }
+  ~DeviceScope() {
+    if (before >= 0) (void)cudaSetDevice(before);
+  }
+};
+
+dx_status check_rows(const void* p, int32_t dtype, int32_t N, int32_t len, int64_t ld) {
+  if (dtype != DX_DTYPE_FP32 && dtype != DX_DTYPE_BF16) return DX_ERR_INVALID_ARG;
+  if (N < 0 || len < 1 || ld < len) return DX_ERR_SHAPE;
+  const int64_t elem = dtype == DX_DTYPE_FP32 ? 4 : 2;
+  if (N > 0 && (!p || (uintptr_t)p % elem)) return DX_ERR_INVALID_ARG;
+  // (the last row's end must be addressable)
+  if (ld > (INT64_MAX / 8) / (N > 0 ? N : 1)) return DX_ERR_SHAPE;
+  return DX_OK;
+}
+// [N rows of len elements, ld apart] against another such matrix of the same element size
+bool rows_overlap(const void* a, int64_t ld_a, const void* b, int64_t ld_b, int32_t N, int32_t len, int64_t elem) {
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  const uintptr_t a1 = a0 + (uintptr_t)(((int64_t)(N - 1) * ld_a + len) * elem);
+  const uintptr_t b1 = b0 + (uintptr_t)(((int64_t)(N - 1) * ld_b + len) * elem);
+  return a0 < b1 && b0 < a1;
+}
+bool temperature_ok(float t) { return t >= 1e-4f && t <= 1e4f; }
+
+dx_status check_route(const dx_route_desc* d, bool groups) {
+  if (!d) return DX_ERR_INVALID_ARG;
+  if (d->score_fn != DX_SCORE_SOFTMAX && d->score_fn != DX_SCORE_SIGMOID) return DX_ERR_INVALID_ARG;
+  if (d->n_experts < 1 || d->top_k < 1 || d->top_k > d->n_experts) return DX_ERR_SHAPE;
+  if (d->n_experts > DX_MAX_E || d->top_k > DX_MAX_TOPK) return DX_ERR_UNSUPPORTED;
+  if (!groups) return DX_OK;
+  if (d->group_score != DX_GROUP_MAX && d->group_score != DX_GROUP_TOP2) return DX_ERR_INVALID_ARG;
+  if (d->n_groups < 1 || d->n_experts % d->n_groups || d->topk_groups < 1 || d->topk_groups > d->n_groups)
+    return DX_ERR_SHAPE;
+  if (d->topk_groups * (d->n_experts / d->n_groups) < d->top_k) return DX_ERR_SHAPE;
+  if (d->n_groups > DX_MAX_GROUPS) return DX_ERR_UNSUPPORTED;
+  return DX_OK;
+}
+
+}  // namespace
+
+extern "C" dx_status spec_token_logprobs(dx_ctx* ctx, const void* logits, int32_t dtype, int32_t N, int32_t V, int64_t ld,
+                                         const int32_t* tokens, float temperature, int32_t n_top, float* logprob,
+                                         float* entropy, int32_t* top_ids, float* top_logprobs, void* stream) {
+  if (!ctx || !temperature_ok(temperature)) return DX_ERR_INVALID_ARG;
+  dx_status s = check_rows(logits, dtype, N, V, ld);
+  if (s != DX_OK) return s;
+  if (n_top < 0 || n_top > V) return DX_ERR_SHAPE;
+  if (n_top > DX_MAX_TOP) return DX_ERR_UNSUPPORTED;
+  if (N == 0) return DX_OK;
+  if ((tokens == nullptr) != (logprob == nullptr)) return DX_ERR_INVALID_ARG;
+  if (n_top > 0 && (!top_ids || !top_logprobs)) return DX_ERR_INVALID_ARG;
+  if (!logprob && !entropy && n_top == 0) return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DX_CUDA(ctx, dx_launch_logprobs(ctx, logits, dtype, N, V, (long long)ld, tokens, temperature, n_top, logprob, entropy,
+                                  top_ids, top_logprobs, (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+extern "C" dx_status spec_distill_topk(dx_ctx* ctx, const void* logits, int32_t dtype, int32_t N, int32_t V, int64_t ld,
+                                       const int32_t* teacher_ids, const float* teacher_logprobs, int32_t k, int32_t tail,
+                                       float temperature, const float* row_weight, float* loss, void* dlogits,
+                                       int64_t ld_d, void* stream) {
+  if (!ctx || !temperature_ok(temperature) || (tail != 0 && tail != 1)) return DX_ERR_INVALID_ARG;
+  dx_status s = check_rows(logits, dtype, N, V, ld);
+  if (s != DX_OK) return s;
+  if (k < 1) return DX_ERR_SHAPE;
+  if (k > DX_MAX_TEACHER) return DX_ERR_UNSUPPORTED;
+  const int64_t elem = dtype == DX_DTYPE_FP32 ? 4 : 2;
+  if ((uint64_t)V * (uint64_t)elem > (uint64_t)dx_distill_max_row_bytes(ctx)) return DX_ERR_UNSUPPORTED;
+  if (dlogits) {
+    s = check_rows(dlogits, dtype, N, V, ld_d);
+    if (s != DX_OK) return s;
+  }
+  if (N == 0) return DX_OK;
+  if (!teacher_ids || !teacher_logprobs || (!loss && !dlogits)) return DX_ERR_INVALID_ARG;
+  if (dlogits && !(dlogits == logits && ld == ld_d) && rows_overlap(logits, ld, dlogits, ld_d, N, V, elem))
+    return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DX_CUDA(ctx, dx_launch_distill(ctx, logits, dtype, N, V, (long long)ld, teacher_ids, teacher_logprobs, k, tail,
+                                 temperature, row_weight, loss, dlogits, (long long)ld_d, (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+extern "C" dx_status moe_route_tokens(dx_ctx* ctx, const dx_route_desc* desc, const void* logits, int32_t dtype, int32_t N,
+                                      int64_t ld, const float* select_bias, int32_t* topk_ids, float* topk_w,
+                                      int32_t* offsets, int32_t* perm, void* stream) {
+  if (!ctx) return DX_ERR_INVALID_ARG;
+  dx_status s = check_route(desc, true);
+  if (s != DX_OK) return s;
+  s = check_rows(logits, dtype, N, desc->n_experts, ld);
+  if (s != DX_OK) return s;
+  if ((int64_t)N * desc->top_k > INT32_MAX) return DX_ERR_UNSUPPORTED;
+  if (N > 0 && (!topk_ids || !topk_w || (offsets == nullptr) != (perm == nullptr))) return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  if (N == 0) {   // no pairs: every expert's run is empty
+    if (offsets)
+      DX_CUDA(ctx, cudaMemsetAsync(offsets, 0, sizeof(int32_t) * (desc->n_experts + 1), (cudaStream_t)stream));
+    return DX_OK;
+  }
+  int n = 0;
+  DX_CUDA(ctx, dx_launch_batch_route(ctx, *desc, logits, dtype, N, (long long)ld, select_bias, topk_ids, topk_w, offsets,
+                                     perm, (cudaStream_t)stream, &n));
+  ctx->launches += n;
+  return DX_OK;
+}
+
+extern "C" dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, const void* logits, int32_t dtype,
+                                               int32_t N, int64_t ld, const int32_t* topk_ids, const float* d_topk_w,
+                                               void* d_logits, int64_t ld_d, void* stream) {
+  if (!ctx) return DX_ERR_INVALID_ARG;
+  dx_status s = check_route(desc, false);
+  if (s != DX_OK) return s;
+  s = check_rows(logits, dtype, N, desc->n_experts, ld);
+  if (s == DX_OK) s = check_rows(d_logits, dtype, N, desc->n_experts, ld_d);
+  if (s != DX_OK) return s;
+  if (N == 0) return DX_OK;
+  if (!topk_ids || !d_topk_w) return DX_ERR_INVALID_ARG;
+  if (rows_overlap(logits, ld, d_logits, ld_d, N, desc->n_experts, dtype == DX_DTYPE_FP32 ? 4 : 2))
+    return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DX_CUDA(ctx, dx_launch_route_grad(ctx, *desc, logits, dtype, N, (long long)ld, topk_ids, d_topk_w, d_logits,
+                                    (long long)ld_d, (cudaStream_t)stream));
   ctx->launches++;
   return DX_OK;
 }

@@ -18,6 +18,11 @@
 #define DX_MAX_ENTRIES (DX_MAX_SHARED + 1 + DX_MAX_PAIRS)
 #define DX_TILE_I 8            // intermediate rows per streamed weight tile
 #define DX_MAX_M 16            // accept rows
+#define DX_MAX_TOP 32          // alternatives per row of spec_token_logprobs
+#define DX_MAX_TEACHER 128     // teacher entries per row of spec_distill_topk
+#define DX_ROW_CLUSTER_MAX 16  // CTAs that share a row of logits
+#define DX_ROW_SLICE_BYTES 52000   // ... and the bytes of it one CTA holds when there are many rows (four CTAs per SM)
+#define DX_MAX_GROUPS 32       // expert groups of moe_route_tokens
 #define DX_ROUTE_CLUSTER 4     // CTAs (and SMs) of the routing kernel; the expert kernel leaves them free
 
 // What the routing kernel hands to the expert kernels.  The routing-independent groups (shared experts, draft
@@ -79,6 +84,7 @@ struct dx_ctx {
   int32_t* dev_status;
   unsigned int* handover;      // device word {block input final}: see DxExpertParams
   float2* conf_part;           // [8 * sm_count][DX_MAX_M] per-CTA online-softmax pairs of the confidence variant
+  int32_t* route_counts;       // [2 * sm_count][DX_MAX_E] experts selected per CTA of the batch routing kernel
   int32_t* scratch_i32;        // two ints the draft-token entry point parks unused outputs in
   int32_t* union_dev;          // [DX_MAX_E] union ids, [1] union count, [DX_MAX_TOPK] draft selection: what the
   int32_t* union_host;         //   cached entry points read on the host (page-locked and mapped; the routing kernel writes it)
@@ -246,6 +252,22 @@ cudaError_t dx_launch_accept(dx_ctx* ctx, const float* h, int M, const void* W_l
 cudaError_t dx_launch_router_agreement(const dx_layer* L, const float* h_star, const float* h_draft, int K, float* kl,
                                        int32_t* agree, cudaStream_t st);
 cudaError_t dx_launch_squared_error(const float* a, const float* b, long long n, float* out, cudaStream_t st);
+cudaError_t dx_logprobs_prepare();
+cudaError_t dx_launch_logprobs(dx_ctx* ctx, const void* logits, int dtype, int N, int V, long long ld,
+                               const int32_t* tokens, float temperature, int n_top, float* logprob, float* entropy,
+                               int32_t* top_ids, float* top_logprobs, cudaStream_t st);
+cudaError_t dx_distill_prepare(const dx_ctx* ctx);
+size_t dx_distill_max_row_bytes(const dx_ctx* ctx);
+cudaError_t dx_launch_distill(dx_ctx* ctx, const void* logits, int dtype, int N, int V, long long ld,
+                              const int32_t* teacher_ids, const float* teacher_logprobs, int k, int tail,
+                              float temperature, const float* row_weight, float* loss, void* dlogits, long long ld_d,
+                              cudaStream_t st);
+cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const void* logits, int dtype, int N,
+                                  long long ld, const float* bias, int32_t* topk_ids, float* topk_w, int32_t* offsets,
+                                  int32_t* perm, cudaStream_t st, int* n_launches);
+cudaError_t dx_launch_route_grad(dx_ctx* ctx, const dx_route_desc& d, const void* logits, int dtype, int N,
+                                 long long ld, const int32_t* topk_ids, const float* d_topk_w, void* d_logits,
+                                 long long ld_d, cudaStream_t st);
 cudaError_t dx_experts_prepare(dx_ctx* ctx);   // opt-in shared memory attributes, once per context
 
 // cache hooks used by the layer code
