@@ -6,15 +6,18 @@
 // One launch reads each logit once and writes each gradient once: a cluster of CTAs holds the row in shared memory
 // between the statistics and the gradient.
 //
-// The unlisted words are summed apart from the listed ones (whose places in shared memory are set to -inf before the
-// sweep), relative to their own maximum: R never comes out of a difference of nearly equal sums, and neither R nor the
-// factor r / R can under- or overflow however far the listed words stand above the rest.  Per-row scalars (teacher
-// mass, loss) are 64-bit: the loss is a small difference of logarithms.
+// The unlisted words are summed apart from the listed ones, relative to their own maximum: R never comes out of a
+// difference of nearly equal sums, and neither R nor the factor r / R can under- or overflow however far the listed
+// words stand above the rest.  The sweep leaves vectors that hold a listed word out (a bit per vector says so); a thread
+// per list entry adds what else is in them afterwards.  Per-row scalars (teacher mass, loss) are 64-bit: the loss is a
+// small difference of logarithms.
 #include "dx_rows.cuh"
 
 namespace {
 
-constexpr int kListLanes = DX_MAX_TEACHER / 32;   // list entries per lane of the warp that handles the list
+constexpr int kUnroll = 4;
+constexpr int kStaticBytes = 1024;                // at least the kernel's static shared memory
+constexpr int kListWarps = DX_MAX_TEACHER / 32;   // thread j < k has list entry j
 
 struct DistillParams {
   const void* logits;
@@ -22,7 +25,7 @@ struct DistillParams {
   long long ld, ld_d;
   const int32_t* ids;
   const float* lp;
-  float c, T;                 // log2(e) / T, T
+  float c, c_lo, T;           // log2(e) / T in two parts, T
   const float* weight;
   float* loss;
   void* dlogits;
@@ -46,20 +49,26 @@ __device__ __forceinline__ float warp_max(float v) {
   for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
-__device__ __forceinline__ void copy16(uint4* dst_smem, const uint4* src) {
-  const uint32_t d = static_cast<uint32_t>(__cvta_generic_to_shared(dst_smem));
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
-}
+
+// What the list entries of one warp contribute, relative to the warp's largest listed logit (unnormalised p).
+struct ListPart {
+  double mass, p_log_p, p_u, sum_e;
+  float z_ref;
+  int pad;
+};
 
 template <typename T, bool kGrad>
 __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParams p, int C) {
   using V16 = RowVec<T>;
-  extern __shared__ uint4 s_row[];                 // this CTA's vectors of the row
+  extern __shared__ uint4 s_dyn[];                 // bit u of byte [chunk][thread]: vector u of that chunk holds a listed
+  unsigned int* s_mark = reinterpret_cast<unsigned int*>(s_dyn);   // word; behind it (kGrad) the CTA's vectors of the row
   __shared__ MaxSum s_warp[kRowWarps];
   __shared__ MaxSum s_cta;
-  __shared__ float s_coef, s_ref;
+  __shared__ ListPart s_list[kListWarps];
+  __shared__ int s_ids[DX_MAX_TEACHER];
+  __shared__ float s_coef, s_ref, s_max;
+  __shared__ double s_norm, s_beta;
   __shared__ unsigned int s_edge;                  // head (bits 0..7) and tail (8..15) elements that are listed
-  __shared__ int s_used;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = C > 1 ? (int)cluster_rank() : 0;
   const int t = blockIdx.x / C;
@@ -67,6 +76,8 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
   T* out = kGrad ? reinterpret_cast<T*>(p.dlogits) + (size_t)t * (size_t)p.ld_d : nullptr;
   const RowSplit sp = row_split(row, p.V, rank, C);
   const int n_vec = sp.v_hi - sp.v_lo;
+  const int chunks = (n_vec + kUnroll * kRowThreads - 1) / (kUnroll * kRowThreads);
+  uint4* s_row = s_dyn + chunks * (kRowThreads / 16);
   const bool has_head = rank == 0 && tid < sp.head, has_tail = rank == C - 1 && tid < sp.tail;
   const int tail0 = p.V - sp.tail;
   // gradient vectors can be stored as such where the output row is aligned like the input row
@@ -74,28 +85,20 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
   const float c = p.c;
   const float w = p.weight ? p.weight[t] : 1.f;
 
-  // ---- the teacher's list (first warp): ids in range, an id counts once
-  int id[kListLanes];
-  bool live = false;
-  if (warp == 0) {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < kListLanes; ++i) {
-      const int j = lane + 32 * i;
-      id[i] = j < p.k ? p.ids[(size_t)t * p.k + j] : -1;
-      bad |= id[i] < -1 || id[i] >= p.V;
-      if (id[i] < 0 || id[i] >= p.V) id[i] = -1;
-      live |= id[i] >= 0;
-    }
-    if (bad && rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
-    live = __any_sync(0xffffffffu, live);
-    if (lane == 0) {
-      s_used = live;
-      s_edge = 0;
+  // ---- the teacher's list
+  int id = -1;
+  if (tid < p.k) {
+    id = p.ids[(size_t)t * p.k + tid];
+    if (id < -1 || id >= p.V) {
+      if (rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
+      id = -1;
     }
   }
-  __syncthreads();
-  if (w == 0.f || !s_used) {   // (the same for every CTA of the row) nothing to learn: the logits are not looked at
+  for (int i = tid; i < chunks * (kRowThreads / 4); i += kRowThreads) s_mark[i] = 0;
+  if (tid < DX_MAX_TEACHER) s_ids[tid] = id;
+  if (tid == 0) s_edge = 0;
+  const int live = __syncthreads_or(id >= 0);
+  if (w == 0.f || !live) {   // (the same for every CTA of the row) nothing to learn: the logits are not looked at
     if (rank == 0 && tid == 0 && p.loss) p.loss[t] = 0.f;
     if (kGrad) {
       if (has_head) out[tid] = V16::round(0.f);
@@ -112,125 +115,146 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
     }
     return;
   }
-  // ---- the row on its way into shared memory
-  const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo;
-  for (int i = tid; i < n_vec; i += kRowThreads) copy16(s_row + i, src + i);
-  asm volatile("cp.async.commit_group;" ::: "memory");
-  float edge_head = has_head ? V16::load(row + tid) : -INFINITY;
-  float edge_tail = has_tail ? V16::load(row + tail0 + tid) : -INFINITY;
-
-  // ---- list statistics relative to the largest listed logit, while the row arrives
-  float z[kListLanes];
-  double pj[kListLanes];
-  float z_ref = 0.f, sum_e = 0.f;
-  double mass = 0.0, p_log_p = 0.0, p_u = 0.0;
-  if (warp == 0) {
-#pragma unroll
-    for (int i = 0; i < kListLanes; ++i) {
-      z[i] = -INFINITY;
-      pj[i] = 0.0;
-      if (32 * i < p.k) {
-        unsigned int same = __match_any_sync(0xffffffffu, id[i]);
-        if (__ffs(same) - 1 != lane) id[i] = -1;   // an earlier lane has it
-#pragma unroll
-        for (int h = 0; h < i; ++h) {
-          for (int o = 0; o < 32; ++o) {
-            const int other = __shfl_sync(0xffffffffu, id[h], o);
-            if (other == id[i]) id[i] = -1;
-          }
-        }
-      }
-      if (id[i] >= 0) {
-        z[i] = V16::load(row + id[i]);
-        pj[i] = exp((double)p.lp[(size_t)t * p.k + lane + 32 * i]);
-      }
-    }
-    z_ref = z[0];
-#pragma unroll
-    for (int i = 1; i < kListLanes; ++i) z_ref = fmaxf(z_ref, z[i]);
-    z_ref = fmaxf(warp_max(z_ref), -FLT_MAX);
-#pragma unroll
-    for (int i = 0; i < kListLanes; ++i) mass += pj[i];
-    mass = warp_sum(mass);
-    const double norm = p.tail || !(mass > 0.0) ? 1.0 : 1.0 / mass;
-    double se = 0.0;
-#pragma unroll
-    for (int i = 0; i < kListLanes; ++i) {
-      pj[i] *= norm;
-      if (id[i] >= 0) {
-        const double u = ((double)z[i] - (double)z_ref) / (double)p.T;
-        se += (double)expf((float)u);
-        if (pj[i] > 0.0) {
-          p_log_p += pj[i] * log(pj[i]);
-          p_u += pj[i] * u;
-        } else {
-          p_log_p += pj[i];   // (0, or the NaN of a NaN entry)
-        }
-      }
-    }
-    p_log_p = warp_sum(p_log_p);
-    p_u = warp_sum(p_u);
-    sum_e = (float)warp_sum(se);
-    mass *= norm;
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();
-  // ---- listed places are taken out of the row
-  if (warp == 0) {
-#pragma unroll
-    for (int i = 0; i < kListLanes; ++i) {
-      if (id[i] < 0) continue;
-      if (id[i] < sp.head) {
-        atomicOr(&s_edge, 1u << id[i]);
-      } else if (id[i] >= tail0) {
-        atomicOr(&s_edge, 256u << (id[i] - tail0));
-      } else {
-        const int e = id[i] - sp.head - sp.v_lo * V16::kN;
-        if (e >= 0 && e < n_vec * V16::kN) reinterpret_cast<T*>(s_row)[e] = V16::round(-INFINITY);
-      }
+  // marks; `vec` is the slice's vector an entry lies in (-1: not this CTA's, or a head / tail element)
+  int vec = -1;
+  bool mine = false;
+  if (id >= 0) {
+    if (id < sp.head) {
+      mine = rank == 0;
+      atomicOr(&s_edge, 1u << id);
+    } else if (id >= tail0) {
+      mine = rank == C - 1;
+      atomicOr(&s_edge, 256u << (id - tail0));
+    } else {
+      const int v = (id - sp.head) / V16::kN - sp.v_lo;
+      mine = v >= 0 && v < n_vec;
+      if (mine) vec = v;
     }
   }
+  const int m_byte = vec / (kUnroll * kRowThreads) * kRowThreads + vec % kRowThreads;     // (of entries with vec >= 0)
+  const unsigned int m_bit = 1u << ((m_byte & 3) * 8 + vec / kRowThreads % kUnroll);
+  if (vec >= 0) atomicOr(&s_mark[m_byte >> 2], m_bit);
+  // an id counts once, with its first entry
+  if (warp * 32 < p.k) {
+    const unsigned int same = __match_any_sync(0xffffffffu, id);
+    if (__ffs(same) - 1 != lane) id = -1;
+    for (int j = 0; j < warp * 32; ++j)
+      if (s_ids[j] == id) id = -1;
+  }
+  if (id < 0) {
+    mine = false;
+    vec = -1;
+  }
+  float z = -INFINITY;
+  double pj = 0.0;
+  if (id >= 0 && (mine || rank == 0)) {
+    z = V16::load(row + id);
+    pj = exp((double)p.lp[(size_t)t * p.k + tid]);
+  }
+  if (rank == 0 && warp * 32 < p.k) {
+    const float z_ref = fmaxf(warp_max(z), -FLT_MAX);
+    const double u = ((double)z - (double)z_ref) / (double)p.T;
+    const double se = warp_sum(id >= 0 ? (double)expf((float)u) : 0.0);
+    const double mass = warp_sum(pj);
+    const bool has = pj > 0.0;                        // (a NaN entry makes the mass NaN, and with it the loss)
+    const double plp = warp_sum(has ? pj * log(pj) : 0.0), pu = warp_sum(has ? pj * u : 0.0);
+    if (lane == 0) s_list[warp] = ListPart{mass, plp, pu, se, z_ref, 0};
+  }
   __syncthreads();
-  const bool head_listed = has_head && (s_edge >> tid & 1u), tail_listed = has_tail && (s_edge >> (8 + tid) & 1u);
-  if (head_listed) edge_head = -INFINITY;
-  if (tail_listed) edge_tail = -INFINITY;
+  const unsigned int edge = s_edge;
+  const bool head_listed = has_head && (edge >> tid & 1u), tail_listed = has_tail && (edge >> (8 + tid) & 1u);
   // ---- maximum and sum of exponentials of the unlisted words
   MaxSum st{-FLT_MAX, 0.f};
-  if (has_head || has_tail) {
-    st.m = fmaxf(st.m, fmaxf(edge_head, edge_tail));
-    if (has_head) st.s += row_ex2((edge_head - st.m) * c);
-    if (has_tail) st.s += row_ex2((edge_tail - st.m) * c);
-  }
-  const unsigned long long c2 = f2_pack(c, c);
-  constexpr int kUnroll = 4;
-  for (int i = tid; i < n_vec; i += kUnroll * kRowThreads) {
-    uint4 v[kUnroll];
-    float top = -INFINITY;
+  const unsigned long long c2 = f2_pack(c, c), cl2 = f2_pack(p.c_lo, p.c_lo);
+  const float edge_head = has_head ? V16::load(row + tid) : -INFINITY;
+  const float edge_tail = has_tail ? V16::load(row + tail0 + tid) : -INFINITY;
+  auto single = [&](float x) {
+    if (x > st.m) {
+      st.s *= row_ex2((st.m - x) * c);
+      st.m = x;
+    }
+    st.s += row_ex2((x - st.m) * c);
+  };
+  if (has_head && !head_listed) single(edge_head);
+  if (has_tail && !tail_listed) single(edge_tail);
+  unsigned long long s2 = f2_pack(st.s, 0.f);
+  auto add = [&](const uint4* v, int n_v, unsigned int skip) {
+    float top;
+    if (skip == 0) {
+      top = V16::largest(v, n_v);
+    } else {
+      top = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      v[u] = i + u * kRowThreads < n_vec
-                 ? s_row[i + u * kRowThreads]
-                 : make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
-      top = fmaxf(top, V16::largest(v[u]));
+      for (int u = 0; u < kUnroll; ++u)
+        if (u < n_v && !(skip >> u & 1u)) top = fmaxf(top, V16::largest(v[u]));
     }
     if (top > st.m) {
-      st.s *= row_ex2((st.m - top) * c);
+      float s0, s1;
+      f2_unpack(s2, s0, s1);
+      s2 = f2_pack((s0 + s1) * row_ex2((st.m - top) * c), 0.f);
       st.m = top;
     }
     const unsigned long long nm2 = f2_pack(-st.m, -st.m);
-    unsigned long long s2 = f2_pack(st.s, 0.f);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
+      if (u < n_v && !(skip >> u & 1u)) {
 #pragma unroll
-      for (int q = 0; q < V16::kN / 2; ++q) {
-        float x0, x1;
-        f2_unpack(f2_mul(f2_add(V16::pair(v[u], q), nm2), c2), x0, x1);
-        s2 = f2_add(s2, f2_pack(row_ex2(x0), row_ex2(x1)));
+        for (int q = 0; q < V16::kN / 2; ++q) {
+          // (the factor in two parts: rounded to one, it would shift the exponents of all words the same way)
+          const unsigned long long d2 = f2_add(V16::pair(v[u], q), nm2);
+          float x0, x1;
+          f2_unpack(f2_fma(d2, cl2, f2_mul(d2, c2)), x0, x1);
+          s2 = f2_add(s2, f2_pack(row_ex2(x0), row_ex2(x1)));
+        }
       }
     }
+  };
+  for (int ch = 0, i = tid; ch < chunks; ++ch, i += kUnroll * kRowThreads) {
+    const unsigned int skip = reinterpret_cast<const unsigned char*>(s_mark)[ch * kRowThreads + tid];
+    uint4 v[kUnroll];
+    if (i + (kUnroll - 1) * kRowThreads < n_vec) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) v[u] = row_vec_stream(row, sp, sp.v_lo + i + u * kRowThreads);
+      if (kGrad) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) s_row[i + u * kRowThreads] = v[u];
+      }
+      add(v, kUnroll, skip);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUnroll - 1; ++u)
+        if (i + u * kRowThreads < n_vec) v[u] = row_vec_stream(row, sp, sp.v_lo + i + u * kRowThreads);
+#pragma unroll
+      for (int u = 0; u < kUnroll - 1; ++u) {
+        if (i + u * kRowThreads < n_vec) {
+          if (kGrad) s_row[i + u * kRowThreads] = v[u];
+          if (!(skip >> u & 1u)) add(v + u, 1, 0);
+        }
+      }
+    }
+  }
+  {
     float s0, s1;
     f2_unpack(s2, s0, s1);
     st.s = s0 + s1;
+  }
+  __syncthreads();
+  // ---- the vectors left out: the first entry that lies in one takes it
+  if (vec >= 0 && (atomicAnd(&s_mark[m_byte >> 2], ~m_bit) & m_bit)) {
+    const uint4 v = row_vec_stream(row, sp, sp.v_lo + vec);
+    const int e0 = sp.head + (sp.v_lo + vec) * V16::kN;
+    unsigned int listed = 0;
+    for (int j = 0; j < p.k; ++j) {
+      const int e = s_ids[j] - e0;
+      if (e >= 0 && e < V16::kN) listed |= 1u << e;
+    }
+#pragma unroll
+    for (int q = 0; q < V16::kN / 2; ++q) {
+      float x0, x1;
+      f2_unpack(V16::pair(v, q), x0, x1);
+      if (!(listed >> (2 * q) & 1u)) single(x0);
+      if (!(listed >> (2 * q + 1) & 1u)) single(x1);
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
@@ -238,17 +262,18 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
   if (lane == 0) s_warp[warp] = st;
   __syncthreads();
   if (C > 1) {
-    if (tid == 0) {
-      MaxSum x = s_warp[0];
-      for (int r = 1; r < kRowWarps; ++r) x = join(x, s_warp[r], c);
-      s_cta = x;
+    if (warp == 0) {
+      MaxSum x = lane < kRowWarps ? s_warp[lane] : MaxSum{-FLT_MAX, 0.f};
+#pragma unroll
+      for (int o = kRowWarps / 2; o > 0; o >>= 1)
+        x = join(x, MaxSum{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o)}, c);
+      if (lane == 0) s_cta = x;
+      __syncwarp();
     }
-    __syncthreads();
     cluster_arrive();
     cluster_wait();
   }
   // ---- the row's scalars (first warp of every CTA, the same arithmetic in the same order)
-  float coef_listed = 0.f;    // beta q_j = coef_listed * e^{(z_j - z_ref) / T}
   if (warp == 0) {
     MaxSum x{-FLT_MAX, 0.f};
     if (C > 1) {
@@ -259,42 +284,73 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
     } else if (lane < kRowWarps) {
       x = s_warp[lane];
     }
+    // the list's parts (the first CTA has them)
+    double mass = 0.0, p_log_p = 0.0, p_u = 0.0, sum_e = 0.0;
+    float z_ref = -FLT_MAX;
+    if (lane < kListWarps && lane * 32 < p.k) {
+      if (C > 1) {
+        const uint32_t a = cluster_addr(&s_list[lane], 0);
+        mass = cluster_load_f64(a);
+        p_log_p = cluster_load_f64(a + 8);
+        p_u = cluster_load_f64(a + 16);
+        sum_e = cluster_load_f64(a + 24);
+        z_ref = cluster_load_f32(a + 32);
+      } else {
+        const ListPart l = s_list[lane];
+        mass = l.mass; p_log_p = l.p_log_p; p_u = l.p_u; sum_e = l.sum_e; z_ref = l.z_ref;
+      }
+    }
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1)
       x = join(x, MaxSum{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o)}, c);
     x.m = __shfl_sync(0xffffffffu, x.m, 0);
     x.s = __shfl_sync(0xffffffffu, x.s, 0);
     const double T64 = (double)p.T;
-    const float M = fmaxf(x.m, z_ref);
-    const double du_rest = ((double)x.m - (double)M) / T64, du_list = ((double)z_ref - (double)M) / T64;
-    const float w_rest = x.s > 0.f ? expf((float)du_rest) : x.s, w_list = expf((float)du_list);
-    const double S = (double)w_rest * (double)x.s + (double)w_list * (double)sum_e;
-    const double log_S = log(S);
-    // - sum_j p_j log q_j = -( sum p_j (z_j - z_ref) / T + P (z_ref - M) / T - P log S )
-    double loss = p_log_p - (p_u + mass * (du_list - log_S));
-    double beta = mass, coef = 0.0;
-    double rest = 0.0;
-    if (p.tail) {
-      rest = 1.0 - mass;
-      if (rest < 0.0) rest = 0.0;
-      beta = mass + rest;
-      if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)x.s) - log_S));
+    const float M = fmaxf(x.m, warp_max(z_ref));
+    // list sums relative to M
+    const double du = ((double)z_ref - (double)M) / T64;
+    sum_e = sum_e > 0.0 || sum_e != sum_e ? sum_e * exp(du) : 0.0;
+    p_u += mass > 0.0 ? mass * du : 0.0;
+#pragma unroll
+    for (int o = kListWarps / 2; o > 0; o >>= 1) {
+      mass += __shfl_xor_sync(0xffffffffu, mass, o);
+      p_log_p += __shfl_xor_sync(0xffffffffu, p_log_p, o);
+      p_u += __shfl_xor_sync(0xffffffffu, p_u, o);
+      sum_e += __shfl_xor_sync(0xffffffffu, sum_e, o);
     }
-    if (x.s != 0.f) coef = beta * (double)w_rest / S - rest / (double)x.s;
-    const bool none = S == 0.0;      // nothing but -inf in the row
-    if (none) {
-      coef = 0.0;
-      loss = beta > 0.0 ? INFINITY : 0.0;
-    }
-    coef_listed = none ? 0.f : (float)(beta * (double)w_list / S);
     if (lane == 0) {
+      double norm = 1.0;
+      if (!p.tail && mass != 1.0 && mass != 0.0) {    // p' = norm p:  sum p' log p' = norm (sum p log p + mass log norm)
+        norm = 1.0 / mass;
+        p_log_p = norm * (p_log_p - mass * log(mass));
+        p_u *= norm;
+        mass = mass == mass ? 1.0 : mass;
+      }
+      const double du_rest = ((double)x.m - (double)M) / T64;
+      const double w_rest = x.s > 0.f ? exp(du_rest) : (double)x.s;
+      const double S = w_rest * (double)x.s + sum_e;
+      const double log_S = log(S);
+      double loss = p_log_p - (p_u - mass * log_S);
+      double rest = 0.0, coef = 0.0;
+      if (p.tail) {
+        rest = 1.0 - mass;
+        if (rest < 0.0) rest = 0.0;
+        if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)x.s) - log_S));
+      }
+      const double beta = mass + rest;
+      if (x.s != 0.f) coef = beta * w_rest / S - rest / (double)x.s;
+      double listed = beta / S;
+      if (S == 0.0) {                                 // nothing but -inf in the row
+        listed = coef = norm = 0.0;
+        loss = beta > 0.0 ? INFINITY : 0.0;
+      }
       s_coef = (float)(coef * (double)w / T64);
       s_ref = x.m;
+      s_max = M;
+      s_norm = norm;
+      s_beta = listed;
       if (rank == 0 && p.loss) p.loss[t] = (float)loss;
     }
-#pragma unroll
-    for (int i = 0; i < kListLanes; ++i)
-      if (none) pj[i] = 0.0;
   }
   __syncwarp();
   if (C > 1) cluster_arrive();   // this CTA is done with the others' shared memory (waited for before it ends)
@@ -323,19 +379,11 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
       }
     }
     __syncthreads();
-    // listed words: over the zeros the sweep has left in their places
-    if (warp == 0) {
-#pragma unroll
-      for (int i = 0; i < kListLanes; ++i) {
-        if (id[i] < 0) continue;
-        const int e = id[i] - sp.head - sp.v_lo * V16::kN;
-        const bool mine = id[i] < sp.head ? rank == 0 : id[i] >= tail0 ? rank == C - 1 : e >= 0 && e < n_vec * V16::kN;
-        if (mine) {
-          const double u = ((double)z[i] - (double)z_ref) / (double)p.T;
-          const double d = (double)coef_listed * (double)expf((float)u) - pj[i];
-          out[id[i]] = V16::round((float)(d * (double)w / (double)p.T));
-        }
-      }
+    // listed words: over what the sweep has left in their places
+    if (mine) {
+      const double u = ((double)z - (double)s_max) / (double)p.T;
+      const double d = (z == -INFINITY ? 0.0 : s_beta * exp(u)) - pj * s_norm;
+      out[id] = V16::round((float)(d * (double)w / (double)p.T));
     }
   }
   __syncwarp();
@@ -344,8 +392,9 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
 
 template <typename T, bool kGrad>
 cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
-  // CTAs per row: few enough bytes per CTA that four fit an SM (one loads while another computes or stores), and as
-  // many as fill the GPU when there are few rows
+  // CTAs per row: few enough bytes per CTA that four fit an SM (one loads while another computes or stores), and as many
+  // as fill the GPU when there are few rows.  (Without the gradient nothing has to fit; the same split gives the same
+  // loss, bit for bit.)
   const long long bytes = (long long)p.V * (long long)sizeof(T);
   const int slots = 4 * ctx->sm_count;
   int C = 1;
@@ -353,8 +402,9 @@ cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
          (bytes > (long long)C * DX_ROW_SLICE_BYTES ||
           ((long long)p.N * C * 2 <= slots && (long long)C * 2 * kRowThreads * 16 <= bytes)))
     C *= 2;
-  const long long n_vec = bytes / 16 + 1;
-  const size_t smem = (size_t)((n_vec + C - 1) / C + 1) * 16;
+  const long long slice = (bytes / 16 + C - 1) / C;      // vectors of a CTA, at most
+  const long long chunks = (slice + kUnroll * kRowThreads - 1) / (kUnroll * kRowThreads);
+  const size_t smem = (size_t)(chunks * kRowThreads + (kGrad ? slice * 16 : 0));
   return dx_launch_pdl(false, dx_distill_kernel<T, kGrad>, dim3((unsigned)p.N * C), dim3(kRowThreads), smem, st, C, p, C);
 }
 
@@ -367,13 +417,13 @@ cudaError_t prepare(K kernel, int smem) {
 
 }  // namespace
 
-// (2 KB of the opt-in limit stay for the kernel's static variables)
+// (of the opt-in limit 1 KB stays for the kernel's static variables, 4 KB for the marks: a byte per 64 of the row)
 size_t dx_distill_max_row_bytes(const dx_ctx* ctx) {
-  return (size_t)(ctx->smem_optin - 2048 - 64) * DX_ROW_CLUSTER_MAX;
+  return (size_t)(ctx->smem_optin - kStaticBytes - 4096) * DX_ROW_CLUSTER_MAX;
 }
 
 cudaError_t dx_distill_prepare(const dx_ctx* ctx) {
-  const int smem = ctx->smem_optin - 2048;
+  const int smem = ctx->smem_optin - kStaticBytes;
   cudaError_t e = prepare(dx_distill_kernel<float, true>, smem);
   if (e == cudaSuccess) e = prepare(dx_distill_kernel<float, false>, smem);
   if (e == cudaSuccess) e = prepare(dx_distill_kernel<__nv_bfloat16, true>, smem);
@@ -385,9 +435,9 @@ cudaError_t dx_launch_distill(dx_ctx* ctx, const void* logits, int dtype, int N,
                               const int32_t* teacher_ids, const float* teacher_logprobs, int k, int tail,
                               float temperature, const float* row_weight, float* loss, void* dlogits, long long ld_d,
                               cudaStream_t st) {
+  const double c = 1.4426950408889634 / (double)temperature;
   DistillParams p{logits, N, V, k, tail, ld, ld_d, teacher_ids, teacher_logprobs,
-                  (float)(1.4426950408889634 / (double)temperature), temperature, row_weight, loss, dlogits,
-                  ctx->dev_status};
+                  (float)c, (float)(c - (double)(float)c), temperature, row_weight, loss, dlogits, ctx->dev_status};
   if (dtype == DX_DTYPE_FP32) return dlogits ? launch<float, true>(ctx, p, st) : launch<float, false>(ctx, p, st);
   return dlogits ? launch<__nv_bfloat16, true>(ctx, p, st) : launch<__nv_bfloat16, false>(ctx, p, st);
 }

@@ -3,26 +3,30 @@
 // (Both terms of H are non-negative, nothing cancels.)  The n alternatives are the largest z, ties to the lower id.
 //
 // One pass: every logit is read from HBM once.  Threads carry (running maximum, S, sum u e^u); a chunk of four
-// 16-byte vectors shares one rescaling.  Alternatives ride along as each thread's largest logit and the vector it
-// sits in.  Of those, one warp picks a threshold that at least n and at most kFlagCap threads reach; only elements of
-// these threads can be among the n largest, so they alone are read again (from L2) against the threshold, and the few
-// elements that pass are ranked by counting.  A row of few-row calls is split over a cluster of up to 16 CTAs, whose
-// statistics and candidate lists the first CTA joins through distributed shared memory: no workspace, no atomics
-// on device memory, one launch, the same result on every run.
+// 16-byte vectors shares one rescaling.  Alternatives ride along as each thread's largest logit, one per segment of its
+// share of the row.  From the threads' maxima one warp picks a threshold that at least n and at most n + kFlagSlack
+// threads reach; only the runs (thread, segment) that reach it can hold one of the n largest, so they alone -- one or
+// two percent of the row -- are read again, and the few elements that pass are ranked by counting.  Where more threads
+// share the threshold (a row of equal or masked words), what exceeds it is taken the same way and the equal elements in
+// the order of their ids.  A row of few-row calls is split over a cluster of up to 16 CTAs, whose statistics and lists
+// the first CTA joins through distributed shared memory: no workspace, no atomics on device memory, one launch, the
+// same result on every run.
 #include "dx_rows.cuh"
 
 namespace {
 
 constexpr int kUnroll = 4;
-constexpr int kFlagCap = 64;      // threads whose elements are looked at again
-constexpr int kCandCap = 1024;    // elements that may pass the threshold before the slow path takes over
+constexpr int kSegments = 8;      // parts of a thread's share of the row that have a maximum of their own
+constexpr int kFlagSlack = 12;    // the threshold may be reached by n + this many threads
+constexpr int kRunCap = (DX_MAX_TOP + kFlagSlack) * kSegments;   // (thread, segment) runs looked at again
+constexpr int kCandCap = 768;     // elements that may pass the threshold before the slow path takes over
 
 struct LogprobParams {
   const void* logits;
   int N, V, n_top;
   long long ld;
   const int32_t* tokens;
-  float c, T;                     // log2(e) / T, T
+  float c, T, dc;                 // log2(e) / T rounded, T, what the rounding has left out (times ln 2)
   float* logprob;
   float* entropy;
   int32_t* top_ids;
@@ -67,55 +71,141 @@ template <typename T>
 __device__ __forceinline__ uint4 row_vec(const T* row, const RowSplit& sp, int v) {
   return __ldg(reinterpret_cast<const uint4*>(row + sp.head) + v);
 }
+// Which elements can be among the n largest: those of the runs listed (thread, segment), and the head / tail elements.
+template <typename T>
+struct Picker {
+  const T* row;
+  RowSplit sp;
+  int V, rank, C, n, seg_vecs;          // vectors of one thread in one segment
+  unsigned long long* cand;             // [kCandCap + DX_MAX_TOP]
+  int* n_cand;
+
+  __device__ __forceinline__ void offer(float z, int idx, unsigned long long floor) const {
+    const unsigned long long k = top_key(z, idx);
+    if (k >= floor) {
+      const int q = atomicAdd(n_cand, 1);
+      if (q < kCandCap) cand[q] = k;
+    }
+  }
+  // every element of the listed runs with a key of at least `floor`
+  __device__ __forceinline__ void rescan(const int* runs, int n_runs, unsigned long long floor) const {
+    using V16 = RowVec<T>;
+    for (int x = threadIdx.x; x < n_runs * seg_vecs; x += kRowThreads) {
+      const int run = runs[x / seg_vecs];
+      const int v = sp.v_lo + run % kRowThreads + (run / kRowThreads * seg_vecs + x % seg_vecs) * kRowThreads;
+      if (v < sp.v_hi) {
+        const uint4 w = row_vec(row, sp, v);
+        if (top_key(V16::largest(w), 0) >= floor) {
+#pragma unroll
+          for (int q = 0; q < V16::kN / 2; ++q) {
+            float x0, x1;
+            f2_unpack(V16::pair(w, q), x0, x1);
+            offer(x0, sp.head + v * V16::kN + 2 * q, floor);
+            offer(x1, sp.head + v * V16::kN + 2 * q + 1, floor);
+          }
+        }
+      }
+    }
+    if (rank == 0 && threadIdx.x < sp.head) offer(element(row, threadIdx.x), threadIdx.x, floor);
+    if (rank == C - 1 && threadIdx.x < sp.tail)
+      offer(element(row, V - sp.tail + threadIdx.x), V - sp.tail + threadIdx.x, floor);
+  }
+  // the first n elements, in the order of their ids, whose key has the high word `hi`; returns how many there are
+  // (at most n), their keys in out[0 .. )
+  __device__ __forceinline__ int first_equal(unsigned int hi, unsigned long long* out, int* s_scan) const {
+    using V16 = RowVec<T>;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int found = 0;
+    const int tiles = (sp.v_hi - sp.v_lo + kRowThreads - 1) / kRowThreads;
+    for (int tile = -1; tile <= tiles && found < n; ++tile) {
+      unsigned int mask = 0;
+      int first = 0;
+      if (tile == -1) {
+        first = threadIdx.x;
+        if (rank == 0 && threadIdx.x < sp.head) mask = (unsigned int)(top_key(element(row, first), 0) >> 32) == hi;
+      } else if (tile == tiles) {
+        first = V - sp.tail + threadIdx.x;
+        if (rank == C - 1 && threadIdx.x < sp.tail)
+          mask = (unsigned int)(top_key(element(row, first), 0) >> 32) == hi;
+      } else {
+        const int v = sp.v_lo + tile * kRowThreads + threadIdx.x;
+        first = sp.head + v * V16::kN;
+        if (v < sp.v_hi) {
+          const uint4 w = row_vec(row, sp, v);
+#pragma unroll
+          for (int q = 0; q < V16::kN / 2; ++q) {
+            float x0, x1;
+            f2_unpack(V16::pair(w, q), x0, x1);
+            mask |= (unsigned int)((unsigned int)(top_key(x0, 0) >> 32) == hi) << (2 * q);
+            mask |= (unsigned int)((unsigned int)(top_key(x1, 0) >> 32) == hi) << (2 * q + 1);
+          }
+        }
+      }
+      int at = __popc(mask);
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, at, o);
+        if (lane >= o) at += y;
+      }
+      if (lane == 31) s_scan[warp] = at;
+      __syncthreads();
+      int total = 0;
+      at += found - __popc(mask);
+      for (int w = 0; w < kRowWarps; ++w) {
+        at += w < warp ? s_scan[w] : 0;
+        total += s_scan[w];
+      }
+      for (; mask && at < n; mask &= mask - 1, ++at)
+        out[at] = ((unsigned long long)hi << 32) | (unsigned long long)(~(unsigned int)(first + __ffs(mask) - 1));
+      found += total;
+      __syncthreads();
+    }
+    return min(found, n);
+  }
+};
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobParams p, int C) {
   using V16 = RowVec<T>;
   __shared__ Stats s_warp[kRowWarps];
   __shared__ Stats s_cta;
-  __shared__ unsigned long long s_keys[kRowThreads];
-  __shared__ unsigned long long s_cand[kCandCap];
-  __shared__ unsigned long long s_top[DX_MAX_TOP];
-  __shared__ unsigned long long s_tau;
-  __shared__ int s_flag[kFlagCap];
-  __shared__ int s_nflag, s_ncand;
+  __shared__ float s_seg[kSegments][kRowThreads];          // largest element of each thread in each segment
+  __shared__ unsigned long long s_cand[kCandCap + DX_MAX_TOP];
+  __shared__ unsigned long long s_top[DX_MAX_TOP], s_out[DX_MAX_TOP];
+  __shared__ unsigned int s_keys[kRowThreads];
+  __shared__ unsigned int s_tau;
+  __shared__ int s_runs[kRunCap];
+  __shared__ int s_scan[kRowWarps];
+  __shared__ int s_nrun, s_ncand, s_ties;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = C > 1 ? (int)cluster_rank() : 0;
   const int t = blockIdx.x / C;
   const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
   const RowSplit sp = row_split(row, p.V, rank, C);
   const float c = p.c;
+  const int n = p.n_top;
 
   // ---- the pass over the row
   Stats st{-FLT_MAX, 0.f, 0.f};
-  float best = -INFINITY;
-  int pos = -1;                   // of `best`: vector >= 0, or -2 - element for a head / tail element
-  // the head and the tail element of this thread, if any; a thread meets its elements in the order of their ids, so that
-  // the first of several equal maxima is the one it keeps
+  // the head and the tail element of this thread, if any
   const int extra = rank == 0 && tid < sp.head ? tid : -1;
   const int extra2 = rank == C - 1 && tid < sp.tail ? p.V - sp.tail + tid : -1;
+  float best = -INFINITY;
   auto single = [&](int i) {
     if (i < 0) return;
     const float z = element(row, i);
-    if (z > best || (pos == -1 && z >= best)) { best = z; pos = -2 - i; }
+    best = fmaxf(best, z);
     if (z > st.m) rebase(st, z, c);
     const float u = max_nan(z - st.m, -FLT_MAX), x = row_ex2(u * c);
     st.s += x;
     st.a = fmaf(u, x, st.a);
   };
   single(extra);
+  single(extra2);
   unsigned long long s2 = f2_pack(st.s, 0.f), a2 = f2_pack(st.a, 0.f);
   const unsigned long long c2 = f2_pack(c, c);
-  auto chunk = [&](const uint4* v, int n, int first) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (u < n) {
-        const float vm = V16::largest(v[u]);
-        if (vm > best || (pos == -1 && vm >= best)) { best = vm; pos = first + u * kRowThreads; }
-        top = fmaxf(top, vm);
-      }
-    }
+  auto chunk = [&](const uint4* v, int n_v) {              // n_v vectors of this thread; returns their largest element
+    float top = V16::largest(v, n_v);
     if (top > st.m) {
       float s0, s1, a0, a1;
       f2_unpack(s2, s0, s1);
@@ -129,7 +219,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     const unsigned long long nm2 = f2_pack(-st.m, -st.m);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      if (u < n) {
+      if (u < n_v) {
 #pragma unroll
         for (int q = 0; q < V16::kN / 2; ++q) {
           float d0, d1, x0, x1;
@@ -143,24 +233,33 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
         }
       }
     }
+    return top;
   };
+  const int n_vec = sp.v_hi - sp.v_lo;
+  const int chunks = (n_vec + kUnroll * kRowThreads - 1) / (kUnroll * kRowThreads);
+  const int seg_chunks = max(1, (chunks + kSegments - 1) / kSegments);
   int i = sp.v_lo + tid;
-  uint4 v[kUnroll];
-  for (; i + (kUnroll - 1) * kRowThreads < sp.v_hi; i += kUnroll * kRowThreads) {
+  for (int g = 0; g < kSegments; ++g) {
+    float top = -INFINITY;
+    for (int h = 0; h < seg_chunks; ++h, i += kUnroll * kRowThreads) {
+      uint4 v[kUnroll];
+      if (i + (kUnroll - 1) * kRowThreads < sp.v_hi) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) v[u] = row_vec(row, sp, i + u * kRowThreads);
-    chunk(v, kUnroll, i);
+        for (int u = 0; u < kUnroll; ++u) v[u] = row_vec_stream(row, sp, i + u * kRowThreads);
+        top = fmaxf(top, chunk(v, kUnroll));
+      } else if (i < sp.v_hi) {
+#pragma unroll
+        for (int u = 0; u < kUnroll - 1; ++u)
+          if (i + u * kRowThreads < sp.v_hi) v[u] = row_vec_stream(row, sp, i + u * kRowThreads);
+#pragma unroll
+        for (int u = 0; u < kUnroll - 1; ++u)
+          if (i + u * kRowThreads < sp.v_hi) top = fmaxf(top, chunk(v + u, 1));
+      }
+    }
+    if (n > 0) s_seg[g][tid] = top;
+    best = fmaxf(best, top);
+    if ((g + 1) * seg_chunks >= chunks) break;
   }
-  int left = 0;
-#pragma unroll
-  for (int u = 0; u < kUnroll - 1; ++u) {
-    const bool in = i + u * kRowThreads < sp.v_hi;
-    v[u] = in ? row_vec(row, sp, i + u * kRowThreads) : make_uint4(0, 0, 0, 0);
-    left += in ? 1 : 0;
-  }
-#pragma unroll
-  for (int u = 0; u < kUnroll - 1; ++u)
-    if (u < left) chunk(v + u, 1, i + u * kRowThreads);
   {
     float s0, s1, a0, a1;
     f2_unpack(s2, s0, s1);
@@ -168,7 +267,6 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     st.s = s0 + s1;
     st.a = a0 + a1;
   }
-  single(extra2);
   // ---- statistics of the CTA
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -180,103 +278,79 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
   }
   if (lane == 0) s_warp[warp] = st;
   // ---- the CTA's n largest elements
-  const int n = p.n_top;
   if (n > 0) {
-    unsigned long long key = 0;
-    if (pos >= 0) {
-      const uint4 w = row_vec(row, sp, pos);
-      float x[V16::kN];
-#pragma unroll
-      for (int q = 0; q < V16::kN / 2; ++q) f2_unpack(V16::pair(w, q), x[2 * q], x[2 * q + 1]);
-      int j = 0;
-#pragma unroll
-      for (int q = V16::kN - 1; q >= 0; --q) j = x[q] == best ? q : j;
-      key = top_key(best, sp.head + pos * V16::kN + j);
-    } else if (pos <= -2) {
-      key = top_key(best, -2 - pos);
-    } else {   // nothing but NaN, or no element at all
-      const int first = extra >= 0 ? extra : (sp.v_lo + tid < sp.v_hi ? sp.head + (sp.v_lo + tid) * V16::kN : extra2);
-      if (first >= 0) key = top_key(__uint_as_float(0x7fc00000u), first);
-    }
-    s_keys[tid] = key;
+    // (best is -inf for a thread that met nothing but -inf and NaN; zero: no element at all)
+    const bool any = extra >= 0 || extra2 >= 0 || sp.v_lo + tid < sp.v_hi;
+    const unsigned int mine = any ? dx_orderable(best + 0.f) : 0u;
+    s_keys[tid] = mine;
     if (tid < n) s_top[tid] = 0;
-    if (tid == 0) s_nflag = s_ncand = 0;
+    if (tid == 0) s_nrun = s_ncand = 0;
     __syncthreads();
     if (warp == 0) {
-      unsigned long long k[kRowThreads / 32];
-      unsigned int any = 0u, all = ~0u;
+      unsigned int k[kRowThreads / 32];
+      unsigned int some = 0u, all = ~0u;
       int have = 0;
 #pragma unroll
       for (int q = 0; q < kRowThreads / 32; ++q) {
         k[q] = s_keys[lane + 32 * q];
         have += k[q] != 0;
-        any |= (unsigned int)(k[q] >> 32);
-        all &= (unsigned int)(k[q] >> 32);
+        some |= k[q];
+        all &= k[q];
       }
       have = __reduce_add_sync(0xffffffffu, have);
-      unsigned long long tau = 1;
-      if (have > kFlagCap) {
-        // the bits all high words agree on, then bit by bit the largest threshold that n keys reach, until few enough do
-        any = __reduce_or_sync(0xffffffffu, any);
+      unsigned int tau = 1;
+      int count = have;
+      const int enough = n + kFlagSlack;
+      if (have > enough) {
+        // the bits all keys agree on, then bit by bit the largest threshold that n keys reach, until few enough do
+        some = __reduce_or_sync(0xffffffffu, some);
         all = __reduce_and_sync(0xffffffffu, all);
-        const int same = __clz(any ^ all);
-        unsigned int hi = same ? any & ~(same >= 32 ? 0u : 0xffffffffu >> same) : 0u;
-        int count = kRowThreads;
-        for (int b = 31 - same; b >= 0 && count > kFlagCap; --b) {
-          const unsigned int cand = hi | (1u << b);
-          int r = 0;
-#pragma unroll
-          for (int q = 0; q < kRowThreads / 32; ++q) r += (unsigned int)(k[q] >> 32) >= cand;
-          r = __reduce_add_sync(0xffffffffu, r);
-          if (r >= n) { hi = cand; count = r; }
-        }
-        tau = (unsigned long long)hi << 32;
-        for (int b = 31; b >= 0 && count > kFlagCap; --b) {   // many equal maxima: the order of their indices
-          const unsigned long long cand = tau | (1ull << b);
+        const int same = __clz(some ^ all);
+        tau = same == 0 ? 0u : same >= 32 ? some : some & ~(0xffffffffu >> same);
+        for (int b = 31 - same; b >= 0 && count > enough; --b) {
+          const unsigned int cand = tau | (1u << b);
           int r = 0;
 #pragma unroll
           for (int q = 0; q < kRowThreads / 32; ++q) r += k[q] >= cand;
           r = __reduce_add_sync(0xffffffffu, r);
-          if (r >= n) { tau = cand; count = r; }
+          if (r >= n) {
+            tau = cand;
+            count = r;
+          }
         }
         if (tau == 0) tau = 1;
       }
-      if (lane == 0) s_tau = tau;
-    }
-    __syncthreads();
-    const unsigned long long tau = s_tau;
-    if (key >= tau) {
-      const int q = atomicAdd(&s_nflag, 1);
-      if (q < kFlagCap) s_flag[q] = tid;
-    }
-    __syncthreads();
-    auto offer = [&](float z, int idx) {
-      const unsigned long long k = top_key(z, idx);
-      if (k >= tau) {
-        const int q = atomicAdd(&s_ncand, 1);
-        if (q < kCandCap) s_cand[q] = k;
+      if (lane == 0) {
+        s_tau = tau;
+        s_ties = count > enough;      // tau is then a value that many threads share, and fewer than n exceed
       }
-    };
-    const int nflag = s_nflag;
-    for (int f = warp; f < min(nflag, kFlagCap); f += kRowWarps) {
-      const int who = s_flag[f];
-      for (int w = sp.v_lo + who + lane * kRowThreads; w < sp.v_hi; w += 32 * kRowThreads) {
-        const uint4 x = row_vec(row, sp, w);
-#pragma unroll
-        for (int q = 0; q < V16::kN / 2; ++q) {
-          float x0, x1;
-          f2_unpack(V16::pair(x, q), x0, x1);
-          offer(x0, sp.head + w * V16::kN + 2 * q);
-          offer(x1, sp.head + w * V16::kN + 2 * q + 1);
+    }
+    __syncthreads();
+    const unsigned int tau = s_tau;
+    const bool ties = s_ties != 0;
+    Picker<T> pick{row, sp, p.V, rank, C, n, seg_chunks * kUnroll, s_cand, &s_ncand};
+    // (a threshold that everything reaches takes NaN in as well)
+    const unsigned int low = ties ? tau + 1u : tau <= 0x007fffffu ? 1u : tau;
+    if (ties ? mine > tau : mine >= tau) {
+      const int segs = min(kSegments, (chunks + seg_chunks - 1) / seg_chunks);
+      for (int g = 0; g < segs; ++g) {
+        if (low == 1u || dx_orderable(s_seg[g][tid] + 0.f) >= low) {
+          const int q = atomicAdd(&s_nrun, 1);
+          if (q < kRunCap) s_runs[q] = g * kRowThreads + tid;
         }
       }
-      if (lane == 0 && rank == 0 && who < sp.head) offer(element(row, who), who);
-      if (lane == 0 && rank == C - 1 && who < sp.tail)
-        offer(element(row, p.V - sp.tail + who), p.V - sp.tail + who);
     }
     __syncthreads();
-    const int ncand = s_ncand;
-    if (ncand <= kCandCap && nflag <= kFlagCap) {
+    pick.rescan(s_runs, min(s_nrun, kRunCap), (unsigned long long)low << 32);
+    __syncthreads();
+    int ncand = s_ncand;
+    if (ties && ncand <= kCandCap) {
+      ncand += pick.first_equal(tau, s_cand + ncand, s_scan);
+      // (fewer than n numbers in all: NaN follow)
+      if (tau == 0x007fffffu && ncand < n) ncand += pick.first_equal(0x007ffffeu, s_cand + ncand, s_scan);
+    }
+    if (ncand <= kCandCap + DX_MAX_TOP && s_ncand <= kCandCap && s_nrun <= kRunCap) {
+      __syncthreads();
       for (int x = tid; x < ncand; x += kRowThreads) {
         const unsigned long long k = s_cand[x];
         int r = 0;
@@ -284,7 +358,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
         if (r < n) s_top[r] = k;
       }
     } else {
-      // a few threads hold nearly all of the row's largest elements: find them one after the other
+      // a few threads hold more large elements than the list takes: find the n largest one after the other
       unsigned long long last = ~0ull;
       for (int r = 0; r < n; ++r) {
         unsigned long long k = 0;
@@ -304,15 +378,17 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
         }
         if (extra >= 0) look(element(row, extra), extra);
         if (extra2 >= 0) look(element(row, extra2), extra2);
-        s_keys[tid] = k;
-        __syncthreads();
-        for (int o = kRowThreads / 2; o > 0; o >>= 1) {
-          if (tid < o && s_keys[tid + o] > s_keys[tid]) s_keys[tid] = s_keys[tid + o];
-          __syncthreads();
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const unsigned long long y = __shfl_xor_sync(0xffffffffu, k, o);
+          k = y > k ? y : k;
         }
-        last = s_keys[0];
-        if (tid == 0) s_top[r] = last;
         __syncthreads();
+        if (lane == 0) s_cand[warp] = k;
+        __syncthreads();
+        last = s_cand[0];
+        for (int w = 1; w < kRowWarps; ++w) last = s_cand[w] > last ? s_cand[w] : last;
+        if (tid == 0) s_top[r] = last;
         if (last == 0) break;
       }
     }
@@ -324,39 +400,63 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     s_cta = x;
   }
   // ---- the first CTA of the row joins and writes
+  Stats x{0.f, 0.f, 0.f};
   if (C > 1) {
+    if (tid == 0) s_ncand = 0;
     __syncthreads();
     cluster_arrive();
     cluster_wait();
     if (rank == 0) {
-      if (tid == 0) {
-        Stats x = s_cta;
-        for (int r = 1; r < C; ++r) {
-          const uint32_t a = cluster_addr(&s_cta, r);
-          x = join(x, Stats{cluster_load_f32(a), cluster_load_f32(a + 4), cluster_load_f32(a + 8)}, c);
+      if (warp == 0) {
+        x = Stats{-FLT_MAX, 0.f, 0.f};
+        unsigned long long floor = 0;      // the n-th largest of any one CTA: at least n elements reach it
+        if (lane < C) {
+          const uint32_t a = cluster_addr(&s_cta, lane);
+          x = Stats{cluster_load_f32(a), cluster_load_f32(a + 4), cluster_load_f32(a + 8)};
+          if (n > 0) floor = cluster_load_u64(cluster_addr(&s_top[n - 1], lane));
         }
-        s_warp[0] = x;   // (s_cta stays what the other CTAs might still be told it is)
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) {
+          Stats y;
+          y.m = __shfl_xor_sync(0xffffffffu, x.m, o);
+          y.s = __shfl_xor_sync(0xffffffffu, x.s, o);
+          y.a = __shfl_xor_sync(0xffffffffu, x.a, o);
+          x = join(x, y, c);
+          const unsigned long long f = __shfl_xor_sync(0xffffffffu, floor, o);
+          floor = f > floor ? f : floor;
+        }
+        if (lane == 0) {
+          s_warp[0] = x;
+          s_cand[kCandCap] = floor;
+        }
       }
-      for (int q = tid; q < C * n; q += kRowThreads)
-        s_cand[q] = cluster_load_u64(cluster_addr(&s_top[q % n], q / n));
       __syncthreads();
+      const unsigned long long floor = s_cand[kCandCap];
       for (int q = tid; q < C * n; q += kRowThreads) {
+        const unsigned long long k = cluster_load_u64(cluster_addr(&s_top[q % n], q / n));
+        if (k != 0 && k >= floor) s_cand[atomicAdd(&s_ncand, 1)] = k;
+      }
+      __syncthreads();
+      const int ncand = s_ncand;
+      for (int q = tid; q < ncand; q += kRowThreads) {
         const unsigned long long k = s_cand[q];
         int r = 0;
-        for (int y = 0; y < C * n; ++y) r += s_cand[y] > k;
-        if (k != 0 && r < n) s_keys[r] = k;
+        for (int y = 0; y < ncand; ++y) r += s_cand[y] > k;
+        if (r < n) s_out[r] = k;
       }
     }
+    __syncwarp();
     cluster_arrive();   // (this CTA has read all it wants of the others)
     cluster_wait();
     if (rank != 0) return;
   }
   __syncthreads();
-  const Stats x = C > 1 ? s_warp[0] : s_cta;
-  const unsigned long long* top = C > 1 ? s_keys : s_top;
+  x = C > 1 ? s_warp[0] : s_cta;
+  const unsigned long long* top = C > 1 ? s_out : s_top;
   // a row of nothing but -inf has no distribution: probabilities 0, entropy 0
   const bool none = x.s == 0.f;
-  const float log_s = logf(x.s);
+  // (c is log2(e) / T rounded to fp32: what the rounding takes from every exponent, to first order)
+  const float log_s = logf(fmaf(p.dc, x.a, x.s));
   if (tid == 0) {
     if (p.logprob) {
       const int tok = p.tokens[t];
@@ -401,7 +501,9 @@ cudaError_t dx_logprobs_prepare() {
 cudaError_t dx_launch_logprobs(dx_ctx* ctx, const void* logits, int dtype, int N, int V, long long ld,
                                const int32_t* tokens, float temperature, int n_top, float* logprob, float* entropy,
                                int32_t* top_ids, float* top_logprobs, cudaStream_t st) {
-  LogprobParams p{logits, N, V, n_top, ld, tokens, (float)(1.4426950408889634 / (double)temperature), temperature,
-                  logprob, entropy, top_ids, top_logprobs, ctx->dev_status};
+  const double c = 1.4426950408889634 / (double)temperature;
+  LogprobParams p{logits, N, V, n_top, ld, tokens, (float)c, temperature,
+                  (float)((c - (double)(float)c) * 0.6931471805599453), logprob, entropy, top_ids, top_logprobs,
+                  ctx->dev_status};
   return dtype == DX_DTYPE_FP32 ? launch<float>(ctx, p, st) : launch<__nv_bfloat16>(ctx, p, st);
 }

@@ -63,6 +63,13 @@ struct RowVec<float> {
   static __device__ __forceinline__ float largest(const uint4& v) {
     return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
+  static __device__ __forceinline__ float largest(const uint4* v, int n) {   // (n is known after inlining)
+    float m = largest(v[0]);
+#pragma unroll
+    for (int u = 1; u < 4; ++u)
+      if (u < n) m = fmaxf(m, largest(v[u]));
+    return m;
+  }
   static __device__ __forceinline__ float load(const float* p) { return *p; }
   static __device__ __forceinline__ float round(float x) { return x; }
   static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
@@ -80,14 +87,22 @@ struct RowVec<__nv_bfloat16> {
     const uint32_t w = word(v, i);
     return f2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
-  static __device__ __forceinline__ float largest(const uint4& v) {
-    __nv_bfloat162 a, b, c, d;
-    *reinterpret_cast<uint32_t*>(&a) = v.x;
-    *reinterpret_cast<uint32_t*>(&b) = v.y;
-    *reinterpret_cast<uint32_t*>(&c) = v.z;
-    *reinterpret_cast<uint32_t*>(&d) = v.w;
-    const __nv_bfloat162 m = __hmax2(__hmax2(a, b), __hmax2(c, d));
-    return fmaxf(__low2float(m), __high2float(m));
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ uint32_t largest2(const uint4& v) { return max2(max2(v.x, v.y), max2(v.z, v.w)); }
+  static __device__ __forceinline__ float larger_half(uint32_t m) {
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+  static __device__ __forceinline__ float largest(const uint4& v) { return larger_half(largest2(v)); }
+  static __device__ __forceinline__ float largest(const uint4* v, int n) {   // (n is known after inlining)
+    uint32_t m = largest2(v[0]);
+#pragma unroll
+    for (int u = 1; u < 4; ++u)
+      if (u < n) m = max2(m, largest2(v[u]));
+    return larger_half(m);
   }
   static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
   static __device__ __forceinline__ __nv_bfloat16 round(float x) { return __float2bfloat16_rn(x); }
@@ -121,6 +136,17 @@ __device__ __forceinline__ RowSplit row_split(const T* row, int V, int rank, int
   return s;
 }
 
+// vector v of the row's aligned vectors; each logit is read once, L1 is left to what is read again
+template <typename T>
+__device__ __forceinline__ uint4 row_vec_stream(const T* row, const RowSplit& sp, int v) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "l"(reinterpret_cast<const uint4*>(row + sp.head) + v)
+               : "memory");
+  return r;
+}
+
 // ---- clusters ---------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -138,6 +164,11 @@ __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
 __device__ __forceinline__ float cluster_load_f32(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ double cluster_load_f64(uint32_t addr) {
+  double v;
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
   return v;
 }
 __device__ __forceinline__ unsigned long long cluster_load_u64(uint32_t addr) {
