@@ -8,16 +8,22 @@
 //
 // The unlisted words are summed apart from the listed ones, relative to their own maximum: R never comes out of a
 // difference of nearly equal sums, and neither R nor the factor r / R can under- or overflow however far the listed
-// words stand above the rest.  The sweep leaves vectors that hold a listed word out (a bit per vector says so); a thread
-// per list entry adds what else is in them afterwards.  Per-row scalars (teacher mass, loss) are 64-bit: the loss is a
-// small difference of logarithms.
+// words stand above the rest.  A bit per vector tells the sweep which vectors hold listed words; a small hash table says
+// which of their elements, and those count as -inf.  A ninth warp does the arithmetic on the list while the other eight
+// stream the row.  The warps' sums go straight into the shared memory of all CTAs of the row, so that one cluster
+// barrier is all that stands between the sweep and the gradient.  Per-row scalars of the loss are 64-bit (it is a small
+// difference of logarithms) and are not waited for by the gradient.
 #include "dx_rows.cuh"
 
 namespace {
 
 constexpr int kUnroll = 4;
-constexpr int kStaticBytes = 1024;                // at least the kernel's static shared memory
-constexpr int kListWarps = DX_MAX_TEACHER / 32;   // thread j < k has list entry j
+constexpr int kStaticBytes = 3584;                // at least the kernel's static shared memory
+constexpr int kLists = DX_MAX_TEACHER / 32;       // list entries per lane of the list's warp
+constexpr int kHash = 2 * DX_MAX_TEACHER;
+constexpr int kMarkBytes = 3584;                  // at most a byte per thread and chunk of the longest slice
+constexpr int kThreads = kRowThreads + 32;        // eight warps that stream, one that handles the list
+constexpr int kWarps = kThreads / 32;
 
 struct DistillParams {
   const void* logits;
@@ -25,7 +31,8 @@ struct DistillParams {
   long long ld, ld_d;
   const int32_t* ids;
   const float* lp;
-  float c, c_lo, T;           // log2(e) / T in two parts, T
+  float c, c_lo;              // log2(e) / T in two parts
+  double inv_T;
   const float* weight;
   float* loss;
   void* dlogits;
@@ -50,26 +57,41 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
-// What the list entries of one warp contribute, relative to the warp's largest listed logit (unnormalised p).
-struct ListPart {
-  double mass, p_log_p, p_u, sum_e;
-  float z_ref;
-  int pad;
+// What the gradient needs to know of the list: the largest listed logit, sum_j e^{(z_j - z_ref) / T}, the teacher's mass
+// with and of the tail bucket, and what its p_j are multiplied with.
+struct ListSums {
+  float z_ref, sum_e, beta, rest, norm;
 };
 
+// vector `v` with the elements in `drop` at -inf
+template <typename T>
+__device__ __forceinline__ void mask_vector(uint4& v, unsigned int drop) {
+  uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (sizeof(T) == 4) {
+      if (drop >> q & 1u) x[q] = 0xff800000u;
+    } else {
+      if (drop >> (2 * q) & 1u) x[q] = (x[q] & 0xffff0000u) | 0xff80u;
+      if (drop >> (2 * q + 1) & 1u) x[q] = (x[q] & 0xffffu) | 0xff800000u;
+    }
+  }
+  v = make_uint4(x[0], x[1], x[2], x[3]);
+}
+
 template <typename T, bool kGrad>
-__global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParams p, int C) {
+__global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p, int C) {
   using V16 = RowVec<T>;
   extern __shared__ uint4 s_dyn[];                 // bit u of byte [chunk][thread]: vector u of that chunk holds a listed
   unsigned int* s_mark = reinterpret_cast<unsigned int*>(s_dyn);   // word; behind it (kGrad) the CTA's vectors of the row
-  __shared__ MaxSum s_warp[kRowWarps];
-  __shared__ MaxSum s_cta;
-  __shared__ ListPart s_list[kListWarps];
-  __shared__ int s_ids[DX_MAX_TEACHER];
-  __shared__ float s_coef, s_ref, s_max;
-  __shared__ double s_norm, s_beta;
+  __shared__ MaxSum s_all[DX_ROW_CLUSTER_MAX * kWarps];   // sums of all warps of all CTAs of the row
+  __shared__ ListSums s_list;
+  __shared__ int s_key[kHash];                     // vectors that hold listed words (-1: free) ...
+  __shared__ unsigned int s_drop[kHash];           // ... and which of their elements those are
   __shared__ unsigned int s_edge;                  // head (bits 0..7) and tail (8..15) elements that are listed
+  __shared__ int s_live;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool list_warp = warp == kRowWarps;
   const int rank = C > 1 ? (int)cluster_rank() : 0;
   const int t = blockIdx.x / C;
   const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
@@ -78,32 +100,80 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
   const int n_vec = sp.v_hi - sp.v_lo;
   const int chunks = (n_vec + kUnroll * kRowThreads - 1) / (kUnroll * kRowThreads);
   uint4* s_row = s_dyn + chunks * (kRowThreads / 16);
-  const bool has_head = rank == 0 && tid < sp.head, has_tail = rank == C - 1 && tid < sp.tail;
   const int tail0 = p.V - sp.tail;
   // gradient vectors can be stored as such where the output row is aligned like the input row
   const bool same_align = kGrad && ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15u) == 0;
   const float c = p.c;
   const float w = p.weight ? p.weight[t] : 1.f;
 
-  // ---- the teacher's list
-  int id = -1;
-  if (tid < p.k) {
-    id = p.ids[(size_t)t * p.k + tid];
-    if (id < -1 || id >= p.V) {
-      if (rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
-      id = -1;
-    }
+  if (C > 1) cluster_arrive();
+  // ---- marks of the listed words (list warp), while the first vectors are on their way
+  uint4 v[kUnroll];
+  int id[kLists];                                  // list warp: entry lane + 32 i
+  for (int i = tid; i < chunks * (kRowThreads / 4); i += kThreads) s_mark[i] = 0;
+  for (int i = tid; i < kHash; i += kThreads) {
+    s_key[i] = -1;
+    s_drop[i] = 0;
   }
-  for (int i = tid; i < chunks * (kRowThreads / 4); i += kRowThreads) s_mark[i] = 0;
-  if (tid < DX_MAX_TEACHER) s_ids[tid] = id;
   if (tid == 0) s_edge = 0;
-  const int live = __syncthreads_or(id >= 0);
-  if (w == 0.f || !live) {   // (the same for every CTA of the row) nothing to learn: the logits are not looked at
+  if (list_warp) {
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) id[i] = lane + 32 * i < p.k ? p.ids[(size_t)t * p.k + lane + 32 * i] : -1;
+  } else if (tid + (kUnroll - 1) * kRowThreads < n_vec) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = row_vec_stream(row, sp, sp.v_lo + tid + u * kRowThreads);
+  }
+  __syncthreads();
+  if (list_warp) {
+    bool live = false, bad = false;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+      if (32 * i >= p.k) continue;
+      bad |= id[i] < -1 || id[i] >= p.V;
+      if (id[i] < 0 || id[i] >= p.V) id[i] = -1;
+      live |= id[i] >= 0;
+      // an id counts once, with its first entry: the first of equal lanes, and not if an earlier 32 have left its bit
+      const unsigned int same = __match_any_sync(0xffffffffu, id[i]);
+      if (__ffs(same) - 1 != lane) id[i] = -1;
+      if (id[i] >= 0) {
+        unsigned int bit, old;
+        if (id[i] < sp.head) {
+          bit = 1u << id[i];
+          old = atomicOr(&s_edge, bit);
+        } else if (id[i] >= tail0) {
+          bit = 256u << (id[i] - tail0);
+          old = atomicOr(&s_edge, bit);
+        } else {
+          const int x = (id[i] - sp.head) / V16::kN;
+          int h = x & (kHash - 1);
+          for (int tries = 0; tries < kHash; ++tries) {   // (at most kHash / 2 keys: a free or equal one is found)
+            const int key = atomicCAS(&s_key[h], -1, x);
+            if (key == -1 || key == x) break;
+            h = (h + 1) & (kHash - 1);
+          }
+          bit = 1u << ((id[i] - sp.head) % V16::kN);
+          old = atomicOr(&s_drop[h], bit);
+          const int mine = x - sp.v_lo;
+          if (mine >= 0 && mine < n_vec) {
+            const int at = mine / (kUnroll * kRowThreads) * kRowThreads + mine % kRowThreads;
+            atomicOr(&s_mark[at >> 2], 1u << ((at & 3) * 8 + mine / kRowThreads % kUnroll));
+          }
+        }
+        if (old & bit) id[i] = -1;
+      }
+      __syncwarp();
+    }
+    if (bad && rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
+    live = __any_sync(0xffffffffu, live);
+    if (lane == 0) s_live = live;
+  }
+  __syncthreads();
+  if (w == 0.f || !s_live) {   // (the same for every CTA of the row) nothing to learn: the logits do not matter
     if (rank == 0 && tid == 0 && p.loss) p.loss[t] = 0.f;
     if (kGrad) {
-      if (has_head) out[tid] = V16::round(0.f);
-      if (has_tail) out[tail0 + tid] = V16::round(0.f);
-      for (int i = tid; i < n_vec; i += kRowThreads) {
+      if (rank == 0 && tid < sp.head) out[tid] = V16::round(0.f);
+      if (rank == C - 1 && tid < sp.tail) out[tail0 + tid] = V16::round(0.f);
+      for (int i = tid; i < n_vec; i += kThreads) {
         const int e = sp.head + (sp.v_lo + i) * V16::kN;
         if (same_align) {
           *reinterpret_cast<uint4*>(out + e) = make_uint4(0, 0, 0, 0);
@@ -115,279 +185,225 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_distill_kernel(DistillParam
     }
     return;
   }
-  // marks; `vec` is the slice's vector an entry lies in (-1: not this CTA's, or a head / tail element)
-  int vec = -1;
-  bool mine = false;
-  if (id >= 0) {
-    if (id < sp.head) {
-      mine = rank == 0;
-      atomicOr(&s_edge, 1u << id);
-    } else if (id >= tail0) {
-      mine = rank == C - 1;
-      atomicOr(&s_edge, 256u << (id - tail0));
-    } else {
-      const int v = (id - sp.head) / V16::kN - sp.v_lo;
-      mine = v >= 0 && v < n_vec;
-      if (mine) vec = v;
-    }
-  }
-  const int m_byte = vec / (kUnroll * kRowThreads) * kRowThreads + vec % kRowThreads;     // (of entries with vec >= 0)
-  const unsigned int m_bit = 1u << ((m_byte & 3) * 8 + vec / kRowThreads % kUnroll);
-  if (vec >= 0) atomicOr(&s_mark[m_byte >> 2], m_bit);
-  // an id counts once, with its first entry
-  if (warp * 32 < p.k) {
-    const unsigned int same = __match_any_sync(0xffffffffu, id);
-    if (__ffs(same) - 1 != lane) id = -1;
-    for (int j = 0; j < warp * 32; ++j)
-      if (s_ids[j] == id) id = -1;
-  }
-  if (id < 0) {
-    mine = false;
-    vec = -1;
-  }
-  float z = -INFINITY;
-  double pj = 0.0;
-  if (id >= 0 && (mine || rank == 0)) {
-    z = V16::load(row + id);
-    pj = exp((double)p.lp[(size_t)t * p.k + tid]);
-  }
-  if (rank == 0 && warp * 32 < p.k) {
-    const float z_ref = fmaxf(warp_max(z), -FLT_MAX);
-    const double u = ((double)z - (double)z_ref) / (double)p.T;
-    const double se = warp_sum(id >= 0 ? (double)expf((float)u) : 0.0);
-    const double mass = warp_sum(pj);
-    const bool has = pj > 0.0;                        // (a NaN entry makes the mass NaN, and with it the loss)
-    const double plp = warp_sum(has ? pj * log(pj) : 0.0), pu = warp_sum(has ? pj * u : 0.0);
-    if (lane == 0) s_list[warp] = ListPart{mass, plp, pu, se, z_ref, 0};
-  }
-  __syncthreads();
   const unsigned int edge = s_edge;
-  const bool head_listed = has_head && (edge >> tid & 1u), tail_listed = has_tail && (edge >> (8 + tid) & 1u);
-  // ---- maximum and sum of exponentials of the unlisted words
+  const bool head_in = !list_warp && rank == 0 && tid < sp.head && !(edge >> tid & 1u);      // this thread's unlisted
+  const bool tail_in = !list_warp && rank == C - 1 && tid < sp.tail && !(edge >> (8 + tid) & 1u);   // edge elements
+  float edge_head = -INFINITY, edge_tail = -INFINITY;
   MaxSum st{-FLT_MAX, 0.f};
-  const unsigned long long c2 = f2_pack(c, c), cl2 = f2_pack(p.c_lo, p.c_lo);
-  const float edge_head = has_head ? V16::load(row + tid) : -INFINITY;
-  const float edge_tail = has_tail ? V16::load(row + tail0 + tid) : -INFINITY;
-  auto single = [&](float x) {
-    if (x > st.m) {
-      st.s *= row_ex2((st.m - x) * c);
-      st.m = x;
+  const unsigned long long c2 = f2_pack(c, c);
+  float lp[kLists], e[kLists];                     // list warp: log p_j, e^{(z_j - z_ref) / T}
+  double mass = 0.0, p_log_p = 0.0, p_u = 0.0;     // ... and, in the first CTA, sums over the list
+  float z_ref = -FLT_MAX, sum_e = 0.f;
+  if (!list_warp) {
+    // ---- maximum and sum of exponentials of the unlisted words
+    const unsigned long long cl2 = f2_pack(p.c_lo, p.c_lo);
+    if (head_in) edge_head = V16::load(row + tid);
+    if (tail_in) edge_tail = V16::load(row + tail0 + tid);
+    if (head_in || tail_in) {
+      st.m = fmaxf(st.m, fmaxf(edge_head, edge_tail));
+      if (head_in) st.s += row_ex2((edge_head - st.m) * c);
+      if (tail_in) st.s += row_ex2((edge_tail - st.m) * c);
     }
-    st.s += row_ex2((x - st.m) * c);
-  };
-  if (has_head && !head_listed) single(edge_head);
-  if (has_tail && !tail_listed) single(edge_tail);
-  unsigned long long s2 = f2_pack(st.s, 0.f);
-  auto add = [&](const uint4* v, int n_v, unsigned int skip) {
-    float top;
-    if (skip == 0) {
-      top = V16::largest(v, n_v);
-    } else {
-      top = -INFINITY;
+    unsigned long long s2 = f2_pack(st.s, 0.f);
+    auto add = [&](const uint4* x, int n_v) {
+      const float top = V16::largest(x, n_v);
+      if (top > st.m) {
+        float s0, s1;
+        f2_unpack(s2, s0, s1);
+        s2 = f2_pack((s0 + s1) * row_ex2((st.m - top) * c), 0.f);
+        st.m = top;
+      }
+      const unsigned long long nm2 = f2_pack(-st.m, -st.m);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (u < n_v) {
+#pragma unroll
+          for (int q = 0; q < V16::kN / 2; ++q) {
+            // (the factor in two parts: rounded to one, it would shift the exponents of all words the same way)
+            const unsigned long long d2 = f2_add(V16::pair(x[u], q), nm2);
+            float x0, x1;
+            f2_unpack(f2_fma(d2, cl2, f2_mul(d2, c2)), x0, x1);
+            s2 = f2_add(s2, f2_pack(row_ex2(x0), row_ex2(x1)));
+          }
+        }
+      }
+    };
+    auto mask = [&](uint4& x, int vec) {             // a vector with listed words
+      int h = vec & (kHash - 1);
+      for (int tries = 0; tries < kHash && s_key[h] != vec; ++tries) h = (h + 1) & (kHash - 1);
+      mask_vector<T>(x, s_drop[h]);
+    };
+    for (int ch = 0, i = tid; ch < chunks; ++ch, i += kUnroll * kRowThreads) {
+      const unsigned int marked = reinterpret_cast<const unsigned char*>(s_mark)[ch * kRowThreads + tid];
+      const bool whole = i + (kUnroll - 1) * kRowThreads < n_vec;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u)
-        if (u < n_v && !(skip >> u & 1u)) top = fmaxf(top, V16::largest(v[u]));
-    }
-    if (top > st.m) {
-      float s0, s1;
-      f2_unpack(s2, s0, s1);
-      s2 = f2_pack((s0 + s1) * row_ex2((st.m - top) * c), 0.f);
-      st.m = top;
-    }
-    const unsigned long long nm2 = f2_pack(-st.m, -st.m);
+        if (whole ? ch > 0 : i + u * kRowThreads < n_vec) v[u] = row_vec_stream(row, sp, sp.v_lo + i + u * kRowThreads);
+      if (marked) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (u < n_v && !(skip >> u & 1u)) {
+        for (int u = 0; u < kUnroll; ++u)
+          if (marked >> u & 1u) mask(v[u], sp.v_lo + i + u * kRowThreads);
+      }
 #pragma unroll
-        for (int q = 0; q < V16::kN / 2; ++q) {
-          // (the factor in two parts: rounded to one, it would shift the exponents of all words the same way)
-          const unsigned long long d2 = f2_add(V16::pair(v[u], q), nm2);
-          float x0, x1;
-          f2_unpack(f2_fma(d2, cl2, f2_mul(d2, c2)), x0, x1);
-          s2 = f2_add(s2, f2_pack(row_ex2(x0), row_ex2(x1)));
-        }
+      for (int u = 0; u < kUnroll; ++u)
+        if (kGrad && i + u * kRowThreads < n_vec) s_row[i + u * kRowThreads] = v[u];
+      if (whole) {
+        add(v, kUnroll);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll - 1; ++u)
+          if (i + u * kRowThreads < n_vec) add(v + u, 1);
       }
     }
-  };
-  for (int ch = 0, i = tid; ch < chunks; ++ch, i += kUnroll * kRowThreads) {
-    const unsigned int skip = reinterpret_cast<const unsigned char*>(s_mark)[ch * kRowThreads + tid];
-    uint4 v[kUnroll];
-    if (i + (kUnroll - 1) * kRowThreads < n_vec) {
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) v[u] = row_vec_stream(row, sp, sp.v_lo + i + u * kRowThreads);
-      if (kGrad) {
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) s_row[i + u * kRowThreads] = v[u];
-      }
-      add(v, kUnroll, skip);
-    } else {
-#pragma unroll
-      for (int u = 0; u < kUnroll - 1; ++u)
-        if (i + u * kRowThreads < n_vec) v[u] = row_vec_stream(row, sp, sp.v_lo + i + u * kRowThreads);
-#pragma unroll
-      for (int u = 0; u < kUnroll - 1; ++u) {
-        if (i + u * kRowThreads < n_vec) {
-          if (kGrad) s_row[i + u * kRowThreads] = v[u];
-          if (!(skip >> u & 1u)) add(v + u, 1, 0);
-        }
-      }
-    }
-  }
-  {
     float s0, s1;
     f2_unpack(s2, s0, s1);
     st.s = s0 + s1;
-  }
-  __syncthreads();
-  // ---- the vectors left out: the first entry that lies in one takes it
-  if (vec >= 0 && (atomicAnd(&s_mark[m_byte >> 2], ~m_bit) & m_bit)) {
-    const uint4 v = row_vec_stream(row, sp, sp.v_lo + vec);
-    const int e0 = sp.head + (sp.v_lo + vec) * V16::kN;
-    unsigned int listed = 0;
-    for (int j = 0; j < p.k; ++j) {
-      const int e = s_ids[j] - e0;
-      if (e >= 0 && e < V16::kN) listed |= 1u << e;
-    }
+    __syncwarp();
+    if (C > 1) cluster_wait();                       // (all CTAs of the row have started)
+  } else {
+    // ---- the list (log p_j is what the caller has given)
+    float z[kLists], top = -FLT_MAX;
 #pragma unroll
-    for (int q = 0; q < V16::kN / 2; ++q) {
-      float x0, x1;
-      f2_unpack(V16::pair(v, q), x0, x1);
-      if (!(listed >> (2 * q) & 1u)) single(x0);
-      if (!(listed >> (2 * q + 1) & 1u)) single(x1);
+    for (int i = 0; i < kLists; ++i) {
+      z[i] = id[i] >= 0 ? V16::load(row + id[i]) : -INFINITY;
+      lp[i] = id[i] >= 0 ? p.lp[(size_t)t * p.k + lane + 32 * i] : -INFINITY;
+      top = fmaxf(top, z[i]);
     }
+    z_ref = warp_max(top);
+    double se = 0.0;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+      e[i] = 0.f;
+      if (32 * i >= p.k) continue;
+      const double u = ((double)z[i] - (double)z_ref) * p.inv_T;
+      e[i] = id[i] >= 0 ? expf((float)u) : 0.f;
+      if (rank == 0) {
+        const double pj = exp((double)lp[i]);        // (a NaN entry makes the mass NaN, and with it the loss)
+        se += (double)e[i];
+        mass += pj;
+        if (pj > 0.0) {
+          p_log_p += pj * (double)lp[i];
+          p_u += pj * u;
+        }
+      }
+    }
+    if (rank == 0) {
+      sum_e = (float)warp_sum(se);
+      mass = warp_sum(mass);
+      p_log_p = warp_sum(p_log_p);
+      p_u = warp_sum(p_u);
+    }
+    if (C > 1) cluster_wait();                       // (all CTAs of the row have started)
+    if (rank == 0) {
+      if (!p.tail && mass != 0.0) {                  // p' = p / mass:  sum p' log p' = (sum p log p) / mass - log mass
+        p_log_p = (p_log_p - mass * log(mass)) / mass;
+        p_u /= mass;
+      }
+      double rest = p.tail ? 1.0 - mass : 0.0;
+      if (rest < 0.0) rest = 0.0;
+      const double P = p.tail || mass == 0.0 ? mass : mass / mass;
+      if (lane < C) {
+        const ListSums l{z_ref, sum_e, (float)(P + rest), (float)rest, p.tail || mass == 0.0 ? 1.f : (float)(1.0 / mass)};
+        if (C > 1) {
+          const uint32_t a = cluster_addr(&s_list, lane);
+          cluster_store_f32(a, l.z_ref);
+          cluster_store_f32(a + 4, l.sum_e);
+          cluster_store_f32(a + 8, l.beta);
+          cluster_store_f32(a + 12, l.rest);
+          cluster_store_f32(a + 16, l.norm);
+        } else {
+          s_list = l;
+        }
+      }
+    }
+    __syncwarp();
   }
+  // ---- sums of the warp, to all CTAs of the row
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
     st = join(st, MaxSum{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o)}, c);
-  if (lane == 0) s_warp[warp] = st;
-  __syncthreads();
-  if (C > 1) {
-    if (warp == 0) {
-      MaxSum x = lane < kRowWarps ? s_warp[lane] : MaxSum{-FLT_MAX, 0.f};
-#pragma unroll
-      for (int o = kRowWarps / 2; o > 0; o >>= 1)
-        x = join(x, MaxSum{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o)}, c);
-      if (lane == 0) s_cta = x;
-      __syncwarp();
+  if (lane < C) {
+    if (C > 1) {
+      const uint32_t a = cluster_addr(&s_all[rank * kWarps + warp], lane);
+      cluster_store_f32(a, st.m);
+      cluster_store_f32(a + 4, st.s);
+    } else {
+      s_all[warp] = st;
     }
+  }
+  __syncwarp();
+  if (C > 1) {
     cluster_arrive();
     cluster_wait();
+  } else {
+    __syncthreads();
   }
-  // ---- the row's scalars (first warp of every CTA, the same arithmetic in the same order)
-  if (warp == 0) {
-    MaxSum x{-FLT_MAX, 0.f};
-    if (C > 1) {
-      if (lane < C) {
-        const uint32_t a = cluster_addr(&s_cta, lane);
-        x = MaxSum{cluster_load_f32(a), cluster_load_f32(a + 4)};
-      }
-    } else if (lane < kRowWarps) {
-      x = s_warp[lane];
-    }
-    // the list's parts (the first CTA has them)
-    double mass = 0.0, p_log_p = 0.0, p_u = 0.0, sum_e = 0.0;
-    float z_ref = -FLT_MAX;
-    if (lane < kListWarps && lane * 32 < p.k) {
-      if (C > 1) {
-        const uint32_t a = cluster_addr(&s_list[lane], 0);
-        mass = cluster_load_f64(a);
-        p_log_p = cluster_load_f64(a + 8);
-        p_u = cluster_load_f64(a + 16);
-        sum_e = cluster_load_f64(a + 24);
-        z_ref = cluster_load_f32(a + 32);
-      } else {
-        const ListPart l = s_list[lane];
-        mass = l.mass; p_log_p = l.p_log_p; p_u = l.p_u; sum_e = l.sum_e; z_ref = l.z_ref;
-      }
-    }
+  // ---- the row's scalars (every warp, the same arithmetic in the same order)
+  MaxSum x{-FLT_MAX, 0.f};
+  for (int i = lane; i < C * kWarps; i += 32) x = join(x, s_all[i], c);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1)
-      x = join(x, MaxSum{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o)}, c);
-    x.m = __shfl_sync(0xffffffffu, x.m, 0);
-    x.s = __shfl_sync(0xffffffffu, x.s, 0);
-    const double T64 = (double)p.T;
-    const float M = fmaxf(x.m, warp_max(z_ref));
-    // list sums relative to M
-    const double du = ((double)z_ref - (double)M) / T64;
-    sum_e = sum_e > 0.0 || sum_e != sum_e ? sum_e * exp(du) : 0.0;
-    p_u += mass > 0.0 ? mass * du : 0.0;
+  for (int o = 16; o > 0; o >>= 1)
+    x = join(x, MaxSum{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o)}, c);
+  const ListSums l = s_list;
+  const float M = fmaxf(x.m, l.z_ref);
+  // (fp32: the gradient's factors; a sum that is NaN stays NaN)
+  const float w_rest = x.s > 0.f ? row_ex2((x.m - M) * c) : x.s;
+  const float w_list = row_ex2((l.z_ref - M) * c);
+  const float S = w_rest * x.s + w_list * l.sum_e;
+  const float scale = w * (float)p.inv_T;
+  if (kGrad) {
+    float coef = 0.f;
+    if (x.s != 0.f && S != 0.f) coef = (l.beta * w_rest / S - l.rest / x.s) * scale;
+    if (!list_warp) {
+      if (head_in) out[tid] = V16::round(coef * row_ex2((edge_head - x.m) * c));
+      if (tail_in) out[tail0 + tid] = V16::round(coef * row_ex2((edge_tail - x.m) * c));
+      const unsigned long long nm2 = f2_pack(-x.m, -x.m), k2 = f2_pack(coef, coef);
+      T* out_vec = out + sp.head + (long long)sp.v_lo * V16::kN;
+#pragma unroll 2
+      for (int i = tid; i < n_vec; i += kRowThreads) {
+        const uint4 y = s_row[i];
+        float g[V16::kN];
 #pragma unroll
-    for (int o = kListWarps / 2; o > 0; o >>= 1) {
-      mass += __shfl_xor_sync(0xffffffffu, mass, o);
-      p_log_p += __shfl_xor_sync(0xffffffffu, p_log_p, o);
-      p_u += __shfl_xor_sync(0xffffffffu, p_u, o);
-      sum_e += __shfl_xor_sync(0xffffffffu, sum_e, o);
-    }
-    if (lane == 0) {
-      double norm = 1.0;
-      if (!p.tail && mass != 1.0 && mass != 0.0) {    // p' = norm p:  sum p' log p' = norm (sum p log p + mass log norm)
-        norm = 1.0 / mass;
-        p_log_p = norm * (p_log_p - mass * log(mass));
-        p_u *= norm;
-        mass = mass == mass ? 1.0 : mass;
+        for (int q = 0; q < V16::kN / 2; ++q) {
+          float x0, x1;
+          f2_unpack(f2_mul(f2_add(V16::pair(y, q), nm2), c2), x0, x1);
+          f2_unpack(f2_mul(f2_pack(row_ex2(x0), row_ex2(x1)), k2), g[2 * q], g[2 * q + 1]);
+        }
+        if (same_align) {
+          *reinterpret_cast<uint4*>(out_vec + (long long)i * V16::kN) = V16::pack(g);
+        } else {
+#pragma unroll
+          for (int q = 0; q < V16::kN; ++q) out_vec[(long long)i * V16::kN + q] = V16::round(g[q]);
+        }
       }
-      const double du_rest = ((double)x.m - (double)M) / T64;
-      const double w_rest = x.s > 0.f ? exp(du_rest) : (double)x.s;
-      const double S = w_rest * (double)x.s + sum_e;
-      const double log_S = log(S);
-      double loss = p_log_p - (p_u - mass * log_S);
-      double rest = 0.0, coef = 0.0;
-      if (p.tail) {
-        rest = 1.0 - mass;
-        if (rest < 0.0) rest = 0.0;
-        if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)x.s) - log_S));
-      }
-      const double beta = mass + rest;
-      if (x.s != 0.f) coef = beta * w_rest / S - rest / (double)x.s;
-      double listed = beta / S;
-      if (S == 0.0) {                                 // nothing but -inf in the row
-        listed = coef = norm = 0.0;
-        loss = beta > 0.0 ? INFINITY : 0.0;
-      }
-      s_coef = (float)(coef * (double)w / T64);
-      s_ref = x.m;
-      s_max = M;
-      s_norm = norm;
-      s_beta = listed;
-      if (rank == 0 && p.loss) p.loss[t] = (float)loss;
     }
   }
-  __syncwarp();
-  if (C > 1) cluster_arrive();   // this CTA is done with the others' shared memory (waited for before it ends)
+  if (list_warp && rank == 0 && p.loss) {
+    const double du_rest = ((double)x.m - (double)M) * p.inv_T, du_list = ((double)l.z_ref - (double)M) * p.inv_T;
+    const double S64 = (x.s > 0.f ? exp(du_rest) : 1.0) * (double)x.s + exp(du_list) * (double)l.sum_e;
+    const double log_S = log(S64);
+    double rest = p.tail ? 1.0 - mass : 0.0;
+    if (rest < 0.0) rest = 0.0;
+    const double P = p.tail || mass == 0.0 ? mass : mass / mass;
+    // - sum_j p_j log q_j = -( sum p_j (z_j - z_ref) / T + P (z_ref - M) / T - P log S )
+    double loss = p_log_p - (p_u + (P != 0.0 ? P * (du_list - log_S) : 0.0));
+    if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)x.s) - log_S));
+    if (S64 == 0.0) loss = P + rest > 0.0 ? INFINITY : 0.0;      // nothing but -inf in the row
+    if (lane == 0) p.loss[t] = (float)loss;
+  }
   if (kGrad) {
     __syncthreads();
-    const float coef = s_coef, ref = s_ref;
-    if (has_head && !head_listed) out[tid] = V16::round(coef * row_ex2((edge_head - ref) * c));
-    if (has_tail && !tail_listed) out[tail0 + tid] = V16::round(coef * row_ex2((edge_tail - ref) * c));
-    const unsigned long long nm2 = f2_pack(-ref, -ref), k2 = f2_pack(coef, coef);
-    T* out_vec = out + sp.head + (long long)sp.v_lo * V16::kN;
-#pragma unroll 2
-    for (int i = tid; i < n_vec; i += kRowThreads) {
-      const uint4 v = s_row[i];
-      float g[V16::kN];
-#pragma unroll
-      for (int q = 0; q < V16::kN / 2; ++q) {
-        float x0, x1;
-        f2_unpack(f2_mul(f2_add(V16::pair(v, q), nm2), c2), x0, x1);
-        f2_unpack(f2_mul(f2_pack(row_ex2(x0), row_ex2(x1)), k2), g[2 * q], g[2 * q + 1]);
-      }
-      if (same_align) {
-        *reinterpret_cast<uint4*>(out_vec + (long long)i * V16::kN) = V16::pack(g);
-      } else {
-#pragma unroll
-        for (int q = 0; q < V16::kN; ++q) out_vec[(long long)i * V16::kN + q] = V16::round(g[q]);
-      }
-    }
-    __syncthreads();
     // listed words: over what the sweep has left in their places
-    if (mine) {
-      const double u = ((double)z - (double)s_max) / (double)p.T;
-      const double d = (z == -INFINITY ? 0.0 : s_beta * exp(u)) - pj * s_norm;
-      out[id] = V16::round((float)(d * (double)w / (double)p.T));
+    if (list_warp) {
+      const float f = S == 0.f ? 0.f : l.beta * w_list / S;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) {
+        const int v_at = (id[i] - sp.head) / V16::kN - sp.v_lo;
+        const bool mine = id[i] >= 0 && (id[i] < sp.head ? rank == 0 : id[i] >= tail0 ? rank == C - 1 : v_at >= 0 && v_at < n_vec);
+        if (mine) out[id[i]] = V16::round(S == 0.f ? 0.f : (f * e[i] - expf(lp[i]) * l.norm) * scale);
+      }
     }
   }
-  __syncwarp();
-  if (C > 1) cluster_wait();
 }
 
 template <typename T, bool kGrad>
@@ -405,7 +421,7 @@ cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
   const long long slice = (bytes / 16 + C - 1) / C;      // vectors of a CTA, at most
   const long long chunks = (slice + kUnroll * kRowThreads - 1) / (kUnroll * kRowThreads);
   const size_t smem = (size_t)(chunks * kRowThreads + (kGrad ? slice * 16 : 0));
-  return dx_launch_pdl(false, dx_distill_kernel<T, kGrad>, dim3((unsigned)p.N * C), dim3(kRowThreads), smem, st, C, p, C);
+  return dx_launch_pdl(false, dx_distill_kernel<T, kGrad>, dim3((unsigned)p.N * C), dim3(kThreads), smem, st, C, p, C);
 }
 
 template <typename K>
@@ -417,9 +433,8 @@ cudaError_t prepare(K kernel, int smem) {
 
 }  // namespace
 
-// (of the opt-in limit 1 KB stays for the kernel's static variables, 4 KB for the marks: a byte per 64 of the row)
 size_t dx_distill_max_row_bytes(const dx_ctx* ctx) {
-  return (size_t)(ctx->smem_optin - kStaticBytes - 4096) * DX_ROW_CLUSTER_MAX;
+  return (size_t)(ctx->smem_optin - kStaticBytes - kMarkBytes) * DX_ROW_CLUSTER_MAX;
 }
 
 cudaError_t dx_distill_prepare(const dx_ctx* ctx) {
@@ -437,7 +452,7 @@ cudaError_t dx_launch_distill(dx_ctx* ctx, const void* logits, int dtype, int N,
                               cudaStream_t st) {
   const double c = 1.4426950408889634 / (double)temperature;
   DistillParams p{logits, N, V, k, tail, ld, ld_d, teacher_ids, teacher_logprobs,
-                  (float)c, (float)(c - (double)(float)c), temperature, row_weight, loss, dlogits, ctx->dev_status};
+                  (float)c, (float)(c - (double)(float)c), 1.0 / (double)temperature, row_weight, loss, dlogits, ctx->dev_status};
   if (dtype == DX_DTYPE_FP32) return dlogits ? launch<float, true>(ctx, p, st) : launch<float, false>(ctx, p, st);
   return dlogits ? launch<__nv_bfloat16, true>(ctx, p, st) : launch<__nv_bfloat16, false>(ctx, p, st);
 }
