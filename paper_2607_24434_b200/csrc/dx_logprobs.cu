@@ -2,8 +2,8 @@
 //   u_v = (z_v - max z) / T,  S = sum_v e^{u_v},  log p_v = u_v - log S,  H = log S - (sum_v u_v e^{u_v}) / S.
 // (Both terms of H are non-negative, nothing cancels.)  The n alternatives are the largest z, ties to the lower id.
 //
-// One pass: every logit is read from HBM once.  Threads carry (running maximum, S, sum u e^u); a chunk of four
-// 16-byte vectors shares one rescaling.  Alternatives ride along as each thread's largest logit, one per segment of its
+// One pass: every logit is read from HBM once.  Threads carry (a reference near the maximum, S, sum u e^u)
+// relative to it, four 16-byte vectors at a time.  Alternatives ride along as each thread's largest logit, one per segment of its
 // share of the row.  From the threads' maxima one warp picks a threshold that at least n and at most n + kFlagSlack
 // threads reach; only the runs (thread, segment) that reach it can hold one of the n largest, so they alone -- one or
 // two percent of the row -- are read again, and the few elements that pass are ranked by counting.  Where more threads
@@ -16,6 +16,7 @@
 namespace {
 
 constexpr int kUnroll = 4;
+constexpr float kSlack = 8.f;      // powers of two by which an element may exceed the reference of its thread's sums
 constexpr int kSegments = 8;      // parts of a thread's share of the row that have a maximum of their own
 constexpr int kFlagSlack = 12;    // the threshold may be reached by n + this many threads
 constexpr int kRunCap = (DX_MAX_TOP + kFlagSlack) * kSegments;   // (thread, segment) runs looked at again
@@ -47,7 +48,7 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
 }
 
 struct Stats {
-  float m, s, a;   // maximum, sum of e^u, sum of (z - m) e^u
+  float m, s, a;   // reference, sum of e^{(z - m) / T}, sum of (z - m) e^{(z - m) / T}
 };
 // brings the sums to another reference maximum m >= st.m (NaN sums stay NaN).  Where the factor vanishes so does the
 // old sum: the distance may then be as large as that of a mask of the type's lowest value, and is not multiplied out.
@@ -62,6 +63,17 @@ __device__ __forceinline__ Stats join(Stats x, Stats y, float c) {
   rebase(x, m, c);
   rebase(y, m, c);
   return Stats{m, x.s + y.s, x.a + y.a};
+}
+
+// the sums of a warp's lanes, relative to their largest reference; every lane gets them
+__device__ __forceinline__ Stats warp_join(Stats x, float c) {
+  rebase(x, warp_max(x.m), c);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
+    x.a += __shfl_xor_sync(0xffffffffu, x.a, o);
+  }
+  return x;
 }
 
 template <typename T>
@@ -187,31 +199,38 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
 
   // ---- the pass over the row
   Stats st{-FLT_MAX, 0.f, 0.f};
-  // the head and the tail element of this thread, if any
-  const int extra = rank == 0 && tid < sp.head ? tid : -1;
-  const int extra2 = rank == C - 1 && tid < sp.tail ? p.V - sp.tail + tid : -1;
   float best = -INFINITY;
-  auto single = [&](int i) {
-    if (i < 0) return;
-    const float z = element(row, i);
-    best = fmaxf(best, z);
-    if (z > st.m) rebase(st, z, c);
-    const float u = max_nan(z - st.m, -FLT_MAX), x = row_ex2(u * c);
-    st.s += x;
-    st.a = fmaf(u, x, st.a);
-  };
-  single(extra);
-  single(extra2);
-  unsigned long long s2 = f2_pack(st.s, 0.f), a2 = f2_pack(st.a, 0.f);
+  // All warps start from the largest element of their first chunk as the reference of the exponents; a thread takes
+  // another only when it meets an element more than 2^kSlack times as likely (the sums stay far from fp32's limits, and
+  // what they lose is a few bits of the entropy's last place).
+  unsigned long long s2 = 0ull, a2 = 0ull;
   const unsigned long long c2 = f2_pack(c, c);
-  auto chunk = [&](const uint4* v, int n_v) {              // n_v vectors of this thread; returns their largest element
-    float top = V16::largest(v, n_v);
-    if (top > st.m) {
-      float s0, s1, a0, a1;
-      f2_unpack(s2, s0, s1);
-      f2_unpack(a2, a0, a1);
-      st.s = s0 + s1;
-      st.a = a0 + a1;
+  auto take = [&]() {
+    float s0, s1, a0, a1;
+    f2_unpack(s2, s0, s1);
+    f2_unpack(a2, a0, a1);
+    st.s = s0 + s1;
+    st.a = a0 + a1;
+  };
+  const int n_vec = sp.v_hi - sp.v_lo;
+  const int chunks = (n_vec + kUnroll * kRowThreads - 1) / (kUnroll * kRowThreads);
+  const int seg_chunks = max(1, (chunks + kSegments - 1) / kSegments);
+  const uint4 none4 = make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
+  float seg = -INFINITY;
+  int g = 0, in_seg = 0;
+#pragma unroll 1
+  for (int ch = 0, i = sp.v_lo + tid; ch < chunks; ++ch, i += kUnroll * kRowThreads) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      v[u] = none4;                                        // (adds nothing to any sum)
+      if (i + u * kRowThreads < sp.v_hi) v[u] = row_vec_stream(row, sp, i + u * kRowThreads);
+    }
+    const float top = V16::largest(v, kUnroll);
+    if (ch == 0) {
+      st.m = fmaxf(warp_max(top), -FLT_MAX);
+    } else if ((top - st.m) * c > kSlack) {
+      take();
       rebase(st, top, c);
       s2 = f2_pack(st.s, 0.f);
       a2 = f2_pack(st.a, 0.f);
@@ -219,63 +238,47 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     const unsigned long long nm2 = f2_pack(-st.m, -st.m);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      if (u < n_v) {
 #pragma unroll
-        for (int q = 0; q < V16::kN / 2; ++q) {
-          float d0, d1, x0, x1;
-          f2_unpack(f2_add(V16::pair(v[u], q), nm2), d0, d1);
-          // (a masked logit of -inf: the difference stays finite so that its product with e^u = 0 is 0)
-          const unsigned long long d2 = f2_pack(max_nan(d0, -FLT_MAX), max_nan(d1, -FLT_MAX));
-          f2_unpack(f2_mul(d2, c2), x0, x1);
-          const unsigned long long e2 = f2_pack(row_ex2(x0), row_ex2(x1));
-          s2 = f2_add(s2, e2);
-          a2 = f2_fma(d2, e2, a2);
-        }
+      for (int q = 0; q < V16::kN / 2; ++q) {
+        float d0, d1, x0, x1;
+        f2_unpack(f2_add(V16::pair(v[u], q), nm2), d0, d1);
+        // (a masked logit of -inf: the difference stays finite so that its product with e^u = 0 is 0)
+        const unsigned long long d2 = f2_pack(max_nan(d0, -FLT_MAX), max_nan(d1, -FLT_MAX));
+        f2_unpack(f2_mul(d2, c2), x0, x1);
+        const unsigned long long e2 = f2_pack(row_ex2(x0), row_ex2(x1));
+        s2 = f2_add(s2, e2);
+        a2 = f2_fma(d2, e2, a2);
       }
     }
-    return top;
-  };
-  const int n_vec = sp.v_hi - sp.v_lo;
-  const int chunks = (n_vec + kUnroll * kRowThreads - 1) / (kUnroll * kRowThreads);
-  const int seg_chunks = max(1, (chunks + kSegments - 1) / kSegments);
-  int i = sp.v_lo + tid;
-  for (int g = 0; g < kSegments; ++g) {
-    float top = -INFINITY;
-    for (int h = 0; h < seg_chunks; ++h, i += kUnroll * kRowThreads) {
-      uint4 v[kUnroll];
-      if (i + (kUnroll - 1) * kRowThreads < sp.v_hi) {
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) v[u] = row_vec_stream(row, sp, i + u * kRowThreads);
-        top = fmaxf(top, chunk(v, kUnroll));
-      } else if (i < sp.v_hi) {
-#pragma unroll
-        for (int u = 0; u < kUnroll - 1; ++u)
-          if (i + u * kRowThreads < sp.v_hi) v[u] = row_vec_stream(row, sp, i + u * kRowThreads);
-#pragma unroll
-        for (int u = 0; u < kUnroll - 1; ++u)
-          if (i + u * kRowThreads < sp.v_hi) top = fmaxf(top, chunk(v + u, 1));
-      }
+    seg = fmaxf(seg, top);
+    if (++in_seg == seg_chunks) {
+      s_seg[g++][tid] = seg;
+      best = fmaxf(best, seg);
+      seg = -INFINITY;
+      in_seg = 0;
     }
-    if (n > 0) s_seg[g][tid] = top;
-    best = fmaxf(best, top);
-    if ((g + 1) * seg_chunks >= chunks) break;
   }
-  {
-    float s0, s1, a0, a1;
-    f2_unpack(s2, s0, s1);
-    f2_unpack(a2, a0, a1);
-    st.s = s0 + s1;
-    st.a = a0 + a1;
+  if (in_seg > 0) {
+    s_seg[g][tid] = seg;
+    best = fmaxf(best, seg);
+  }
+  take();
+  // the head and the tail element of this thread, if any
+  const int extra = rank == 0 && tid < sp.head ? tid : -1;
+  const int extra2 = rank == C - 1 && tid < sp.tail ? p.V - sp.tail + tid : -1;
+#pragma unroll 1
+  for (int e = 0; e < 2; ++e) {
+    const int i = e ? extra2 : extra;
+    if (i < 0) continue;
+    const float z = element(row, i);
+    best = fmaxf(best, z);
+    if (z > st.m) rebase(st, z, c);
+    const float u = max_nan(z - st.m, -FLT_MAX), x = row_ex2(u * c);
+    st.s += x;
+    st.a = fmaf(u, x, st.a);
   }
   // ---- statistics of the CTA
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Stats y;
-    y.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-    y.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-    y.a = __shfl_xor_sync(0xffffffffu, st.a, o);
-    st = join(st, y, c);
-  }
+  st = warp_join(st, c);
   if (lane == 0) s_warp[warp] = st;
   // ---- the CTA's n largest elements
   if (n > 0) {
@@ -415,13 +418,9 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
           x = Stats{cluster_load_f32(a), cluster_load_f32(a + 4), cluster_load_f32(a + 8)};
           if (n > 0) floor = cluster_load_u64(cluster_addr(&s_top[n - 1], lane));
         }
+        x = warp_join(x, c);
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) {
-          Stats y;
-          y.m = __shfl_xor_sync(0xffffffffu, x.m, o);
-          y.s = __shfl_xor_sync(0xffffffffu, x.s, o);
-          y.a = __shfl_xor_sync(0xffffffffu, x.a, o);
-          x = join(x, y, c);
           const unsigned long long f = __shfl_xor_sync(0xffffffffu, floor, o);
           floor = f > floor ? f : floor;
         }

@@ -23,6 +23,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on eithe
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
 // Two fp32 values in one 64-bit register: Blackwell adds, multiplies and multiply-adds both in one instruction.
 __device__ __forceinline__ unsigned long long f2_pack(float lo, float hi) {
   unsigned long long r;
