@@ -19,20 +19,20 @@ namespace {
 
 constexpr int kUnroll = 2;
 constexpr float kSlack = 8.f;                     // powers of two by which an element may exceed its sum's reference
-constexpr int kStaticBytes = 5632;                // at least the kernel's static shared memory
+constexpr int kStaticBytes = 4608;                // at least the kernel's static shared memory
 constexpr int kLists = DX_MAX_TEACHER / 32;       // list entries per lane of the list's warp
 constexpr int kHash = 2 * DX_MAX_TEACHER;
 constexpr int kThreads = kRowThreads + 32;        // eight warps that stream, one that handles the list
-constexpr int kWarps = kThreads / 32;
 
 struct DistillParams {
   const void* logits;
-  int N, V, k, tail;
+  int N, V, k, tail, half;    // half: 16-bit words of marks per thread
   long long ld, ld_d;
   const int32_t* ids;
   const float* lp;
   float c, c_lo;              // log2(e) / T in two parts
   double inv_T;
+  float inv_Tf;
   const float* weight;
   float* loss;
   void* dlogits;
@@ -86,335 +86,462 @@ __device__ __forceinline__ MaxSum warp_join(MaxSum x, float c) {
   return MaxSum{m, s};
 }
 
+// Barrier of all nine warps (the two roles meet it at different places of the program).
+__device__ __forceinline__ void cta_barrier() { asm volatile("bar.sync 0, %0;" ::"n"(kThreads) : "memory"); }
+
+// The sums of a row, from all warps of its CTAs and from the list.
+struct RowSums {
+  MaxSum rest;                // unlisted words
+  ListSums l;
+  float M;                    // the larger of the two references
+  float w_rest, w_list, S;    // factors that bring the two sums to M; the whole sum relative to it
+};
+__device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l, int n, float c) {
+  RowSums r;
+  const int lane = threadIdx.x & 31;
+  MaxSum x = lane < n ? all[lane] : MaxSum{-FLT_MAX, 0.f};
+  for (int i = lane + 32; i < n; i += 32) x = join(x, all[i], c);
+  r.rest = warp_join(x, c);
+  r.l = l;
+  r.M = fmaxf(r.rest.m, l.z_ref);
+  // (fp32: the gradient's factors; a sum that is NaN stays NaN)
+  r.w_rest = r.rest.s > 0.f ? row_ex2((r.rest.m - r.M) * c) : r.rest.s;
+  r.w_list = row_ex2((l.z_ref - r.M) * c);
+  r.S = r.w_rest * r.rest.s + r.w_list * l.sum_e;
+  return r;
+}
+
 template <typename T, bool kGrad>
-__global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p, int C) {
+__global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p, int C, int buffers) {
   using V16 = RowVec<T>;
-  extern __shared__ uint4 s_row[];                 // (kGrad) the CTA's vectors of the row
-  // bit q of a thread's pair of words: its q-th vector holds a listed word
-  __shared__ __align__(16) unsigned int s_mark[2 * kRowThreads];
-  __shared__ __align__(16) int s_key[kHash];                       // vectors that hold listed words (-1: free) ...
-  __shared__ __align__(16) unsigned int s_drop[kHash];             // ... and which of their elements those are
-  __shared__ MaxSum s_all[DX_ROW_CLUSTER_MAX * kWarps];   // sums of all warps of all CTAs of the row
-  __shared__ ListSums s_list;
-  __shared__ unsigned int s_edge;                  // head (bits 0..7) and tail (8..15) elements that are listed
-  __shared__ int s_live;
+  // [buffers][kRowThreads][half] 16-bit words -- bit q of a thread's words: its q-th vector holds a listed word -- and
+  // behind them (kGrad) the CTA's vectors of the row
+  extern __shared__ uint4 s_dyn[];
+  __shared__ __align__(16) unsigned int s_hash[2][kHash];   // vector + 1 << 8 | its listed elements; 0: free
+  __shared__ MaxSum s_all[2][DX_ROW_CLUSTER_MAX * kRowWarps];   // sums of all warps of all CTAs of the row
+  __shared__ ListSums s_list[2];
+  __shared__ unsigned int s_edge[2];               // head (bits 0..7) and tail (8..15) elements that are listed
+  __shared__ float s_weight[2];                    // 0: nothing to learn from the row
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const bool list_warp = warp == kRowWarps;
   const int rank = C > 1 ? (int)cluster_rank() : 0;
-  const int t = blockIdx.x / C;
-  const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
-  T* out = kGrad ? reinterpret_cast<T*>(p.dlogits) + (size_t)t * (size_t)p.ld_d : nullptr;
-  const RowSplit sp = row_split(row, p.V, rank, C);
-  const int n_vec = sp.v_hi - sp.v_lo;
-  const int tail0 = p.V - sp.tail;
-  // gradient vectors can be stored as such where the output row is aligned like the input row
-  const bool same_align = kGrad && ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15u) == 0;
+  const int n_rows = gridDim.x / C;                // rows in flight: row t is followed by row t + n_rows
   const float c = p.c;
+  const int half = p.half;
+  unsigned int* s_mark = reinterpret_cast<unsigned int*>(s_dyn);
   if (C > 1) cluster_arrive();
 
-  // ---- the row on its way into shared memory, in two parts that can be waited for one by one (every thread copies
-  // what it reads itself); the list warp marks the listed words meanwhile
-  const int deep = (n_vec + kRowThreads - 1) / kRowThreads;        // vectors of a thread, at most
-  const int part = ((deep + 1) / 2 + kUnroll - 1) / kUnroll * kUnroll;
-  int id[kLists];                                  // list warp: entry lane + 32 i
-  float w;
-  if (list_warp) {
+  // Both roles walk the same rows and meet at the same barriers: one of the CTA in front of a row (its marks are there,
+  // the previous row's gradient has been stored), one of all CTAs of the row between the sums and the gradient.  The
+  // sums are kept in two sets, taken in turn by the rows that have any: a CTA that is one row ahead cannot overwrite
+  // what another still reads, and it cannot be two rows ahead of that barrier.
+  if (warp == kRowWarps) {
+    // ==== the list warp
+    int id[kLists];                                // entry lane + 32 i (-1: unused, out of range, listed before)
+    float w = 0.f;
+    auto load_ids = [&](int t) {
+      if (t >= p.N) return;
 #pragma unroll
-    for (int i = 0; i < kLists; ++i) id[i] = lane + 32 * i < p.k ? p.ids[(size_t)t * p.k + lane + 32 * i] : -1;
-    w = p.weight ? p.weight[t] : 1.f;
+      for (int i = 0; i < kLists; ++i) id[i] = lane + 32 * i < p.k ? p.ids[(size_t)t * p.k + lane + 32 * i] : -1;
+      w = p.weight ? p.weight[t] : 1.f;
+    };
+    auto mark = [&](int t, int b) {                // ids -> marks, hash table and state of buffer b
+      if (t >= p.N) return;
+      const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
+      const RowSplit sp = row_split(row, p.V, rank, C);
+      const int n_vec = sp.v_hi - sp.v_lo, tail0 = p.V - sp.tail;
+      unsigned int* marks = s_mark + b * half * (kRowThreads / 2);
+      for (int i = lane; i < half * (kRowThreads / 8); i += 32)
+        reinterpret_cast<uint4*>(marks)[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 2 * kRowThreads / 128; ++i) reinterpret_cast<uint4*>(s_mark)[lane + 32 * i] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < kHash / 128; ++i) {
-      reinterpret_cast<int4*>(s_key)[lane + 32 * i] = make_int4(-1, -1, -1, -1);
-      reinterpret_cast<uint4*>(s_drop)[lane + 32 * i] = make_uint4(0, 0, 0, 0);
-    }
-    if (lane == 0) s_edge = 0;
-    __syncwarp();
-    bool live = false, bad = false;
-#pragma unroll
-    for (int i = 0; i < kLists; ++i) {
-      if (32 * i >= p.k) continue;
-      bad |= id[i] < -1 || id[i] >= p.V;
-      if (id[i] < 0 || id[i] >= p.V) id[i] = -1;
-      live |= id[i] >= 0;
-      // an id counts once, with its first entry: the first of equal lanes, and not if an earlier 32 have left its bit
-      const unsigned int same = __match_any_sync(0xffffffffu, id[i]);
-      if (__ffs(same) - 1 != lane) id[i] = -1;
-      if (id[i] >= 0) {
-        unsigned int bit, old;
-        if (id[i] < sp.head) {
-          bit = 1u << id[i];
-          old = atomicOr(&s_edge, bit);
-        } else if (id[i] >= tail0) {
-          bit = 256u << (id[i] - tail0);
-          old = atomicOr(&s_edge, bit);
-        } else {
-          const int x = (id[i] - sp.head) / V16::kN;
-          int h = x & (kHash - 1);
-          for (int tries = 0; tries < kHash; ++tries) {   // (at most kHash / 2 keys: a free or equal one is found)
-            const int key = atomicCAS(&s_key[h], -1, x);
-            if (key == -1 || key == x) break;
-            h = (h + 1) & (kHash - 1);
-          }
-          bit = 1u << ((id[i] - sp.head) % V16::kN);
-          old = atomicOr(&s_drop[h], bit);
-          const int mine = x - sp.v_lo;
-          if (mine >= 0 && mine < n_vec) {
-            const int q = mine / kRowThreads;
-            atomicOr(&s_mark[2 * (mine % kRowThreads) + (q >> 5)], 1u << (q & 31));
-          }
-        }
-        if (old & bit) id[i] = -1;
-      }
+      for (int i = 0; i < kHash / 128; ++i) reinterpret_cast<uint4*>(s_hash[b])[lane + 32 * i] = make_uint4(0, 0, 0, 0);
+      if (lane == 0) s_edge[b] = 0;
       __syncwarp();
-    }
-    if (bad && rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
-    live = __any_sync(0xffffffffu, live);
-    if (lane == 0) s_live = live;
-  } else {
-    if (kGrad) {
-      const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo;
-#pragma unroll 4
-      for (int q = 0; q < deep; ++q) {
-        if (q == part) asm volatile("cp.async.commit_group;" ::: "memory");
-        if (tid + q * kRowThreads < n_vec) copy16(s_row + tid + q * kRowThreads, src + tid + q * kRowThreads);
-      }
-      if (part >= deep) asm volatile("cp.async.commit_group;" ::: "memory");
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    w = p.weight ? p.weight[t] : 1.f;
-  }
-  __syncthreads();
-  if (w == 0.f || !s_live) {   // (the same for every CTA of the row) nothing to learn: the logits do not matter
-    if (rank == 0 && tid == 0 && p.loss) p.loss[t] = 0.f;
-    if (kGrad) {
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      __syncthreads();         // (in place: nobody overwrites what is still being copied)
-      if (rank == 0 && tid < sp.head) out[tid] = V16::round(0.f);
-      if (rank == C - 1 && tid < sp.tail) out[tail0 + tid] = V16::round(0.f);
-      for (int i = tid; i < n_vec; i += kThreads) {
-        const int e = sp.head + (sp.v_lo + i) * V16::kN;
-        if (same_align) {
-          *reinterpret_cast<uint4*>(out + e) = make_uint4(0, 0, 0, 0);
-        } else {
+      bool live = false, bad = false;
 #pragma unroll
-          for (int q = 0; q < V16::kN; ++q) out[e + q] = V16::round(0.f);
+      for (int i = 0; i < kLists; ++i) {
+        if (32 * i >= p.k) continue;
+        int x = id[i];
+        bad |= x < -1 || x >= p.V;
+        if (x < 0 || x >= p.V) x = -1;
+        live |= x >= 0;
+        // an id counts once, with its first entry: the first of equal lanes, and not if an earlier 32 have left its bit
+        const unsigned int same = __match_any_sync(0xffffffffu, x);
+        if (__ffs(same) - 1 != lane) x = -1;
+        if (x >= 0) {
+          unsigned int bit, old;
+          if (x < sp.head) {
+            bit = 1u << x;
+            old = atomicOr(&s_edge[b], bit);
+          } else if (x >= tail0) {
+            bit = 256u << (x - tail0);
+            old = atomicOr(&s_edge[b], bit);
+          } else {
+            const int vec = (x - sp.head) / V16::kN;
+            const unsigned int key = (unsigned int)(vec + 1) << 8;
+            bit = 1u << ((x - sp.head) % V16::kN);
+            old = 0;
+            int h = vec & (kHash - 1);
+            for (int tries = 0; tries < kHash; ++tries) {   // (at most kHash / 2 vectors: a free or equal one is found)
+              const unsigned int found = atomicCAS(&s_hash[b][h], 0u, key | bit);
+              if (found == 0u) break;
+              if ((found & 0xffffff00u) == key) {
+                old = atomicOr(&s_hash[b][h], bit);
+                break;
+              }
+              h = (h + 1) & (kHash - 1);
+            }
+            const int mine = vec - sp.v_lo;
+            if (mine >= 0 && mine < n_vec) {
+              const int q = mine / kRowThreads, at = (mine % kRowThreads) * half + (q >> 4);
+              atomicOr(&marks[at >> 1], 1u << ((at & 1) * 16 + (q & 15)));
+            }
+          }
+          if (old & bit) x = -1;
+        }
+        id[i] = x;
+        __syncwarp();
+      }
+      if (bad && rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
+      live = __any_sync(0xffffffffu, live);
+      if (lane == 0) s_weight[b] = live ? w : 0.f;
+    };
+    // The list's part in a row, made ready while the row in front of it is worked on: sums for the gradient, sums for the
+    // loss, and per entry e^{(z_j - z_ref) / T} and p_j (log p_j is what the caller has given).
+    float z[kLists], lp[kLists], e[kLists], pj[kLists];
+    ListSums l{};
+    double mass = 0.0, p_log_p = 0.0, p_u = 0.0, sum_e = 0.0;
+    auto load_list = [&](int t) {
+      if (t >= p.N) return;
+      const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) {
+        z[i] = id[i] >= 0 ? V16::load(row + id[i]) : -INFINITY;
+        lp[i] = id[i] >= 0 ? p.lp[(size_t)t * p.k + lane + 32 * i] : -INFINITY;
+      }
+    };
+    auto list_sums = [&](int slot) {
+      float top = -FLT_MAX;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) top = fmaxf(top, z[i]);
+      l.z_ref = warp_max(top);
+      mass = p_log_p = p_u = sum_e = 0.0;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) {
+        e[i] = pj[i] = 0.f;
+        if (32 * i >= p.k) continue;
+        const double u = ((double)z[i] - (double)l.z_ref) * p.inv_T;
+        e[i] = id[i] >= 0 ? expf((float)u) : 0.f;
+        const double pd = exp((double)lp[i]);      // (a NaN entry makes the mass NaN, and with it the loss)
+        pj[i] = (float)pd;
+        sum_e += (double)e[i];
+        mass += pd;
+        if (pd > 0.0) {
+          p_log_p += pd * (double)lp[i];
+          p_u += pd * u;
         }
       }
+      sum_e = warp_sum(sum_e);
+      mass = warp_sum(mass);
+      p_log_p = warp_sum(p_log_p);
+      p_u = warp_sum(p_u);
+      l.norm = 1.f;
+      if (!p.tail && mass != 0.0) {                // p' = p / mass:  sum p' log p' = (sum p log p) / mass - log mass
+        const double norm = 1.0 / mass;
+        l.norm = (float)norm;
+        p_log_p = p_log_p * norm - log(mass);
+        p_u *= norm;
+        mass = mass == mass ? 1.0 : mass;
+      }
+      const double rest = p.tail && mass < 1.0 ? 1.0 - mass : 0.0;
+      l.sum_e = (float)sum_e;
+      l.beta = (float)(mass + rest);
+      l.rest = (float)rest;
+      if (lane == 0) s_list[slot] = l;
+      __syncwarp();
+    };
+    int at[kLists];                                // listed words of the previous row, their gradients, the row
+    float grad[kLists];
+    T* last_out = nullptr;
+    auto store_listed = [&]() {                    // over what the sweep has left in their places
+      if constexpr (kGrad) {
+        if (!last_out) return;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i)
+          if (at[i] >= 0) last_out[at[i]] = V16::round(grad[i]);
+        last_out = nullptr;
+      }
+    };
+    int t = blockIdx.x / C, turn = 0;
+    load_ids(t);
+    mark(t, 0);
+    load_list(t);
+    list_sums(0);
+    if (C > 1) cluster_wait();                     // (all CTAs of the row have started)
+#pragma unroll 1
+    for (int it = 0; t < p.N; ++it, t += n_rows) {
+      cta_barrier();
+      store_listed();
+      const float scale = s_weight[it & (buffers - 1)] * p.inv_Tf;
+      if (s_weight[it & (buffers - 1)] == 0.f) {   // nothing to learn from this row
+        if (rank == 0 && lane == 0 && p.loss) p.loss[t] = 0.f;
+        load_ids(t + n_rows);
+        mark(t + n_rows, (it + 1) & (buffers - 1));
+        load_list(t + n_rows);
+        list_sums(turn);
+        continue;
+      }
+      const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) at[i] = id[i];
+      if (C > 1) cluster_arrive();
+      load_ids(t + n_rows);
+      mark(t + n_rows, (it + 1) & (buffers - 1));
+      load_list(t + n_rows);
+      __syncwarp();
+      if (C > 1) cluster_wait();
+      else cta_barrier();
+      const RowSums r = row_sums(s_all[turn], l, C * kRowWarps, c);
+      turn ^= 1;
+      if (kGrad) {
+        const float f = r.S == 0.f ? 0.f : l.beta * r.w_list / r.S;
+        last_out = reinterpret_cast<T*>(p.dlogits) + (size_t)t * (size_t)p.ld_d;
+        const RowSplit sp = row_split(row, p.V, rank, C);
+#pragma unroll
+        for (int i = 0; i < kLists; ++i) {
+          grad[i] = r.S == 0.f ? 0.f : (f * e[i] - pj[i] * l.norm) * scale;
+          const int v = (at[i] - sp.head) / V16::kN;
+          if (at[i] < sp.head ? rank != 0 : at[i] >= p.V - sp.tail ? rank != C - 1 : v < sp.v_lo || v >= sp.v_hi) at[i] = -1;
+        }
+      }
+      if (rank == 0 && p.loss) {
+        const double rest = p.tail && mass < 1.0 ? 1.0 - mass : 0.0;
+        const double du_rest = ((double)r.rest.m - (double)r.M) * p.inv_T;
+        const double du_list = ((double)l.z_ref - (double)r.M) * p.inv_T;
+        const double S = (r.rest.s > 0.f ? exp(du_rest) : 1.0) * (double)r.rest.s + exp(du_list) * sum_e;
+        const double log_S = log(S);
+        // - sum_j p_j log q_j = -( sum p_j (z_j - z_ref) / T + P (z_ref - M) / T - P log S )
+        double loss = p_log_p - (p_u + (mass != 0.0 ? mass * (du_list - log_S) : 0.0));
+        if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)r.rest.s) - log_S));
+        if (S == 0.0) loss = mass + rest > 0.0 ? INFINITY : 0.0;   // nothing but -inf in the row
+        if (lane == 0) p.loss[t] = (float)loss;
+      }
+      list_sums(turn);
+    }
+    if (kGrad) {
+      cta_barrier();
+      store_listed();
     }
     return;
   }
-  const unsigned int edge = s_edge;
-  const bool head_in = !list_warp && rank == 0 && tid < sp.head && !(edge >> tid & 1u);      // this thread's unlisted
-  const bool tail_in = !list_warp && rank == C - 1 && tid < sp.tail && !(edge >> (8 + tid) & 1u);   // edge elements
-  float edge_head = -INFINITY, edge_tail = -INFINITY;
-  MaxSum st{-FLT_MAX, 0.f};
-  const unsigned long long c2 = f2_pack(c, c);
-  float pj[kLists], e[kLists];                     // list warp: p_j, e^{(z_j - z_ref) / T}
-  double mass = 0.0, p_log_p = 0.0, p_u = 0.0;     // ... and, in the first CTA, sums over the list
-  if (!list_warp) {
-    // ---- maximum and sum of exponentials of the unlisted words
-    const unsigned long long cl2 = f2_pack(p.c_lo, p.c_lo);
-    const uint2 marks = *reinterpret_cast<const uint2*>(s_mark + 2 * tid);
-    const uint4 none4 = make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
-    unsigned long long s2 = f2_pack(0.f, 0.f);
-    // All warps start from the largest unlisted element of their first chunk as the reference of the exponents; a thread
-    // takes another only when it meets an element more than 2^kSlack times as likely.
+
+  // ==== the eight warps that go over the row
+  uint4* s_row = s_dyn + buffers * half * (kRowThreads / 8);
+  const unsigned long long c2 = f2_pack(c, c), cl2 = f2_pack(p.c_lo, p.c_lo);
+  const uint4 none4 = make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
+  int t = blockIdx.x / C, turn = 0;
+  const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
+  RowSplit sp = row_split(row, p.V, rank, C);
+  // Every thread copies the vectors tid, tid + 256, ... that it reads itself, in two groups: those of the first half can
+  // be waited for alone.
+  if (kGrad) {
+    const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo;
+    const int n_vec = sp.v_hi - sp.v_lo, deep = (n_vec + kRowThreads - 1) / kRowThreads;
+#pragma unroll 2
+    for (int q = 0; q < deep; ++q) {
+      if (2 * q == (deep & ~(2 * kUnroll - 1))) asm volatile("cp.async.commit_group;" ::: "memory");
+      const int i = tid + q * kRowThreads;
+      if (i < n_vec) copy16(s_row + i, src + i);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  if (C > 1) cluster_wait();                       // (all CTAs of the row have started)
 #pragma unroll 1
-    for (int q = 0, arrived = 0; q < deep; q += kUnroll) {
-      if (kGrad && q >= arrived) {
-        if (arrived == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        else asm volatile("cp.async.wait_group 0;" ::: "memory");
-        arrived = arrived == 0 ? part : deep;
-      }
-      uint4 v[kUnroll];
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int i = tid + (q + u) * kRowThreads;
-        v[u] = none4;                                // (adds nothing)
-        if (i < n_vec) v[u] = kGrad ? s_row[i] : row_vec_stream(row, sp, sp.v_lo + i);
-      }
-      const unsigned int marked = (q < 32 ? marks.x >> q : marks.y >> (q - 32)) & ((1u << kUnroll) - 1u);
-      if (marked) {
+  for (int it = 0; t < p.N; ++it) {
+    const int b = it & (buffers - 1);
+    T* out = kGrad ? reinterpret_cast<T*>(p.dlogits) + (size_t)t * (size_t)p.ld_d : nullptr;
+    const int n_vec = sp.v_hi - sp.v_lo, deep = (n_vec + kRowThreads - 1) / kRowThreads;
+    const int tail0 = p.V - sp.tail;
+    const bool has_head = rank == 0 && tid < sp.head, has_tail = rank == C - 1 && tid < sp.tail;
+    // gradient vectors can be stored as such where the output row is aligned like the input row
+    const bool same_align = kGrad && ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15u) == 0;
+    T* out_vec = out + sp.head + (long long)sp.v_lo * V16::kN;
+    cta_barrier();
+    const float w = s_weight[b];
+    float coef = 0.f, ref = 0.f;                   // gradient of an unlisted word: coef * e^{(z - ref) / T}
+    float edge_head = -INFINITY, edge_tail = -INFINITY;
+    bool head_in = has_head, tail_in = has_tail;   // this thread's edge elements that are not listed
+    if (w != 0.f) {                                // (the same for every CTA of the row)
+      const unsigned int edge = s_edge[b];
+      head_in = has_head && !(edge >> tid & 1u);
+      tail_in = has_tail && !(edge >> (8 + tid) & 1u);
+      // ---- sum of exponentials of the unlisted words
+      MaxSum st{-FLT_MAX, 0.f};
+      const unsigned short* marks = reinterpret_cast<const unsigned short*>(s_mark) + (b * kRowThreads + tid) * half;
+      unsigned long long s2 = f2_pack(0.f, 0.f);
+      // All warps start from the largest unlisted element of their first chunk as the reference of the exponents; a
+      // thread takes another only when it meets an element more than 2^kSlack times as likely.
+      bool whole = false;
+#pragma unroll 1
+      for (int q = 0; q < deep; q += kUnroll) {
+        if (kGrad && q == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (kGrad && !whole && 2 * (q + kUnroll) > deep) {
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          whole = true;
+        }
+        uint4 v[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-          if (marked >> u & 1u) {
-            const int vec = sp.v_lo + tid + (q + u) * kRowThreads;
-            int h = vec & (kHash - 1);
-            for (int tries = 0; tries < kHash && s_key[h] != vec; ++tries) h = (h + 1) & (kHash - 1);
-            mask_vector<T>(v[u], s_drop[h]);
+          const int i = tid + (q + u) * kRowThreads;
+          v[u] = none4;                            // (adds nothing)
+          if (i < n_vec) v[u] = kGrad ? s_row[i] : row_vec_stream(row, sp, sp.v_lo + i);
+        }
+        const unsigned int marked = marks[q >> 4] >> (q & 15) & ((1u << kUnroll) - 1u);
+        if (marked) {
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) {
+            if (marked >> u & 1u) {
+              const int vec = sp.v_lo + tid + (q + u) * kRowThreads;
+              int h = vec & (kHash - 1);
+              for (int tries = 0; tries < kHash && s_hash[b][h] >> 8 != (unsigned int)vec + 1u; ++tries)
+                h = (h + 1) & (kHash - 1);
+              mask_vector<T>(v[u], s_hash[b][h]);
+            }
+          }
+        }
+        const float top = V16::largest(v, kUnroll);
+        if (q == 0) {
+          st.m = fmaxf(warp_max(top), -FLT_MAX);
+        } else if ((top - st.m) * c > kSlack) {
+          float s0, s1;
+          f2_unpack(s2, s0, s1);
+          s2 = f2_pack((s0 + s1) * row_ex2((st.m - top) * c), 0.f);
+          st.m = top;
+        }
+        const unsigned long long nm2 = f2_pack(-st.m, -st.m);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+#pragma unroll
+          for (int h = 0; h < V16::kN / 2; ++h) {
+            // (the factor in two parts: rounded to one, it would shift the exponents of all words the same way)
+            const unsigned long long d2 = f2_add(V16::pair(v[u], h), nm2);
+            float x0, x1;
+            f2_unpack(f2_fma(d2, cl2, f2_mul(d2, c2)), x0, x1);
+            s2 = f2_add(s2, f2_pack(row_ex2(x0), row_ex2(x1)));
           }
         }
       }
-      const float top = V16::largest(v, kUnroll);
-      if (q == 0) {
-        st.m = fmaxf(warp_max(top), -FLT_MAX);
-      } else if ((top - st.m) * c > kSlack) {
-        float s0, s1;
-        f2_unpack(s2, s0, s1);
-        s2 = f2_pack((s0 + s1) * row_ex2((st.m - top) * c), 0.f);
-        st.m = top;
+      float s0, s1;
+      f2_unpack(s2, s0, s1);
+      st.s = s0 + s1;
+      if (head_in || tail_in) {
+        edge_head = head_in ? V16::load(row + tid) : -INFINITY;
+        edge_tail = tail_in ? V16::load(row + tail0 + tid) : -INFINITY;
+        const float top = fmaxf(edge_head, edge_tail);
+        if (top > st.m) {
+          st.s *= row_ex2((st.m - top) * c);
+          st.m = top;
+        }
+        if (head_in) st.s += row_ex2((edge_head - st.m) * c);
+        if (tail_in) st.s += row_ex2((edge_tail - st.m) * c);
       }
-      const unsigned long long nm2 = f2_pack(-st.m, -st.m);
+      __syncwarp();
+      st = warp_join(st, c);
+      if (C > 1) {                                 // to all CTAs of the row
+        if (lane < C) {
+          const uint32_t a = cluster_addr(&s_all[turn][rank * kRowWarps + warp], lane);
+          cluster_store_f32(a, st.m);
+          cluster_store_f32(a + 4, st.s);
+        }
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+      } else {
+        if (lane == 0) s_all[turn][warp] = st;
+        cta_barrier();
+      }
+      if (kGrad) {
+        const RowSums r = row_sums(s_all[turn], s_list[turn], C * kRowWarps, c);
+        if (r.rest.s != 0.f && r.S != 0.f)
+          coef = (__fdividef(r.l.beta * r.w_rest, r.S) - __fdividef(r.l.rest, r.rest.s)) * (w * p.inv_Tf);
+        ref = r.rest.m;
+      }
+      turn ^= 1;
+    } else if (kGrad) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+    // ---- the gradient (zeros where there is nothing to learn); a vector's place takes the next row's vector as soon as
+    // it has been read
+    const T* next = row + (size_t)n_rows * (size_t)p.ld;
+    t += n_rows;
+    const RowSplit np = t < p.N ? row_split(next, p.V, rank, C) : sp;
+    if (kGrad) {
+      const uint4* next_src = reinterpret_cast<const uint4*>(next + np.head) + np.v_lo;
+      const int next_vecs = t < p.N ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
+      if (head_in) out[tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_head - ref) * c));
+      if (tail_in) out[tail0 + tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_tail - ref) * c));
+      const unsigned long long nm2 = f2_pack(-ref, -ref), k2 = f2_pack(coef, coef);
+      // (rows of the same length differ by one vector at most, where their alignment differs)
+#pragma unroll 1
+      for (int q = 0; q < max(deep, next_deep); q += kUnroll) {
+        if (2 * q == (next_deep & ~(2 * kUnroll - 1))) asm volatile("cp.async.commit_group;" ::: "memory");
+        uint4 v[kUnroll];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < kUnroll; ++u) {
+          const int i = tid + (q + u) * kRowThreads;
+          if (i < n_vec) v[u] = s_row[i];
+          if (i < next_vecs) copy16(s_row + i, next_src + i);
+        }
 #pragma unroll
-        for (int h = 0; h < V16::kN / 2; ++h) {
-          // (the factor in two parts: rounded to one, it would shift the exponents of all words the same way)
-          const unsigned long long d2 = f2_add(V16::pair(v[u], h), nm2);
-          float x0, x1;
-          f2_unpack(f2_fma(d2, cl2, f2_mul(d2, c2)), x0, x1);
-          s2 = f2_add(s2, f2_pack(row_ex2(x0), row_ex2(x1)));
+        for (int u = 0; u < kUnroll; ++u) {
+          const int i = tid + (q + u) * kRowThreads;
+          if (i >= n_vec) continue;
+          float g[V16::kN];
+#pragma unroll
+          for (int h = 0; h < V16::kN / 2; ++h) {
+            float x0, x1;
+            f2_unpack(f2_mul(f2_add(V16::pair(v[u], h), nm2), c2), x0, x1);
+            f2_unpack(f2_mul(f2_pack(row_ex2(x0), row_ex2(x1)), k2), g[2 * h], g[2 * h + 1]);
+          }
+          uint4 packed = V16::pack(g);
+          if (w == 0.f) packed = make_uint4(0, 0, 0, 0);   // (whatever the logits hold)
+          if (same_align) {
+            *reinterpret_cast<uint4*>(out_vec + (long long)i * V16::kN) = packed;
+          } else {
+#pragma unroll
+            for (int h = 0; h < V16::kN; ++h) out_vec[(long long)i * V16::kN + h] = V16::element(packed, h);
+          }
         }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    float s0, s1;
-    f2_unpack(s2, s0, s1);
-    st.s = s0 + s1;
-    if (head_in || tail_in) {
-      edge_head = head_in ? V16::load(row + tid) : -INFINITY;
-      edge_tail = tail_in ? V16::load(row + tail0 + tid) : -INFINITY;
-      const float top = fmaxf(edge_head, edge_tail);
-      if (top > st.m) {
-        st.s *= row_ex2((st.m - top) * c);
-        st.m = top;
-      }
-      if (head_in) st.s += row_ex2((edge_head - st.m) * c);
-      if (tail_in) st.s += row_ex2((edge_tail - st.m) * c);
-    }
-    st = warp_join(st, c);
-  } else {
-    // ---- the list (log p_j is what the caller has given)
-    float z[kLists], lp[kLists], top = -FLT_MAX;
-#pragma unroll
-    for (int i = 0; i < kLists; ++i) {
-      z[i] = id[i] >= 0 ? V16::load(row + id[i]) : -INFINITY;
-      lp[i] = id[i] >= 0 ? p.lp[(size_t)t * p.k + lane + 32 * i] : -INFINITY;
-      top = fmaxf(top, z[i]);
-    }
-    ListSums l{warp_max(top), 0.f, 0.f, 0.f, 1.f};
-    double se = 0.0;
-#pragma unroll
-    for (int i = 0; i < kLists; ++i) {
-      e[i] = pj[i] = 0.f;
-      if (32 * i >= p.k) continue;
-      const double u = ((double)z[i] - (double)l.z_ref) * p.inv_T;
-      e[i] = id[i] >= 0 ? expf((float)u) : 0.f;
-      const double pd = exp((double)lp[i]);          // (a NaN entry makes the mass NaN, and with it the loss)
-      pj[i] = (float)pd;
-      se += (double)e[i];
-      mass += pd;
-      if (pd > 0.0) {
-        p_log_p += pd * (double)lp[i];
-        p_u += pd * u;
-      }
-    }
-    se = warp_sum(se);
-    mass = warp_sum(mass);
-    p_log_p = warp_sum(p_log_p);
-    p_u = warp_sum(p_u);
-    if (!p.tail && mass != 0.0) {                    // p' = p / mass:  sum p' log p' = (sum p log p) / mass - log mass
-      const double norm = 1.0 / mass;
-      l.norm = (float)norm;
-      p_log_p = p_log_p * norm - log(mass);
-      p_u *= norm;
-      mass = mass == mass ? 1.0 : mass;
-    }
-    const double rest = p.tail && mass < 1.0 ? 1.0 - mass : 0.0;
-    l.sum_e = (float)se;
-    l.beta = (float)(mass + rest);
-    l.rest = (float)rest;
-    if (lane == 0) s_list = l;
+    row = next;
+    sp = np;
   }
-  // ---- sums of the warp, to all CTAs of the row (the list warp has none)
-  if (C > 1) {
-    __syncwarp();
-    cluster_wait();                                  // (all CTAs of the row have started)
-    if (!list_warp && lane < C) {
-      const uint32_t a = cluster_addr(&s_all[rank * kRowWarps + warp], lane);
-      cluster_store_f32(a, st.m);
-      cluster_store_f32(a + 4, st.s);
-    }
-    __syncwarp();
-    cluster_arrive();
-    cluster_wait();
-  } else {
-    if (!list_warp && lane == 0) s_all[warp] = st;
-    __syncthreads();
+  if (kGrad) cta_barrier();
+}
+
+// clusters of C CTAs that run on the GPU at a time (asked once per context and size)
+template <typename T, bool kGrad>
+cudaError_t max_clusters(dx_ctx* ctx, int C, size_t smem, int* out) {
+  DxClusterCount& known = ctx->distill_clusters[(sizeof(T) == 4 ? 2 : 0) + (kGrad ? 1 : 0)];
+  if (known.cluster != C || known.smem != smem) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(C * ctx->sm_count);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    cudaError_t e = cudaOccupancyMaxActiveClusters(&n, dx_distill_kernel<T, kGrad>, &cfg);
+    if (e != cudaSuccess) return e;
+    known = DxClusterCount{C, smem, n};
   }
-  // ---- the row's scalars (every warp, the same arithmetic in the same order)
-  MaxSum x{-FLT_MAX, 0.f};
-  for (int i = lane; i < C * kRowWarps; i += 32) x = join(x, s_all[i], c);
-  x = warp_join(x, c);
-  const ListSums l = s_list;
-  const float M = fmaxf(x.m, l.z_ref);
-  // (fp32: the gradient's factors; a sum that is NaN stays NaN)
-  const float w_rest = x.s > 0.f ? row_ex2((x.m - M) * c) : x.s;
-  const float w_list = row_ex2((l.z_ref - M) * c);
-  const float S = w_rest * x.s + w_list * l.sum_e;
-  const float scale = w * (float)p.inv_T;
-  if (kGrad && !list_warp) {
-    float coef = 0.f;
-    if (x.s != 0.f && S != 0.f) coef = (l.beta * w_rest / S - l.rest / x.s) * scale;
-    if (head_in) out[tid] = V16::round(coef * row_ex2((edge_head - x.m) * c));
-    if (tail_in) out[tail0 + tid] = V16::round(coef * row_ex2((edge_tail - x.m) * c));
-    const unsigned long long nm2 = f2_pack(-x.m, -x.m), k2 = f2_pack(coef, coef);
-    T* out_vec = out + sp.head + (long long)sp.v_lo * V16::kN;
-    auto gradient = [&](const uint4& y, float (&g)[V16::kN]) {
-#pragma unroll
-      for (int q = 0; q < V16::kN / 2; ++q) {
-        float x0, x1;
-        f2_unpack(f2_mul(f2_add(V16::pair(y, q), nm2), c2), x0, x1);
-        f2_unpack(f2_mul(f2_pack(row_ex2(x0), row_ex2(x1)), k2), g[2 * q], g[2 * q + 1]);
-      }
-    };
-    if (same_align) {
-#pragma unroll 2
-      for (int i = tid; i < n_vec; i += kRowThreads) {
-        float g[V16::kN];
-        gradient(s_row[i], g);
-        *reinterpret_cast<uint4*>(out_vec + (long long)i * V16::kN) = V16::pack(g);
-      }
-    } else {
-#pragma unroll 1
-      for (int i = tid; i < n_vec; i += kRowThreads) {
-        float g[V16::kN];
-        gradient(s_row[i], g);
-#pragma unroll
-        for (int q = 0; q < V16::kN; ++q) out_vec[(long long)i * V16::kN + q] = V16::round(g[q]);
-      }
-    }
-  }
-  if (list_warp && rank == 0 && p.loss) {
-    const double du_rest = ((double)x.m - (double)M) * p.inv_T, du_list = ((double)l.z_ref - (double)M) * p.inv_T;
-    const double S64 = (x.s > 0.f ? exp(du_rest) : 1.0) * (double)x.s + exp(du_list) * (double)l.sum_e;
-    const double log_S = log(S64);
-    const double rest = p.tail && mass < 1.0 ? 1.0 - mass : 0.0;
-    // - sum_j p_j log q_j = -( sum p_j (z_j - z_ref) / T + P (z_ref - M) / T - P log S )
-    double loss = p_log_p - (p_u + (mass != 0.0 ? mass * (du_list - log_S) : 0.0));
-    if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)x.s) - log_S));
-    if (S64 == 0.0) loss = mass + rest > 0.0 ? INFINITY : 0.0;   // nothing but -inf in the row
-    if (lane == 0) p.loss[t] = (float)loss;
-  }
-  if (kGrad) {
-    if (list_warp) {                                 // gradients of this CTA's listed words
-      const float f = S == 0.f ? 0.f : l.beta * w_list / S;
-#pragma unroll
-      for (int i = 0; i < kLists; ++i) {
-        e[i] = S == 0.f ? 0.f : (f * e[i] - pj[i] * l.norm) * scale;
-        const int v_at = (id[i] - sp.head) / V16::kN - sp.v_lo;
-        if (id[i] < sp.head ? rank != 0 : id[i] >= tail0 ? rank != C - 1 : v_at < 0 || v_at >= n_vec) id[i] = -1;
-      }
-    }
-    __syncthreads();
-    // ... over what the sweep has left in their places
-    if (list_warp) {
-#pragma unroll
-      for (int i = 0; i < kLists; ++i)
-        if (id[i] >= 0) out[id[i]] = V16::round(e[i]);
-    }
-  }
+  *out = known.count;
+  return cudaSuccess;
 }
 
 template <typename T, bool kGrad>
@@ -430,8 +557,24 @@ cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
           ((long long)p.N * C * 2 <= slots && (long long)C * 2 * kRowThreads * 16 <= bytes)))
     C *= 2;
   const long long slice = (bytes / 16 + C - 1) / C;      // vectors of a CTA, at most
-  const size_t smem = kGrad ? (size_t)slice * 16 : 0;
-  return dx_launch_pdl(false, dx_distill_kernel<T, kGrad>, dim3((unsigned)p.N * C), dim3(kThreads), smem, st, C, p, C);
+  DistillParams q = p;
+  q.half = (int)((slice + kRowThreads * 16 - 1) / (kRowThreads * 16));
+  if (q.half < 1) q.half = 1;
+  const size_t held = kGrad ? (size_t)slice * 16 : 0;
+  // As many clusters as run at a time, each going from row to row with the next row's logits and marks on their way;
+  // rows so long that only one set of marks fits get a cluster each.
+  const int buffers = held + 2 * 512 * (size_t)q.half + kStaticBytes <= (size_t)ctx->smem_optin ? 2 : 1;
+  const size_t smem = held + buffers * 512 * (size_t)q.half;
+  int rows = p.N;
+  if (buffers == 2) {
+    int active = 0;
+    cudaError_t e = max_clusters<T, kGrad>(ctx, C, smem, &active);
+    if (e != cudaSuccess) return e;
+    if (active < 1) return cudaErrorInvalidConfiguration;
+    if (rows > active) rows = active;
+  }
+  return dx_launch_pdl(false, dx_distill_kernel<T, kGrad>, dim3((unsigned)rows * C), dim3(kThreads), smem, st, C, q, C,
+                       buffers);
 }
 
 template <typename K>
@@ -444,7 +587,7 @@ cudaError_t prepare(K kernel, int smem) {
 }  // namespace
 
 size_t dx_distill_max_row_bytes(const dx_ctx* ctx) {
-  return (size_t)(ctx->smem_optin - kStaticBytes - 16) * DX_ROW_CLUSTER_MAX;
+  return (size_t)(ctx->smem_optin - kStaticBytes - 2048 - 16) * DX_ROW_CLUSTER_MAX;
 }
 
 cudaError_t dx_distill_prepare(const dx_ctx* ctx) {
@@ -461,8 +604,8 @@ cudaError_t dx_launch_distill(dx_ctx* ctx, const void* logits, int dtype, int N,
                               float temperature, const float* row_weight, float* loss, void* dlogits, long long ld_d,
                               cudaStream_t st) {
   const double c = 1.4426950408889634 / (double)temperature;
-  DistillParams p{logits, N, V, k, tail, ld, ld_d, teacher_ids, teacher_logprobs,
-                  (float)c, (float)(c - (double)(float)c), 1.0 / (double)temperature, row_weight, loss, dlogits, ctx->dev_status};
+  DistillParams p{logits, N, V, k, tail, 0, ld, ld_d, teacher_ids, teacher_logprobs,
+                  (float)c, (float)(c - (double)(float)c), 1.0 / (double)temperature, (float)(1.0 / (double)temperature), row_weight, loss, dlogits, ctx->dev_status};
   if (dtype == DX_DTYPE_FP32) return dlogits ? launch<float, true>(ctx, p, st) : launch<float, false>(ctx, p, st);
   return dlogits ? launch<__nv_bfloat16, true>(ctx, p, st) : launch<__nv_bfloat16, false>(ctx, p, st);
 }

@@ -80,6 +80,9 @@ struct RowVec<float> {
   static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
   }
+  static __device__ __forceinline__ float element(const uint4& v, int i) {
+    return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+  }
 };
 template <>
 struct RowVec<__nv_bfloat16> {
@@ -111,7 +114,10 @@ struct RowVec<__nv_bfloat16> {
   }
   static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
   static __device__ __forceinline__ __nv_bfloat16 round(float x) { return __float2bfloat16_rn(x); }
-  // one rounding of at most half a bf16 step, 2^-9 relative
+  static __device__ __forceinline__ __nv_bfloat16 element(const uint4& v, int i) {
+    return __ushort_as_bfloat16((unsigned short)(word(v, i >> 1) >> (16 * (i & 1))));
+  }
+  // one rounding of at most half a bf16 step, 2^-8 relative
   static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
     uint4 r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(f[1]), "f"(f[0]));
