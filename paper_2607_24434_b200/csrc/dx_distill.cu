@@ -57,9 +57,8 @@ struct ListSums {
   float z_ref, sum_e, beta, rest, norm;
 };
 
-__device__ __forceinline__ void copy16(uint4* dst_smem, const uint4* src) {
-  const uint32_t d = static_cast<uint32_t>(__cvta_generic_to_shared(dst_smem));
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+__device__ __forceinline__ void copy16(uint32_t dst_smem, const uint4* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
 }
 // vector `v` with the elements in `drop` at -inf
 template <typename T>
@@ -335,7 +334,9 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
   }
 
   // ==== the eight warps that go over the row
-  uint4* s_row = s_dyn + buffers * half * (kRowThreads / 8);
+  // this thread's vectors of the row: every 4096 bytes from here
+  const uint32_t s_mine =
+      static_cast<uint32_t>(__cvta_generic_to_shared(s_dyn + buffers * half * (kRowThreads / 8) + tid));
   const unsigned long long c2 = f2_pack(c, c), cl2 = f2_pack(p.c_lo, p.c_lo);
   const uint4 none4 = make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
   int t = blockIdx.x / C, turn = 0;
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
     for (int q = 0; q < deep; ++q) {
       if (2 * q == (deep & ~(2 * kUnroll - 1))) asm volatile("cp.async.commit_group;" ::: "memory");
       const int i = tid + q * kRowThreads;
-      if (i < n_vec) copy16(s_row + i, src + i);
+      if (i < n_vec) copy16(s_mine + q * kRowThreads * 16, src + i);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
@@ -378,25 +379,12 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
       MaxSum st{-FLT_MAX, 0.f};
       const unsigned short* marks = reinterpret_cast<const unsigned short*>(s_mark) + (b * kRowThreads + tid) * half;
       unsigned long long s2 = f2_pack(0.f, 0.f);
-      // All warps start from the largest unlisted element of their first chunk as the reference of the exponents; a
+      unsigned int marked = 0;
+      // All warps start from the largest unlisted element of their first vectors as the reference of the exponents; a
       // thread takes another only when it meets an element more than 2^kSlack times as likely.
-      bool whole = false;
-#pragma unroll 1
-      for (int q = 0; q < deep; q += kUnroll) {
-        if (kGrad && q == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        if (kGrad && !whole && 2 * (q + kUnroll) > deep) {
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-          whole = true;
-        }
-        uint4 v[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int i = tid + (q + u) * kRowThreads;
-          v[u] = none4;                            // (adds nothing)
-          if (i < n_vec) v[u] = kGrad ? s_row[i] : row_vec_stream(row, sp, sp.v_lo + i);
-        }
-        const unsigned int marked = marks[q >> 4] >> (q & 15) & ((1u << kUnroll) - 1u);
-        if (marked) {
+      auto add = [&](uint4 (&v)[kUnroll], int q, int n_v) {
+        if ((q & 15) == 0) marked = marks[q >> 4];
+        if (marked & ((1u << kUnroll) - 1u)) {
 #pragma unroll
           for (int u = 0; u < kUnroll; ++u) {
             if (marked >> u & 1u) {
@@ -408,7 +396,8 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
             }
           }
         }
-        const float top = V16::largest(v, kUnroll);
+        marked >>= kUnroll;
+        const float top = n_v == 1 ? V16::largest(v[0]) : V16::largest(v, kUnroll);
         if (q == 0) {
           st.m = fmaxf(warp_max(top), -FLT_MAX);
         } else if ((top - st.m) * c > kSlack) {
@@ -420,6 +409,7 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
         const unsigned long long nm2 = f2_pack(-st.m, -st.m);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
+          if (u >= n_v) continue;
 #pragma unroll
           for (int h = 0; h < V16::kN / 2; ++h) {
             // (the factor in two parts: rounded to one, it would shift the exponents of all words the same way)
@@ -429,6 +419,35 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
             s2 = f2_add(s2, f2_pack(row_ex2(x0), row_ex2(x1)));
           }
         }
+      };
+      const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo + tid;
+      uint32_t held = s_mine;
+      int q = 0;
+      if (kGrad) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      const int late = (deep & ~(2 * kUnroll - 1)) / 2;          // vectors from here on are in the second group
+#pragma unroll 1
+      for (; (q + kUnroll) * kRowThreads <= n_vec; q += kUnroll, src += kUnroll * kRowThreads) {
+        if (kGrad && q == late) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        uint4 v[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          v[u] = kGrad ? load_shared(held + u * kRowThreads * 16) : load_stream(src + u * kRowThreads);
+        held += kUnroll * kRowThreads * 16;
+        add(v, q, kUnroll);
+      }
+      if (kGrad) asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll 1
+      for (; q < deep; q += kUnroll) {                           // what is left: less than kUnroll vectors per thread,
+        uint4 v[kUnroll];                                        // and one more for some
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          v[u] = none4;                                          // (adds nothing)
+          if (tid + (q + u) * kRowThreads < n_vec)
+            v[u] = kGrad ? load_shared(held + u * kRowThreads * 16) : load_stream(src + u * kRowThreads);
+        }
+        // (a single vector: the warps that have no second one)
+        if ((q + 1) * kRowThreads + (tid & ~31) < n_vec) add(v, q, kUnroll);
+        else add(v, q, 1);
       }
       float s0, s1;
       f2_unpack(s2, s0, s1);
@@ -480,37 +499,57 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
       if (head_in) out[tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_head - ref) * c));
       if (tail_in) out[tail0 + tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_tail - ref) * c));
       const unsigned long long nm2 = f2_pack(-ref, -ref), k2 = f2_pack(coef, coef);
-      // (rows of the same length differ by one vector at most, where their alignment differs)
+      auto gradient = [&](const uint4& v) {
+        float g[V16::kN];
+#pragma unroll
+        for (int h = 0; h < V16::kN / 2; ++h) {
+          float x0, x1;
+          f2_unpack(f2_mul(f2_add(V16::pair(v, h), nm2), c2), x0, x1);
+          f2_unpack(f2_mul(f2_pack(row_ex2(x0), row_ex2(x1)), k2), g[2 * h], g[2 * h + 1]);
+        }
+        return V16::pack(g);
+      };
+      const uint4* fetch = next_src + tid;
+      uint4* store = reinterpret_cast<uint4*>(out_vec) + tid;
+      uint32_t held = s_mine;
+      const int late = (next_deep & ~(2 * kUnroll - 1)) / 2;     // vectors from here on make the second group
+      const int plain = same_align && w != 0.f ? min(n_vec, next_vecs ? next_vecs : n_vec) : 0;
+      int q = 0;
 #pragma unroll 1
-      for (int q = 0; q < max(deep, next_deep); q += kUnroll) {
-        if (2 * q == (next_deep & ~(2 * kUnroll - 1))) asm volatile("cp.async.commit_group;" ::: "memory");
+      for (; (q + kUnroll) * kRowThreads <= plain; q += kUnroll) {
+        if (q == late) asm volatile("cp.async.commit_group;" ::: "memory");
         uint4 v[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int i = tid + (q + u) * kRowThreads;
-          if (i < n_vec) v[u] = s_row[i];
-          if (i < next_vecs) copy16(s_row + i, next_src + i);
+        for (int u = 0; u < kUnroll; ++u) v[u] = load_shared(held + u * kRowThreads * 16);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) store[u * kRowThreads] = gradient(v[u]);
+        if (next_vecs) {
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) copy16(held + u * kRowThreads * 16, fetch + u * kRowThreads);
         }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int i = tid + (q + u) * kRowThreads;
-          if (i >= n_vec) continue;
-          float g[V16::kN];
-#pragma unroll
-          for (int h = 0; h < V16::kN / 2; ++h) {
-            float x0, x1;
-            f2_unpack(f2_mul(f2_add(V16::pair(v[u], h), nm2), c2), x0, x1);
-            f2_unpack(f2_mul(f2_pack(row_ex2(x0), row_ex2(x1)), k2), g[2 * h], g[2 * h + 1]);
-          }
-          uint4 packed = V16::pack(g);
-          if (w == 0.f) packed = make_uint4(0, 0, 0, 0);   // (whatever the logits hold)
+        held += kUnroll * kRowThreads * 16;
+        fetch += kUnroll * kRowThreads;
+        store += kUnroll * kRowThreads;
+      }
+      // the rest, rows of another alignment than the logits', rows there is nothing to learn from (rows of the same
+      // length differ by one vector at most, where their alignment differs)
+#pragma unroll 1
+      for (; q < max(deep, next_deep); ++q, held += kRowThreads * 16, fetch += kRowThreads, store += kRowThreads) {
+        if (q == late) asm volatile("cp.async.commit_group;" ::: "memory");
+        const int i = tid + q * kRowThreads;
+        uint4 v = none4;
+        if (i < n_vec) v = load_shared(held);
+        if (i < n_vec) {
+          v = w == 0.f ? make_uint4(0, 0, 0, 0) : gradient(v);   // (whatever the logits hold)
           if (same_align) {
-            *reinterpret_cast<uint4*>(out_vec + (long long)i * V16::kN) = packed;
+            *store = v;
           } else {
+            T* at = out_vec + (long long)i * V16::kN;
 #pragma unroll
-            for (int h = 0; h < V16::kN; ++h) out_vec[(long long)i * V16::kN + h] = V16::element(packed, h);
+            for (int h = 0; h < V16::kN; ++h) at[h] = V16::element(v, h);
           }
         }
+        if (i < next_vecs) copy16(held, fetch);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     }

@@ -218,13 +218,19 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
   const uint4 none4 = make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
   float seg = -INFINITY;
   int g = 0, in_seg = 0;
+  const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo + tid;
 #pragma unroll 1
-  for (int ch = 0, i = sp.v_lo + tid; ch < chunks; ++ch, i += kUnroll * kRowThreads) {
+  for (int ch = 0; ch < chunks; ++ch, src += kUnroll * kRowThreads) {
     uint4 v[kUnroll];
+    if ((ch + 1) * (kUnroll * kRowThreads) <= n_vec) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      v[u] = none4;                                        // (adds nothing to any sum)
-      if (i + u * kRowThreads < sp.v_hi) v[u] = row_vec_stream(row, sp, i + u * kRowThreads);
+      for (int u = 0; u < kUnroll; ++u) v[u] = load_stream(src + u * kRowThreads);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        v[u] = none4;                                      // (adds nothing to any sum)
+        if ((ch * kUnroll + u) * kRowThreads + tid < n_vec) v[u] = load_stream(src + u * kRowThreads);
+      }
     }
     const float top = V16::largest(v, kUnroll);
     if (ch == 0) {

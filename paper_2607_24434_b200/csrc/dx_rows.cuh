@@ -147,14 +147,18 @@ __device__ __forceinline__ RowSplit row_split(const T* row, int V, int rank, int
   return s;
 }
 
-// vector v of the row's aligned vectors; each logit is read once, L1 is left to what is read again
-template <typename T>
-__device__ __forceinline__ uint4 row_vec_stream(const T* row, const RowSplit& sp, int v) {
+// (each logit is read once; L1 is left to what is read again)
+__device__ __forceinline__ uint4 load_stream(const uint4* p) {
   uint4 r;
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
-               : "l"(reinterpret_cast<const uint4*>(row + sp.head) + v)
+               : "l"(p)
                : "memory");
+  return r;
+}
+__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
+  uint4 r;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr) : "memory");
   return r;
 }
 
