@@ -20,7 +20,6 @@ namespace {
 constexpr int kUnroll = 2;
 constexpr float kSlack = 8.f;                     // powers of two by which an element may exceed its sum's reference
 constexpr int kStaticBytes = 4608;                // at least the kernel's static shared memory
-constexpr int kLists = DX_MAX_TEACHER / 32;       // list entries per lane of the list's warp
 constexpr int kHash = 2 * DX_MAX_TEACHER;
 constexpr int kThreads = kRowThreads + 32;        // eight warps that stream, one that handles the list
 
@@ -110,7 +109,8 @@ __device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l
   return r;
 }
 
-template <typename T, bool kGrad>
+// kLists: list entries per lane of the list's warp, at least k / 32 (its registers would not last for four where two do)
+template <typename T, bool kGrad, int kLists>
 __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p, int C, int buffers) {
   using V16 = RowVec<T>;
   // [buffers][kRowThreads][half] 16-bit words -- bit q of a thread's words: its q-th vector holds a listed word -- and
@@ -204,9 +204,12 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
       live = __any_sync(0xffffffffu, live);
       if (lane == 0) s_weight[b] = live ? w : 0.f;
     };
-    // The list's part in a row, made ready while the row in front of it is worked on: sums for the gradient, sums for the
-    // loss, and per entry e^{(z_j - z_ref) / T} and p_j (log p_j is what the caller has given).
+    // The list's part in a row: logits and log p_j, on their way while the row in front is worked on; then per entry
+    // e^{(z_j - z_ref) / T} -- later the word's gradient, stored when the next row begins -- and p_j, the sums for the
+    // gradient, and the sums for the loss (log p_j is what the caller has given).
     float z[kLists], lp[kLists], e[kLists], pj[kLists];
+    int at[kLists];
+    T* last_out = nullptr;
     ListSums l{};
     double mass = 0.0, p_log_p = 0.0, p_u = 0.0, sum_e = 0.0;
     auto load_list = [&](int t) {
@@ -221,7 +224,10 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
     auto list_sums = [&](int slot) {
       float top = -FLT_MAX;
 #pragma unroll
-      for (int i = 0; i < kLists; ++i) top = fmaxf(top, z[i]);
+      for (int i = 0; i < kLists; ++i) {
+        at[i] = id[i];
+        top = fmaxf(top, z[i]);
+      }
       l.z_ref = warp_max(top);
       mass = p_log_p = p_u = sum_e = 0.0;
 #pragma unroll
@@ -229,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
         e[i] = pj[i] = 0.f;
         if (32 * i >= p.k) continue;
         const double u = ((double)z[i] - (double)l.z_ref) * p.inv_T;
-        e[i] = id[i] >= 0 ? expf((float)u) : 0.f;
+        e[i] = at[i] >= 0 ? expf((float)u) : 0.f;
         const double pd = exp((double)lp[i]);      // (a NaN entry makes the mass NaN, and with it the loss)
         pj[i] = (float)pd;
         sum_e += (double)e[i];
@@ -258,15 +264,12 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
       if (lane == 0) s_list[slot] = l;
       __syncwarp();
     };
-    int at[kLists];                                // listed words of the previous row, their gradients, the row
-    float grad[kLists];
-    T* last_out = nullptr;
     auto store_listed = [&]() {                    // over what the sweep has left in their places
       if constexpr (kGrad) {
         if (!last_out) return;
 #pragma unroll
         for (int i = 0; i < kLists; ++i)
-          if (at[i] >= 0) last_out[at[i]] = V16::round(grad[i]);
+          if (at[i] >= 0) last_out[at[i]] = V16::round(e[i]);
         last_out = nullptr;
       }
     };
@@ -274,7 +277,6 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
     load_ids(t);
     mark(t, 0);
     load_list(t);
-    list_sums(0);
     if (C > 1) cluster_wait();                     // (all CTAs of the row have started)
 #pragma unroll 1
     for (int it = 0; t < p.N; ++it, t += n_rows) {
@@ -286,12 +288,10 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
         load_ids(t + n_rows);
         mark(t + n_rows, (it + 1) & (buffers - 1));
         load_list(t + n_rows);
-        list_sums(turn);
         continue;
       }
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
-#pragma unroll
-      for (int i = 0; i < kLists; ++i) at[i] = id[i];
+      list_sums(turn);
       if (C > 1) cluster_arrive();
       load_ids(t + n_rows);
       mark(t + n_rows, (it + 1) & (buffers - 1));
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
         const RowSplit sp = row_split(row, p.V, rank, C);
 #pragma unroll
         for (int i = 0; i < kLists; ++i) {
-          grad[i] = r.S == 0.f ? 0.f : (f * e[i] - pj[i] * l.norm) * scale;
+          e[i] = r.S == 0.f ? 0.f : (f * e[i] - pj[i] * l.norm) * scale;
           const int v = (at[i] - sp.head) / V16::kN;
           if (at[i] < sp.head ? rank != 0 : at[i] >= p.V - sp.tail ? rank != C - 1 : v < sp.v_lo || v >= sp.v_hi) at[i] = -1;
         }
@@ -324,7 +324,6 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
         if (S == 0.0) loss = mass + rest > 0.0 ? INFINITY : 0.0;   // nothing but -inf in the row
         if (lane == 0) p.loss[t] = (float)loss;
       }
-      list_sums(turn);
     }
     if (kGrad) {
       cta_barrier();
@@ -560,9 +559,9 @@ __global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p
 }
 
 // clusters of C CTAs that run on the GPU at a time (asked once per context and size)
-template <typename T, bool kGrad>
+template <typename T, bool kGrad, int kLists>
 cudaError_t max_clusters(dx_ctx* ctx, int C, size_t smem, int* out) {
-  DxClusterCount& known = ctx->distill_clusters[(sizeof(T) == 4 ? 2 : 0) + (kGrad ? 1 : 0)];
+  DxClusterCount& known = ctx->distill_clusters[(sizeof(T) == 4 ? 4 : 0) + (kGrad ? 2 : 0) + (kLists == 4 ? 1 : 0)];
   if (known.cluster != C || known.smem != smem) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(C * ctx->sm_count);
@@ -575,7 +574,7 @@ cudaError_t max_clusters(dx_ctx* ctx, int C, size_t smem, int* out) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int n = 0;
-    cudaError_t e = cudaOccupancyMaxActiveClusters(&n, dx_distill_kernel<T, kGrad>, &cfg);
+    cudaError_t e = cudaOccupancyMaxActiveClusters(&n, dx_distill_kernel<T, kGrad, kLists>, &cfg);
     if (e != cudaSuccess) return e;
     known = DxClusterCount{C, smem, n};
   }
@@ -583,7 +582,7 @@ cudaError_t max_clusters(dx_ctx* ctx, int C, size_t smem, int* out) {
   return cudaSuccess;
 }
 
-template <typename T, bool kGrad>
+template <typename T, bool kGrad, int kLists>
 cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
   // CTAs per row: few enough bytes per CTA that four fit an SM (one loads while another computes or stores), and as many
   // as fill the GPU when there are few rows.  (Without the gradient nothing has to fit; the same split gives the same
@@ -607,13 +606,18 @@ cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
   int rows = p.N;
   if (buffers == 2) {
     int active = 0;
-    cudaError_t e = max_clusters<T, kGrad>(ctx, C, smem, &active);
+    cudaError_t e = max_clusters<T, kGrad, kLists>(ctx, C, smem, &active);
     if (e != cudaSuccess) return e;
     if (active < 1) return cudaErrorInvalidConfiguration;
     if (rows > active) rows = active;
   }
-  return dx_launch_pdl(false, dx_distill_kernel<T, kGrad>, dim3((unsigned)rows * C), dim3(kThreads), smem, st, C, q, C,
+  return dx_launch_pdl(false, dx_distill_kernel<T, kGrad, kLists>, dim3((unsigned)rows * C), dim3(kThreads), smem, st, C, q, C,
                        buffers);
+}
+
+template <typename T, bool kGrad>
+cudaError_t launch_lists(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
+  return p.k <= 64 ? launch<T, kGrad, 2>(ctx, p, st) : launch<T, kGrad, 4>(ctx, p, st);
 }
 
 template <typename K>
@@ -631,10 +635,14 @@ size_t dx_distill_max_row_bytes(const dx_ctx* ctx) {
 
 cudaError_t dx_distill_prepare(const dx_ctx* ctx) {
   const int smem = ctx->smem_optin - kStaticBytes;
-  cudaError_t e = prepare(dx_distill_kernel<float, true>, smem);
-  if (e == cudaSuccess) e = prepare(dx_distill_kernel<float, false>, smem);
-  if (e == cudaSuccess) e = prepare(dx_distill_kernel<__nv_bfloat16, true>, smem);
-  if (e == cudaSuccess) e = prepare(dx_distill_kernel<__nv_bfloat16, false>, smem);
+  cudaError_t e = prepare(dx_distill_kernel<float, true, 2>, smem);
+  if (e == cudaSuccess) e = prepare(dx_distill_kernel<float, true, 4>, smem);
+  if (e == cudaSuccess) e = prepare(dx_distill_kernel<float, false, 2>, smem);
+  if (e == cudaSuccess) e = prepare(dx_distill_kernel<float, false, 4>, smem);
+  if (e == cudaSuccess) e = prepare(dx_distill_kernel<__nv_bfloat16, true, 2>, smem);
+  if (e == cudaSuccess) e = prepare(dx_distill_kernel<__nv_bfloat16, true, 4>, smem);
+  if (e == cudaSuccess) e = prepare(dx_distill_kernel<__nv_bfloat16, false, 2>, smem);
+  if (e == cudaSuccess) e = prepare(dx_distill_kernel<__nv_bfloat16, false, 4>, smem);
   return e;
 }
 
@@ -645,6 +653,6 @@ cudaError_t dx_launch_distill(dx_ctx* ctx, const void* logits, int dtype, int N,
   const double c = 1.4426950408889634 / (double)temperature;
   DistillParams p{logits, N, V, k, tail, 0, ld, ld_d, teacher_ids, teacher_logprobs,
                   (float)c, (float)(c - (double)(float)c), 1.0 / (double)temperature, (float)(1.0 / (double)temperature), row_weight, loss, dlogits, ctx->dev_status};
-  if (dtype == DX_DTYPE_FP32) return dlogits ? launch<float, true>(ctx, p, st) : launch<float, false>(ctx, p, st);
-  return dlogits ? launch<__nv_bfloat16, true>(ctx, p, st) : launch<__nv_bfloat16, false>(ctx, p, st);
+  if (dtype == DX_DTYPE_FP32) return dlogits ? launch_lists<float, true>(ctx, p, st) : launch_lists<float, false>(ctx, p, st);
+  return dlogits ? launch_lists<__nv_bfloat16, true>(ctx, p, st) : launch_lists<__nv_bfloat16, false>(ctx, p, st);
 }

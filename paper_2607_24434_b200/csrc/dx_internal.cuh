@@ -92,7 +92,7 @@ struct dx_ctx {
   unsigned int* handover;      // device word {block input final}: see DxExpertParams
   float2* conf_part;           // [8 * sm_count][DX_MAX_M] per-CTA online-softmax pairs of the confidence variant
   int32_t* route_counts;       // [2 * sm_count][DX_MAX_E] experts selected per CTA of the batch routing kernel
-  DxClusterCount distill_clusters[4];   // last answers, per kernel of the distillation
+  DxClusterCount distill_clusters[8];   // last answers, per kernel of the distillation
   int32_t* scratch_i32;        // two ints the draft-token entry point parks unused outputs in
   int32_t* union_dev;          // [DX_MAX_E] union ids, [1] union count, [DX_MAX_TOPK] draft selection: what the
   int32_t* union_host;         //   cached entry points read on the host (page-locked and mapped; the routing kernel writes it)

@@ -142,8 +142,9 @@ __device__ __forceinline__ RowSplit row_split(const T* row, int V, int rank, int
   s.head = mis ? min(V, RowVec<T>::kN - mis) : 0;
   s.nvec = (V - s.head) / RowVec<T>::kN;
   s.tail = V - s.head - s.nvec * RowVec<T>::kN;
-  s.v_lo = (int)((long long)s.nvec * rank / n_ranks);
-  s.v_hi = (int)((long long)s.nvec * (rank + 1) / n_ranks);
+  const int shift = __ffs(n_ranks) - 1;   // (a power of two)
+  s.v_lo = (int)(((long long)s.nvec * rank) >> shift);
+  s.v_hi = (int)(((long long)s.nvec * (rank + 1)) >> shift);
   return s;
 }
 
