@@ -17,7 +17,7 @@
 
 namespace {
 
-constexpr int kUnroll = 2;
+constexpr int kUnroll = 4;
 constexpr float kSlack = 8.f;                     // powers of two by which an element may exceed its sum's reference
 constexpr int kStaticBytes = 4608;                // at least the kernel's static shared memory
 constexpr int kHash = 2 * DX_MAX_TEACHER;
@@ -111,7 +111,7 @@ __device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l
 
 // kLists: list entries per lane of the list's warp, at least k / 32 (its registers would not last for four where two do)
 template <typename T, bool kGrad, int kLists>
-__global__ void __launch_bounds__(kThreads, 4) dx_distill_kernel(DistillParams p, int C, int buffers) {
+__global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(DistillParams p, int C, int buffers) {
   using V16 = RowVec<T>;
   // [buffers][kRowThreads][half] 16-bit words -- bit q of a thread's words: its q-th vector holds a listed word -- and
   // behind them (kGrad) the CTA's vectors of the row
@@ -584,11 +584,11 @@ cudaError_t max_clusters(dx_ctx* ctx, int C, size_t smem, int* out) {
 
 template <typename T, bool kGrad, int kLists>
 cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
-  // CTAs per row: few enough bytes per CTA that four fit an SM (one loads while another computes or stores), and as many
+  // CTAs per row: few enough bytes per CTA that two fit an SM (one works while the other waits for its row), and as many
   // as fill the GPU when there are few rows.  (Without the gradient nothing has to fit; the same split gives the same
   // loss, bit for bit.)
   const long long bytes = (long long)p.V * (long long)sizeof(T);
-  const int slots = 4 * ctx->sm_count;
+  const int slots = 2 * ctx->sm_count;
   int C = 1;
   while (C < DX_ROW_CLUSTER_MAX &&
          (bytes > (long long)C * DX_ROW_SLICE_BYTES ||

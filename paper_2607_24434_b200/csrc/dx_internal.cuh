@@ -21,7 +21,7 @@
 #define DX_MAX_TOP 32          // alternatives per row of spec_token_logprobs
 #define DX_MAX_TEACHER 128     // teacher entries per row of spec_distill_topk
 #define DX_ROW_CLUSTER_MAX 16  // CTAs that share a row of logits
-#define DX_ROW_SLICE_BYTES 52000   // ... and the bytes of it one CTA holds when there are many rows (four CTAs per SM)
+#define DX_ROW_SLICE_BYTES 106000  // ... and the bytes of it one CTA holds when there are many rows (two CTAs per SM)
 #define DX_MAX_GROUPS 32       // expert groups of moe_route_tokens
 #define DX_ROUTE_CLUSTER 4     // CTAs (and SMs) of the routing kernel; the expert kernel leaves them free
 
