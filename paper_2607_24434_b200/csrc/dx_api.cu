@@ -46,7 +46,7 @@ extern "C" dx_status dx_create(int device, dx_ctx** out) {
   if (e == cudaSuccess) e = cudaMalloc(&ctx->handover, 4 * sizeof(unsigned int));
   if (e == cudaSuccess) e = cudaMemset(ctx->handover, 0, 4 * sizeof(unsigned int));
   if (e == cudaSuccess) e = cudaMalloc(&ctx->conf_part, sizeof(float2) * 8 * ctx->sm_count * DX_MAX_M);
-  if (e == cudaSuccess) e = cudaMalloc(&ctx->route_counts, sizeof(int32_t) * 2 * ctx->sm_count * DX_MAX_E);
+  if (e == cudaSuccess) e = cudaMalloc(&ctx->route_counts, sizeof(int32_t) * DX_ROUTE_CTAS_PER_SM * ctx->sm_count * DX_MAX_E);
   if (e == cudaSuccess) e = dx_logprobs_prepare();
   if (e == cudaSuccess) e = dx_distill_prepare(ctx);
   if (e == cudaSuccess) e = cudaMalloc(&ctx->scratch_i32, sizeof(int32_t) * 2);

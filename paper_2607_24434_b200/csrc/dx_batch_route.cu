@@ -7,15 +7,16 @@
 //   `keep` of them stay;  the k largest values among the experts left are selected, ties to the lower id
 //   gate    w_j = scale * r_j  or  scale * r_j / sum_i r_i
 //
-// The selection is that of exact arithmetic.  It is made in 32 bits first: a lane holds eight consecutive experts, their
-// values become unique integer keys (24 bits of the value's place in the token's range, then the reversed expert id),
-// which a sorting network and k + 1 rounds of a maximum over the token's lanes put in order.  Where two neighbours of
-// the result are closer than the arithmetic can tell apart (about one token in a thousand), the whole warp makes that
-// token's selection again with 64-bit scores.
+// The selection is that of exact arithmetic.  It is made on unique 32-bit keys first: a lane holds eight consecutive
+// experts, whose keys are 24 bits of the value and the reversed expert id -- with a bias the value's place between the
+// smallest and the largest that a score plus a bias can have, without one the leading bits of the logit (all of a bf16
+// logit).  A sorting network and k + 1 rounds of a maximum over the token's lanes put them in order.  Where two
+// neighbours of the result are closer than keys and arithmetic can tell apart (a few tokens in a thousand), the whole
+// warp makes that token's selection again with 64-bit scores.
 //
-// Two launches for a large batch: selection with one histogram of experts per CTA, then the permutation, every CTA
-// adding up the histograms in front of it (a stable counting sort without atomics on device memory; the order does not
-// depend on timing).  A small batch is one CTA and one launch.
+// Two launches for a large batch: selection with one histogram of experts per CTA, then the permutation, clusters of
+// CTAs adding up the histograms in front of them (a stable counting sort without atomics on device memory; the order
+// does not depend on timing).  A small batch is one CTA and one launch.
 #include "dx_internal.cuh"
 
 namespace {
@@ -23,11 +24,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kEpl = 8;           // experts per lane
-// How far the difference of two 32-bit selection values may be off, relative to the largest score + bias: expf is good
-// to 2 steps of 2^-23, the row's sum and the difference in its exponent add as much again, the quotient and the
+// How far the difference of two 32-bit selection values may be off, relative to 1 + the largest bias: exponential and
+// reciprocal of a score are good to 2^-22 and 2^-23, a softmax's sum adds as much again, the exponent's rounding and the
 // addition of the bias half a step each; less than 8e-7 per value.
 constexpr float kScoreError = 2e-6f;
-constexpr float kKeyRange = 256.f;   // values this far below the token's largest share one key
 
 struct BatchRouteParams {
   const void* logits;
@@ -102,12 +102,6 @@ template <int G>
 __device__ __forceinline__ float lanes_max(float v) {
 #pragma unroll
   for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
-template <int G>
-__device__ __forceinline__ float lanes_min(float v) {
-#pragma unroll
-  for (int o = G / 2; o > 0; o >>= 1) v = fminf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
 template <int G>
@@ -206,42 +200,53 @@ __device__ __noinline__ int select_exact(const BatchRouteParams& p, const T* row
   return mine;
 }
 
-// Where the pairs of this CTA go: base[e] = first place of expert e's pairs of this CTA.  The pairs of the CTA's tokens
-// are taken in runs of 32, a contiguous stretch of them per warp, so that equal experts keep the order of their pairs.
-__device__ __forceinline__ void place_pairs(const int32_t* ids, long long p0, int n, int E, int (*s_hist)[DX_MAX_E],
-                                            const int* s_base, int32_t* perm) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int run = (n + kWarps * 32 - 1) / (kWarps * 32) * 32;
-  const int lo = min(n, warp * run), hi = min(n, lo + run);
-  for (int e = lane; e < E; e += 32) s_hist[warp][e] = 0;
-  __syncwarp();
-  for (int i = lo; i < hi; i += 32) {
-    const int id = i + lane < hi ? ids[p0 + i + lane] : -1;
-    const unsigned int same = __match_any_sync(0xffffffffu, id);
-    if (id >= 0 && __ffs(same) - 1 == lane) s_hist[warp][id] += __popc(same);
-    __syncwarp();
-  }
-  __syncthreads();
-  for (int e = threadIdx.x; e < E; e += kThreads) {
-    int at = s_base[e];
+// Where the pairs of a CTA's tokens go: s_base[e] = first place of expert e's.  The pairs are taken kTile at a time, a
+// contiguous stretch of 32 * kDeep per warp, so that equal experts keep the order of their pairs.
+constexpr int kDeep = 4;
+constexpr int kTile = kWarps * 32 * kDeep;
+__device__ __forceinline__ void load_pairs(const int32_t* ids, long long p0, int at, int n, int (&id)[kDeep]) {
+  const int first = at + (threadIdx.x >> 5) * 32 * kDeep + (threadIdx.x & 31);
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const int c = s_hist[w][e];
-      s_hist[w][e] = at;
-      at += c;
-    }
-  }
-  __syncthreads();
-  for (int i = lo; i < hi; i += 32) {
-    const int id = i + lane < hi ? ids[p0 + i + lane] : -1;
-    const unsigned int same = __match_any_sync(0xffffffffu, id);
-    const int at = id >= 0 ? s_hist[warp][id] : 0;
+  for (int d = 0; d < kDeep; ++d) id[d] = first + 32 * d < n ? ids[p0 + first + 32 * d] : -1;
+}
+__device__ __forceinline__ void place_pairs(const int32_t* ids, long long p0, int n, int E, int (*s_hist)[DX_MAX_E],
+                                            int* s_base, int32_t* perm, int (&id)[kDeep]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll 1
+  for (int at = 0; at < n; at += kTile) {
+    if (at > 0) load_pairs(ids, p0, at, n, id);
+    for (int e = lane; e < E; e += 32) s_hist[warp][e] = 0;
     __syncwarp();
-    if (id >= 0) {
-      perm[at + __popc(same & ((1u << lane) - 1u))] = (int32_t)(p0 + i + lane);
-      if (__ffs(same) - 1 == lane) s_hist[warp][id] = at + __popc(same);
+    unsigned int same[kDeep];
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) {
+      same[d] = __match_any_sync(0xffffffffu, id[d]);
+      if (id[d] >= 0 && __ffs(same[d]) - 1 == lane) s_hist[warp][id[d]] += __popc(same[d]);
+      __syncwarp();
     }
-    __syncwarp();
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += kThreads) {
+      int x = s_base[e];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const int c = s_hist[w][e];
+        s_hist[w][e] = x;
+        x += c;
+      }
+      s_base[e] = x;
+    }
+    __syncthreads();
+    const long long first = p0 + at + warp * 32 * kDeep + lane;
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) {
+      const int x = id[d] >= 0 ? s_hist[warp][id[d]] : 0;
+      __syncwarp();
+      if (id[d] >= 0) {
+        perm[x + __popc(same[d] & ((1u << lane) - 1u))] = (int32_t)(first + 32 * d);
+        if (__ffs(same[d]) - 1 == lane) s_hist[warp][id[d]] = x + __popc(same[d]);
+      }
+      __syncwarp();
+    }
   }
 }
 
@@ -261,75 +266,126 @@ __device__ __forceinline__ int prefix_counts(int c, int* s_scan) {
   return before_warp + x - c;
 }
 
-template <typename T, int G>
-__global__ void __launch_bounds__(kThreads) dx_batch_route_kernel(BatchRouteParams p) {
+// Score as the keys see it: ex2 and rcp of the hardware, good to 2^-22 and 1 step; |z| adds |z| 2^-24 to the exponent,
+// and |z| sigmoid'(z) stays below 0.23.
+__device__ __forceinline__ float sigmoid_fast(float z) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+__device__ __forceinline__ float exp_fast(float x) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
+  return e;
+}
+
+// G lanes per token.  kScores: the selection goes by scores (a bias, or groups ranked by a sum), else by the logits.
+template <typename T, int G, bool kScores>
+__global__ void __launch_bounds__(kThreads, 3) dx_batch_route_kernel(BatchRouteParams p) {
   constexpr int kTok = 32 / G;                       // tokens a warp works on side by side
+  constexpr int kPicks = G == 4 ? 3 : G == 8 ? 2 : 1;   // picks (of k + 1) per lane
+  constexpr unsigned int kMask = G == 32 ? 0xffffffffu : (1u << (G % 32)) - 1u;
   __shared__ int s_count[DX_MAX_E];
-  __shared__ int s_hist[kWarps][DX_MAX_E];
+  __shared__ __align__(16) float s_bias[DX_MAX_E];
+  __shared__ unsigned char s_gid[DX_MAX_E];
   __shared__ int s_base[DX_MAX_E];
   __shared__ int s_scan[kWarps];
-  __shared__ double s_exact[kWarps][DX_MAX_E];
-  float* s_vals = reinterpret_cast<float*>(s_exact[threadIdx.x >> 5]);   // (the general group path stages values here)
+  __shared__ __align__(16) union {
+    double exact[kWarps][DX_MAX_E];                  // 64-bit scores of the token a warp selects again, or its values
+    int hist[kWarps][DX_MAX_E];
+  } s_mem;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % G, tok = lane / G;
   const int E = p.E, k = p.k, e0 = sub * kEpl;
   const int per = E / p.groups;
   // a group is a whole number of lanes, a power of two of them: its score comes out of a few exchanges
   const int gl = per / kEpl;
   const bool lane_groups = p.groups > 1 && per % kEpl == 0 && (gl & (gl - 1)) == 0;
-  for (int e = threadIdx.x; e < E; e += kThreads) s_count[e] = 0;
-  __syncthreads();
-
-  float b[kEpl];
-  float bmax = 0.f;
-#pragma unroll
-  for (int i = 0; i < kEpl; ++i) {
-    b[i] = p.bias && e0 + i < E ? p.bias[e0 + i] : 0.f;
-    bmax = fmaxf(bmax, fabsf(b[i]));
+  const int gl_log = lane_groups ? __ffs(gl) - 1 : 0;
+  const bool biased = kScores && p.bias != nullptr;
+  const bool softmax = p.score_fn == DX_SCORE_SOFTMAX;
+  dx_pdl_trigger();            // (the permutation waits for this kernel's end before it reads anything)
+  for (int e = threadIdx.x; e < DX_MAX_E; e += kThreads) {
+    s_count[e] = 0;
+    s_bias[e] = biased && e < E ? p.bias[e] : 0.f;
+    s_gid[e] = (unsigned char)(min(e, E - 1) / per);
   }
-  bmax = lanes_max<G>(bmax);
-  int gid[kEpl];                                     // groups of this lane's experts (general path)
+  __syncthreads();
+  // keys of biased values: their place in [least bias, 1 + greatest bias]
+  float key_mul = 0.f, key_add = 0.f, bias_abs = 0.f;
+  bool key_ok = true;
+  unsigned int near = 0;                             // keys of that many quanta or fewer apart are not told apart
+  if (biased) {
+    float lo = INFINITY, hi = -INFINITY;
+    for (int e = lane; e < E; e += 32) {
+      lo = fminf(lo, s_bias[e]);
+      hi = fmaxf(hi, s_bias[e]);
+    }
 #pragma unroll
-  for (int i = 0; i < kEpl; ++i) gid[i] = p.groups > 1 ? min(e0 + i, E - 1) / per : 0;
+    for (int o = 16; o > 0; o >>= 1) {
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    bias_abs = fmaxf(fabsf(lo), fabsf(hi));
+    key_mul = 16777000.f / (1.f + hi - lo);
+    // (8 quanta above the masked experts: key_add is rounded, by less than 4 up to the bound that follows)
+    key_add = 8.f - lo * key_mul;
+    key_ok = fabsf(key_add) < 6e7f && key_mul > 0.f;   // (infinite or far-off biases: every token is selected in 64 bits)
+    near = 4u + (unsigned int)fminf(kScoreError * (1.f + bias_abs) * key_mul, 1.6e7f);
+  }
+  float b[kEpl];
+  if (kScores) {
+#pragma unroll
+    for (int i = 0; i < kEpl; ++i) b[i] = s_bias[min(e0 + i, DX_MAX_E - 1)];
+  }
 
   const long long t_lo = (long long)blockIdx.x * p.per_cta;
   const long long t_hi = min((long long)p.N, t_lo + p.per_cta);
+#pragma unroll 1
   for (long long t0 = t_lo + warp * kTok; t0 < t_hi; t0 += kWarps * kTok) {
     const bool active = t0 + tok < t_hi;
     const long long t = active ? t0 + tok : t_hi - 1;   // (lanes without a token repeat the last one and write nothing)
     const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
-    float z[kEpl], v[kEpl];
+    float z[kEpl];                                   // logits, then values; -inf: masked (a NaN is)
     load8(row, e0, E, p.vec != 0, z);
-    // ---- scores and selection values; masked experts have value -inf
-    float m = -INFINITY, ssum = 0.f, rmax = 1.f;
-    if (p.score_fn == DX_SCORE_SOFTMAX) {
+    float m = -INFINITY, inv = 0.f;
+    bool odd = false;                                // a sum that is not a number: no score says anything
+    if (softmax && (kScores || !p.norm)) {
+      float s = 0.f, bad = 0.f;
 #pragma unroll
-      for (int i = 0; i < kEpl; ++i) m = fmaxf(m, z[i]);
+      for (int i = 0; i < kEpl; ++i) {
+        m = fmaxf(m, z[i]);
+        bad += z[i] != z[i] ? 1.f : 0.f;
+      }
       m = lanes_max<G>(m);
 #pragma unroll
-      for (int i = 0; i < kEpl; ++i) ssum += z[i] == -INFINITY ? 0.f : expf(z[i] - m);
-      ssum = lanes_sum<G>(ssum);
+      for (int i = 0; i < kEpl; ++i) s += z[i] > -INFINITY ? exp_fast(z[i] - m) : 0.f;
+      s = lanes_sum<G>(s + (bad > 0.f ? __uint_as_float(0x7fc00000u) : 0.f));
+      odd = s != s;
+      inv = s;
     }
-    const bool scores = p.bias != nullptr || (p.groups > 1 && p.group_score != DX_GROUP_MAX);
-    float rs[kEpl];
-#pragma unroll
-    for (int i = 0; i < kEpl; ++i) {
-      const bool masked = !(z[i] > -INFINITY);
-      float r = z[i];
-      if (scores) r = p.score_fn == DX_SCORE_SOFTMAX ? expf(z[i] - m) / ssum : sigmoid_f(z[i]);
-      rs[i] = masked ? -INFINITY : r + b[i];
-      v[i] = masked ? -INFINITY : p.bias ? rs[i] : z[i];
-    }
-    if (p.score_fn == DX_SCORE_SOFTMAX) rmax = 1.f / ssum;
-    bool doubt = false;
-    // ---- groups
+    bool doubt = biased && !key_ok;
     unsigned int kept = 0xffffffffu;
+    if (kScores) {
+      const float rcp = softmax ? 1.f / inv : 0.f;
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i) {
+        const bool live = z[i] > -INFINITY && !odd;
+        const float r = softmax ? exp_fast(z[i] - m) * rcp : sigmoid_fast(z[i]);
+        z[i] = live ? r + b[i] : -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i) z[i] = fmaxf(z[i], -INFINITY);
+    }
+    // ---- groups
     if (p.groups > 1) {
-      float g1 = -INFINITY, g2 = -INFINITY;            // two largest values of the group
+      float g1 = -INFINITY, g2 = -INFINITY;          // two largest values of the group
       if (lane_groups) {
 #pragma unroll
         for (int i = 0; i < kEpl; ++i) {
-          g2 = fmaxf(g2, fminf(g1, rs[i]));
-          g1 = fmaxf(g1, rs[i]);
+          g2 = fmaxf(g2, fminf(g1, z[i]));
+          g1 = fmaxf(g1, z[i]);
         }
         for (int o = 1; o < gl; o <<= 1) {
           const float o1 = __shfl_xor_sync(0xffffffffu, g1, o), o2 = __shfl_xor_sync(0xffffffffu, g2, o);
@@ -337,15 +393,16 @@ __global__ void __launch_bounds__(kThreads) dx_batch_route_kernel(BatchRoutePara
           g1 = fmaxf(g1, o1);
         }
         // lane g of the token's lanes takes group g
-        g1 = __shfl_sync(0xffffffffu, g1, tok * G + min(sub, p.groups - 1) * gl);
-        g2 = __shfl_sync(0xffffffffu, g2, tok * G + min(sub, p.groups - 1) * gl);
+        const int from = tok * G + (min(sub, p.groups - 1) << gl_log);
+        g1 = __shfl_sync(0xffffffffu, g1, from);
+        g2 = __shfl_sync(0xffffffffu, g2, from);
       } else {
-        float* stage = s_vals + tok * G * kEpl;
+        float* stage = reinterpret_cast<float*>(s_mem.exact[warp]) + tok * G * kEpl;
 #pragma unroll
-        for (int i = 0; i < kEpl; ++i) stage[e0 + i] = rs[i];
+        for (int i = 0; i < kEpl; ++i) stage[e0 + i] = z[i];
         __syncwarp();
         if (sub < p.groups) {
-          int at = sub % per;                          // (start apart: the lanes read different banks)
+          int at = sub % per;                        // (start apart: the lanes read different banks)
           for (int i = 0; i < per; ++i) {
             const float x = stage[sub * per + at];
             g2 = fmaxf(g2, fminf(g1, x));
@@ -357,47 +414,40 @@ __global__ void __launch_bounds__(kThreads) dx_batch_route_kernel(BatchRoutePara
       }
       const float gs = p.group_score == DX_GROUP_MAX || g2 == -INFINITY ? g1 : g1 + g2;
       // rank of this lane's group; neighbours at the border too close to tell apart raise the doubt
-      const float eps = scores ? 2.f * kScoreError * (rmax + bmax) : 0.f;
+      const float eps = kScores ? 2.f * kScoreError * (1.f + bias_abs) : 0.f;
       int r = 0;
       bool close = false;
       for (int g = 0; g < p.groups; ++g) {
         const float o = __shfl_sync(0xffffffffu, gs, tok * G + g);
         r += o > gs || (o == gs && g < sub);
-        close |= g != sub && fabsf(o - gs) <= eps && finite_f(o) && finite_f(gs);
+        close |= g != sub && fabsf(o - gs) <= eps;   // (infinite on both sides: not a number, not close)
       }
       const bool in = sub < p.groups;
-      const unsigned int mask = (G == 32 ? 0xffffffffu : ((1u << G) - 1u)) << (tok * G);
-      kept = (__ballot_sync(0xffffffffu, in && r < p.keep) & mask) >> (tok * G);
-      const bool border = in && close && scores && p.keep < p.groups && (r == p.keep - 1 || r == p.keep);
-      doubt = (__ballot_sync(0xffffffffu, border) & mask) != 0;
+      kept = __ballot_sync(0xffffffffu, in && r < p.keep) >> (tok * G) & kMask;
+      doubt |= (__ballot_sync(0xffffffffu, kScores && in && close && (r == p.keep - 1 || r == p.keep)) >> (tok * G) & kMask) != 0;
     }
-    // ---- unique keys: 24 bits of the value within the token's range, then the reversed id
-    float lo = INFINITY, hi = -INFINITY;
-    const int e_id = e0;
+    if (kScores && !biased) {                        // (the scores were for the groups; experts go by their logits)
+      load8(row, e0, E, p.vec != 0, z);
 #pragma unroll
-    for (int i = 0; i < kEpl; ++i) {
-      if (finite_f(v[i])) {
-        lo = fminf(lo, v[i]);
-        hi = fmaxf(hi, v[i]);
-      }
+      for (int i = 0; i < kEpl; ++i) z[i] = fmaxf(z[i], -INFINITY);
     }
-    hi = lanes_max<G>(hi);
-    lo = fmaxf(lanes_min<G>(lo), hi - kKeyRange);
-    const float span = hi - lo;
-    const float quanta = span > 0.f ? 16777000.f / span : 0.f;
-    doubt |= hi > lo && !finite_f(quanta);             // (a range too narrow for the factor: the keys say nothing)
+    // ---- unique keys; 0: excluded or no expert
     unsigned int key[kEpl];
 #pragma unroll
     for (int i = 0; i < kEpl; ++i) {
-      const int e = e_id + i;
-      unsigned int q = 1;                              // masked
-      if (v[i] > -INFINITY) q = v[i] == INFINITY ? 0xffffffu : 2u + (unsigned int)fminf(fmaxf((v[i] - lo) * quanta, 0.f), 16777000.f);
-      if (p.groups > 1) {
-        const int g = lane_groups ? sub / gl : gid[i];
-        if (!(kept >> g & 1u)) q = 0;
+      unsigned int q;
+      if (biased) {
+        const float f = fmaf(z[i], key_mul, key_add);   // (not a number, or below: masked)
+        q = min(max((unsigned int)__float2uint_rz(f), 1u), 0xffffffu) << 8;
+      } else {
+        q = dx_orderable(z[i] + 0.f) & 0xffffff00u;
       }
-      key[i] = e < E ? (q << 8 | (unsigned int)(255 - e)) : 0u;
-      if (q == 0) key[i] = 0;                          // excluded: never selected
+      key[i] = q | (unsigned int)(255 - e0 - i);
+      if (e0 + i >= E) key[i] = 0;
+      if (p.groups > 1) {
+        const int g = lane_groups ? sub >> gl_log : s_gid[min(e0 + i, DX_MAX_E - 1)];
+        if (!(kept >> g & 1u)) key[i] = 0;
+      }
     }
     // ---- the lane's keys in descending order (19 exchanges)
 #define DX_EXCHANGE(a, c) { const unsigned int hi_ = max(key[a], key[c]), lo_ = min(key[a], key[c]); key[a] = hi_; key[c] = lo_; }
@@ -409,89 +459,109 @@ __global__ void __launch_bounds__(kThreads) dx_batch_route_kernel(BatchRoutePara
     DX_EXCHANGE(2, 4) DX_EXCHANGE(3, 5)
     DX_EXCHANGE(3, 4)
 #undef DX_EXCHANGE
-    // ---- k + 1 rounds: lane j of the token's lanes gets the j-th key (a token of four lanes keeps two apiece)
-    unsigned int mine = 0, mine2 = 0, mine3 = 0;
-    for (int j = 0; j <= k; ++j) {
-      const unsigned int top = lanes_umax<G>(key[0]);
-      const bool won = key[0] == top && top != 0;
+    // ---- k + 1 rounds: lane j of the token's lanes keeps pick j (j + G, j + 2 G)
+    unsigned int pick[kPicks] = {};
 #pragma unroll
-      for (int i = 0; i < kEpl - 1; ++i) key[i] = won ? key[i + 1] : key[i];
-      key[kEpl - 1] = won ? 0 : key[kEpl - 1];
-      if (j % G == sub) {
-        if (j < G) mine = top;
-        else if (j < 2 * G) mine2 = top;
-        else mine3 = top;
+    for (int j = 0; j <= DX_MAX_TOPK; ++j) {
+      if (j <= k) {
+        const unsigned int top = lanes_umax<G>(key[0]);
+        if (sub == j % G) pick[j / G] = top;
+        const bool won = key[0] == top;
+#pragma unroll
+        for (int i = 0; i < kEpl - 1; ++i) key[i] = won ? key[i + 1] : key[i];
+        key[kEpl - 1] = won ? 0u : key[kEpl - 1];
       }
     }
-    // ---- neighbours too close for 32 bits (equal logits and biases are a true tie, in the right order already)
-    const float slack = p.bias ? kScoreError * (rmax + bmax) * quanta : 0.f;
-    const unsigned int near = 4u + (unsigned int)fminf(slack, 1.6e7f);
+    // ---- the picks' logits, and neighbours that 32 bits cannot tell apart
+    int id[kPicks];
+    float x[kPicks];
+    bool close = false;
 #pragma unroll
-    for (int h = 0; h < (G == 4 ? 3 : G == 8 ? 2 : 1); ++h) {
-      const unsigned int a = h == 0 ? mine : h == 1 ? mine2 : mine3;
-      const unsigned int up = __shfl_sync(0xffffffffu, h == 0 ? mine : h == 1 ? mine2 : mine3, tok * G + (sub + 1) % G);
-      const unsigned int wrap = __shfl_sync(0xffffffffu, h == 0 ? mine2 : h == 1 ? mine3 : 0u, tok * G);
-      const unsigned int c = sub == G - 1 ? wrap : up;
-      const int j = h * G + sub;                       // neighbours j and j + 1
-      bool close = j < k && a != 0 && c != 0 && (a >> 8) >= 2u && (c >> 8) >= 2u && (a >> 8) - (c >> 8) <= near;
-      if (close && j + 1 < k) {
-        const int ea = 255 - (int)(a & 255u), ec = 255 - (int)(c & 255u);
-        const float za = to_f(row[ea]), zc = to_f(row[ec]);
-        if (za == zc && (!p.bias || p.bias[ea] == p.bias[ec])) close = false;
-      }
-      const unsigned int mask = (G == 32 ? 0xffffffffu : ((1u << G) - 1u)) << (tok * G);
-      doubt |= (__ballot_sync(0xffffffffu, close) & mask) != 0;
+    for (int h = 0; h < kPicks; ++h) {
+      id[h] = 255 - (int)(pick[h] & 255u);
+      x[h] = h * G + sub <= k && pick[h] != 0 ? to_f(row[id[h]]) : -INFINITY;
     }
-    int id0 = 255 - (int)(mine & 255u), id1 = 255 - (int)(mine2 & 255u);
+#pragma unroll
+    for (int h = 0; h < kPicks; ++h) {
+      const int src = tok * G + (sub + 1) % G;
+      unsigned int below = __shfl_sync(0xffffffffu, pick[h], src);
+      float xb = __shfl_sync(0xffffffffu, x[h], src);
+      if (h + 1 < kPicks) {                          // (the last lane's neighbour is the first lane's next pick)
+        const unsigned int w = __shfl_sync(0xffffffffu, pick[h + 1 < kPicks ? h + 1 : h], tok * G);
+        const float xw = __shfl_sync(0xffffffffu, x[h + 1 < kPicks ? h + 1 : h], tok * G);
+        if (sub == G - 1) {
+          below = w;
+          xb = xw;
+        }
+      }
+      const int j = h * G + sub;                     // neighbours j and j + 1 (j + 1 == k: the first that is left out)
+      if (j < k && below != 0 && x[h] > -INFINITY && xb > -INFINITY && (pick[h] >> 8) - (below >> 8) <= near) {
+        // equal logits under equal biases are a true tie, in the right order already -- but at the border only if equal
+        // keys are equal logits
+        bool tie = x[h] == xb;
+        if (biased) tie = tie && s_bias[id[h]] == s_bias[255 - (int)(below & 255u)];
+        if (j + 1 == k) tie = tie && !biased && sizeof(T) == 2;
+        close |= !tie;
+      }
+    }
+    doubt |= (__ballot_sync(0xffffffffu, close) >> (tok * G) & kMask) != 0;
     unsigned int redo = __ballot_sync(0xffffffffu, doubt);
-    for (int q = 0; q < kTok; ++q) {
-      if (!(redo >> (q * G) & 1u)) continue;           // (the same for the whole warp)
-      const long long tq = min(t0 + q, t_hi - 1);
-      const T* rq = reinterpret_cast<const T*>(p.logits) + (size_t)tq * (size_t)p.ld;
-      const int got = select_exact(p, rq, s_exact[warp]);
-      const int x0 = __shfl_sync(0xffffffffu, got, sub), x1 = __shfl_sync(0xffffffffu, got, (sub + G) % 32);
-      if (tok == q) {
-        id0 = x0;
-        id1 = x1;
+    if (redo != 0) {
+#pragma unroll 1
+      for (int q = 0; q < kTok; ++q) {
+        if (!(redo >> (q * G) & 1u)) continue;       // (the same for the whole warp)
+        const long long tq = min(t0 + q, t_hi - 1);
+        const T* rq = reinterpret_cast<const T*>(p.logits) + (size_t)tq * (size_t)p.ld;
+        const int got = select_exact(p, rq, s_mem.exact[warp]);
+#pragma unroll
+        for (int h = 0; h < kPicks; ++h) {
+          const int y = __shfl_sync(0xffffffffu, got, (sub + h * G) % 32);
+          if (tok == q && h * G + sub < k) {
+            id[h] = y;
+            x[h] = to_f(row[y]);
+          }
+        }
       }
     }
     // ---- gate weights of the selected experts
-    const bool on0 = sub < k, on1 = G < DX_MAX_TOPK && sub + G < k;
-    const float x0 = on0 ? to_f(row[id0]) : -INFINITY, x1 = on1 ? to_f(row[id1]) : -INFINITY;
-    auto gate = [&](float x, float top) {   // e^{x - top}: renormalised softmax gates need nothing else of the row
-      return x == -INFINITY ? 0.f : expf(x - top);
-    };
-    float w0, w1, sum = 1.f;
-    if (p.norm) {
-      const float top = lanes_max<G>(fmaxf(x0, x1));
-      if (p.score_fn == DX_SCORE_SOFTMAX) {
-        w0 = gate(x0, top);
-        w1 = gate(x1, top);
-      } else {
-        // (sigmoid(x) is e^x to 32 bits where it is this small: the ratio survives the underflow)
-        w0 = top < -64.f ? gate(x0, top) : x0 == -INFINITY ? 0.f : sigmoid_f(x0);
-        w1 = top < -64.f ? gate(x1, top) : x1 == -INFINITY ? 0.f : sigmoid_f(x1);
-      }
-      sum = lanes_sum<G>(w0 + w1);
-    } else if (p.score_fn == DX_SCORE_SOFTMAX) {
-      w0 = gate(x0, m) / ssum;
-      w1 = gate(x1, m) / ssum;
-      if (m == -INFINITY) w0 = w1 = 0.f;
-    } else {
-      w0 = x0 == -INFINITY ? 0.f : sigmoid_f(x0);
-      w1 = x1 == -INFINITY ? 0.f : sigmoid_f(x1);
+    constexpr int kH = G < DX_MAX_TOPK ? 2 : 1;      // pairs per lane
+    float w[kH], top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < kH; ++h) {
+      if (h * G + sub >= k) x[h] = -INFINITY;
+      top = fmaxf(top, x[h]);
     }
-    const float f = sum > 0.f || sum != sum ? p.scale / sum : 0.f;
-    if (active) {
-      if (on0) {
-        p.topk_ids[t * k + sub] = id0;
-        p.topk_w[t * k + sub] = w0 * f;
-        atomicAdd(&s_count[id0], 1);
-      }
-      if (on1) {
-        p.topk_ids[t * k + sub + G] = id1;
-        p.topk_w[t * k + sub + G] = w1 * f;
-        atomicAdd(&s_count[id1], 1);
+    if (p.norm) top = lanes_max<G>(top);
+#pragma unroll
+    for (int h = 0; h < kH; ++h) {
+      // Renormalised gates are ratios: softmax needs no more of the row than e^{x - top}, and sigmoid(x) is e^x to 32
+      // bits where it is small enough to underflow.
+      const bool ratio = p.norm && (softmax || top < -64.f);
+      const float ref = softmax || ratio ? (p.norm ? top : m) : 0.f;
+      const float e = expf(softmax || ratio ? x[h] - ref : -x[h]);
+      w[h] = x[h] == -INFINITY ? 0.f : softmax || ratio ? e : 1.f / (1.f + e);
+      sum += w[h];
+    }
+    float f = p.scale;
+    if (p.norm) {
+      sum = lanes_sum<G>(sum);
+      f = sum > 0.f || sum != sum ? p.scale / sum : 0.f;
+    } else if (softmax) {
+      // (the keys' fast sum is not good enough for the gates)
+      float z8[kEpl], s = 0.f;
+      load8(row, e0, E, p.vec != 0, z8);
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i) s += z8[i] == -INFINITY ? 0.f : expf(z8[i] - m);
+      s = lanes_sum<G>(s);
+      f = s > 0.f || s != s ? p.scale / s : 0.f;
+    }
+#pragma unroll
+    for (int h = 0; h < kH; ++h) {
+      const int j = h * G + sub;
+      if (active && j < k) {
+        p.topk_ids[t * k + j] = id[h];
+        p.topk_w[t * k + j] = w[h] * f;
+        atomicAdd(&s_count[id[h]], 1);
       }
     }
   }
@@ -510,7 +580,9 @@ __global__ void __launch_bounds__(kThreads) dx_batch_route_kernel(BatchRoutePara
   }
   if (threadIdx.x == 0) p.offsets[E] = p.N * k;
   __syncthreads();
-  place_pairs(p.topk_ids, 0, p.N * k, E, s_hist, s_base, p.perm);
+  int id[kDeep];
+  load_pairs(p.topk_ids, 0, 0, p.N * k, id);
+  place_pairs(p.topk_ids, 0, p.N * k, E, s_mem.hist, s_base, p.perm, id);
 }
 
 // Clusters of kPermCluster CTAs share the sums over the histograms: CTA r of a cluster adds up every kPermCluster-th part
@@ -523,6 +595,12 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
   __shared__ int2 s_part[DX_MAX_E];
   const int E = p.E, e = threadIdx.x;
   const int rank = blockIdx.x % kPermCluster, first = blockIdx.x - rank;   // (clusters are runs of the grid)
+  const long long t_lo = (long long)blockIdx.x * p.per_cta;
+  const long long t_hi = min((long long)p.N, t_lo + p.per_cta);
+  const int n = t_lo < t_hi ? (int)(t_hi - t_lo) * p.k : 0;
+  dx_pdl_wait();               // (launched while the selection drains)
+  int id[kDeep];
+  load_pairs(p.topk_ids, t_lo * p.k, 0, n, id);
   const int32_t* col = p.counts + e;
   int front = 0, total = 0;
   if (e < E) {
@@ -560,9 +638,7 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
   }
   if (blockIdx.x == 0 && e == 0) p.offsets[E] = p.N * p.k;
   __syncthreads();
-  const long long t_lo = (long long)blockIdx.x * p.per_cta;
-  const long long t_hi = min((long long)p.N, t_lo + p.per_cta);
-  if (t_lo < t_hi) place_pairs(p.topk_ids, t_lo * p.k, (int)(t_hi - t_lo) * p.k, E, s_hist, s_base, p.perm);
+  place_pairs(p.topk_ids, t_lo * p.k, n, E, s_hist, s_base, p.perm, id);
   __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -587,106 +663,150 @@ struct RouteGradParams {
   int32_t* dev_status;
 };
 
+// A pair of a token: lane j of the token's lanes holds pair j (id -1: none).
+struct Pair {
+  int id;
+  float g, x;                 // gradient of the gate, logit
+};
+template <typename T>
+__device__ __forceinline__ Pair load_pair(const RouteGradParams& p, long long t, const T* row, int j) {
+  Pair q{-1, 0.f, -INFINITY};
+  if (j < p.k) {
+    q.id = p.ids[t * p.k + j];
+    q.g = p.dw[t * p.k + j] * p.scale;
+    if (q.id < 0 || q.id >= p.E) {
+      *p.dev_status = DX_DEV_BAD_EXPERT_ID;
+      q.id = -1;
+      q.g = 0.f;
+    } else {
+      q.x = to_f(row[q.id]);
+    }
+  }
+  return q;
+}
+// an expert listed twice gets the sum of its pairs' gradients (`tok`: the token's place in the warp)
+template <int G>
+__device__ __forceinline__ float sum_duplicates(int id, float g, int tok, int k) {
+  const unsigned int same = __match_any_sync(0xffffffffu, id < 0 ? -1 - (int)(threadIdx.x & 31) : tok << 16 | id);
+  float both = g;
+  if (__any_sync(0xffffffffu, __popc(same) > 1)) {
+    both = 0.f;
+    for (int j = 0; j < k; ++j) {
+      const int src = tok * G + j;
+      const float og = __shfl_sync(0xffffffffu, g, src);
+      if (same >> src & 1u) both += og;
+    }
+  }
+  return both;
+}
+
+// Gradients that are zero outside the selection: a warp takes four tokens, eight lanes for the pairs of each, writes
+// the zeros of their rows with all lanes and then the selected experts' places.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dx_route_grad_sparse_kernel(RouteGradParams p) {
+  constexpr int G = DX_MAX_TOPK, kTok = 32 / G, kN = 16 / sizeof(T);
+  const int lane = threadIdx.x & 31, sub = lane % G, tok = lane / G;
+  const int E = p.E;
+  const bool softmax = p.score_fn == DX_SCORE_SOFTMAX;
+  const long long warps = (long long)gridDim.x * kWarps;
+#pragma unroll 1
+  for (long long t0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kTok; t0 < p.N; t0 += warps * kTok) {
+    const bool active = t0 + tok < p.N;
+    const long long t = active ? t0 + tok : p.N - 1;
+    const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
+    T* out0 = reinterpret_cast<T*>(p.dlogits) + (size_t)t0 * (size_t)p.ld_d;
+    const int rows = (int)min((long long)kTok, p.N - t0);
+    // the pairs' loads are on their way while the zeros are written
+    const Pair q = load_pair(p, t, row, sub);
+    for (int r = 0; r < rows; ++r) {
+      T* out = out0 + (size_t)r * (size_t)p.ld_d;
+      if (p.vec_out) {
+        for (int e = lane * kN; e + kN <= E; e += 32 * kN) *reinterpret_cast<uint4*>(out + e) = make_uint4(0, 0, 0, 0);
+        if (lane < E % kN) store1(out + E - E % kN + lane, 0.f);
+      } else {
+        for (int e = lane; e < E; e += 32) store1(out + e, 0.f);
+      }
+    }
+    const float top = lanes_max<G>(q.x);
+    // renormalised gates: a common factor of the scores cancels (e^{x - top} for softmax; sigmoid(x) is e^x where it is
+    // small)
+    const bool ratio = softmax || (p.norm && top < -64.f);
+    const float e = expf(ratio ? q.x - top : -q.x);
+    const float r = q.x == -INFINITY ? 0.f : ratio ? e : 1.f / (1.f + e);
+    const float slope = softmax ? 1.f : sigmoid_f(-q.x);             // 1 - sigmoid
+    float g = q.g;
+    if (p.norm) {
+      const float S = lanes_sum<G>(r);
+      const float mean = lanes_sum<G>(g * r) / S;
+      g = S == 0.f || q.id < 0 ? 0.f : (g - mean) / S;
+    }
+    const float both = sum_duplicates<G>(q.id, g, tok, p.k);
+    __syncwarp();                                      // the zeros are written before the selected experts' places are
+    if (active && q.id >= 0)
+      store1(reinterpret_cast<T*>(p.dlogits) + (size_t)t * (size_t)p.ld_d + q.id, both * r * slope);
+    __syncwarp();
+  }
+}
+
+// Softmax gates that are not renormalised: every expert's logit has a gradient.  G lanes per token, at least eight.
 template <typename T, int G>
-__global__ void __launch_bounds__(kThreads) dx_route_grad_kernel(RouteGradParams p) {
+__global__ void __launch_bounds__(kThreads) dx_route_grad_dense_kernel(RouteGradParams p) {
   constexpr int kTok = 32 / G;
   const int lane = threadIdx.x & 31, sub = lane % G, tok = lane / G;
-  const int E = p.E, k = p.k, e0 = sub * kEpl;
+  const int E = p.E, e0 = sub * kEpl;
   const long long warps = (long long)gridDim.x * kWarps;
+#pragma unroll 1
   for (long long t0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kTok; t0 < p.N; t0 += warps * kTok) {
     const bool active = t0 + tok < p.N;
     const long long t = active ? t0 + tok : p.N - 1;
     const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
     T* out = reinterpret_cast<T*>(p.dlogits) + (size_t)t * (size_t)p.ld_d;
-    // the pairs of the token: lane j of its lanes takes pair j (a token of four lanes two apiece)
-    int id[2];
-    float g[2], x[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int j = sub + h * G;
-      const bool on = j < k && (h == 0 || G < DX_MAX_TOPK);
-      id[h] = on ? p.ids[t * k + j] : -1;
-      g[h] = on ? p.dw[t * k + j] * p.scale : 0.f;
-      if (on && (id[h] < 0 || id[h] >= E)) {
-        *p.dev_status = DX_DEV_BAD_EXPERT_ID;
-        id[h] = -1;
-        g[h] = 0.f;
-      }
-      x[h] = id[h] >= 0 ? to_f(row[id[h]]) : -INFINITY;
-    }
-    const bool dense = p.score_fn == DX_SCORE_SOFTMAX && !p.norm;
     float d[kEpl];
-    float r[2], slope[2] = {1.f, 1.f};                 // scores of the pairs; sigmoid: 1 - r
-    float dot = 0.f;
-    if (dense) {
-      float m = -INFINITY, s = 0.f;
-      load8(row, e0, E, p.vec_in != 0, d);
+    load8(row, e0, E, p.vec_in != 0, d);
+    const Pair q = load_pair(p, t, row, sub);
+    float m = d[0], s = 0.f;
 #pragma unroll
-      for (int i = 0; i < kEpl; ++i) m = fmaxf(m, d[i]);
-      m = lanes_max<G>(m);
+    for (int i = 1; i < kEpl; ++i) m = fmaxf(m, d[i]);
+    m = lanes_max<G>(m);
 #pragma unroll
-      for (int i = 0; i < kEpl; ++i) {
-        d[i] = d[i] == -INFINITY ? 0.f : expf(d[i] - m);
-        s += d[i];
-      }
-      s = lanes_sum<G>(s);
-      const float inv = s == 0.f ? 0.f : 1.f / s;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) r[h] = x[h] == -INFINITY ? 0.f : expf(x[h] - m) * inv;
-      dot = lanes_sum<G>(g[0] * r[0] + g[1] * r[1]);
-#pragma unroll
-      for (int i = 0; i < kEpl; ++i) d[i] *= -inv * dot;
-    } else {
-      const float top = lanes_max<G>(fmaxf(x[0], x[1]));
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // renormalised gates: a common factor of the scores cancels (e^{x - top} for softmax; sigmoid(x) is e^x where
-        // it is small)
-        const bool ratio = p.score_fn == DX_SCORE_SOFTMAX || (p.norm && top < -64.f);
-        r[h] = x[h] == -INFINITY ? 0.f : ratio ? expf(x[h] - top) : sigmoid_f(x[h]);
-        if (p.score_fn != DX_SCORE_SOFTMAX) slope[h] = sigmoid_f(-x[h]);
-      }
-      if (p.norm) {
-        const float S = lanes_sum<G>(r[0] + r[1]);
-        const float mean = lanes_sum<G>(g[0] * r[0] + g[1] * r[1]) / S;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) g[h] = S == 0.f || id[h] < 0 ? 0.f : (g[h] - mean) / S;
-      }
-#pragma unroll
-      for (int i = 0; i < kEpl; ++i) d[i] = 0.f;
+    for (int i = 0; i < kEpl; ++i) {
+      d[i] = d[i] == -INFINITY ? 0.f : expf(d[i] - m);
+      s += d[i];
     }
-    // an expert listed twice gets the sum of its pairs' gradients
-    float both[2] = {0.f, 0.f};
-    for (int j = 0; j < k; ++j) {
-      const int src = tok * G + j % G;
-      const int oi = __shfl_sync(0xffffffffu, j < G ? id[0] : id[1], src);
-      const float og = __shfl_sync(0xffffffffu, j < G ? g[0] : g[1], src);
+    s = lanes_sum<G>(s);
+    const float inv = s == 0.f ? 0.f : 1.f / s;
+    const float r = q.x == -INFINITY ? 0.f : expf(q.x - m) * inv;
+    const float dot = lanes_sum<G>(q.g * r);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) both[h] += oi == id[h] ? og : 0.f;
-    }
+    for (int i = 0; i < kEpl; ++i) d[i] *= -inv * dot;
+    const float both = sum_duplicates<G>(q.id, q.g, tok, p.k);
     if (active) store8(out, e0, E, p.vec_out != 0, d);
     __syncwarp();                                      // the row is written before the selected experts' places are
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (active && id[h] >= 0)
-        store1(out + id[h], r[h] * (both[h] - dot) * slope[h]);
+    if (active && q.id >= 0) store1(out + q.id, r * (both - dot));
+    __syncwarp();
   }
 }
 
-template <typename T>
+template <typename T, bool kScores>
 cudaError_t launch_route(int grid, const BatchRouteParams& p, cudaStream_t st) {
-  if (p.E <= 4 * kEpl && p.groups <= 4) dx_batch_route_kernel<T, 4><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 8 * kEpl && p.groups <= 8) dx_batch_route_kernel<T, 8><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 16 * kEpl && p.groups <= 16) dx_batch_route_kernel<T, 16><<<grid, kThreads, 0, st>>>(p);
-  else dx_batch_route_kernel<T, 32><<<grid, kThreads, 0, st>>>(p);
+  if (p.E <= 4 * kEpl && p.groups <= 4) dx_batch_route_kernel<T, 4, kScores><<<grid, kThreads, 0, st>>>(p);
+  else if (p.E <= 8 * kEpl && p.groups <= 8) dx_batch_route_kernel<T, 8, kScores><<<grid, kThreads, 0, st>>>(p);
+  else if (p.E <= 16 * kEpl && p.groups <= 16) dx_batch_route_kernel<T, 16, kScores><<<grid, kThreads, 0, st>>>(p);
+  else dx_batch_route_kernel<T, 32, kScores><<<grid, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 template <typename T>
+cudaError_t launch_route(int grid, const BatchRouteParams& p, cudaStream_t st) {
+  // (the logits stand for the scores wherever only their order counts)
+  const bool scores = p.bias != nullptr || (p.groups > 1 && p.group_score != DX_GROUP_MAX);
+  return scores ? launch_route<T, true>(grid, p, st) : launch_route<T, false>(grid, p, st);
+}
+template <typename T>
 cudaError_t launch_grad(int grid, const RouteGradParams& p, cudaStream_t st) {
-  if (p.E <= 4 * kEpl) dx_route_grad_kernel<T, 4><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 8 * kEpl) dx_route_grad_kernel<T, 8><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 16 * kEpl) dx_route_grad_kernel<T, 16><<<grid, kThreads, 0, st>>>(p);
-  else dx_route_grad_kernel<T, 32><<<grid, kThreads, 0, st>>>(p);
+  if (p.score_fn != DX_SCORE_SOFTMAX || p.norm) dx_route_grad_sparse_kernel<T><<<grid, kThreads, 0, st>>>(p);
+  else if (p.E <= 8 * kEpl) dx_route_grad_dense_kernel<T, 8><<<grid, kThreads, 0, st>>>(p);
+  else if (p.E <= 16 * kEpl) dx_route_grad_dense_kernel<T, 16><<<grid, kThreads, 0, st>>>(p);
+  else dx_route_grad_dense_kernel<T, 32><<<grid, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 bool rows_aligned(const void* base, long long ld, int elem) {
@@ -709,8 +829,8 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
   p.vec = rows_aligned(logits, ld, elem) ? 1 : 0;
   p.topk_ids = topk_ids; p.topk_w = topk_w; p.offsets = offsets; p.perm = perm;
   p.counts = ctx->route_counts;
-  // one CTA up to 64 tokens (a second launch would cost more than the work), else at most two per SM
-  const int max_ctas = 2 * ctx->sm_count;
+  // one CTA up to 64 tokens (a second launch would cost more than the work), else at most three per SM
+  const int max_ctas = DX_ROUTE_CTAS_PER_SM * ctx->sm_count;
   int grid = N <= 64 ? 1 : (N + 31) / 32;
   if (grid > max_ctas) grid = max_ctas;
   p.per_cta = (N + grid - 1) / grid;
@@ -719,7 +839,7 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
   *n_launches = 1;
   if (e == cudaSuccess && perm && grid > 1) {
     const unsigned int padded = (unsigned)((grid + kPermCluster - 1) / kPermCluster * kPermCluster);
-    e = dx_launch_pdl(false, dx_batch_permute_kernel, dim3(padded), dim3(kThreads), 0, st, kPermCluster, p, grid);
+    e = dx_launch_pdl((ctx->pdl_mask & DX_PDL_ROUTE) != 0, dx_batch_permute_kernel, dim3(padded), dim3(kThreads), 0, st, kPermCluster, p, grid);
     *n_launches = 2;
   }
   return e;

@@ -23,6 +23,7 @@
 #define DX_ROW_CLUSTER_MAX 16  // CTAs that share a row of logits
 #define DX_ROW_SLICE_BYTES 106000  // ... and the bytes of it one CTA holds when there are many rows (two CTAs per SM)
 #define DX_MAX_GROUPS 32       // expert groups of moe_route_tokens
+#define DX_ROUTE_CTAS_PER_SM 3 // of its selection kernel
 #define DX_ROUTE_CLUSTER 4     // CTAs (and SMs) of the routing kernel; the expert kernel leaves them free
 
 // What the routing kernel hands to the expert kernels.  The routing-independent groups (shared experts, draft
@@ -91,7 +92,7 @@ struct dx_ctx {
   int32_t* dev_status;
   unsigned int* handover;      // device word {block input final}: see DxExpertParams
   float2* conf_part;           // [8 * sm_count][DX_MAX_M] per-CTA online-softmax pairs of the confidence variant
-  int32_t* route_counts;       // [2 * sm_count][DX_MAX_E] experts selected per CTA of the batch routing kernel
+  int32_t* route_counts;       // [DX_ROUTE_CTAS_PER_SM * sm_count][DX_MAX_E] experts selected per CTA of the batch routing kernel
   DxClusterCount distill_clusters[8];   // last answers, per kernel of the distillation
   int32_t* scratch_i32;        // two ints the draft-token entry point parks unused outputs in
   int32_t* union_dev;          // [DX_MAX_E] union ids, [1] union count, [DX_MAX_TOPK] draft selection: what the
