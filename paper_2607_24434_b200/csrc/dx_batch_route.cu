@@ -21,7 +21,7 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kEpl = 8;           // experts per lane
 // How far the difference of two 32-bit selection values may be off, relative to 1 + the largest bias: exponential and
@@ -121,50 +121,69 @@ __device__ __forceinline__ unsigned int lanes_umax(unsigned int v) {
 __device__ __forceinline__ bool finite_f(float x) { return fabsf(x) <= 3.402823466e38f; }
 __device__ __forceinline__ float sigmoid_f(float z) { return 1.f / (1.f + expf(-z)); }
 
-// (value, expert) in the order of selection: larger value first, then the lower expert; masked experts (value -inf)
-// behind all others, excluded ones (expert -1) never
-struct Pick {
-  double v;
-  int e;
-};
-__device__ __forceinline__ bool before(const Pick& a, const Pick& b) {
-  if (a.e < 0 || b.e < 0) return b.e < 0 && a.e >= 0;
-  return a.v > b.v || (a.v == b.v && a.e < b.e);
+// Larger double -> larger integer; -inf (masked experts) -> 1 or more, 0 is left for what is excluded.
+__device__ __forceinline__ unsigned long long orderable64(double v) {
+  const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
+  return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-// The selection of one token in 64 bits by a whole warp (lane j < k + 1 ... receives the j-th id in `mine`).
-// s_row: E doubles of the warp.
+// The selection of one token in 64 bits by a whole warp: lane j < k returns the j-th id.  s_row: E doubles of the warp.
+// A lane has the experts lane, lane + 32, ...; what depends on nothing else is done for all eight side by side (64-bit
+// arithmetic has long latencies, and a kernel ends with the last token that comes here).
 template <typename T>
 __device__ __noinline__ int select_exact(const BatchRouteParams& p, const T* row, double* s_row) {
   const int lane = threadIdx.x & 31;
-  double m = -INFINITY, s = 0.0;
   const bool scores = p.bias != nullptr || (p.groups > 1 && p.group_score != DX_GROUP_MAX);
-  if (p.score_fn == DX_SCORE_SOFTMAX && scores) {
-    for (int e = lane; e < p.E; e += 32) m = fmax(m, (double)to_f(row[e]));
-    for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (m > -INFINITY)
-      for (int e = lane; e < p.E; e += 32) s += exp((double)to_f(row[e]) - m);
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  float z[kEpl];
+  double v[kEpl];                                    // selection values; -inf: masked
+#pragma unroll
+  for (int i = 0; i < kEpl; ++i) {
+    const int e = lane + 32 * i;
+    z[i] = e < p.E ? to_f(row[e]) : -INFINITY;
+    v[i] = (double)z[i];
   }
-  auto score = [&](int e) {   // -inf marks a masked expert
-    const double z = (double)to_f(row[e]);
-    if (!(z > -INFINITY)) return (double)-INFINITY;
-    double r = z;
-    if (scores) r = p.score_fn == DX_SCORE_SOFTMAX ? exp(z - m) / s : 1.0 / (1.0 + exp(-z));
-    if (p.bias) r += (double)p.bias[e];
-    return r == r ? r : (double)-INFINITY;
-  };
-  for (int e = lane; e < p.E; e += 32) s_row[e] = score(e);
-  __syncwarp();
+  if (scores) {
+    double m = -INFINITY, s = 1.0;
+    if (p.score_fn == DX_SCORE_SOFTMAX) {
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i) m = fmax(m, v[i]);
+      for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
+      if (m == -INFINITY) m = 0.0;
+    }
+#pragma unroll
+    for (int i = 0; i < kEpl; ++i) v[i] = exp(p.score_fn == DX_SCORE_SOFTMAX ? v[i] - m : -v[i]);
+    if (p.score_fn == DX_SCORE_SOFTMAX) {
+      s = 0.0;
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i) s += lane + 32 * i < p.E ? v[i] : 0.0;
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    }
+#pragma unroll
+    for (int i = 0; i < kEpl; ++i) {
+      const int e = lane + 32 * i;
+      v[i] = p.score_fn == DX_SCORE_SOFTMAX ? v[i] / s : 1.0 / (1.0 + v[i]);
+      if (p.bias && e < p.E) v[i] += (double)p.bias[e];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kEpl; ++i)
+    if (!(z[i] > -INFINITY) || !(v[i] == v[i])) v[i] = -INFINITY;   // (nothing that is not a number is compared)
   unsigned int kept = 0xffffffffu;
   const int per = p.E / p.groups;
   if (p.groups > 1) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kEpl; ++i)
+      if (lane + 32 * i < p.E) s_row[lane + 32 * i] = v[i];
+    __syncwarp();
     double a = -INFINITY, b = -INFINITY;
     if (lane < p.groups) {
+      int at = lane % per;                           // (start apart: the lanes read different banks)
       for (int i = 0; i < per; ++i) {
-        const double v = s_row[lane * per + i];
-        if (v > a) { b = a; a = v; }
-        else if (v > b) b = v;
+        const double x = s_row[lane * per + at];
+        if (x > a) { b = a; a = x; }
+        else if (x > b) b = x;
+        at = at + 1 == per ? 0 : at + 1;
       }
       if (p.group_score != DX_GROUP_MAX && b > -INFINITY) a += b;
     }
@@ -174,35 +193,43 @@ __device__ __noinline__ int select_exact(const BatchRouteParams& p, const T* row
       r += o > a || (o == a && g < lane);
     }
     kept = __ballot_sync(0xffffffffu, lane < p.groups && r < p.keep);
+    __syncwarp();
   }
-  // without a bias the experts themselves are compared by their logits
-  Pick last{INFINITY, -1};
-  bool first = true;
-  int mine = -1;
+  // keys: without a bias the experts themselves are compared by their logits
+  unsigned long long key[kEpl], head = 0;
+#pragma unroll
+  for (int i = 0; i < kEpl; ++i) {
+    const int e = lane + 32 * i;
+    const bool on = e < p.E && (p.groups == 1 || (kept >> (min(e, p.E - 1) / per) & 1u));
+    const double x = p.bias || v[i] == -INFINITY ? v[i] : (double)z[i];
+    key[i] = on ? orderable64(x) : 0ull;
+  }
+  int mine = 0, head_e = 0;
   for (int j = 0; j < p.k; ++j) {
-    Pick best{0.0, -1};
-    for (int e = lane; e < p.E; e += 32) {
-      if (p.groups > 1 && !(kept >> (e / per) & 1u)) continue;
-      double v = s_row[e];
-      if (scores && !p.bias && v > -INFINITY) v = (double)to_f(row[e]);
-      const Pick c{v, e};
-      if ((first || before(last, c)) && before(c, best)) best = c;
+    // the lane's first (its lowest expert among equals), then the warp's: high word, low word, expert
+    head = 0;
+#pragma unroll
+    for (int i = 0; i < kEpl; ++i) {
+      if (key[i] > head) {
+        head = key[i];
+        head_e = lane + 32 * i;
+      }
     }
-    for (int o = 16; o > 0; o >>= 1) {
-      const Pick c{__shfl_xor_sync(0xffffffffu, best.v, o), __shfl_xor_sync(0xffffffffu, best.e, o)};
-      if (before(c, best)) best = c;
-    }
-    last = best;
-    first = false;
-    if (lane == j) mine = best.e;
+    const unsigned int hi = __reduce_max_sync(0xffffffffu, (unsigned int)(head >> 32));
+    const unsigned int lo = __reduce_max_sync(0xffffffffu, (unsigned int)(head >> 32) == hi ? (unsigned int)head : 0u);
+    const unsigned long long best = (unsigned long long)hi << 32 | lo;
+    const int e = (int)__reduce_min_sync(0xffffffffu, head == best ? (unsigned int)head_e : 0xffffu);
+    if (lane == j) mine = e;
+#pragma unroll
+    for (int i = 0; i < kEpl; ++i)
+      if (lane + 32 * i == e) key[i] = 0;
   }
-  __syncwarp();
   return mine;
 }
 
 // Where the pairs of a CTA's tokens go: s_base[e] = first place of expert e's.  The pairs are taken kTile at a time, a
 // contiguous stretch of 32 * kDeep per warp, so that equal experts keep the order of their pairs.
-constexpr int kDeep = 4;
+constexpr int kDeep = 2;
 constexpr int kTile = kWarps * 32 * kDeep;
 __device__ __forceinline__ void load_pairs(const int32_t* ids, long long p0, int at, int n, int (&id)[kDeep]) {
   const int first = at + (threadIdx.x >> 5) * 32 * kDeep + (threadIdx.x & 31);
@@ -282,7 +309,7 @@ __device__ __forceinline__ float exp_fast(float x) {
 
 // G lanes per token.  kScores: the selection goes by scores (a bias, or groups ranked by a sum), else by the logits.
 template <typename T, int G, bool kScores>
-__global__ void __launch_bounds__(kThreads, 3) dx_batch_route_kernel(BatchRouteParams p) {
+__global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteParams p) {
   constexpr int kTok = 32 / G;                       // tokens a warp works on side by side
   constexpr int kPicks = G == 4 ? 3 : G == 8 ? 2 : 1;   // picks (of k + 1) per lane
   constexpr unsigned int kMask = G == 32 ? 0xffffffffu : (1u << (G % 32)) - 1u;
@@ -333,11 +360,7 @@ __global__ void __launch_bounds__(kThreads, 3) dx_batch_route_kernel(BatchRouteP
     key_ok = fabsf(key_add) < 6e7f && key_mul > 0.f;   // (infinite or far-off biases: every token is selected in 64 bits)
     near = 4u + (unsigned int)fminf(kScoreError * (1.f + bias_abs) * key_mul, 1.6e7f);
   }
-  float b[kEpl];
-  if (kScores) {
-#pragma unroll
-    for (int i = 0; i < kEpl; ++i) b[i] = s_bias[min(e0 + i, DX_MAX_E - 1)];
-  }
+  const float4* bias8 = reinterpret_cast<const float4*>(s_bias + min(e0, DX_MAX_E - kEpl));
 
   const long long t_lo = (long long)blockIdx.x * p.per_cta;
   const long long t_hi = min((long long)p.N, t_lo + p.per_cta);
@@ -368,6 +391,8 @@ __global__ void __launch_bounds__(kThreads, 3) dx_batch_route_kernel(BatchRouteP
     unsigned int kept = 0xffffffffu;
     if (kScores) {
       const float rcp = softmax ? 1.f / inv : 0.f;
+      const float4 b0 = bias8[0], b1 = bias8[1];
+      const float b[kEpl] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
 #pragma unroll
       for (int i = 0; i < kEpl; ++i) {
         const bool live = z[i] > -INFINITY && !odd;
@@ -443,10 +468,17 @@ __global__ void __launch_bounds__(kThreads, 3) dx_batch_route_kernel(BatchRouteP
         q = dx_orderable(z[i] + 0.f) & 0xffffff00u;
       }
       key[i] = q | (unsigned int)(255 - e0 - i);
-      if (e0 + i >= E) key[i] = 0;
-      if (p.groups > 1) {
-        const int g = lane_groups ? sub >> gl_log : s_gid[min(e0 + i, DX_MAX_E - 1)];
-        if (!(kept >> g & 1u)) key[i] = 0;
+    }
+    if (lane_groups || p.groups == 1) {              // the lane's experts stay or go together
+      const bool on = e0 < E && (kept >> (lane_groups ? sub >> gl_log : 0) & 1u);
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i) key[i] = on ? key[i] : 0u;
+    }
+    if (!lane_groups && (p.groups > 1 || (E & (kEpl - 1)) != 0)) {
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i) {
+        const bool on = e0 + i < E && (kept >> s_gid[min(e0 + i, DX_MAX_E - 1)] & 1u);
+        key[i] = on ? key[i] : 0u;
       }
     }
     // ---- the lane's keys in descending order (19 exchanges)
@@ -459,19 +491,28 @@ __global__ void __launch_bounds__(kThreads, 3) dx_batch_route_kernel(BatchRouteP
     DX_EXCHANGE(2, 4) DX_EXCHANGE(3, 5)
     DX_EXCHANGE(3, 4)
 #undef DX_EXCHANGE
-    // ---- k + 1 rounds: lane j of the token's lanes keeps pick j (j + G, j + 2 G)
+    // ---- k + 1 rounds: lane j of the token's lanes keeps pick j (j + G, j + 2 G); a lane's next key comes out of shared
+    // memory when its first has been taken
     unsigned int pick[kPicks] = {};
+    unsigned int* list = reinterpret_cast<unsigned int*>(s_mem.exact[warp]) + lane;
+    __syncwarp();
+#pragma unroll
+    for (int i = 1; i < kEpl; ++i) list[i * 32] = key[i];
+    list[kEpl * 32] = 0u;
+    unsigned int head = key[0];
+    list += 32;
 #pragma unroll
     for (int j = 0; j <= DX_MAX_TOPK; ++j) {
       if (j <= k) {
-        const unsigned int top = lanes_umax<G>(key[0]);
+        const unsigned int top = lanes_umax<G>(head);
         if (sub == j % G) pick[j / G] = top;
-        const bool won = key[0] == top;
-#pragma unroll
-        for (int i = 0; i < kEpl - 1; ++i) key[i] = won ? key[i + 1] : key[i];
-        key[kEpl - 1] = won ? 0u : key[kEpl - 1];
+        if (head == top && top != 0u) {
+          head = *list;
+          list += 32;
+        }
       }
     }
+    __syncwarp();
     // ---- the picks' logits, and neighbours that 32 bits cannot tell apart
     int id[kPicks];
     float x[kPicks];
@@ -605,11 +646,15 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
   int front = 0, total = 0;
   if (e < E) {
     const int lo = (int)((long long)n_ctas * rank / kPermCluster), hi = (int)((long long)n_ctas * (rank + 1) / kPermCluster);
-#pragma unroll 8
-    for (int b = lo; b < hi; ++b) {
-      const int c = col[(size_t)b * E];
-      total += c;
-      front += b < first ? c : 0;
+    for (int b = lo; b < hi; b += 20) {              // (one round trip for up to 160 CTAs in the grid, two up to 320)
+      int c[20];
+#pragma unroll
+      for (int i = 0; i < 20; ++i) c[i] = b + i < hi ? col[(size_t)(b + i) * E] : 0;
+#pragma unroll
+      for (int i = 0; i < 20; ++i) {
+        total += c[i];
+        front += b + i < first ? c[i] : 0;
+      }
     }
     s_part[e] = make_int2(total, front);
   }
@@ -627,7 +672,9 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
       total += x;
       front += y;
     }
-    for (int b = first; b < min((int)blockIdx.x, n_ctas); ++b) front += col[(size_t)b * E];
+#pragma unroll
+    for (int r = 0; r < kPermCluster - 1; ++r)
+      front += first + r < min((int)blockIdx.x, n_ctas) ? col[(size_t)(first + r) * E] : 0;
   }
   __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -829,12 +876,14 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
   p.vec = rows_aligned(logits, ld, elem) ? 1 : 0;
   p.topk_ids = topk_ids; p.topk_w = topk_w; p.offsets = offsets; p.perm = perm;
   p.counts = ctx->route_counts;
-  // one CTA up to 64 tokens (a second launch would cost more than the work), else at most three per SM
+  // one CTA up to 64 tokens (a second launch would cost more than the work), else at most two per SM, each with a
+  // multiple of the tokens its warps take at a time
+  const int lanes = p.E <= 4 * kEpl && p.groups <= 4 ? 4 : p.E <= 8 * kEpl && p.groups <= 8 ? 8
+                    : p.E <= 16 * kEpl && p.groups <= 16 ? 16 : 32;
+  const int turn = kWarps * (32 / lanes);
   const int max_ctas = DX_ROUTE_CTAS_PER_SM * ctx->sm_count;
-  int grid = N <= 64 ? 1 : (N + 31) / 32;
-  if (grid > max_ctas) grid = max_ctas;
-  p.per_cta = (N + grid - 1) / grid;
-  grid = (N + p.per_cta - 1) / p.per_cta;
+  p.per_cta = N <= 64 ? N : (int)((((long long)N + max_ctas - 1) / max_ctas + turn - 1) / turn * turn);
+  const int grid = (N + p.per_cta - 1) / p.per_cta;
   cudaError_t e = dtype == DX_DTYPE_FP32 ? launch_route<float>(grid, p, st) : launch_route<__nv_bfloat16>(grid, p, st);
   *n_launches = 1;
   if (e == cudaSuccess && perm && grid > 1) {
@@ -852,8 +901,11 @@ cudaError_t dx_launch_route_grad(dx_ctx* ctx, const dx_route_desc& d, const void
   RouteGradParams p{logits, N, d.n_experts, d.top_k, ld, topk_ids, d_topk_w, d.score_fn, d.norm_topk, d.routed_scale,
                     rows_aligned(logits, ld, elem) ? 1 : 0, rows_aligned(d_logits, ld_d, elem) ? 1 : 0, d_logits, ld_d,
                     ctx->dev_status};
-  long long grid = ((long long)N + 31) / 32;
-  const long long most = 8ll * ctx->sm_count;
+  // four tokens per warp and turn, fewer where every expert's logit has a gradient and E takes more lanes
+  const bool dense = d.score_fn == DX_SCORE_SOFTMAX && !d.norm_topk;
+  const int turn = kWarps * (!dense || d.n_experts <= 8 * kEpl ? 4 : d.n_experts <= 16 * kEpl ? 2 : 1);
+  long long grid = ((long long)N + turn - 1) / turn;
+  const long long most = 4ll * ctx->sm_count;
   if (grid > most) grid = most;
   return dtype == DX_DTYPE_FP32 ? launch_grad<float>((int)grid, p, st) : launch_grad<__nv_bfloat16>((int)grid, p, st);
 }

@@ -23,7 +23,7 @@
 #define DX_ROW_CLUSTER_MAX 16  // CTAs that share a row of logits
 #define DX_ROW_SLICE_BYTES 106000  // ... and the bytes of it one CTA holds when there are many rows (two CTAs per SM)
 #define DX_MAX_GROUPS 32       // expert groups of moe_route_tokens
-#define DX_ROUTE_CTAS_PER_SM 3 // of its selection kernel
+#define DX_ROUTE_CTAS_PER_SM 2 // of its selection kernel
 #define DX_ROUTE_CLUSTER 4     // CTAs (and SMs) of the routing kernel; the expert kernel leaves them free
 
 // What the routing kernel hands to the expert kernels.  The routing-independent groups (shared experts, draft
