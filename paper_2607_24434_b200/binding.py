@@ -695,27 +695,34 @@ def squared_error(ctx: Context, a: torch.Tensor, b: torch.Tensor) -> torch.Tenso
 
 
 # ---- whole batches of tokens: scoring, distillation, routing (the library takes raw pointers, so what a pointer cannot
-# show -- type, device, layout -- is checked here) -----------------------------------------------------------------------
+# show -- type, device, layout -- is checked here; outputs made here need no check) ---------------------------------------
 def _matrix(ctx: Context, t: torch.Tensor, name: str) -> Tuple[int, int]:
     """dtype code and row pitch of a [rows, cols] matrix of logits on the context's GPU."""
-    if t.dim() != 2 or t.device.type != "cuda" or t.device.index != ctx.device:
+    if t.dim() != 2 or not t.is_cuda or t.get_device() != ctx.device:
         raise ValueError(f"{name}: a 2-d tensor on cuda:{ctx.device} is expected")
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"{name}: float32 or bfloat16 is expected, not {t.dtype}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    dtype = t.dtype
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise ValueError(f"{name}: float32 or bfloat16 is expected, not {dtype}")
+    ld, step = t.stride()
+    rows, cols = t.shape
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent")
-    return (1 if t.dtype == torch.bfloat16 else 0), (int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1]))
+    return (1 if dtype is torch.bfloat16 else 0), (ld if rows > 1 else cols)
 
 
-def _dense(ctx: Context, t: Optional[torch.Tensor], name: str, shape: Sequence[int], dtype: torch.dtype) -> None:
-    if t is None:
-        return
-    if t.device.type != "cuda" or t.device.index != ctx.device or t.dtype != dtype or tuple(t.shape) != tuple(shape) \
-            or not t.is_contiguous():
+def _dense(ctx: Context, t: Optional[torch.Tensor], name: str, shape: Tuple[int, ...], dtype: torch.dtype) -> None:
+    if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_cuda or t.get_device() != ctx.device
+                          or not t.is_contiguous()):
         raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on cuda:{ctx.device} is expected")
 
 
+# (the handle alone: a Stream object costs a microsecond, and a small call takes but a few)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _ctx_stream(ctx: Context) -> int:
+    if _raw_stream is not None:
+        return _raw_stream(ctx.device)
     return torch.cuda.current_stream(ctx.device).cuda_stream
 
 
@@ -726,19 +733,20 @@ def spec_token_logprobs(ctx: Context, logits: torch.Tensor, tokens: Optional[tor
     none), ``entropy`` [N] and, with ``top_n`` > 0, ``top_ids`` / ``top_logprobs`` [N, top_n]."""
     dt, ld = _matrix(ctx, logits, "logits")
     N, V = logits.shape
-    if out is None:
-        f32 = dict(dtype=torch.float32, device=logits.device)
-        out = {} if tokens is None else {"logprob": torch.empty((N,), **f32)}
-        out["entropy"] = torch.empty((N,), **f32)
-        if top_n > 0:
-            out["top_ids"] = torch.empty((N, top_n), dtype=torch.int32, device=logits.device)
-            out["top_logprobs"] = torch.empty((N, top_n), **f32)
     _dense(ctx, tokens, "tokens", (N,), torch.int32)
-    _dense(ctx, out.get("logprob"), "logprob", (N,), torch.float32)
-    _dense(ctx, out.get("entropy"), "entropy", (N,), torch.float32)
-    _dense(ctx, out.get("top_ids"), "top_ids", (N, top_n), torch.int32)
-    _dense(ctx, out.get("top_logprobs"), "top_logprobs", (N, top_n), torch.float32)
-    _check(ctx.lib.spec_token_logprobs(ctx.handle, _ptr(logits), dt, N, V, ld, _ptr(tokens), float(temperature), top_n,
+    if out is None:
+        f32 = torch.float32
+        out = {} if tokens is None else {"logprob": logits.new_empty((N,), dtype=f32)}
+        out["entropy"] = logits.new_empty((N,), dtype=f32)
+        if top_n > 0:
+            out["top_ids"] = logits.new_empty((N, top_n), dtype=torch.int32)
+            out["top_logprobs"] = logits.new_empty((N, top_n), dtype=f32)
+    else:
+        _dense(ctx, out.get("logprob"), "logprob", (N,), torch.float32)
+        _dense(ctx, out.get("entropy"), "entropy", (N,), torch.float32)
+        _dense(ctx, out.get("top_ids"), "top_ids", (N, top_n), torch.int32)
+        _dense(ctx, out.get("top_logprobs"), "top_logprobs", (N, top_n), torch.float32)
+    _check(ctx.lib.spec_token_logprobs(ctx.handle, _ptr(logits), dt, N, V, ld, _ptr(tokens), temperature, top_n,
                                        _ptr(out.get("logprob")), _ptr(out.get("entropy")), _ptr(out.get("top_ids")),
                                        _ptr(out.get("top_logprobs")), _ctx_stream(ctx)), "spec_token_logprobs")
     return out
@@ -753,23 +761,25 @@ def spec_distill_topk(ctx: Context, logits: torch.Tensor, teacher_ids: torch.Ten
     N, V = logits.shape
     if teacher_ids.dim() != 2:
         raise ValueError("teacher_ids: [N, k] is expected")
-    k = int(teacher_ids.shape[1])
-    if out is None:
-        out = {"loss": torch.empty((N,), dtype=torch.float32, device=logits.device)}
-        if grad:
-            out["dlogits"] = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+    k = teacher_ids.shape[1]
     _dense(ctx, teacher_ids, "teacher_ids", (N, k), torch.int32)
     _dense(ctx, teacher_logprobs, "teacher_logprobs", (N, k), torch.float32)
     _dense(ctx, row_weight, "row_weight", (N,), torch.float32)
-    _dense(ctx, out.get("loss"), "loss", (N,), torch.float32)
-    d, ld_d = out.get("dlogits") if grad else None, V
-    if d is not None:
-        if d.dtype != logits.dtype or tuple(d.shape) != (N, V):
-            raise ValueError("dlogits: the logits' shape and type are expected")
-        ld_d = _matrix(ctx, d, "dlogits")[1]
+    ld_d = V
+    if out is None:
+        out = {"loss": logits.new_empty((N,), dtype=torch.float32)}
+        if grad:
+            out["dlogits"] = logits.new_empty((N, V))
+    else:
+        _dense(ctx, out.get("loss"), "loss", (N,), torch.float32)
+        if grad and out.get("dlogits") is not None:
+            if out["dlogits"].dtype is not logits.dtype or out["dlogits"].shape != logits.shape:
+                raise ValueError("dlogits: the logits' shape and type are expected")
+            ld_d = _matrix(ctx, out["dlogits"], "dlogits")[1]
     _check(ctx.lib.spec_distill_topk(ctx.handle, _ptr(logits), dt, N, V, ld, _ptr(teacher_ids), _ptr(teacher_logprobs),
-                                     k, 1 if tail else 0, float(temperature), _ptr(row_weight), _ptr(out.get("loss")),
-                                     _ptr(d), ld_d, _ctx_stream(ctx)), "spec_distill_topk")
+                                     k, 1 if tail else 0, temperature, _ptr(row_weight), _ptr(out.get("loss")),
+                                     _ptr(out.get("dlogits") if grad else None), ld_d, _ctx_stream(ctx)),
+           "spec_distill_topk")
     return out
 
 
@@ -781,17 +791,18 @@ def moe_route_tokens(ctx: Context, logits: torch.Tensor, top_k: int, score_fn: i
     ``perm`` [N*k] (token-expert pairs by expert).  ``group_score``: 0 largest value, 1 sum of the two largest."""
     dt, ld = _matrix(ctx, logits, "logits")
     N, E = logits.shape
-    if out is None:
-        i32 = dict(dtype=torch.int32, device=logits.device)
-        out = {"topk_ids": torch.empty((N, top_k), **i32),
-               "topk_w": torch.empty((N, top_k), dtype=torch.float32, device=logits.device),
-               "offsets": torch.empty((E + 1,), **i32), "perm": torch.empty((N * top_k,), **i32)}
     _dense(ctx, select_bias, "select_bias", (E,), torch.float32)
-    _dense(ctx, out["topk_ids"], "topk_ids", (N, top_k), torch.int32)
-    _dense(ctx, out["topk_w"], "topk_w", (N, top_k), torch.float32)
-    _dense(ctx, out.get("offsets"), "offsets", (E + 1,), torch.int32)
-    _dense(ctx, out.get("perm"), "perm", (N * top_k,), torch.int32)
-    d = RouteDesc(E, top_k, score_fn, norm_topk, n_groups, topk_groups, group_score, float(routed_scale))
+    if out is None:
+        i32 = torch.int32
+        out = {"topk_ids": logits.new_empty((N, top_k), dtype=i32),
+               "topk_w": logits.new_empty((N, top_k), dtype=torch.float32),
+               "offsets": logits.new_empty((E + 1,), dtype=i32), "perm": logits.new_empty((N * top_k,), dtype=i32)}
+    else:
+        _dense(ctx, out["topk_ids"], "topk_ids", (N, top_k), torch.int32)
+        _dense(ctx, out["topk_w"], "topk_w", (N, top_k), torch.float32)
+        _dense(ctx, out.get("offsets"), "offsets", (E + 1,), torch.int32)
+        _dense(ctx, out.get("perm"), "perm", (N * top_k,), torch.int32)
+    d = RouteDesc(E, top_k, score_fn, norm_topk, n_groups, topk_groups, group_score, routed_scale)
     _check(ctx.lib.moe_route_tokens(ctx.handle, C.byref(d), _ptr(logits), dt, N, ld, _ptr(select_bias),
                                     _ptr(out["topk_ids"]), _ptr(out["topk_w"]), _ptr(out.get("offsets")),
                                     _ptr(out.get("perm")), _ctx_stream(ctx)), "moe_route_tokens")
@@ -806,15 +817,17 @@ def moe_route_tokens_backward(ctx: Context, logits: torch.Tensor, topk_ids: torc
     N, E = logits.shape
     if topk_ids.dim() != 2:
         raise ValueError("topk_ids: [N, k] is expected")
-    k = int(topk_ids.shape[1])
+    k = topk_ids.shape[1]
     _dense(ctx, topk_ids, "topk_ids", (N, k), torch.int32)
     _dense(ctx, d_topk_w, "d_topk_w", (N, k), torch.float32)
+    ld_d = E
     if out is None:
-        out = torch.empty((N, E), dtype=logits.dtype, device=logits.device)
-    if out.dtype != logits.dtype or tuple(out.shape) != (N, E):
-        raise ValueError("out: the logits' shape and type are expected")
-    ld_d = _matrix(ctx, out, "out")[1]
-    d = RouteDesc(E, k, score_fn, norm_topk, 1, 1, 0, float(routed_scale))
+        out = logits.new_empty((N, E))
+    else:
+        if out.dtype is not logits.dtype or out.shape != logits.shape:
+            raise ValueError("out: the logits' shape and type are expected")
+        ld_d = _matrix(ctx, out, "out")[1]
+    d = RouteDesc(E, k, score_fn, norm_topk, 1, 1, 0, routed_scale)
     _check(ctx.lib.moe_route_tokens_backward(ctx.handle, C.byref(d), _ptr(logits), dt, N, ld, _ptr(topk_ids),
                                              _ptr(d_topk_w), _ptr(out), ld_d, _ctx_stream(ctx)),
            "moe_route_tokens_backward")

@@ -10,9 +10,10 @@
 // The selection is that of exact arithmetic.  It is made on unique 32-bit keys first: a lane holds eight consecutive
 // experts, whose keys are 24 bits of the value and the reversed expert id -- with a bias the value's place between the
 // smallest and the largest that a score plus a bias can have, without one the leading bits of the logit (all of a bf16
-// logit).  A sorting network and k + 1 rounds of a maximum over the token's lanes put them in order.  Where two
-// neighbours of the result are closer than keys and arithmetic can tell apart (a few tokens in a thousand), the whole
-// warp makes that token's selection again with 64-bit scores.
+// logit).  A sorting network and k + 2 rounds of a maximum over the token's lanes put them in order.  Where two
+// neighbours of the result are closer than keys and arithmetic can tell apart (a few tokens in a thousand), the picks are
+// put in order by their 64-bit values, and where that cannot settle it the whole warp makes the token's selection again
+// in 64 bits.
 //
 // Two launches for a large batch: selection with one histogram of experts per CTA, then the permutation, clusters of
 // CTAs adding up the histograms in front of them (a stable counting sort without atomics on device memory; the order
@@ -118,7 +119,6 @@ __device__ __forceinline__ unsigned int lanes_umax(unsigned int v) {
   return v;
 }
 
-__device__ __forceinline__ bool finite_f(float x) { return fabsf(x) <= 3.402823466e38f; }
 __device__ __forceinline__ float sigmoid_f(float z) { return 1.f / (1.f + expf(-z)); }
 
 // Larger double -> larger integer; -inf (masked experts) -> 1 or more, 0 is left for what is excluded.
@@ -231,49 +231,71 @@ __device__ __noinline__ int select_exact(const BatchRouteParams& p, const T* row
 // contiguous stretch of 32 * kDeep per warp, so that equal experts keep the order of their pairs.
 constexpr int kDeep = 2;
 constexpr int kTile = kWarps * 32 * kDeep;
-__device__ __forceinline__ void load_pairs(const int32_t* ids, long long p0, int at, int n, int (&id)[kDeep]) {
+struct Pairs {
+  int id[kDeep];
+  unsigned int same[kDeep];   // the warp's lanes with the same expert
+};
+__device__ __forceinline__ void load_pairs(const int32_t* ids, long long p0, int at, int n, Pairs& q) {
   const int first = at + (threadIdx.x >> 5) * 32 * kDeep + (threadIdx.x & 31);
 #pragma unroll
-  for (int d = 0; d < kDeep; ++d) id[d] = first + 32 * d < n ? ids[p0 + first + 32 * d] : -1;
+  for (int d = 0; d < kDeep; ++d) q.id[d] = first + 32 * d < n ? ids[p0 + first + 32 * d] : -1;
 }
-__device__ __forceinline__ void place_pairs(const int32_t* ids, long long p0, int n, int E, int (*s_hist)[DX_MAX_E],
-                                            int* s_base, int32_t* perm, int (&id)[kDeep]) {
+// pairs of each expert per warp
+__device__ __forceinline__ void count_pairs(Pairs& q, int E, int (*s_hist)[DX_MAX_E]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int e = lane; e < E; e += 32) s_hist[warp][e] = 0;
+  __syncwarp();
+#pragma unroll
+  for (int d = 0; d < kDeep; ++d) {
+    q.same[d] = __match_any_sync(0xffffffffu, q.id[d]);
+    if (q.id[d] >= 0 && __ffs(q.same[d]) - 1 == lane) s_hist[warp][q.id[d]] += __popc(q.same[d]);
+    __syncwarp();
+  }
+}
+// ... turned into the pairs of the warps in front; s_total[e] += those of all warps
+__device__ __forceinline__ void front_of_warps(int E, int (*s_hist)[DX_MAX_E], int* s_total) {
+  for (int e = threadIdx.x; e < E; e += kThreads) {
+    int c[kWarps], x = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) c[w] = s_hist[w][e];
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      s_hist[w][e] = x;
+      x += c[w];
+    }
+    s_total[e] = x;
+  }
+}
+__device__ __forceinline__ void scatter_pairs(const Pairs& q, long long first_pair, const int* s_base,
+                                              int (*s_hist)[DX_MAX_E], int32_t* perm) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long first = first_pair + warp * 32 * kDeep + lane;
+#pragma unroll
+  for (int d = 0; d < kDeep; ++d) {
+    const int x = q.id[d] >= 0 ? s_hist[warp][q.id[d]] : 0;
+    __syncwarp();
+    if (q.id[d] >= 0) {
+      perm[s_base[q.id[d]] + x + __popc(q.same[d] & ((1u << lane) - 1u))] = (int32_t)(first + 32 * d);
+      if (__ffs(q.same[d]) - 1 == lane) s_hist[warp][q.id[d]] = x + __popc(q.same[d]);
+    }
+    __syncwarp();
+  }
+}
+// the tiles from the first on (whose counts are in place, s_total and s_base filled)
+__device__ __forceinline__ void place_pairs(const int32_t* ids, long long p0, int n, int E, int (*s_hist)[DX_MAX_E],
+                                            int* s_base, int* s_total, int32_t* perm, Pairs& q) {
 #pragma unroll 1
   for (int at = 0; at < n; at += kTile) {
-    if (at > 0) load_pairs(ids, p0, at, n, id);
-    for (int e = lane; e < E; e += 32) s_hist[warp][e] = 0;
-    __syncwarp();
-    unsigned int same[kDeep];
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d) {
-      same[d] = __match_any_sync(0xffffffffu, id[d]);
-      if (id[d] >= 0 && __ffs(same[d]) - 1 == lane) s_hist[warp][id[d]] += __popc(same[d]);
-      __syncwarp();
+    if (at > 0) {
+      load_pairs(ids, p0, at, n, q);
+      __syncthreads();                               // (the tile in front has been placed)
+      for (int e = threadIdx.x; e < E; e += kThreads) s_base[e] += s_total[e];
+      count_pairs(q, E, s_hist);
+      __syncthreads();
+      front_of_warps(E, s_hist, s_total);
+      __syncthreads();
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < E; e += kThreads) {
-      int x = s_base[e];
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const int c = s_hist[w][e];
-        s_hist[w][e] = x;
-        x += c;
-      }
-      s_base[e] = x;
-    }
-    __syncthreads();
-    const long long first = p0 + at + warp * 32 * kDeep + lane;
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d) {
-      const int x = id[d] >= 0 ? s_hist[warp][id[d]] : 0;
-      __syncwarp();
-      if (id[d] >= 0) {
-        perm[x + __popc(same[d] & ((1u << lane) - 1u))] = (int32_t)(first + 32 * d);
-        if (__ffs(same[d]) - 1 == lane) s_hist[warp][id[d]] = x + __popc(same[d]);
-      }
-      __syncwarp();
-    }
+    scatter_pairs(q, p0 + at, s_base, s_hist, perm);
   }
 }
 
@@ -311,7 +333,7 @@ __device__ __forceinline__ float exp_fast(float x) {
 template <typename T, int G, bool kScores>
 __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteParams p) {
   constexpr int kTok = 32 / G;                       // tokens a warp works on side by side
-  constexpr int kPicks = G == 4 ? 3 : G == 8 ? 2 : 1;   // picks (of k + 1) per lane
+  constexpr int kPicks = G == 4 ? 3 : G == 8 ? 2 : 1;   // picks (of k + 2) per lane
   constexpr unsigned int kMask = G == 32 ? 0xffffffffu : (1u << (G % 32)) - 1u;
   __shared__ int s_count[DX_MAX_E];
   __shared__ __align__(16) float s_bias[DX_MAX_E];
@@ -491,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     DX_EXCHANGE(2, 4) DX_EXCHANGE(3, 5)
     DX_EXCHANGE(3, 4)
 #undef DX_EXCHANGE
-    // ---- k + 1 rounds: lane j of the token's lanes keeps pick j (j + G, j + 2 G); a lane's next key comes out of shared
+    // ---- k + 2 rounds: lane j of the token's lanes keeps pick j (j + G, j + 2 G); a lane's next key comes out of shared
     // memory when its first has been taken
     unsigned int pick[kPicks] = {};
     unsigned int* list = reinterpret_cast<unsigned int*>(s_mem.exact[warp]) + lane;
@@ -502,8 +524,8 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     unsigned int head = key[0];
     list += 32;
 #pragma unroll
-    for (int j = 0; j <= DX_MAX_TOPK; ++j) {
-      if (j <= k) {
+    for (int j = 0; j <= DX_MAX_TOPK + 1; ++j) {
+      if (j <= k + 1) {
         const unsigned int top = lanes_umax<G>(head);
         if (sub == j % G) pick[j / G] = top;
         if (head == top && top != 0u) {
@@ -545,9 +567,53 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
         close |= !tie;
       }
     }
-    doubt |= (__ballot_sync(0xffffffffu, close) >> (tok * G) & kMask) != 0;
-    unsigned int redo = __ballot_sync(0xffffffffu, doubt);
-    if (redo != 0) {
+    const bool unsure = (__ballot_sync(0xffffffffu, close) >> (tok * G) & kMask) != 0;
+    if (__any_sync(0xffffffffu, doubt || unsure)) {
+      // The true selection is among the first k + 1 picks unless the one behind them is as close to the border as well.
+      // Then their exact values put them in order: the logits, or the sigmoid in 64 bits and the bias (a softmax's needs
+      // the whole row in 64 bits).
+      unsigned int border = 0, behind = 0;
+#pragma unroll
+      for (int h = 0; h < kPicks; ++h) {
+        const unsigned int x0 = __shfl_sync(0xffffffffu, pick[h], tok * G + (k - 1) % G);
+        const unsigned int x1 = __shfl_sync(0xffffffffu, pick[h], tok * G + (k + 1) % G);
+        if (h == (k - 1) / G) border = x0;
+        if (h == (k + 1) / G) behind = x1;
+      }
+      const bool inside = !doubt && !(biased && softmax) && (behind == 0 || (border >> 8) - (behind >> 8) > near);
+      double v[kPicks];
+#pragma unroll
+      for (int h = 0; h < kPicks; ++h) {
+        v[h] = -INFINITY;
+        if (h * G + sub <= k && pick[h] != 0 && x[h] > -INFINITY)
+          v[h] = biased ? 1.0 / (1.0 + exp(-(double)x[h])) + (double)s_bias[id[h]] : (double)x[h];
+      }
+      int rank[kPicks] = {};
+#pragma unroll
+      for (int h = 0; h < kPicks; ++h) {
+        for (int j = 0; j < G; ++j) {
+          if (h * G + j > k) break;
+          const double o = __shfl_sync(0xffffffffu, v[h], tok * G + j);
+          const int oe = __shfl_sync(0xffffffffu, pick[h] != 0 ? id[h] : DX_MAX_E, tok * G + j);
+#pragma unroll
+          for (int i = 0; i < kPicks; ++i) rank[i] += o > v[i] || (o == v[i] && oe < id[i]);
+        }
+      }
+      int* order = reinterpret_cast<int*>(s_mem.exact[warp]) + tok * (DX_MAX_TOPK + 2);
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < kPicks; ++h)
+        if (h * G + sub <= k && pick[h] != 0) order[rank[h]] = id[h];
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < kPicks; ++h) {
+        if (unsure && inside && h * G + sub < k) {
+          id[h] = order[h * G + sub];
+          x[h] = to_f(row[id[h]]);
+        }
+      }
+      __syncwarp();
+      const unsigned int redo = __ballot_sync(0xffffffffu, doubt || (unsure && !inside));
 #pragma unroll 1
       for (int q = 0; q < kTok; ++q) {
         if (!(redo >> (q * G) & 1u)) continue;       // (the same for the whole warp)
@@ -621,48 +687,71 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
   }
   if (threadIdx.x == 0) p.offsets[E] = p.N * k;
   __syncthreads();
-  int id[kDeep];
-  load_pairs(p.topk_ids, 0, 0, p.N * k, id);
-  place_pairs(p.topk_ids, 0, p.N * k, E, s_mem.hist, s_base, p.perm, id);
+  Pairs q;
+  load_pairs(p.topk_ids, 0, 0, p.N * k, q);
+  count_pairs(q, E, s_mem.hist);
+  __syncthreads();
+  front_of_warps(E, s_mem.hist, s_count);
+  __syncthreads();
+  place_pairs(p.topk_ids, 0, p.N * k, E, s_mem.hist, s_base, s_count, p.perm, q);
 }
 
 // Clusters of kPermCluster CTAs share the sums over the histograms: CTA r of a cluster adds up every kPermCluster-th part
-// of them, once over all CTAs (the experts' totals) and once over those in front of the cluster.
+// of them, once over all CTAs (the experts' totals) and once over those in front of the cluster; its threads take the
+// experts several times over.  What needs the CTA's own pairs alone is done while the sums are on their way.
 constexpr int kPermCluster = 8;
-__global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRouteParams p, int n_ctas) {
+constexpr int kMaxRows = 5;                          // histograms a thread has in flight
+__global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRouteParams p, int n_ctas, int e_pad) {
   __shared__ int s_hist[kWarps][DX_MAX_E];
-  __shared__ int s_base[DX_MAX_E];
+  __shared__ int s_base[DX_MAX_E], s_total[DX_MAX_E];
   __shared__ int s_scan[kWarps];
   __shared__ int2 s_part[DX_MAX_E];
-  const int E = p.E, e = threadIdx.x;
+  const int E = p.E, e = threadIdx.x % e_pad, seg = threadIdx.x / e_pad, segs = kThreads / e_pad;
   const int rank = blockIdx.x % kPermCluster, first = blockIdx.x - rank;   // (clusters are runs of the grid)
   const long long t_lo = (long long)blockIdx.x * p.per_cta;
   const long long t_hi = min((long long)p.N, t_lo + p.per_cta);
   const int n = t_lo < t_hi ? (int)(t_hi - t_lo) * p.k : 0;
+  if (threadIdx.x < DX_MAX_E) s_part[threadIdx.x] = make_int2(0, 0);
+  __syncthreads();
   dx_pdl_wait();               // (launched while the selection drains)
-  int id[kDeep];
-  load_pairs(p.topk_ids, t_lo * p.k, 0, n, id);
+  Pairs q;
+  load_pairs(p.topk_ids, t_lo * p.k, 0, n, q);
   const int32_t* col = p.counts + e;
-  int front = 0, total = 0;
+  int front = 0, total = 0, near = 0;
   if (e < E) {
-    const int lo = (int)((long long)n_ctas * rank / kPermCluster), hi = (int)((long long)n_ctas * (rank + 1) / kPermCluster);
-    for (int b = lo; b < hi; b += 20) {              // (one round trip for up to 160 CTAs in the grid, two up to 320)
-      int c[20];
+    const int all_lo = (int)((long long)n_ctas * rank / kPermCluster);
+    const int all_hi = (int)((long long)n_ctas * (rank + 1) / kPermCluster);
+    const int lo = all_lo + (all_hi - all_lo) * seg / segs, hi = all_lo + (all_hi - all_lo) * (seg + 1) / segs;
+    for (int b = lo; b < hi; b += 4 * kMaxRows) {
+      int c[4 * kMaxRows];
 #pragma unroll
-      for (int i = 0; i < 20; ++i) c[i] = b + i < hi ? col[(size_t)(b + i) * E] : 0;
+      for (int i = 0; i < 4 * kMaxRows; ++i) c[i] = b + i < hi ? col[(size_t)(b + i) * E] : 0;
 #pragma unroll
-      for (int i = 0; i < 20; ++i) {
+      for (int i = 0; i < 4 * kMaxRows; ++i) {
         total += c[i];
         front += b + i < first ? c[i] : 0;
       }
     }
-    s_part[e] = make_int2(total, front);
+    // (the CTAs of the cluster in front of this one)
+    for (int r = seg; r < kPermCluster - 1; r += segs)
+      near += first + r < min((int)blockIdx.x, n_ctas) ? col[(size_t)(first + r) * E] : 0;
   }
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  count_pairs(q, E, s_hist);
   if (e < E) {
-    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(&s_part[e]));
-    total = front = 0;
+    atomicAdd(&s_part[e].x, total);
+    atomicAdd(&s_part[e].y, front);
+  }
+  __syncthreads();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  if (threadIdx.x < DX_MAX_E) s_base[threadIdx.x] = 0;
+  front_of_warps(E, s_hist, s_total);
+  __syncthreads();
+  if (e < E && near != 0) atomicAdd(&s_base[e], near);
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  total = front = 0;
+  if (threadIdx.x < E) {
+    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(&s_part[threadIdx.x]));
 #pragma unroll
     for (int r = 0; r < kPermCluster; ++r) {
       uint32_t a;
@@ -672,20 +761,17 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
       total += x;
       front += y;
     }
-#pragma unroll
-    for (int r = 0; r < kPermCluster - 1; ++r)
-      front += first + r < min((int)blockIdx.x, n_ctas) ? col[(size_t)(first + r) * E] : 0;
   }
   __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  const int at = prefix_counts(total, s_scan);
-  if (e < E) {
-    s_base[e] = at + front;
-    if (blockIdx.x == 0) p.offsets[e] = at;
+  const int at = prefix_counts(total, s_scan);       // (a barrier of the CTA among it: s_base is complete)
+  if (threadIdx.x < E) {
+    s_base[threadIdx.x] += at + front;
+    if (blockIdx.x == 0) p.offsets[threadIdx.x] = at;
   }
-  if (blockIdx.x == 0 && e == 0) p.offsets[E] = p.N * p.k;
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[E] = p.N * p.k;
   __syncthreads();
-  place_pairs(p.topk_ids, t_lo * p.k, n, E, s_hist, s_base, p.perm, id);
+  place_pairs(p.topk_ids, t_lo * p.k, n, E, s_hist, s_base, s_total, p.perm, q);
   __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -888,7 +974,8 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
   *n_launches = 1;
   if (e == cudaSuccess && perm && grid > 1) {
     const unsigned int padded = (unsigned)((grid + kPermCluster - 1) / kPermCluster * kPermCluster);
-    e = dx_launch_pdl((ctx->pdl_mask & DX_PDL_ROUTE) != 0, dx_batch_permute_kernel, dim3(padded), dim3(kThreads), 0, st, kPermCluster, p, grid);
+    e = dx_launch_pdl((ctx->pdl_mask & DX_PDL_ROUTE) != 0, dx_batch_permute_kernel, dim3(padded), dim3(kThreads), 0, st, kPermCluster, p, grid,
+                      p.E <= 32 ? 32 : p.E <= 64 ? 64 : p.E <= 128 ? 128 : 256);
     *n_launches = 2;
   }
   return e;
