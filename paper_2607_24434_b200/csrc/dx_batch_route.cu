@@ -22,7 +22,8 @@
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreadsLog = 9;
+constexpr int kThreads = 1 << kThreadsLog;
 constexpr int kWarps = kThreads / 32;
 constexpr int kEpl = 8;           // experts per lane
 // How far the difference of two 32-bit selection values may be off, relative to 1 + the largest bias: exponential and
@@ -376,11 +377,13 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
       hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
     bias_abs = fmaxf(fabsf(lo), fabsf(hi));
-    key_mul = 16777000.f / (1.f + hi - lo);
-    // (8 quanta above the masked experts: key_add is rounded, by less than 4 up to the bound that follows)
-    key_add = 8.f - lo * key_mul;
-    key_ok = fabsf(key_add) < 6e7f && key_mul > 0.f;   // (infinite or far-off biases: every token is selected in 64 bits)
-    near = 4u + (unsigned int)fminf(kScoreError * (1.f + bias_abs) * key_mul, 1.6e7f);
+    // value -> 2^23 + quanta: the low 23 bits of the float are the quanta (at least 8, masked experts have 1: key_add's
+    // share is rounded, by less than 4 up to the bound that follows)
+    key_mul = 8388000.f / (1.f + hi - lo);
+    const float shift = 8.f - lo * key_mul;
+    key_add = 8388608.f + shift;
+    key_ok = fabsf(shift) < 6e7f && key_mul > 0.f;   // (infinite or far-off biases: every token is selected in 64 bits)
+    near = 4u + (unsigned int)fminf(kScoreError * (1.f + bias_abs) * key_mul, 8e6f);
   }
   const float4* bias8 = reinterpret_cast<const float4*>(s_bias + min(e0, DX_MAX_E - kEpl));
 
@@ -460,18 +463,24 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
         __syncwarp();
       }
       const float gs = p.group_score == DX_GROUP_MAX || g2 == -INFINITY ? g1 : g1 + g2;
-      // rank of this lane's group; neighbours at the border too close to tell apart raise the doubt
-      const float eps = kScores ? 2.f * kScoreError * (1.f + bias_abs) : 0.f;
-      int r = 0;
-      bool close = false;
-      for (int g = 0; g < p.groups; ++g) {
-        const float o = __shfl_sync(0xffffffffu, gs, tok * G + g);
-        r += o > gs || (o == gs && g < sub);
-        close |= g != sub && fabsf(o - gs) <= eps;   // (infinite on both sides: not a number, not close)
+      // the best groups one after the other, on unique keys: 26 bits of the score's order, then the reversed group; scores
+      // that the cut bits or the arithmetic cannot tell apart at the border raise the doubt
+      const unsigned int gkey = sub < p.groups ? (dx_orderable(gs + 0.f) & 0xffffffe0u) | (unsigned int)(31 - sub) : 0u;
+      unsigned int left = gkey, last = 0, next = 0;
+      for (int j = 0; j <= p.keep; ++j) {            // (keep < groups)
+        next = lanes_umax<G>(left);
+        if (j < p.keep) last = next;
+        if (left == next) left = 0;
       }
-      const bool in = sub < p.groups;
-      kept = __ballot_sync(0xffffffffu, in && r < p.keep) >> (tok * G) & kMask;
-      doubt |= (__ballot_sync(0xffffffffu, kScores && in && close && (r == p.keep - 1 || r == p.keep)) >> (tok * G) & kMask) != 0;
+      kept = __ballot_sync(0xffffffffu, gkey != 0 && gkey >= last) >> (tok * G) & kMask;
+      const float g_in = __shfl_sync(0xffffffffu, gs, tok * G + 31 - (int)(last & 31u));
+      const float g_out = __shfl_sync(0xffffffffu, gs, tok * G + 31 - (int)(next & 31u));
+      if (kScores) {   // (the key's cut: 32 steps of the score's last place; infinite on both sides: not close)
+        const float eps = 2.f * kScoreError * (1.f + bias_abs);
+        doubt |= fabsf(g_in - g_out) <= eps + 6e-6f * fmaxf(fabsf(g_in), fabsf(g_out));
+      } else if (sizeof(T) == 4) {   // (a bf16 logit fits the key: equal keys are a true tie)
+        doubt |= (last >> 5) == (next >> 5) && g_in > -INFINITY;
+      }
     }
     if (kScores && !biased) {                        // (the scores were for the groups; experts go by their logits)
       load8(row, e0, E, p.vec != 0, z);
@@ -482,14 +491,12 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     unsigned int key[kEpl];
 #pragma unroll
     for (int i = 0; i < kEpl; ++i) {
-      unsigned int q;
-      if (biased) {
-        const float f = fmaf(z[i], key_mul, key_add);   // (not a number, or below: masked)
-        q = min(max((unsigned int)__float2uint_rz(f), 1u), 0xffffffu) << 8;
+      const unsigned int id = (unsigned int)(255 - e0 - i);
+      if (biased) {   // (not a number, or below: masked)
+        key[i] = __byte_perm(__float_as_uint(fmaxf(fmaf(z[i], key_mul, key_add), 8388609.f)) & 0x7fffffu, id, 0x2104);
       } else {
-        q = dx_orderable(z[i] + 0.f) & 0xffffff00u;
+        key[i] = __byte_perm(dx_orderable(z[i] + 0.f), id, 0x3214);
       }
-      key[i] = q | (unsigned int)(255 - e0 - i);
     }
     if (lane_groups || p.groups == 1) {              // the lane's experts stay or go together
       const bool on = e0 < E && (kept >> (lane_groups ? sub >> gl_log : 0) & 1u);
@@ -538,33 +545,34 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     // ---- the picks' logits, and neighbours that 32 bits cannot tell apart
     int id[kPicks];
     float x[kPicks];
+    unsigned int below[kPicks];
     bool close = false;
 #pragma unroll
     for (int h = 0; h < kPicks; ++h) {
       id[h] = 255 - (int)(pick[h] & 255u);
       x[h] = h * G + sub <= k && pick[h] != 0 ? to_f(row[id[h]]) : -INFINITY;
-    }
-#pragma unroll
-    for (int h = 0; h < kPicks; ++h) {
-      const int src = tok * G + (sub + 1) % G;
-      unsigned int below = __shfl_sync(0xffffffffu, pick[h], src);
-      float xb = __shfl_sync(0xffffffffu, x[h], src);
+      below[h] = __shfl_sync(0xffffffffu, pick[h], tok * G + (sub + 1) % G);
       if (h + 1 < kPicks) {                          // (the last lane's neighbour is the first lane's next pick)
         const unsigned int w = __shfl_sync(0xffffffffu, pick[h + 1 < kPicks ? h + 1 : h], tok * G);
-        const float xw = __shfl_sync(0xffffffffu, x[h + 1 < kPicks ? h + 1 : h], tok * G);
-        if (sub == G - 1) {
-          below = w;
-          xb = xw;
-        }
+        if (sub == G - 1) below[h] = w;
       }
-      const int j = h * G + sub;                     // neighbours j and j + 1 (j + 1 == k: the first that is left out)
-      if (j < k && below != 0 && x[h] > -INFINITY && xb > -INFINITY && (pick[h] >> 8) - (below >> 8) <= near) {
-        // equal logits under equal biases are a true tie, in the right order already -- but at the border only if equal
-        // keys are equal logits
-        bool tie = x[h] == xb;
-        if (biased) tie = tie && s_bias[id[h]] == s_bias[255 - (int)(below & 255u)];
-        if (j + 1 == k) tie = tie && !biased && sizeof(T) == 2;
-        close |= !tie;
+      close |= h * G + sub < k && below[h] != 0 && (pick[h] >> 8) - (below[h] >> 8) <= near;
+    }
+    if (__any_sync(0xffffffffu, close)) {
+      close = false;
+#pragma unroll
+      for (int h = 0; h < kPicks; ++h) {
+        const int j = h * G + sub;                   // neighbours j and j + 1 (j + 1 == k: the first that is left out)
+        if (j < k && below[h] != 0 && x[h] > -INFINITY && (pick[h] >> 8) - (below[h] >> 8) <= near) {
+          const int eb = 255 - (int)(below[h] & 255u);
+          const float xb = to_f(row[eb]);
+          // equal logits under equal biases are a true tie, in the right order already -- but at the border only if
+          // equal keys are equal logits
+          bool tie = x[h] == xb || !(xb > -INFINITY);
+          if (biased && xb > -INFINITY) tie = tie && s_bias[id[h]] == s_bias[eb];
+          if (j + 1 == k && xb > -INFINITY) tie = tie && !biased && sizeof(T) == 2;
+          close |= !tie;
+        }
       }
     }
     const bool unsure = (__ballot_sync(0xffffffffu, close) >> (tok * G) & kMask) != 0;
@@ -646,7 +654,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
       const bool ratio = p.norm && (softmax || top < -64.f);
       const float ref = softmax || ratio ? (p.norm ? top : m) : 0.f;
       const float e = expf(softmax || ratio ? x[h] - ref : -x[h]);
-      w[h] = x[h] == -INFINITY ? 0.f : softmax || ratio ? e : 1.f / (1.f + e);
+      w[h] = x[h] == -INFINITY ? 0.f : softmax || ratio ? e : __fdividef(1.f, 1.f + e);
       sum += w[h];
     }
     float f = p.scale;
@@ -701,12 +709,12 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
 // experts several times over.  What needs the CTA's own pairs alone is done while the sums are on their way.
 constexpr int kPermCluster = 8;
 constexpr int kMaxRows = 5;                          // histograms a thread has in flight
-__global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRouteParams p, int n_ctas, int e_pad) {
+__global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRouteParams p, int n_ctas, int e_log) {
   __shared__ int s_hist[kWarps][DX_MAX_E];
   __shared__ int s_base[DX_MAX_E], s_total[DX_MAX_E];
   __shared__ int s_scan[kWarps];
   __shared__ int2 s_part[DX_MAX_E];
-  const int E = p.E, e = threadIdx.x % e_pad, seg = threadIdx.x / e_pad, segs = kThreads / e_pad;
+  const int E = p.E, e = threadIdx.x & ((1 << e_log) - 1), seg = threadIdx.x >> e_log, segs_log = kThreadsLog - e_log;
   const int rank = blockIdx.x % kPermCluster, first = blockIdx.x - rank;   // (clusters are runs of the grid)
   const long long t_lo = (long long)blockIdx.x * p.per_cta;
   const long long t_hi = min((long long)p.N, t_lo + p.per_cta);
@@ -719,9 +727,9 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
   const int32_t* col = p.counts + e;
   int front = 0, total = 0, near = 0;
   if (e < E) {
-    const int all_lo = (int)((long long)n_ctas * rank / kPermCluster);
-    const int all_hi = (int)((long long)n_ctas * (rank + 1) / kPermCluster);
-    const int lo = all_lo + (all_hi - all_lo) * seg / segs, hi = all_lo + (all_hi - all_lo) * (seg + 1) / segs;
+    const int all_lo = n_ctas * rank / kPermCluster;
+    const int all_hi = n_ctas * (rank + 1) / kPermCluster;
+    const int lo = all_lo + ((all_hi - all_lo) * seg >> segs_log), hi = all_lo + ((all_hi - all_lo) * (seg + 1) >> segs_log);
     for (int b = lo; b < hi; b += 4 * kMaxRows) {
       int c[4 * kMaxRows];
 #pragma unroll
@@ -733,8 +741,9 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
       }
     }
     // (the CTAs of the cluster in front of this one)
-    for (int r = seg; r < kPermCluster - 1; r += segs)
-      near += first + r < min((int)blockIdx.x, n_ctas) ? col[(size_t)(first + r) * E] : 0;
+#pragma unroll
+    for (int r = 0; r < kPermCluster - 1; ++r)
+      near += (r & ((1 << segs_log) - 1)) == seg && first + r < min((int)blockIdx.x, n_ctas) ? col[(size_t)(first + r) * E] : 0;
   }
   count_pairs(q, E, s_hist);
   if (e < E) {
@@ -975,7 +984,7 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
   if (e == cudaSuccess && perm && grid > 1) {
     const unsigned int padded = (unsigned)((grid + kPermCluster - 1) / kPermCluster * kPermCluster);
     e = dx_launch_pdl((ctx->pdl_mask & DX_PDL_ROUTE) != 0, dx_batch_permute_kernel, dim3(padded), dim3(kThreads), 0, st, kPermCluster, p, grid,
-                      p.E <= 32 ? 32 : p.E <= 64 ? 64 : p.E <= 128 ? 128 : 256);
+                      p.E <= 32 ? 5 : p.E <= 64 ? 6 : p.E <= 128 ? 7 : 8);
     *n_launches = 2;
   }
   return e;
