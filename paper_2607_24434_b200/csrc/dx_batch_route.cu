@@ -708,7 +708,6 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
 // of them, once over all CTAs (the experts' totals) and once over those in front of the cluster; its threads take the
 // experts several times over.  What needs the CTA's own pairs alone is done while the sums are on their way.
 constexpr int kPermCluster = 8;
-constexpr int kMaxRows = 5;                          // histograms a thread has in flight
 __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRouteParams p, int n_ctas, int e_log) {
   __shared__ int s_hist[kWarps][DX_MAX_E];
   __shared__ int s_base[DX_MAX_E], s_total[DX_MAX_E];
@@ -730,20 +729,19 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
     const int all_lo = n_ctas * rank / kPermCluster;
     const int all_hi = n_ctas * (rank + 1) / kPermCluster;
     const int lo = all_lo + ((all_hi - all_lo) * seg >> segs_log), hi = all_lo + ((all_hi - all_lo) * (seg + 1) >> segs_log);
-    for (int b = lo; b < hi; b += 4 * kMaxRows) {
-      int c[4 * kMaxRows];
-#pragma unroll
-      for (int i = 0; i < 4 * kMaxRows; ++i) c[i] = b + i < hi ? col[(size_t)(b + i) * E] : 0;
-#pragma unroll
-      for (int i = 0; i < 4 * kMaxRows; ++i) {
-        total += c[i];
-        front += b + i < first ? c[i] : 0;
-      }
+    // (short code: every instruction of this kernel comes out of L2 once, and that is a good part of its time)
+    const int32_t* at = col + (size_t)lo * E;
+#pragma unroll 8
+    for (int b = lo; b < hi; ++b, at += E) {
+      const int c = *at;
+      total += c;
+      front += b < first ? c : 0;
     }
-    // (the CTAs of the cluster in front of this one)
+    // (the CTAs of the cluster in front of this one; up to two experts per warp lane: four loads side by side)
+    at = col + (size_t)(first + seg) * E;
 #pragma unroll
-    for (int r = 0; r < kPermCluster - 1; ++r)
-      near += (r & ((1 << segs_log) - 1)) == seg && first + r < min((int)blockIdx.x, n_ctas) ? col[(size_t)(first + r) * E] : 0;
+    for (int i = 0; i < 4; ++i, at += (size_t)E << segs_log)
+      if (first + seg + (i << segs_log) < min((int)blockIdx.x, n_ctas)) near += *at;
   }
   count_pairs(q, E, s_hist);
   if (e < E) {
