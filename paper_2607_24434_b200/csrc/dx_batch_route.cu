@@ -530,15 +530,15 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     list[kEpl * 32] = 0u;
     unsigned int head = key[0];
     list += 32;
+#pragma unroll 1
+    for (int j = 0, at = sub; j <= k + 1; ++j, --at) {
+      const unsigned int top = lanes_umax<G>(head);
 #pragma unroll
-    for (int j = 0; j <= DX_MAX_TOPK + 1; ++j) {
-      if (j <= k + 1) {
-        const unsigned int top = lanes_umax<G>(head);
-        if (sub == j % G) pick[j / G] = top;
-        if (head == top && top != 0u) {
-          head = *list;
-          list += 32;
-        }
+      for (int h = 0; h < kPicks; ++h)
+        if (at == -h * G) pick[h] = top;             // (j == h * G + sub)
+      if (head == top && top != 0u) {
+        head = *list;
+        list += 32;
       }
     }
     __syncwarp();
