@@ -15,7 +15,7 @@
 
 namespace {
 
-constexpr int kUnroll = 4;
+constexpr int kUnroll = 3;
 constexpr float kSlack = 8.f;      // powers of two by which an element may exceed the reference of its thread's sums
 constexpr int kSegments = 8;      // parts of a thread's share of the row that have a maximum of their own
 constexpr int kFlagSlack = 12;    // the threshold may be reached by n + this many threads
@@ -219,19 +219,27 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
   float seg = -INFINITY;
   int g = 0, in_seg = 0;
   const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo + tid;
-#pragma unroll 1
-  for (int ch = 0; ch < chunks; ++ch, src += kUnroll * kRowThreads) {
-    uint4 v[kUnroll];
+  auto fetch = [&](uint4 (&x)[kUnroll], int ch) {
     if ((ch + 1) * (kUnroll * kRowThreads) <= n_vec) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) v[u] = load_stream(src + u * kRowThreads);
+      for (int u = 0; u < kUnroll; ++u) x[u] = load_stream(src + u * kRowThreads);
     } else {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        v[u] = none4;                                      // (adds nothing to any sum)
-        if ((ch * kUnroll + u) * kRowThreads + tid < n_vec) v[u] = load_stream(src + u * kRowThreads);
+        x[u] = none4;                                      // (adds nothing to any sum)
+        if ((ch * kUnroll + u) * kRowThreads + tid < n_vec) x[u] = load_stream(src + u * kRowThreads);
       }
     }
+    src += kUnroll * kRowThreads;
+  };
+  uint4 ahead[kUnroll];
+  fetch(ahead, 0);
+#pragma unroll 1
+  for (int ch = 0; ch < chunks; ++ch) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = ahead[u];
+    if (ch + 1 < chunks) fetch(ahead, ch + 1);
     const float top = V16::largest(v, kUnroll);
     if (ch == 0) {
       st.m = fmaxf(warp_max(top), -FLT_MAX);
