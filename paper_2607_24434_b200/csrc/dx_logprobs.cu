@@ -184,6 +184,8 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
   __shared__ float s_seg[kSegments][kRowThreads];          // largest element of each thread in each segment
   __shared__ unsigned long long s_cand[kCandCap + DX_MAX_TOP];
   __shared__ unsigned long long s_top[DX_MAX_TOP], s_out[DX_MAX_TOP];
+  __shared__ unsigned long long s_in[DX_ROW_CLUSTER_MAX * DX_MAX_TOP], s_floor;   // (first CTA) the lists of all CTAs
+  __shared__ Stats s_stats[DX_ROW_CLUSTER_MAX];
   __shared__ unsigned int s_keys[kRowThreads];
   __shared__ unsigned int s_tau;
   __shared__ int s_runs[kRunCap];
@@ -197,6 +199,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
   const float c = p.c;
   const int n = p.n_top;
 
+  if (C > 1) cluster_arrive();
   // ---- the pass over the row
   Stats st{-FLT_MAX, 0.f, 0.f};
   float best = -INFINITY;
@@ -416,52 +419,58 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     for (int w = 1; w < kRowWarps; ++w) x = join(x, s_warp[w], c);
     s_cta = x;
   }
-  // ---- the first CTA of the row joins and writes
+  // ---- the first CTA of the row joins and writes: the others put their sums and lists into its shared memory
   Stats x{0.f, 0.f, 0.f};
   if (C > 1) {
-    if (tid == 0) s_ncand = 0;
     __syncthreads();
-    cluster_arrive();
-    cluster_wait();
-    if (rank == 0) {
-      if (warp == 0) {
-        x = Stats{-FLT_MAX, 0.f, 0.f};
-        unsigned long long floor = 0;      // the n-th largest of any one CTA: at least n elements reach it
-        if (lane < C) {
-          const uint32_t a = cluster_addr(&s_cta, lane);
-          x = Stats{cluster_load_f32(a), cluster_load_f32(a + 4), cluster_load_f32(a + 8)};
-          if (n > 0) floor = cluster_load_u64(cluster_addr(&s_top[n - 1], lane));
-        }
-        x = warp_join(x, c);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-          const unsigned long long f = __shfl_xor_sync(0xffffffffu, floor, o);
-          floor = f > floor ? f : floor;
-        }
-        if (lane == 0) {
-          s_warp[0] = x;
-          s_cand[kCandCap] = floor;
-        }
-      }
-      __syncthreads();
-      const unsigned long long floor = s_cand[kCandCap];
-      for (int q = tid; q < C * n; q += kRowThreads) {
-        const unsigned long long k = cluster_load_u64(cluster_addr(&s_top[q % n], q / n));
-        if (k != 0 && k >= floor) s_cand[atomicAdd(&s_ncand, 1)] = k;
-      }
-      __syncthreads();
-      const int ncand = s_ncand;
-      for (int q = tid; q < ncand; q += kRowThreads) {
-        const unsigned long long k = s_cand[q];
-        int r = 0;
-        for (int y = 0; y < ncand; ++y) r += s_cand[y] > k;
-        if (r < n) s_out[r] = k;
-      }
+    cluster_wait();                                        // (all CTAs of the row have started)
+    if (tid < n) cluster_store_u64(cluster_addr(&s_in[rank * n + tid], 0), s_top[tid]);
+    if (tid == 0) {
+      const uint32_t a = cluster_addr(&s_stats[rank], 0);
+      cluster_store_f32(a, s_cta.m);
+      cluster_store_f32(a + 4, s_cta.s);
+      cluster_store_f32(a + 8, s_cta.a);
+      s_ncand = 0;
     }
     __syncwarp();
-    cluster_arrive();   // (this CTA has read all it wants of the others)
+    cluster_arrive();
     cluster_wait();
     if (rank != 0) return;
+    if (warp == 0) {
+      x = lane < C ? s_stats[lane] : Stats{-FLT_MAX, 0.f, 0.f};
+      // What at least n elements reach: the n-th of any one CTA, and the least of their m-th if m per CTA make n.
+      const int m = (n + C - 1) / C;
+      unsigned long long floor = 0, least = ~0ull;
+      if (n > 0 && lane < C) {
+        floor = s_in[lane * n + n - 1];
+        least = s_in[lane * n + m - 1];
+      }
+      x = warp_join(x, c);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) {
+        const unsigned long long f = __shfl_xor_sync(0xffffffffu, floor, o), l = __shfl_xor_sync(0xffffffffu, least, o);
+        floor = f > floor ? f : floor;
+        least = l < least ? l : least;
+      }
+      if (lane == 0) {
+        s_warp[0] = x;
+        s_floor = least > floor ? least : floor;
+      }
+    }
+    __syncthreads();
+    const unsigned long long floor = s_floor;
+    for (int q = tid; q < C * n; q += kRowThreads) {
+      const unsigned long long k = s_in[q];
+      if (k != 0 && k >= floor) s_cand[atomicAdd(&s_ncand, 1)] = k;
+    }
+    __syncthreads();
+    const int ncand = s_ncand;
+    for (int q = tid; q < ncand; q += kRowThreads) {
+      const unsigned long long k = s_cand[q];
+      int r = 0;
+      for (int y = 0; y < ncand; ++y) r += s_cand[y] > k;
+      if (r < n) s_out[r] = k;
+    }
   }
   __syncthreads();
   x = C > 1 ? s_warp[0] : s_cta;
