@@ -601,6 +601,106 @@ def test_binding_refusals(dx):
         assert err.value.status == status
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("N,V,k", [(400, 9001, 100), (310, 61003, 9), (40, 410001, 70)])
+def test_distill_rows_that_follow_one_another(dx, dtype, tail, N, V, k):
+    """More rows than run at a time, of an odd length (their alignment changes from row to row), rows of weight zero, of
+    no list and of NaN among them: what a CTA keeps from one row to the next must not show.  Rows
+    equal themselves in calls of their own, in a second call and in place."""
+    binding, ctx = dx
+    g = torch.Generator(device="cuda").manual_seed(N)
+    z = torch.randn((N, V), generator=g, device="cuda") * 2
+    z[5] = NAN
+    view = rows(z, dtype)
+    lp, ids = torch.log_softmax(torch.randn((N, V), generator=g, device="cuda") * 2, 1).topk(k, dim=1)
+    ids = ids.to(torch.int32).contiguous()
+    lp = lp.contiguous()
+    w = torch.rand((N,), generator=g, device="cuda") + 0.5
+    w[::3] = 0.0
+    ids[1::7] = -1
+    whole = binding.spec_distill_topk(ctx, view, ids, lp, tail=tail, row_weight=w)
+    again = binding.spec_distill_topk(ctx, view, ids, lp, tail=tail, row_weight=w)
+    bits = lambda t: t.view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)  # noqa: E731
+    assert torch.equal(bits(whole["dlogits"]), bits(again["dlogits"])) and torch.equal(bits(whole["loss"]), bits(again["loss"]))
+    for r in range(0, N, 97):
+        one = binding.spec_distill_topk(ctx, view[r:r + 1], ids[r:r + 1], lp[r:r + 1], tail=tail, row_weight=w[r:r + 1].contiguous())
+        live = bool(w[r] != 0) and bool((ids[r] >= 0).any())
+        if not live:
+            assert float(whole["loss"][r]) == 0 and not whole["dlogits"][r].any() and not one["dlogits"].any()
+        elif r != 5:
+            # (a lone row is split over more CTAs: other partial sums)
+            assert abs(float(one["loss"][0]) - float(whole["loss"][r])) <= 4 * S_ERR
+            diff = (one["dlogits"][0].double() - whole["dlogits"][r].double()).abs()
+            assert bool((diff <= 4 * S_ERR * float(w[r]) + 2 * HALF[dtype] * whole["dlogits"][r].double().abs()).all())
+    assert torch.isnan(whole["dlogits"][5]).all() == bool(w[5] != 0 and (ids[5] >= 0).any())
+    mine = rows(z, dtype)
+    binding.spec_distill_topk(ctx, mine, ids, lp, tail=tail, row_weight=w,
+                              out={"loss": torch.empty(N, device="cuda"), "dlogits": mine})
+    assert torch.equal(bits(mine.contiguous()), bits(whole["dlogits"]))
+
+
+@pytest.mark.parametrize("N,E,k,groups,keep,biased,dtype", [
+    (40000, 256, 8, 8, 4, True, torch.bfloat16), (40000, 256, 8, 1, 1, False, torch.bfloat16),
+    (120001, 32, 8, 1, 1, True, torch.float32), (33333, 64, 6, 4, 2, False, torch.float32),
+    (20000, 100, 7, 10, 3, True, torch.bfloat16), (30000, 64, 8, 1, 1, False, torch.bfloat16)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_route_large_batches_of_every_form(dx, N, E, k, groups, keep, biased, dtype, sigmoid):
+    """Selection in fp64 torch: thousands of tokens whose selection 32 bits cannot settle are among these."""
+    binding, ctx = dx
+    g = torch.Generator(device="cuda").manual_seed(N + E)
+    z = (torch.randn((N, E), generator=g, device="cuda") * 1.3).to(dtype)
+    bias = torch.randn((E,), generator=g, device="cuda") * 0.05 if biased else None
+    out = binding.moe_route_tokens(ctx, z, k, score_fn=int(sigmoid), select_bias=bias, n_groups=groups, topk_groups=keep,
+                                   group_score=1 if groups > 1 else 0, routed_scale=1.5)
+    x = z.double()
+    r = torch.sigmoid(x) if sigmoid else torch.softmax(x, 1)
+    v = x if bias is None else r + bias.double()
+    if groups > 1:
+        by = (r if bias is None else v).view(N, groups, -1).topk(2, dim=2).values.sum(2)
+        kept = torch.sort(by, dim=1, descending=True, stable=True).indices[:, :keep]
+        on = torch.zeros((N, groups), dtype=torch.bool, device="cuda").scatter_(1, kept, True)
+        v = v.masked_fill(~on.repeat_interleave(E // groups, 1), -INF)
+    ids = torch.sort(v, dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(out["topk_ids"].long(), ids)
+    w = r.gather(1, ids)
+    w = 1.5 * w / w.sum(1, keepdim=True)
+    assert bool(((out["topk_w"].double() - w).abs() <= GATE * w).all())
+    flat = ids.reshape(-1)
+    assert torch.equal(out["perm"].long(), torch.sort(flat, stable=True).indices)
+    assert out["offsets"].tolist() == [0] + torch.cumsum(torch.bincount(flat, minlength=E), 0).tolist()
+
+
+def test_results_do_not_depend_on_the_launch_overlap(dx):
+    binding, ctx = dx
+    z = torch.randn((5000, 64), device="cuda")
+    want = binding.moe_route_tokens(ctx, z, 6, score_fn=1)
+    for mask in (0, 1, 7):
+        ctx.set_launch_overlap(mask)
+        for _ in range(20):
+            got = binding.moe_route_tokens(ctx, z, 6, score_fn=1)
+            assert all(torch.equal(got[n], want[n]) for n in want)
+    ctx.set_launch_overlap(3)
+
+
+def test_first_call_of_a_context_inside_a_capture(dx):
+    binding, ctx = dx
+    s = _state(6, 30001, 5)
+    want = [t.clone() for t in _all_calls(binding, ctx, s)]
+    fresh = binding.Context(0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = _all_calls(binding, fresh, s)
+    for _ in range(50):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs, want))
+    assert fresh.device_status() == 0
+    del graph
+    fresh.close()
+
+
 # ---- the operators together: one training step of a small drafter --------------------------------------------------------
 def test_training_step_of_a_small_drafter(dx):
     """The target's logits are scored and cut to a top list; the drafter (a routed layer of linear experts and an LM
