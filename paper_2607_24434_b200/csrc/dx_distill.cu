@@ -13,6 +13,8 @@
 // stream the row.  The warps' sums go straight into the shared memory of all CTAs of the row, so that one cluster
 // barrier is all that stands between the sweep and the gradient.  Per-row scalars of the loss are 64-bit (it is a small
 // difference of logarithms) and are not waited for by the gradient.
+#include <cmath>
+
 #include "dx_rows.cuh"
 
 namespace {
@@ -650,9 +652,12 @@ cudaError_t dx_launch_distill(dx_ctx* ctx, const void* logits, int dtype, int N,
                               const int32_t* teacher_ids, const float* teacher_logprobs, int k, int tail,
                               float temperature, const float* row_weight, float* loss, void* dlogits, long long ld_d,
                               cudaStream_t st) {
+  // the first part rounded down, the second positive: a masked logit (-inf) stays -inf times either
   const double c = 1.4426950408889634 / (double)temperature;
+  float c_hi = (float)c;
+  if ((double)c_hi >= c) c_hi = nextafterf(c_hi, 0.f);
   DistillParams p{logits, N, V, k, tail, 0, ld, ld_d, teacher_ids, teacher_logprobs,
-                  (float)c, (float)(c - (double)(float)c), 1.0 / (double)temperature, (float)(1.0 / (double)temperature), row_weight, loss, dlogits, ctx->dev_status};
+                  c_hi, (float)(c - (double)c_hi), 1.0 / (double)temperature, (float)(1.0 / (double)temperature), row_weight, loss, dlogits, ctx->dev_status};
   if (dtype == DX_DTYPE_FP32) return dlogits ? launch_lists<float, true>(ctx, p, st) : launch_lists<float, false>(ctx, p, st);
   return dlogits ? launch_lists<__nv_bfloat16, true>(ctx, p, st) : launch_lists<__nv_bfloat16, false>(ctx, p, st);
 }

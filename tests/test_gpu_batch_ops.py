@@ -296,6 +296,22 @@ def test_distill_masks_infinities_nan_and_odd_lists(dx, dtype, tail, V):
     assert torch.isnan(got["dlogits"][11]).all() and torch.isnan(got["loss"][11])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [1e-4, 0.03, 0.7, 0.9, 1.1, 1.3, 1.7, 3.0, 5.0, 7.7, 100.0, 1e4])
+def test_temperatures(dx, dtype, T):
+    """Over the whole range, with masked words: log2(e) / T rounds up for some temperatures and down for others."""
+    z = draw_logits(31, 6, 3000)
+    z[1, 100:200] = -INF
+    z[2, 1:] = -INF
+    z[3, 5:] = torch.finfo(dtype).min
+    ids, lp = teacher_lists(32, z.clamp(min=-50), 9, ragged=False)
+    ids[2, 0], ids[2, 1] = 0, -1
+    view = rows(z, dtype, 1)
+    check_logprobs(dx, view, [1, 2, 0, 3, 2999, -1], 12, T)
+    check_distill(dx, view, ids, lp, True, T)
+    check_distill(dx, view, ids, lp, False, T)
+
+
 def test_distill_whole_vocabulary_listed(dx):
     z = draw_logits(14, 3, 100)
     ids, lp = teacher_lists(15, z, 100, ragged=False)
