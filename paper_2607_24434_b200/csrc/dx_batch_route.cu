@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
       hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
     bias_abs = fmaxf(fabsf(lo), fabsf(hi));
-    // value -> 2^23 + quanta: the low 23 bits of the float are the quanta (at least 8, masked experts have 1: key_add's
+    // value -> 2^23 + quanta: the low 24 bits of the float are the quanta, bit 23 being zero (at least 8, masked experts have 1: key_add's
     // share is rounded, by less than 4 up to the bound that follows)
     key_mul = 8388000.f / (1.f + hi - lo);
     const float shift = 8.f - lo * key_mul;
@@ -493,21 +493,18 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     for (int i = 0; i < kEpl; ++i) {
       const unsigned int id = (unsigned int)(255 - e0 - i);
       if (biased) {   // (not a number, or below: masked)
-        key[i] = __byte_perm(__float_as_uint(fmaxf(fmaf(z[i], key_mul, key_add), 8388609.f)) & 0x7fffffu, id, 0x2104);
+        key[i] = __byte_perm(__float_as_uint(fmaxf(fmaf(z[i], key_mul, key_add), 8388609.f)), id, 0x2104);
       } else {
         key[i] = __byte_perm(dx_orderable(z[i] + 0.f), id, 0x3214);
       }
     }
-    if (lane_groups || p.groups == 1) {              // the lane's experts stay or go together
-      const bool on = e0 < E && (kept >> (lane_groups ? sub >> gl_log : 0) & 1u);
-#pragma unroll
-      for (int i = 0; i < kEpl; ++i) key[i] = on ? key[i] : 0u;
-    }
+    // (where the lane's experts stay or go together, it is enough that the lane has no first key)
+    const bool on = e0 < E && (p.groups == 1 || !lane_groups || (kept >> (sub >> gl_log) & 1u));
     if (!lane_groups && (p.groups > 1 || (E & (kEpl - 1)) != 0)) {
 #pragma unroll
       for (int i = 0; i < kEpl; ++i) {
-        const bool on = e0 + i < E && (kept >> s_gid[min(e0 + i, DX_MAX_E - 1)] & 1u);
-        key[i] = on ? key[i] : 0u;
+        const bool in = e0 + i < E && (kept >> s_gid[min(e0 + i, DX_MAX_E - 1)] & 1u);
+        key[i] = in ? key[i] : 0u;
       }
     }
     // ---- the lane's keys in descending order (19 exchanges)
@@ -528,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
 #pragma unroll
     for (int i = 1; i < kEpl; ++i) list[i * 32] = key[i];
     list[kEpl * 32] = 0u;
-    unsigned int head = key[0];
+    unsigned int head = on ? key[0] : 0u;
     list += 32;
 #pragma unroll 1
     for (int j = 0, at = sub; j <= k + 1; ++j, --at) {
