@@ -417,7 +417,8 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *               unlisted words: L_t = sum_j p_j (log p_j - log q_j) + r (log r - log R).
  *   loss [N] = L_t.  dlogits (pitch ld_d) = row_weight[t] * dL_t / dlogits, zeros and loss 0 for rows whose weight is 0
  *   or that list no word (their logits are not looked at).  row_weight NULL: all 1.  loss or dlogits may be NULL.
- *   dlogits may be the logits buffer itself (same pitch); it must not overlap it otherwise (DX_ERR_INVALID_ARG).
+ *   dlogits may be the logits buffer itself (same pitch), or lie between its rows; its rows must not overlap the logits'
+ *   otherwise (DX_ERR_INVALID_ARG).
  *   A listed word that the student gives no mass makes the loss +inf (its gradient stays finite); a row of nothing but
  *   -inf has loss +inf and gradient 0.  A row must fit the shared memory of 16 SMs (about 1.8 million bf16 logits;
  *   DX_ERR_UNSUPPORTED beyond).

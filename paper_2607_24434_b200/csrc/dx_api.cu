@@ -839,7 +839,12 @@ bool rows_overlap(const void* a, int64_t ld_a, const void* b, int64_t ld_b, int3
   const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
   const uintptr_t a1 = a0 + (uintptr_t)(((int64_t)(N - 1) * ld_a + len) * elem);
   const uintptr_t b1 = b0 + (uintptr_t)(((int64_t)(N - 1) * ld_b + len) * elem);
-  return a0 < b1 && b0 < a1;
+  if (!(a0 < b1 && b0 < a1)) return false;
+  if (ld_a != ld_b || N == 1) return true;
+  // one pitch: rows of the one may lie between the rows of the other
+  const int64_t pitch = ld_a * elem, row = (int64_t)len * elem;
+  const int64_t d = (((int64_t)(b0 - a0)) % pitch + pitch) % pitch;
+  return d < row || d > pitch - row;
 }
 bool temperature_ok(float t) { return t >= 1e-4f && t <= 1e4f; }
 
@@ -887,7 +892,7 @@ extern "C" dx_status spec_distill_topk(dx_ctx* ctx, const void* logits, int32_t 
   dx_status s = check_rows(logits, dtype, N, V, ld);
   if (s != DX_OK) return s;
   if (k < 1) return DX_ERR_SHAPE;
-  if (k > DX_MAX_TEACHER) return DX_ERR_UNSUPPORTED;
+  if (k > DX_MAX_TEACHER || N > DX_MAX_ROWS) return DX_ERR_UNSUPPORTED;
   const int64_t elem = dtype == DX_DTYPE_FP32 ? 4 : 2;
   if ((uint64_t)V * (uint64_t)elem > (uint64_t)dx_distill_max_row_bytes(ctx)) return DX_ERR_UNSUPPORTED;
   if (dlogits) {

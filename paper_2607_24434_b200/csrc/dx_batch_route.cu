@@ -973,7 +973,7 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
   const int turn = kWarps * (32 / lanes);
   const int max_ctas = DX_ROUTE_CTAS_PER_SM * ctx->sm_count;
   p.per_cta = N <= 64 ? N : (int)((((long long)N + max_ctas - 1) / max_ctas + turn - 1) / turn * turn);
-  const int grid = (N + p.per_cta - 1) / p.per_cta;
+  const int grid = (int)(((long long)N + p.per_cta - 1) / p.per_cta);
   cudaError_t e = dtype == DX_DTYPE_FP32 ? launch_route<float>(grid, p, st) : launch_route<__nv_bfloat16>(grid, p, st);
   *n_launches = 1;
   if (e == cudaSuccess && perm && grid > 1) {

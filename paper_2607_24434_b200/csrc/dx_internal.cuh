@@ -19,6 +19,7 @@
 #define DX_TILE_I 8            // intermediate rows per streamed weight tile
 #define DX_MAX_M 16            // accept rows
 #define DX_MAX_TOP 32          // alternatives per row of spec_token_logprobs
+#define DX_MAX_ROWS 0x7ff00000 // rows of spec_distill_topk (a row number plus the rows in flight fits 32 bits)
 #define DX_MAX_TEACHER 128     // teacher entries per row of spec_distill_topk
 #define DX_ROW_CLUSTER_MAX 16  // CTAs that share a row of logits
 #define DX_ROW_SLICE_BYTES 106000  // ... and the bytes of it one CTA holds when there are many rows (two CTAs per SM)

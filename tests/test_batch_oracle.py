@@ -154,6 +154,11 @@ def test_distill_refusals(lib):
     assert call(ids=None) == 1 and call(lp=None) == 1 and call(loss=None, d=None) == 1
     assert call(d=4096, ld_d=101) == 1                     # the logits buffer at another pitch
     assert call(d=4096 + 200) == 1 and call(d=4096 + 398) == 1 and call(d=4096 - 2) == 1
+    # between rows of a larger pitch: one element short of the room is refused (room enough goes on to the device)
+    assert call(ld=199, ld_d=199, d=4096 + 200) == 1 and call(ld=200, ld_d=200, d=4096 + 198) == 1
+    assert call(ld=200, ld_d=200, d=4096 + 200) == 3 and call(ld=200, ld_d=200, d=4096 - 200) == 3
+    assert call(ld=200, ld_d=201, d=4096 + 200) == 1
+    assert call(N=0x7ff00001) == 8
     assert call(d=4097) == 1
     assert call(N=0, logits=None, ids=None, lp=None, loss=None, d=None) == 0
 

@@ -321,6 +321,21 @@ def test_distill_whole_vocabulary_listed(dx):
     assert torch.isinf(got["loss"]).all() and torch.isfinite(got["dlogits"]).all()
 
 
+def test_distill_gradient_between_the_logits_rows(dx):
+    binding, ctx = dx
+    N, V = 20, 3001
+    z = draw_logits(33, N, V)
+    ids, lp = teacher_lists(34, z, 8, ragged=False)
+    buf = torch.zeros((N, 2 * V + 3), device="cuda")
+    buf[:, :V] = z.cuda()
+    got = binding.spec_distill_topk(ctx, buf[:, :V], ids.cuda(), lp.cuda(),
+                                    out={"loss": torch.empty(N, device="cuda"), "dlogits": buf[:, V:2 * V]})
+    want = binding.spec_distill_topk(ctx, z.cuda(), ids.cuda(), lp.cuda())
+    assert torch.equal(buf[:, :V].cpu(), z) and not buf[:, 2 * V:].any()
+    # (rows at other offsets from a vector's border add up in another order)
+    assert bool(((got["dlogits"].double() - want["dlogits"].double()).abs() <= 4 * S_ERR).all())
+
+
 def test_distill_bad_ids_and_sizes(dx):
     binding, ctx = dx
     z = draw_logits(16, 2, 50)
@@ -479,6 +494,22 @@ def test_route_nan_and_infinite_logits_keep_the_ids_valid(dx):
                 assert torch.equal(out["perm"].cpu().long(), torch.sort(flat, stable=True).indices)
     ids = binding.moe_route_tokens(ctx, z[:1].cuda(), 8, score_fn=1)["topk_ids"][0].tolist()
     assert 5 not in ids                                   # NaN behind everything else
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_route_biases_far_from_the_scores(dx, dtype):
+    """Biases whose common part leaves a 32-bit sum nothing of the scores: the selection is still exact."""
+    z = draw_logits(35, 70, 64, scale=1.2).clamp(-9, 9)
+    small = torch.randn((64,), generator=torch.Generator().manual_seed(36)) * 0.01
+    for bias in (small + 50.0, small - 3000.0, small * 1e6, torch.full((64,), 1e30), small.clone().fill_(-INF)):
+        for sigmoid in (False, True):
+            ref_bias = bias
+            if not torch.isfinite(bias).all():
+                out = dx[0].moe_route_tokens(dx[1], rows(z, dtype), 6, score_fn=int(sigmoid), select_bias=bias.cuda())
+                assert torch.equal(out["topk_ids"].cpu(), torch.arange(6, dtype=torch.int32).expand(70, 6))
+                continue
+            check_route(dx, rows(z, dtype), 6, sigmoid, True, 1.0, ref_bias)
+            check_route(dx, rows(z, dtype), 6, sigmoid, True, 1.0, ref_bias, groups=8, keep=3, top2=True)
 
 
 def test_route_no_tokens_and_optional_outputs(dx):
