@@ -786,6 +786,9 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
 // sigmoid: dz_e = dL/dr_e r_e (1 - r_e);  softmax: dz_e = r_e (dL/dr_e - sum_j dL/dr_j r_j), dL/dr zero for experts that
 // were not selected.  For renormalised gates that last sum is zero, so only softmax gates that are not renormalised
 // have a gradient outside the selection, and only they need the whole row of logits.
+constexpr int kGradThreads = 256;
+constexpr int kGradWarps = kGradThreads / 32;
+
 struct RouteGradParams {
   const void* logits;
   int N, E, k;
@@ -840,14 +843,14 @@ __device__ __forceinline__ float sum_duplicates(int id, float g, int tok, int k)
 // Gradients that are zero outside the selection: a warp takes four tokens, eight lanes for the pairs of each, writes
 // the zeros of their rows with all lanes and then the selected experts' places.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dx_route_grad_sparse_kernel(RouteGradParams p) {
+__global__ void __launch_bounds__(kGradThreads) dx_route_grad_sparse_kernel(RouteGradParams p) {
   constexpr int G = DX_MAX_TOPK, kTok = 32 / G, kN = 16 / sizeof(T);
   const int lane = threadIdx.x & 31, sub = lane % G, tok = lane / G;
   const int E = p.E;
   const bool softmax = p.score_fn == DX_SCORE_SOFTMAX;
-  const long long warps = (long long)gridDim.x * kWarps;
+  const long long warps = (long long)gridDim.x * kGradWarps;
 #pragma unroll 1
-  for (long long t0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kTok; t0 < p.N; t0 += warps * kTok) {
+  for (long long t0 = ((long long)blockIdx.x * kGradWarps + (threadIdx.x >> 5)) * kTok; t0 < p.N; t0 += warps * kTok) {
     const bool active = t0 + tok < p.N;
     const long long t = active ? t0 + tok : p.N - 1;
     const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
@@ -887,13 +890,13 @@ __global__ void __launch_bounds__(kThreads) dx_route_grad_sparse_kernel(RouteGra
 
 // Softmax gates that are not renormalised: every expert's logit has a gradient.  G lanes per token, at least eight.
 template <typename T, int G>
-__global__ void __launch_bounds__(kThreads) dx_route_grad_dense_kernel(RouteGradParams p) {
+__global__ void __launch_bounds__(kGradThreads) dx_route_grad_dense_kernel(RouteGradParams p) {
   constexpr int kTok = 32 / G;
   const int lane = threadIdx.x & 31, sub = lane % G, tok = lane / G;
   const int E = p.E, e0 = sub * kEpl;
-  const long long warps = (long long)gridDim.x * kWarps;
+  const long long warps = (long long)gridDim.x * kGradWarps;
 #pragma unroll 1
-  for (long long t0 = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kTok; t0 < p.N; t0 += warps * kTok) {
+  for (long long t0 = ((long long)blockIdx.x * kGradWarps + (threadIdx.x >> 5)) * kTok; t0 < p.N; t0 += warps * kTok) {
     const bool active = t0 + tok < p.N;
     const long long t = active ? t0 + tok : p.N - 1;
     const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
@@ -940,10 +943,10 @@ cudaError_t launch_route(int grid, const BatchRouteParams& p, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t launch_grad(int grid, const RouteGradParams& p, cudaStream_t st) {
-  if (p.score_fn != DX_SCORE_SOFTMAX || p.norm) dx_route_grad_sparse_kernel<T><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 8 * kEpl) dx_route_grad_dense_kernel<T, 8><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 16 * kEpl) dx_route_grad_dense_kernel<T, 16><<<grid, kThreads, 0, st>>>(p);
-  else dx_route_grad_dense_kernel<T, 32><<<grid, kThreads, 0, st>>>(p);
+  if (p.score_fn != DX_SCORE_SOFTMAX || p.norm) dx_route_grad_sparse_kernel<T><<<grid, kGradThreads, 0, st>>>(p);
+  else if (p.E <= 8 * kEpl) dx_route_grad_dense_kernel<T, 8><<<grid, kGradThreads, 0, st>>>(p);
+  else if (p.E <= 16 * kEpl) dx_route_grad_dense_kernel<T, 16><<<grid, kGradThreads, 0, st>>>(p);
+  else dx_route_grad_dense_kernel<T, 32><<<grid, kGradThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 bool rows_aligned(const void* base, long long ld, int elem) {
@@ -994,9 +997,9 @@ cudaError_t dx_launch_route_grad(dx_ctx* ctx, const dx_route_desc& d, const void
                     ctx->dev_status};
   // four tokens per warp and turn, fewer where every expert's logit has a gradient and E takes more lanes
   const bool dense = d.score_fn == DX_SCORE_SOFTMAX && !d.norm_topk;
-  const int turn = kWarps * (!dense || d.n_experts <= 8 * kEpl ? 4 : d.n_experts <= 16 * kEpl ? 2 : 1);
+  const int turn = kGradWarps * (!dense || d.n_experts <= 8 * kEpl ? 4 : d.n_experts <= 16 * kEpl ? 2 : 1);
   long long grid = ((long long)N + turn - 1) / turn;
-  const long long most = 4ll * ctx->sm_count;
+  const long long most = 8ll * ctx->sm_count;
   if (grid > most) grid = most;
   return dtype == DX_DTYPE_FP32 ? launch_grad<float>((int)grid, p, st) : launch_grad<__nv_bfloat16>((int)grid, p, st);
 }

@@ -92,35 +92,45 @@ struct Picker {
   unsigned long long* cand;             // [kCandCap + DX_MAX_TOP]
   int* n_cand;
 
-  __device__ __forceinline__ void offer(float z, int idx, unsigned long long floor) const {
-    const unsigned long long k = top_key(z, idx);
-    if (k >= floor) {
+  // (`least`: the smallest value wanted; a NaN is taken where -inf is)
+  __device__ __forceinline__ void offer(float z, int idx, float least) const {
+    if (!(z < least) && (z == z || least == -INFINITY)) {
       const int q = atomicAdd(n_cand, 1);
-      if (q < kCandCap) cand[q] = k;
+      if (q < kCandCap) cand[q] = top_key(z, idx);
     }
   }
-  // every element of the listed runs with a key of at least `floor`
-  __device__ __forceinline__ void rescan(const int* runs, int n_runs, unsigned long long floor) const {
+  // every element of the listed runs that is not below `least`
+  __device__ __forceinline__ void rescan(const int* runs, int n_runs, float least) const {
     using V16 = RowVec<T>;
-    for (int x = threadIdx.x; x < n_runs * seg_vecs; x += kRowThreads) {
-      const int run = runs[x / seg_vecs];
-      const int v = sp.v_lo + run % kRowThreads + (run / kRowThreads * seg_vecs + x % seg_vecs) * kRowThreads;
-      if (v < sp.v_hi) {
-        const uint4 w = row_vec(row, sp, v);
-        if (top_key(V16::largest(w), 0) >= floor) {
+    const float inv = 1.f / (float)seg_vecs;
+    const int items = n_runs * seg_vecs;
+#pragma unroll 1
+    for (int x = threadIdx.x; x < items; x += 2 * kRowThreads) {
+      int v[2];
+      uint4 w[2];
 #pragma unroll
-          for (int q = 0; q < V16::kN / 2; ++q) {
-            float x0, x1;
-            f2_unpack(V16::pair(w, q), x0, x1);
-            offer(x0, sp.head + v * V16::kN + 2 * q, floor);
-            offer(x1, sp.head + v * V16::kN + 2 * q + 1, floor);
-          }
+      for (int h = 0; h < 2; ++h) {
+        const int y = x + h * kRowThreads, r = (int)(((float)y + 0.5f) * inv);   // y / seg_vecs
+        const int run = y < items ? runs[r] : 0;
+        v[h] = sp.v_lo + run % kRowThreads + (run / kRowThreads * seg_vecs + y - r * seg_vecs) * kRowThreads;
+        if (y >= items || v[h] >= sp.v_hi) v[h] = -1;
+        if (v[h] >= 0) w[h] = row_vec(row, sp, v[h]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (v[h] < 0 || (V16::largest(w[h]) < least)) continue;
+#pragma unroll
+        for (int q = 0; q < V16::kN / 2; ++q) {
+          float x0, x1;
+          f2_unpack(V16::pair(w[h], q), x0, x1);
+          offer(x0, sp.head + v[h] * V16::kN + 2 * q, least);
+          offer(x1, sp.head + v[h] * V16::kN + 2 * q + 1, least);
         }
       }
     }
-    if (rank == 0 && threadIdx.x < sp.head) offer(element(row, threadIdx.x), threadIdx.x, floor);
+    if (rank == 0 && threadIdx.x < sp.head) offer(element(row, threadIdx.x), threadIdx.x, least);
     if (rank == C - 1 && threadIdx.x < sp.tail)
-      offer(element(row, V - sp.tail + threadIdx.x), V - sp.tail + threadIdx.x, floor);
+      offer(element(row, V - sp.tail + threadIdx.x), V - sp.tail + threadIdx.x, least);
   }
   // the first n elements, in the order of their ids, whose key has the high word `hi`; returns how many there are
   // (at most n), their keys in out[0 .. )
@@ -326,16 +336,24 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
         some = __reduce_or_sync(0xffffffffu, some);
         all = __reduce_and_sync(0xffffffffu, all);
         const int same = __clz(some ^ all);
-        tau = same == 0 ? 0u : same >= 32 ? some : some & ~(0xffffffffu >> same);
-        for (int b = 31 - same; b >= 0 && count > enough; --b) {
-          const unsigned int cand = tau | (1u << b);
-          int r = 0;
+        const int first = (31 - same) | 1;                 // (-1: all keys are equal)
+        tau = first < 0 ? some : some & ~((2u << first) - 1u);
+        // (two bits at a time: the three counts of one step share a reduction)
+        for (int b = first; b > 0 && count > enough; b -= 2) {
+          const unsigned int step = 1u << (b - 1);
+          unsigned int r = 0;
 #pragma unroll
-          for (int q = 0; q < kRowThreads / 32; ++q) r += k[q] >= cand;
+          for (int q = 0; q < kRowThreads / 32; ++q)
+            r += (k[q] >= tau + step) + (k[q] >= tau + 2 * step) * 1024u + (k[q] >= tau + 3 * step) * (1024u * 1024u);
           r = __reduce_add_sync(0xffffffffu, r);
-          if (r >= n) {
-            tau = cand;
-            count = r;
+#pragma unroll
+          for (int h = 2; h >= 0; --h) {
+            const int reached = (int)(r >> (10 * h) & 1023u);
+            if (reached >= n) {
+              tau += (unsigned int)(h + 1) * step;
+              count = reached;
+              break;
+            }
           }
         }
         if (tau == 0) tau = 1;
@@ -361,7 +379,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
       }
     }
     __syncthreads();
-    pick.rescan(s_runs, min(s_nrun, kRunCap), (unsigned long long)low << 32);
+    pick.rescan(s_runs, min(s_nrun, kRunCap), low <= 0x007fffffu ? -INFINITY : key_value((unsigned long long)low << 32));
     __syncthreads();
     int ncand = s_ncand;
     if (ties && ncand <= kCandCap) {
