@@ -432,8 +432,8 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *     topk_ids [N, k], topk_w [N, k] = routed_scale * r_e, or routed_scale * r_e / sum of the selected (norm_topk).
  *     offsets [E+1] and perm [N*k] as in moe_verify_block (both or neither may be NULL).
  *   A logit of -inf is a masked expert: selected only where too few others are left, with gate weight 0 (so is a whole
- *   row of them), whatever its bias; a NaN is selected like a masked expert.  E <= 256, k <= 8, n_groups <= 32,
- *   N * k < 2^31.
+ *   row of them), whatever its bias; a NaN is selected like a masked expert, and so is an expert whose bias is -inf or
+ *   NaN (its gate weight stays that of its logit).  E <= 256, k <= 8, n_groups <= 32, N * k < 2^31.
  * moe_route_tokens_backward: d_logits [N, E] (pitch ld_d, type of the logits, written whole) from the gradient of topk_w,
  *   for the selection in topk_ids (which has no gradient).  An id outside [0, E) is left out and reported as
  *   DX_DEV_BAD_EXPERT_ID; an expert listed twice gets both gradients.  d_logits must not overlap the logits. */

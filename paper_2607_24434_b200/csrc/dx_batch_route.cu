@@ -357,7 +357,8 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
   dx_pdl_trigger();            // (the permutation waits for this kernel's end before it reads anything)
   for (int e = threadIdx.x; e < DX_MAX_E; e += kThreads) {
     s_count[e] = 0;
-    s_bias[e] = biased && e < E ? p.bias[e] : 0.f;
+    const float b = biased && e < E ? p.bias[e] : 0.f;
+    s_bias[e] = b == b ? b : -INFINITY;              // (a NaN would be in no place of any order)
     s_gid[e] = (unsigned char)(min(e, E - 1) / per);
   }
   __syncthreads();
@@ -368,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
   if (biased) {
     float lo = INFINITY, hi = -INFINITY;
     for (int e = lane; e < E; e += 32) {
-      lo = fminf(lo, s_bias[e]);
+      if (s_bias[e] > -INFINITY) lo = fminf(lo, s_bias[e]);   // (experts at -inf get the key of the masked ones)
       hi = fmaxf(hi, s_bias[e]);
     }
 #pragma unroll

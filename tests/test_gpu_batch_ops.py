@@ -512,6 +512,28 @@ def test_route_biases_far_from_the_scores(dx, dtype):
             check_route(dx, rows(z, dtype), 6, sigmoid, True, 1.0, ref_bias, groups=8, keep=3, top2=True)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("N,E,k,off,groups,keep", [
+    (1, 8, 7, 3, 1, 1),                                   # all experts but one are selected, three of them without a bias
+    (9, 8, 8, 8, 1, 1), (70, 8, 7, 4, 2, 2), (300, 64, 6, 40, 1, 1), (300, 64, 6, 40, 8, 3), (33, 130, 8, 126, 1, 1),
+    (130, 256, 8, 100, 8, 4), (20, 30, 5, 12, 5, 2),
+])
+def test_route_experts_put_aside_by_their_bias(dx, dtype, sigmoid, N, E, k, off, groups, keep):
+    """Biases of -inf and NaN beside finite ones: such experts are selected last, in the order of their ids."""
+    z = draw_logits(37 + E, N, E, scale=1.2).clamp(-9, 9)
+    bias = torch.randn((E,), generator=torch.Generator().manual_seed(38)) * 0.05
+    aside = torch.randperm(E, generator=torch.Generator().manual_seed(39))[:off]
+    for values in ((NAN,), (-INF,), (-INF, NAN)):
+        bias[aside] = torch.tensor(values).repeat(off)[:off]
+        plain = torch.where(torch.isnan(bias), torch.full_like(bias, -INF), bias)
+        for top2 in (False, True):
+            out = dx[0].moe_route_tokens(dx[1], rows(z, dtype), k, score_fn=int(sigmoid), select_bias=bias.cuda(),
+                                         n_groups=groups, topk_groups=keep, group_score=int(top2))
+            want = check_route(dx, rows(z, dtype), k, sigmoid, True, 1.0, plain, groups, keep, top2)
+            assert all(torch.equal(out[name], want[name]) for name in want)
+
+
 def test_route_no_tokens_and_optional_outputs(dx):
     binding, ctx = dx
     empty = binding.moe_route_tokens(ctx, torch.empty((0, 16), device="cuda"), 4)
