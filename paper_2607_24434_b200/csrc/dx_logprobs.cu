@@ -110,7 +110,9 @@ struct Picker {
       uint4 w[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int y = x + h * kRowThreads, r = (int)(((float)y + 0.5f) * inv);   // y / seg_vecs
+        const int y = x + h * kRowThreads;
+        int r = (int)(((float)y + 0.5f) * inv);           // y / seg_vecs, one off at most where y passes 24 bits
+        r += (y >= (r + 1) * seg_vecs) - (y < r * seg_vecs);
         const int run = y < items ? runs[r] : 0;
         v[h] = sp.v_lo + run % kRowThreads + (run / kRowThreads * seg_vecs + y - r * seg_vecs) * kRowThreads;
         if (y >= items || v[h] >= sp.v_hi) v[h] = -1;
