@@ -10,7 +10,7 @@
 // The selection is that of exact arithmetic.  It is made on unique 32-bit keys first: a lane holds eight consecutive
 // experts, whose keys are 24 bits of the value and the reversed expert id -- with a bias the value's place between the
 // smallest and the largest that a score plus a bias can have, without one the leading bits of the logit (all of a bf16
-// logit).  A sorting network and k + 2 rounds of a maximum over the token's lanes put them in order.  Where two
+// logit).  A sorting network and k + 1 rounds of a maximum over the token's lanes put them in order.  Where two
 // neighbours of the result are closer than keys and arithmetic can tell apart (a few tokens in a thousand), the picks are
 // put in order by their 64-bit values, and where that cannot settle it the whole warp makes the token's selection again
 // in 64 bits.
@@ -114,12 +114,20 @@ __device__ __forceinline__ float lanes_sum(float v) {
 }
 template <int G>
 __device__ __forceinline__ unsigned int lanes_umax(unsigned int v) {
-  if (G == 32) return __reduce_max_sync(0xffffffffu, v);
+  if constexpr (G == 32) {
+    return __reduce_max_sync(0xffffffffu, v);
+  } else {
 #pragma unroll
-  for (int o = G / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
+    for (int o = G / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  }
 }
 
+__device__ __forceinline__ float min_nan(float a, float b) {   // a NaN on either side stays
+  float y;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
 __device__ __forceinline__ float sigmoid_f(float z) { return 1.f / (1.f + expf(-z)); }
 
 // Larger double -> larger integer; -inf (masked experts) -> 1 or more, 0 is left for what is excluded.
@@ -128,58 +136,72 @@ __device__ __forceinline__ unsigned long long orderable64(double v) {
   return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-// The selection of one token in 64 bits by a whole warp: lane j < k returns the j-th id.  s_row: E doubles of the warp.
-// A lane has the experts lane, lane + 32, ...; what depends on nothing else is done for all eight side by side (64-bit
-// arithmetic has long latencies, and a kernel ends with the last token that comes here).
+// Puts a token right that 32 bits cannot settle, by a whole warp: lane j < k returns the j-th id.  Lane j <= k has the
+// token's j-th pick, `behind` is the key after those, s_row holds E doubles of the warp.
+//   The true selection is among the first k + 1 picks unless the key behind them is as close to the border as well; then
+// their exact values put them in order: the logits, or the sigmoid in 64 bits and the bias.  Otherwise (`whole`, or a
+// softmax's scores, which need the whole row) the selection is made again from the logits in 64 bits.
+//   Loops stay rolled and exponentials are calls: few tokens come here, each of them brings this code in from L2 once
+// per SM, and the kernel ends with the last one (16384 x 64 fp32, selection alone: 9.8 us unrolled).
+__device__ __noinline__ double exact_exp(double x) { return exp(x); }
+__device__ __noinline__ double exact_sigmoid(double x) { return 1.0 / (1.0 + exact_exp(-x)); }
 template <typename T>
-__device__ __noinline__ int select_exact(const BatchRouteParams& p, const T* row, double* s_row) {
+__device__ __noinline__ int settle(const BatchRouteParams& p, const T* row, double* s_row, unsigned int pick,
+                                   unsigned int behind, bool whole, unsigned int near) {
   const int lane = threadIdx.x & 31;
+  const bool softmax = p.score_fn == DX_SCORE_SOFTMAX;
+  const unsigned int border = __shfl_sync(0xffffffffu, pick, p.k - 1);
+  whole = whole || (p.bias && softmax) || (behind != 0 && (border >> 8) - (behind >> 8) <= near);
+  if (!whole) {
+    const int id = pick != 0 ? 255 - (int)(pick & 255u) : DX_MAX_E;
+    const float x = pick != 0 ? to_f(row[id]) : -INFINITY;
+    double v = (double)x;
+    if (p.bias && x > -INFINITY) v = exact_sigmoid(v) + (double)p.bias[id];
+    if (!(x > -INFINITY) || !(v == v)) v = -INFINITY;   // (nothing that is not a number is compared)
+    int rank = 0;
+#pragma unroll 1
+    for (int j = 0; j <= p.k; ++j) {
+      const double o = __shfl_sync(0xffffffffu, v, j);
+      const int oe = __shfl_sync(0xffffffffu, id, j);
+      rank += o > v || (o == v && oe < id);
+    }
+    int* order = reinterpret_cast<int*>(s_row);
+    __syncwarp();
+    if (pick != 0) order[rank] = id;
+    __syncwarp();
+    const int mine = order[lane];
+    __syncwarp();
+    return mine;
+  }
   const bool scores = p.bias != nullptr || (p.groups > 1 && p.group_score != DX_GROUP_MAX);
-  float z[kEpl];
-  double v[kEpl];                                    // selection values; -inf: masked
-#pragma unroll
-  for (int i = 0; i < kEpl; ++i) {
-    const int e = lane + 32 * i;
-    z[i] = e < p.E ? to_f(row[e]) : -INFINITY;
-    v[i] = (double)z[i];
+  double m = -INFINITY, s = 0.0;
+  if (scores && softmax) {
+#pragma unroll 1
+    for (int e = lane; e < p.E; e += 32) m = fmax(m, (double)to_f(row[e]));
+    for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (m == -INFINITY) m = 0.0;
+#pragma unroll 1
+    for (int e = lane; e < p.E; e += 32) s += exact_exp((double)to_f(row[e]) - m);
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   }
-  if (scores) {
-    double m = -INFINITY, s = 1.0;
-    if (p.score_fn == DX_SCORE_SOFTMAX) {
-#pragma unroll
-      for (int i = 0; i < kEpl; ++i) m = fmax(m, v[i]);
-      for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (m == -INFINITY) m = 0.0;
-    }
-#pragma unroll
-    for (int i = 0; i < kEpl; ++i) v[i] = exp(p.score_fn == DX_SCORE_SOFTMAX ? v[i] - m : -v[i]);
-    if (p.score_fn == DX_SCORE_SOFTMAX) {
-      s = 0.0;
-#pragma unroll
-      for (int i = 0; i < kEpl; ++i) s += lane + 32 * i < p.E ? v[i] : 0.0;
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    }
-#pragma unroll
-    for (int i = 0; i < kEpl; ++i) {
-      const int e = lane + 32 * i;
-      v[i] = p.score_fn == DX_SCORE_SOFTMAX ? v[i] / s : 1.0 / (1.0 + v[i]);
-      if (p.bias && e < p.E) v[i] += (double)p.bias[e];
-    }
+  __syncwarp();
+#pragma unroll 1
+  for (int e = lane; e < p.E; e += 32) {
+    const float z = to_f(row[e]);
+    double v = (double)z;
+    if (scores) v = softmax ? exact_exp(v - m) / s : exact_sigmoid(v);
+    if (p.bias) v += (double)p.bias[e];
+    if (!(z > -INFINITY) || !(v == v)) v = -INFINITY;
+    s_row[e] = v;
   }
-#pragma unroll
-  for (int i = 0; i < kEpl; ++i)
-    if (!(z[i] > -INFINITY) || !(v[i] == v[i])) v[i] = -INFINITY;   // (nothing that is not a number is compared)
+  __syncwarp();
   unsigned int kept = 0xffffffffu;
   const int per = p.E / p.groups;
   if (p.groups > 1) {
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < kEpl; ++i)
-      if (lane + 32 * i < p.E) s_row[lane + 32 * i] = v[i];
-    __syncwarp();
     double a = -INFINITY, b = -INFINITY;
     if (lane < p.groups) {
       int at = lane % per;                           // (start apart: the lanes read different banks)
+#pragma unroll 1
       for (int i = 0; i < per; ++i) {
         const double x = s_row[lane * per + at];
         if (x > a) { b = a; a = x; }
@@ -189,26 +211,29 @@ __device__ __noinline__ int select_exact(const BatchRouteParams& p, const T* row
       if (p.group_score != DX_GROUP_MAX && b > -INFINITY) a += b;
     }
     int r = 0;
+#pragma unroll 1
     for (int g = 0; g < p.groups; ++g) {
       const double o = __shfl_sync(0xffffffffu, a, g);
       r += o > a || (o == a && g < lane);
     }
     kept = __ballot_sync(0xffffffffu, lane < p.groups && r < p.keep);
-    __syncwarp();
   }
   // keys: without a bias the experts themselves are compared by their logits
-  unsigned long long key[kEpl], head = 0;
+  unsigned long long key[kEpl];
 #pragma unroll
   for (int i = 0; i < kEpl; ++i) {
     const int e = lane + 32 * i;
-    const bool on = e < p.E && (p.groups == 1 || (kept >> (min(e, p.E - 1) / per) & 1u));
-    const double x = p.bias || v[i] == -INFINITY ? v[i] : (double)z[i];
-    key[i] = on ? orderable64(x) : 0ull;
+    key[i] = 0ull;
+    if (e < p.E && (p.groups == 1 || (kept >> (e / per) & 1u))) {
+      const double v = s_row[e];
+      key[i] = orderable64(p.bias || v == -INFINITY ? v : (double)to_f(row[e]));
+    }
   }
   int mine = 0, head_e = 0;
+#pragma unroll 1
   for (int j = 0; j < p.k; ++j) {
     // the lane's first (its lowest expert among equals), then the warp's: high word, low word, expert
-    head = 0;
+    unsigned long long head = 0;
 #pragma unroll
     for (int i = 0; i < kEpl; ++i) {
       if (key[i] > head) {
@@ -225,6 +250,7 @@ __device__ __noinline__ int select_exact(const BatchRouteParams& p, const T* row
     for (int i = 0; i < kEpl; ++i)
       if (lane + 32 * i == e) key[i] = 0;
   }
+  __syncwarp();
   return mine;
 }
 
@@ -330,11 +356,14 @@ __device__ __forceinline__ float exp_fast(float x) {
   return e;
 }
 
-// G lanes per token.  kScores: the selection goes by scores (a bias, or groups ranked by a sum), else by the logits.
-template <typename T, int G, bool kScores>
-__global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteParams p) {
+// G lanes per token.  What the selection goes by: the logits, or scores (a bias, or groups ranked by a sum).
+enum { kByLogits, kBySigmoid, kBySoftmax };
+template <typename T, int G, int kBy>
+__global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __grid_constant__ BatchRouteParams p) {
   constexpr int kTok = 32 / G;                       // tokens a warp works on side by side
-  constexpr int kPicks = G == 4 ? 3 : G == 8 ? 2 : 1;   // picks (of k + 2) per lane
+  constexpr int kPicks = G == 4 ? 3 : G == 8 ? 2 : 1;   // picks (of k + 1) per lane
+  constexpr int kGateLanes = G < DX_MAX_TOPK ? G : DX_MAX_TOPK;   // the lanes that have the selected experts
+  constexpr bool kScores = kBy != kByLogits;
   constexpr unsigned int kMask = G == 32 ? 0xffffffffu : (1u << (G % 32)) - 1u;
   __shared__ int s_count[DX_MAX_E];
   __shared__ __align__(16) float s_bias[DX_MAX_E];
@@ -353,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
   const bool lane_groups = p.groups > 1 && per % kEpl == 0 && (gl & (gl - 1)) == 0;
   const int gl_log = lane_groups ? __ffs(gl) - 1 : 0;
   const bool biased = kScores && p.bias != nullptr;
-  const bool softmax = p.score_fn == DX_SCORE_SOFTMAX;
+  const bool softmax = kScores ? kBy == kBySoftmax : p.score_fn == DX_SCORE_SOFTMAX;
   dx_pdl_trigger();            // (the permutation waits for this kernel's end before it reads anything)
   for (int e = threadIdx.x; e < DX_MAX_E; e += kThreads) {
     s_count[e] = 0;
@@ -419,11 +448,20 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
       const float rcp = softmax ? 1.f / inv : 0.f;
       const float4 b0 = bias8[0], b1 = bias8[1];
       const float b[kEpl] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+      float least = z[0];
 #pragma unroll
-      for (int i = 0; i < kEpl; ++i) {
-        const bool live = z[i] > -INFINITY && !odd;
-        const float r = softmax ? exp_fast(z[i] - m) * rcp : sigmoid_fast(z[i]);
-        z[i] = live ? r + b[i] : -INFINITY;
+      for (int i = 1; i < kEpl; ++i) least = min_nan(least, z[i]);
+      unsigned int masked = 0;                       // (masked experts are rare: a warp that has none skips them)
+      if (__any_sync(0xffffffffu, !(least > -INFINITY) || odd)) {
+#pragma unroll
+        for (int i = 0; i < kEpl; ++i) masked |= (unsigned int)(!(z[i] > -INFINITY) || odd) << i;
+      }
+#pragma unroll
+      for (int i = 0; i < kEpl; ++i)
+        z[i] = (softmax ? exp_fast(z[i] - m) * rcp : sigmoid_fast(z[i])) + b[i];
+      if (__any_sync(0xffffffffu, masked != 0)) {
+#pragma unroll
+        for (int i = 0; i < kEpl; ++i) z[i] = masked >> i & 1u ? -INFINITY : z[i];
       }
     } else {
 #pragma unroll
@@ -518,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     DX_EXCHANGE(2, 4) DX_EXCHANGE(3, 5)
     DX_EXCHANGE(3, 4)
 #undef DX_EXCHANGE
-    // ---- k + 2 rounds: lane j of the token's lanes keeps pick j (j + G, j + 2 G); a lane's next key comes out of shared
+    // ---- k + 1 rounds: lane j of the token's lanes keeps pick j (j + G, j + 2 G); a lane's next key comes out of shared
     // memory when its first has been taken
     unsigned int pick[kPicks] = {};
     unsigned int* list = reinterpret_cast<unsigned int*>(s_mem.exact[warp]) + lane;
@@ -529,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     unsigned int head = on ? key[0] : 0u;
     list += 32;
 #pragma unroll 1
-    for (int j = 0, at = sub; j <= k + 1; ++j, --at) {
+    for (int j = 0, at = sub; j <= k; ++j, --at) {
       const unsigned int top = lanes_umax<G>(head);
 #pragma unroll
       for (int h = 0; h < kPicks; ++h)
@@ -554,7 +592,9 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
         const unsigned int w = __shfl_sync(0xffffffffu, pick[h + 1 < kPicks ? h + 1 : h], tok * G);
         if (sub == G - 1) below[h] = w;
       }
-      close |= h * G + sub < k && below[h] != 0 && (pick[h] >> 8) - (below[h] >> 8) <= near;
+      // (the keys of bf16 logits hold all of them)
+      if (kScores || sizeof(T) == 4)
+        close |= h * G + sub < k && below[h] != 0 && (pick[h] >> 8) - (below[h] >> 8) <= near;
     }
     if (__any_sync(0xffffffffu, close)) {
       close = false;
@@ -574,58 +614,21 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
       }
     }
     const bool unsure = (__ballot_sync(0xffffffffu, close) >> (tok * G) & kMask) != 0;
-    if (__any_sync(0xffffffffu, doubt || unsure)) {
-      // The true selection is among the first k + 1 picks unless the one behind them is as close to the border as well.
-      // Then their exact values put them in order: the logits, or the sigmoid in 64 bits and the bias (a softmax's needs
-      // the whole row in 64 bits).
-      unsigned int border = 0, behind = 0;
-#pragma unroll
-      for (int h = 0; h < kPicks; ++h) {
-        const unsigned int x0 = __shfl_sync(0xffffffffu, pick[h], tok * G + (k - 1) % G);
-        const unsigned int x1 = __shfl_sync(0xffffffffu, pick[h], tok * G + (k + 1) % G);
-        if (h == (k - 1) / G) border = x0;
-        if (h == (k + 1) / G) behind = x1;
-      }
-      const bool inside = !doubt && !(biased && softmax) && (behind == 0 || (border >> 8) - (behind >> 8) > near);
-      double v[kPicks];
-#pragma unroll
-      for (int h = 0; h < kPicks; ++h) {
-        v[h] = -INFINITY;
-        if (h * G + sub <= k && pick[h] != 0 && x[h] > -INFINITY)
-          v[h] = biased ? 1.0 / (1.0 + exp(-(double)x[h])) + (double)s_bias[id[h]] : (double)x[h];
-      }
-      int rank[kPicks] = {};
-#pragma unroll
-      for (int h = 0; h < kPicks; ++h) {
-        for (int j = 0; j < G; ++j) {
-          if (h * G + j > k) break;
-          const double o = __shfl_sync(0xffffffffu, v[h], tok * G + j);
-          const int oe = __shfl_sync(0xffffffffu, pick[h] != 0 ? id[h] : DX_MAX_E, tok * G + j);
-#pragma unroll
-          for (int i = 0; i < kPicks; ++i) rank[i] += o > v[i] || (o == v[i] && oe < id[i]);
-        }
-      }
-      int* order = reinterpret_cast<int*>(s_mem.exact[warp]) + tok * (DX_MAX_TOPK + 2);
-      __syncwarp();
-#pragma unroll
-      for (int h = 0; h < kPicks; ++h)
-        if (h * G + sub <= k && pick[h] != 0) order[rank[h]] = id[h];
-      __syncwarp();
-#pragma unroll
-      for (int h = 0; h < kPicks; ++h) {
-        if (unsure && inside && h * G + sub < k) {
-          id[h] = order[h * G + sub];
-          x[h] = to_f(row[id[h]]);
-        }
-      }
-      __syncwarp();
-      const unsigned int redo = __ballot_sync(0xffffffffu, doubt || (unsure && !inside));
+    const unsigned int open = __ballot_sync(0xffffffffu, doubt || unsure);
+    if (open != 0) {
+      const unsigned int behind = lanes_umax<G>(head);
 #pragma unroll 1
       for (int q = 0; q < kTok; ++q) {
-        if (!(redo >> (q * G) & 1u)) continue;       // (the same for the whole warp)
+        if (!(open >> (q * G) & 1u)) continue;       // (the same for the whole warp)
         const long long tq = min(t0 + q, t_hi - 1);
-        const T* rq = reinterpret_cast<const T*>(p.logits) + (size_t)tq * (size_t)p.ld;
-        const int got = select_exact(p, rq, s_mem.exact[warp]);
+        unsigned int mine = 0;                       // pick j of the token in lane j
+#pragma unroll
+        for (int h = 0; h < kPicks; ++h) {
+          const unsigned int y = __shfl_sync(0xffffffffu, pick[h], q * G + sub);
+          if (tok == h) mine = y;
+        }
+        const int got = settle(p, reinterpret_cast<const T*>(p.logits) + (size_t)tq * (size_t)p.ld, s_mem.exact[warp], mine,
+                               __shfl_sync(0xffffffffu, behind, q * G), __shfl_sync(0xffffffffu, (int)doubt, q * G) != 0, near);
 #pragma unroll
         for (int h = 0; h < kPicks; ++h) {
           const int y = __shfl_sync(0xffffffffu, got, (sub + h * G) % 32);
@@ -644,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
       if (h * G + sub >= k) x[h] = -INFINITY;
       top = fmaxf(top, x[h]);
     }
-    if (p.norm) top = lanes_max<G>(top);
+    if (p.norm) top = lanes_max<kGateLanes>(top);
 #pragma unroll
     for (int h = 0; h < kH; ++h) {
       // Renormalised gates are ratios: softmax needs no more of the row than e^{x - top}, and sigmoid(x) is e^x to 32
@@ -657,7 +660,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(BatchRouteP
     }
     float f = p.scale;
     if (p.norm) {
-      sum = lanes_sum<G>(sum);
+      sum = lanes_sum<kGateLanes>(sum);
       f = sum > 0.f || sum != sum ? p.scale / sum : 0.f;
     } else if (softmax) {
       // (the keys' fast sum is not good enough for the gates)
@@ -928,19 +931,20 @@ __global__ void __launch_bounds__(kGradThreads) dx_route_grad_dense_kernel(Route
   }
 }
 
-template <typename T, bool kScores>
+template <typename T, int kBy>
 cudaError_t launch_route(int grid, const BatchRouteParams& p, cudaStream_t st) {
-  if (p.E <= 4 * kEpl && p.groups <= 4) dx_batch_route_kernel<T, 4, kScores><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 8 * kEpl && p.groups <= 8) dx_batch_route_kernel<T, 8, kScores><<<grid, kThreads, 0, st>>>(p);
-  else if (p.E <= 16 * kEpl && p.groups <= 16) dx_batch_route_kernel<T, 16, kScores><<<grid, kThreads, 0, st>>>(p);
-  else dx_batch_route_kernel<T, 32, kScores><<<grid, kThreads, 0, st>>>(p);
+  if (p.E <= 4 * kEpl && p.groups <= 4) dx_batch_route_kernel<T, 4, kBy><<<grid, kThreads, 0, st>>>(p);
+  else if (p.E <= 8 * kEpl && p.groups <= 8) dx_batch_route_kernel<T, 8, kBy><<<grid, kThreads, 0, st>>>(p);
+  else if (p.E <= 16 * kEpl && p.groups <= 16) dx_batch_route_kernel<T, 16, kBy><<<grid, kThreads, 0, st>>>(p);
+  else dx_batch_route_kernel<T, 32, kBy><<<grid, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 template <typename T>
 cudaError_t launch_route(int grid, const BatchRouteParams& p, cudaStream_t st) {
   // (the logits stand for the scores wherever only their order counts)
   const bool scores = p.bias != nullptr || (p.groups > 1 && p.group_score != DX_GROUP_MAX);
-  return scores ? launch_route<T, true>(grid, p, st) : launch_route<T, false>(grid, p, st);
+  if (!scores) return launch_route<T, kByLogits>(grid, p, st);
+  return p.score_fn == DX_SCORE_SOFTMAX ? launch_route<T, kBySoftmax>(grid, p, st) : launch_route<T, kBySigmoid>(grid, p, st);
 }
 template <typename T>
 cudaError_t launch_grad(int grid, const RouteGradParams& p, cudaStream_t st) {
