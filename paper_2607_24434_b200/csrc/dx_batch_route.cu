@@ -254,6 +254,40 @@ __device__ __noinline__ int settle(const BatchRouteParams& p, const T* row, doub
   return mine;
 }
 
+// Ranks of the groups of a warp's tokens (G lanes each, 1 << gl_log lanes per group) where 32-bit scores leave the border
+// open; the scores are sigmoids.  `open`: the lane's group is close to the border; `cand`: those of the lane's experts e0
+// + i that can be among the two largest of such a group (two or three, mostly).  Their exact values give the group's
+// score in 64 bits; the others keep theirs, which are on their side of the border whatever their last bits.
+template <typename T>
+__device__ __noinline__ int settle_groups(const BatchRouteParams& p, const T* row, const float* bias, int e0, bool open,
+                                          unsigned int cand, float gs, int gl_log, int G) {
+  const int lane = threadIdx.x & 31, grp = (lane & (G - 1)) >> gl_log, base = lane & ~(G - 1);
+  double a = -INFINITY, b = -INFINITY;
+#pragma unroll 1
+  while (__any_sync(0xffffffffu, cand != 0)) {
+    const int e = e0 + __ffs(cand) - 1;
+    const double v = cand ? exact_sigmoid((double)to_f(row[e])) + (double)bias[e] : -INFINITY;
+    __syncwarp();
+    cand &= cand - 1;
+    if (v > a) { b = a; a = v; }
+    else if (v > b) b = v;
+  }
+#pragma unroll 1
+  for (int o = 1; o < 1 << gl_log; o <<= 1) {
+    const double oa = __shfl_xor_sync(0xffffffffu, a, o), ob = __shfl_xor_sync(0xffffffffu, b, o);
+    b = fmax(fmax(b, ob), fmin(a, oa));
+    a = fmax(a, oa);
+  }
+  const double g = !open ? (double)gs : p.group_score == DX_GROUP_MAX || b == -INFINITY ? a : a + b;
+  int r = 0;
+#pragma unroll 1
+  for (int i = 0; i < p.groups; ++i) {
+    const double o = __shfl_sync(0xffffffffu, g, base + (i << gl_log));
+    r += o > g || (o == g && i < grp);
+  }
+  return r;
+}
+
 // Where the pairs of a CTA's tokens go: s_base[e] = first place of expert e's.  The pairs are taken kTile at a time, a
 // contiguous stretch of 32 * kDeep per warp, so that equal experts keep the order of their pairs.
 constexpr int kDeep = 2;
@@ -481,10 +515,6 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
           g2 = fmaxf(fmaxf(g2, o2), fminf(g1, o1));
           g1 = fmaxf(g1, o1);
         }
-        // lane g of the token's lanes takes group g
-        const int from = tok * G + (min(sub, p.groups - 1) << gl_log);
-        g1 = __shfl_sync(0xffffffffu, g1, from);
-        g2 = __shfl_sync(0xffffffffu, g2, from);
       } else {
         float* stage = reinterpret_cast<float*>(s_mem.exact[warp]) + tok * G * kEpl;
 #pragma unroll
@@ -502,24 +532,40 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
         __syncwarp();
       }
       const float gs = p.group_score == DX_GROUP_MAX || g2 == -INFINITY ? g1 : g1 + g2;
-      // the best groups one after the other, on unique keys: 26 bits of the score's order, then the reversed group; scores
-      // that the cut bits or the arithmetic cannot tell apart at the border raise the doubt
-      const unsigned int gkey = sub < p.groups ? (dx_orderable(gs + 0.f) & 0xffffffe0u) | (unsigned int)(31 - sub) : 0u;
-      unsigned int left = gkey, last = 0, next = 0;
-      for (int j = 0; j <= p.keep; ++j) {            // (keep < groups)
-        next = lanes_umax<G>(left);
-        if (j < p.keep) last = next;
-        if (left == next) left = 0;
+      // A group's rank is the number of groups in front of it, counted by its lanes side by side (lane g has group g
+      // where a group is not a number of lanes); scores that the arithmetic cannot tell apart at the border raise the doubt.
+      const int grp = sub >> gl_log;
+      int r = 0;
+      for (int i0 = 0; i0 < p.groups; i0 += 1 << gl_log) {
+        const int i = i0 + (sub & ((1 << gl_log) - 1));
+        const float o = __shfl_sync(0xffffffffu, gs, tok * G + (min(i, p.groups - 1) << gl_log));
+        r += i < p.groups && (o > gs || (o == gs && i < grp));
       }
-      kept = __ballot_sync(0xffffffffu, gkey != 0 && gkey >= last) >> (tok * G) & kMask;
-      const float g_in = __shfl_sync(0xffffffffu, gs, tok * G + 31 - (int)(last & 31u));
-      const float g_out = __shfl_sync(0xffffffffu, gs, tok * G + 31 - (int)(next & 31u));
-      if (kScores) {   // (the key's cut: 32 steps of the score's last place; infinite on both sides: not close)
-        const float eps = 2.f * kScoreError * (1.f + bias_abs);
-        doubt |= fabsf(g_in - g_out) <= eps + 6e-6f * fmaxf(fabsf(g_in), fabsf(g_out));
-      } else if (sizeof(T) == 4) {   // (a bf16 logit fits the key: equal keys are a true tie)
-        doubt |= (last >> 5) == (next >> 5) && g_in > -INFINITY;
+      for (int o = 1; o < 1 << gl_log; o <<= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+      if (grp >= p.groups) r = DX_MAX_GROUPS;
+      const unsigned int last = __ballot_sync(0xffffffffu, r == p.keep - 1) >> (tok * G) & kMask;
+      const unsigned int next = __ballot_sync(0xffffffffu, r == p.keep) >> (tok * G) & kMask;   // (keep < groups)
+      const float g_in = __shfl_sync(0xffffffffu, gs, tok * G + __ffs(last) - 1);
+      const float g_out = __shfl_sync(0xffffffffu, gs, tok * G + __ffs(next) - 1);
+      // (logits are compared as they are; infinite on both sides: not close)
+      if (kScores) {
+        const float err = kScoreError * (1.f + bias_abs);
+        const bool open = fabsf(g_in - g_out) <= 2.f * err;
+        if (kBy == kBySigmoid && lane_groups) {
+          if (__any_sync(0xffffffffu, open)) {
+            const bool mine = open && grp < p.groups && (fabsf(gs - g_in) <= 2.f * err || fabsf(gs - g_out) <= 2.f * err);
+            const float from = (p.group_score == DX_GROUP_MAX ? g1 : g2) - err;
+            unsigned int cand = 0;
+#pragma unroll
+            for (int i = 0; i < kEpl; ++i) cand |= (unsigned int)(mine && z[i] >= from && z[i] > -INFINITY) << i;
+            r = settle_groups(p, row, s_bias, e0, mine, cand, gs, gl_log, G);
+            if (grp >= p.groups) r = DX_MAX_GROUPS;
+          }
+        } else {
+          doubt |= open;
+        }
       }
+      kept = __ballot_sync(0xffffffffu, r < p.keep) >> (tok * G) & kMask;   // by lane
     }
     if (kScores && !biased) {                        // (the scores were for the groups; experts go by their logits)
       load8(row, e0, E, p.vec != 0, z);
@@ -538,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
       }
     }
     // (where the lane's experts stay or go together, it is enough that the lane has no first key)
-    const bool on = e0 < E && (p.groups == 1 || !lane_groups || (kept >> (sub >> gl_log) & 1u));
+    const bool on = e0 < E && (p.groups == 1 || !lane_groups || (kept >> sub & 1u));
     if (!lane_groups && (p.groups > 1 || (E & (kEpl - 1)) != 0)) {
 #pragma unroll
       for (int i = 0; i < kEpl; ++i) {

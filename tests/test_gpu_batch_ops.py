@@ -512,6 +512,25 @@ def test_route_biases_far_from_the_scores(dx, dtype):
             check_route(dx, rows(z, dtype), 6, sigmoid, True, 1.0, ref_bias, groups=8, keep=3, top2=True)
 
 
+@pytest.mark.parametrize("top2", [False, True])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,groups,keep", [(64, 8, 3), (64, 4, 2), (256, 8, 4), (256, 32, 3), (128, 2, 1), (60, 6, 2), (96, 4, 1)])
+def test_route_groups_of_nearly_equal_scores(dx, E, groups, keep, top2, sigmoid):
+    """Groups that hold the same values in another order, apart by less than fp32 sums tell, or not at all."""
+    N, per = 97, E // groups
+    g = torch.Generator().manual_seed(40 + E + groups)
+    one = torch.randn((N, 1, per), generator=g).expand(N, groups, per)
+    bias_one = torch.randn((1, 1, per), generator=g) * 0.05
+    order = torch.rand((1, groups, per), generator=g).argsort(dim=2)
+    bias = bias_one.expand(1, groups, per).gather(2, order).reshape(E).contiguous()
+    for step in (0.0, 2.0 ** -24, 2.0 ** -21, 2.0 ** -16):
+        z = one.gather(2, order.expand(N, groups, per))
+        z = (z + z.abs() * step * torch.randint(-3, 4, z.shape, generator=g)).reshape(N, E)
+        z[5, : E // 2] = -INF
+        check_route(dx, rows(z, torch.float32), 4, sigmoid, True, 1.0, bias, groups, keep, top2)
+        check_route(dx, rows(z, torch.float32), 4, sigmoid, True, 1.0, None, groups, keep, False)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("N,E,k,off,groups,keep", [
