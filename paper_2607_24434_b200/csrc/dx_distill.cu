@@ -21,13 +21,14 @@ namespace {
 
 constexpr int kUnroll = 4;
 constexpr float kSlack = 8.f;                     // powers of two by which an element may exceed its sum's reference
-constexpr int kStaticBytes = 4608;                // at least the kernel's static shared memory
+constexpr int kStaticBytes = 5120;                // at least the kernel's static shared memory
 constexpr int kHash = 2 * DX_MAX_TEACHER;
 constexpr int kThreads = kRowThreads + 32;        // eight warps that stream, one that handles the list
 
 struct DistillParams {
   const void* logits;
-  int N, V, k, tail, half;    // half: 16-bit words of marks per thread
+  int N, V, k, tail;
+  int half, late;             // 16-bit words of marks per thread; the vector of a thread that begins its second half
   long long ld, ld_d;
   const int32_t* ids;
   const float* lp;
@@ -56,6 +57,13 @@ __device__ __forceinline__ double warp_sum(double v) {
 // with and of the tail bucket, and what its p_j are multiplied with.
 struct ListSums {
   float z_ref, sum_e, beta, rest, norm;
+};
+// What the loss of a row is made of.  64-bit logarithms are long chains: kRing rows are finished at a time, a lane each.
+constexpr int kRing = 16;
+struct LossTerms {
+  double mass, p_log_p, p_u, sum_e;
+  float z_ref, rest_m, rest_s;
+  int t;
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst_smem, const uint4* src) {
@@ -116,13 +124,14 @@ template <typename T, bool kGrad, int kLists>
 __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(DistillParams p, int C, int buffers) {
   using V16 = RowVec<T>;
   // [buffers][kRowThreads][half] 16-bit words -- bit q of a thread's words: its q-th vector holds a listed word -- and
-  // behind them (kGrad) the CTA's vectors of the row
+  // behind them the CTA's vectors of the row
   extern __shared__ uint4 s_dyn[];
   __shared__ __align__(16) unsigned int s_hash[2][kHash];   // vector + 1 << 8 | its listed elements; 0: free
   __shared__ MaxSum s_all[2][DX_ROW_CLUSTER_MAX * kRowWarps];   // sums of all warps of all CTAs of the row
   __shared__ ListSums s_list[2];
   __shared__ unsigned int s_edge[2];               // head (bits 0..7) and tail (8..15) elements that are listed
   __shared__ float s_weight[2];                    // 0: nothing to learn from the row
+  __shared__ LossTerms s_ring[kRing];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = C > 1 ? (int)cluster_rank() : 0;
   const int n_rows = gridDim.x / C;                // rows in flight: row t is followed by row t + n_rows
@@ -138,15 +147,20 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   if (warp == kRowWarps) {
     // ==== the list warp
     int id[kLists];                                // entry lane + 32 i (-1: unused, out of range, listed before)
+    int raw[kLists];                               // ... of the row behind, as given; its weight
     float w = 0.f;
     auto load_ids = [&](int t) {
       if (t >= p.N) return;
 #pragma unroll
-      for (int i = 0; i < kLists; ++i) id[i] = lane + 32 * i < p.k ? p.ids[(size_t)t * p.k + lane + 32 * i] : -1;
+      for (int i = 0; i < kLists; ++i) raw[i] = lane + 32 * i < p.k ? p.ids[(size_t)t * p.k + lane + 32 * i] : -1;
       w = p.weight ? p.weight[t] : 1.f;
     };
     auto mark = [&](int t, int b) {                // ids -> marks, hash table and state of buffer b
       if (t >= p.N) return;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) id[i] = raw[i];
+      const float weight = w;
+      load_ids(t + n_rows);
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
       const RowSplit sp = row_split(row, p.V, rank, C);
       const int n_vec = sp.v_hi - sp.v_lo, tail0 = p.V - sp.tail;
@@ -204,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       }
       if (bad && rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
       live = __any_sync(0xffffffffu, live);
-      if (lane == 0) s_weight[b] = live ? w : 0.f;
+      if (lane == 0) s_weight[b] = live ? weight : 0.f;
     };
     // The list's part in a row: logits and log p_j, on their way while the row in front is worked on; then per entry
     // e^{(z_j - z_ref) / T} -- later the word's gradient, stored when the next row begins -- and p_j, the sums for the
@@ -275,6 +289,22 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         last_out = nullptr;
       }
     };
+    int in_ring = 0;
+    auto finish = [&]() {                          // the losses of the rows in the ring
+      if (lane >= in_ring) return;
+      const LossTerms x = s_ring[lane];
+      const float M = fmaxf(x.rest_m, x.z_ref);
+      const double rest = p.tail && x.mass < 1.0 ? 1.0 - x.mass : 0.0;
+      const double du_rest = ((double)x.rest_m - (double)M) * p.inv_T;
+      const double du_list = ((double)x.z_ref - (double)M) * p.inv_T;
+      const double S = (x.rest_s > 0.f ? exp(du_rest) : 1.0) * (double)x.rest_s + exp(du_list) * x.sum_e;
+      const double log_S = log(S);
+      // - sum_j p_j log q_j = -( sum p_j (z_j - z_ref) / T + P (z_ref - M) / T - P log S )
+      double loss = x.p_log_p - (x.p_u + (x.mass != 0.0 ? x.mass * (du_list - log_S) : 0.0));
+      if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)x.rest_s) - log_S));
+      if (S == 0.0) loss = x.mass + rest > 0.0 ? INFINITY : 0.0;   // nothing but -inf in the row
+      p.loss[x.t] = (float)loss;
+    };
     int t = blockIdx.x / C, turn = 0;
     load_ids(t);
     mark(t, 0);
@@ -287,7 +317,6 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       const float scale = s_weight[it & (buffers - 1)] * p.inv_Tf;
       if (s_weight[it & (buffers - 1)] == 0.f) {   // nothing to learn from this row
         if (rank == 0 && lane == 0 && p.loss) p.loss[t] = 0.f;
-        load_ids(t + n_rows);
         mark(t + n_rows, (it + 1) & (buffers - 1));
         load_list(t + n_rows);
         continue;
@@ -295,7 +324,6 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
       list_sums(turn);
       if (C > 1) cluster_arrive();
-      load_ids(t + n_rows);
       mark(t + n_rows, (it + 1) & (buffers - 1));
       load_list(t + n_rows);
       __syncwarp();
@@ -315,18 +343,16 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         }
       }
       if (rank == 0 && p.loss) {
-        const double rest = p.tail && mass < 1.0 ? 1.0 - mass : 0.0;
-        const double du_rest = ((double)r.rest.m - (double)r.M) * p.inv_T;
-        const double du_list = ((double)l.z_ref - (double)r.M) * p.inv_T;
-        const double S = (r.rest.s > 0.f ? exp(du_rest) : 1.0) * (double)r.rest.s + exp(du_list) * sum_e;
-        const double log_S = log(S);
-        // - sum_j p_j log q_j = -( sum p_j (z_j - z_ref) / T + P (z_ref - M) / T - P log S )
-        double loss = p_log_p - (p_u + (mass != 0.0 ? mass * (du_list - log_S) : 0.0));
-        if (rest > 0.0) loss += rest * (log(rest) - (du_rest + log((double)r.rest.s) - log_S));
-        if (S == 0.0) loss = mass + rest > 0.0 ? INFINITY : 0.0;   // nothing but -inf in the row
-        if (lane == 0) p.loss[t] = (float)loss;
+        if (lane == 0) s_ring[in_ring] = LossTerms{mass, p_log_p, p_u, sum_e, l.z_ref, r.rest.m, r.rest.s, t};
+        __syncwarp();
+        if (++in_ring == kRing) {
+          finish();
+          __syncwarp();
+          in_ring = 0;
+        }
       }
     }
+    finish();
     if (kGrad) {
       cta_barrier();
       store_listed();
@@ -343,14 +369,15 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   int t = blockIdx.x / C, turn = 0;
   const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
   RowSplit sp = row_split(row, p.V, rank, C);
-  // Every thread copies the vectors tid, tid + 256, ... that it reads itself, in two groups: those of the first half can
+  // Every thread copies the vectors tid, tid + 256, ... that it reads itself, in two groups: those in front of `late` can
   // be waited for alone.
-  if (kGrad) {
+  const int late = p.late;
+  {
     const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo;
     const int n_vec = sp.v_hi - sp.v_lo, deep = (n_vec + kRowThreads - 1) / kRowThreads;
 #pragma unroll 2
     for (int q = 0; q < deep; ++q) {
-      if (2 * q == (deep & ~(2 * kUnroll - 1))) asm volatile("cp.async.commit_group;" ::: "memory");
+      if (q == late) asm volatile("cp.async.commit_group;" ::: "memory");
       const int i = tid + q * kRowThreads;
       if (i < n_vec) copy16(s_mine + q * kRowThreads * 16, src + i);
     }
@@ -367,6 +394,13 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     // gradient vectors can be stored as such where the output row is aligned like the input row
     const bool same_align = kGrad && ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15u) == 0;
     T* out_vec = out + sp.head + (long long)sp.v_lo * V16::kN;
+    // the next row: its vectors take the places of this one's as soon as those have been read for the last time
+    const T* next = row + (size_t)n_rows * (size_t)p.ld;
+    t += n_rows;
+    const RowSplit np = t < p.N ? row_split(next, p.V, rank, C) : sp;
+    const int next_vecs = t < p.N ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
+    const int plain = min(n_vec, next_vecs ? next_vecs : n_vec);
+    const uint4* fetch = reinterpret_cast<const uint4*>(next + np.head) + np.v_lo + tid;
     cta_barrier();
     const float w = s_weight[b];
     float coef = 0.f, ref = 0.f;                   // gradient of an unlisted word: coef * e^{(z - ref) / T}
@@ -421,35 +455,52 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
           }
         }
       };
-      const uint4* src = reinterpret_cast<const uint4*>(row + sp.head) + sp.v_lo + tid;
       uint32_t held = s_mine;
       int q = 0;
-      if (kGrad) asm volatile("cp.async.wait_group 1;" ::: "memory");
-      const int late = (deep & ~(2 * kUnroll - 1)) / 2;          // vectors from here on are in the second group
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
 #pragma unroll 1
-      for (; (q + kUnroll) * kRowThreads <= n_vec; q += kUnroll, src += kUnroll * kRowThreads) {
-        if (kGrad && q == late) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      for (; (q + kUnroll) * kRowThreads <= (kGrad ? n_vec : plain); q += kUnroll) {
+        if (q == late) {
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          if (!kGrad) asm volatile("cp.async.commit_group;" ::: "memory");
+        }
         uint4 v[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-          v[u] = kGrad ? load_shared(held + u * kRowThreads * 16) : load_stream(src + u * kRowThreads);
-        held += kUnroll * kRowThreads * 16;
+        for (int u = 0; u < kUnroll; ++u) v[u] = load_shared(held + u * kRowThreads * 16);
         add(v, q, kUnroll);
+        if (!kGrad && next_vecs) {
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) copy16(held + u * kRowThreads * 16, fetch + u * kRowThreads);
+        }
+        held += kUnroll * kRowThreads * 16;
+        if (!kGrad) fetch += kUnroll * kRowThreads;
       }
       if (kGrad) asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll 1
-      for (; q < deep; q += kUnroll) {                           // what is left: less than kUnroll vectors per thread,
-        uint4 v[kUnroll];                                        // and one more for some
+      for (; q < (kGrad ? deep : max(deep, next_deep)); q += kUnroll) {   // what is left: less than kUnroll vectors per
+        if (!kGrad && q == late) {                                        // thread, and one more for some
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        uint4 v[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
+          const int i = tid + (q + u) * kRowThreads;
           v[u] = none4;                                          // (adds nothing)
-          if (tid + (q + u) * kRowThreads < n_vec)
-            v[u] = kGrad ? load_shared(held + u * kRowThreads * 16) : load_stream(src + u * kRowThreads);
+          if (i < n_vec) v[u] = load_shared(held + u * kRowThreads * 16);
         }
         // (a single vector: the warps that have no second one)
         if ((q + 1) * kRowThreads + (tid & ~31) < n_vec) add(v, q, kUnroll);
         else add(v, q, 1);
+        if (!kGrad) {
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u)
+            if (tid + (q + u) * kRowThreads < next_vecs) copy16(held + u * kRowThreads * 16, fetch + u * kRowThreads);
+          fetch += kUnroll * kRowThreads;
+        }
+        held += kUnroll * kRowThreads * 16;
       }
+      if (!kGrad) asm volatile("cp.async.commit_group;" ::: "memory");
       float s0, s1;
       f2_unpack(s2, s0, s1);
       st.s = s0 + s1;
@@ -486,17 +537,18 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         ref = r.rest.m;
       }
       turn ^= 1;
-    } else if (kGrad) {
+    } else {
       asm volatile("cp.async.wait_all;" ::: "memory");
+      if (!kGrad) {
+        for (int q = 0; q < next_deep; ++q) {
+          if (q == late) asm volatile("cp.async.commit_group;" ::: "memory");
+          if (tid + q * kRowThreads < next_vecs) copy16(s_mine + q * kRowThreads * 16, fetch + q * kRowThreads);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
     }
-    // ---- the gradient (zeros where there is nothing to learn); a vector's place takes the next row's vector as soon as
-    // it has been read
-    const T* next = row + (size_t)n_rows * (size_t)p.ld;
-    t += n_rows;
-    const RowSplit np = t < p.N ? row_split(next, p.V, rank, C) : sp;
+    // ---- the gradient (zeros where there is nothing to learn)
     if (kGrad) {
-      const uint4* next_src = reinterpret_cast<const uint4*>(next + np.head) + np.v_lo;
-      const int next_vecs = t < p.N ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
       if (head_in) out[tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_head - ref) * c));
       if (tail_in) out[tail0 + tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_tail - ref) * c));
       const unsigned long long nm2 = f2_pack(-ref, -ref), k2 = f2_pack(coef, coef);
@@ -510,14 +562,12 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         }
         return V16::pack(g);
       };
-      const uint4* fetch = next_src + tid;
       uint4* store = reinterpret_cast<uint4*>(out_vec) + tid;
       uint32_t held = s_mine;
-      const int late = (next_deep & ~(2 * kUnroll - 1)) / 2;     // vectors from here on make the second group
-      const int plain = same_align && w != 0.f ? min(n_vec, next_vecs ? next_vecs : n_vec) : 0;
+      const int whole = same_align && w != 0.f ? plain : 0;
       int q = 0;
 #pragma unroll 1
-      for (; (q + kUnroll) * kRowThreads <= plain; q += kUnroll) {
+      for (; (q + kUnroll) * kRowThreads <= whole; q += kUnroll) {
         if (q == late) asm volatile("cp.async.commit_group;" ::: "memory");
         uint4 v[kUnroll];
 #pragma unroll
@@ -587,8 +637,7 @@ cudaError_t max_clusters(dx_ctx* ctx, int C, size_t smem, int* out) {
 template <typename T, bool kGrad, int kLists>
 cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
   // CTAs per row: few enough bytes per CTA that two fit an SM (one works while the other waits for its row), and as many
-  // as fill the GPU when there are few rows.  (Without the gradient nothing has to fit; the same split gives the same
-  // loss, bit for bit.)
+  // as fill the GPU when there are few rows.  (The same with and without the gradient: so is the loss, bit for bit.)
   const long long bytes = (long long)p.V * (long long)sizeof(T);
   const int slots = 2 * ctx->sm_count;
   int C = 1;
@@ -600,7 +649,8 @@ cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
   DistillParams q = p;
   q.half = (int)((slice + kRowThreads * 16 - 1) / (kRowThreads * 16));
   if (q.half < 1) q.half = 1;
-  const size_t held = kGrad ? (size_t)slice * 16 : 0;
+  q.late = (int)(slice / kRowThreads & ~(2 * kUnroll - 1)) / 2;
+  const size_t held = (size_t)slice * 16;
   // As many clusters as run at a time, each going from row to row with the next row's logits and marks on their way;
   // rows so long that only one set of marks fits get a cluster each.
   const int buffers = held + 2 * 512 * (size_t)q.half + kStaticBytes <= (size_t)ctx->smem_optin ? 2 : 1;
@@ -656,7 +706,7 @@ cudaError_t dx_launch_distill(dx_ctx* ctx, const void* logits, int dtype, int N,
   const double c = 1.4426950408889634 / (double)temperature;
   float c_hi = (float)c;
   if ((double)c_hi >= c) c_hi = nextafterf(c_hi, 0.f);
-  DistillParams p{logits, N, V, k, tail, 0, ld, ld_d, teacher_ids, teacher_logprobs,
+  DistillParams p{logits, N, V, k, tail, 0, 0, ld, ld_d, teacher_ids, teacher_logprobs,
                   c_hi, (float)(c - (double)c_hi), 1.0 / (double)temperature, (float)(1.0 / (double)temperature), row_weight, loss, dlogits, ctx->dev_status};
   if (dtype == DX_DTYPE_FP32) return dlogits ? launch_lists<float, true>(ctx, p, st) : launch_lists<float, false>(ctx, p, st);
   return dlogits ? launch_lists<__nv_bfloat16, true>(ctx, p, st) : launch_lists<__nv_bfloat16, false>(ctx, p, st);
