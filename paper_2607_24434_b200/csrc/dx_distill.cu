@@ -149,6 +149,14 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     int id[kLists];                                // entry lane + 32 i (-1: unused, out of range, listed before)
     int raw[kLists];                               // ... of the row behind, as given; its weight
     float w = 0.f;
+    // The list's part in a row: logits and log p_j, on their way while the row in front is worked on; then per entry
+    // e^{(z_j - z_ref) / T} -- later the word's gradient, stored when the next row begins -- and p_j, the sums for the
+    // gradient, and the sums for the loss (log p_j is what the caller has given).
+    float z[kLists], lp[kLists], e[kLists], pj[kLists];
+    int at[kLists];
+    T* last_out = nullptr;
+    ListSums l{};
+    double mass = 0.0, p_log_p = 0.0, p_u = 0.0, sum_e = 0.0;
     auto load_ids = [&](int t) {
       if (t >= p.N) return;
 #pragma unroll
@@ -157,11 +165,16 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     };
     auto mark = [&](int t, int b) {                // ids -> marks, hash table and state of buffer b
       if (t >= p.N) return;
-#pragma unroll
-      for (int i = 0; i < kLists; ++i) id[i] = raw[i];
       const float weight = w;
-      load_ids(t + n_rows);
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) {
+        const bool in = raw[i] >= 0 && raw[i] < p.V;
+        id[i] = raw[i];
+        z[i] = in ? V16::load(row + raw[i]) : -INFINITY;
+        lp[i] = in ? p.lp[(size_t)t * p.k + lane + 32 * i] : -INFINITY;
+      }
+      load_ids(t + n_rows);
       const RowSplit sp = row_split(row, p.V, rank, C);
       const int n_vec = sp.v_hi - sp.v_lo, tail0 = p.V - sp.tail;
       unsigned int* marks = s_mark + b * half * (kRowThreads / 2);
@@ -220,28 +233,12 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       live = __any_sync(0xffffffffu, live);
       if (lane == 0) s_weight[b] = live ? weight : 0.f;
     };
-    // The list's part in a row: logits and log p_j, on their way while the row in front is worked on; then per entry
-    // e^{(z_j - z_ref) / T} -- later the word's gradient, stored when the next row begins -- and p_j, the sums for the
-    // gradient, and the sums for the loss (log p_j is what the caller has given).
-    float z[kLists], lp[kLists], e[kLists], pj[kLists];
-    int at[kLists];
-    T* last_out = nullptr;
-    ListSums l{};
-    double mass = 0.0, p_log_p = 0.0, p_u = 0.0, sum_e = 0.0;
-    auto load_list = [&](int t) {
-      if (t >= p.N) return;
-      const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
-#pragma unroll
-      for (int i = 0; i < kLists; ++i) {
-        z[i] = id[i] >= 0 ? V16::load(row + id[i]) : -INFINITY;
-        lp[i] = id[i] >= 0 ? p.lp[(size_t)t * p.k + lane + 32 * i] : -INFINITY;
-      }
-    };
     auto list_sums = [&](int slot) {
       float top = -FLT_MAX;
 #pragma unroll
       for (int i = 0; i < kLists; ++i) {
         at[i] = id[i];
+        if (at[i] < 0) z[i] = lp[i] = -INFINITY;   // (listed before)
         top = fmaxf(top, z[i]);
       }
       l.z_ref = warp_max(top);
@@ -305,28 +302,47 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       if (S == 0.0) loss = x.mass + rest > 0.0 ? INFINITY : 0.0;   // nothing but -inf in the row
       p.loss[x.t] = (float)loss;
     };
+    auto keep = [&](const RowSums& r, int t) {     // a row's terms into the ring
+      if (lane == 0) s_ring[in_ring] = LossTerms{mass, p_log_p, p_u, sum_e, l.z_ref, r.rest.m, r.rest.s, t};
+      __syncwarp();
+      if (++in_ring == kRing) {
+        finish();
+        __syncwarp();
+        in_ring = 0;
+      }
+    };
     int t = blockIdx.x / C, turn = 0;
+    int pending = -1;                              // (loss alone) the row whose sums are still to be collected
+    auto collect = [&]() {
+      if (pending < 0) return;
+      if (C > 1) cluster_wait();
+      if (rank == 0) keep(row_sums(s_all[turn ^ 1], l, C * kRowWarps, c), pending);
+      pending = -1;
+    };
     load_ids(t);
     mark(t, 0);
-    load_list(t);
     if (C > 1) cluster_wait();                     // (all CTAs of the row have started)
 #pragma unroll 1
     for (int it = 0; t < p.N; ++it, t += n_rows) {
       cta_barrier();
+      if (!kGrad) collect();
       store_listed();
       const float scale = s_weight[it & (buffers - 1)] * p.inv_Tf;
       if (s_weight[it & (buffers - 1)] == 0.f) {   // nothing to learn from this row
         if (rank == 0 && lane == 0 && p.loss) p.loss[t] = 0.f;
         mark(t + n_rows, (it + 1) & (buffers - 1));
-        load_list(t + n_rows);
         continue;
       }
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
       list_sums(turn);
       if (C > 1) cluster_arrive();
       mark(t + n_rows, (it + 1) & (buffers - 1));
-      load_list(t + n_rows);
       __syncwarp();
+      if (!kGrad) {
+        pending = t;
+        turn ^= 1;
+        continue;
+      }
       if (C > 1) cluster_wait();
       else cta_barrier();
       const RowSums r = row_sums(s_all[turn], l, C * kRowWarps, c);
@@ -342,20 +358,17 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
           if (at[i] < sp.head ? rank != 0 : at[i] >= p.V - sp.tail ? rank != C - 1 : v < sp.v_lo || v >= sp.v_hi) at[i] = -1;
         }
       }
-      if (rank == 0 && p.loss) {
-        if (lane == 0) s_ring[in_ring] = LossTerms{mass, p_log_p, p_u, sum_e, l.z_ref, r.rest.m, r.rest.s, t};
-        __syncwarp();
-        if (++in_ring == kRing) {
-          finish();
-          __syncwarp();
-          in_ring = 0;
-        }
-      }
+      if (rank == 0 && p.loss) keep(r, t);
     }
-    finish();
     if (kGrad) {
+      finish();
+      __syncwarp();
       cta_barrier();
       store_listed();
+    } else {
+      cta_barrier();
+      collect();
+      finish();
     }
     return;
   }
@@ -367,6 +380,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   const unsigned long long c2 = f2_pack(c, c), cl2 = f2_pack(p.c_lo, p.c_lo);
   const uint4 none4 = make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
   int t = blockIdx.x / C, turn = 0;
+  bool pending = false;                            // (loss alone) arrived at the cluster's barrier, not waited
   const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
   RowSplit sp = row_split(row, p.V, rank, C);
   // Every thread copies the vectors tid, tid + 256, ... that it reads itself, in two groups: those in front of `late` can
@@ -517,7 +531,23 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       }
       __syncwarp();
       st = warp_join(st, c);
-      if (C > 1) {                                 // to all CTAs of the row
+      if (!kGrad) {
+        // The loss alone is the first CTA's business: its list warp collects the sums while these warps are a row ahead
+        // (at the latest when the second row behind has its own to give).
+        if (C > 1) {
+          if (pending) cluster_wait();
+          if (lane == 0) {
+            const uint32_t a = cluster_addr(&s_all[turn][rank * kRowWarps + warp], 0);
+            cluster_store_f32(a, st.m);
+            cluster_store_f32(a + 4, st.s);
+          }
+          __syncwarp();
+          cluster_arrive();
+          pending = true;
+        } else if (lane == 0) {
+          s_all[turn][warp] = st;                  // (read behind the barrier in front of the next row)
+        }
+      } else if (C > 1) {                          // to all CTAs of the row
         if (lane < C) {
           const uint32_t a = cluster_addr(&s_all[turn][rank * kRowWarps + warp], lane);
           cluster_store_f32(a, st.m);
@@ -607,7 +637,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     row = next;
     sp = np;
   }
-  if (kGrad) cta_barrier();
+  cta_barrier();
+  if (!kGrad && C > 1 && pending) cluster_wait();
 }
 
 // clusters of C CTAs that run on the GPU at a time (asked once per context and size)
