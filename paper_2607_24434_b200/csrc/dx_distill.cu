@@ -428,24 +428,30 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       MaxSum st{-FLT_MAX, 0.f};
       const unsigned short* marks = reinterpret_cast<const unsigned short*>(s_mark) + (b * kRowThreads + tid) * half;
       unsigned long long s2 = f2_pack(0.f, 0.f);
-      unsigned int marked = 0;
+      // The listed words are left out of the sums: their elements of this thread's vectors q0 .. q1 - 1 become -inf where
+      // they lie (a warp has a handful per row; the sweep knows nothing of them).
+      auto leave_out = [&](int q0, int q1) {
+#pragma unroll 1
+        for (int w16 = q0 >> 4; w16 << 4 < q1; ++w16) {
+          unsigned int marked = marks[w16];
+          if (w16 << 4 < q0) marked &= ~0u << (q0 & 15);
+          if (q1 - (w16 << 4) < 16) marked &= (1u << (q1 - (w16 << 4))) - 1u;
+#pragma unroll 1
+          for (; marked; marked &= marked - 1) {
+            const int q = (w16 << 4) + __ffs(marked) - 1, vec = sp.v_lo + tid + q * kRowThreads;
+            int h = vec & (kHash - 1);
+            for (int tries = 0; tries < kHash && s_hash[b][h] >> 8 != (unsigned int)vec + 1u; ++tries)
+              h = (h + 1) & (kHash - 1);
+            uint4 v = load_shared(s_mine + q * kRowThreads * 16);
+            mask_vector<T>(v, s_hash[b][h]);
+            store_shared(s_mine + q * kRowThreads * 16, v);
+          }
+        }
+        __syncwarp();
+      };
       // All warps start from the largest unlisted element of their first vectors as the reference of the exponents; a
       // thread takes another only when it meets an element more than 2^kSlack times as likely.
       auto add = [&](uint4 (&v)[kUnroll], int q, int n_v) {
-        if ((q & 15) == 0) marked = marks[q >> 4];
-        if (marked & ((1u << kUnroll) - 1u)) {
-#pragma unroll
-          for (int u = 0; u < kUnroll; ++u) {
-            if (marked >> u & 1u) {
-              const int vec = sp.v_lo + tid + (q + u) * kRowThreads;
-              int h = vec & (kHash - 1);
-              for (int tries = 0; tries < kHash && s_hash[b][h] >> 8 != (unsigned int)vec + 1u; ++tries)
-                h = (h + 1) & (kHash - 1);
-              mask_vector<T>(v[u], s_hash[b][h]);
-            }
-          }
-        }
-        marked >>= kUnroll;
         const float top = n_v == 1 ? V16::largest(v[0]) : V16::largest(v, kUnroll);
         if (q == 0) {
           st.m = fmaxf(warp_max(top), -FLT_MAX);
@@ -471,13 +477,16 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       };
       uint32_t held = s_mine;
       int q = 0;
+      auto second_half = [&]() {                     // the vectors from `late` on are there; the next row's first half is asked for
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (!kGrad) asm volatile("cp.async.commit_group;" ::: "memory");
+        leave_out(late, deep);
+      };
       asm volatile("cp.async.wait_group 1;" ::: "memory");
+      leave_out(0, late);
 #pragma unroll 1
       for (; (q + kUnroll) * kRowThreads <= (kGrad ? n_vec : plain); q += kUnroll) {
-        if (q == late) {
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-          if (!kGrad) asm volatile("cp.async.commit_group;" ::: "memory");
-        }
+        if (q == late) second_half();
         uint4 v[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) v[u] = load_shared(held + u * kRowThreads * 16);
@@ -489,13 +498,9 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         held += kUnroll * kRowThreads * 16;
         if (!kGrad) fetch += kUnroll * kRowThreads;
       }
-      if (kGrad) asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll 1
       for (; q < (kGrad ? deep : max(deep, next_deep)); q += kUnroll) {   // what is left: less than kUnroll vectors per
-        if (!kGrad && q == late) {                                        // thread, and one more for some
-          asm volatile("cp.async.wait_group 0;" ::: "memory");
-          asm volatile("cp.async.commit_group;" ::: "memory");
-        }
+        if (q == late) second_half();                                     // thread, and one more for some
         uint4 v[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {

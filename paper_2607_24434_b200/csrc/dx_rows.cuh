@@ -163,6 +163,10 @@ __device__ __forceinline__ uint4 load_shared(uint32_t addr) {
   return r;
 }
 
+__device__ __forceinline__ void store_shared(uint32_t addr, const uint4& v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 // ---- clusters ---------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
