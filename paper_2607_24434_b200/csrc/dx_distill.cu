@@ -41,12 +41,19 @@ struct DistillParams {
   int32_t* dev_status;
 };
 
+// log2(e) / T in two parts, the first rounded down: rounded to one, it would shift the exponents of all words the same way,
+// and a gradient that is a small difference of q and p would show it.
+struct Factor {
+  float hi, lo;
+};
+__device__ __forceinline__ float scaled_ex2(float d, Factor f) { return row_ex2(fmaf(d, f.lo, d * f.hi)); }
+
 struct MaxSum {
   float m, s;
 };
-__device__ __forceinline__ MaxSum join(MaxSum x, MaxSum y, float c) {
+__device__ __forceinline__ MaxSum join(MaxSum x, MaxSum y, Factor c) {
   const float m = fmaxf(x.m, y.m);
-  return MaxSum{m, x.s * row_ex2((x.m - m) * c) + y.s * row_ex2((y.m - m) * c)};
+  return MaxSum{m, x.s * scaled_ex2(x.m - m, c) + y.s * scaled_ex2(y.m - m, c)};
 }
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
@@ -56,7 +63,7 @@ __device__ __forceinline__ double warp_sum(double v) {
 // What the gradient needs to know of the list: the largest listed logit, sum_j e^{(z_j - z_ref) / T}, the teacher's mass
 // with and of the tail bucket, and what its p_j are multiplied with.
 struct ListSums {
-  float z_ref, sum_e, beta, rest, norm;
+  float z_ref, sum_e, beta, rest;
 };
 // What the loss of a row is made of.  64-bit logarithms are long chains: kRing rows are finished at a time, a lane each.
 constexpr int kRing = 16;
@@ -86,9 +93,9 @@ __device__ __forceinline__ void mask_vector(uint4& v, unsigned int drop) {
 }
 
 // (maximum, sum) of a warp's lanes; every lane gets them
-__device__ __forceinline__ MaxSum warp_join(MaxSum x, float c) {
+__device__ __forceinline__ MaxSum warp_join(MaxSum x, Factor c) {
   const float m = warp_max(x.m);
-  float s = x.s * row_ex2((x.m - m) * c);
+  float s = x.s * scaled_ex2(x.m - m, c);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return MaxSum{m, s};
@@ -104,7 +111,7 @@ struct RowSums {
   float M;                    // the larger of the two references
   float w_rest, w_list, S;    // factors that bring the two sums to M; the whole sum relative to it
 };
-__device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l, int n, float c) {
+__device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l, int n, Factor c) {
   RowSums r;
   const int lane = threadIdx.x & 31;
   MaxSum x = lane < n ? all[lane] : MaxSum{-FLT_MAX, 0.f};
@@ -113,8 +120,8 @@ __device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l
   r.l = l;
   r.M = fmaxf(r.rest.m, l.z_ref);
   // (fp32: the gradient's factors; a sum that is NaN stays NaN)
-  r.w_rest = r.rest.s > 0.f ? row_ex2((r.rest.m - r.M) * c) : r.rest.s;
-  r.w_list = row_ex2((l.z_ref - r.M) * c);
+  r.w_rest = r.rest.s > 0.f ? scaled_ex2(r.rest.m - r.M, c) : r.rest.s;
+  r.w_list = scaled_ex2(l.z_ref - r.M, c);
   r.S = r.w_rest * r.rest.s + r.w_list * l.sum_e;
   return r;
 }
@@ -125,7 +132,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   using V16 = RowVec<T>;
   // [buffers][kRowThreads][half] 16-bit words -- bit q of a thread's words: its q-th vector holds a listed word -- and
   // behind them the CTA's vectors of the row
-  extern __shared__ uint4 s_dyn[];
+  // (on a 128-byte border: 16 bytes beside a 32-byte one cost a tenth of the time)
+  extern __shared__ __align__(128) uint4 s_dyn[];
   __shared__ __align__(16) unsigned int s_hash[2][kHash];   // vector + 1 << 8 | its listed elements; 0: free
   __shared__ MaxSum s_all[2][DX_ROW_CLUSTER_MAX * kRowWarps];   // sums of all warps of all CTAs of the row
   __shared__ ListSums s_list[2];
@@ -135,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = C > 1 ? (int)cluster_rank() : 0;
   const int n_rows = gridDim.x / C;                // rows in flight: row t is followed by row t + n_rows
-  const float c = p.c;
+  const Factor c{p.c, p.c_lo};
   const int half = p.half;
   unsigned int* s_mark = reinterpret_cast<unsigned int*>(s_dyn);
   if (C > 1) cluster_arrive();
@@ -152,7 +160,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     // The list's part in a row: logits and log p_j, on their way while the row in front is worked on; then per entry
     // e^{(z_j - z_ref) / T} -- later the word's gradient, stored when the next row begins -- and p_j, the sums for the
     // gradient, and the sums for the loss (log p_j is what the caller has given).
-    float z[kLists], lp[kLists], e[kLists], pj[kLists];
+    float z[kLists], lp[kLists], g[kLists];
+    double e[kLists], pj[kLists], norm = 1.0;      // (64 bits: where q is close to p, their difference shows every rounding)
     int at[kLists];
     T* last_out = nullptr;
     ListSums l{};
@@ -233,56 +242,73 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       live = __any_sync(0xffffffffu, live);
       if (lane == 0) s_weight[b] = live ? weight : 0.f;
     };
+    // the teacher's part in the row whose ids and log p_j are at hand: p_j, their mass, sum p log p, renormalisation
+    auto teacher = [&]() {
+      mass = p_log_p = 0.0;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) {
+        pj[i] = 0.0;
+        if (32 * i >= p.k) continue;
+        const double pd = id[i] >= 0 ? exp((double)lp[i]) : 0.0;   // (a NaN makes the mass NaN, and with it the loss)
+        pj[i] = pd;
+        mass += pd;
+        if (pd > 0.0) p_log_p += pd * (double)lp[i];
+      }
+      mass = warp_sum(mass);
+      p_log_p = warp_sum(p_log_p);
+      norm = 1.0;
+      if (!p.tail && mass != 0.0) {                // p' = p / mass:  sum p' log p' = (sum p log p) / mass - log mass
+        norm = 1.0 / mass;
+        p_log_p = p_log_p * norm - log(mass);
+        mass = mass == mass ? 1.0 : mass;
+      }
+    };
+    // what the sweep's warps wait for
     auto list_sums = [&](int slot) {
       float top = -FLT_MAX;
 #pragma unroll
       for (int i = 0; i < kLists; ++i) {
         at[i] = id[i];
-        if (at[i] < 0) z[i] = lp[i] = -INFINITY;   // (listed before)
+        if (at[i] < 0) z[i] = -INFINITY;           // (unused, or listed before)
         top = fmaxf(top, z[i]);
       }
       l.z_ref = warp_max(top);
-      mass = p_log_p = p_u = sum_e = 0.0;
+      if (kGrad) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i)
+          if (32 * i < p.k && at[i] >= 0) s += expf((float)(((double)z[i] - (double)l.z_ref) * p.inv_T));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        const double rest = p.tail && mass < 1.0 ? 1.0 - mass : 0.0;
+        l.sum_e = s;
+        l.beta = (float)(mass + rest);
+        l.rest = (float)rest;
+        if (lane == 0) s_list[slot] = l;
+        __syncwarp();
+      }
+    };
+    // the student's part in 64 bits, for the loss and the listed words' gradient (nobody waits for it)
+    auto student = [&]() {
+      p_u = sum_e = 0.0;
 #pragma unroll
       for (int i = 0; i < kLists; ++i) {
-        e[i] = pj[i] = 0.f;
+        e[i] = 0.0;
         if (32 * i >= p.k) continue;
         const double u = ((double)z[i] - (double)l.z_ref) * p.inv_T;
-        e[i] = at[i] >= 0 ? expf((float)u) : 0.f;
-        const double pd = exp((double)lp[i]);      // (a NaN entry makes the mass NaN, and with it the loss)
-        pj[i] = (float)pd;
-        sum_e += (double)e[i];
-        mass += pd;
-        if (pd > 0.0) {
-          p_log_p += pd * (double)lp[i];
-          p_u += pd * u;
-        }
+        e[i] = at[i] >= 0 ? exp(u) : 0.0;
+        sum_e += e[i];
+        if (pj[i] > 0.0) p_u += pj[i] * u;
       }
       sum_e = warp_sum(sum_e);
-      mass = warp_sum(mass);
-      p_log_p = warp_sum(p_log_p);
-      p_u = warp_sum(p_u);
-      l.norm = 1.f;
-      if (!p.tail && mass != 0.0) {                // p' = p / mass:  sum p' log p' = (sum p log p) / mass - log mass
-        const double norm = 1.0 / mass;
-        l.norm = (float)norm;
-        p_log_p = p_log_p * norm - log(mass);
-        p_u *= norm;
-        mass = mass == mass ? 1.0 : mass;
-      }
-      const double rest = p.tail && mass < 1.0 ? 1.0 - mass : 0.0;
-      l.sum_e = (float)sum_e;
-      l.beta = (float)(mass + rest);
-      l.rest = (float)rest;
-      if (lane == 0) s_list[slot] = l;
-      __syncwarp();
+      p_u = warp_sum(p_u) * norm;
     };
     auto store_listed = [&]() {                    // over what the sweep has left in their places
       if constexpr (kGrad) {
         if (!last_out) return;
 #pragma unroll
         for (int i = 0; i < kLists; ++i)
-          if (at[i] >= 0) last_out[at[i]] = V16::round(e[i]);
+          if (at[i] >= 0) last_out[at[i]] = V16::round(g[i]);
         last_out = nullptr;
       }
     };
@@ -326,16 +352,20 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     for (int it = 0; t < p.N; ++it, t += n_rows) {
       cta_barrier();
       if (!kGrad) collect();
+      if (kGrad && it == 0) teacher();             // (of later rows it is ready by now)
       store_listed();
       const float scale = s_weight[it & (buffers - 1)] * p.inv_Tf;
       if (s_weight[it & (buffers - 1)] == 0.f) {   // nothing to learn from this row
         if (rank == 0 && lane == 0 && p.loss) p.loss[t] = 0.f;
         mark(t + n_rows, (it + 1) & (buffers - 1));
+        if (kGrad) teacher();
         continue;
       }
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
       list_sums(turn);
       if (C > 1) cluster_arrive();
+      if (!kGrad) teacher();
+      student();
       mark(t + n_rows, (it + 1) & (buffers - 1));
       __syncwarp();
       if (!kGrad) {
@@ -348,17 +378,20 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       const RowSums r = row_sums(s_all[turn], l, C * kRowWarps, c);
       turn ^= 1;
       if (kGrad) {
-        const float f = r.S == 0.f ? 0.f : l.beta * r.w_list / r.S;
+        const double M = (double)fmaxf(r.rest.m, l.z_ref), w_list = exp(((double)l.z_ref - M) * p.inv_T);
+        const double S = (r.rest.s > 0.f ? exp(((double)r.rest.m - M) * p.inv_T) : 1.0) * (double)r.rest.s + w_list * sum_e;
+        const double f = S == 0.0 ? 0.0 : (p.tail && mass < 1.0 ? 1.0 : mass) * w_list / S;
         last_out = reinterpret_cast<T*>(p.dlogits) + (size_t)t * (size_t)p.ld_d;
         const RowSplit sp = row_split(row, p.V, rank, C);
 #pragma unroll
         for (int i = 0; i < kLists; ++i) {
-          e[i] = r.S == 0.f ? 0.f : (f * e[i] - pj[i] * l.norm) * scale;
+          g[i] = S == 0.0 ? 0.f : (float)(f * e[i] - pj[i] * norm) * scale;
           const int v = (at[i] - sp.head) / V16::kN;
           if (at[i] < sp.head ? rank != 0 : at[i] >= p.V - sp.tail ? rank != C - 1 : v < sp.v_lo || v >= sp.v_hi) at[i] = -1;
         }
       }
       if (rank == 0 && p.loss) keep(r, t);
+      teacher();
     }
     if (kGrad) {
       finish();
@@ -377,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   // this thread's vectors of the row: every 4096 bytes from here
   const uint32_t s_mine =
       static_cast<uint32_t>(__cvta_generic_to_shared(s_dyn + buffers * half * (kRowThreads / 8) + tid));
-  const unsigned long long c2 = f2_pack(c, c), cl2 = f2_pack(p.c_lo, p.c_lo);
+  const unsigned long long c2 = f2_pack(c.hi, c.hi), cl2 = f2_pack(p.c_lo, p.c_lo);
   const uint4 none4 = make_uint4(V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord, V16::kNegInfWord);
   int t = blockIdx.x / C, turn = 0;
   bool pending = false;                            // (loss alone) arrived at the cluster's barrier, not waited
@@ -455,10 +488,10 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         const float top = n_v == 1 ? V16::largest(v[0]) : V16::largest(v, kUnroll);
         if (q == 0) {
           st.m = fmaxf(warp_max(top), -FLT_MAX);
-        } else if ((top - st.m) * c > kSlack) {
+        } else if ((top - st.m) * c.hi > kSlack) {
           float s0, s1;
           f2_unpack(s2, s0, s1);
-          s2 = f2_pack((s0 + s1) * row_ex2((st.m - top) * c), 0.f);
+          s2 = f2_pack((s0 + s1) * scaled_ex2(st.m - top, c), 0.f);
           st.m = top;
         }
         const unsigned long long nm2 = f2_pack(-st.m, -st.m);
@@ -467,7 +500,6 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
           if (u >= n_v) continue;
 #pragma unroll
           for (int h = 0; h < V16::kN / 2; ++h) {
-            // (the factor in two parts: rounded to one, it would shift the exponents of all words the same way)
             const unsigned long long d2 = f2_add(V16::pair(v[u], h), nm2);
             float x0, x1;
             f2_unpack(f2_fma(d2, cl2, f2_mul(d2, c2)), x0, x1);
@@ -528,11 +560,11 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         edge_tail = tail_in ? V16::load(row + tail0 + tid) : -INFINITY;
         const float top = fmaxf(edge_head, edge_tail);
         if (top > st.m) {
-          st.s *= row_ex2((st.m - top) * c);
+          st.s *= scaled_ex2(st.m - top, c);
           st.m = top;
         }
-        if (head_in) st.s += row_ex2((edge_head - st.m) * c);
-        if (tail_in) st.s += row_ex2((edge_tail - st.m) * c);
+        if (head_in) st.s += scaled_ex2(edge_head - st.m, c);
+        if (tail_in) st.s += scaled_ex2(edge_tail - st.m, c);
       }
       __syncwarp();
       st = warp_join(st, c);
@@ -584,15 +616,16 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     }
     // ---- the gradient (zeros where there is nothing to learn)
     if (kGrad) {
-      if (head_in) out[tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_head - ref) * c));
-      if (tail_in) out[tail0 + tid] = V16::round(w == 0.f ? 0.f : coef * row_ex2((edge_tail - ref) * c));
+      if (head_in) out[tid] = V16::round(w == 0.f ? 0.f : coef * scaled_ex2(edge_head - ref, c));
+      if (tail_in) out[tail0 + tid] = V16::round(w == 0.f ? 0.f : coef * scaled_ex2(edge_tail - ref, c));
       const unsigned long long nm2 = f2_pack(-ref, -ref), k2 = f2_pack(coef, coef);
       auto gradient = [&](const uint4& v) {
         float g[V16::kN];
 #pragma unroll
         for (int h = 0; h < V16::kN / 2; ++h) {
           float x0, x1;
-          f2_unpack(f2_mul(f2_add(V16::pair(v, h), nm2), c2), x0, x1);
+          const unsigned long long d2 = f2_add(V16::pair(v, h), nm2);
+          f2_unpack(f2_fma(d2, cl2, f2_mul(d2, c2)), x0, x1);
           f2_unpack(f2_mul(f2_pack(row_ex2(x0), row_ex2(x1)), k2), g[2 * h], g[2 * h + 1]);
         }
         return V16::pack(g);
