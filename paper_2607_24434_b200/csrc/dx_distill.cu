@@ -4,15 +4,23 @@
 //     L = sum_j p_j (log p_j - log q_j)  [ + r (log r - log R) ]
 //     dL/dz_v = ( beta q_v - p_v ) / T  for listed v,   ( beta - r / R ) q_v / T  otherwise,  beta = sum p + r
 // One launch reads each logit once and writes each gradient once: a cluster of CTAs holds the row in shared memory
-// between the statistics and the gradient.
+// between the statistics and the gradient, and each vector's place takes the next row's vector as soon as it has been
+// read for the last time.
 //
 // The unlisted words are summed apart from the listed ones, relative to their own maximum: R never comes out of a
 // difference of nearly equal sums, and neither R nor the factor r / R can under- or overflow however far the listed
-// words stand above the rest.  A bit per vector tells the sweep which vectors hold listed words; a small hash table says
-// which of their elements, and those count as -inf.  A ninth warp does the arithmetic on the list while the other eight
-// stream the row.  The warps' sums go straight into the shared memory of all CTAs of the row, so that one cluster
-// barrier is all that stands between the sweep and the gradient.  Per-row scalars of the loss are 64-bit (it is a small
-// difference of logarithms) and are not waited for by the gradient.
+// words stand above the rest.  A bit per vector says which vectors hold listed words, a small hash table which of their
+// elements; those become -inf in shared memory in front of the sweep.  A ninth warp does the arithmetic on the list while
+// the other eight go over the row: in 64 bits for the loss and the listed words' gradient (both are small differences),
+// in 32 bits and first of all for what the eight wait for.  The warps' sums go straight into the shared memory of all
+// CTAs of the row, so that one cluster barrier is all that stands between the sweep and the gradient; without a gradient
+// nobody waits at all, and a row's sums are collected while the next row is summed.
+//
+// What bounds it: HBM for fp32 (1024 x 163840 with gradient 236 us, 83 % of the measured copy bandwidth; loss alone
+// 120 us, 87 %); for bf16 there are twice as many exponentials per byte and the two that a logit needs with a gradient keep
+// their pipe busy for 55 % of the time (2048 x 102400, list of 64: 164 us, 79 %; loss alone 97 us, 67 %).  Short rows pay
+// the fixed part of a row per warp -- about half as many instructions as a sweep of 25 vectors -- more often: 8192 x 32000
+// bf16 220 us, 74 %.
 #include <cmath>
 
 #include "dx_rows.cuh"
@@ -126,7 +134,8 @@ __device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l
   return r;
 }
 
-// kLists: list entries per lane of the list's warp, at least k / 32 (its registers would not last for four where two do)
+// kLists: list entries per lane of the list's warp, at least k / 32 (with four for all the batch above took 201 us, the
+// list's registers being spilled)
 template <typename T, bool kGrad, int kLists>
 __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(DistillParams p, int C, int buffers) {
   using V16 = RowVec<T>;
@@ -705,8 +714,9 @@ cudaError_t max_clusters(dx_ctx* ctx, int C, size_t smem, int* out) {
 
 template <typename T, bool kGrad, int kLists>
 cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
-  // CTAs per row: few enough bytes per CTA that two fit an SM (one works while the other waits for its row), and as many
-  // as fill the GPU when there are few rows.  (The same with and without the gradient: so is the loss, bit for bit.)
+  // CTAs per row: few enough bytes per CTA that two fit an SM (one works while the other waits for its row; four with half
+  // the slice took 182 us where two took 172), and as many as fill the GPU when there are few rows (8 x 102400 bf16: 8.0 us,
+  // without that 9.9).  (The same with and without the gradient: so is the loss, bit for bit.)
   const long long bytes = (long long)p.V * (long long)sizeof(T);
   const int slots = 2 * ctx->sm_count;
   int C = 1;

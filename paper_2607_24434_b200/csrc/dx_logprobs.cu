@@ -3,7 +3,7 @@
 // (Both terms of H are non-negative, nothing cancels.)  The n alternatives are the largest z, ties to the lower id.
 //
 // One pass: every logit is read from HBM once.  Threads carry (a reference near the maximum, S, sum u e^u)
-// relative to it, four 16-byte vectors at a time.  Alternatives ride along as each thread's largest logit, one per segment of its
+// relative to it, three 16-byte vectors at a time.  Alternatives ride along as each thread's largest logit, one per segment of its
 // share of the row.  From the threads' maxima one warp picks a threshold that at least n and at most n + kFlagSlack
 // threads reach; only the runs (thread, segment) that reach it can hold one of the n largest, so they alone -- one or
 // two percent of the row -- are read again, and the few elements that pass are ranked by counting.  Where more threads
@@ -11,11 +11,16 @@
 // the order of their ids.  A row of few-row calls is split over a cluster of up to 16 CTAs, whose statistics and lists
 // the first CTA joins through distributed shared memory: no workspace, no atomics on device memory, one launch, the
 // same result on every run.
+//
+// What bounds it: without alternatives HBM and the exponentials (2048 x 102400 bf16: 75 us, 87 % of the measured copy
+// bandwidth); with 20 alternatives 86 us, 76 %: the second look and its barriers stop a CTA's loads for a quarter of its
+// row, and the other three CTAs of the SM do not cover all of it (a ninth warp that did the selection alone: 106 us).
+// Few rows are a chain of latencies: 1 x 102400 9 us, 16 x 163840 fp32 12 us.
 #include "dx_rows.cuh"
 
 namespace {
 
-constexpr int kUnroll = 3;
+constexpr int kUnroll = 3;        // vectors at a time, as many on their way (2: 101 us, 4: 96 us, 3: 87 us for the batch above)
 constexpr float kSlack = 8.f;      // powers of two by which an element may exceed the reference of its thread's sums
 constexpr int kSegments = 8;      // parts of a thread's share of the row that have a maximum of their own
 constexpr int kFlagSlack = 12;    // the threshold may be reached by n + this many threads
@@ -522,7 +527,8 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
 
 template <typename T>
 cudaError_t launch(dx_ctx* ctx, const LogprobParams& p, cudaStream_t st) {
-  // As many CTAs per row as fill the GPU (four per SM), while each still has a vector for every thread.
+  // As many CTAs per row as fill the GPU (four per SM), while each still has a vector for every thread (a row of 102400 bf16
+  // alone: 9.1 us, with one CTA 11.7; sixteen of 163840 fp32: 11.6 and 19.7 us).
   const int slots = 4 * ctx->sm_count;
   int C = 1;
   while (C < DX_ROW_CLUSTER_MAX && (long long)p.N * C * 2 <= slots &&
