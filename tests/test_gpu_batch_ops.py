@@ -847,3 +847,49 @@ def test_training_step_of_a_small_drafter(dx):
     for have, ref in zip((d_r, d_e, d_lm), want):
         # (fp32 matrix products of a few hundred terms on top of the operators' own error)
         assert float((have.double() - ref).abs().max()) <= 1e-4 * float(ref.abs().max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("N,V,k", [(9000, 1001, 7), (9001, 1000, 40), (2600, 60003, 9), (1000, 400001, 33)])
+def test_distill_many_rows_per_cta(dx, dtype, tail, N, V, k):
+    """Rows by the dozen on every CTA, with and without a gradient, rows of weight zero and of no list among them: all
+    losses against 64 bits, the same with and without gradient, and the gradients' sums (zero up to roundings)."""
+    binding, ctx = dx
+    if dtype is torch.float32 and V > 100000:
+        N //= 2
+    g = torch.Generator(device="cuda").manual_seed(N + V)
+    z = torch.empty((N, V), dtype=dtype, device="cuda")
+    ids = torch.empty((N, k), dtype=torch.int32, device="cuda")
+    lp = torch.empty((N, k), device="cuda")
+    w = torch.rand((N,), generator=g, device="cuda") + 0.5
+    w[2::5] = 0.0
+    loss = torch.empty((N,), dtype=torch.float64, device="cuda")
+    for a in range(0, N, 100):
+        b = min(a + 100, N)
+        x = torch.randn((b - a, V), generator=g, device="cuda") * 2
+        z[a:b] = x.to(dtype)
+        t = torch.log_softmax(x + torch.randn((b - a, V), generator=g, device="cuda"), 1)
+        l, i = t.topk(k, dim=1)
+        ids[a:b], lp[a:b] = i.int(), l
+        logq = torch.log_softmax(z[a:b].double(), 1).gather(1, i)
+        p = l.double().exp()
+        if tail:
+            r = 1 - p.sum(1)
+            loss[a:b] = (p * (l.double() - logq)).sum(1) + r * (r.log() - torch.log1p(-logq.exp().sum(1)))
+        else:
+            p = p / p.sum(1, keepdim=True)
+            loss[a:b] = (p * (p.log() - logq)).sum(1)
+    ids[4::11] = -1
+    loss[4::11] = 0
+    loss[2::5] = 0
+    only = binding.spec_distill_topk(ctx, z, ids, lp, tail=tail, row_weight=w, grad=False)["loss"]
+    got = binding.spec_distill_topk(ctx, z, ids, lp, tail=tail, row_weight=w)
+    assert torch.equal(only, got["loss"])
+    assert bool(((only.double() - loss).abs() <= 2 * S_ERR + 2.0 ** -22 * loss.abs()).all())
+    # a row's gradient is w / T (beta q - p): its sum is that of the errors, S_ERR and a rounding of each part
+    for a in range(0, N, 500):
+        d = got["dlogits"][a:a + 500].double()
+        assert bool((d.sum(1).abs() <= 4 * S_ERR * w[a:a + 500] + HALF[dtype] * d.abs().sum(1)).all())
+        dead = (w[a:a + 500] == 0) | (ids[a:a + 500] < 0).all(1)
+        assert not d[dead].any() and bool((d[~dead].abs().sum(1) > 0).all())
