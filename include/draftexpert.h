@@ -412,7 +412,8 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *   Eq. 8, with the teacher cut to a list of k <= 128 words per row).  teacher_ids / teacher_logprobs [N, k]; an id of -1
  *   is an unused entry, an id listed twice in a row counts once (its first entry), any other id outside [0, V) is left
  *   out and reported as DX_DEV_BAD_TOKEN.  With q = softmax(logits[t] / temperature) and p_j = exp(teacher_logprobs):
- *     tail = 0: p renormalised over the listed words, L_t = sum_j p_j (log p_j - log q_j)  (a list without mass: 0);
+ *     tail = 0: p renormalised over the listed words, L_t = sum_j p_j (log p_j - log q_j)  (a list of nothing but -inf: 0);
+ *               only the differences of a row's teacher_logprobs count, however large or small they are;
  *     tail = 1: p as given, and the rest r = max(0, 1 - sum_j p_j) in one bucket against the student's mass R on all
  *               unlisted words: L_t = sum_j p_j (log p_j - log q_j) + r (log r - log R).
  *   loss [N] = L_t.  dlogits (pitch ld_d) = row_weight[t] * dL_t / dlogits, zeros and loss 0 for rows whose weight is 0

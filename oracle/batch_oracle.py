@@ -51,7 +51,10 @@ def distill_topk(z, ids, lp, tail, temperature, weight=None):
         seen = {}
         for e, l in zip(ids[t], lp[t]):
             if 0 <= e < V and int(e) not in seen:
-                seen[int(e)] = float(np.exp(np.float64(l)))
+                seen[int(e)] = float(l)
+        # (a list that is renormalised: relative to its largest entry, whose exponential may be out of range)
+        top = max((l for l in seen.values() if l > -np.inf), default=0.0) if not tail else 0.0
+        seen = {e: float(np.exp(np.float64(l) - top)) for e, l in seen.items()}
         if w == 0.0 or not seen:
             continue
         mass = sum(seen.values())

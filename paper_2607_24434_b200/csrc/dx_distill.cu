@@ -254,14 +254,26 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     // the teacher's part in the row whose ids and log p_j are at hand: p_j, their mass, sum p log p, renormalisation
     auto teacher = [&]() {
       mass = p_log_p = 0.0;
+      // (a renormalised list is taken relative to its largest entry: only differences count, and no exponential of it
+      // over- or underflows)
+      float top = 0.f;
+      if (!p.tail) {
+        top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kLists; ++i)
+          if (id[i] >= 0) top = fmaxf(top, lp[i]);
+        top = warp_max(top);
+        if (top == -INFINITY) top = 0.f;
+      }
 #pragma unroll
       for (int i = 0; i < kLists; ++i) {
         pj[i] = 0.0;
         if (32 * i >= p.k) continue;
-        const double pd = id[i] >= 0 ? exp((double)lp[i]) : 0.0;   // (a NaN makes the mass NaN, and with it the loss)
+        const double x = (double)lp[i] - (double)top;
+        const double pd = id[i] >= 0 ? exp(x) : 0.0;   // (a NaN makes the mass NaN, and with it the loss)
         pj[i] = pd;
         mass += pd;
-        if (pd > 0.0) p_log_p += pd * (double)lp[i];
+        if (pd > 0.0) p_log_p += pd * x;
       }
       mass = warp_sum(mass);
       p_log_p = warp_sum(p_log_p);

@@ -204,3 +204,13 @@ def test_binding_checks_what_a_pointer_cannot_show():
     with pytest.raises(ValueError):
         binding.moe_route_tokens(Ctx(), torch.zeros(2, 8), 2)
     assert ctypes.sizeof(binding.RouteDesc) == 8 * 4
+
+
+def test_distill_lists_outside_the_range_of_exp():
+    rng = np.random.default_rng(7)
+    z = rng.normal(0, 2, (3, 30))
+    ids = np.tile(np.arange(5), (3, 1))
+    base = -rng.integers(0, 160, 5) / 16.0
+    lp = np.stack([base, base - 1024.0, base + 1024.0])
+    loss, grad, _ = B.distill_topk(np.tile(z[:1], (3, 1)), ids, lp, False, 1.0)
+    assert np.isfinite(loss).all() and loss[0] > 0 and (loss == loss[0]).all() and (grad == grad[0]).all()
