@@ -51,3 +51,56 @@ def test_distill_lists_outside_the_range_of_exp(dx, dtype):
     live = torch.arange(N, device="cuda") != 1
     assert (got["loss"][live] == got["loss"][0]).all() and float(got["loss"][1]) == 0
     assert torch.isfinite(got["dlogits"]).all() and not got["dlogits"][1].any()
+
+
+def near_teacher(N, V, k, eps, T, dtype, seed):
+    """Logits, and the lists of a teacher whose logits differ from them by `eps` at random."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = torch.randn((N, V), generator=g, device="cuda") * 2
+    lift = torch.rand((N, 30), generator=g, device="cuda") * 9 + 3
+    z.scatter_add_(1, torch.randint(0, V, (N, 30), generator=g, device="cuda"), lift)
+    z = z.to(dtype)
+    noise = torch.randn((N, V), generator=g, device="cuda", dtype=torch.float64)
+    lp, ids = torch.log_softmax(z.double() / T + eps * noise, 1).topk(k, dim=1)
+    return z, ids.to(torch.int32), lp.float()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("N,V,k,T", [(512, 2000, 20, 1.0), (128, 32003, 20, 1.0), (128, 32003, 70, 1.0), (64, 102400, 20, 1.0),
+                                     (400, 9000, 5, 2.0), (40, 163840, 100, 0.7)])
+@pytest.mark.parametrize("eps", [1e-3, 1e-5])
+def test_distill_gradient_of_a_student_close_to_its_teacher(dx, dtype, tail, N, V, k, T, eps):
+    """The gradient is then a small difference.  With R the student's mass on the unlisted words, r the teacher's, P = 1 - R,
+    the only inexact sum is R's: its exponentials are good to 2^-22 and to 2^-24 on average, their arguments and the sums add
+    errors of either sign that average out over the words, so R is good to 2^-23 (rms over rows).  An unlisted word's
+    factor beta - r / R is off by P times that (r close to R), a listed word's beta q - p by p R times that; either is rounded to
+    the output's type."""
+    binding, ctx = dx
+    T = float(np.float32(T))                            # (what the entry point gets)
+    z, ids, lp = near_teacher(N, V, k, eps, T, dtype, seed=N + V)
+    d = binding.spec_distill_topk(ctx, z, ids, lp, tail=tail, temperature=T)["dlogits"].double() * T
+    q = torch.softmax(z.double() / T, 1)
+    at = ids.long()
+    p = lp.double().exp()
+    other = q.scatter(1, at, 0.0)
+    R = other.sum(1)
+    if not tail:
+        p = p / p.sum(1, keepdim=True)
+    rest = (1 - p.sum(1)) if tail else torch.zeros_like(R)
+    beta = p.sum(1) + rest
+    want = beta[:, None] * q.gather(1, at) - p
+    tol = 2.0 ** -23 * p * R[:, None] + HALF[dtype] * want.abs()
+    err = (d.gather(1, at) - want) / tol
+    assert float(err.pow(2).mean().sqrt()) <= 1, float(err.pow(2).mean().sqrt())
+    factor = beta - rest / R
+    # (the factor as the row's unlisted words show it together: each of them is factor times an exponential, whose argument of
+    # at most 20 powers of two is rounded twice, 2 * 20 * 2^-24 * ln 2, and which is good to 2^-22 itself; the factor's last
+    # quotient and products add 2^-21: below 2^-18 together; words of equal logits, which bf16 has many of, are rounded alike,
+    # so the roundings of the output add up to half a step of the sum)
+    have = d.scatter(1, at, 0.0).sum(1) / R
+    tol = 2.0 ** -23 * (1 - R) + (HALF[dtype] + 2.0 ** -18) * factor.abs()
+    err = (have - factor) / tol
+    assert float(err.pow(2).mean().sqrt()) <= 1, float(err.pow(2).mean().sqrt())
+    if tail and eps == 1e-3:
+        assert bool((have.sign() == factor.sign())[factor.abs() > 2.0 ** -20].all())
