@@ -417,7 +417,8 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *     tail = 1: p as given, and the rest r = max(0, 1 - sum_j p_j) in one bucket against the student's mass R on all
  *               unlisted words: L_t = sum_j p_j (log p_j - log q_j) + r (log r - log R).
  *   loss [N] = L_t.  dlogits (pitch ld_d) = row_weight[t] * dL_t / dlogits, zeros and loss 0 for rows whose weight is 0
- *   or that list no word (their logits are not looked at).  row_weight NULL: all 1.  loss or dlogits may be NULL.
+ *   or that list no word (their logits do not matter; but for the row that a CTA begins with they are not fetched).
+ *   row_weight NULL: all 1.  loss or dlogits may be NULL.
  *   dlogits may be the logits buffer itself (same pitch), or lie between its rows; its rows must not overlap the logits'
  *   otherwise (DX_ERR_INVALID_ARG).
  *   A listed word that the student gives no mass makes the loss +inf (its gradient stays finite); a row of nothing but

@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   __shared__ ListSums s_list[2];
   __shared__ double s_list64[2][2];                // (tail bucket) the teacher's mass on the list, the student's sum in 64 bits
   __shared__ unsigned int s_edge[2];               // head (bits 0..7) and tail (8..15) elements that are listed
-  __shared__ float s_weight[2];                    // 0: nothing to learn from the row
+  __shared__ float2 s_weight[2];                   // x = 0: nothing to learn from the row; y = 0: from the row behind
   __shared__ LossTerms s_ring[kRing];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = C > 1 ? (int)cluster_rank() : 0;
@@ -210,8 +210,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
   if (warp == kRowWarps) {
     // ==== the list warp
     int id[kLists];                                // entry lane + 32 i (-1: unused, out of range, listed before)
-    int raw[kLists];                               // ... of the row behind, as given; its weight
-    float w = 0.f;
+    int raw[kLists];                               // ... of the row behind, as given
+    float w = 0.f, weight = 0.f;                   // weight of the row behind; of the row that is marked
     // The list's part in a row: logits and log p_j, on their way while the row in front is worked on; then per entry
     // e^{(z_j - z_ref) / T} -- later the word's gradient, stored when the next row begins -- and p_j, the sums for the
     // gradient, and the sums for the loss (log p_j is what the caller has given).
@@ -227,18 +227,32 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       for (int i = 0; i < kLists; ++i) raw[i] = lane + 32 * i < p.k ? p.ids[(size_t)t * p.k + lane + 32 * i] : -1;
       w = p.weight ? p.weight[t] : 1.f;
     };
+    // The ids of row t are at hand, those of the row behind it are asked for: early in the row in front of t, so that they
+    // are there when that row ends (asked for among the marks they kept everyone waiting, 2 % of a loss alone).
+    auto take_ids = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) id[i] = raw[i];
+      weight = w;
+      load_ids(t + n_rows);
+    };
+    // whether there is something to learn from the row behind, for those who fetch it
+    auto announce = [&](int t, int b) {
+      if (t >= p.N) return;
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < kLists; ++i) any |= raw[i] >= 0 && raw[i] < p.V;
+      any = __any_sync(0xffffffffu, any);
+      if (lane == 0) s_weight[b].y = any && w != 0.f ? 1.f : 0.f;
+    };
     auto mark = [&](int t, int b) {                // ids -> marks, hash table and state of buffer b
       if (t >= p.N) return;
-      const float weight = w;
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
 #pragma unroll
       for (int i = 0; i < kLists; ++i) {
-        const bool in = raw[i] >= 0 && raw[i] < p.V;
-        id[i] = raw[i];
-        z[i] = in ? V16::load(row + raw[i]) : -INFINITY;
+        const bool in = id[i] >= 0 && id[i] < p.V;
+        z[i] = in ? V16::load(row + id[i]) : -INFINITY;
         lp[i] = in ? p.lp[(size_t)t * p.k + lane + 32 * i] : -INFINITY;
       }
-      load_ids(t + n_rows);
       const RowSplit sp = row_split(row, p.V, rank, C);
       const int n_vec = sp.v_hi - sp.v_lo, tail0 = p.V - sp.tail;
       unsigned int* marks = s_mark + b * half * (kRowThreads / 2);
@@ -295,10 +309,10 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       }
       if (bad && rank == 0) *p.dev_status = DX_DEV_BAD_TOKEN;
       live = __any_sync(0xffffffffu, live);
-      if (lane == 0) s_weight[b] = live ? weight : 0.f;
+      if (lane == 0) s_weight[b].x = live ? weight : 0.f;
     };
     // the teacher's part in the row whose ids and log p_j are at hand: p_j, their mass, sum p log p, renormalisation
-    auto teacher = [&]() {
+    auto teacher = [&](const int (&ids)[kLists]) {
       mass = p_log_p = 0.0;
       // (a renormalised list is taken relative to its largest entry: only differences count, and no exponential of it
       // over- or underflows)
@@ -307,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kLists; ++i)
-          if (id[i] >= 0) top = fmaxf(top, lp[i]);
+          if (ids[i] >= 0) top = fmaxf(top, lp[i]);
         top = warp_max(top);
         if (top == -INFINITY) top = 0.f;
       }
@@ -316,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         pj[i] = 0.0;
         if (32 * i >= p.k) continue;
         const double x = (double)lp[i] - (double)top;
-        const double pd = id[i] >= 0 ? exp(x) : 0.0;   // (a NaN makes the mass NaN, and with it the loss)
+        const double pd = ids[i] >= 0 ? exp(x) : 0.0;   // (a NaN makes the mass NaN, and with it the loss)
         pj[i] = pd;
         mass += pd;
         if (pd > 0.0) p_log_p += pd * x;
@@ -419,27 +433,31 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       pending = -1;
     };
     load_ids(t);
+    take_ids(t);
     mark(t, 0);
     if (C > 1) cluster_wait();                     // (all CTAs of the row have started)
 #pragma unroll 1
     for (int it = 0; t < p.N; ++it, t += n_rows) {
+      announce(t + n_rows, it & (buffers - 1));
       cta_barrier();
       if (!kGrad) collect();
-      if (kGrad && it == 0) teacher();             // (of later rows it is ready by now)
+      if (kGrad && it == 0) teacher(id);           // (of later rows it is ready by now)
       store_listed();
-      const float scale = s_weight[it & (buffers - 1)] * p.inv_Tf;
-      if (s_weight[it & (buffers - 1)] == 0.f) {   // nothing to learn from this row
+      const float scale = s_weight[it & (buffers - 1)].x * p.inv_Tf;
+      if (s_weight[it & (buffers - 1)].x == 0.f) {   // nothing to learn from this row
         if (rank == 0 && lane == 0 && p.loss) p.loss[t] = 0.f;
+        take_ids(t + n_rows);
         mark(t + n_rows, (it + 1) & (buffers - 1));
-        if (kGrad) teacher();
+        if (kGrad) teacher(id);
         continue;
       }
       const T* row = reinterpret_cast<const T*>(p.logits) + (size_t)t * (size_t)p.ld;
       list_top();
+      take_ids(t + n_rows);
       const bool wide = kGrad && p.tail != 0;
       if (kGrad && !wide) publish(turn);
       if (C > 1 && !wide) cluster_arrive();
-      if (!kGrad) teacher();
+      if (!kGrad) teacher(at);
       student();
       if (wide) {
         publish(turn);
@@ -470,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         }
       }
       if (rank == 0 && p.loss) keep(r, t);
-      teacher();
+      teacher(id);
     }
     if (kGrad) {
       finish();
@@ -524,11 +542,12 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     const T* next = row + (size_t)n_rows * (size_t)p.ld;
     t += n_rows;
     const RowSplit np = t < p.N ? row_split(next, p.V, rank, C) : sp;
-    const int next_vecs = t < p.N ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
-    const int plain = min(n_vec, next_vecs ? next_vecs : n_vec);
     const uint4* fetch = reinterpret_cast<const uint4*>(next + np.head) + np.v_lo + tid;
     cta_barrier();
-    const float w = s_weight[b];
+    const float2 wn = s_weight[b];                 // (a row there is nothing to learn from stays where it is)
+    const int next_vecs = t < p.N && wn.y != 0.f ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
+    const int plain = min(n_vec, next_vecs ? next_vecs : n_vec);
+    const float w = wn.x;
     float coef = 0.f, ref = 0.f;                   // gradient of an unlisted word: coef * e^{(z - ref) / T}
     float edge_head = -INFINITY, edge_tail = -INFINITY;
     bool head_in = has_head, tail_in = has_tail;   // this thread's edge elements that are not listed
@@ -741,10 +760,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
       for (; q < max(deep, next_deep); ++q, held += kRowThreads * 16, fetch += kRowThreads, store += kRowThreads) {
         if (q == late) asm volatile("cp.async.commit_group;" ::: "memory");
         const int i = tid + q * kRowThreads;
-        uint4 v = none4;
-        if (i < n_vec) v = load_shared(held);
         if (i < n_vec) {
-          v = w == 0.f ? make_uint4(0, 0, 0, 0) : gradient(v);   // (whatever the logits hold)
+          const uint4 v = w == 0.f ? make_uint4(0, 0, 0, 0) : gradient(load_shared(held));   // (whatever the logits hold)
           if (same_align) {
             *store = v;
           } else {

@@ -104,3 +104,41 @@ def test_distill_gradient_of_a_student_close_to_its_teacher(dx, dtype, tail, N, 
     assert float(err.pow(2).mean().sqrt()) <= 1, float(err.pow(2).mean().sqrt())
     if tail and eps == 1e-3:
         assert bool((have.sign() == factor.sign())[factor.abs() > 2.0 ** -20].all())
+
+
+def microseconds(call, repeats=9):
+    times = []
+    for _ in range(repeats):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        call()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b) * 1e3)
+    return sorted(times)[repeats // 2]
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_distill_rows_without_weight_or_list_are_not_fetched(dx, grad):
+    """The logits of such rows are not read (but for the few that a CTA begins with): a batch of 840 MB of them takes a
+    fraction of the time of one whose rows all count -- with a gradient half of it, the zeros being written, else next
+    to nothing -- and so does a batch whose second half is padding."""
+    binding, ctx = dx
+    N, V, k = 4096, 102400, 8
+    z = torch.zeros((N, V), dtype=torch.bfloat16, device="cuda")
+    ids = torch.randint(0, V, (N, k), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.int32)
+    lp = torch.full((N, k), -3.0, device="cuda")
+    one, half = torch.ones(N, device="cuda"), torch.arange(N, device="cuda") < N // 2
+    out = {"loss": torch.empty(N, device="cuda")}
+    if grad:
+        out["dlogits"] = torch.empty_like(z)
+
+    def time(weight, lists):
+        call = lambda: binding.spec_distill_topk(ctx, z, lists, lp, row_weight=weight, grad=grad, out=out)  # noqa: E731
+        call()
+        return microseconds(call)
+
+    none = torch.full_like(ids, -1)
+    whole = time(one, ids)
+    assert time(0 * one, ids) <= 0.65 * whole and time(one, none) <= 0.65 * whole
+    assert time(half.float(), ids) <= 0.8 * whole and time(one, torch.where(half[:, None], ids, none)) <= 0.8 * whole
