@@ -50,6 +50,7 @@ struct BatchRouteParams {
   int32_t* offsets;
   int32_t* perm;
   int32_t* counts;                // [CTAs][E] context scratch
+  int32_t* dev_status;
 };
 
 __device__ __forceinline__ float to_f(float x) { return x; }
@@ -172,7 +173,7 @@ __device__ __noinline__ int settle(const BatchRouteParams& p, const T* row, doub
     }
     int* order = reinterpret_cast<int*>(s_row);
     __syncwarp();
-    if (pick != 0) order[rank] = id;
+    if (pick != 0 && DX_BOUNDS(rank <= p.k, p.dev_status)) order[rank] = id;
     __syncwarp();
     const int mine = order[lane];
     __syncwarp();
@@ -271,7 +272,7 @@ __device__ __noinline__ int settle_groups(const BatchRouteParams& p, const T* ro
 #pragma unroll 1
   while (__any_sync(0xffffffffu, cand != 0)) {
     const int e = e0 + __ffs(cand) - 1;
-    const double v = cand ? exact_sigmoid((double)to_f(row[e])) + (double)bias[e] : -INFINITY;
+    const double v = cand && DX_BOUNDS(e < p.E, p.dev_status) ? exact_sigmoid((double)to_f(row[e])) + (double)bias[e] : -INFINITY;
     __syncwarp();
     cand &= cand - 1;
     if (v > a) { b = a; a = v; }
@@ -307,12 +308,13 @@ __device__ __forceinline__ void load_pairs(const int32_t* ids, long long p0, int
   for (int d = 0; d < kDeep; ++d) q.id[d] = first + 32 * d < n ? ids[p0 + first + 32 * d] : -1;
 }
 // pairs of each expert per warp
-__device__ __forceinline__ void count_pairs(Pairs& q, int E, int (*s_hist)[DX_MAX_E]) {
+__device__ __forceinline__ void count_pairs(Pairs& q, int E, int (*s_hist)[DX_MAX_E], int32_t* dev_status) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int e = lane; e < E; e += 32) s_hist[warp][e] = 0;
   __syncwarp();
 #pragma unroll
   for (int d = 0; d < kDeep; ++d) {
+    if (!DX_BOUNDS(q.id[d] < E, dev_status)) q.id[d] = -1;
     q.same[d] = __match_any_sync(0xffffffffu, q.id[d]);
     if (q.id[d] >= 0 && __ffs(q.same[d]) - 1 == lane) s_hist[warp][q.id[d]] += __popc(q.same[d]);
     __syncwarp();
@@ -333,7 +335,7 @@ __device__ __forceinline__ void front_of_warps(int E, int (*s_hist)[DX_MAX_E], i
   }
 }
 __device__ __forceinline__ void scatter_pairs(const Pairs& q, long long first_pair, const int* s_base,
-                                              int (*s_hist)[DX_MAX_E], int32_t* perm) {
+                                              int (*s_hist)[DX_MAX_E], const BatchRouteParams& p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long first = first_pair + warp * 32 * kDeep + lane;
 #pragma unroll
@@ -341,27 +343,29 @@ __device__ __forceinline__ void scatter_pairs(const Pairs& q, long long first_pa
     const int x = q.id[d] >= 0 ? s_hist[warp][q.id[d]] : 0;
     __syncwarp();
     if (q.id[d] >= 0) {
-      perm[s_base[q.id[d]] + x + __popc(q.same[d] & ((1u << lane) - 1u))] = (int32_t)(first + 32 * d);
+      const int at = s_base[q.id[d]] + x + __popc(q.same[d] & ((1u << lane) - 1u));
+      if (DX_BOUNDS(at >= 0 && at < p.N * p.k, p.dev_status)) p.perm[at] = (int32_t)(first + 32 * d);
       if (__ffs(q.same[d]) - 1 == lane) s_hist[warp][q.id[d]] = x + __popc(q.same[d]);
     }
     __syncwarp();
   }
 }
 // the tiles from the first on (whose counts are in place, s_total and s_base filled)
-__device__ __forceinline__ void place_pairs(const int32_t* ids, long long p0, int n, int E, int (*s_hist)[DX_MAX_E],
-                                            int* s_base, int* s_total, int32_t* perm, Pairs& q) {
+__device__ __forceinline__ void place_pairs(const BatchRouteParams& p, long long p0, int n, int (*s_hist)[DX_MAX_E],
+                                            int* s_base, int* s_total, Pairs& q) {
+  const int E = p.E;
 #pragma unroll 1
   for (int at = 0; at < n; at += kTile) {
     if (at > 0) {
-      load_pairs(ids, p0, at, n, q);
+      load_pairs(p.topk_ids, p0, at, n, q);
       __syncthreads();                               // (the tile in front has been placed)
       for (int e = threadIdx.x; e < E; e += kThreads) s_base[e] += s_total[e];
-      count_pairs(q, E, s_hist);
+      count_pairs(q, E, s_hist, p.dev_status);
       __syncthreads();
       front_of_warps(E, s_hist, s_total);
       __syncthreads();
     }
-    scatter_pairs(q, p0 + at, s_base, s_hist, perm);
+    scatter_pairs(q, p0 + at, s_base, s_hist, p);
   }
 }
 
@@ -637,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
 #pragma unroll
     for (int h = 0; h < kPicks; ++h) {
       id[h] = 255 - (int)(pick[h] & 255u);
-      x[h] = h * G + sub <= k && pick[h] != 0 ? to_f(row[id[h]]) : -INFINITY;
+      x[h] = h * G + sub <= k && pick[h] != 0 && DX_BOUNDS(id[h] >= 0 && id[h] < E, p.dev_status) ? to_f(row[id[h]]) : -INFINITY;
       below[h] = __shfl_sync(0xffffffffu, pick[h], tok * G + (sub + 1) % G);
       if (h + 1 < kPicks) {                          // (the last lane's neighbour is the first lane's next pick)
         const unsigned int w = __shfl_sync(0xffffffffu, pick[h + 1 < kPicks ? h + 1 : h], tok * G);
@@ -683,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
 #pragma unroll
         for (int h = 0; h < kPicks; ++h) {
           const int y = __shfl_sync(0xffffffffu, got, (sub + h * G) % 32);
-          if (tok == q && h * G + sub < k) {
+          if (tok == q && h * G + sub < k && DX_BOUNDS(y >= 0 && y < E, p.dev_status)) {
             id[h] = y;
             x[h] = to_f(row[y]);
           }
@@ -725,7 +729,7 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
 #pragma unroll
     for (int h = 0; h < kH; ++h) {
       const int j = h * G + sub;
-      if (active && j < k) {
+      if (active && j < k && DX_BOUNDS(id[h] >= 0 && id[h] < E, p.dev_status)) {
         p.topk_ids[t * k + j] = id[h];
         p.topk_w[t * k + j] = w[h] * f;
         atomicAdd(&s_count[id[h]], 1);
@@ -749,11 +753,11 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
   __syncthreads();
   Pairs q;
   load_pairs(p.topk_ids, 0, 0, p.N * k, q);
-  count_pairs(q, E, s_mem.hist);
+  count_pairs(q, E, s_mem.hist, p.dev_status);
   __syncthreads();
   front_of_warps(E, s_mem.hist, s_count);
   __syncthreads();
-  place_pairs(p.topk_ids, 0, p.N * k, E, s_mem.hist, s_base, s_count, p.perm, q);
+  place_pairs(p, 0, p.N * k, s_mem.hist, s_base, s_count, q);
 }
 
 // Clusters of kPermCluster CTAs share the sums over the histograms: CTA r of a cluster adds up every kPermCluster-th part
@@ -795,7 +799,7 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
     for (int i = 0; i < 4; ++i, at += (size_t)E << segs_log)
       if (first + seg + (i << segs_log) < min((int)blockIdx.x, n_ctas)) near += *at;
   }
-  count_pairs(q, E, s_hist);
+  count_pairs(q, E, s_hist, p.dev_status);
   if (e < E) {
     atomicAdd(&s_part[e].x, total);
     atomicAdd(&s_part[e].y, front);
@@ -830,7 +834,7 @@ __global__ void __launch_bounds__(kThreads) dx_batch_permute_kernel(BatchRoutePa
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[E] = p.N * p.k;
   __syncthreads();
-  place_pairs(p.topk_ids, t_lo * p.k, n, E, s_hist, s_base, s_total, p.perm, q);
+  place_pairs(p, t_lo * p.k, n, s_hist, s_base, s_total, q);
   __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -1026,6 +1030,7 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
   p.vec = rows_aligned(logits, ld, elem) ? 1 : 0;
   p.topk_ids = topk_ids; p.topk_w = topk_w; p.offsets = offsets; p.perm = perm;
   p.counts = ctx->route_counts;
+  p.dev_status = ctx->dev_status;
   // One CTA up to two turns of its warps (128 tokens of 64 experts: 8.1 us against 7.1 us for two launches, the second of
   // which costs the host 3 us; four turns: 10.9 against 7.1 us), else at most two per SM, each with whole turns.
   const int lanes = p.E <= 4 * kEpl && p.groups <= 4 ? 4 : p.E <= 8 * kEpl && p.groups <= 8 ? 8

@@ -48,6 +48,11 @@ struct DistillParams {
   void* dlogits;
   int32_t* dev_status;
 };
+// vectors of a row that each of its C CTAs has room for
+template <typename T>
+__host__ __device__ __forceinline__ long long slice_vectors(int V, int C) {
+  return ((long long)V * (long long)sizeof(T) / 16 + C - 1) / C;
+}
 
 // log2(e) / T in two parts, the first rounded down: rounded to one, it would shift the exponents of all words the same way,
 // and a gradient that is a small difference of q and p would show it.
@@ -299,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
             const int mine = vec - sp.v_lo;
             if (mine >= 0 && mine < n_vec) {
               const int q = mine / kRowThreads, at = (mine % kRowThreads) * half + (q >> 4);
-              atomicOr(&marks[at >> 1], 1u << ((at & 1) * 16 + (q & 15)));
+              if (DX_BOUNDS(q < 16 * half, p.dev_status)) atomicOr(&marks[at >> 1], 1u << ((at & 1) * 16 + (q & 15)));
             }
           }
           if (old & bit) x = -1;
@@ -395,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         if (!last_out) return;
 #pragma unroll
         for (int i = 0; i < kLists; ++i)
-          if (at[i] >= 0) last_out[at[i]] = V16::round(g[i]);
+          if (at[i] >= 0 && DX_BOUNDS(at[i] < p.V, p.dev_status)) last_out[at[i]] = V16::round(g[i]);
         last_out = nullptr;
       }
     };
@@ -403,6 +408,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     auto finish = [&]() {                          // the losses of the rows in the ring
       if (lane >= in_ring) return;
       const LossTerms x = s_ring[lane];
+      if (!DX_BOUNDS(x.t >= 0 && x.t < p.N, p.dev_status)) return;
       const float M = fmaxf(x.rest_m, x.z_ref);
       const double rest = p.tail && x.mass < 1.0 ? 1.0 - x.mass : 0.0;
       const double du_rest = ((double)x.rest_m - (double)M) * p.inv_T;
@@ -523,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     for (int q = 0; q < deep; ++q) {
       if (q == late) asm volatile("cp.async.commit_group;" ::: "memory");
       const int i = tid + q * kRowThreads;
-      if (i < n_vec) copy16(s_mine + q * kRowThreads * 16, src + i);
+      if (i < n_vec && DX_BOUNDS(i < slice_vectors<T>(p.V, C), p.dev_status)) copy16(s_mine + q * kRowThreads * 16, src + i);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
@@ -545,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     const uint4* fetch = reinterpret_cast<const uint4*>(next + np.head) + np.v_lo + tid;
     cta_barrier();
     const float2 wn = s_weight[b];                 // (a row there is nothing to learn from stays where it is)
-    const int next_vecs = t < p.N && wn.y != 0.f ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
+    const int next_vecs = t < p.N && wn.y != 0.f && DX_BOUNDS(np.v_hi - np.v_lo <= slice_vectors<T>(p.V, C), p.dev_status) ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
     const int plain = min(n_vec, next_vecs ? next_vecs : n_vec);
     const float w = wn.x;
     float coef = 0.f, ref = 0.f;                   // gradient of an unlisted word: coef * e^{(z - ref) / T}
@@ -573,6 +579,7 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
             int h = vec & (kHash - 1);
             for (int tries = 0; tries < kHash && s_hash[b][h] >> 8 != (unsigned int)vec + 1u; ++tries)
               h = (h + 1) & (kHash - 1);
+            if (!DX_BOUNDS(tid + q * kRowThreads < n_vec && s_hash[b][h] >> 8 == (unsigned int)vec + 1u, p.dev_status)) continue;
             uint4 v = load_shared(s_mine + q * kRowThreads * 16);
             mask_vector<T>(v, s_hash[b][h]);
             store_shared(s_mine + q * kRowThreads * 16, v);
@@ -817,7 +824,7 @@ cudaError_t launch(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
          (bytes > (long long)C * DX_ROW_SLICE_BYTES ||
           ((long long)p.N * C * 2 <= slots && (long long)C * 2 * kRowThreads * 16 <= bytes)))
     C *= 2;
-  const long long slice = (bytes / 16 + C - 1) / C;      // vectors of a CTA, at most
+  const long long slice = slice_vectors<T>(p.V, C);
   DistillParams q = p;
   q.half = (int)((slice + kRowThreads * 16 - 1) / (kRowThreads * 16));
   if (q.half < 1) q.half = 1;

@@ -96,6 +96,7 @@ struct Picker {
   int V, rank, C, n, seg_vecs;          // vectors of one thread in one segment
   unsigned long long* cand;             // [kCandCap + DX_MAX_TOP]
   int* n_cand;
+  int32_t* dev_status;
 
   // (`least`: the smallest value wanted; a NaN is taken where -inf is)
   __device__ __forceinline__ void offer(float z, int idx, float least) const {
@@ -118,7 +119,7 @@ struct Picker {
         const int y = x + h * kRowThreads;
         int r = (int)(((float)y + 0.5f) * inv);           // y / seg_vecs, one off at most where y passes 24 bits
         r += (y >= (r + 1) * seg_vecs) - (y < r * seg_vecs);
-        const int run = y < items ? runs[r] : 0;
+        const int run = y < items && DX_BOUNDS(r >= 0 && r < n_runs, dev_status) ? runs[r] : 0;
         v[h] = sp.v_lo + run % kRowThreads + (run / kRowThreads * seg_vecs + y - r * seg_vecs) * kRowThreads;
         if (y >= items || v[h] >= sp.v_hi) v[h] = -1;
         if (v[h] >= 0) w[h] = row_vec(row, sp, v[h]);
@@ -184,7 +185,7 @@ struct Picker {
         at += w < warp ? s_scan[w] : 0;
         total += s_scan[w];
       }
-      for (; mask && at < n; mask &= mask - 1, ++at)
+      for (; mask && at < n && DX_BOUNDS(at >= 0 && out + at < cand + kCandCap + DX_MAX_TOP, dev_status); mask &= mask - 1, ++at)
         out[at] = ((unsigned long long)hi << 32) | (unsigned long long)(~(unsigned int)(first + __ffs(mask) - 1));
       found += total;
       __syncthreads();
@@ -286,13 +287,13 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     }
     seg = fmaxf(seg, top);
     if (++in_seg == seg_chunks) {
-      s_seg[g++][tid] = seg;
+      if (DX_BOUNDS(g < kSegments, p.dev_status)) s_seg[g++][tid] = seg;
       best = fmaxf(best, seg);
       seg = -INFINITY;
       in_seg = 0;
     }
   }
-  if (in_seg > 0) {
+  if (in_seg > 0 && DX_BOUNDS(g < kSegments, p.dev_status)) {
     s_seg[g][tid] = seg;
     best = fmaxf(best, seg);
   }
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     __syncthreads();
     const unsigned int tau = s_tau;
     const bool ties = s_ties != 0;
-    Picker<T> pick{row, sp, p.V, rank, C, n, seg_chunks * kUnroll, s_cand, &s_ncand};
+    Picker<T> pick{row, sp, p.V, rank, C, n, seg_chunks * kUnroll, s_cand, &s_ncand, p.dev_status};
     // (a threshold that everything reaches takes NaN in as well)
     const unsigned int low = ties ? tau + 1u : tau <= 0x007fffffu ? 1u : tau;
     if (ties ? mine > tau : mine >= tau) {
@@ -486,7 +487,10 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
     const unsigned long long floor = s_floor;
     for (int q = tid; q < C * n; q += kRowThreads) {
       const unsigned long long k = s_in[q];
-      if (k != 0 && k >= floor) s_cand[atomicAdd(&s_ncand, 1)] = k;
+      if (k != 0 && k >= floor) {
+        const int at = atomicAdd(&s_ncand, 1);
+        if (DX_BOUNDS(at < kCandCap + DX_MAX_TOP, p.dev_status)) s_cand[at] = k;
+      }
     }
     __syncthreads();
     const int ncand = s_ncand;
@@ -520,6 +524,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) dx_logprobs_kernel(LogprobPara
   }
   if (tid < n) {
     const unsigned long long k = top[tid];
+    (void)DX_BOUNDS(~(unsigned int)k < (unsigned int)p.V, p.dev_status);
     p.top_ids[(size_t)t * n + tid] = (int32_t)(~(unsigned int)k);
     p.top_logprobs[(size_t)t * n + tid] = none ? -INFINITY : (key_value(k) - x.m) / p.T - log_s;
   }
