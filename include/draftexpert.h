@@ -392,8 +392,9 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
 /* ---- whole batches of tokens: scoring, distillation, routing --------------------------------------------------------
  * What a drafter is scored, trained and routed with outside the decode step: any number of rows N >= 0 (N = 0 does
  * nothing), one launch per call (moe_route_tokens: two for large batches), no device memory besides the context's
- * scratch, the same results on every run, safe to capture into CUDA graphs.  The context's GPU need not be the
- * current device.  Logits and their gradients are fp32 or bf16 (dtype: DX_DTYPE_FP32 / DX_DTYPE_BF16), rows `ld`
+ * scratch, the same results on every run, safe to capture into CUDA graphs (graphs of one context are ordered like its
+ * calls: replayed at once, moe_route_tokens leaves its permutation undefined; the others use no scratch).  The context's GPU
+ * need not be the current device.  Logits and their gradients are fp32 or bf16 (dtype: DX_DTYPE_FP32 / DX_DTYPE_BF16), rows `ld`
  * elements apart (ld >= the row's length, any value; columns behind the row are neither read nor written), their
  * address a multiple of the element size; 16-byte aligned rows are fastest.  Everything else is fp32 / int32, dense.
  * Arithmetic is fp32 (per-row scalars of the loss: fp64); a bf16 gradient is rounded once.

@@ -334,6 +334,8 @@ __device__ __forceinline__ void front_of_warps(int E, int (*s_hist)[DX_MAX_E], i
     s_total[e] = x;
   }
 }
+// (a place past the permutation can only come of counts that another call has overwritten -- the context's scratch shared by
+// streams that are not ordered: it is not written)
 __device__ __forceinline__ void scatter_pairs(const Pairs& q, long long first_pair, const int* s_base,
                                               int (*s_hist)[DX_MAX_E], const BatchRouteParams& p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -344,7 +346,8 @@ __device__ __forceinline__ void scatter_pairs(const Pairs& q, long long first_pa
     __syncwarp();
     if (q.id[d] >= 0) {
       const int at = s_base[q.id[d]] + x + __popc(q.same[d] & ((1u << lane) - 1u));
-      if (DX_BOUNDS(at >= 0 && at < p.N * p.k, p.dev_status)) p.perm[at] = (int32_t)(first + 32 * d);
+      if ((unsigned int)at < (unsigned int)(p.N * p.k)) p.perm[at] = (int32_t)(first + 32 * d);
+      else (void)DX_BOUNDS(false, p.dev_status);
       if (__ffs(q.same[d]) - 1 == lane) s_hist[warp][q.id[d]] = x + __popc(q.same[d]);
     }
     __syncwarp();

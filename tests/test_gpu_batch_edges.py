@@ -142,3 +142,38 @@ def test_distill_rows_without_weight_or_list_are_not_fetched(dx, grad):
     whole = time(one, ids)
     assert time(0 * one, ids) <= 0.65 * whole and time(one, none) <= 0.65 * whole
     assert time(half.float(), ids) <= 0.8 * whole and time(one, torch.where(half[:, None], ids, none)) <= 0.8 * whole
+
+
+def test_route_calls_that_share_a_context_unordered_stay_inside_their_outputs(dx):
+    """Two captured graphs of one context share its scratch.  Replayed one after the other they give their own results;
+    replayed at once, which the header rules out, the permutations are undefined but nothing beside them is written."""
+    binding, ctx = dx
+    N, E, k, pad = 40000, 64, 6, 1 << 20
+    graphs, outs, buffers, wants = [], [], [], []
+    for i in range(2):
+        z = torch.randn((N, E), generator=torch.Generator(device="cuda").manual_seed(i), device="cuda")
+        z[:, (0 if i else E // 2):(E // 2 if i else E)] += 4.0          # (the two select other experts)
+        want = binding.moe_route_tokens(ctx, z, k, score_fn=1)
+        buf = torch.full((N * k + 2 * pad,), -7, dtype=torch.int32, device="cuda")
+        out = {name: torch.empty_like(want[name]) for name in ("topk_ids", "topk_w", "offsets")}
+        out["perm"] = buf[pad:pad + N * k]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            binding.moe_route_tokens(ctx, z, k, score_fn=1, out=out)
+        graphs.append(graph), outs.append(out), buffers.append((buf, z)), wants.append(want)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(200):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for (buf, _), out, want in zip(buffers, outs, wants):
+        assert (buf[:pad] == -7).all() and (buf[pad + N * k:] == -7).all()
+        assert torch.equal(out["topk_ids"], want["topk_ids"]) and torch.equal(out["topk_w"], want["topk_w"])
+    ctx.device_status()
+    for graph in graphs:
+        graph.replay()
+    torch.cuda.synchronize()
+    for out, want in zip(outs, wants):
+        assert all(torch.equal(out[name], want[name]) for name in want)
