@@ -853,7 +853,11 @@ cudaError_t launch_lists(dx_ctx* ctx, const DistillParams& p, cudaStream_t st) {
 
 template <typename K>
 cudaError_t prepare(K kernel, int smem) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  // (what the row's slices are sized by must hold for the kernel as it was compiled)
+  cudaFuncAttributes a;
+  cudaError_t e = cudaFuncGetAttributes(&a, kernel);
+  if (e == cudaSuccess && a.sharedSizeBytes > (size_t)kStaticBytes) e = cudaErrorInvalidConfiguration;
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   return e;
 }
