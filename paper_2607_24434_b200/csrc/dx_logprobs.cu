@@ -1,6 +1,9 @@
 // Log probabilities of given tokens, entropy and the most likely alternatives of rows of logits:
-//   u_v = (z_v - max z) / T,  S = sum_v e^{u_v},  log p_v = u_v - log S,  H = log S - (sum_v u_v e^{u_v}) / S.
-// (Both terms of H are non-negative, nothing cancels.)  The n alternatives are the largest z, ties to the lower id.
+//   u_v = (z_v - m) / T,  S = sum_v e^{u_v},  log p_v = u_v - log S,  H = log S - (sum_v u_v e^{u_v}) / S.
+// The reference m is one of the row's logits, the largest or one at least 2^-8 (kSlack) times as likely: where it is not the
+// largest, log S and log p_v + log S reach up to log 2^8 = 5.5 and cancel, so H and log p_v are good to a few steps of 5.5 in 32
+// bits (2e-6) besides the error of the sums; log p_v <= 0 and H >= 0 hold all the same, the reference's own mass being at
+// least 2^-8 of the largest's.  The n alternatives are the largest z, ties to the lower id.
 //
 // One pass: every logit is read from HBM once.  Threads carry (a reference near the maximum, S, sum u e^u)
 // relative to it, three 16-byte vectors at a time.  Alternatives ride along as each thread's largest logit, one per segment of its

@@ -177,3 +177,55 @@ def test_route_calls_that_share_a_context_unordered_stay_inside_their_outputs(dx
     torch.cuda.synchronize()
     for out, want in zip(outs, wants):
         assert all(torch.equal(out[name], want[name]) for name in want)
+
+
+@pytest.mark.parametrize("up", [False, True])
+def test_logprobs_are_corrected_for_the_rounding_of_their_factor(dx, up):
+    """log2(e) / T is rounded to fp32, by up to 2^-24 of it, which would shift the log probabilities of a row by that times its
+    mean |u|: at the temperature with the largest rounding, and rows whose mass lies seven below their largest logit, by 3e-7
+    and more, in one direction.  What is left has either sign from row to row -- the mean over 2000 rows loses it -- but for
+    the mean error of ex2, at most 2^-24: together less than 2^-23."""
+    binding, ctx = dx
+    grid = np.arange(1.2, 1.44, 1e-4).astype(np.float32)
+    c = 1.4426950408889634 / grid.astype(np.float64)
+    rounding = (c - c.astype(np.float32).astype(np.float64)) / c
+    i = int(rounding.argmin() if up else rounding.argmax())
+    T, rounding = float(grid[i]), float(rounding[i])
+    assert abs(rounding) > 2.0 ** -24.5
+    N, V = 2000, 20000
+    z = torch.randn((N, V), generator=torch.Generator(device="cuda").manual_seed(60), device="cuda")
+    z[:, 100] = 12.0
+    tokens = torch.arange(N, dtype=torch.int32, device="cuda") % 100
+    got = binding.spec_token_logprobs(ctx, z, tokens, temperature=T)
+    logq = torch.log_softmax(z.double() / T, 1)
+    want = logq.gather(1, tokens.long()[:, None])[:, 0]
+    q = logq.exp()
+    u = (z.double() - 12.0) / T
+    mean_u = (q * u).sum(1)
+    shift = float(mean_u.mean()) * rounding                                      # ... of an uncorrected log probability
+    assert abs(shift) > 2.0 ** -22
+    assert abs(float((got["logprob"].double() - want).mean())) <= 2.0 ** -23
+    entropy = -(q * logq).sum(1)
+    # The correction makes log S that of T and leaves the mean u with the weights of the rounded factor: together the entropy
+    # at log2(e) / c instead of T, which the derivative, the variance of u, tells from the one at T.  (log S as above; the
+    # quotient of two sums with the same errors up to 7 times 2^-24 off on average.)
+    variance = float((q * u * u).sum(1).mean() - (mean_u ** 2).mean())
+    assert abs(float((got["entropy"].double() - entropy).mean())) <= 2.0 ** -23 + 7 * 2.0 ** -24 + abs(rounding) * variance
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_logprobs_are_probabilities_where_one_word_has_nearly_all(dx, dtype):
+    """log p <= 0 and entropy >= 0, wherever in the row the likely word lies and however far it stands above the rest."""
+    binding, ctx = dx
+    N, V = 300, 30011
+    z = torch.randn((N, V), generator=torch.Generator(device="cuda").manual_seed(61), device="cuda")
+    at = torch.randint(0, V, (N,), generator=torch.Generator(device="cuda").manual_seed(62), device="cuda")
+    z[torch.arange(N), at] = torch.linspace(4.0, 60.0, N, device="cuda")
+    z = z.to(dtype)
+    for T in (1.0, 0.3, 1.3):
+        got = binding.spec_token_logprobs(ctx, z, at.to(torch.int32), top_n=4, temperature=T)
+        assert (got["logprob"] <= 0).all() and (got["top_logprobs"] <= 0).all() and (got["entropy"] >= 0).all()
+        logq = torch.log_softmax(z.double() / float(np.float32(T)), 1)
+        want = logq.gather(1, at[:, None])[:, 0]
+        # (5.5 in 32 bits, a few steps; the sums' own error, an exponential's 2^-22 and its argument's rounding, relative to S)
+        assert float((got["logprob"].double() - want).abs().max()) <= 5.5 * 2.0 ** -22 + 2.0 ** -20 + 2.0 ** -22 * float(want.abs().max())
