@@ -229,3 +229,53 @@ def test_logprobs_are_probabilities_where_one_word_has_nearly_all(dx, dtype):
         want = logq.gather(1, at[:, None])[:, 0]
         # (5.5 in 32 bits, a few steps; the sums' own error, an exponential's 2^-22 and its argument's rounding, relative to S)
         assert float((got["logprob"].double() - want).abs().max()) <= 5.5 * 2.0 ** -22 + 2.0 ** -20 + 2.0 ** -22 * float(want.abs().max())
+
+
+@pytest.mark.parametrize("N,V,T", [(2000, 20000, 1.0), (300, 102400, 2.0), (1500, 3001, 0.7)])
+def test_rounding_errors_of_log_probabilities_and_losses(dx, N, V, T):
+    """Root mean squares over the rows.  A log probability is (z - m) / T - log S: the difference and its quotient, the logarithm
+    and the result are each rounded to fp32, by 2^-24 of a magnitude below M, uniformly (rms: 3^-1/2 of that), and S, a sum
+    over many words, is good to 2^-23: twice M 2^-24 + 2^-23.  A loss is put together in 64 bits from that S, whatever its
+    size, and rounded once."""
+    binding, ctx = dx
+    T = float(np.float32(T))
+    g = torch.Generator(device="cuda").manual_seed(N)
+    z = torch.randn((N, V), generator=g, device="cuda") * 2
+    tokens = torch.randint(0, V, (N,), generator=g, device="cuda").to(torch.int32)
+    got = binding.spec_token_logprobs(ctx, z, tokens, top_n=16, temperature=T)
+    logq = torch.log_softmax(z.double() / T, 1)
+    rms = lambda x: float(x.double().pow(2).mean().sqrt())  # noqa: E731
+    for have, at in ((got["logprob"][:, None], tokens[:, None]), (got["top_logprobs"], got["top_ids"])):
+        want = logq.gather(1, at.long())
+        assert rms(have.double() - want) <= 2 * (float(want.abs().max()) * 2.0 ** -24 + 2.0 ** -23)
+    lists = torch.log_softmax(z + torch.randn((N, V), generator=g, device="cuda"), 1).topk(16, dim=1)
+    ids, lp = lists.indices.to(torch.int32), lists.values
+    p = lp.double().exp()
+    listed = logq.gather(1, ids.long())
+    rest = 1 - p.sum(1)
+    log_r = torch.log1p(-listed.exp().sum(1))
+    tail = (p * (lp.double() - listed)).sum(1) + rest * (rest.log() - log_r)
+    p = p / p.sum(1, keepdim=True)
+    plain = (p * (p.log() - listed)).sum(1)
+    for want, with_tail in ((tail, True), (plain, False)):
+        have = binding.spec_distill_topk(ctx, z, ids, lp, tail=with_tail, temperature=T, grad=False)["loss"]
+        assert rms(have.double() - want) <= 2.0 ** -23 + float(want.abs().max()) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_route_scores_that_64_bits_cannot_tell_apart_are_ties(dx, dtype):
+    """Selection values are compared as they are in 64 bits: sigmoids of logits beyond 37 are all 1, scores far below their
+    biases' last place add nothing to them.  Without a bias the logits themselves are compared."""
+    binding, ctx = dx
+    z = torch.full((4, 16), -2.0, device="cuda")
+    z[0, 3:9] = torch.arange(40.0, 46.0, device="cuda")
+    z[1, 3:9] = torch.arange(-60.0, -54.0, device="cuda")
+    z[1, 9:], z[1, :3] = -80.0, -80.0
+    z[2, 3:9] = torch.arange(1.0, 7.0, device="cuda")
+    z = z.to(dtype)
+    bias = torch.zeros(16, device="cuda")
+    bias[3:9] = 0.25
+    ids = binding.moe_route_tokens(ctx, z, 4, score_fn=1, select_bias=bias)["topk_ids"].tolist()
+    assert ids[0] == [3, 4, 5, 6] and ids[1] == [3, 4, 5, 6] and ids[2] == [8, 7, 6, 5] and ids[3] == [3, 4, 5, 6]
+    ids = binding.moe_route_tokens(ctx, z, 4, score_fn=1)["topk_ids"].tolist()
+    assert ids[0] == ids[1] == ids[2] == [8, 7, 6, 5] and ids[3] == [0, 1, 2, 3]
