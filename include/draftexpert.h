@@ -124,8 +124,8 @@ dx_status dx_last_device_status(dx_ctx* ctx, void* stream, int32_t* dev_status_o
  * plain bf16. */
 dx_status dx_set_activation_split(dx_ctx* ctx, int32_t on);
 /* Which kernels are launched so that they may begin while the kernel in front of them on the stream drains
- * (programmatic stream serialization): bit 0 the routing kernel, bit 1 the expert kernels, bit 2 the greedy-accept
- * kernels.  Default 3.  0 gives plain stream order everywhere; results never depend on the mask. */
+ * (programmatic stream serialization): bit 0 the routing kernel and the second kernel of moe_route_tokens, bit 1 the expert
+ * kernels, bit 2 the greedy-accept kernels.  Default 3.  0 gives plain stream order everywhere; results never depend on the mask. */
 dx_status dx_set_launch_overlap(dx_ctx* ctx, int32_t mask);
 /* Every wait inside a kernel (for a word another kernel publishes, for a copy into shared memory, for the other CTAs
  * of a cooperative launch) polls at most `polls` times, then records DX_DEV_WAIT_EXPIRED in the device status word and
@@ -422,8 +422,9 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *   row_weight NULL: all 1.  loss or dlogits may be NULL.
  *   dlogits may be the logits buffer itself (same pitch), or lie between its rows; its rows must not overlap the logits'
  *   otherwise (DX_ERR_INVALID_ARG).
- *   A listed word that the student gives no mass makes the loss +inf (its gradient stays finite); a row of nothing but
- *   -inf has loss +inf and gradient 0.  A row must fit the shared memory of 16 SMs (about 1.8 million bf16 logits;
+ *   A listed word that the student gives no mass makes the loss +inf, and so does a rest r > 0 -- if only by the rounding of
+ *   teacher_logprobs -- where no unlisted word has any (a list of the whole vocabulary, or of all words that are not
+ *   masked: take tail = 0 there); the gradient stays finite.  A row of nothing but -inf has loss +inf and gradient 0.  A row must fit the shared memory of 16 SMs (about 1.8 million bf16 logits;
  *   DX_ERR_UNSUPPORTED beyond).
  *
  * moe_route_tokens: the router of Eq. 4 from its logits [N, E], for a batch, with the forms larger MoE models use:
@@ -431,7 +432,9 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *     -- takes part in the selection only; NULL: by the logits, whose order is that of the scores);  n_groups groups of
  *     E / n_groups consecutive experts, ranked by their largest selection value (group_score DX_GROUP_MAX) or the sum
  *     of their two largest (DX_GROUP_TOP2; without a bias both rank the scores), of which the topk_groups best stay;
- *     the top_k best experts of those.  Ties go to the lower id; the selection is that of exact arithmetic.
+ *     the top_k best experts of those.  Ties go to the lower id.  The selection is that of 64-bit arithmetic: scores, their
+ *     sums with the biases and the groups' sums are compared as they are in 64 bits (sigmoids of logits beyond 37 are all 1
+ *     there: ties); without a bias experts are compared by the logits themselves, exactly.
  *     topk_ids [N, k], topk_w [N, k] = routed_scale * r_e, or routed_scale * r_e / sum of the selected (norm_topk).
  *     offsets [E+1] and perm [N*k] as in moe_verify_block (both or neither may be NULL).
  *   A logit of -inf is a masked expert: selected only where too few others are left, with gate weight 0 (so is a whole

@@ -7,20 +7,24 @@
 // between the statistics and the gradient, and each vector's place takes the next row's vector as soon as it has been
 // read for the last time.
 //
-// The unlisted words are summed apart from the listed ones, relative to their own maximum: R never comes out of a
-// difference of nearly equal sums, and neither R nor the factor r / R can under- or overflow however far the listed
-// words stand above the rest.  A bit per vector says which vectors hold listed words, a small hash table which of their
+// The unlisted words are summed apart from the listed ones, relative to a reference of their own: R never comes out of a
+// difference of nearly equal sums, and neither R nor the factor r / R can under- or overflow however far the listed words
+// stand above the rest.  A bit per vector says which vectors hold listed words, a small hash table which of their
 // elements; those become -inf in shared memory in front of the sweep.  A ninth warp does the arithmetic on the list while
-// the other eight go over the row: in 64 bits for the loss and the listed words' gradient (both are small differences),
-// in 32 bits and first of all for what the eight wait for.  The warps' sums go straight into the shared memory of all
-// CTAs of the row, so that one cluster barrier is all that stands between the sweep and the gradient; without a gradient
-// nobody waits at all, and a row's sums are collected while the next row is summed.
+// the other eight go over the row: in 64 bits for the loss, the listed words' gradient and, with a tail bucket, the
+// unlisted words' factor (all are small differences), in 32 bits and first of all for what the eight wait for otherwise.
+// It also says a row ahead whether there is anything to learn from the next row: rows without weight or list are not
+// fetched.  The warps' sums go straight into the shared memory of all CTAs of the row, so that one cluster barrier is all
+// that stands between the sweep and the gradient; without a gradient nobody waits at all, and a row's sums are collected
+// while the next row is summed.
 //
-// What bounds it: HBM for fp32 (1024 x 163840 with gradient 236 us, 83 % of the measured copy bandwidth; loss alone
-// 120 us, 87 %); for bf16 there are twice as many exponentials per byte and the two that a logit needs with a gradient keep
-// their pipe busy for 55 % of the time (2048 x 102400, list of 64: 164 us, 79 %; loss alone 97 us, 67 %).  Short rows pay
-// the fixed part of a row per warp -- about half as many instructions as a sweep of 25 vectors -- more often: 8192 x 32000
-// bf16 220 us, 74 %.
+// What bounds it: HBM for fp32 (1024 x 163840 with gradient 254 us, 82 % of the measured copy bandwidth, with a tail
+// bucket 259; loss alone 119 us, 88 %); for bf16 there are twice as many exponentials per byte and the two that a logit
+// needs with a gradient keep their pipe busy for 55 % of the time (2048 x 102400, list of 64: 164 us, 79 %, with a tail
+// bucket 166).  The loss alone needs one exponential per logit, but goes through shared memory, marks and barriers like
+// the gradient: 96 us, 68 %, where the log probabilities of the same rows, which stay in registers, take 75.  Short rows
+// pay the fixed part of a row per warp -- about half as many instructions as a sweep of 25 vectors -- more often: 8192 x
+// 32000 bf16 217 us, 75 %, loss alone 111.
 #include <cmath>
 
 #include "dx_rows.cuh"
@@ -184,8 +188,8 @@ __device__ __forceinline__ float tail_factor(const Row64& r, double mass, double
   return __fdividef(__fdividef((float)((r.R * mass - rest * P) * scale), (float)(S * scale)), (float)r.R);
 }
 
-// kLists: list entries per lane of the list's warp, at least k / 32 (with four for all the batch above took 201 us, the
-// list's registers being spilled)
+// kLists: list entries per lane of the list's warp, at least k / 32: two up to 64 words, four up to 128 (four for all: 170 us
+// instead of 164.6 for the batch above, 62 instead of 46 us for 4096 x 1001; lists of 128 words 184 us)
 template <typename T, bool kGrad, int kLists>
 __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(DistillParams p, int C, int buffers) {
   using V16 = RowVec<T>;

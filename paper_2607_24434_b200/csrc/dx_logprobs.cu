@@ -16,7 +16,8 @@
 // same result on every run.
 //
 // What bounds it: without alternatives HBM and the exponentials (2048 x 102400 bf16: 75 us, 87 % of the measured copy
-// bandwidth); with 20 alternatives 86 us, 76 %: the second look and its barriers stop a CTA's loads for a quarter of its
+// bandwidth); with 20 alternatives 93 us, 70 % (86 us in a loop over one batch, part of which is still in L2; so are the other
+// figures of variants here): the second look and its barriers stop a CTA's loads for a quarter of its
 // row, and the other three CTAs of the SM do not cover all of it (a ninth warp that did the selection alone: 106 us).
 // Few rows are a chain of latencies: 1 x 102400 9 us, 16 x 163840 fp32 12 us.
 #include "dx_rows.cuh"
