@@ -943,7 +943,7 @@ __global__ void __launch_bounds__(kGradThreads) dx_route_grad_sparse_kernel(Rout
     float g = q.g;
     if (p.norm) {
       const float S = lanes_sum<G>(r);
-      const float mean = lanes_sum<G>(g * r) / S;
+      const float mean = lanes_sum<G>(g * (r / S));    // (shares first: an only expert's is 1 and its gradient zero)
       g = S == 0.f || q.id < 0 ? 0.f : (g - mean) / S;
     }
     const float both = sum_duplicates<G>(q.id, g, tok, p.k);

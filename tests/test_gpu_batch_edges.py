@@ -279,3 +279,15 @@ def test_route_scores_that_64_bits_cannot_tell_apart_are_ties(dx, dtype):
     assert ids[0] == [3, 4, 5, 6] and ids[1] == [3, 4, 5, 6] and ids[2] == [8, 7, 6, 5] and ids[3] == [3, 4, 5, 6]
     ids = binding.moe_route_tokens(ctx, z, 4, score_fn=1)["topk_ids"].tolist()
     assert ids[0] == ids[1] == ids[2] == [8, 7, 6, 5] and ids[3] == [0, 1, 2, 3]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_route_grad_of_one_renormalised_gate_is_zero(dx, dtype, sigmoid):
+    """The gate of the only selected expert is routed_scale whatever its logit: no gradient, not even a rounding of one."""
+    binding, ctx = dx
+    z = (torch.randn((500, 24), generator=torch.Generator(device="cuda").manual_seed(70), device="cuda") * 3).to(dtype)
+    ids = binding.moe_route_tokens(ctx, z, 1, score_fn=int(sigmoid))["topk_ids"]
+    dw = torch.randn((500, 1), generator=torch.Generator(device="cuda").manual_seed(71), device="cuda")
+    got = binding.moe_route_tokens_backward(ctx, z, ids, dw, score_fn=int(sigmoid), norm_topk=1, routed_scale=2.446)
+    assert not got.any()
