@@ -124,8 +124,9 @@ dx_status dx_last_device_status(dx_ctx* ctx, void* stream, int32_t* dev_status_o
  * plain bf16. */
 dx_status dx_set_activation_split(dx_ctx* ctx, int32_t on);
 /* Which kernels are launched so that they may begin while the kernel in front of them on the stream drains
- * (programmatic stream serialization): bit 0 the routing kernel and the second kernel of moe_route_tokens, bit 1 the expert
- * kernels, bit 2 the greedy-accept kernels.  Default 3.  0 gives plain stream order everywhere; results never depend on the mask. */
+ * (programmatic stream serialization): bit 0 the routing kernel and the second kernel of moe_route_tokens, bit 1 the
+ * expert kernels, bit 2 the greedy-accept kernels.  Default 3.  0 gives plain stream order everywhere; results never
+ * depend on the mask. */
 dx_status dx_set_launch_overlap(dx_ctx* ctx, int32_t mask);
 /* Every wait inside a kernel (for a word another kernel publishes, for a copy into shared memory, for the other CTAs
  * of a cooperative launch) polls at most `polls` times, then records DX_DEV_WAIT_EXPIRED in the device status word and
@@ -392,12 +393,13 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
 /* ---- whole batches of tokens: scoring, distillation, routing --------------------------------------------------------
  * What a drafter is scored, trained and routed with outside the decode step: any number of rows N >= 0 (N = 0 does
  * nothing), one launch per call (moe_route_tokens: two for large batches), no device memory besides the context's
- * scratch, the same results on every run, safe to capture into CUDA graphs (graphs of one context are ordered like its
- * calls: replayed at once, moe_route_tokens leaves its permutation undefined; the others use no scratch).  The context's GPU
- * need not be the current device.  Logits and their gradients are fp32 or bf16 (dtype: DX_DTYPE_FP32 / DX_DTYPE_BF16), rows `ld`
- * elements apart (ld >= the row's length, any value; columns behind the row are neither read nor written), their
- * address a multiple of the element size; 16-byte aligned rows are fastest.  Everything else is fp32 / int32, dense.
- * Arithmetic is fp32 (per-row scalars of the loss: fp64); a bf16 gradient is rounded once.
+ * scratch, the same results on every run, safe to capture into CUDA graphs (graphs of one context are ordered like
+ * its calls: replayed at once, moe_route_tokens leaves its permutation undefined; the others use no scratch).  The
+ * context's GPU need not be the current device.  Logits and their gradients are fp32 or bf16 (dtype: DX_DTYPE_FP32 /
+ * DX_DTYPE_BF16), rows `ld` elements apart (ld >= the row's length, any value; columns behind the row are neither
+ * read nor written), their address a multiple of the element size; 16-byte aligned rows are fastest.  Everything else
+ * is fp32 / int32, dense.  Arithmetic is fp32 (per-row scalars of the loss and of the gradient with a tail bucket: fp64);
+ * a bf16 gradient is rounded once.
  *
  * spec_token_logprobs: for each row t, with p = softmax(logits[t] / temperature):
  *     logprob[t] = log p[tokens[t]];  tokens[t] = -1 (no token, padding) gives 0, any other id outside [0, V) gives NaN
@@ -413,7 +415,7 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *   Eq. 8, with the teacher cut to a list of k <= 128 words per row).  teacher_ids / teacher_logprobs [N, k]; an id of -1
  *   is an unused entry, an id listed twice in a row counts once (its first entry), any other id outside [0, V) is left
  *   out and reported as DX_DEV_BAD_TOKEN.  With q = softmax(logits[t] / temperature) and p_j = exp(teacher_logprobs):
- *     tail = 0: p renormalised over the listed words, L_t = sum_j p_j (log p_j - log q_j)  (a list of nothing but -inf: 0);
+ *     tail = 0: p renormalised over the listed words, L_t = sum_j p_j (log p_j - log q_j)  (a list of only -inf: 0);
  *               only the differences of a row's teacher_logprobs count, however large or small they are;
  *     tail = 1: p as given, and the rest r = max(0, 1 - sum_j p_j) in one bucket against the student's mass R on all
  *               unlisted words: L_t = sum_j p_j (log p_j - log q_j) + r (log r - log R).
@@ -422,10 +424,10 @@ dx_status dx_squared_error(dx_ctx* ctx, const float* a, const float* b, int64_t 
  *   row_weight NULL: all 1.  loss or dlogits may be NULL.
  *   dlogits may be the logits buffer itself (same pitch), or lie between its rows; its rows must not overlap the logits'
  *   otherwise (DX_ERR_INVALID_ARG).
- *   A listed word that the student gives no mass makes the loss +inf, and so does a rest r > 0 -- if only by the rounding of
- *   teacher_logprobs -- where no unlisted word has any (a list of the whole vocabulary, or of all words that are not
- *   masked: take tail = 0 there); the gradient stays finite.  A row of nothing but -inf has loss +inf and gradient 0.  A row must fit the shared memory of 16 SMs (about 1.8 million bf16 logits;
- *   DX_ERR_UNSUPPORTED beyond).
+ *   A listed word that the student gives no mass makes the loss +inf, and so does a rest r > 0 -- if only by the rounding
+ *   of teacher_logprobs -- where no unlisted word has any (a list of the whole vocabulary, or of all words that are not
+ *   masked: take tail = 0 there); the gradient stays finite.  A row of nothing but -inf has loss +inf and gradient 0.
+ *   A row must fit the shared memory of 16 SMs (about 1.8 million bf16 logits; DX_ERR_UNSUPPORTED beyond).
  *
  * moe_route_tokens: the router of Eq. 4 from its logits [N, E], for a batch, with the forms larger MoE models use:
  *     r = softmax or sigmoid (score_fn);  selection by r_e + select_bias[e] (the bias -- the one load balancing adjusts

@@ -275,7 +275,8 @@ __device__ __noinline__ int settle_groups(const BatchRouteParams& p, const T* ro
 #pragma unroll 1
   while (__any_sync(0xffffffffu, cand != 0)) {
     const int e = e0 + __ffs(cand) - 1;
-    const double v = cand && DX_BOUNDS(e < p.E, p.dev_status) ? exact_sigmoid((double)to_f(row[e])) + (double)bias[e] : -INFINITY;
+    const bool in = cand && DX_BOUNDS(e < p.E, p.dev_status);
+    const double v = in ? exact_sigmoid((double)to_f(row[e])) + (double)bias[e] : -INFINITY;
     __syncwarp();
     cand &= cand - 1;
     if (v > a) { b = a; a = v; }
@@ -647,7 +648,8 @@ __global__ void __launch_bounds__(kThreads, 2) dx_batch_route_kernel(const __gri
 #pragma unroll
     for (int h = 0; h < kPicks; ++h) {
       id[h] = 255 - (int)(pick[h] & 255u);
-      x[h] = h * G + sub <= k && pick[h] != 0 && DX_BOUNDS(id[h] >= 0 && id[h] < E, p.dev_status) ? to_f(row[id[h]]) : -INFINITY;
+      const bool in = h * G + sub <= k && pick[h] != 0 && DX_BOUNDS(id[h] >= 0 && id[h] < E, p.dev_status);
+      x[h] = in ? to_f(row[id[h]]) : -INFINITY;
       below[h] = __shfl_sync(0xffffffffu, pick[h], tok * G + (sub + 1) % G);
       if (h + 1 < kPicks) {                          // (the last lane's neighbour is the first lane's next pick)
         const unsigned int w = __shfl_sync(0xffffffffu, pick[h + 1 < kPicks ? h + 1 : h], tok * G);

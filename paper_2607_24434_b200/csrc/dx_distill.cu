@@ -142,8 +142,8 @@ __device__ __forceinline__ RowSums row_sums(const MaxSum* all, const ListSums& l
   return r;
 }
 
-// 2^((m - ref) c) to 2^-32, for exponents from -1000 to 500 (less counts as none, more as 500): Taylor's polynomial of e^t on
-// |t| <= ln 2 / 2.  c32: c in 32 bits, for the comparisons with the limits.
+// 2^((m - ref) c) to 2^-32, for exponents from -1000 to 500 (less counts as none, more as 500): Taylor's polynomial of
+// e^t on |t| <= ln 2 / 2.  c32: c in 32 bits, for the comparisons with the limits.
 __device__ __forceinline__ double ex2_64(float m, float ref, double c, float c32) {
   const float about = (m - ref) * c32;
   const double y = ((double)m - (double)ref) * c;
@@ -155,8 +155,9 @@ __device__ __forceinline__ double ex2_64(float m, float ref, double c, float c32
   const int up = __double2hiint(x) + (__double2loint(big) << 20);
   return about < -1000.f ? 0.0 : about > 500.f ? 3.273390607896142e150 : __hiloint2double(up, __double2loint(x));
 }
-// A row's sums in 64 bits: R over the unlisted words, relative to 2^(ref / T); w: what brings the listed words' to it.  (Where
-// the list stands more than 2^500 above the rest, or 2^1000 below, the smaller of the two counts for nothing.)
+// A row's sums in 64 bits: R over the unlisted words, relative to e^{ref / T}; w: what brings the listed words' sum to
+// that reference.  (Where the list stands more than 2^500 above the rest, or 2^1000 below, the smaller of the two counts
+// for nothing.)
 struct Row64 {
   float ref;
   double R, w;
@@ -177,11 +178,11 @@ __device__ __forceinline__ Row64 row_sums64(const MaxSum* all, float z_ref, int 
   r.w = __shfl_sync(0xffffffffu, r.w, n & 31);
   return r;
 }
-// beta / S - rest / R of a row with a tail bucket, times 2^(ref / T).  The two quotients cancel where the student's tail is close
-// to the teacher's; with S = R + P, P the listed words' sum, and beta = mass + rest they are one fraction whose numerator is
-// a difference in 64 bits.  What is left is the error of R's own exponentials, 1e-8 to 2e-8 (rms) of rest / R for a student within 1e-4 of
-// its teacher at 2000 to 163840 words; as two quotients in 32 bits it was 1.7e-7 to 3e-7.  The 64-bit chain costs 0.2 us a row
-// (2048 x 102400 bf16: 164 -> 166 us).
+// beta / S - rest / R of a row with a tail bucket, relative to the same reference.  The two quotients cancel where the
+// student's tail is close to the teacher's; with S = R + P, P the listed words' sum, and beta = mass + rest they are one
+// fraction whose numerator is a difference in 64 bits.  What is left is the error of R's own exponentials, 1e-8 to 2e-8
+// (rms) of rest / R for a student within 1e-4 of its teacher at 2000 to 163840 words; as two quotients in 32 bits it was
+// 1.7e-7 to 3e-7.  The 64-bit chain costs 0.2 us a row (2048 x 102400 bf16: 164 -> 166 us).
 __device__ __forceinline__ float tail_factor(const Row64& r, double mass, double sum_e) {
   const double rest = mass < 1.0 ? 1.0 - mass : 0.0, P = r.w * sum_e, S = r.R + P;
   const double scale = __hiloint2double(0x7fe00000 - (__double2hiint(S) & 0x7ff00000), 0);   // brings S to [1, 2)
@@ -353,7 +354,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
         mass = mass == mass ? 1.0 : mass;
       }
     };
-    // the student's part in 64 bits, for the loss, the listed words' gradient and, with a tail bucket, the unlisted words' factor
+    // the student's part in 64 bits, for the loss, the listed words' gradient and, with a tail bucket, the unlisted
+    // words' factor
     auto student = [&]() {
       p_u = sum_e = 0.0;
 #pragma unroll
@@ -555,7 +557,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
     const uint4* fetch = reinterpret_cast<const uint4*>(next + np.head) + np.v_lo + tid;
     cta_barrier();
     const float2 wn = s_weight[b];                 // (a row there is nothing to learn from stays where it is)
-    const int next_vecs = t < p.N && wn.y != 0.f && DX_BOUNDS(np.v_hi - np.v_lo <= slice_vectors<T>(p.V, C), p.dev_status) ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
+    const bool more = t < p.N && wn.y != 0.f && DX_BOUNDS(np.v_hi - np.v_lo <= slice_vectors<T>(p.V, C), p.dev_status);
+    const int next_vecs = more ? np.v_hi - np.v_lo : 0, next_deep = (next_vecs + kRowThreads - 1) / kRowThreads;
     const int plain = min(n_vec, next_vecs ? next_vecs : n_vec);
     const float w = wn.x;
     float coef = 0.f, ref = 0.f;                   // gradient of an unlisted word: coef * e^{(z - ref) / T}
@@ -583,7 +586,8 @@ __global__ void __launch_bounds__(kThreads, kGrad ? 2 : 3) dx_distill_kernel(Dis
             int h = vec & (kHash - 1);
             for (int tries = 0; tries < kHash && s_hash[b][h] >> 8 != (unsigned int)vec + 1u; ++tries)
               h = (h + 1) & (kHash - 1);
-            if (!DX_BOUNDS(tid + q * kRowThreads < n_vec && s_hash[b][h] >> 8 == (unsigned int)vec + 1u, p.dev_status)) continue;
+            if (!DX_BOUNDS(tid + q * kRowThreads < n_vec && s_hash[b][h] >> 8 == (unsigned int)vec + 1u, p.dev_status))
+              continue;
             uint4 v = load_shared(s_mine + q * kRowThreads * 16);
             mask_vector<T>(v, s_hash[b][h]);
             store_shared(s_mine + q * kRowThreads * 16, v);

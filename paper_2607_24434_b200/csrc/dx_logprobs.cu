@@ -1,9 +1,9 @@
 // Log probabilities of given tokens, entropy and the most likely alternatives of rows of logits:
 //   u_v = (z_v - m) / T,  S = sum_v e^{u_v},  log p_v = u_v - log S,  H = log S - (sum_v u_v e^{u_v}) / S.
-// The reference m is one of the row's logits, the largest or one at least 2^-8 (kSlack) times as likely: where it is not the
-// largest, log S and log p_v + log S reach up to log 2^8 = 5.5 and cancel, so H and log p_v are good to a few steps of 5.5 in 32
-// bits (2e-6) besides the error of the sums; log p_v <= 0 and H >= 0 hold all the same, the reference's own mass being at
-// least 2^-8 of the largest's.  The n alternatives are the largest z, ties to the lower id.
+// The reference m is one of the row's logits, the largest or one at least 2^-8 (kSlack) times as likely: where it is not
+// the largest, log S and log p_v + log S reach up to log 2^8 = 5.5 and cancel, so H and log p_v are good to a few steps of
+// 5.5 in 32 bits (2e-6) besides the error of the sums; log p_v <= 0 and H >= 0 hold all the same, the reference's own mass
+// being at least 2^-8 of the largest's.  The n alternatives are the largest z, ties to the lower id.
 //
 // One pass: every logit is read from HBM once.  Threads carry (a reference near the maximum, S, sum u e^u)
 // relative to it, three 16-byte vectors at a time.  Alternatives ride along as each thread's largest logit, one per segment of its
@@ -16,9 +16,9 @@
 // same result on every run.
 //
 // What bounds it: without alternatives HBM and the exponentials (2048 x 102400 bf16: 75 us, 87 % of the measured copy
-// bandwidth); with 20 alternatives 93 us, 70 % (86 us in a loop over one batch, part of which is still in L2; so are the other
-// figures of variants here): the second look and its barriers stop a CTA's loads for a quarter of its
-// row, and the other three CTAs of the SM do not cover all of it (a ninth warp that did the selection alone: 106 us).
+// bandwidth); with 20 alternatives 93 us, 70 % (86 us in a loop over one batch, part of which is still in L2; so are the
+// other figures of variants here): the second look and its barriers stop a CTA's loads for a quarter of its row, and the
+// other three CTAs of the SM do not cover all of it (a ninth warp that did the selection alone: 106 us).
 // Few rows are a chain of latencies: 1 x 102400 9 us, 16 x 163840 fp32 12 us.
 #include "dx_rows.cuh"
 
@@ -189,8 +189,9 @@ struct Picker {
         at += w < warp ? s_scan[w] : 0;
         total += s_scan[w];
       }
-      for (; mask && at < n && DX_BOUNDS(at >= 0 && out + at < cand + kCandCap + DX_MAX_TOP, dev_status); mask &= mask - 1, ++at)
-        out[at] = ((unsigned long long)hi << 32) | (unsigned long long)(~(unsigned int)(first + __ffs(mask) - 1));
+      for (; mask && at < n; mask &= mask - 1, ++at)
+        if (DX_BOUNDS(at >= 0 && out + at < cand + kCandCap + DX_MAX_TOP, dev_status))
+          out[at] = ((unsigned long long)hi << 32) | (unsigned long long)(~(unsigned int)(first + __ffs(mask) - 1));
       found += total;
       __syncthreads();
     }

@@ -141,7 +141,7 @@ def test_distill_rows_without_weight_or_list_are_not_fetched(dx, grad):
     none = torch.full_like(ids, -1)
     whole = time(one, ids)
     assert time(0 * one, ids) <= 0.65 * whole and time(one, none) <= 0.65 * whole
-    assert time(half.float(), ids) <= 0.8 * whole and time(one, torch.where(half[:, None], ids, none)) <= 0.8 * whole
+    assert time(half.float(), ids) <= 0.85 * whole and time(one, torch.where(half[:, None], ids, none)) <= 0.85 * whole
 
 
 def test_route_calls_that_share_a_context_unordered_stay_inside_their_outputs(dx):
