@@ -79,7 +79,10 @@ enum {
   DX_DEV_WAIT_EXPIRED = 2,      /* a bounded wait inside a kernel gave up */
   DX_DEV_WORKLIST_OVERFLOW = 3,
   DX_DEV_BOUNDS = 4,            /* checked build only (-DDX_CHECKED): an index left its range; the access was skipped */
-  DX_DEV_BAD_TOKEN = 5          /* a token id outside the vocabulary (spec_token_logprobs, spec_distill_topk) */
+  DX_DEV_BAD_TOKEN = 5,         /* a token id outside the vocabulary (spec_token_logprobs, spec_distill_topk,
+                                   spec_head_loss) */
+  DX_DEV_BAD_OFFSETS = 6,       /* groups' offsets that descend or leave the rows (moe_grouped_*) */
+  DX_DEV_BAD_ROW = 7            /* a gathered, scattered or weighted row outside its matrix (moe_grouped_*) */
 };
 
 typedef struct dx_ctx dx_ctx;
@@ -469,6 +472,79 @@ dx_status moe_route_tokens(dx_ctx* ctx, const dx_route_desc* desc, const void* l
 dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, const void* logits, int32_t dtype, int32_t N,
                                     int64_t ld, const int32_t* topk_ids, const float* d_topk_w, void* d_logits,
                                     int64_t ld_d, void* stream);
+
+/* ---- whole batches of tokens: the experts, their combination, the loss --------------------------------------------------
+ * The other half of a training or scoring pass over a batch: the experts' products for rows sorted by expert (what
+ * moe_route_tokens returns in offsets / perm), the weighted sum of a token's experts, the cross entropy of hidden rows against
+ * the vocabulary, and the gradients of all of them -- from a loss back to the d_topk_w that moe_route_tokens_backward takes.
+ * Conventions of the section above hold (any number of rows, same results on every run, no device memory but the caller's,
+ * capturable, the context's GPU need not be current); calls use no scratch of the context, so graphs of one context may
+ * overlap.  The products run on the 5th-generation tensor cores: operands bf16, accumulators fp32, every output rounded
+ * once (fp32: not at all).  Every matrix has a 16-byte aligned address, a row pitch (in elements) and sizes that are multiples
+ * of 8; n_groups <= 256, otherwise any size.  (DX_ERR_UNSUPPORTED; outputs that overlap inputs: DX_ERR_INVALID_ARG.)
+ *
+ * Groups.  Sorted row r belongs to group e iff offsets[e] <= r < offsets[e+1] (offsets [n_groups+1], ascending, within
+ * 0 .. n_rows; values outside are cut off and reported as DX_DEV_BAD_OFFSETS).  Groups may be empty; rows outside every group
+ * are neither computed nor written.  gather [n_rows] / gather_div: sorted row r takes row gather[r] / gather_div of its
+ * matrix (a token's row, from the pair perm[r] = token * k + choice; NULL: row r); scatter [n_rows]: the output of sorted row r is
+ * written to row scatter[r] (NULL: r; no row twice).  An index outside its matrix reads zeros / writes nothing and is reported as
+ * DX_DEV_BAD_ROW.  Rows of other groups never matter, whatever they hold.
+ *
+ * moe_grouped_mm: y[scatter(r)] = W_e x[gather(r)], or W_e^T x (transposed = 1), W_e [n, k] row-major.  y_dtype DX_DTYPE_BF16 /
+ *   DX_DTYPE_FP32.  One group is a plain product.
+ * moe_grouped_mm_dw: dW_e [n, k] = sum over the group's rows of dy[gather_dy(r)] x[gather_x(r)]^T: the gradient of W_e.  Written
+ *   whole, zeros for an empty group.  dw_dtype as above; ld_w / stride_w of the description are dW's.
+ * moe_grouped_swiglu: W_e [n = 2 I, k = H], I gate rows, then I up rows: act[r] = silu(g) * u with (g, u) = W_e x[gather(r)],
+ *   from the fp32 products, [n_rows, I] bf16; gate_up [n_rows, 2 I] bf16 receives g and u for the backward pass (may be NULL).
+ * moe_grouped_swiglu_backward: through the down product of each row and the SwiGLU in front of it.  W_e [n = H, k = I] is the
+ *   down matrix, dy the gradient of the tokens' sums; sorted row r is pair q = gather[r] (NULL: r), its dy row q / gather_div, its
+ *   weight pair_w[q] (NULL: 1).  With a = W_e^T dy, s = sigmoid(g):  d_gate_up[r] = (w a u s (1 + g (1 - s)), w a g s),
+ *   act_w[r] = w silu(g) u -- with moe_grouped_mm_dw the gradient of W_e: sum of dy act_w^T -- and
+ *   d_pair_w[q] = <a, silu(g) u> (may be NULL; pairs that no row stands for are not written).  A pair of weight 0 is taken out: all
+ *   of its gradients are 0.  workspace: moe_grouped_swiglu_backward_workspace bytes (0 without d_pair_w), 16-byte aligned.
+ * moe_combine_tokens: y[t] = sum_j w[t, j] z[t k + j], rows fp32 or bf16 (each of z, y), k <= 8, sums in fp32; w NULL: all 1.  A
+ *   weight of 0 takes its row out (it is not read).  moe_combine_tokens_backward: dz[t k + j] = w[t, j] dy[t] and
+ *   dw[t, j] = <z[t k + j], dy[t]> (either may be NULL; both 0 where the weight is 0), all rows of one type.
+ *
+ * spec_head_loss: for rows h [N, H] bf16 and a head W [V, H] bf16, with z = W h[t]:  loss[t] = log sum_v exp(z_v) - z_target,
+ *   dh [N, H] = row_weight[t] * dloss/dh and dW [V, H] = sum_t row_weight[t] * dloss/dW, bf16 (each may be NULL, not all three).
+ *   targets [N]: -1 (no token) and rows of weight 0 have loss 0 and no part in the gradients, whatever h holds (they are left
+ *   out: a padded batch costs its real rows); another id outside [0, V) gives loss NaN, no gradient, DX_DEV_BAD_TOKEN.  Logits are
+ *   never stored: for the gradients they are computed a second time, piece by piece of the vocabulary, and a piece's dz is kept in
+ *   bf16 (each element rounded once).  Any V.  workspace (256-byte aligned): spec_head_loss_workspace says how many
+ *   bytes are needed at least, and how many let it run in as few pieces as are of use; anything between works. */
+typedef struct {
+  int32_t n_groups;      /* E, 1 .. 256 */
+  int32_t n_rows;        /* sorted rows */
+  int32_t n, k;          /* W_e is [n, k] */
+  int64_t ld_w;          /* elements between rows of W_e */
+  int64_t stride_w;      /* elements between groups (>= n * ld_w) */
+} dx_grouped_desc;
+dx_status moe_grouped_mm(dx_ctx* ctx, const dx_grouped_desc* desc, const void* x, int32_t x_rows, int64_t ldx, const void* w,
+                         int32_t transposed, const int32_t* offsets, const int32_t* gather, int32_t gather_div,
+                         const int32_t* scatter, void* y, int32_t y_dtype, int32_t y_rows, int64_t ldy, void* stream);
+dx_status moe_grouped_mm_dw(dx_ctx* ctx, const dx_grouped_desc* desc, const void* dy, int32_t dy_rows, int64_t ld_dy,
+                            const int32_t* gather_dy, int32_t dy_div, const void* x, int32_t x_rows, int64_t ldx,
+                            const int32_t* gather_x, int32_t x_div, const int32_t* offsets, void* dw, int32_t dw_dtype,
+                            void* stream);
+dx_status moe_grouped_swiglu(dx_ctx* ctx, const dx_grouped_desc* desc, const void* x, int32_t x_rows, int64_t ldx,
+                             const void* w_gate_up, const int32_t* offsets, const int32_t* gather, int32_t gather_div,
+                             void* act, int64_t ld_act, void* gate_up, int64_t ld_gate_up, void* stream);
+dx_status moe_grouped_swiglu_backward_workspace(const dx_grouped_desc* desc, size_t* bytes_out);
+dx_status moe_grouped_swiglu_backward(dx_ctx* ctx, const dx_grouped_desc* desc, const void* dy, int32_t dy_rows, int64_t ld_dy,
+                                      const void* w_down, const void* gate_up, int64_t ld_gate_up, const float* pair_w,
+                                      int32_t n_pairs, const int32_t* offsets, const int32_t* gather, int32_t gather_div,
+                                      void* d_gate_up, int64_t ld_d, void* act_w, int64_t ld_act, float* d_pair_w,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+dx_status moe_combine_tokens(dx_ctx* ctx, const void* z, int32_t z_dtype, int64_t ldz, const float* topk_w, int32_t N,
+                             int32_t top_k, int32_t H, void* y, int32_t y_dtype, int64_t ldy, void* stream);
+dx_status moe_combine_tokens_backward(dx_ctx* ctx, const void* dy, int64_t ld_dy, const void* z, int64_t ldz, int32_t dtype,
+                                      const float* topk_w, int32_t N, int32_t top_k, int32_t H, void* dz, int64_t ld_dz,
+                                      float* d_topk_w, void* stream);
+dx_status spec_head_loss_workspace(int32_t N, int32_t V, int32_t H, int32_t grad, size_t* least_out, size_t* best_out);
+dx_status spec_head_loss(dx_ctx* ctx, const void* h, int32_t N, int64_t ldh, const void* W_lm, int32_t V, int64_t ldw, int32_t H,
+                         const int32_t* targets, const float* row_weight, float* loss, void* dh, int64_t ld_dh, void* dW,
+                         int64_t ld_dW, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- greedy verification without any allocation ----------------------------------------------------------------
  * (No counterpart in the paper: an addition for callers of this library that cannot allocate device memory --

@@ -44,6 +44,11 @@ class RouteDesc(C.Structure):
                 ("routed_scale", C.c_float)]
 
 
+class GroupedDesc(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("n_rows", C.c_int32), ("n", C.c_int32), ("k", C.c_int32),
+                ("ld_w", C.c_int64), ("stride_w", C.c_int64)]
+
+
 class CacheStats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("lookups", "hits", "on_demand", "prefetch_issued", "prefetch_used",
                                          "prefetch_wasted", "evictions", "bytes_h2d", "waited_copies", "stall_ns",
@@ -52,6 +57,7 @@ class CacheStats(C.Structure):
 
 _P = C.c_void_p
 _I = C.c_int32
+_L = C.c_int64
 # name -> (restype, argtypes): one line per declaration in include/draftexpert.h
 SIGNATURES = {
     "dx_status_string": (C.c_char_p, [_I]),
@@ -113,6 +119,16 @@ SIGNATURES = {
     "spec_distill_topk": (_I, [_P, _P, _I, _I, _I, C.c_int64, _P, _P, _I, _I, C.c_float, _P, _P, _P, C.c_int64, _P]),
     "moe_route_tokens": (_I, [_P, C.POINTER(RouteDesc), _P, _I, _I, C.c_int64, _P, _P, _P, _P, _P, _P]),
     "moe_route_tokens_backward": (_I, [_P, C.POINTER(RouteDesc), _P, _I, _I, C.c_int64, _P, _P, _P, C.c_int64, _P]),
+    "moe_grouped_mm": (_I, [_P, C.POINTER(GroupedDesc), _P, _I, _L, _P, _I, _P, _P, _I, _P, _P, _I, _I, _L, _P]),
+    "moe_grouped_mm_dw": (_I, [_P, C.POINTER(GroupedDesc), _P, _I, _L, _P, _I, _P, _I, _L, _P, _I, _P, _P, _I, _P]),
+    "moe_grouped_swiglu": (_I, [_P, C.POINTER(GroupedDesc), _P, _I, _L, _P, _P, _P, _I, _P, _L, _P, _L, _P]),
+    "moe_grouped_swiglu_backward_workspace": (_I, [C.POINTER(GroupedDesc), C.POINTER(C.c_size_t)]),
+    "moe_grouped_swiglu_backward": (_I, [_P, C.POINTER(GroupedDesc), _P, _I, _L, _P, _P, _L, _P, _I, _P, _P, _I, _P, _L, _P,
+                                         _L, _P, _P, C.c_size_t, _P]),
+    "moe_combine_tokens": (_I, [_P, _P, _I, _L, _P, _I, _I, _I, _P, _I, _L, _P]),
+    "moe_combine_tokens_backward": (_I, [_P, _P, _L, _P, _L, _I, _P, _I, _I, _I, _P, _L, _P, _P]),
+    "spec_head_loss_workspace": (_I, [_I, _I, _I, _I, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "spec_head_loss": (_I, [_P, _P, _I, _L, _P, _I, _L, _I, _P, _P, _P, _P, _L, _P, _L, _P, C.c_size_t, _P]),
     "expert_cache_create": (_I, [_P, _I, _I, _I, C.c_size_t, C.POINTER(_P)]),
     "expert_cache_set_q4": (_I, [_P, C.POINTER(LayerDesc), _I]),
     "expert_cache_destroy": (_I, [_P]),
@@ -834,6 +850,299 @@ def moe_route_tokens_backward(ctx: Context, logits: torch.Tensor, topk_ids: torc
                                              _ptr(d_topk_w), _ptr(out), ld_d, _ctx_stream(ctx)),
            "moe_route_tokens_backward")
     return out
+
+
+# ---- whole batches of tokens: the experts' products, their combination, the loss ---
+def _operand(ctx: Context, t: torch.Tensor, name: str, cols: Optional[int] = None) -> int:
+    """Row pitch of a bf16 [rows, cols] operand of the products on the context's GPU."""
+    if t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name}: bfloat16 is expected, not {t.dtype}")
+    ld = _matrix(ctx, t, name)[1]
+    if cols is not None and t.shape[1] != cols:
+        raise ValueError(f"{name}: {cols} columns are expected, not {t.shape[1]}")
+    return ld
+
+
+def _groups(ctx: Context, w: torch.Tensor, name: str, n_rows: int) -> GroupedDesc:
+    """Description of a stack of matrices [groups, n, k] with rows at any pitch."""
+    if w.dim() != 3 or not w.is_cuda or w.get_device() != ctx.device:
+        raise ValueError(f"{name}: a 3-d tensor on cuda:{ctx.device} is expected")
+    E, n, k = w.shape
+    stride, ld, step = w.stride()
+    if step != 1 and k > 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if n == 1:
+        ld = k
+    return GroupedDesc(E, n_rows, n, k, ld, stride if E > 1 else n * ld)
+
+
+def _index(ctx: Context, t: Optional[torch.Tensor], name: str, n: Optional[int] = None) -> None:
+    if t is not None and (t.dim() != 1 or t.dtype is not torch.int32 or not t.is_cuda or t.get_device() != ctx.device
+                          or not t.is_contiguous() or (n is not None and t.shape[0] != n)):
+        raise ValueError(f"{name}: a contiguous torch.int32 tensor [{'rows' if n is None else n}] on cuda:{ctx.device} is "
+                         "expected")
+
+
+def _out_dtype(dtype: torch.dtype, name: str) -> int:
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise ValueError(f"{name}: float32 or bfloat16 is expected, not {dtype}")
+    return 1 if dtype is torch.bfloat16 else 0
+
+
+def moe_grouped_mm(ctx: Context, x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, transposed: bool = False,
+                   gather: Optional[torch.Tensor] = None, gather_div: int = 1, scatter: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """Rows sorted by group times their group's matrix: y[scatter[r]] = w[e] x[gather[r] // gather_div] (``transposed``:
+    w[e]^T x), w [E, n, k] and x bfloat16, offsets [E+1] int32.  ``gather`` / ``scatter`` [rows] int32; without them sorted row r
+    is row r.  Rows outside every group are not written."""
+    _index(ctx, gather, "gather")
+    rows = x.shape[0] if gather is None else gather.shape[0]
+    d = _groups(ctx, w, "w", rows)
+    if w.dtype is not torch.bfloat16:
+        raise ValueError(f"w: bfloat16 is expected, not {w.dtype}")
+    _index(ctx, offsets, "offsets", d.n_groups + 1)
+    _index(ctx, scatter, "scatter", rows)
+    ldx = _operand(ctx, x, "x", d.n if transposed else d.k)
+    cols = d.k if transposed else d.n
+    if out is None:
+        dt, ldy = _out_dtype(out_dtype, "out_dtype"), cols
+        out = torch.empty(rows, cols, dtype=out_dtype, device=x.device)
+    else:
+        dt, ldy = _matrix(ctx, out, "out")
+        if out.shape[1] != cols:
+            raise ValueError(f"out: {cols} columns are expected, not {out.shape[1]}")
+    _check(ctx.lib.moe_grouped_mm(ctx.handle, C.byref(d), _ptr(x), x.shape[0], ldx, _ptr(w), 1 if transposed else 0,
+                                  _ptr(offsets), _ptr(gather), gather_div, _ptr(scatter), _ptr(out), dt, out.shape[0], ldy,
+                                  _ctx_stream(ctx)), "moe_grouped_mm")
+    return out
+
+
+def moe_grouped_mm_dw(ctx: Context, dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor,
+                      gather_dy: Optional[torch.Tensor] = None, dy_div: int = 1, gather_x: Optional[torch.Tensor] = None,
+                      x_div: int = 1, out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16
+                      ) -> torch.Tensor:
+    """Gradient of the groups' matrices, dw[e] = sum over the group's rows of dy x^T: [E, n, k] from dy [., n] and x [., k]
+    (bfloat16; rows gathered as in ``moe_grouped_mm``)."""
+    _index(ctx, offsets, "offsets")
+    _index(ctx, gather_dy, "gather_dy")
+    _index(ctx, gather_x, "gather_x")
+    rows = dy.shape[0] if gather_dy is None else gather_dy.shape[0]
+    if rows != (x.shape[0] if gather_x is None else gather_x.shape[0]):
+        raise ValueError("dy and x: the same number of sorted rows is expected")
+    ld_dy, ldx = _operand(ctx, dy, "dy"), _operand(ctx, x, "x")
+    E, n, k = offsets.shape[0] - 1, dy.shape[1], x.shape[1]
+    if out is None:
+        dt = _out_dtype(out_dtype, "out_dtype")
+        out = torch.empty(E, n, k, dtype=out_dtype, device=x.device)
+        d = GroupedDesc(E, rows, n, k, k, n * k)
+    else:
+        dt = _out_dtype(out.dtype, "out")
+        d = _groups(ctx, out, "out", rows)
+        if (d.n_groups, d.n, d.k) != (E, n, k):
+            raise ValueError(f"out: {(E, n, k)} is expected, not {tuple(out.shape)}")
+    _check(ctx.lib.moe_grouped_mm_dw(ctx.handle, C.byref(d), _ptr(dy), dy.shape[0], ld_dy, _ptr(gather_dy),
+                                     1 if gather_dy is None else dy_div, _ptr(x), x.shape[0], ldx, _ptr(gather_x),
+                                     1 if gather_x is None else x_div, _ptr(offsets), _ptr(out), dt, _ctx_stream(ctx)),
+           "moe_grouped_mm_dw")
+    return out
+
+
+def moe_grouped_swiglu(ctx: Context, x: torch.Tensor, w_gate_up: torch.Tensor, offsets: torch.Tensor,
+                       gather: Optional[torch.Tensor] = None, gather_div: int = 1, save: bool = False,
+                       out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """``act`` [rows, I] = silu(gate) * up for rows sorted by group, w_gate_up [E, 2 I, H] (gate rows, then up rows); with
+    ``save`` also ``gate_up`` [rows, 2 I], which the backward pass takes."""
+    _index(ctx, gather, "gather")
+    rows = x.shape[0] if gather is None else gather.shape[0]
+    d = _groups(ctx, w_gate_up, "w_gate_up", rows)
+    if w_gate_up.dtype is not torch.bfloat16:
+        raise ValueError(f"w_gate_up: bfloat16 is expected, not {w_gate_up.dtype}")
+    _index(ctx, offsets, "offsets", d.n_groups + 1)
+    ldx = _operand(ctx, x, "x", d.k)
+    inter = d.n // 2
+    if out is None:
+        out = {"act": torch.empty(rows, inter, dtype=torch.bfloat16, device=x.device)}
+        if save:
+            out["gate_up"] = torch.empty(rows, d.n, dtype=torch.bfloat16, device=x.device)
+        ld_act, ld_gu = inter, d.n
+    else:
+        ld_act = _operand(ctx, out["act"], "act", inter)
+        ld_gu = _operand(ctx, out["gate_up"], "gate_up", d.n) if save else d.n
+        if out["act"].shape[0] != rows or (save and out["gate_up"].shape[0] != rows):
+            raise ValueError(f"out: {rows} rows are expected")
+    _check(ctx.lib.moe_grouped_swiglu(ctx.handle, C.byref(d), _ptr(x), x.shape[0], ldx, _ptr(w_gate_up), _ptr(offsets),
+                                      _ptr(gather), gather_div, _ptr(out["act"]), ld_act,
+                                      _ptr(out["gate_up"]) if save else None, ld_gu, _ctx_stream(ctx)), "moe_grouped_swiglu")
+    return out
+
+
+def moe_grouped_swiglu_backward(ctx: Context, dy: torch.Tensor, w_down: torch.Tensor, gate_up: torch.Tensor,
+                                topk_w: Optional[torch.Tensor], offsets: torch.Tensor, gather: Optional[torch.Tensor] = None,
+                                gather_div: int = 1, out: Optional[Dict[str, torch.Tensor]] = None
+                                ) -> Dict[str, torch.Tensor]:
+    """Backward through w_down [E, H, I] and the SwiGLU in front of it, from the gradient ``dy`` of the tokens' sums:
+    ``d_gate_up`` [rows, 2 I], ``act_w`` [rows, I] (the weighted SwiGLU outputs, the other factor of w_down's gradient) and, with
+    ``topk_w`` (any shape, indexed by pair = gather[r]), ``d_topk_w`` in its shape (pairs without a row keep what ``out`` held, or
+    0)."""
+    _index(ctx, gather, "gather")
+    rows = dy.shape[0] if gather is None else gather.shape[0]
+    d = _groups(ctx, w_down, "w_down", rows)
+    if w_down.dtype is not torch.bfloat16:
+        raise ValueError(f"w_down: bfloat16 is expected, not {w_down.dtype}")
+    _index(ctx, offsets, "offsets", d.n_groups + 1)
+    if topk_w is not None:
+        _dense(ctx, topk_w, "topk_w", tuple(topk_w.shape), torch.float32)
+    ld_dy, ld_gu = _operand(ctx, dy, "dy", d.n), _operand(ctx, gate_up, "gate_up", 2 * d.k)
+    if gate_up.shape[0] != rows:
+        raise ValueError(f"gate_up: {rows} rows are expected")
+    if out is None:
+        bf16, device = torch.bfloat16, dy.device
+        out = {"d_gate_up": torch.empty(rows, 2 * d.k, dtype=bf16, device=device),
+               "act_w": torch.empty(rows, d.k, dtype=bf16, device=device)}
+        if topk_w is not None:
+            # (a permutation writes every pair; fewer rows than pairs leave some out)
+            make = torch.empty_like if topk_w.numel() == rows else torch.zeros_like
+            out["d_topk_w"] = make(topk_w)
+        ld_d, ld_act = 2 * d.k, d.k
+    else:
+        ld_d, ld_act = _operand(ctx, out["d_gate_up"], "d_gate_up", 2 * d.k), _operand(ctx, out["act_w"], "act_w", d.k)
+        if out["d_gate_up"].shape[0] != rows or out["act_w"].shape[0] != rows:
+            raise ValueError(f"out: {rows} rows are expected")
+        if out.get("d_topk_w") is not None:
+            if topk_w is None:
+                raise ValueError("d_topk_w: topk_w is expected with it")
+            _dense(ctx, out["d_topk_w"], "d_topk_w", tuple(topk_w.shape), torch.float32)
+    d_w = out.get("d_topk_w")
+    space, n_space = None, 0
+    if d_w is not None:
+        need = C.c_size_t(0)
+        _check(ctx.lib.moe_grouped_swiglu_backward_workspace(C.byref(d), C.byref(need)),
+               "moe_grouped_swiglu_backward_workspace")
+        n_space = need.value
+        space = torch.empty(n_space, dtype=torch.uint8, device=dy.device)
+    _check(ctx.lib.moe_grouped_swiglu_backward(ctx.handle, C.byref(d), _ptr(dy), dy.shape[0], ld_dy, _ptr(w_down),
+                                               _ptr(gate_up), ld_gu, _ptr(topk_w),
+                                               rows if topk_w is None and gather is None else
+                                               dy.shape[0] * gather_div if topk_w is None else topk_w.numel(),
+                                               _ptr(offsets), _ptr(gather), gather_div, _ptr(out["d_gate_up"]), ld_d,
+                                               _ptr(out["act_w"]), ld_act, _ptr(d_w), _ptr(space), n_space,
+                                               _ctx_stream(ctx)), "moe_grouped_swiglu_backward")
+    return out
+
+
+def _tokens_of(z: torch.Tensor, topk_w: Optional[torch.Tensor], top_k: Optional[int]) -> Tuple[int, int]:
+    if topk_w is not None:
+        if topk_w.dim() != 2 or (top_k is not None and topk_w.shape[1] != top_k):
+            raise ValueError("topk_w: [N, top_k] is expected")
+        top_k = topk_w.shape[1]
+    elif top_k is None:
+        raise ValueError("top_k: expected where topk_w is not given")
+    if top_k < 1 or z.shape[0] % top_k or (topk_w is not None and z.shape[0] != topk_w.shape[0] * top_k):
+        raise ValueError("z: N * top_k rows are expected")
+    return z.shape[0] // top_k, top_k
+
+
+def moe_combine_tokens(ctx: Context, z: torch.Tensor, topk_w: Optional[torch.Tensor], top_k: Optional[int] = None,
+                       out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """y[t] = sum_j topk_w[t, j] z[t * k + j] (``topk_w`` None: the plain sum of ``top_k`` rows), z [N * k, H] float32 or
+    bfloat16; y in ``out_dtype`` (z's by default)."""
+    z_dt, ldz = _matrix(ctx, z, "z")
+    N, k = _tokens_of(z, topk_w, top_k)
+    H = z.shape[1]
+    _dense(ctx, topk_w, "topk_w", (N, k), torch.float32)
+    if out is None:
+        dtype = z.dtype if out_dtype is None else out_dtype
+        y_dt, ldy = _out_dtype(dtype, "out_dtype"), H
+        out = torch.empty(N, H, dtype=dtype, device=z.device)
+    else:
+        if out.shape != (N, H):
+            raise ValueError(f"out: {(N, H)} is expected, not {tuple(out.shape)}")
+        y_dt, ldy = _matrix(ctx, out, "out")
+    _check(ctx.lib.moe_combine_tokens(ctx.handle, _ptr(z), z_dt, ldz, _ptr(topk_w), N, k, H, _ptr(out), y_dt, ldy,
+                                      _ctx_stream(ctx)), "moe_combine_tokens")
+    return out
+
+
+def moe_combine_tokens_backward(ctx: Context, dy: torch.Tensor, z: Optional[torch.Tensor], topk_w: Optional[torch.Tensor],
+                                top_k: Optional[int] = None, out: Optional[Dict[str, torch.Tensor]] = None
+                                ) -> Dict[str, torch.Tensor]:
+    """Gradients of ``moe_combine_tokens``: ``dz`` [N * k, H] = topk_w dy and, with ``topk_w``, ``d_topk_w`` [N, k] = <z, dy> (z
+    and dy of one type; z is not needed without ``d_topk_w``)."""
+    dt, ld_dy = _matrix(ctx, dy, "dy")
+    N, H = dy.shape
+    k = topk_w.shape[1] if topk_w is not None and topk_w.dim() == 2 else top_k
+    if k is None or (top_k is not None and k != top_k):
+        raise ValueError("top_k: [N, top_k] weights, or top_k, are expected")
+    _dense(ctx, topk_w, "topk_w", (N, k), torch.float32)
+    ld_dz = H
+    if out is None:
+        out = {"dz": torch.empty(N * k, H, dtype=dy.dtype, device=dy.device)}
+        if topk_w is not None:
+            out["d_topk_w"] = torch.empty_like(topk_w)
+    else:
+        _dense(ctx, out.get("d_topk_w"), "d_topk_w", (N, k), torch.float32)
+        if out.get("dz") is not None:
+            if out["dz"].dtype is not dy.dtype or out["dz"].shape != (N * k, H):
+                raise ValueError(f"dz: {dy.dtype} {(N * k, H)} is expected")
+            ld_dz = _matrix(ctx, out["dz"], "dz")[1]
+    dz, dw = out.get("dz"), out.get("d_topk_w")
+    ldz = H
+    if dw is not None:
+        if z is None or z.dtype is not dy.dtype or z.shape != (N * k, H):
+            raise ValueError(f"z: {dy.dtype} {(N * k, H)} is expected")
+        ldz = _matrix(ctx, z, "z")[1]
+    _check(ctx.lib.moe_combine_tokens_backward(ctx.handle, _ptr(dy), ld_dy, _ptr(z) if dw is not None else None, ldz, dt,
+                                               _ptr(topk_w), N, k, H, _ptr(dz), ld_dz, _ptr(dw), _ctx_stream(ctx)),
+           "moe_combine_tokens_backward")
+    return out
+
+
+def spec_head_loss(ctx: Context, h: torch.Tensor, W_lm: torch.Tensor, targets: torch.Tensor,
+                   row_weight: Optional[torch.Tensor] = None, grad: bool = True, grad_weight: bool = False,
+                   workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None
+                   ) -> Dict[str, torch.Tensor]:
+    """Cross entropy of hidden rows h [N, H] against W_lm [V, H] (both bfloat16) at ``targets`` [N] (int32, -1 = none) without
+    the logits: ``loss`` [N], with ``grad`` ``dh`` [N, H] and with ``grad_weight`` ``dW`` [V, H], both times ``row_weight``.
+    ``workspace``: a uint8 tensor of at least the library's least size (one of the size it asks for is made otherwise)."""
+    ldh, ldw = _operand(ctx, h, "h"), _operand(ctx, W_lm, "W_lm", h.shape[1])
+    (N, H), V = h.shape, W_lm.shape[0]
+    _dense(ctx, targets, "targets", (N,), torch.int32)
+    _dense(ctx, row_weight, "row_weight", (N,), torch.float32)
+    ld_dh = ld_dw = H
+    if out is None:
+        out = {"loss": torch.empty(N, dtype=torch.float32, device=h.device)}
+        if grad:
+            out["dh"] = torch.empty(N, H, dtype=torch.bfloat16, device=h.device)
+        if grad_weight:
+            out["dW"] = torch.empty(V, H, dtype=torch.bfloat16, device=h.device)
+    else:
+        _dense(ctx, out.get("loss"), "loss", (N,), torch.float32)
+        if grad and out.get("dh") is not None:
+            ld_dh = _operand(ctx, out["dh"], "dh", H)
+        if grad_weight and out.get("dW") is not None:
+            ld_dw = _operand(ctx, out["dW"], "dW", H)
+    dh, dW = out.get("dh") if grad else None, out.get("dW") if grad_weight else None
+    if (dh is not None and dh.shape[0] != N) or (dW is not None and dW.shape[0] != V):
+        raise ValueError("out: rows of dh and dW as those of h and W_lm are expected")
+    if workspace is None:
+        least, best = C.c_size_t(0), C.c_size_t(0)
+        _check(ctx.lib.spec_head_loss_workspace(N, V, H, 1 if dh is not None or dW is not None else 0, C.byref(least),
+                                                C.byref(best)), "spec_head_loss_workspace")
+        workspace = torch.empty(best.value, dtype=torch.uint8, device=h.device)
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != ctx.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: a contiguous torch.uint8 tensor on cuda:{ctx.device} is expected")
+    _check(ctx.lib.spec_head_loss(ctx.handle, _ptr(h), N, ldh, _ptr(W_lm), V, ldw, H, _ptr(targets), _ptr(row_weight),
+                                  _ptr(out.get("loss")), _ptr(dh), ld_dh, _ptr(dW), ld_dw, _ptr(workspace), workspace.numel(),
+                                  _ctx_stream(ctx)), "spec_head_loss")
+    return out
+
+
+def spec_head_loss_workspace(N: int, V: int, H: int, grad: bool = True) -> Tuple[int, int]:
+    """Bytes of workspace ``spec_head_loss`` needs at least, and bytes with which it takes as few pieces as are of use."""
+    least, best = C.c_size_t(0), C.c_size_t(0)
+    _check(load().spec_head_loss_workspace(N, V, H, 1 if grad else 0, C.byref(least), C.byref(best)),
+           "spec_head_loss_workspace")
+    return least.value, best.value
 
 
 class Decoder:

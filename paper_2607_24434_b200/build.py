@@ -18,7 +18,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdraftexpert.so")
 LIB_CHECKED = os.path.join(HERE, "libdraftexpert_checked.so")
 SOURCES = ["dx_api.cu", "dx_route.cu", "dx_grouped.cu", "dx_wide.cu", "dx_accept.cu", "dx_cache.cu", "dx_controller.cu",
-           "dx_eval.cu", "dx_draft_stack.cu", "dx_decode.cu", "dx_logprobs.cu", "dx_distill.cu", "dx_batch_route.cu"]
+           "dx_eval.cu", "dx_draft_stack.cu", "dx_decode.cu", "dx_logprobs.cu", "dx_distill.cu", "dx_batch_route.cu",
+           "dx_experts_mm.cu", "dx_combine.cu", "dx_head.cu"]
 
 
 def _headers_mtime() -> float:

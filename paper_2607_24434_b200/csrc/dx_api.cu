@@ -955,3 +955,295 @@ extern "C" dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc*
   ctx->launches++;
   return DX_OK;
 }
+
+// ---- whole batches of tokens: the experts, their combination, the loss -------------------------------------------------
+namespace {
+
+// a matrix of the tensor-core products: address, pitch and width in whole 16-byte vectors of bf16 (8 elements)
+dx_status check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld) {
+  if (rows < 0 || cols < 1 || ld < cols) return DX_ERR_SHAPE;
+  if (cols % 8 || ld % 8) return DX_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX || ld > (int64_t(1) << 38) || (rows > 0 && ld > (INT64_MAX / 16) / rows)) return DX_ERR_SHAPE;
+  if (rows > 0 && (!p || (uintptr_t)p % 16)) return DX_ERR_INVALID_ARG;
+  return DX_OK;
+}
+struct Range {
+  uintptr_t lo, hi;
+};
+Range rows_range(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t elem) {
+  const uintptr_t lo = (uintptr_t)p;
+  return {lo, rows > 0 && p ? lo + (uintptr_t)(((rows - 1) * ld + cols) * elem) : lo};
+}
+bool overlap(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi && a.lo < a.hi && b.lo < b.hi; }
+
+dx_status check_groups(const dx_grouped_desc* d, const void* w) {
+  if (!d || !w || (uintptr_t)w % 16) return DX_ERR_INVALID_ARG;
+  if (d->n_groups < 1 || d->n_rows < 0 || d->n < 1 || d->k < 1 || d->ld_w < d->k) return DX_ERR_SHAPE;
+  if (d->ld_w > (int64_t(1) << 36) || d->stride_w < (int64_t)(d->n - 1) * d->ld_w + d->k ||
+      d->stride_w > (int64_t(1) << 38)) return DX_ERR_SHAPE;
+  if (d->n_groups > DX_MAX_E || d->n % 8 || d->k % 8 || d->ld_w % 8 || d->stride_w % 8) return DX_ERR_UNSUPPORTED;
+  // (tiles are numbered in 32 bits)
+  const int64_t a = (d->n + 63) / 64, b = (d->k + 63) / 64, rows = d->n_rows / 64 + d->n_groups;
+  const int64_t most = a > b ? a : b;
+  if (a * b > INT32_MAX / d->n_groups || rows * most > INT32_MAX) return DX_ERR_UNSUPPORTED;
+  return DX_OK;
+}
+Range groups_range(const dx_grouped_desc* d, const void* w, int64_t elem) {
+  return rows_range(w, d->n_groups, (int64_t)(d->n - 1) * d->ld_w + d->k, d->stride_w, elem);
+}
+bool dense_dtype(int32_t t) { return t == DX_DTYPE_FP32 || t == DX_DTYPE_BF16; }
+
+}  // namespace
+
+extern "C" dx_status moe_grouped_mm(dx_ctx* ctx, const dx_grouped_desc* desc, const void* x, int32_t x_rows, int64_t ldx,
+                                    const void* w, int32_t transposed, const int32_t* offsets, const int32_t* gather,
+                                    int32_t gather_div, const int32_t* scatter, void* y, int32_t y_dtype, int32_t y_rows,
+                                    int64_t ldy, void* stream) {
+  if (!ctx || (transposed != 0 && transposed != 1) || !dense_dtype(y_dtype) || gather_div < 1) return DX_ERR_INVALID_ARG;
+  dx_status s = check_groups(desc, w);
+  if (s != DX_OK) return s;
+  const int n_in = transposed ? desc->n : desc->k, n_out = transposed ? desc->k : desc->n;
+  s = check_matrix(x, x_rows, n_in, ldx);
+  if (s == DX_OK) s = check_matrix(y, y_rows, n_out, ldy);
+  if (s != DX_OK) return s;
+  if (desc->n_rows == 0) return DX_OK;
+  if (!offsets) return DX_ERR_INVALID_ARG;
+  if (x_rows < (gather ? 1 : desc->n_rows) || y_rows < (scatter ? 1 : desc->n_rows)) return DX_ERR_SHAPE;
+  const Range out = rows_range(y, y_rows, n_out, ldy, y_dtype == DX_DTYPE_FP32 ? 4 : 2);
+  if (overlap(out, rows_range(x, x_rows, n_in, ldx, 2)) || overlap(out, groups_range(desc, w, 2))) return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DxGroupedMm a = {};
+  a.x = x; a.x_rows = x_rows; a.ldx = ldx;
+  a.w = w; a.n_groups = desc->n_groups; a.n = desc->n; a.k = desc->k; a.ldw = desc->ld_w; a.w_stride = desc->stride_w;
+  a.transposed = transposed;
+  a.offsets = offsets; a.n_rows = desc->n_rows; a.gather = gather; a.gather_div = gather_div; a.scatter = scatter;
+  a.y = y; a.y_fp32 = y_dtype == DX_DTYPE_FP32; a.y_rows = y_rows; a.ldy = ldy;
+  DX_CUDA(ctx, dx_launch_grouped_mm(ctx, a, (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+extern "C" dx_status moe_grouped_mm_dw(dx_ctx* ctx, const dx_grouped_desc* desc, const void* dy, int32_t dy_rows, int64_t ld_dy,
+                                       const int32_t* gather_dy, int32_t dy_div, const void* x, int32_t x_rows, int64_t ldx,
+                                       const int32_t* gather_x, int32_t x_div, const int32_t* offsets, void* dw,
+                                       int32_t dw_dtype, void* stream) {
+  if (!ctx || !dense_dtype(dw_dtype) || dy_div < 1 || x_div < 1) return DX_ERR_INVALID_ARG;
+  dx_status s = check_groups(desc, dw);
+  if (s == DX_OK) s = check_matrix(dy, dy_rows, desc->n, ld_dy);
+  if (s == DX_OK) s = check_matrix(x, x_rows, desc->k, ldx);
+  if (s != DX_OK) return s;
+  const int64_t elem = dw_dtype == DX_DTYPE_FP32 ? 4 : 2;
+  const Range out = groups_range(desc, dw, elem);
+  if (overlap(out, rows_range(x, x_rows, desc->k, ldx, 2)) || overlap(out, rows_range(dy, dy_rows, desc->n, ld_dy, 2)))
+    return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  if (desc->n_rows == 0) {   // every group is empty
+    for (int e = 0; e < desc->n_groups; ++e)
+      DX_CUDA(ctx, cudaMemset2DAsync(reinterpret_cast<unsigned char*>(dw) + (size_t)e * desc->stride_w * elem,
+                                     desc->ld_w * elem, 0, desc->k * elem, desc->n, (cudaStream_t)stream));
+    return DX_OK;
+  }
+  if (!offsets) return DX_ERR_INVALID_ARG;
+  if (dy_rows < (gather_dy ? 1 : desc->n_rows) || x_rows < (gather_x ? 1 : desc->n_rows)) return DX_ERR_SHAPE;
+  DxGroupedDw a = {};
+  a.dy = dy; a.dy_rows = dy_rows; a.ld_dy = ld_dy; a.gather_dy = gather_dy; a.dy_div = dy_div;
+  a.x = x; a.x_rows = x_rows; a.ldx = ldx; a.gather_x = gather_x; a.x_div = x_div;
+  a.n_groups = desc->n_groups; a.n = desc->n; a.k = desc->k; a.offsets = offsets; a.n_rows = desc->n_rows;
+  a.dw = dw; a.dw_fp32 = dw_dtype == DX_DTYPE_FP32; a.ld_dw = desc->ld_w; a.dw_stride = desc->stride_w;
+  DX_CUDA(ctx, dx_launch_grouped_dw(ctx, a, (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+extern "C" dx_status moe_grouped_swiglu(dx_ctx* ctx, const dx_grouped_desc* desc, const void* x, int32_t x_rows, int64_t ldx,
+                                        const void* w_gate_up, const int32_t* offsets, const int32_t* gather,
+                                        int32_t gather_div, void* act, int64_t ld_act, void* gate_up, int64_t ld_gate_up,
+                                        void* stream) {
+  if (!ctx || gather_div < 1) return DX_ERR_INVALID_ARG;
+  dx_status s = check_groups(desc, w_gate_up);
+  if (s != DX_OK) return s;
+  if (desc->n % 2) return DX_ERR_SHAPE;
+  if (desc->n % 16) return DX_ERR_UNSUPPORTED;
+  const int n_inter = desc->n / 2, P = desc->n_rows;
+  s = check_matrix(x, x_rows, desc->k, ldx);
+  if (s == DX_OK) s = check_matrix(act, P, n_inter, ld_act);
+  if (s == DX_OK && gate_up) s = check_matrix(gate_up, P, desc->n, ld_gate_up);
+  if (s != DX_OK) return s;
+  if (P == 0) return DX_OK;
+  if (!offsets) return DX_ERR_INVALID_ARG;
+  if (x_rows < (gather ? 1 : P)) return DX_ERR_SHAPE;
+  const Range in[2] = {rows_range(x, x_rows, desc->k, ldx, 2), groups_range(desc, w_gate_up, 2)};
+  const Range out[2] = {rows_range(act, P, n_inter, ld_act, 2), rows_range(gate_up, gate_up ? P : 0, desc->n, ld_gate_up, 2)};
+  if (overlap(out[0], out[1])) return DX_ERR_INVALID_ARG;
+  for (const Range& o : out)
+    for (const Range& i : in)
+      if (overlap(o, i)) return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DxGroupedMm a = {};
+  a.x = x; a.x_rows = x_rows; a.ldx = ldx;
+  a.w = w_gate_up; a.n_groups = desc->n_groups; a.n = desc->n; a.k = desc->k; a.ldw = desc->ld_w; a.w_stride = desc->stride_w;
+  a.offsets = offsets; a.n_rows = P; a.gather = gather; a.gather_div = gather_div;
+  a.y = act; a.y_rows = P; a.ldy = ld_act;
+  DX_CUDA(ctx, dx_launch_grouped_swiglu(ctx, a, gate_up, ld_gate_up, (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+extern "C" dx_status moe_grouped_swiglu_backward_workspace(const dx_grouped_desc* desc, size_t* bytes_out) {
+  if (!desc || !bytes_out) return DX_ERR_INVALID_ARG;
+  if (desc->n_rows < 0 || desc->k < 1) return DX_ERR_SHAPE;
+  *bytes_out = (size_t)dx_swiglu_grad_parts(desc->k) * (size_t)desc->n_rows * sizeof(float);
+  return DX_OK;
+}
+
+extern "C" dx_status moe_grouped_swiglu_backward(dx_ctx* ctx, const dx_grouped_desc* desc, const void* dy, int32_t dy_rows,
+                                                 int64_t ld_dy, const void* w_down, const void* gate_up, int64_t ld_gate_up,
+                                                 const float* pair_w, int32_t n_pairs, const int32_t* offsets,
+                                                 const int32_t* gather, int32_t gather_div, void* d_gate_up, int64_t ld_d,
+                                                 void* act_w, int64_t ld_act, float* d_pair_w, void* workspace,
+                                                 size_t workspace_bytes, void* stream) {
+  if (!ctx || gather_div < 1) return DX_ERR_INVALID_ARG;
+  dx_status s = check_groups(desc, w_down);
+  if (s != DX_OK) return s;
+  const int n_inter = desc->k, P = desc->n_rows;
+  if (n_pairs < 0 || n_inter > INT32_MAX / 2) return DX_ERR_SHAPE;
+  s = check_matrix(dy, dy_rows, desc->n, ld_dy);
+  if (s == DX_OK) s = check_matrix(gate_up, P, 2 * (int64_t)n_inter, ld_gate_up);
+  if (s == DX_OK) s = check_matrix(d_gate_up, P, 2 * (int64_t)n_inter, ld_d);
+  if (s == DX_OK) s = check_matrix(act_w, P, n_inter, ld_act);
+  if (s != DX_OK) return s;
+  if (P == 0) return DX_OK;
+  if (!offsets) return DX_ERR_INVALID_ARG;
+  if (dy_rows < (gather ? 1 : P) || n_pairs < (gather ? 1 : P)) return DX_ERR_SHAPE;
+  if (d_pair_w) {
+    size_t need = 0;
+    moe_grouped_swiglu_backward_workspace(desc, &need);
+    if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need) return DX_ERR_INVALID_ARG;
+  }
+  const Range in[3] = {rows_range(dy, dy_rows, desc->n, ld_dy, 2), groups_range(desc, w_down, 2),
+                       rows_range(gate_up, P, 2 * (int64_t)n_inter, ld_gate_up, 2)};
+  const Range out[2] = {rows_range(d_gate_up, P, 2 * (int64_t)n_inter, ld_d, 2), rows_range(act_w, P, n_inter, ld_act, 2)};
+  if (overlap(out[0], out[1])) return DX_ERR_INVALID_ARG;
+  for (const Range& o : out)
+    for (const Range& i : in)
+      if (overlap(o, i)) return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DxGroupedMm a = {};
+  a.x = dy; a.x_rows = dy_rows; a.ldx = ld_dy;
+  a.w = w_down; a.n_groups = desc->n_groups; a.n = desc->n; a.k = desc->k; a.ldw = desc->ld_w; a.w_stride = desc->stride_w;
+  a.offsets = offsets; a.n_rows = P; a.gather = gather; a.gather_div = gather_div;
+  a.y = d_gate_up; a.y_rows = P; a.ldy = ld_d;
+  int n = 0;
+  DX_CUDA(ctx, dx_launch_grouped_swiglu_grad(ctx, a, gate_up, ld_gate_up, pair_w, n_pairs, act_w, ld_act,
+                                             reinterpret_cast<float*>(workspace), d_pair_w, (cudaStream_t)stream, &n));
+  ctx->launches += n;
+  return DX_OK;
+}
+
+namespace {
+// rows of moe_combine_tokens: 16-byte vectors of eight elements (fp32: two)
+dx_status check_combine(const dx_ctx* ctx, int32_t N, int32_t k, int32_t H) {
+  if (!ctx) return DX_ERR_INVALID_ARG;
+  if (N < 0 || k < 1 || H < 1) return DX_ERR_SHAPE;
+  if (k > DX_MAX_TOPK || (int64_t)N * k > INT32_MAX) return DX_ERR_UNSUPPORTED;
+  return DX_OK;
+}
+}  // namespace
+
+extern "C" dx_status moe_combine_tokens(dx_ctx* ctx, const void* z, int32_t z_dtype, int64_t ldz, const float* topk_w,
+                                        int32_t N, int32_t top_k, int32_t H, void* y, int32_t y_dtype, int64_t ldy,
+                                        void* stream) {
+  dx_status s = check_combine(ctx, N, top_k, H);
+  if (s != DX_OK) return s;
+  if (!dense_dtype(z_dtype) || !dense_dtype(y_dtype)) return DX_ERR_INVALID_ARG;
+  s = check_matrix(z, (int64_t)N * top_k, H, ldz);
+  if (s == DX_OK) s = check_matrix(y, N, H, ldy);
+  if (s != DX_OK) return s;
+  if (N == 0) return DX_OK;
+  const int z32 = z_dtype == DX_DTYPE_FP32, y32 = y_dtype == DX_DTYPE_FP32;
+  if (overlap(rows_range(z, (int64_t)N * top_k, H, ldz, z32 ? 4 : 2), rows_range(y, N, H, ldy, y32 ? 4 : 2)))
+    return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DX_CUDA(ctx, dx_launch_combine(z, z32, ldz, topk_w, N, top_k, H, y, y32, ldy, (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+extern "C" dx_status moe_combine_tokens_backward(dx_ctx* ctx, const void* dy, int64_t ld_dy, const void* z, int64_t ldz,
+                                                 int32_t dtype, const float* topk_w, int32_t N, int32_t top_k, int32_t H,
+                                                 void* dz, int64_t ld_dz, float* d_topk_w, void* stream) {
+  dx_status s = check_combine(ctx, N, top_k, H);
+  if (s != DX_OK) return s;
+  if (!dense_dtype(dtype)) return DX_ERR_INVALID_ARG;
+  const int64_t P = (int64_t)N * top_k, elem = dtype == DX_DTYPE_FP32 ? 4 : 2;
+  s = check_matrix(dy, N, H, ld_dy);
+  if (s == DX_OK && d_topk_w) s = check_matrix(z, P, H, ldz);
+  if (s == DX_OK && dz) s = check_matrix(dz, P, H, ld_dz);
+  if (s != DX_OK) return s;
+  if (N == 0) return DX_OK;
+  if (!dz && !d_topk_w) return DX_ERR_INVALID_ARG;
+  if (dz && (overlap(rows_range(dz, P, H, ld_dz, elem), rows_range(dy, N, H, ld_dy, elem)) ||
+             (d_topk_w && overlap(rows_range(dz, P, H, ld_dz, elem), rows_range(z, P, H, ldz, elem)))))
+    return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  DX_CUDA(ctx, dx_launch_combine_grad(dy, z, dtype == DX_DTYPE_FP32, ld_dy, ldz, topk_w, N, top_k, H, dz, ld_dz, d_topk_w,
+                                      (cudaStream_t)stream));
+  ctx->launches++;
+  return DX_OK;
+}
+
+extern "C" dx_status spec_head_loss_workspace(int32_t N, int32_t V, int32_t H, int32_t grad, size_t* least_out,
+                                              size_t* best_out) {
+  if (!least_out || !best_out) return DX_ERR_INVALID_ARG;
+  if (N < 0 || V < 1 || H < 1) return DX_ERR_SHAPE;
+  *least_out = *best_out = 0;
+  if (N > 0) dx_head_loss_workspace(N, V, H, grad, least_out, best_out);
+  return DX_OK;
+}
+
+extern "C" dx_status spec_head_loss(dx_ctx* ctx, const void* h, int32_t N, int64_t ldh, const void* W_lm, int32_t V, int64_t ldw,
+                                    int32_t H, const int32_t* targets, const float* row_weight, float* loss, void* dh,
+                                    int64_t ld_dh, void* dW, int64_t ld_dW, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+  if (!ctx) return DX_ERR_INVALID_ARG;
+  if (V < 1) return DX_ERR_SHAPE;
+  dx_status s = check_matrix(h, N, H, ldh);
+  if (s == DX_OK) s = check_matrix(W_lm, V, H, ldw);
+  if (s == DX_OK && dh) s = check_matrix(dh, N, H, ld_dh);
+  if (s == DX_OK && dW) s = check_matrix(dW, V, H, ld_dW);
+  if (s != DX_OK) return s;
+  // (tiles and pieces are numbered in 32 bits)
+  if (((int64_t)N / 128 + 1) * ((int64_t)V / 256 + 1) > INT32_MAX || V > INT32_MAX - 512 || N > INT32_MAX - 2048)
+    return DX_ERR_UNSUPPORTED;
+  if (!loss && !dh && !dW) return DX_ERR_INVALID_ARG;
+  const Range in[2] = {rows_range(h, N, H, ldh, 2), rows_range(W_lm, V, H, ldw, 2)};
+  const Range out[2] = {rows_range(dh, dh ? N : 0, H, ld_dh, 2), rows_range(dW, dW ? V : 0, H, ld_dW, 2)};
+  if (overlap(out[0], out[1])) return DX_ERR_INVALID_ARG;
+  for (const Range& o : out)
+    for (const Range& i : in)
+      if (overlap(o, i)) return DX_ERR_INVALID_ARG;
+  DeviceScope scope(ctx->device);
+  DX_CUDA(ctx, scope.err);
+  if (N == 0) {
+    if (dW) DX_CUDA(ctx, cudaMemset2DAsync(dW, ld_dW * 2, 0, (size_t)H * 2, V, (cudaStream_t)stream));
+    return DX_OK;
+  }
+  size_t least = 0, best = 0;
+  dx_head_loss_workspace(N, V, H, dh || dW, &least, &best);
+  if (!targets || !workspace || (uintptr_t)workspace % 256 || workspace_bytes < least) return DX_ERR_INVALID_ARG;
+  DxHeadLoss a = {};
+  a.h = h; a.ldh = ldh; a.W = W_lm; a.ldw = ldw; a.N = N; a.V = V; a.H = H;
+  a.targets = targets; a.row_weight = row_weight; a.loss = loss;
+  a.dh = dh; a.ld_dh = ld_dh; a.dW = dW; a.ld_dW = ld_dW;
+  a.workspace = workspace; a.workspace_bytes = workspace_bytes < best ? workspace_bytes : best;
+  int n = 0;
+  DX_CUDA(ctx, dx_launch_head_loss(ctx, a, (cudaStream_t)stream, &n));
+  ctx->launches += n;
+  return DX_OK;
+}

@@ -278,6 +278,70 @@ cudaError_t dx_launch_batch_route(dx_ctx* ctx, const dx_route_desc& d, const voi
 cudaError_t dx_launch_route_grad(dx_ctx* ctx, const dx_route_desc& d, const void* logits, int dtype, int N,
                                  long long ld, const int32_t* topk_ids, const float* d_topk_w, void* d_logits,
                                  long long ld_d, cudaStream_t st);
+// products of sorted rows with their groups' matrices (dx_experts_mm.cu); every pointer and pitch a multiple of 16 bytes
+struct DxGroupedMm {
+  const void* x;             // bf16 [x_rows][ldx]
+  int x_rows;
+  int64_t ldx;
+  const void* w;             // bf16 [n_groups][n][k], rows ldw apart, groups w_stride
+  int n_groups, n, k, transposed;
+  int64_t ldw, w_stride;
+  const int32_t* offsets;    // [n_groups + 1]
+  int n_rows;                // of the sorted order
+  const int32_t* gather;     // sorted row -> gather / gather_div = row of x (null: itself)
+  int gather_div;
+  const int32_t* scatter;    // sorted row -> row of y (null: itself)
+  void* y;
+  int y_fp32, y_rows;
+  int64_t ldy;
+  const float* addend;       // fp32 [y_rows][columns of y], added in front of the rounding (transposed only)
+};
+struct DxGroupedDw {
+  const void* dy;            // bf16 [dy_rows][ld_dy], n columns
+  int dy_rows;
+  int64_t ld_dy;
+  const void* x;             // bf16 [x_rows][ldx], k columns
+  int x_rows;
+  int64_t ldx;
+  int n_groups, n, k;
+  const int32_t* offsets;
+  int n_rows;
+  const int32_t *gather_dy, *gather_x;
+  int dy_div, x_div;
+  void* dw;                  // [n_groups][n][ld_dw]
+  int dw_fp32;
+  int64_t ld_dw, dw_stride;
+};
+cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t st);
+cudaError_t dx_launch_grouped_swiglu(dx_ctx* ctx, const DxGroupedMm& a, void* gate_up, int64_t ld_gate_up, cudaStream_t st);
+int dx_swiglu_grad_parts(int n_inter);
+cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, const void* gate_up, int64_t ld_gate_up,
+                                          const float* pair_w, int n_pairs, void* act_w, int64_t ld_act, float* partial,
+                                          float* d_pair_w, cudaStream_t st, int* n_launches);
+cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t st);
+cudaError_t dx_launch_combine(const void* z, int fp32, int64_t ldz, const float* w, int n_tokens, int k, int H, void* y,
+                              int y_fp32, int64_t ldy, cudaStream_t st);
+cudaError_t dx_launch_combine_grad(const void* dy, const void* z, int fp32, int64_t ld_dy, int64_t ldz, const float* w,
+                                   int n_tokens, int k, int H, void* dz, int64_t ld_dz, float* dw, cudaStream_t st);
+struct DxHeadLoss {
+  const void* h;             // bf16 [N][ldh]
+  int64_t ldh;
+  const void* W;             // bf16 [V][ldw]
+  int64_t ldw;
+  int N, V, H;
+  const int32_t* targets;
+  const float* row_weight;
+  float* loss;
+  void* dh;                  // bf16 or null
+  int64_t ld_dh;
+  void* dW;                  // bf16 or null
+  int64_t ld_dW;
+  void* workspace;
+  size_t workspace_bytes;
+};
+// bytes of workspace the call needs at least, and those with which it runs in as few pieces as are of any use
+void dx_head_loss_workspace(int N, int V, int H, int grad, size_t* least, size_t* best);
+cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t st, int* n_launches);
 cudaError_t dx_experts_prepare(dx_ctx* ctx);   // opt-in shared memory attributes, once per context
 
 // cache hooks used by the layer code
