@@ -9,25 +9,40 @@
 
 namespace {
 
-// The two lanes 2 i, 2 i + 1 hold two neighbouring elements of columns c and c + 1; after the exchange the even lane has
-// both elements of column c and the odd lane both of column c + 1.
-__device__ __forceinline__ void pair_up(float v0, float v1, int odd, float& x, float& y) {
-  const float got = __shfl_xor_sync(0xffffffffu, odd ? v0 : v1, 1);
-  x = odd ? got : v0;
-  y = odd ? v1 : got;
+// ---- out of tensor memory ------------------------------------------------------------------------------------------
+// A warp turns 32 lanes x 32 columns around in shared memory: fragments as the tensor memory gives them (mm_ld_frag),
+// rounded and stored as transposed 8 x 8 matrices -- a column's lanes next to each other -- and read back in 16-byte pieces, so
+// that global memory sees 64 or 128 neighbouring bytes per row.  About 60 instructions for 1024 elements; exchanging them by
+// shuffles took over 200, and the four storing warps, not the products, were what a tile waited for.
+
+// bf16: 64 bytes per column, pieces of 16 bytes in an order that keeps the eight columns of a matrix in different banks
+__device__ __forceinline__ uint32_t piece64(int column, int piece) {
+  return (uint32_t)(column * 64 + ((piece ^ ((column >> 1) & 3)) << 4));
 }
-__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {   // rounded to nearest even
-  const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
-  return *reinterpret_cast<const uint32_t*>(&b);
+// four pieces of lanes, packed pairs of columns: matrix j = piece j, eight columns from 8 n
+__device__ __forceinline__ void stage64(uint32_t at, int lane, int n, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  stmatrix_t(at + piece64(8 * n + (lane & 7), lane >> 3), a, b, c, d);
 }
-__device__ __forceinline__ float2 bf16_unpair(uint32_t u) {
-  return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+__device__ __forceinline__ void stage_bf16(uint32_t at, int lane, const float (&v)[2][16]) {
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+    stage64(at, lane, n, bf16_pair(v[0][4 * n], v[0][4 * n + 1]), bf16_pair(v[0][4 * n + 2], v[0][4 * n + 3]),
+            bf16_pair(v[1][4 * n], v[1][4 * n + 1]), bf16_pair(v[1][4 * n + 2], v[1][4 * n + 3]));
 }
-__device__ __forceinline__ void put2(float* at, float x, float y) { *reinterpret_cast<float2*>(at) = make_float2(x, y); }
-__device__ __forceinline__ void put2(__nv_bfloat16* at, float x, float y) {
-  *reinterpret_cast<uint32_t*>(at) = bf16_pair(x, y);
+// fp32: 144 bytes per column
+constexpr int kColumn32 = 144;
+__device__ __forceinline__ void stage_fp32(uint32_t at, int lane, const float (&v)[2][16]) {
+  const uint32_t mine = at + (uint32_t)(2 * (lane & 3) * kColumn32 + (lane >> 2) * 4);
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        sts4(mine + (uint32_t)((8 * n + (q & 1)) * kColumn32 + (16 * h + 8 * (q >> 1)) * 4), v[h][4 * n + q]);
 }
-// sorted row of a chunk's column `c0 + lane` (-1: none)
+
+// sorted row of a chunk's column `c0 + lane` (-1: none), and the row of the output it goes to
 __device__ __forceinline__ int sorted_row(const MmTile& t, int c0, int lane) {
   return c0 + lane < t.ncols ? t.n0 + c0 + lane : -1;
 }
@@ -39,117 +54,185 @@ __device__ __forceinline__ int scattered(const MmParams& p, int row) {
   return -1;
 }
 
-// out[row of the column][lane] = D (+ addend), rounded once
-template <class T, bool ADD>
-struct StoreRows {
+struct Fragments {
+  float v[2][16];
+};
+struct FragmentEpilogue {
+  using Values = Fragments;
   const MmParams& p;
-  const int lane, odd;
-  __device__ StoreRows(const MmParams& p_, int lane_) : p(p_), lane(lane_), odd(lane_ & 1) {}
-  __device__ void begin(const MmTile&, int, int) {}
-  __device__ void end(const MmTile&, int, int) {}
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const float (&v)[32]) {
-    const int mine = scattered(p, sorted_row(t, c0, lane));
-    const int m = (lane0 + lane) & ~1;
-    const bool in = m < p.lanes;
-    T* out = reinterpret_cast<T*>(p.out) + m;
+  const int lane;
+  const uint32_t at;       // the warp's staging
+  __device__ FragmentEpilogue(const MmParams& p_, int lane_, uint32_t at_) : p(p_), lane(lane_), at(at_) {}
+  __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld_frag(taddr, x.v); }
+  __device__ __forceinline__ void zero(Values& x) {
 #pragma unroll
-    for (int c = 0; c < 32; c += 2) {
-      float x, y;
-      pair_up(v[c], v[c + 1], odd, x, y);
-      const int row = __shfl_sync(0xffffffffu, mine, c + odd);
-      if (row >= 0 && in) {
+    for (int i = 0; i < 16; ++i) x.v[0][i] = x.v[1][i] = 0.0f;
+  }
+  __device__ __forceinline__ void begin(const MmTile&, int) {}
+  __device__ __forceinline__ void end(const MmTile&) {}
+};
+
+// The chunk's 32 columns are rows `mine` (of lane = column) of a matrix; m: first of the warp's 32 elements in a row.
+template <class T, bool ADD>
+__device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_t at, const float (&v)[2][16], int mine, int m,
+                                            T* out, int64_t ld) {
+  if constexpr (sizeof(T) == 2 && !ADD) {
+    stage_bf16(at, lane, v);
+    __syncwarp();
+    const int piece = lane & 3, x = m + 8 * piece;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
+      const uint4 u = lds16(at + piece64(column, piece));
+      if (row >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(out + (int64_t)row * ld + x) = u;
+    }
+  } else if constexpr (sizeof(T) == 4) {
+    stage_fp32(at, lane, v);
+    __syncwarp();
+    const int x = m + 4 * (lane & 7);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int column = 4 * i + (lane >> 3), row = __shfl_sync(0xffffffffu, mine, column);
+      const uint4 u = lds16(at + (uint32_t)(column * kColumn32 + (lane & 7) * 16));
+      if (row >= 0 && x < p.lanes) {
+        float4 f = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
         if constexpr (ADD) {
-          const float2 a = *reinterpret_cast<const float2*>(p.addend + (int64_t)row * p.lanes + m);
-          x += a.x;
-          y += a.y;
+          const float4 a = *reinterpret_cast<const float4*>(p.addend + (int64_t)row * p.lanes + x);
+          f = make_float4(f.x + a.x, f.y + a.y, f.z + a.z, f.w + a.w);
         }
-        put2(out + (int64_t)row * p.ld, x, y);
+        *reinterpret_cast<float4*>(out + (int64_t)row * ld + x) = f;
       }
     }
+  } else {      // (summed in fp32, then rounded)
+    stage_fp32(at, lane, v);
+    __syncwarp();
+    const int x = m + 8 * (lane & 3);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
+      const uint32_t src = at + (uint32_t)(column * kColumn32 + (lane & 3) * 32);
+      const uint4 u = lds16(src), w = lds16(src + 16);
+      if (row >= 0 && x < p.lanes) {
+        const float4* a = reinterpret_cast<const float4*>(p.addend + (int64_t)row * p.lanes + x);
+        const float4 a0 = a[0], a1 = a[1];
+        *reinterpret_cast<uint4*>(out + (int64_t)row * ld + x) =
+            make_uint4(bf16_pair(__uint_as_float(u.x) + a0.x, __uint_as_float(u.y) + a0.y),
+                       bf16_pair(__uint_as_float(u.z) + a0.z, __uint_as_float(u.w) + a0.w),
+                       bf16_pair(__uint_as_float(w.x) + a1.x, __uint_as_float(w.y) + a1.y),
+                       bf16_pair(__uint_as_float(w.z) + a1.z, __uint_as_float(w.w) + a1.w));
+      }
+    }
+  }
+  __syncwarp();      // (the staging is written again)
+}
+
+// out[row of the column][lane] = D (+ addend), rounded once
+template <class T, bool ADD>
+struct StoreRows : FragmentEpilogue {
+  static constexpr int kStaging = sizeof(T) == 2 && !ADD ? 32 * 64 : 32 * kColumn32;
+  using FragmentEpilogue::FragmentEpilogue;
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
+    const int mine = scattered(p, sorted_row(t, c0, lane));
+    store_chunk<T, ADD>(p, lane, at, x.v, mine, lane0, reinterpret_cast<T*>(p.out), p.ld);
   }
 };
 
 // out of group e: [columns][lanes], element (n, m) = D
 template <class T>
-struct StoreOuter {
-  const MmParams& p;
-  const int lane, odd;
-  __device__ StoreOuter(const MmParams& p_, int lane_) : p(p_), lane(lane_), odd(lane_ & 1) {}
-  __device__ void begin(const MmTile&, int, int) {}
-  __device__ void end(const MmTile&, int, int) {}
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const float (&v)[32]) {
-    const int m = (lane0 + lane) & ~1;
-    const bool in = m < p.lanes;
-    T* out = reinterpret_cast<T*>(p.out) + (int64_t)t.e * p.group_stride + (int64_t)(t.n0 + c0 + odd) * p.ld + m;
-    const int left = t.ncols - c0 - odd;
-#pragma unroll
-    for (int c = 0; c < 32; c += 2) {
-      float x, y;
-      pair_up(v[c], v[c + 1], odd, x, y);
-      if (c < left && in) put2(out + (int64_t)c * p.ld, x, y);
-    }
+struct StoreOuter : FragmentEpilogue {
+  static constexpr int kStaging = sizeof(T) == 2 ? 32 * 64 : 32 * kColumn32;
+  using FragmentEpilogue::FragmentEpilogue;
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
+    store_chunk<T, false>(p, lane, at, x.v, sorted_row(t, c0, lane), lane0,
+                          reinterpret_cast<T*>(p.out) + (int64_t)t.e * p.group_stride, p.ld);
   }
 };
 
 // act = silu(gate) * up from the fp32 products; SAVE: the products themselves, rounded once, for the backward pass.
-// Lane r of 16: r < 8 gate row 8 b + r, else up row 8 b + r - 8 (b = block of eight).
+// Of 16 lanes the first eight are gate rows, the others the same eight up rows: a thread holds both of an element.
 template <bool SAVE>
-struct StoreSwiglu {
-  const MmParams& p;
-  const int lane, odd;
-  __device__ StoreSwiglu(const MmParams& p_, int lane_) : p(p_), lane(lane_), odd(lane_ & 1) {}
-  __device__ void begin(const MmTile&, int, int) {}
-  __device__ void end(const MmTile&, int, int) {}
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const float (&v)[32]) {
-    const int n_inter = p.lanes >> 1;
-    const int up = (lane >> 3) & 1;
-    const int i = ((lane0 + lane) >> 4) * 8 + (lane & 7);
-    const bool in = i < n_inter;
-    const int at = i & ~1;
+struct StoreSwiglu : FragmentEpilogue {
+  static constexpr int kStaging = 32 * 64;
+  using FragmentEpilogue::FragmentEpilogue;
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
+    const float(&v)[2][16] = x.v;
+    const int n_inter = p.lanes >> 1, i0 = lane0 >> 1;      // the warp's 16 elements
+    const int mine = sorted_row(t, c0, lane);
     if constexpr (SAVE) {
-      __nv_bfloat16* save = reinterpret_cast<__nv_bfloat16*>(p.save) + (int64_t)(t.n0 + c0 + odd) * p.ld_save +
-                            (up ? n_inter : 0) + at;
-      const int left = t.ncols - c0 - odd;
 #pragma unroll
-      for (int c = 0; c < 32; c += 2) {
-        float x, y;
-        pair_up(v[c], v[c + 1], odd, x, y);
-        if (c < left && in) put2(save + (int64_t)c * p.ld_save, x, y);
+      for (int n = 0; n < 4; ++n)     // per column: sixteen gates, sixteen ups
+        stage64(at, lane, n, bf16_pair(v[0][4 * n], v[0][4 * n + 1]), bf16_pair(v[1][4 * n], v[1][4 * n + 1]),
+                bf16_pair(v[0][4 * n + 2], v[0][4 * n + 3]), bf16_pair(v[1][4 * n + 2], v[1][4 * n + 3]));
+      __syncwarp();
+      const int piece = lane & 3, i = i0 + 8 * (piece & 1);
+      __nv_bfloat16* save = reinterpret_cast<__nv_bfloat16*>(p.save) + (piece >> 1) * (int64_t)n_inter + i;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int column = 8 * k + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
+        const uint4 u = lds16(at + piece64(column, piece));
+        if (row >= 0 && i < n_inter) *reinterpret_cast<uint4*>(save + (int64_t)row * p.ld_save) = u;
       }
+      __syncwarp();
     }
-    // the gate lane takes the even columns of a pair, the up lane the odd ones
-    float a[16];
+    uint32_t a[2][4];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const float got = __shfl_xor_sync(0xffffffffu, up ? v[2 * j] : v[2 * j + 1], 8);
-      const float g = up ? got : v[2 * j], u = up ? v[2 * j + 1] : got;
-      a[j] = fast_silu(g) * u;
-    }
-    __nv_bfloat16* act = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)(t.n0 + c0 + 2 * odd + up) * p.ld + at;
-    const int left = t.ncols - c0 - 2 * odd - up;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int j = 0; j < 16; j += 2) {      // columns 2 j + up and 2 j + 2 + up
-      float x, y;
-      pair_up(a[j], a[j + 1], odd, x, y);
-      if (2 * j < left && in) put2(act + (int64_t)(2 * j) * p.ld, x, y);
+      for (int n = 0; n < 4; ++n)
+        a[h][n] = bf16_pair(fast_silu(v[h][4 * n]) * v[h][4 * n + 2], fast_silu(v[h][4 * n + 1]) * v[h][4 * n + 3]);
+    // 32 bytes per column; matrices: (eight lanes h, eight columns n)
+#pragma unroll
+    for (int n = 0; n < 4; n += 2) {
+      const int column = 8 * (n + (lane >> 4)) + (lane & 7), h = (lane >> 3) & 1;
+      stmatrix_t(at + (uint32_t)(column * 32 + ((h ^ ((column >> 2) & 1)) << 4)), a[0][n], a[1][n], a[0][n + 1], a[1][n + 1]);
     }
+    __syncwarp();
+    const int h = lane & 1, i = i0 + 8 * h;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int column = 16 * k + (lane >> 1), row = __shfl_sync(0xffffffffu, mine, column);
+      const uint4 u = lds16(at + (uint32_t)(column * 32 + ((h ^ ((column >> 2) & 1)) << 4)));
+      if (row >= 0 && i < n_inter)
+        *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)row * p.ld + i) = u;
+    }
+    __syncwarp();
   }
 };
 
 // D = W_down^T dy = the gradient of an unweighted act.  With q the row's pair, w its weight, s = sigmoid(gate):
 //   d gate = w D up s (1 + gate (1 - s)),  d up = w D gate s,  act_w = w gate s up,  share of d w = sum over lanes of D gate s up.
-// A pair of weight 0 contributes nothing, whatever its rows hold.
-struct StoreSwigluGrad {
-  const MmParams& p;
-  const int lane, odd;
-  int part;
-  __device__ StoreSwigluGrad(const MmParams& p_, int lane_) : p(p_), lane(lane_), odd(lane_ & 1), part(0) {}
-  __device__ void begin(const MmTile& t, int lane0, int) { part = lane0 >> 5; }
-  __device__ void end(const MmTile&, int, int) {}
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const float (&v)[32]) {
-    const int n_inter = p.lanes;
-    const int m = (lane0 + lane) & ~1;
-    const bool in = m < n_inter;
+// A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come in 16-byte pieces, a chunk ahead.
+struct StoreSwigluGrad : FragmentEpilogue {
+  static constexpr int kStaging = 2 * 32 * 64;
+  uint4 gate[4], up[4];
+  __device__ StoreSwigluGrad(const MmParams& p_, int lane_, uint32_t at_) : FragmentEpilogue(p_, lane_, at_) {}
+  __device__ __forceinline__ void fetch(const MmTile& t, int lane0, int c0) {
+    const int x = lane0 + 8 * (lane & 3);
+    const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.gate_up) +
+                               (int64_t)(t.n0 + c0 + (lane >> 2)) * p.ld_gate_up + x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool in = c0 + 8 * i + (lane >> 2) < t.ncols && x < p.lanes;
+      const uint4* g = reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * p.ld_gate_up);
+      gate[i] = in ? __ldcs(g) : make_uint4(0u, 0u, 0u, 0u);
+      up[i] = in ? __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * p.ld_gate_up + p.lanes)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0) { fetch(t, lane0, 0); }
+  __device__ __forceinline__ void out(const uint32_t (&a)[4][4], int mine, int lane0, __nv_bfloat16* to, int64_t ld) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) stage64(at, lane, n, a[n][0], a[n][1], a[n][2], a[n][3]);
+    __syncwarp();
+    const int piece = lane & 3, x = lane0 + 8 * piece;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
+      const uint4 u = lds16(at + piece64(column, piece));
+      if (row >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(to + (int64_t)row * ld + x) = u;
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
     const int mine = sorted_row(t, c0, lane);
     float weight = 0.0f;
     if (mine >= 0) {
@@ -157,57 +240,67 @@ struct StoreSwigluGrad {
       if (q >= 0 && q < p.n_pairs) weight = p.pair_w ? __ldg(p.pair_w + q) : 1.0f;
       else atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
     }
-    const int row0 = t.n0 + c0 + odd, left = t.ncols - c0 - odd;
-    const __nv_bfloat16* gu = reinterpret_cast<const __nv_bfloat16*>(p.gate_up) + (int64_t)row0 * p.ld_gate_up + m;
-    uint32_t gate[16], up[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const bool there = 2 * j < left && in;
-      gate[j] = there ? __ldg(reinterpret_cast<const uint32_t*>(gu + (int64_t)(2 * j) * p.ld_gate_up)) : 0u;
-      up[j] = there ? __ldg(reinterpret_cast<const uint32_t*>(gu + (int64_t)(2 * j) * p.ld_gate_up + n_inter)) : 0u;
+    for (int i = 0; i < 4; ++i) {
+      const int column = 8 * i + (lane >> 2);
+      sts16(at + piece64(column, lane & 3), gate[i]);
+      sts16(at + 2048u + piece64(column, lane & 3), up[i]);
     }
-    __nv_bfloat16* dgu = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)row0 * p.ld + m;
-    __nv_bfloat16* actw = reinterpret_cast<__nv_bfloat16*>(p.act_w) + (int64_t)row0 * p.ld_act + m;
-    float dw[16];
+    __syncwarp();
+    if (c0 + 32 < t.ncols) fetch(t, lane0, c0 + 32);
+    uint32_t dg[4][4], du[4][4], aw[4][4];
+    float dw[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      float a[2];
-      pair_up(v[2 * j], v[2 * j + 1], odd, a[0], a[1]);
-      const float w = __shfl_sync(0xffffffffu, weight, 2 * j + odd);
-      const float2 g2 = bf16_unpair(gate[j]), u2 = bf16_unpair(up[j]);
-      const float g[2] = {g2.x, g2.y}, u[2] = {u2.x, u2.y};
-      float dg[2], du[2], aw[2];
-      dw[j] = 0.0f;
+    for (int n = 0; n < 4; ++n) {
+      const uint32_t from = at + piece64(8 * n + (lane & 7), lane >> 3);
+      uint32_t g4[4], u4[4];
+      ldmatrix_t(from, g4);
+      ldmatrix_t(from + 2048u, u4);
+      const float w2[2] = {__shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3)),
+                           __shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3) + 1)};
+      dw[2 * n] = dw[2 * n + 1] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float e = __expf(-fabsf(g[i])), r = __fdividef(1.0f, 1.0f + e);      // sigmoid of either sign
-        const float sg = g[i] >= 0.0f ? r : e * r, not_sg = g[i] >= 0.0f ? e * r : r;
-        const float gs = g[i] * sg, act = gs * u[i], d = w * a[i];
-        dg[i] = d * u[i] * fmaf(gs, not_sg, sg);
-        du[i] = d * gs;
-        aw[i] = w * act;
-        dw[j] = fmaf(a[i], act, dw[j]);
-        if (w == 0.0f) dg[i] = du[i] = aw[i] = 0.0f;
-      }
-      const bool there = 2 * j < left && in;
-      if (!there || w == 0.0f) dw[j] = 0.0f;
-      if (there) {
-        put2(dgu + (int64_t)(2 * j) * p.ld, dg[0], dg[1]);
-        put2(dgu + (int64_t)(2 * j) * p.ld + n_inter, du[0], du[1]);
-        put2(actw + (int64_t)(2 * j) * p.ld_act, aw[0], aw[1]);
-      }
-    }
-    // sixteen lanes of one parity hold shares of the same sixteen columns: folded so that lane l ends with column l
+      for (int j = 0; j < 4; ++j) {       // eight lanes from 8 j
+        const float2 g2 = bf16_unpair(g4[j]), u2 = bf16_unpair(u4[j]);
+        const float g[2] = {g2.x, g2.y}, u[2] = {u2.x, u2.y};
+        float a[3][2];
 #pragma unroll
-    for (int h = 8; h >= 1; h >>= 1) {
-      const bool high = (lane & (2 * h)) != 0;
-#pragma unroll
-      for (int j = 0; j < h; ++j) {
-        const float got = __shfl_xor_sync(0xffffffffu, high ? dw[j] : dw[j + h], 2 * h);
-        dw[j] = (high ? dw[j + h] : dw[j]) + got;
+        for (int i = 0; i < 2; ++i) {
+          const float d1 = x.v[j >> 1][4 * n + 2 * (j & 1) + i];
+          const float e = __expf(-fabsf(g[i])), r = __fdividef(1.0f, 1.0f + e);      // sigmoid of either sign
+          const float sg = g[i] >= 0.0f ? r : e * r, not_sg = g[i] >= 0.0f ? e * r : r;
+          const float gs = g[i] * sg, act = gs * u[i], d = w2[i] * d1;
+          const bool on = w2[i] != 0.0f;
+          a[0][i] = on ? d * u[i] * fmaf(gs, not_sg, sg) : 0.0f;
+          a[1][i] = on ? d * gs : 0.0f;
+          a[2][i] = on ? w2[i] * act : 0.0f;
+          if (on && lane0 + 8 * j < p.lanes) dw[2 * n + i] = fmaf(d1, act, dw[2 * n + i]);
+        }
+        dg[n][j] = bf16_pair(a[0][0], a[0][1]);
+        du[n][j] = bf16_pair(a[1][0], a[1][1]);
+        aw[n][j] = bf16_pair(a[2][0], a[2][1]);
       }
     }
-    if (p.partial && mine >= 0) p.partial[(int64_t)part * p.n_rows + mine] = dw[0];
+    __syncwarp();
+    __nv_bfloat16* d_gate_up = reinterpret_cast<__nv_bfloat16*>(p.out);
+    out(dg, mine, lane0, d_gate_up, p.ld);
+    out(du, mine, lane0, d_gate_up + p.lanes, p.ld);
+    out(aw, mine, lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
+    if (p.partial) {
+      // eight threads (t / 4) hold shares of the same columns 8 n + 2 (t % 4) + i: folded so that each ends with one column
+#pragma unroll
+      for (int b = 0; b < 3; ++b) {
+        const int h = 4 >> b, bit = 16 >> b;
+        const bool high = (lane & bit) != 0;
+#pragma unroll
+        for (int j = 0; j < h; ++j) {
+          const float got = __shfl_xor_sync(0xffffffffu, high ? dw[j] : dw[j + h], bit);
+          dw[j] = (high ? dw[j + h] : dw[j]) + got;
+        }
+      }
+      const int k = lane >> 2, column = c0 + 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
+      if (column < t.ncols) p.partial[(int64_t)(lane0 >> 5) * p.n_rows + t.n0 + column] = dw[0];
+    }
   }
 };
 
@@ -279,13 +372,22 @@ cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cuda
   // (every group may end in a tile that is not full)
   const long long most = ((p.lanes + lanes - 1) / lanes) *
                          ((p.n_rows + bn - 1) / bn + (p.n_groups < p.n_rows ? p.n_groups : p.n_rows));
-  return few ? mm_launch<FORM, 1, 64, 8, Epilogue>(ctx, maps, p, most, st)
-             : mm_launch<FORM, 2, 256, 6, Epilogue>(ctx, maps, p, most, st);
+  if (p.b_index)
+    return few ? mm_launch<FORM, true, 1, 64, 8, Epilogue>(ctx, maps, p, most, st)
+               : mm_launch<FORM, true, 2, 256, 6, Epilogue>(ctx, maps, p, most, st);
+  return few ? mm_launch<FORM, false, 1, 64, 8, Epilogue>(ctx, maps, p, most, st)
+             : mm_launch<FORM, false, 2, 256, 6, Epilogue>(ctx, maps, p, most, st);
 }
 
-// tensor maps of the rows (columns of D) and of the weights, [groups][n][k] or [groups][2][inter][k]
-bool rows_map(MmMaps* m, const void* x, int64_t x_rows, int cols, int64_t ldx, bool gathered) {
-  return gathered ? dx_matrix_map(&m->bg, x, x_rows, cols, ldx, 1) : dx_matrix_map(&m->b, x, x_rows, cols, ldx, 32);
+// the rows (columns of D): a tensor map, or the matrix they are gathered from
+bool rows_source(MmMaps* m, MmParams* p, const DxGroupedMm& a, int cols) {
+  p->b_index = a.gather;
+  p->b_div = mm_div(a.gather_div);
+  p->b_rows = a.x_rows;
+  p->b_src = a.x;
+  p->b_ld = a.ldx;
+  return a.gather || (dx_matrix_map(&m->b, a.x, a.x_rows, cols, a.ldx, 128) &&
+                      dx_matrix_map(&m->b_few, a.x, a.x_rows, cols, a.ldx, 32));
 }
 
 MmParams base_params(const dx_ctx* ctx, const int32_t* offsets, int groups, int rows) {
@@ -293,7 +395,6 @@ MmParams base_params(const dx_ctx* ctx, const int32_t* offsets, int groups, int 
   p.offsets = offsets;
   p.n_groups = groups;
   p.n_rows = rows;
-  p.a_div = p.b_div = 1;
   p.dev_status = ctx->dev_status;
   p.wait_limit = ctx->wait_limit;
   return p;
@@ -307,9 +408,6 @@ cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t
   const int n_in = a.transposed ? a.n : a.k, n_out = a.transposed ? a.k : a.n;
   p.lanes = n_out;
   p.kdim = n_in;
-  p.b_rows = a.x_rows;
-  p.b_index = a.gather;
-  p.b_div = a.gather_div;
   p.out = a.y;
   p.ld = a.ldy;
   p.scatter = a.scatter;
@@ -318,7 +416,7 @@ cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t
   const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)a.n, (uint64_t)a.n_groups};
   const uint64_t strides[2] = {(uint64_t)a.ldw, (uint64_t)a.w_stride};
   const uint32_t box[3] = {64, a.transposed ? 64u : 128u, 1};
-  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_map(&m, a.x, a.x_rows, n_in, a.ldx, a.gather != nullptr))
+  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, n_in))
     return cudaErrorInvalidValue;
   if (a.transposed) {
     if (a.addend)
@@ -337,9 +435,6 @@ cudaError_t dx_launch_grouped_swiglu(dx_ctx* ctx, const DxGroupedMm& a, void* ga
   const int n_inter = a.n / 2;
   p.lanes = a.n;
   p.kdim = a.k;
-  p.b_rows = a.x_rows;
-  p.b_index = a.gather;
-  p.b_div = a.gather_div;
   p.out = a.y;
   p.ld = a.ldy;
   p.save = gate_up;
@@ -348,7 +443,7 @@ cudaError_t dx_launch_grouped_swiglu(dx_ctx* ctx, const DxGroupedMm& a, void* ga
   const uint64_t dims[5] = {(uint64_t)a.k, 8, 2, (uint64_t)(n_inter / 8), (uint64_t)a.n_groups};
   const uint64_t strides[4] = {(uint64_t)a.ldw, (uint64_t)(n_inter * a.ldw), (uint64_t)(8 * a.ldw), (uint64_t)a.w_stride};
   const uint32_t box[5] = {64, 8, 2, 8, 1};
-  if (!dx_tensor_map(&m.a, a.w, 5, dims, strides, box) || !rows_map(&m, a.x, a.x_rows, a.k, a.ldx, a.gather != nullptr))
+  if (!dx_tensor_map(&m.a, a.w, 5, dims, strides, box) || !rows_source(&m, &p, a, a.k))
     return cudaErrorInvalidValue;
   return gate_up ? launch_rows<kSwiglu, StoreSwiglu<true>>(ctx, m, p, st)
                  : launch_rows<kSwiglu, StoreSwiglu<false>>(ctx, m, p, st);
@@ -363,9 +458,6 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   MmParams p = base_params(ctx, a.offsets, a.n_groups, a.n_rows);
   p.lanes = a.k;
   p.kdim = a.n;
-  p.b_rows = a.x_rows;
-  p.b_index = a.gather;
-  p.b_div = a.gather_div;
   p.out = a.y;
   p.ld = a.ldy;
   p.gate_up = gate_up;
@@ -378,7 +470,7 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)a.n, (uint64_t)a.n_groups};
   const uint64_t strides[2] = {(uint64_t)a.ldw, (uint64_t)a.w_stride};
   const uint32_t box[3] = {64, 64, 1};
-  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_map(&m, a.x, a.x_rows, a.n, a.ldx, a.gather != nullptr))
+  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, a.n))
     return cudaErrorInvalidValue;
   cudaError_t e = launch_rows<kRowsT, StoreSwigluGrad>(ctx, m, p, st);
   *n_launches = 1;
@@ -396,19 +488,22 @@ cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t
   MmParams p = base_params(ctx, a.offsets, a.n_groups, a.n_rows);
   p.lanes = a.k;
   p.columns = a.n;
+  p.a_src = a.x;
+  p.a_ld = a.ldx;
   p.a_rows = a.x_rows;
+  p.b_src = a.dy;
+  p.b_ld = a.ld_dy;
   p.b_rows = a.dy_rows;
   p.a_index = a.gather_x;
-  p.a_div = a.x_div;
+  p.a_div = mm_div(a.x_div);
   p.b_index = a.gather_dy;
-  p.b_div = a.dy_div;
+  p.b_div = mm_div(a.dy_div);
   p.out = a.dw;
   p.ld = a.ld_dw;
   p.group_stride = a.dw_stride;
-  if (!dx_matrix_map(&m.a, a.x, a.x_rows, a.k, a.ldx, 64) || !dx_matrix_map(&m.ag, a.x, a.x_rows, a.k, a.ldx, 1) ||
-      !dx_matrix_map(&m.b, a.dy, a.dy_rows, a.n, a.ld_dy, 64) || !dx_matrix_map(&m.bg, a.dy, a.dy_rows, a.n, a.ld_dy, 1))
+  if (!dx_matrix_map(&m.a, a.x, a.x_rows, a.k, a.ldx, 64) || !dx_matrix_map(&m.b, a.dy, a.dy_rows, a.n, a.ld_dy, 64))
     return cudaErrorInvalidValue;
   const long long tiles = (long long)a.n_groups * ((a.k + 255) / 256) * ((a.n + 255) / 256);
-  return a.dw_fp32 ? mm_launch<kOuter, 2, 256, 6, StoreOuter<float>>(ctx, m, p, tiles, st)
-                   : mm_launch<kOuter, 2, 256, 6, StoreOuter<__nv_bfloat16>>(ctx, m, p, tiles, st);
+  return a.dw_fp32 ? mm_launch<kOuter, true, 2, 256, 6, StoreOuter<float>>(ctx, m, p, tiles, st)
+                   : mm_launch<kOuter, true, 2, 256, 6, StoreOuter<__nv_bfloat16>>(ctx, m, p, tiles, st);
 }

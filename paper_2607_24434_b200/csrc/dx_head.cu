@@ -66,14 +66,21 @@ struct RowSums {
   const int lane;
   int row, target;
   float top, sum;
-  __device__ RowSums(const MmParams& p_, int lane_) : p(p_), lane(lane_) {}
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int) {
+  static constexpr int kStaging = 0;
+  struct Values {
+    float v[32];
+  };
+  __device__ RowSums(const MmParams& p_, int lane_, uint32_t) : p(p_), lane(lane_) {}
+  __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
+  __device__ __forceinline__ void zero(Values&) {}
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
     target = row >= 0 ? __ldg(p.targets + __ldg(p.a_index + row)) - t.n0 : -1;   // (its place among the tile's columns)
     top = -INFINITY;
     sum = 0.0f;
   }
-  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, float (&v)[32]) {
+  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, Values& x) {
+    float(&v)[32] = x.v;
     const int left = t.ncols - c0;
     if (left < 32) {
 #pragma unroll
@@ -99,7 +106,7 @@ struct RowSums {
     sum = sum * ex2((top - from) * kLog2e) + ((s[0] + s[1]) + (s[2] + s[3]));
     top = m;
   }
-  __device__ __forceinline__ void end(const MmTile& t, int, int) {
+  __device__ __forceinline__ void end(const MmTile& t) {
     if (row >= 0) p.part[(int64_t)(t.n0 >> 8) * p.part_pitch + row] = make_float2(top, sum);
   }
 };
@@ -157,8 +164,14 @@ struct StoreDz {
   const int lane;
   int row, target;
   float lse, weight, at_target;
-  __device__ StoreDz(const MmParams& p_, int lane_) : p(p_), lane(lane_) {}
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int) {
+  static constexpr int kStaging = 0;
+  struct Values {
+    float v[32];
+  };
+  __device__ StoreDz(const MmParams& p_, int lane_, uint32_t) : p(p_), lane(lane_) {}
+  __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
+  __device__ __forceinline__ void zero(Values&) {}
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
     target = -1;
     lse = weight = at_target = 0.0f;
@@ -170,8 +183,9 @@ struct StoreDz {
       at_target = weight * expm1f(-__ldg(p.row_loss + row));
     }
   }
-  __device__ __forceinline__ void end(const MmTile&, int, int) {}
-  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, float (&v)[32]) {
+  __device__ __forceinline__ void end(const MmTile&) {}
+  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, Values& x) {
+    float(&v)[32] = x.v;
 #pragma unroll
     for (int c = 0; c < 32; ++c) v[c] = weight * ex2((v[c] - lse) * kLog2e);
     const int at = target - c0;
@@ -184,8 +198,7 @@ struct StoreDz {
     uint32_t w[16];
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * c], v[2 * c + 1]);
-      w[c] = *reinterpret_cast<const uint32_t*>(&b);
+      w[c] = bf16_pair(v[2 * c], v[2 * c + 1]);
     }
     // (columns behind the piece's last are not read: the matrices of the gradients end there)
     __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)row * p.ld + t.n0 + c0;
@@ -233,8 +246,8 @@ cudaError_t launch_head(dx_ctx* ctx, const MmMaps& m, const MmParams& p, cudaStr
   const bool few = p.n_rows <= 128;
   const long long lanes = few ? 128 : 256;
   const long long tiles = ((p.n_rows + lanes - 1) / lanes) * ((p.columns + 255) / 256);
-  return few ? mm_launch<kHead, 1, 256, 4, Epilogue>(ctx, m, p, tiles, st)
-             : mm_launch<kHead, 2, 256, 6, Epilogue>(ctx, m, p, tiles, st);
+  return few ? mm_launch<kHead, true, 1, 256, 4, Epilogue>(ctx, m, p, tiles, st)
+             : mm_launch<kHead, true, 2, 256, 6, Epilogue>(ctx, m, p, tiles, st);
 }
 
 }  // namespace
@@ -264,17 +277,17 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   int n = 0;
 
   MmMaps m = {};
-  if (!dx_matrix_map(&m.ag, a.h, a.N, a.H, a.ldh, 1) || !dx_matrix_map(&m.b, a.W, a.V, a.H, a.ldw, 128))
-    return cudaErrorInvalidValue;
+  if (!dx_matrix_map(&m.b, a.W, a.V, a.H, a.ldw, 128)) return cudaErrorInvalidValue;
   MmParams p = {};
   p.n_groups = 1;
   p.n_rows = a.N;
   p.n_live = n_live + 1;
   p.columns = a.V;
   p.kdim = a.H;
+  p.a_src = a.h;
+  p.a_ld = a.ldh;
   p.a_rows = a.N;
   p.a_index = live;
-  p.a_div = p.b_div = 1;
   p.targets = a.targets;
   p.row_weight = a.row_weight;
   p.part = part;

@@ -9,11 +9,14 @@
 // The contraction goes in blocks of 64 elements through a ring of shared-memory stages that tensor-map copies (TMA) fill:
 // rows of 128 bytes in the 128-byte swizzle that tcgen05.mma reads.  Either operand may be "K-major" (its rows lie along
 // the contraction) or "MN-major" (its rows lie across it: a box holds 64 contraction rows of 64 lanes or columns), so
-// that transposed weights and products over the rows themselves need no transposed copy.  Rows may be gathered by index
-// (tile::gather4, four rows of 128 bytes per copy); an index outside the matrix reads zeros.
+// that transposed weights and products over the rows themselves need no transposed copy.  Rows gathered by index come in
+// 16-byte pieces (cp.async) from four warps of their own, which write the same swizzle; an index outside the matrix reads
+// zeros.  (Tensor-map copies of four gathered rows took 85 to 120 clocks each, whoever issued them: 2.8 to 3.8 ms where rows
+// in place take 1.0 ms, 98304 rows x 2048 x 2816.)
 //
-// Warps: 0-3 take finished tiles out of tensor memory (lanes 32 w .. 32 w + 31), 4 issues the copies, 5 owns the tensor
-// memory and issues the products (one lane; in a pair only the first CTA's).  Two accumulators take turns, so a tile
+// Warps: 0-3 take finished tiles out of tensor memory (lanes 32 w .. 32 w + 31), 4 asks for A and 6 for B (one warp where only
+// one operand comes by tensor map), 5 owns the tensor memory and issues the products (in a pair only the first CTA's); the last
+// four gather.  Two accumulators take turns, so a tile
 // is stored while the next one is multiplied.  Every wait is bounded; one that runs out raises the CTA's abort flag,
 // after which nothing more is copied or multiplied, copies and products in flight are waited for (bounded), tensor
 // memory is freed and DX_DEV_WAIT_EXPIRED stands in the status word.
@@ -26,7 +29,11 @@
 
 namespace {
 
-constexpr int kMmThreads = 192;
+__host__ __device__ constexpr bool mm_two_copiers(int form, bool gather);
+// four storing warps, one or two copying, one multiplying, four gathering
+__host__ __device__ constexpr int mm_threads(int form, bool gather) {
+  return 32 * (6 + (mm_two_copiers(form, gather) ? 1 : 0) + (gather ? 4 : 0));
+}
 constexpr int kMmK = 64;                    // contraction elements of a stage: 128 bytes of a row
 constexpr int kMmA = 128 * kMmK * 2;        // bytes of a CTA's 128 rows of A in a stage
 constexpr int kMmMaxStages = 8;
@@ -62,16 +69,9 @@ __device__ __forceinline__ void tma5(uint32_t dst, const CUtensorMap* map, int x
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar) : "memory");
 }
-// four rows of the matrix, 128 bytes of each (the map's box is one row high)
-template <int CG>
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap* map, int x, int r0, int r1, int r2, int r3,
-                                            uint32_t bar) {
-  if constexpr (CG == 2)
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar & kFirstCta) : "memory");
-  else
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar) : "memory");
+// 16 bytes, or (bytes = 0) zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
@@ -81,24 +81,26 @@ __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
 // K-major: groups of eight rows are 1024 bytes apart (sbo); a step of 16 contraction elements is 32 bytes further.
 // MN-major: boxes of 64 lanes (columns) x 64 contraction rows of 128 bytes; eight contraction rows are 1024 bytes apart
 // (sbo), the next 64 lanes 8192 (lbo); a step of 16 contraction rows is 2048 bytes further.
-__device__ __forceinline__ uint64_t mm_desc(uint32_t addr, bool mn_major) {
-  const uint32_t lo = ((addr & 0x3FFFFu) >> 4) | ((mn_major ? 8192u >> 4 : 1u) << 16);
-  const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
-  return (uint64_t)hi << 32 | lo;
+// (As two words: only the low one changes from product to product.)
+__device__ __forceinline__ uint32_t mm_desc_lo(uint32_t addr, bool mn_major) {
+  return ((addr & 0x3FFFFu) >> 4) | ((mn_major ? 8192u >> 4 : 1u) << 16);
 }
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 // fp32 accumulators, bf16 operands, the operands' majors, columns / 8, lanes / 16
 __host__ __device__ constexpr uint32_t mm_idesc(bool a_mn, bool b_mn, int lanes, int columns) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
          ((uint32_t)(columns >> 3) << 17) | ((uint32_t)(lanes >> 4) << 24);
 }
 template <int CG>
-__device__ __forceinline__ void mm_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mm_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   if constexpr (CG == 2)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
   else
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
 }
 // arrives at the barrier (in a pair: at both CTAs' barriers of this offset) once all products issued so far are done
 template <int CG>
@@ -140,8 +142,62 @@ __device__ __forceinline__ void mm_ld32(uint32_t taddr, float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+// The same 32 lanes x 32 columns in the fragments of an 8 x 8 matrix load: thread t holds, for the 16 lanes from 16 h and the
+// eight columns from 8 n, v[h][4 n + {0, 1}] = lane t / 4, columns 2 (t % 4) + {0, 1} and v[h][4 n + {2, 3}] = lane 8 + t / 4.
+__device__ __forceinline__ void mm_ld_frag(uint32_t taddr, float (&v)[2][16]) {
+  uint32_t r[2][16];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[h][0]), "=r"(r[h][1]), "=r"(r[h][2]), "=r"(r[h][3]), "=r"(r[h][4]), "=r"(r[h][5]), "=r"(r[h][6]),
+          "=r"(r[h][7]), "=r"(r[h][8]), "=r"(r[h][9]), "=r"(r[h][10]), "=r"(r[h][11]), "=r"(r[h][12]), "=r"(r[h][13]),
+          "=r"(r[h][14]), "=r"(r[h][15])
+        : "r"(taddr + (uint32_t)h * (16u << 16)));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[h][i] = __uint_as_float(r[h][i]);
+}
+// four 8 x 8 matrices of 16-bit elements, transposed: lanes 8 j .. 8 j + 7 name the rows of matrix j
+__device__ __forceinline__ void stmatrix_t(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix_t(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t at, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void sts4(uint32_t at, float v) {
+  asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+}
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {   // rounded to nearest even
+  const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+__device__ __forceinline__ float2 bf16_unpair(uint32_t u) {
+  return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+}
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// One lane of a warp that goes through a loop together: what it computes stays in uniform registers, where copies and products
+// take their operands from.  (With one lane in a branch of its own, every operand is moved there again for every instruction:
+// 100 to 150 clocks for a copy, 400 for the four products of a stage.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ uint32_t cta_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -150,10 +206,24 @@ __device__ __forceinline__ uint32_t cta_rank() {
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// arrive at the first CTA's barrier of this offset
+// a wait for what both CTAs of a pair have written
+__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  for (uint32_t it = 0; it <= limit; ++it) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (ok) return true;
+    if ((it & 63u) == 63u && *abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+// Arrive at the first CTA's barrier of this offset.  What is handed on lies in this CTA's shared or tensor memory and is read
+// by its own SM's tensor core, so the default release at CTA scope orders it; a release at cluster scope costs a memory barrier
+// of its own for every stage (stages then took 2600 clocks instead of 700).
 __device__ __forceinline__ void arrive_at_first(uint32_t bar) {
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\t"
-               "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
+               "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
 }
 // Wait of the warps that store finished tiles: lane 0 polls with pauses, so that their scheduler partitions stay free for
 // the copying and the multiplying warp.
@@ -174,16 +244,29 @@ __device__ __forceinline__ bool mm_store_wait(uint32_t bar, uint32_t parity, vol
 // ---- parameters ----------------------------------------------------------------------------------------------------
 struct MmMaps {
   CUtensorMap a, b;       // boxes of rows
-  CUtensorMap ag, bg;     // the same matrices for gathered rows
+  CUtensorMap b_few;      // of fewer rows
 };
+// Division of 0 <= q < 2^31 by a constant d of the launch: q factor >> shift with shift = 31 + ceil(log2 d) and
+// factor = ceil(2^shift / d) < 2^32 (exact: factor d - 2^shift < d <= 2^(shift - 31), so the error stays below 1 / d).  d = 1: factor 0.
+struct MmDiv {
+  uint32_t factor, shift;
+};
+inline MmDiv mm_div(int d) {
+  if (d <= 1) return {0u, 0u};
+  uint32_t s = 0;
+  while ((1u << s) < (uint32_t)d) ++s;
+  return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), 31 + s};
+}
 struct MmParams {
   int n_groups, n_rows;          // groups; rows of the sorted order (offsets lie in 0 .. n_rows)
   int lanes, columns, kdim;      // extents of D's lanes and columns and of the contraction, where they are not rows
-  int a_rows, b_rows;            // rows of the matrices that are gathered from (an index outside reads zeros)
+  const void *a_src, *b_src;     // matrices that rows are gathered from (bf16), their rows and pitches; an index outside
+  int a_rows, b_rows;            // reads zeros
+  int64_t a_ld, b_ld;
   const int32_t* offsets;        // [n_groups + 1]
   const int32_t* a_index;        // sorted row -> index / a_div = row of A's matrix (null: the row itself)
   const int32_t* b_index;
-  int a_div, b_div;
+  MmDiv a_div, b_div;
   // output: element (row of column n, lane m) at out + row * ld + m
   void* out;
   int64_t ld;
@@ -225,14 +308,15 @@ enum MmForm {
 };
 __host__ __device__ constexpr bool mm_a_mn(int form) { return form == kRowsT || form == kOuter; }
 __host__ __device__ constexpr bool mm_b_mn(int form) { return form == kOuter; }
+// both operands (may) come by tensor map: a warp for each
+__host__ __device__ constexpr bool mm_two_copiers(int form, bool gather) { return form == kOuter || !gather; }
 
-struct MmShared {
+struct __align__(16) MmShared {
   unsigned long long full[kMmMaxStages];
   unsigned long long empty[kMmMaxStages];
   unsigned long long acc_full[2], acc_empty[2], drained;
   uint32_t tmem_base;
   int abort_flag;
-  int tiles;                     // of the launch
   int off[DX_MAX_E + 1];         // first row of a group, and behind it its end where the next begins elsewhere
   int cnt[DX_MAX_E];
   int before[DX_MAX_E + 1];      // row tiles in front of a group
@@ -245,6 +329,9 @@ struct MmTile {
   int ncols;      // columns that exist
   int row0, rows; // (contraction over rows) the group's rows
   int kblocks;
+  __device__ __forceinline__ MmTile uniform_copy() const {
+    return {uniform(e), uniform(m0), uniform(n0), uniform(ncols), uniform(row0), uniform(rows), uniform(kblocks)};
+  }
 };
 
 template <int FORM, int CG, int BN>
@@ -301,36 +388,37 @@ struct MmSchedule {
 template <int CG>
 __device__ __forceinline__ int mm_width(int ncols) { return (ncols + 16 * CG - 1) / (16 * CG) * (16 * CG); }
 
-// row of the matrix that sorted row r takes (-1, which reads zeros, where the index points outside)
-__device__ __forceinline__ int mm_source(const int32_t* index, int div, int r, int n_rows, int32_t* dev_status) {
-  if (!index) return r;
-  const int q = __ldg(index + r);
-  const int row = q < 0 ? -1 : div == 1 ? q : q / div;
+// Row of the matrix that an index (a pair, say) stands for; -1, which reads zeros, where it points outside.  Kept apart from the
+// load of the index: several loads are to be in flight before the first is looked at.
+__device__ __forceinline__ int mm_row(int q, MmDiv div, int n_rows, int32_t* dev_status) {
+  const int row = q < 0 ? -1 : div.factor == 0u ? q : (int)((uint64_t)(uint32_t)q * div.factor >> div.shift);
   if (row >= 0 && row < n_rows) return row;
   atomicExch(dev_status, (int32_t)DX_DEV_BAD_ROW);
   return -1;
 }
 
-template <int FORM, int CG, int BN, int STAGES, class Epilogue>
-__global__ void __launch_bounds__(kMmThreads, 1)
+template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
+__global__ void __launch_bounds__(mm_threads(FORM, GATHER), 1)
 dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmParams p) {
   constexpr int kHalf = BN / CG;                       // columns whose rows a CTA fetches
   constexpr int kB = (kHalf < 32 ? 32 : kHalf) * kMmK * 2;
   constexpr int kStage = kMmA + kB;
-  constexpr bool A_MN = mm_a_mn(FORM), B_MN = mm_b_mn(FORM);
+  constexpr bool A_MN = mm_a_mn(FORM), B_MN = mm_b_mn(FORM), kTwo = mm_two_copiers(FORM, GATHER);
+  constexpr int kFirstGather = kTwo ? 7 : 6;
   constexpr uint32_t kAccCols = BN < 32 ? 32 : BN, kTmemCols = 2 * kAccCols;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   MmShared* s = reinterpret_cast<MmShared*>(ring + (size_t)STAGES * kStage);
+  unsigned char* staging = ring + (size_t)STAGES * kStage + (sizeof(MmShared) + 127) / 128 * 128;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? cta_rank() : 0u;
   const int unit = blockIdx.x / CG, n_units = gridDim.x / CG;
   volatile int* abort_flag = &s->abort_flag;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(smem_u32(&s->full[i]), 1);
+      mbar_init(smem_u32(&s->full[i]), (kTwo ? 2 : 1) + (GATHER ? CG : 0));
       mbar_init(smem_u32(&s->empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -341,8 +429,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     s->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (FORM != kHead) tma_prefetch_map(&maps.a);
-    tma_prefetch_map(FORM != kHead && FORM != kOuter && p.b_index ? &maps.bg : &maps.b);
-    if (FORM == kHead || FORM == kOuter) tma_prefetch_map(&maps.ag);
+    if (!GATHER || FORM == kHead || FORM == kOuter) tma_prefetch_map(&maps.b);
   }
   if (warp == 5) mm_tmem_alloc<CG>(smem_u32(&s->tmem_base), kTmemCols);
   dx_pdl_wait();
@@ -387,108 +474,54 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
                     : FORM == kHead ? schedule.m_tiles * schedule.n_tiles
                                     : s->before[p.n_groups] * schedule.m_tiles;
 
-  if (warp == 4) {
+  if (warp == 4 || (kTwo && warp == 6)) {
     // ------------------------------------------------------------------------------------------------------ copies
+    // warp 4: A, or the only operand that comes by tensor map; warp 6: B
+    const bool for_a = FORM != kHead && warp == 4, for_b = FORM == kHead || warp == 6;
     uint32_t slot = 0, phase = 0, issued = 0;
     bool alive = true;
     for (int t = unit; t < total && alive; t += n_units) {
-      const MmTile tile = schedule.get(t);
-      if (tile.kblocks == 0) continue;
-      const int width = mm_width<CG>(tile.ncols), half = width / CG;
-      const int m0 = tile.m0 + (int)rank * 128;
-      constexpr int kIdx = (FORM == kHead ? 1 : (kHalf + 127) / 128);
-      int rows_at[kIdx][4];
-      uint32_t bytes;
-      bool gathered = false;
-      if constexpr (FORM == kHead) {
-        bytes = kMmA + kB;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = m0 + 4 * lane + i;
-          rows_at[0][i] = r < tile.rows ? mm_source(p.a_index, 1, r, p.a_rows, p.dev_status) : -1;
-        }
-      } else if constexpr (FORM == kOuter) {
-        bytes = kMmA + (uint32_t)((half + 63) / 64) * 8192u;
-      } else {
-        gathered = p.b_index != nullptr;
-        if (gathered) {
-          bytes = kMmA + (uint32_t)((half + 3) / 4) * 512u;
-#pragma unroll
-          for (int j = 0; j < kIdx; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int c = (int)rank * half + 128 * j + 4 * lane + i;
-              rows_at[j][i] = c < tile.ncols ? mm_source(p.b_index, p.b_div, tile.n0 + c, p.b_rows, p.dev_status) : -1;
-            }
-        } else {
-          bytes = kMmA + (uint32_t)((half + 31) / 32) * 4096u;
-        }
-      }
-      // (products over rows: lane l looks up rows 4 (l % 16) .. + 3 of a block, one block ahead of the copies)
-      int ra[4] = {-1, -1, -1, -1}, rb[4] = {-1, -1, -1, -1};
-      auto look_up = [&](int k0) {
-        const bool tail = tile.rows - k0 < kMmK;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int q = k0 + 4 * (lane & 15) + i;
-          if (p.a_index || tail)
-            ra[i] = q < tile.rows ? mm_source(p.a_index, p.a_div, tile.row0 + q, p.a_rows, p.dev_status) : -1;
-          if (p.b_index || tail)
-            rb[i] = q < tile.rows ? mm_source(p.b_index, p.b_div, tile.row0 + q, p.b_rows, p.dev_status) : -1;
-        }
-      };
-      if constexpr (FORM == kOuter) look_up(0);
+      const MmTile tile = schedule.get(t).uniform_copy();
+      const int half = mm_width<CG>(tile.ncols) / CG, m0 = tile.m0 + (int)rank * 128;
+      const int n0 = tile.n0 + (int)rank * half;
+      // rows as columns: copies of 128 rows, or of 32 where those would bring twice what is needed
+      const bool big = FORM == kHead || (kHalf >= 128 && half > 64);
+      const int nb = FORM == kOuter ? (half + 63) / 64 : FORM == kHead ? kHalf / 128 : big ? (half + 127) / 128 : (half + 31) / 32;
+      const uint32_t box = FORM == kOuter ? 8192u : big ? 16384u : 4096u;   // bytes of a copy of B
       for (int kb = 0; kb < tile.kblocks; ++kb) {
-        int ok = 1;
-        if (lane == 0) {
-          ok = mbar_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit) ? 1 : 0;
-          if (ok && rank == 0) mbar_arrive_expect_tx(smem_u32(&s->full[slot]), bytes * CG);
-        }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) { alive = false; break; }
+        const int k0 = kb * kMmK;
+        // Products over rows: a group's last block, where it is not full, is gathered with zeros behind the last row (in
+        // both operands: nothing of another group's rows, not even a NaN, gets in).
+        const bool tail = FORM == kOuter && tile.rows - k0 < kMmK;
+        const bool here = FORM != kOuter || (!tail && !(for_a ? p.a_index : p.b_index));
+        if (!mbar_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
         const uint32_t bar = smem_u32(&s->full[slot]);
         const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
-        const int k0 = kb * kMmK;
-        if constexpr (FORM == kOuter) {
-          // A block of 64 rows of the group; the last one takes its rows one by one, so that the rows behind the
-          // group's last come as zeros (in both operands: nothing of another group's, not even a NaN, gets in).
-          const bool tail = tile.rows - k0 < kMmK;
-          const int x = m0, y = tile.n0 + (int)rank * half, nb = (half + 63) / 64;
-          if (!p.a_index && !tail) {
-            if (lane < 2) tma2<CG>(da + lane * 8192u, &maps.a, x + 64 * lane, tile.row0 + k0, bar);
-          } else {
-            const int g = lane & 15, j = lane >> 4;
-            tma_gather4<CG>(da + j * 8192u + g * 512u, &maps.ag, x + 64 * j, ra[0], ra[1], ra[2], ra[3], bar);
-          }
-          if (!p.b_index && !tail) {
-            if (lane < nb) tma2<CG>(db + lane * 8192u, &maps.b, y + 64 * lane, tile.row0 + k0, bar);
-          } else {
-            const int g = lane & 15;
-            for (int j = lane >> 4; j < nb; j += 2)
-              tma_gather4<CG>(db + j * 8192u + g * 512u, &maps.bg, y + 64 * j, rb[0], rb[1], rb[2], rb[3], bar);
-          }
-          if (kb + 1 < tile.kblocks) look_up(k0 + kMmK);
-        } else {
-          if constexpr (FORM == kHead) {
-            tma_gather4<CG>(da + lane * 512u, &maps.ag, k0, rows_at[0][0], rows_at[0][1], rows_at[0][2], rows_at[0][3], bar);
-            if (lane < kHalf / 128)
-              tma2<CG>(db + lane * 16384u, &maps.b, k0, p.column0 + tile.n0 + (int)rank * half + 128 * lane, bar);
-          } else {
+        if (elect_one()) {
+          if (rank == 0) mbar_arrive_expect_tx(bar, here ? (for_a ? (uint32_t)kMmA : nb * box) * CG : 0u);
+          if (here && for_a) {
             if constexpr (FORM == kRows) {
-              if (lane == 0) tma3<CG>(da, &maps.a, k0, m0, tile.e, bar);
+              tma3<CG>(da, &maps.a, k0, m0, tile.e, bar);
             } else if constexpr (FORM == kSwiglu) {
-              if (lane == 0) tma5<CG>(da, &maps.a, k0, 0, 0, m0 / 16, tile.e, bar);
-            } else {
-              if (lane < 2) tma3<CG>(da + lane * 8192u, &maps.a, m0 + 64 * lane, k0, tile.e, bar);
+              tma5<CG>(da, &maps.a, k0, 0, 0, m0 / 16, tile.e, bar);
+            } else if constexpr (FORM == kRowsT) {
+              tma3<CG>(da, &maps.a, m0, k0, tile.e, bar);
+              tma3<CG>(da + 8192u, &maps.a, m0 + 64, k0, tile.e, bar);
+            } else if constexpr (FORM == kOuter) {
+              tma2<CG>(da, &maps.a, m0, tile.row0 + k0, bar);
+              tma2<CG>(da + 8192u, &maps.a, m0 + 64, tile.row0 + k0, bar);
             }
-            if (gathered) {
+          }
+          if (here && for_b) {
+            if constexpr (FORM == kOuter) {
+              for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 8192u, &maps.b, n0 + 64 * j, tile.row0 + k0, bar);
+            } else if constexpr (FORM == kHead) {
 #pragma unroll
-              for (int j = 0; j < kIdx; ++j)
-                if (128 * j + 4 * lane < half)
-                  tma_gather4<CG>(db + j * 16384u + lane * 512u, &maps.bg, k0, rows_at[j][0], rows_at[j][1], rows_at[j][2],
-                                  rows_at[j][3], bar);
-            } else if (32 * lane < half) {
-              tma2<CG>(db + lane * 4096u, &maps.b, k0, tile.n0 + (int)rank * half + 32 * lane, bar);
+              for (int j = 0; j < kHalf / 128; ++j) tma2<CG>(db + j * 16384u, &maps.b, k0, p.column0 + n0 + 128 * j, bar);
+            } else if (big) {
+              for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 16384u, &maps.b, k0, n0 + 128 * j, bar);
+            } else {
+              for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 4096u, &maps.b_few, k0, n0 + 32 * j, bar);
             }
           }
         }
@@ -497,7 +530,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         if (++slot == STAGES) { slot = 0; phase ^= 1u; }
       }
     }
-    if (rank == 0 && lane == 0 && *abort_flag) {
+    if (rank == 0 && warp == 4 && lane == 0 && *abort_flag) {
       // something gave up: no copy may still be landing when the shared memory is released
       const uint32_t back = issued < STAGES ? issued : STAGES;
       for (uint32_t k = 1; k <= back; ++k) {
@@ -506,14 +539,116 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
           if (mbar_try_wait(smem_u32(&s->full[j % STAGES]), (j / STAGES) & 1u)) break;
       }
     }
+  } else if (GATHER && warp >= kFirstGather) {
+    // ----------------------------------------------------------------------------------------------- gathered rows
+    // Each of the four warps does every fourth stage by itself: its fixed costs (waiting for the slot, for the pieces to land,
+    // making them visible to the tensor core) are spread over the time of four stages.  Eight lanes bring 128 bytes of a row,
+    // the warp four rows at a time: row 4 i + lane / 8; lane l looks up rows l, l + 32, ...
+    const int g = warp - kFirstGather, sub = lane >> 3, piece = lane & 7;
+    // where row 4 i + sub's piece goes: rows of one i parity share their place in the swizzle
+    const uint32_t place[2] = {(uint32_t)(sub * 128 + ((piece ^ sub) << 4)), (uint32_t)(sub * 128 + ((piece ^ (4 + sub)) << 4))};
+    uint32_t base = 0;              // stages in front of the tile
+    bool alive = true;
+    for (int t = unit; t < total && alive; t += n_units) {
+      const MmTile tile = schedule.get(t).uniform_copy();
+      const int half = mm_width<CG>(tile.ncols) / CG, m0 = tile.m0 + (int)rank * 128;
+      const int n0 = tile.n0 + (int)rank * half;
+      constexpr int kRegs = FORM == kHead ? 4 : FORM == kOuter ? 2 : (kHalf + 31) / 32;
+      int row_a[FORM == kOuter ? 2 : 1], row_b[kRegs];
+      const int here = FORM == kHead ? min(128, tile.rows - m0) : min(half, tile.ncols - (int)rank * half);  // rows as lanes / columns
+      if constexpr (FORM != kOuter) {
+        const int32_t* index = FORM == kHead ? p.a_index + m0 : p.b_index + n0;
+#pragma unroll
+        for (int j = 0; j < kRegs; ++j) row_b[j] = 32 * j + lane < here ? __ldg(index + 32 * j + lane) : -1;
+#pragma unroll
+        for (int j = 0; j < kRegs; ++j)
+          if (32 * j + lane < here)
+            row_b[j] = FORM == kHead ? mm_row(row_b[j], MmDiv{0u, 0u}, p.a_rows, p.dev_status)
+                                     : mm_row(row_b[j], p.b_div, p.b_rows, p.dev_status);
+      }
+      // (products over rows: the rows of the warp's next stage are looked up a turn ahead)
+      auto ask = [&](int k0) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = k0 + 32 * j + lane;
+          const bool in = r < tile.rows;
+          row_a[FORM == kOuter ? j : 0] = !in ? -1 : p.a_index ? __ldg(p.a_index + tile.row0 + r) : tile.row0 + r;
+          row_b[j] = !in ? -1 : p.b_index ? __ldg(p.b_index + tile.row0 + r) : tile.row0 + r;
+        }
+      };
+      const int first = (int)((uint32_t)(g - (int)base) & 3u);
+      if constexpr (FORM == kOuter) ask(first * kMmK);
+      for (int kb = first; kb < tile.kblocks; kb += 4) {
+        const int k0 = kb * kMmK;
+        const uint32_t n = base + (uint32_t)kb, slot = n % STAGES, phase = (n / STAGES) & 1u;
+        if (!mbar_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
+        const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
+        if constexpr (FORM == kOuter) {
+          static_assert(FORM != kOuter || kHalf == 128);
+          const bool tail = tile.rows - k0 < kMmK;
+          const bool do_a = p.a_index || tail, do_b = p.b_index || tail;
+          if (do_a || do_b) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              if (row_a[j] >= 0 && p.a_index) row_a[j] = mm_row(row_a[j], p.a_div, p.a_rows, p.dev_status);
+              if (row_b[j] >= 0 && p.b_index) row_b[j] = mm_row(row_b[j], p.b_div, p.b_rows, p.dev_status);
+            }
+            auto copy_block = [&](uint32_t dst, const void* src, int64_t ld, int x0, int width, int boxes, const int (&rows)[2]) {
+              // columns x0 + 64 b + 8 piece of the matrix: inside it, or zeros
+              const unsigned char* from = reinterpret_cast<const unsigned char*>(src) + 2 * (int64_t)(x0 + 8 * piece);
+              const bool in0 = x0 + 8 * piece < width, in1 = x0 + 64 + 8 * piece < width;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int r = __shfl_sync(0xffffffffu, rows[i >> 3], (4 * i + sub) & 31);
+                const unsigned char* at = from + (int64_t)max(r, 0) * (2 * ld);
+                const uint32_t to = dst + place[i & 1] + i * 512u;
+                copy16(to, r >= 0 && in0 ? at : reinterpret_cast<const unsigned char*>(src), r >= 0 && in0 ? 16u : 0u);
+                if (boxes > 1)
+                  copy16(to + 8192u, r >= 0 && in1 ? at + 128 : reinterpret_cast<const unsigned char*>(src),
+                         r >= 0 && in1 ? 16u : 0u);
+              }
+            };
+            if (do_a) copy_block(da, p.a_src, p.a_ld, m0, p.lanes, 2, row_a);
+            if (do_b) copy_block(db, p.b_src, p.b_ld, n0, p.columns, (half + 63) / 64, reinterpret_cast<int(&)[2]>(row_b));
+          }
+          ask(k0 + 4 * kMmK);
+        } else {
+          // (rows that do not exist are left as they are: they only ever meet lanes or columns that do not exist either)
+          const bool in = k0 + 8 * piece < p.kdim;
+          const unsigned char* src = reinterpret_cast<const unsigned char*>(FORM == kHead ? p.a_src : p.b_src);
+          const unsigned char* from = src + 2 * (in ? k0 + 8 * piece : 0);
+          const int64_t ld = 2 * (FORM == kHead ? p.a_ld : p.b_ld);
+          const uint32_t dst = FORM == kHead ? da : db;
+#pragma unroll
+          for (int j = 0; j < kRegs; ++j) {
+            if (32 * j < here) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int r = __shfl_sync(0xffffffffu, row_b[j], 4 * i + sub);
+                copy16(dst + place[i & 1] + j * 4096u + i * 512u, from + (int64_t)max(r, 0) * ld, r >= 0 && in ? 16u : 0u);
+              }
+            }
+          }
+        }
+        asm volatile("cp.async.wait_all;\n\tfence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (CG == 2) arrive_at_first(smem_u32(&s->full[slot]));
+          else mbar_arrive(smem_u32(&s->full[slot]));
+        }
+      }
+      base += (uint32_t)tile.kblocks;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == 5) {
     // ---------------------------------------------------------------------------------------------------- products
-    if (rank == 0 && lane == 0) {
+    if (rank == 0) {
       uint32_t slot = 0, phase = 0;
       int turn = 0;
       bool alive = true;
+      const uint32_t ring_a = mm_desc_lo(smem_u32(ring), A_MN), ring_b = mm_desc_lo(smem_u32(ring) + kMmA, B_MN);
       for (int t = unit; t < total && alive; t += n_units) {
-        const MmTile tile = schedule.get(t);
+        const MmTile tile = schedule.get(t).uniform_copy();
         if (tile.kblocks == 0) continue;
         const uint32_t idesc = mm_idesc(A_MN, B_MN, 128 * CG, mm_width<CG>(tile.ncols));
         const int buf = turn & 1;
@@ -521,39 +656,41 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)buf * kAccCols;
         for (int kb = 0; kb < tile.kblocks; ++kb) {
-          if (!mbar_wait(smem_u32(&s->full[slot]), phase, abort_flag, p.wait_limit)) { alive = false; break; }
-          tc_fence_after();
-          const uint32_t at = smem_u32(ring + (size_t)slot * kStage);
-          const uint64_t a = mm_desc(at, A_MN), b = mm_desc(at + kMmA, B_MN);
+          if (!(CG == 2 ? pair_wait(smem_u32(&s->full[slot]), phase, abort_flag, p.wait_limit)
+                        : mbar_wait(smem_u32(&s->full[slot]), phase, abort_flag, p.wait_limit))) { alive = false; break; }
+          // (no tcgen05 fence: the stage was written in, or made visible to, the tensor core's proxy; a fence drains the pipe)
+          const uint32_t a = ring_a + slot * (uint32_t)(kStage >> 4), b = ring_b + slot * (uint32_t)(kStage >> 4);
+          if (elect_one()) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            mm_mma<CG>(d, a + (uint64_t)(i * (A_MN ? 128 : 2)), b + (uint64_t)(i * (B_MN ? 128 : 2)), idesc,
-                       (kb | i) != 0 ? 1u : 0u);
-          mm_commit<CG>(smem_u32(&s->empty[slot]));
+            for (int i = 0; i < 4; ++i)
+              mm_mma<CG>(d, a + (uint32_t)(i * (A_MN ? 128 : 2)), b + (uint32_t)(i * (B_MN ? 128 : 2)), idesc,
+                         (kb | i) != 0 ? 1u : 0u);
+            mm_commit<CG>(smem_u32(&s->empty[slot]));
+            if (kb + 1 == tile.kblocks) mm_commit<CG>(smem_u32(&s->acc_full[buf]));
+          }
+          __syncwarp();
           if (++slot == STAGES) { slot = 0; phase ^= 1u; }
         }
         if (!alive) break;
-        mm_commit<CG>(smem_u32(&s->acc_full[buf]));
         ++turn;
       }
-      if (*abort_flag) {
+      if (*abort_flag && lane == 0) {
         mm_commit<CG>(smem_u32(&s->drained));
         for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
           if (mbar_try_wait(smem_u32(&s->drained), 0)) break;
       }
     }
-  } else {
+  } else if (warp < 4) {
     // ---------------------------------------------------------------------------------------------- finished tiles
-    Epilogue epi(p, lane);
+    Epilogue epi(p, lane, smem_u32(staging) + (uint32_t)warp * Epilogue::kStaging);
     int turn = 0;
     for (int t = unit; t < total; t += n_units) {
       const MmTile tile = schedule.get(t);
       const int lane0 = tile.m0 + (int)rank * 128 + 32 * warp;      // index of the warp's first lane
-      epi.begin(tile, lane0, (int)rank * 4 + warp);
+      epi.begin(tile, lane0);
+      typename Epilogue::Values v;
       if (tile.kblocks == 0) {                                       // (an empty group's product over its rows)
-        float v[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+        epi.zero(v);
         for (int c = 0; c < tile.ncols; c += 32) epi.chunk(tile, lane0, c, v);
         continue;
       }
@@ -562,8 +699,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       tc_fence_after();
       const uint32_t base = tmem + ((uint32_t)(32 * warp) << 16) + (uint32_t)buf * kAccCols;
       for (int c = 0; c < tile.ncols; c += 32) {
-        float v[32];
-        mm_ld32(base + (uint32_t)c, v);
+        epi.load(base + (uint32_t)c, v);
         if (c + 32 >= tile.ncols) {     // the accumulator may be written again
           tc_fence_before();
           __syncwarp();
@@ -574,7 +710,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         }
         epi.chunk(tile, lane0, c, v);
       }
-      epi.end(tile, lane0, t);
+      epi.end(tile);
       ++turn;
     }
   }
@@ -587,23 +723,25 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   if (warp == 5) mm_tmem_free<CG>(tmem, kTmemCols);
 }
 
-template <int CG, int BN, int STAGES>
+template <int CG, int BN, int STAGES, class Epilogue>
 constexpr size_t mm_smem() {
   constexpr int half = BN / CG < 32 ? 32 : BN / CG;
-  return 1024 + (size_t)STAGES * (kMmA + half * kMmK * 2) + sizeof(MmShared);
+  return 1024 + (size_t)STAGES * (kMmA + half * kMmK * 2) + (sizeof(MmShared) + 127) / 128 * 128 + 4 * Epilogue::kStaging;
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
-template <int FORM, int CG, int BN, int STAGES, class Epilogue>
+template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
 cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long long max_tiles, cudaStream_t st) {
-  auto kernel = dx_mm_kernel<FORM, CG, BN, STAGES, Epilogue>;
-  constexpr size_t smem = mm_smem<CG, BN, STAGES>();
+  auto kernel = dx_mm_kernel<FORM, GATHER, CG, BN, STAGES, Epilogue>;
+  constexpr size_t smem = mm_smem<CG, BN, STAGES, Epilogue>();
+  static_assert(smem <= 227 * 1024);
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   long long units = ctx->sm_count / CG;
   if (max_tiles < units) units = max_tiles;
   if (units < 1) units = 1;
-  return dx_launch_pdl(false, kernel, dim3((unsigned)(units * CG)), dim3(kMmThreads), smem, st, CG, maps, p);
+  return dx_launch_pdl(false, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(FORM, GATHER)), smem,
+                       st, CG, maps, p);
 }
 
 }  // namespace
