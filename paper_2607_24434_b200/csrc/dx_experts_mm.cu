@@ -10,7 +10,7 @@
 namespace {
 
 // ---- out of tensor memory ------------------------------------------------------------------------------------------
-// A warp turns 32 lanes x 32 columns around in shared memory: fragments as the tensor memory gives them (mm_ld_frag),
+// A warp turns 32 lanes x 32 (16) columns around in shared memory: fragments as the tensor memory gives them (mm_ld_frag),
 // rounded and stored as transposed 8 x 8 matrices -- a column's lanes next to each other -- and read back in 16-byte pieces, so
 // that global memory sees 64 or 128 neighbouring bytes per row.  About 60 instructions for 1024 elements; exchanging them by
 // shuffles took over 200, and the four storing warps, not the products, were what a tile waited for.
@@ -23,75 +23,82 @@ __device__ __forceinline__ uint32_t piece64(int column, int piece) {
 __device__ __forceinline__ void stage64(uint32_t at, int lane, int n, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   stmatrix_t(at + piece64(8 * n + (lane & 7), lane >> 3), a, b, c, d);
 }
-__device__ __forceinline__ void stage_bf16(uint32_t at, int lane, const float (&v)[2][16]) {
+template <int COLS>
+__device__ __forceinline__ void stage_bf16(uint32_t at, int lane, const Fragments<COLS>& x) {
 #pragma unroll
-  for (int n = 0; n < 4; ++n)
-    stage64(at, lane, n, bf16_pair(v[0][4 * n], v[0][4 * n + 1]), bf16_pair(v[0][4 * n + 2], v[0][4 * n + 3]),
-            bf16_pair(v[1][4 * n], v[1][4 * n + 1]), bf16_pair(v[1][4 * n + 2], v[1][4 * n + 3]));
+  for (int n = 0; n < COLS / 8; ++n)
+    stage64(at, lane, n, bf16_pair(x.v[0][4 * n], x.v[0][4 * n + 1]), bf16_pair(x.v[0][4 * n + 2], x.v[0][4 * n + 3]),
+            bf16_pair(x.v[1][4 * n], x.v[1][4 * n + 1]), bf16_pair(x.v[1][4 * n + 2], x.v[1][4 * n + 3]));
 }
 // fp32: 144 bytes per column
 constexpr int kColumn32 = 144;
-__device__ __forceinline__ void stage_fp32(uint32_t at, int lane, const float (&v)[2][16]) {
+template <int COLS>
+__device__ __forceinline__ void stage_fp32(uint32_t at, int lane, const Fragments<COLS>& x) {
   const uint32_t mine = at + (uint32_t)(2 * (lane & 3) * kColumn32 + (lane >> 2) * 4);
 #pragma unroll
-  for (int n = 0; n < 4; ++n)
+  for (int n = 0; n < COLS / 8; ++n)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        sts4(mine + (uint32_t)((8 * n + (q & 1)) * kColumn32 + (16 * h + 8 * (q >> 1)) * 4), v[h][4 * n + q]);
+        sts4(mine + (uint32_t)((8 * n + (q & 1)) * kColumn32 + (16 * h + 8 * (q >> 1)) * 4), x.v[h][4 * n + q]);
 }
 
 // sorted row of a chunk's column `c0 + lane` (-1: none), and the row of the output it goes to
 __device__ __forceinline__ int sorted_row(const MmTile& t, int c0, int lane) {
   return c0 + lane < t.ncols ? t.n0 + c0 + lane : -1;
 }
-__device__ __forceinline__ int scattered(const MmParams& p, int row) {
-  if (row < 0 || !p.scatter) return row;
+template <int COLS>
+__device__ __forceinline__ int scattered(const MmParams& p, int row, int lane) {
+  if (row < 0 || !p.scatter || lane >= COLS) return row;
   const int to = __ldg(p.scatter + row);
   if (to >= 0 && to < p.out_rows) return to;
   atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
   return -1;
 }
 
-struct Fragments {
-  float v[2][16];
-};
+template <int COLS>
 struct FragmentEpilogue {
-  using Values = Fragments;
+  static constexpr int kCols = COLS;
+  using Values = Fragments<COLS>;
   const MmParams& p;
   const int lane;
   const uint32_t at;       // the warp's staging
-  __device__ FragmentEpilogue(const MmParams& p_, int lane_, uint32_t at_) : p(p_), lane(lane_), at(at_) {}
-  __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld_frag(taddr, x.v); }
+  __device__ FragmentEpilogue(const MmParams& p_, int lane_, int, uint32_t at_) : p(p_), lane(lane_), at(at_) {}
+  __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld_frag(taddr, x); }
   __device__ __forceinline__ void zero(Values& x) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x.v[0][i] = x.v[1][i] = 0.0f;
+    for (int i = 0; i < COLS / 2; ++i) x.v[0][i] = x.v[1][i] = 0.0f;
   }
-  __device__ __forceinline__ void begin(const MmTile&, int) {}
+  __device__ __forceinline__ void begin(const MmTile&, int, int) {}
   __device__ __forceinline__ void end(const MmTile&) {}
 };
 
-// The chunk's 32 columns are rows `mine` (of lane = column) of a matrix; m: first of the warp's 32 elements in a row.
-template <class T, bool ADD>
-__device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_t at, const float (&v)[2][16], int mine, int m,
+// Staged columns (bf16) to rows `mine` (of lane = column) of a matrix; m: first of the warp's 32 elements in a row.
+template <int COLS>
+__device__ __forceinline__ void flush_bf16(const MmParams& p, int lane, uint32_t at, int mine, int m, __nv_bfloat16* out,
+                                           int64_t ld) {
+  const int piece = lane & 3, x = m + 8 * piece;
+#pragma unroll
+  for (int i = 0; i < COLS / 8; ++i) {
+    const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
+    const uint4 u = lds16(at + piece64(column, piece));
+    if (row >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(out + (int64_t)row * ld + x) = u;
+  }
+}
+template <class T, bool ADD, int COLS>
+__device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_t at, const Fragments<COLS>& v, int mine, int m,
                                             T* out, int64_t ld) {
   if constexpr (sizeof(T) == 2 && !ADD) {
     stage_bf16(at, lane, v);
     __syncwarp();
-    const int piece = lane & 3, x = m + 8 * piece;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
-      const uint4 u = lds16(at + piece64(column, piece));
-      if (row >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(out + (int64_t)row * ld + x) = u;
-    }
+    flush_bf16<COLS>(p, lane, at, mine, m, out, ld);
   } else if constexpr (sizeof(T) == 4) {
     stage_fp32(at, lane, v);
     __syncwarp();
     const int x = m + 4 * (lane & 7);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < COLS / 4; ++i) {
       const int column = 4 * i + (lane >> 3), row = __shfl_sync(0xffffffffu, mine, column);
       const uint4 u = lds16(at + (uint32_t)(column * kColumn32 + (lane & 7) * 16));
       if (row >= 0 && x < p.lanes) {
@@ -108,7 +115,7 @@ __device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_
     __syncwarp();
     const int x = m + 8 * (lane & 3);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < COLS / 8; ++i) {
       const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
       const uint32_t src = at + (uint32_t)(column * kColumn32 + (lane & 3) * 32);
       const uint4 u = lds16(src), w = lds16(src + 16);
@@ -125,35 +132,41 @@ __device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_
   }
   __syncwarp();      // (the staging is written again)
 }
+template <class T, bool ADD>
+constexpr int store_cols() { return sizeof(T) == 2 && !ADD ? 32 : 16; }
+template <class T, bool ADD>
+constexpr int store_staging() { return sizeof(T) == 2 && !ADD ? 32 * 64 : 16 * kColumn32; }
 
 // out[row of the column][lane] = D (+ addend), rounded once
 template <class T, bool ADD>
-struct StoreRows : FragmentEpilogue {
-  static constexpr int kStaging = sizeof(T) == 2 && !ADD ? 32 * 64 : 32 * kColumn32;
-  using FragmentEpilogue::FragmentEpilogue;
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
-    const int mine = scattered(p, sorted_row(t, c0, lane));
-    store_chunk<T, ADD>(p, lane, at, x.v, mine, lane0, reinterpret_cast<T*>(p.out), p.ld);
+struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
+  using Base = FragmentEpilogue<store_cols<T, ADD>()>;
+  static constexpr int kStaging = store_staging<T, ADD>();
+  using Base::Base;
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x) {
+    const int mine = scattered<Base::kCols>(this->p, sorted_row(t, c0, this->lane), this->lane);
+    store_chunk<T, ADD>(this->p, this->lane, this->at, x, mine, lane0, reinterpret_cast<T*>(this->p.out), this->p.ld);
   }
 };
 
 // out of group e: [columns][lanes], element (n, m) = D
 template <class T>
-struct StoreOuter : FragmentEpilogue {
-  static constexpr int kStaging = sizeof(T) == 2 ? 32 * 64 : 32 * kColumn32;
-  using FragmentEpilogue::FragmentEpilogue;
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
-    store_chunk<T, false>(p, lane, at, x.v, sorted_row(t, c0, lane), lane0,
-                          reinterpret_cast<T*>(p.out) + (int64_t)t.e * p.group_stride, p.ld);
+struct StoreOuter : FragmentEpilogue<store_cols<T, false>()> {
+  using Base = FragmentEpilogue<store_cols<T, false>()>;
+  static constexpr int kStaging = store_staging<T, false>();
+  using Base::Base;
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x) {
+    store_chunk<T, false>(this->p, this->lane, this->at, x, sorted_row(t, c0, this->lane), lane0,
+                          reinterpret_cast<T*>(this->p.out) + (int64_t)t.e * this->p.group_stride, this->p.ld);
   }
 };
 
 // act = silu(gate) * up from the fp32 products; SAVE: the products themselves, rounded once, for the backward pass.
 // Of 16 lanes the first eight are gate rows, the others the same eight up rows: a thread holds both of an element.
 template <bool SAVE>
-struct StoreSwiglu : FragmentEpilogue {
+struct StoreSwiglu : FragmentEpilogue<32> {
   static constexpr int kStaging = 32 * 64;
-  using FragmentEpilogue::FragmentEpilogue;
+  using FragmentEpilogue<32>::FragmentEpilogue;
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
     const float(&v)[2][16] = x.v;
     const int n_inter = p.lanes >> 1, i0 = lane0 >> 1;      // the warp's 16 elements
@@ -179,7 +192,8 @@ struct StoreSwiglu : FragmentEpilogue {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int n = 0; n < 4; ++n)
-        a[h][n] = bf16_pair(fast_silu(v[h][4 * n]) * v[h][4 * n + 2], fast_silu(v[h][4 * n + 1]) * v[h][4 * n + 3]);
+        a[h][n] = bf16_pair(v[h][4 * n] * sigmoid(v[h][4 * n]) * v[h][4 * n + 2],
+                            v[h][4 * n + 1] * sigmoid(v[h][4 * n + 1]) * v[h][4 * n + 3]);
     // 32 bytes per column; matrices: (eight lanes h, eight columns n)
 #pragma unroll
     for (int n = 0; n < 4; n += 2) {
@@ -201,96 +215,100 @@ struct StoreSwiglu : FragmentEpilogue {
 
 // D = W_down^T dy = the gradient of an unweighted act.  With q the row's pair, w its weight, s = sigmoid(gate):
 //   d gate = w D up s (1 + gate (1 - s)),  d up = w D gate s,  act_w = w gate s up,  share of d w = sum over lanes of D gate s up.
-// A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come in 16-byte pieces, a chunk ahead.
-struct StoreSwigluGrad : FragmentEpilogue {
-  static constexpr int kStaging = 2 * 32 * 64;
-  uint4 gate[4], up[4];
-  __device__ StoreSwigluGrad(const MmParams& p_, int lane_, uint32_t at_) : FragmentEpilogue(p_, lane_, at_) {}
+// A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come in 16-byte pieces, a chunk ahead; their
+// place in the staging takes the gradients.
+struct StoreSwigluGrad : FragmentEpilogue<16> {
+  static constexpr int kArea = 16 * 64, kStaging = 3 * kArea;
+  uint4 gate[2], up[2];
+  float weight;      // of column `lane`
+  __device__ StoreSwigluGrad(const MmParams& p_, int lane_, int share_, uint32_t at_)
+      : FragmentEpilogue<16>(p_, lane_, share_, at_) {}
   __device__ __forceinline__ void fetch(const MmTile& t, int lane0, int c0) {
     const int x = lane0 + 8 * (lane & 3);
     const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.gate_up) +
                                (int64_t)(t.n0 + c0 + (lane >> 2)) * p.ld_gate_up + x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const bool in = c0 + 8 * i + (lane >> 2) < t.ncols && x < p.lanes;
       const uint4* g = reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * p.ld_gate_up);
       gate[i] = in ? __ldcs(g) : make_uint4(0u, 0u, 0u, 0u);
       up[i] = in ? __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * p.ld_gate_up + p.lanes)) : make_uint4(0u, 0u, 0u, 0u);
     }
-  }
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0) { fetch(t, lane0, 0); }
-  __device__ __forceinline__ void out(const uint32_t (&a)[4][4], int mine, int lane0, __nv_bfloat16* to, int64_t ld) {
-#pragma unroll
-    for (int n = 0; n < 4; ++n) stage64(at, lane, n, a[n][0], a[n][1], a[n][2], a[n][3]);
-    __syncwarp();
-    const int piece = lane & 3, x = lane0 + 8 * piece;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
-      const uint4 u = lds16(at + piece64(column, piece));
-      if (row >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(to + (int64_t)row * ld + x) = u;
-    }
-    __syncwarp();
-  }
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
-    const int mine = sorted_row(t, c0, lane);
-    float weight = 0.0f;
+    const int mine = lane < 16 ? sorted_row(t, c0, lane) : -1;
+    weight = 0.0f;
     if (mine >= 0) {
       const int q = p.b_index ? __ldg(p.b_index + mine) : mine;
       if (q >= 0 && q < p.n_pairs) weight = p.pair_w ? __ldg(p.pair_w + q) : 1.0f;
       else atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
     }
+  }
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int c0) {
+    if (c0 < t.ncols) fetch(t, lane0, c0);
+  }
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
+    const int mine = sorted_row(t, c0, lane);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int column = 8 * i + (lane >> 2);
-      sts16(at + piece64(column, lane & 3), gate[i]);
-      sts16(at + 2048u + piece64(column, lane & 3), up[i]);
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t to = at + piece64(8 * i + (lane >> 2), lane & 3);
+      sts16(to, gate[i]);
+      sts16(to + kArea, up[i]);
     }
     __syncwarp();
-    if (c0 + 32 < t.ncols) fetch(t, lane0, c0 + 32);
-    uint32_t dg[4][4], du[4][4], aw[4][4];
-    float dw[8];
+    uint32_t g4[2][4], u4[2][4], a4[2][4], mask[2];
+    F2 w[2], dw2[2];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < 2; ++n) {
       const uint32_t from = at + piece64(8 * n + (lane & 7), lane >> 3);
-      uint32_t g4[4], u4[4];
-      ldmatrix_t(from, g4);
-      ldmatrix_t(from + 2048u, u4);
-      const float w2[2] = {__shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3)),
-                           __shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3) + 1)};
-      dw[2 * n] = dw[2 * n + 1] = 0.0f;
+      ldmatrix_t(from, g4[n]);
+      ldmatrix_t(from + kArea, u4[n]);
+      const float w0 = __shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3));
+      const float w1 = __shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3) + 1);
+      w[n] = f2(w0, w1);
+      mask[n] = (w0 != 0.0f ? 0xffffu : 0u) | (w1 != 0.0f ? 0xffff0000u : 0u);
+      dw2[n] = f2(0.0f, 0.0f);
+    }
+    __syncwarp();
+    if (c0 + 2 * kCols < t.ncols) fetch(t, lane0, c0 + 2 * kCols);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {       // eight lanes from 8 j
-        const float2 g2 = bf16_unpair(g4[j]), u2 = bf16_unpair(u4[j]);
-        const float g[2] = {g2.x, g2.y}, u[2] = {u2.x, u2.y};
-        float a[3][2];
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float d1 = x.v[j >> 1][4 * n + 2 * (j & 1) + i];
-          const float e = __expf(-fabsf(g[i])), r = __fdividef(1.0f, 1.0f + e);      // sigmoid of either sign
-          const float sg = g[i] >= 0.0f ? r : e * r, not_sg = g[i] >= 0.0f ? e * r : r;
-          const float gs = g[i] * sg, act = gs * u[i], d = w2[i] * d1;
-          const bool on = w2[i] != 0.0f;
-          a[0][i] = on ? d * u[i] * fmaf(gs, not_sg, sg) : 0.0f;
-          a[1][i] = on ? d * gs : 0.0f;
-          a[2][i] = on ? w2[i] * act : 0.0f;
-          if (on && lane0 + 8 * j < p.lanes) dw[2 * n + i] = fmaf(d1, act, dw[2 * n + i]);
-        }
-        dg[n][j] = bf16_pair(a[0][0], a[0][1]);
-        du[n][j] = bf16_pair(a[1][0], a[1][1]);
-        aw[n][j] = bf16_pair(a[2][0], a[2][1]);
+      for (int j = 0; j < 4; ++j) {       // eight lanes from 8 j, two columns
+        const float2 g = bf16_unpair(g4[n][j]), u = bf16_unpair(u4[n][j]);
+        const F2 gg = f2(g.x, g.y), uu = f2(u.x, u.y);
+        const F2 d1 = f2(x.v[j >> 1][4 * n + 2 * (j & 1)], x.v[j >> 1][4 * n + 2 * (j & 1) + 1]);
+        const F2 one = f2(1.0f, 1.0f);
+        float e0, e1;
+        f2_get(f2_mul(gg, f2(-kLog2e, -kLog2e)), e0, e1);
+        f2_get(f2_add(f2(ex2(e0), ex2(e1)), one), e0, e1);
+        const F2 sg = f2(rcp(e0), rcp(e1)), gs = f2_mul(gg, sg);
+        const F2 slope = f2_fma(gs, f2_fma(sg, f2(-1.0f, -1.0f), one), sg);      // of silu: s + gate s (1 - s)
+        const F2 act = f2_mul(gs, uu), d = f2_mul(w[n], d1);
+        g4[n][j] = bf16_pair(f2_mul(f2_mul(d, uu), slope)) & mask[n];
+        u4[n][j] = bf16_pair(f2_mul(d, gs)) & mask[n];
+        a4[n][j] = bf16_pair(f2_mul(w[n], act)) & mask[n];
+        if (lane0 + 8 * j < p.lanes) dw2[n] = f2_fma(d1, act, dw2[n]);
       }
+    float dw[4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      f2_get(dw2[n], dw[2 * n], dw[2 * n + 1]);
+      if (!(mask[n] & 0xffffu)) dw[2 * n] = 0.0f;
+      if (!(mask[n] >> 16)) dw[2 * n + 1] = 0.0f;
+      stage64(at, lane, n, g4[n][0], g4[n][1], g4[n][2], g4[n][3]);
+      stage64(at + kArea, lane, n, u4[n][0], u4[n][1], u4[n][2], u4[n][3]);
+      stage64(at + 2 * kArea, lane, n, a4[n][0], a4[n][1], a4[n][2], a4[n][3]);
     }
     __syncwarp();
     __nv_bfloat16* d_gate_up = reinterpret_cast<__nv_bfloat16*>(p.out);
-    out(dg, mine, lane0, d_gate_up, p.ld);
-    out(du, mine, lane0, d_gate_up + p.lanes, p.ld);
-    out(aw, mine, lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
+    flush_bf16<16>(p, lane, at, mine, lane0, d_gate_up, p.ld);
+    flush_bf16<16>(p, lane, at + kArea, mine, lane0, d_gate_up + p.lanes, p.ld);
+    flush_bf16<16>(p, lane, at + 2 * kArea, mine, lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
+    __syncwarp();
     if (p.partial) {
-      // eight threads (t / 4) hold shares of the same columns 8 n + 2 (t % 4) + i: folded so that each ends with one column
+      // eight threads (t / 4) hold shares of the columns 8 n + 2 (t % 4) + i: folded so that two of them each end with one
 #pragma unroll
-      for (int b = 0; b < 3; ++b) {
-        const int h = 4 >> b, bit = 16 >> b;
+      for (int b = 0; b < 2; ++b) {
+        const int h = 2 >> b, bit = 16 >> b;
         const bool high = (lane & bit) != 0;
 #pragma unroll
         for (int j = 0; j < h; ++j) {
@@ -298,8 +316,9 @@ struct StoreSwigluGrad : FragmentEpilogue {
           dw[j] = (high ? dw[j + h] : dw[j]) + got;
         }
       }
-      const int k = lane >> 2, column = c0 + 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
-      if (column < t.ncols) p.partial[(int64_t)(lane0 >> 5) * p.n_rows + t.n0 + column] = dw[0];
+      dw[0] += __shfl_xor_sync(0xffffffffu, dw[0], 4);
+      const int k = lane >> 3, column = c0 + 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
+      if (!(lane & 4) && column < t.ncols) p.partial[(int64_t)(lane0 >> 5) * p.n_rows + t.n0 + column] = dw[0];
     }
   }
 };

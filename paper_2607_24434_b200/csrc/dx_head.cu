@@ -14,14 +14,6 @@
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // ---- 1: which rows count -------------------------------------------------------------------------------------------
 // One CTA; every turn takes 1024 rows.  live[i]: the i-th row that counts; rows that do not have loss 0 (a target outside the
 // vocabulary: NaN).
@@ -60,20 +52,20 @@ __global__ void __launch_bounds__(1024) dx_head_rows_kernel(const int32_t* targe
   }
 }
 
-// ---- 2: (maximum, sum) of a tile's columns, a row per thread ---------------------------------------------------------
+// ---- 2: (maximum, sum) of a half of a tile's columns (every other 32), a row per thread ---------------------------------------------------------
 struct RowSums {
   const MmParams& p;
-  const int lane;
+  const int lane, share;
   int row, target;
   float top, sum;
-  static constexpr int kStaging = 0;
+  static constexpr int kStaging = 0, kCols = 32;
   struct Values {
     float v[32];
   };
-  __device__ RowSums(const MmParams& p_, int lane_, uint32_t) : p(p_), lane(lane_) {}
+  __device__ RowSums(const MmParams& p_, int lane_, int share_, uint32_t) : p(p_), lane(lane_), share(share_) {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0) {
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
     target = row >= 0 ? __ldg(p.targets + __ldg(p.a_index + row)) - t.n0 : -1;   // (its place among the tile's columns)
     top = -INFINITY;
@@ -107,7 +99,7 @@ struct RowSums {
     top = m;
   }
   __device__ __forceinline__ void end(const MmTile& t) {
-    if (row >= 0) p.part[(int64_t)(t.n0 >> 8) * p.part_pitch + row] = make_float2(top, sum);
+    if (row >= 0) p.part[(int64_t)((t.n0 >> 8) * 2 + share) * p.part_pitch + row] = make_float2(top, sum);
   }
 };
 
@@ -161,17 +153,17 @@ __global__ void __launch_bounds__(256) dx_head_join_kernel(const float2* part, i
 // p - 1 at the target is -(1 - exp(-loss)): where the row is confident that is not the difference of two rounded numbers.
 struct StoreDz {
   const MmParams& p;
-  const int lane;
+  const int lane, share;
   int row, target;
   float lse, weight, at_target;
-  static constexpr int kStaging = 0;
+  static constexpr int kStaging = 0, kCols = 32;
   struct Values {
     float v[32];
   };
-  __device__ StoreDz(const MmParams& p_, int lane_, uint32_t) : p(p_), lane(lane_) {}
+  __device__ StoreDz(const MmParams& p_, int lane_, int share_, uint32_t) : p(p_), lane(lane_), share(share_) {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0) {
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
     target = -1;
     lse = weight = at_target = 0.0f;
@@ -233,7 +225,7 @@ HeadSpace head_space(int N, int V, int H, bool grad) {
   s.target_logit = take((size_t)N * 4);
   s.lse = take((size_t)N * 4);
   s.row_loss = take((size_t)N * 4);
-  s.part = take((size_t)((V + 255) / 256) * s.pitch * sizeof(float2));
+  s.part = take((size_t)((V + 255) / 256) * 2 * s.pitch * sizeof(float2));
   s.dh_acc = take(grad ? (size_t)N * H * 4 : 0);
   s.dz = at;
   s.fixed = at;
@@ -303,7 +295,7 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   if (e == cudaSuccess) { ++n; e = launch_head<RowSums>(ctx, m, p, st); }
   if (e == cudaSuccess) {
     ++n;
-    dx_head_join_kernel<<<(a.N + 31) / 32, 256, 0, st>>>(part, s.pitch, tiles, live, n_live + 1, target_logit, a.loss, lse,
+    dx_head_join_kernel<<<(a.N + 31) / 32, 256, 0, st>>>(part, s.pitch, 2 * tiles, live, n_live + 1, target_logit, a.loss, lse,
                                                          row_loss, a.targets, a.row_weight, a.N, a.V, a.H,
                                                          reinterpret_cast<__nv_bfloat16*>(a.dh), a.ld_dh);
     e = cudaGetLastError();

@@ -14,9 +14,9 @@
 // zeros.  (Tensor-map copies of four gathered rows took 85 to 120 clocks each, whoever issued them: 2.8 to 3.8 ms where rows
 // in place take 1.0 ms, 98304 rows x 2048 x 2816.)
 //
-// Warps: 0-3 take finished tiles out of tensor memory (lanes 32 w .. 32 w + 31), 4 asks for A and 6 for B (one warp where only
-// one operand comes by tensor map), 5 owns the tensor memory and issues the products (in a pair only the first CTA's); the last
-// four gather.  Two accumulators take turns, so a tile
+// Warps: 0-7 take finished tiles out of tensor memory (lanes 32 (w % 4) .. + 31, every other chunk of columns), 8 asks for A and
+// 10 for B (one of them where only one operand comes by tensor map), 9 owns the tensor memory and issues the products (in a pair
+// only the first CTA's), 12-15 gather.  Two accumulators take turns, so a tile
 // is stored while the next one is multiplied.  Every wait is bounded; one that runs out raises the CTA's abort flag,
 // after which nothing more is copied or multiplied, copies and products in flight are waited for (bounded), tensor
 // memory is freed and DX_DEV_WAIT_EXPIRED stands in the status word.
@@ -29,11 +29,9 @@
 
 namespace {
 
-__host__ __device__ constexpr bool mm_two_copiers(int form, bool gather);
-// four storing warps, one or two copying, one multiplying, four gathering
-__host__ __device__ constexpr int mm_threads(int form, bool gather) {
-  return 32 * (6 + (mm_two_copiers(form, gather) ? 1 : 0) + (gather ? 4 : 0));
-}
+constexpr int kMmStoring = 8;               // storing warps: two for each quarter of the tile's lanes, which share its columns
+enum { kWarpA = 8, kWarpMma = 9, kWarpB = 10, kWarpGather = 12 };
+__host__ __device__ constexpr int mm_threads(bool gather) { return gather ? 512 : 352; }
 constexpr int kMmK = 64;                    // contraction elements of a stage: 128 bytes of a row
 constexpr int kMmA = 128 * kMmK * 2;        // bytes of a CTA's 128 rows of A in a stage
 constexpr int kMmMaxStages = 8;
@@ -142,9 +140,13 @@ __device__ __forceinline__ void mm_ld32(uint32_t taddr, float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
-// The same 32 lanes x 32 columns in the fragments of an 8 x 8 matrix load: thread t holds, for the 16 lanes from 16 h and the
+// 32 lanes x 32 (16) columns in the fragments of an 8 x 8 matrix load: thread t holds, for the 16 lanes from 16 h and the
 // eight columns from 8 n, v[h][4 n + {0, 1}] = lane t / 4, columns 2 (t % 4) + {0, 1} and v[h][4 n + {2, 3}] = lane 8 + t / 4.
-__device__ __forceinline__ void mm_ld_frag(uint32_t taddr, float (&v)[2][16]) {
+template <int COLS>
+struct Fragments {
+  float v[2][COLS / 2];
+};
+__device__ __forceinline__ void mm_ld_frag(uint32_t taddr, Fragments<32>& x) {
   uint32_t r[2][16];
 #pragma unroll
   for (int h = 0; h < 2; ++h)
@@ -158,7 +160,21 @@ __device__ __forceinline__ void mm_ld_frag(uint32_t taddr, float (&v)[2][16]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[h][i] = __uint_as_float(r[h][i]);
+    for (int i = 0; i < 16; ++i) x.v[h][i] = __uint_as_float(r[h][i]);
+}
+__device__ __forceinline__ void mm_ld_frag(uint32_t taddr, Fragments<16>& x) {
+  uint32_t r[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[h][0]), "=r"(r[h][1]), "=r"(r[h][2]), "=r"(r[h][3]), "=r"(r[h][4]), "=r"(r[h][5]), "=r"(r[h][6]),
+                   "=r"(r[h][7])
+                 : "r"(taddr + (uint32_t)h * (16u << 16)));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.v[h][i] = __uint_as_float(r[h][i]);
 }
 // four 8 x 8 matrices of 16-bit elements, transposed: lanes 8 j .. 8 j + 7 name the rows of matrix j
 __device__ __forceinline__ void stmatrix_t(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -179,6 +195,48 @@ __device__ __forceinline__ void sts16(uint32_t at, uint4 v) {
 }
 __device__ __forceinline__ void sts4(uint32_t at, float v) {
   asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+// 1 / (1 + exp(-x)): good to a few 2^-22 of itself (the argument's rounding adds 2^-24 |x|), 0 below -87
+__device__ __forceinline__ float sigmoid(float x) { return rcp(1.0f + ex2(-kLog2e * x)); }
+// two fp32 operations in one instruction
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float x, float y) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void f2_get(F2 a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a)); }
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t bf16_pair(F2 a) {
+  float x, y;
+  f2_get(a, x, y);
+  const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&b);
 }
 __device__ __forceinline__ uint32_t bf16_pair(float x, float y) {   // rounded to nearest even
   const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
@@ -398,13 +456,12 @@ __device__ __forceinline__ int mm_row(int q, MmDiv div, int n_rows, int32_t* dev
 }
 
 template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
-__global__ void __launch_bounds__(mm_threads(FORM, GATHER), 1)
+__global__ void __launch_bounds__(mm_threads(GATHER), 1)
 dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmParams p) {
   constexpr int kHalf = BN / CG;                       // columns whose rows a CTA fetches
   constexpr int kB = (kHalf < 32 ? 32 : kHalf) * kMmK * 2;
   constexpr int kStage = kMmA + kB;
   constexpr bool A_MN = mm_a_mn(FORM), B_MN = mm_b_mn(FORM), kTwo = mm_two_copiers(FORM, GATHER);
-  constexpr int kFirstGather = kTwo ? 7 : 6;
   constexpr uint32_t kAccCols = BN < 32 ? 32 : BN, kTmemCols = 2 * kAccCols;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -423,7 +480,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&s->acc_full[i]), 1);
-      mbar_init(smem_u32(&s->acc_empty[i]), 4 * CG);
+      mbar_init(smem_u32(&s->acc_empty[i]), kMmStoring * CG);
     }
     mbar_init(smem_u32(&s->drained), 1);
     s->abort_flag = 0;
@@ -431,7 +488,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     if (FORM != kHead) tma_prefetch_map(&maps.a);
     if (!GATHER || FORM == kHead || FORM == kOuter) tma_prefetch_map(&maps.b);
   }
-  if (warp == 5) mm_tmem_alloc<CG>(smem_u32(&s->tmem_base), kTmemCols);
+  if (warp == kWarpMma) mm_tmem_alloc<CG>(smem_u32(&s->tmem_base), kTmemCols);
   dx_pdl_wait();
   // the groups: rows outside [0, n_rows) and ends in front of their beginnings are cut off and reported
   if (warp == 0) {
@@ -474,10 +531,10 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
                     : FORM == kHead ? schedule.m_tiles * schedule.n_tiles
                                     : s->before[p.n_groups] * schedule.m_tiles;
 
-  if (warp == 4 || (kTwo && warp == 6)) {
+  if (warp == kWarpA || (kTwo && warp == kWarpB)) {
     // ------------------------------------------------------------------------------------------------------ copies
-    // warp 4: A, or the only operand that comes by tensor map; warp 6: B
-    const bool for_a = FORM != kHead && warp == 4, for_b = FORM == kHead || warp == 6;
+    // (the one of them where only one operand comes by tensor map)
+    const bool for_a = FORM != kHead && warp == kWarpA, for_b = FORM == kHead || warp == kWarpB;
     uint32_t slot = 0, phase = 0, issued = 0;
     bool alive = true;
     for (int t = unit; t < total && alive; t += n_units) {
@@ -530,7 +587,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         if (++slot == STAGES) { slot = 0; phase ^= 1u; }
       }
     }
-    if (rank == 0 && warp == 4 && lane == 0 && *abort_flag) {
+    if (rank == 0 && warp == kWarpA && lane == 0 && *abort_flag) {
       // something gave up: no copy may still be landing when the shared memory is released
       const uint32_t back = issued < STAGES ? issued : STAGES;
       for (uint32_t k = 1; k <= back; ++k) {
@@ -539,14 +596,16 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
           if (mbar_try_wait(smem_u32(&s->full[j % STAGES]), (j / STAGES) & 1u)) break;
       }
     }
-  } else if (GATHER && warp >= kFirstGather) {
+  } else if (GATHER && warp >= kWarpGather) {
     // ----------------------------------------------------------------------------------------------- gathered rows
     // Each of the four warps does every fourth stage by itself: its fixed costs (waiting for the slot, for the pieces to land,
     // making them visible to the tensor core) are spread over the time of four stages.  Eight lanes bring 128 bytes of a row,
     // the warp four rows at a time: row 4 i + lane / 8; lane l looks up rows l, l + 32, ...
-    const int g = warp - kFirstGather, sub = lane >> 3, piece = lane & 7;
+    const int g = warp - kWarpGather, sub = lane >> 3, piece = lane & 7;
     // where row 4 i + sub's piece goes: rows of one i parity share their place in the swizzle
     const uint32_t place[2] = {(uint32_t)(sub * 128 + ((piece ^ sub) << 4)), (uint32_t)(sub * 128 + ((piece ^ (4 + sub)) << 4))};
+    // (what a copy of no bytes names as its source)
+    const unsigned char* zeros = reinterpret_cast<const unsigned char*>(FORM == kHead ? p.a_src : p.b_src);
     uint32_t base = 0;              // stages in front of the tile
     bool alive = true;
     for (int t = unit; t < total && alive; t += n_units) {
@@ -554,26 +613,50 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       const int half = mm_width<CG>(tile.ncols) / CG, m0 = tile.m0 + (int)rank * 128;
       const int n0 = tile.n0 + (int)rank * half;
       constexpr int kRegs = FORM == kHead ? 4 : FORM == kOuter ? 2 : (kHalf + 31) / 32;
-      int row_a[FORM == kOuter ? 2 : 1], row_b[kRegs];
       const int here = FORM == kHead ? min(128, tile.rows - m0) : min(half, tile.ncols - (int)rank * half);  // rows as lanes / columns
+      // what this lane has looked up: a row's place in its matrix, in pieces of 16 bytes, and which lanes' rows exist
+      uint32_t at_a[FORM == kOuter ? 2 : 1], at_b[kRegs], ok_a[FORM == kOuter ? 2 : 1], ok_b[kRegs];
+      auto resolve = [&](int q, bool in, bool indexed, MmDiv div, int n_rows, int64_t ld, uint32_t& at, uint32_t& ok) {
+        const int row = !in ? -1 : indexed ? mm_row(q, div, n_rows, p.dev_status) : q;
+        at = (uint32_t)max(row, 0) * (uint32_t)(ld >> 3);
+        ok = __ballot_sync(0xffffffffu, row >= 0);
+      };
+      // eight copies of four rows each: first where they come from, then the copies (one after the other they would wait for
+      // their own address every time)
+      auto copy_rows = [&](uint32_t dst, const unsigned char* from, uint32_t at, uint32_t ok, bool in, uint32_t offset) {
+        uint32_t src[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) src[i] = __shfl_sync(0xffffffffu, at, 4 * i + sub);
+        if (ok == 0xffffffffu && in) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) copy16(dst + place[i & 1] + i * 512u, from + (uint64_t)src[i] * 16u + offset, 16u);
+        } else {
+          const uint32_t mine = in ? ok >> sub : 0u;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            copy16(dst + place[i & 1] + i * 512u, (mine >> (4 * i)) & 1u ? from + (uint64_t)src[i] * 16u + offset : zeros,
+                   ((mine >> (4 * i)) & 1u) * 16u);
+        }
+      };
       if constexpr (FORM != kOuter) {
         const int32_t* index = FORM == kHead ? p.a_index + m0 : p.b_index + n0;
+        int q[kRegs];
 #pragma unroll
-        for (int j = 0; j < kRegs; ++j) row_b[j] = 32 * j + lane < here ? __ldg(index + 32 * j + lane) : -1;
+        for (int j = 0; j < kRegs; ++j) q[j] = 32 * j + lane < here ? __ldg(index + 32 * j + lane) : 0;
 #pragma unroll
         for (int j = 0; j < kRegs; ++j)
-          if (32 * j + lane < here)
-            row_b[j] = FORM == kHead ? mm_row(row_b[j], MmDiv{0u, 0u}, p.a_rows, p.dev_status)
-                                     : mm_row(row_b[j], p.b_div, p.b_rows, p.dev_status);
+          resolve(q[j], 32 * j + lane < here, true, FORM == kHead ? MmDiv{0u, 0u} : p.b_div, FORM == kHead ? p.a_rows : p.b_rows,
+                  FORM == kHead ? p.a_ld : p.b_ld, at_b[j], ok_b[j]);
       }
       // (products over rows: the rows of the warp's next stage are looked up a turn ahead)
+      int next_a[2], next_b[2];
       auto ask = [&](int k0) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int r = k0 + 32 * j + lane;
           const bool in = r < tile.rows;
-          row_a[FORM == kOuter ? j : 0] = !in ? -1 : p.a_index ? __ldg(p.a_index + tile.row0 + r) : tile.row0 + r;
-          row_b[j] = !in ? -1 : p.b_index ? __ldg(p.b_index + tile.row0 + r) : tile.row0 + r;
+          next_a[j] = in && p.a_index ? __ldg(p.a_index + tile.row0 + r) : tile.row0 + r;
+          next_b[j] = in && p.b_index ? __ldg(p.b_index + tile.row0 + r) : tile.row0 + r;
         }
       };
       const int first = (int)((uint32_t)(g - (int)base) & 3u);
@@ -581,54 +664,50 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       for (int kb = first; kb < tile.kblocks; kb += 4) {
         const int k0 = kb * kMmK;
         const uint32_t n = base + (uint32_t)kb, slot = n % STAGES, phase = (n / STAGES) & 1u;
+        const bool tail = FORM == kOuter && tile.rows - k0 < kMmK;
+        const bool do_a = FORM == kOuter && (p.a_index || tail), do_b = FORM == kOuter && (p.b_index || tail);
+        if constexpr (FORM == kOuter) {
+          if (do_a || do_b) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const bool in = k0 + 32 * j + lane < tile.rows;
+              resolve(next_a[j], in, p.a_index != nullptr, p.a_div, p.a_rows, p.a_ld, at_a[FORM == kOuter ? j : 0],
+                      ok_a[FORM == kOuter ? j : 0]);
+              resolve(next_b[j], in, p.b_index != nullptr, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
+            }
+            ask(k0 + 4 * kMmK);
+          }
+        }
         if (!mbar_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
         const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
         if constexpr (FORM == kOuter) {
           static_assert(FORM != kOuter || kHalf == 128);
-          const bool tail = tile.rows - k0 < kMmK;
-          const bool do_a = p.a_index || tail, do_b = p.b_index || tail;
-          if (do_a || do_b) {
+          // columns x0 + 64 b + 8 piece of a matrix: inside it, or zeros
+          if (do_a) {
+            const unsigned char* from = reinterpret_cast<const unsigned char*>(p.a_src) + 2 * (int64_t)(m0 + 8 * piece);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              if (row_a[j] >= 0 && p.a_index) row_a[j] = mm_row(row_a[j], p.a_div, p.a_rows, p.dev_status);
-              if (row_b[j] >= 0 && p.b_index) row_b[j] = mm_row(row_b[j], p.b_div, p.b_rows, p.dev_status);
+              copy_rows(da + j * 4096u, from, at_a[FORM == kOuter ? j : 0], ok_a[FORM == kOuter ? j : 0],
+                        m0 + 8 * piece < p.lanes, 0);
+              copy_rows(da + 8192u + j * 4096u, from, at_a[FORM == kOuter ? j : 0], ok_a[FORM == kOuter ? j : 0],
+                        m0 + 64 + 8 * piece < p.lanes, 128);
             }
-            auto copy_block = [&](uint32_t dst, const void* src, int64_t ld, int x0, int width, int boxes, const int (&rows)[2]) {
-              // columns x0 + 64 b + 8 piece of the matrix: inside it, or zeros
-              const unsigned char* from = reinterpret_cast<const unsigned char*>(src) + 2 * (int64_t)(x0 + 8 * piece);
-              const bool in0 = x0 + 8 * piece < width, in1 = x0 + 64 + 8 * piece < width;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int r = __shfl_sync(0xffffffffu, rows[i >> 3], (4 * i + sub) & 31);
-                const unsigned char* at = from + (int64_t)max(r, 0) * (2 * ld);
-                const uint32_t to = dst + place[i & 1] + i * 512u;
-                copy16(to, r >= 0 && in0 ? at : reinterpret_cast<const unsigned char*>(src), r >= 0 && in0 ? 16u : 0u);
-                if (boxes > 1)
-                  copy16(to + 8192u, r >= 0 && in1 ? at + 128 : reinterpret_cast<const unsigned char*>(src),
-                         r >= 0 && in1 ? 16u : 0u);
-              }
-            };
-            if (do_a) copy_block(da, p.a_src, p.a_ld, m0, p.lanes, 2, row_a);
-            if (do_b) copy_block(db, p.b_src, p.b_ld, n0, p.columns, (half + 63) / 64, reinterpret_cast<int(&)[2]>(row_b));
           }
-          ask(k0 + 4 * kMmK);
+          if (do_b) {
+            const unsigned char* from = reinterpret_cast<const unsigned char*>(p.b_src) + 2 * (int64_t)(n0 + 8 * piece);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              copy_rows(db + j * 4096u, from, at_b[j], ok_b[j], n0 + 8 * piece < p.columns, 0);
+              if (half > 64) copy_rows(db + 8192u + j * 4096u, from, at_b[j], ok_b[j], n0 + 64 + 8 * piece < p.columns, 128);
+            }
+          }
         } else {
-          // (rows that do not exist are left as they are: they only ever meet lanes or columns that do not exist either)
+          // (rows that do not exist come as zeros; they only ever meet lanes or columns that do not exist either)
           const bool in = k0 + 8 * piece < p.kdim;
-          const unsigned char* src = reinterpret_cast<const unsigned char*>(FORM == kHead ? p.a_src : p.b_src);
-          const unsigned char* from = src + 2 * (in ? k0 + 8 * piece : 0);
-          const int64_t ld = 2 * (FORM == kHead ? p.a_ld : p.b_ld);
-          const uint32_t dst = FORM == kHead ? da : db;
+          const unsigned char* from = zeros + 2 * (int64_t)(k0 + 8 * piece);
 #pragma unroll
-          for (int j = 0; j < kRegs; ++j) {
-            if (32 * j < here) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int r = __shfl_sync(0xffffffffu, row_b[j], 4 * i + sub);
-                copy16(dst + place[i & 1] + j * 4096u + i * 512u, from + (int64_t)max(r, 0) * ld, r >= 0 && in ? 16u : 0u);
-              }
-            }
-          }
+          for (int j = 0; j < kRegs; ++j)
+            if (32 * j < here) copy_rows((FORM == kHead ? da : db) + j * 4096u, from, at_b[j], ok_b[j], in, 0);
         }
         asm volatile("cp.async.wait_all;\n\tfence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -640,7 +719,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       base += (uint32_t)tile.kblocks;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-  } else if (warp == 5) {
+  } else if (warp == kWarpMma) {
     // ---------------------------------------------------------------------------------------------------- products
     if (rank == 0) {
       uint32_t slot = 0, phase = 0;
@@ -680,27 +759,30 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
           if (mbar_try_wait(smem_u32(&s->drained), 0)) break;
       }
     }
-  } else if (warp < 4) {
+  } else if (warp < kMmStoring) {
     // ---------------------------------------------------------------------------------------------- finished tiles
-    Epilogue epi(p, lane, smem_u32(staging) + (uint32_t)warp * Epilogue::kStaging);
+    constexpr int kCols = Epilogue::kCols;      // columns of a chunk
+    const int quarter = warp & 3, share = warp >> 2;
+    Epilogue epi(p, lane, share, smem_u32(staging) + (uint32_t)warp * Epilogue::kStaging);
     int turn = 0;
     for (int t = unit; t < total; t += n_units) {
       const MmTile tile = schedule.get(t);
-      const int lane0 = tile.m0 + (int)rank * 128 + 32 * warp;      // index of the warp's first lane
-      epi.begin(tile, lane0);
+      const int lane0 = tile.m0 + (int)rank * 128 + 32 * quarter;   // index of the warp's first lane
+      epi.begin(tile, lane0, kCols * share);
       typename Epilogue::Values v;
       if (tile.kblocks == 0) {                                       // (an empty group's product over its rows)
         epi.zero(v);
-        for (int c = 0; c < tile.ncols; c += 32) epi.chunk(tile, lane0, c, v);
+        for (int c = kCols * share; c < tile.ncols; c += 2 * kCols) epi.chunk(tile, lane0, c, v);
         continue;
       }
       const int buf = turn & 1;
       if (!mm_store_wait(smem_u32(&s->acc_full[buf]), (uint32_t)(turn >> 1) & 1u, abort_flag, p.wait_limit, lane)) break;
       tc_fence_after();
-      const uint32_t base = tmem + ((uint32_t)(32 * warp) << 16) + (uint32_t)buf * kAccCols;
-      for (int c = 0; c < tile.ncols; c += 32) {
-        epi.load(base + (uint32_t)c, v);
-        if (c + 32 >= tile.ncols) {     // the accumulator may be written again
+      const uint32_t base = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)buf * kAccCols;
+      int c = kCols * share;
+      do {
+        if (c < tile.ncols) epi.load(base + (uint32_t)c, v);
+        if (c + 2 * kCols >= tile.ncols) {     // the accumulator may be written again
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -708,8 +790,9 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             else mbar_arrive(smem_u32(&s->acc_empty[buf]));
           }
         }
-        epi.chunk(tile, lane0, c, v);
-      }
+        if (c < tile.ncols) epi.chunk(tile, lane0, c, v);
+        c += 2 * kCols;
+      } while (c < tile.ncols);
       epi.end(tile);
       ++turn;
     }
@@ -720,13 +803,14 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   else __syncthreads();
   tc_fence_after();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.dev_status, (int32_t)DX_DEV_WAIT_EXPIRED);
-  if (warp == 5) mm_tmem_free<CG>(tmem, kTmemCols);
+  if (warp == kWarpMma) mm_tmem_free<CG>(tmem, kTmemCols);
 }
 
 template <int CG, int BN, int STAGES, class Epilogue>
 constexpr size_t mm_smem() {
   constexpr int half = BN / CG < 32 ? 32 : BN / CG;
-  return 1024 + (size_t)STAGES * (kMmA + half * kMmK * 2) + (sizeof(MmShared) + 127) / 128 * 128 + 4 * Epilogue::kStaging;
+  return 1024 + (size_t)STAGES * (kMmA + half * kMmK * 2) + (sizeof(MmShared) + 127) / 128 * 128 +
+         kMmStoring * Epilogue::kStaging;
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
@@ -740,7 +824,7 @@ cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long l
   long long units = ctx->sm_count / CG;
   if (max_tiles < units) units = max_tiles;
   if (units < 1) units = 1;
-  return dx_launch_pdl(false, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(FORM, GATHER)), smem,
+  return dx_launch_pdl(false, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(GATHER)), smem,
                        st, CG, maps, p);
 }
 
