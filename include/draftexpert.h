@@ -541,7 +541,8 @@ dx_status moe_combine_tokens(dx_ctx* ctx, const void* z, int32_t z_dtype, int64_
 dx_status moe_combine_tokens_backward(dx_ctx* ctx, const void* dy, int64_t ld_dy, const void* z, int64_t ldz, int32_t dtype,
                                       const float* topk_w, int32_t N, int32_t top_k, int32_t H, void* dz, int64_t ld_dz,
                                       float* d_topk_w, void* stream);
-dx_status spec_head_loss_workspace(int32_t N, int32_t V, int32_t H, int32_t grad, size_t* least_out, size_t* best_out);
+dx_status spec_head_loss_workspace(dx_ctx* ctx, int32_t N, int32_t V, int32_t H, int32_t grad, size_t* least_out,
+                                   size_t* best_out);
 dx_status spec_head_loss(dx_ctx* ctx, const void* h, int32_t N, int64_t ldh, const void* W_lm, int32_t V, int64_t ldw, int32_t H,
                          const int32_t* targets, const float* row_weight, float* loss, void* dh, int64_t ld_dh, void* dW,
                          int64_t ld_dW, void* workspace, size_t workspace_bytes, void* stream);

@@ -127,7 +127,7 @@ SIGNATURES = {
                                          _L, _P, _P, C.c_size_t, _P]),
     "moe_combine_tokens": (_I, [_P, _P, _I, _L, _P, _I, _I, _I, _P, _I, _L, _P]),
     "moe_combine_tokens_backward": (_I, [_P, _P, _L, _P, _L, _I, _P, _I, _I, _I, _P, _L, _P, _P]),
-    "spec_head_loss_workspace": (_I, [_I, _I, _I, _I, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "spec_head_loss_workspace": (_I, [_P, _I, _I, _I, _I, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
     "spec_head_loss": (_I, [_P, _P, _I, _L, _P, _I, _L, _I, _P, _P, _P, _P, _L, _P, _L, _P, C.c_size_t, _P]),
     "expert_cache_create": (_I, [_P, _I, _I, _I, C.c_size_t, C.POINTER(_P)]),
     "expert_cache_set_q4": (_I, [_P, C.POINTER(LayerDesc), _I]),
@@ -1125,10 +1125,8 @@ def spec_head_loss(ctx: Context, h: torch.Tensor, W_lm: torch.Tensor, targets: t
     if (dh is not None and dh.shape[0] != N) or (dW is not None and dW.shape[0] != V):
         raise ValueError("out: rows of dh and dW as those of h and W_lm are expected")
     if workspace is None:
-        least, best = C.c_size_t(0), C.c_size_t(0)
-        _check(ctx.lib.spec_head_loss_workspace(N, V, H, 1 if dh is not None or dW is not None else 0, C.byref(least),
-                                                C.byref(best)), "spec_head_loss_workspace")
-        workspace = torch.empty(best.value, dtype=torch.uint8, device=h.device)
+        best = spec_head_loss_workspace(ctx, N, V, H, dh is not None or dW is not None)[1]
+        workspace = torch.empty(best, dtype=torch.uint8, device=h.device)
     elif workspace.dtype is not torch.uint8 or workspace.get_device() != ctx.device or not workspace.is_contiguous():
         raise ValueError(f"workspace: a contiguous torch.uint8 tensor on cuda:{ctx.device} is expected")
     _check(ctx.lib.spec_head_loss(ctx.handle, _ptr(h), N, ldh, _ptr(W_lm), V, ldw, H, _ptr(targets), _ptr(row_weight),
@@ -1137,10 +1135,10 @@ def spec_head_loss(ctx: Context, h: torch.Tensor, W_lm: torch.Tensor, targets: t
     return out
 
 
-def spec_head_loss_workspace(N: int, V: int, H: int, grad: bool = True) -> Tuple[int, int]:
+def spec_head_loss_workspace(ctx: Context, N: int, V: int, H: int, grad: bool = True) -> Tuple[int, int]:
     """Bytes of workspace ``spec_head_loss`` needs at least, and bytes with which it takes as few pieces as are of use."""
     least, best = C.c_size_t(0), C.c_size_t(0)
-    _check(load().spec_head_loss_workspace(N, V, H, 1 if grad else 0, C.byref(least), C.byref(best)),
+    _check(ctx.lib.spec_head_loss_workspace(ctx.handle, N, V, H, 1 if grad else 0, C.byref(least), C.byref(best)),
            "spec_head_loss_workspace")
     return least.value, best.value
 

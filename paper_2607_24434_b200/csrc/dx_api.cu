@@ -1198,12 +1198,12 @@ extern "C" dx_status moe_combine_tokens_backward(dx_ctx* ctx, const void* dy, in
   return DX_OK;
 }
 
-extern "C" dx_status spec_head_loss_workspace(int32_t N, int32_t V, int32_t H, int32_t grad, size_t* least_out,
+extern "C" dx_status spec_head_loss_workspace(dx_ctx* ctx, int32_t N, int32_t V, int32_t H, int32_t grad, size_t* least_out,
                                               size_t* best_out) {
-  if (!least_out || !best_out) return DX_ERR_INVALID_ARG;
+  if (!ctx || !least_out || !best_out) return DX_ERR_INVALID_ARG;
   if (N < 0 || V < 1 || H < 1) return DX_ERR_SHAPE;
   *least_out = *best_out = 0;
-  if (N > 0) dx_head_loss_workspace(N, V, H, grad, least_out, best_out);
+  if (N > 0) dx_head_loss_workspace(ctx->sm_count, N, V, H, grad, least_out, best_out);
   return DX_OK;
 }
 
@@ -1235,7 +1235,7 @@ extern "C" dx_status spec_head_loss(dx_ctx* ctx, const void* h, int32_t N, int64
     return DX_OK;
   }
   size_t least = 0, best = 0;
-  dx_head_loss_workspace(N, V, H, dh || dW, &least, &best);
+  dx_head_loss_workspace(ctx->sm_count, N, V, H, dh || dW, &least, &best);
   if (!targets || !workspace || (uintptr_t)workspace % 256 || workspace_bytes < least) return DX_ERR_INVALID_ARG;
   DxHeadLoss a = {};
   a.h = h; a.ldh = ldh; a.W = W_lm; a.ldw = ldw; a.N = N; a.V = V; a.H = H;

@@ -59,7 +59,7 @@ __device__ __forceinline__ int scattered(const MmParams& p, int row, int lane) {
 
 template <int COLS>
 struct FragmentEpilogue {
-  static constexpr int kCols = COLS;
+  static constexpr int kCols = COLS, kRound = 1;
   using Values = Fragments<COLS>;
   const MmParams& p;
   const int lane;
@@ -405,8 +405,12 @@ bool rows_source(MmMaps* m, MmParams* p, const DxGroupedMm& a, int cols) {
   p->b_rows = a.x_rows;
   p->b_src = a.x;
   p->b_ld = a.ldx;
-  return a.gather || (dx_matrix_map(&m->b, a.x, a.x_rows, cols, a.ldx, 128) &&
-                      dx_matrix_map(&m->b_few, a.x, a.x_rows, cols, a.ldx, 32));
+  int64_t rows = a.x_rows;
+  if (a.w_rows) {      // (panels)
+    rows = (int64_t)((a.w_rows + kPanel - 1) / kPanel) * a.group_rows;
+    cols = kPanel;
+  }
+  return a.gather || (dx_matrix_map(&m->b, a.x, rows, cols, a.ldx, 128) && dx_matrix_map(&m->b_few, a.x, rows, cols, a.ldx, 32));
 }
 
 MmParams base_params(const dx_ctx* ctx, const int32_t* offsets, int groups, int rows) {
@@ -432,7 +436,13 @@ cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t
   p.scatter = a.scatter;
   p.out_rows = a.y_rows;
   p.addend = a.addend;
-  const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)a.n, (uint64_t)a.n_groups};
+  if (a.w_rows) {
+    p.n_live = a.n_live;
+    p.group_rows = a.group_rows;
+    p.a_step = a.n;
+    p.kdim = a.w_rows;
+  }
+  const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)(a.w_rows ? a.w_rows : a.n), (uint64_t)(a.w_rows ? 1 : a.n_groups)};
   const uint64_t strides[2] = {(uint64_t)a.ldw, (uint64_t)a.w_stride};
   const uint32_t box[3] = {64, a.transposed ? 64u : 128u, 1};
   if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, n_in))
@@ -520,7 +530,10 @@ cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t
   p.out = a.dw;
   p.ld = a.ld_dw;
   p.group_stride = a.dw_stride;
-  if (!dx_matrix_map(&m.a, a.x, a.x_rows, a.k, a.ldx, 64) || !dx_matrix_map(&m.b, a.dy, a.dy_rows, a.n, a.ld_dy, 64))
+  if (a.dy_panels) p.b_panel = a.dy_rows;
+  if (!dx_matrix_map(&m.a, a.x, a.x_rows, a.k, a.ldx, 64) ||
+      !dx_matrix_map(&m.b, a.dy, (int64_t)(a.dy_panels ? (a.n + kPanel - 1) / kPanel : 1) * a.dy_rows,
+                     a.dy_panels ? kPanel : a.n, a.ld_dy, 64))
     return cudaErrorInvalidValue;
   const long long tiles = (long long)a.n_groups * ((a.k + 255) / 256) * ((a.n + 255) / 256);
   return a.dw_fp32 ? mm_launch<kOuter, true, 2, 256, 6, StoreOuter<float>>(ctx, m, p, tiles, st)

@@ -2,63 +2,113 @@
 //     loss = log sum_v exp(z_v) - z_target,      dz = weight * (softmax(z) - 1_target),      dh = W^T dz,     dW = dz^T h
 // in pieces of the vocabulary; logits exist as tiles in tensor memory only.
 //
-//   1. the rows that count (a target, a weight other than 0) are listed in order: the others cost nothing below
+//   1. the rows that count (a target, a weight other than 0) are listed in order and copied next to each other: the others cost
+//      nothing below, whatever they hold
 //   2. products of the listed rows with the whole vocabulary; of every tile a row keeps (maximum, sum of exponentials) and,
 //      where the tile holds it, the target's logit
 //   3. the tiles' pairs are joined: loss, log of the sum
 //   4. (gradients) for each piece of the vocabulary the products once more, now straight to dz (rounded to bf16 once), then
 //      dh += dz W and dW = dz^T h as products of the kernel of the grouped experts with one group
 // The second pass over the products costs 2 N V H operations beside the 6 N V H of loss and gradients; what it saves is
-// N V logits in fp32 (they cannot be kept in bf16: a logit of 20 would be off by 0.06, its probability by 6 %).
+// N V logits in fp32 (they cannot be kept in bf16: a logit of 20 would be off by 0.06, its probability by 6 %).  For few rows
+// -- a verified block -- the logits are little and the head's bytes are the time: there they are kept (kKeepMost), and the
+// vocabulary is cut into blocks whose shares of dh different SMs sum, in fp32, added up in order afterwards (dh alone has no
+// more tiles than H / 128: 16 of 148 SMs at H = 2048).
 #include "dx_mm.cuh"
 
 namespace {
 
 // ---- 1: which rows count -------------------------------------------------------------------------------------------
-// One CTA; every turn takes 1024 rows.  live[i]: the i-th row that counts; rows that do not have loss 0 (a target outside the
-// vocabulary: NaN).
+// One CTA, a thread for every 1/1024 of the rows: counted, summed over the CTA, listed.  live[i]: the i-th row that counts; rows
+// that do not have loss 0 (a target outside the vocabulary: NaN).
+__device__ __forceinline__ bool row_counts(const int32_t* targets, const float* row_weight, int r, int V, bool& bad) {
+  const int t = __ldg(targets + r);
+  const float w = row_weight ? __ldg(row_weight + r) : 1.0f;
+  bad = t < -1 || t >= V;
+  return t >= 0 && !bad && w != 0.0f;
+}
 __global__ void __launch_bounds__(1024) dx_head_rows_kernel(const int32_t* targets, const float* row_weight, int N, int V,
                                                             int32_t* live, int32_t* n_live, float* loss,
                                                             int32_t* dev_status) {
   __shared__ int sums[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int base = 0;
-  for (int r0 = 0; r0 < N; r0 += 1024) {
-    const int r = r0 + threadIdx.x;
-    bool in = false;
-    if (r < N) {
-      const int t = __ldg(targets + r);
-      const bool bad = t < -1 || t >= V;
-      in = t >= 0 && !bad && (!row_weight || __ldg(row_weight + r) != 0.0f);
-      if (bad) atomicExch(dev_status, (int32_t)DX_DEV_BAD_TOKEN);
-      if (!in && loss) loss[r] = bad ? __int_as_float(0x7fffffff) : 0.0f;
-    }
-    const unsigned int m = __ballot_sync(0xffffffffu, in);
-    if (lane == 0) sums[warp] = __popc(m);
-    __syncthreads();
-    int before = 0, all = 0;
+  const int each = (N + 1023) / 1024, lo = min(N, (int)threadIdx.x * each), hi = min(N, lo + each);
+  int count = 0;
+#pragma unroll 4
+  for (int r = lo; r < hi; ++r) {
+    bool bad;
+    const bool in = row_counts(targets, row_weight, r, V, bad);
+    if (bad) atomicExch(dev_status, (int32_t)DX_DEV_BAD_TOKEN);
+    if (!in && loss) loss[r] = bad ? __int_as_float(0x7fffffff) : 0.0f;
+    count += in ? 1 : 0;
+  }
+  int sum = count;
 #pragma unroll
-    for (int w = 0; w < 32; ++w) {
-      before += w < warp ? sums[w] : 0;
-      all += sums[w];
-    }
-    if (in) live[base + before + __popc(m & ((1u << lane) - 1u))] = r;
-    base += all;
-    __syncthreads();
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, sum, d);
+    if (lane >= d) sum += o;
+  }
+  if (lane == 31) sums[warp] = sum;
+  __syncthreads();
+  int at = sum - count, all = 0;
+#pragma unroll
+  for (int w = 0; w < 32; ++w) {
+    at += w < warp ? sums[w] : 0;
+    all += sums[w];
+  }
+#pragma unroll 4
+  for (int r = lo; r < hi; ++r) {
+    bool bad;
+    if (row_counts(targets, row_weight, r, V, bad)) live[at++] = r;
   }
   if (threadIdx.x == 0) {
     n_live[0] = 0;        // (offsets of the one group that the products of the gradients see)
-    n_live[1] = base;
+    n_live[1] = all;
+  }
+}
+// the listed rows next to each other: four rows per CTA
+__global__ void __launch_bounds__(256) dx_head_pack_kernel(const __nv_bfloat16* h, int64_t ldh, int H, const int32_t* live,
+                                                           const int32_t* n_live, __nv_bfloat16* out) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= __ldg(n_live)) return;
+  const __nv_bfloat16* from = h + (int64_t)__ldg(live + row) * ldh;
+  for (int i = (threadIdx.x & 63) * 8; i < H; i += 512)
+    *reinterpret_cast<uint4*>(out + (int64_t)row * H + i) = __ldg(reinterpret_cast<const uint4*>(from + i));
+}
+
+// 32 bytes of a row per store: a thread has a row of its own, and less than a sector would be written twice
+__device__ __forceinline__ void store_sector(void* at, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void store32(float* at, const float (&v)[32], int n) {   // (n: whole sectors of them)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (8 * i >= n) break;
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
+    store_sector(at + 8 * i, w);
+  }
+}
+__device__ __forceinline__ void store32(__nv_bfloat16* at, const float (&v)[32]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = bf16_pair(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
+    store_sector(at + 16 * i, w);
   }
 }
 
 // ---- 2: (maximum, sum) of a half of a tile's columns (every other 32), a row per thread ---------------------------------------------------------
+template <bool KEEP>
 struct RowSums {
   const MmParams& p;
   const int lane, share;
   int row, target;
   float top, sum;
-  static constexpr int kStaging = 0, kCols = 32;
+  static constexpr int kStaging = 0, kCols = 32, kRound = 1;
   struct Values {
     float v[32];
   };
@@ -67,13 +117,14 @@ struct RowSums {
   __device__ __forceinline__ void zero(Values&) {}
   __device__ __forceinline__ void begin(const MmTile& t, int lane0, int) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
-    target = row >= 0 ? __ldg(p.targets + __ldg(p.a_index + row)) - t.n0 : -1;   // (its place among the tile's columns)
+    target = row >= 0 ? __ldg(p.targets + __ldg(p.live + row)) - t.n0 : -1;   // (its place among the tile's columns)
     top = -INFINITY;
     sum = 0.0f;
   }
   __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, Values& x) {
     float(&v)[32] = x.v;
     const int left = t.ncols - c0;
+    if (KEEP && row >= 0) store32(p.logits + (int64_t)row * p.ld_logits + t.n0 + c0, v, left);
     if (left < 32) {
 #pragma unroll
       for (int c = 0; c < 32; ++c)
@@ -99,28 +150,36 @@ struct RowSums {
     top = m;
   }
   __device__ __forceinline__ void end(const MmTile& t) {
-    if (row >= 0) p.part[(int64_t)((t.n0 >> 8) * 2 + share) * p.part_pitch + row] = make_float2(top, sum);
+    if (row >= 0) p.part[(int64_t)(t.row0 * 2 + share) * p.part_pitch + row] = make_float2(top, sum);
   }
 };
 
 // ---- 3: joined over the tiles ----------------------------------------------------------------------------------------
-// 32 rows per CTA, a lane each; eight warps take the tiles in turns.  The loss is (maximum - target's logit) + log of the sum
+// 32 rows per CTA, a lane each; 32 warps take the tiles in turns.  The loss is (maximum - target's logit) + log of the sum
 // relative to the maximum, so that a confident row's loss is not a difference of two large numbers.  With gradients also the
 // zeros of the rows that do not count.
-__global__ void __launch_bounds__(256) dx_head_join_kernel(const float2* part, int part_pitch, int tiles, const int32_t* live,
+__global__ void __launch_bounds__(1024) dx_head_join_kernel(const float2* part, int part_pitch, int tiles, const int32_t* live,
                                                            const int32_t* n_live_at, const float* target_logit, float* loss,
                                                            float* lse, float* row_loss, const int32_t* targets,
                                                            const float* row_weight, int N, int V, int H,
                                                            __nv_bfloat16* dh, int64_t ld_dh) {
-  __shared__ float tops[8][32], sums[8][32];
+  __shared__ float tops[32][33], sums[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
   const int n_live = __ldg(n_live_at);
   float top = -INFINITY, sum = 0.0f;
   if (row < n_live) {
-    for (int i = warp; i < tiles; i += 8) {
-      const float2 q = part[(int64_t)i * part_pitch + row];
-      const float m = fmaxf(top, q.x), from = m == -INFINITY ? 0.0f : m;
-      sum = sum * ex2((top - from) * kLog2e) + q.y * ex2((q.x - from) * kLog2e);
+    for (int i = warp; i < tiles; i += 256) {     // (eight of them under way at a time)
+      float2 q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        q[j] = i + 32 * j < tiles ? __ldg(part + (int64_t)(i + 32 * j) * part_pitch + row) : make_float2(-INFINITY, 0.0f);
+      float m = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, q[j].x);
+      const float from = m == -INFINITY ? 0.0f : m;
+      sum *= ex2((top - from) * kLog2e);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += q[j].y * ex2((q[j].x - from) * kLog2e);
       top = m;
     }
   }
@@ -130,11 +189,11 @@ __global__ void __launch_bounds__(256) dx_head_join_kernel(const float2* part, i
   if (warp == 0 && row < n_live) {
     float m = tops[0][lane];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) m = fmaxf(m, tops[w][lane]);
+    for (int w = 1; w < 32; ++w) m = fmaxf(m, tops[w][lane]);
     const float from = m == -INFINITY ? 0.0f : m;
     float s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += sums[w][lane] * ex2((tops[w][lane] - from) * kLog2e);
+    for (int w = 0; w < 32; ++w) s += sums[w][lane] * ex2((tops[w][lane] - from) * kLog2e);
     const double log_sum = log((double)s);
     const float l = (float)(((double)m - (double)target_logit[row]) + log_sum);
     if (loss) loss[live[row]] = l;
@@ -142,7 +201,7 @@ __global__ void __launch_bounds__(256) dx_head_join_kernel(const float2* part, i
     row_loss[row] = l;
   }
   if (!dh) return;
-  for (int r = blockIdx.x * 32 + warp; r < min(N, blockIdx.x * 32 + 32); r += 8) {
+  for (int r = blockIdx.x * 32 + warp; r < min(N, blockIdx.x * 32 + 32); r += 32) {
     const int t = __ldg(targets + r);
     if (t >= 0 && t < V && (!row_weight || __ldg(row_weight + r) != 0.0f)) continue;
     for (int i = lane; i < H / 8; i += 32) *reinterpret_cast<uint4*>(dh + r * ld_dh + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
@@ -156,7 +215,7 @@ struct StoreDz {
   const int lane, share;
   int row, target;
   float lse, weight, at_target;
-  static constexpr int kStaging = 0, kCols = 32;
+  static constexpr int kStaging = 0, kCols = 32, kRound = 64;   // (the products of the gradients read whole blocks of 64)
   struct Values {
     float v[32];
   };
@@ -168,7 +227,7 @@ struct StoreDz {
     target = -1;
     lse = weight = at_target = 0.0f;
     if (row >= 0) {
-      const int r = __ldg(p.a_index + row);
+      const int r = __ldg(p.live + row);
       target = __ldg(p.targets + r) - p.column0 - t.n0;
       weight = p.row_weight ? __ldg(p.row_weight + r) : 1.0f;
       lse = __ldg(p.lse + row);
@@ -186,50 +245,156 @@ struct StoreDz {
       for (int c = 0; c < 32; ++c)
         if (c == at) v[c] = at_target;
     }
-    if (row < 0) return;
-    uint32_t w[16];
+    if (t.ncols - c0 < 32) {
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
-      w[c] = bf16_pair(v[2 * c], v[2 * c + 1]);
+      for (int c = 0; c < 32; ++c)
+        if (c >= t.ncols - c0) v[c] = 0.0f;
     }
-    // (columns behind the piece's last are not read: the matrices of the gradients end there)
-    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)row * p.ld + t.n0 + c0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + 16 * i), "r"(w[8 * i]), "r"(w[8 * i + 1]),
-                   "r"(w[8 * i + 2]), "r"(w[8 * i + 3]), "r"(w[8 * i + 4]), "r"(w[8 * i + 5]), "r"(w[8 * i + 6]),
-                   "r"(w[8 * i + 7]) : "memory");
+    if (row < 0) return;
+    store32(reinterpret_cast<__nv_bfloat16*>(p.out) + ((int64_t)(t.n0 / kPanel) * p.panel + row) * kPanel + c0, v);
   }
 };
 
+// ... from logits that were kept: eight per thread, rows in blockIdx.y
+__global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, int64_t ld_logits, int V, const int32_t* live,
+                                                         const int32_t* n_live, const int32_t* targets,
+                                                         const float* row_weight, const float* lse, const float* row_loss,
+                                                         __nv_bfloat16* dz, int panel) {
+  const int row = blockIdx.y, v0 = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (row >= __ldg(n_live) || v0 >= (V + 63) / 64 * 64) return;
+  const int r = __ldg(live + row), target = __ldg(targets + r) - v0;
+  const float weight = row_weight ? __ldg(row_weight + r) : 1.0f, l = __ldg(lse + row);
+  const float4 a = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0);
+  const float4 b = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0 + 4);
+  float z[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  const float at_target = target >= 0 && target < 8 ? weight * expm1f(-__ldg(row_loss + row)) : 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    z[i] = weight * ex2((z[i] - l) * kLog2e);
+    if (i == target) z[i] = at_target;
+    if (v0 + i >= V) z[i] = 0.0f;
+  }
+  *reinterpret_cast<uint4*>(dz + ((int64_t)(v0 / kPanel) * panel + row) * kPanel + v0 % kPanel) =
+      make_uint4(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]), bf16_pair(z[4], z[5]), bf16_pair(z[6], z[7]));
+}
+
+// dh of the rows that count: the blocks' shares in order, rounded once
+__global__ void __launch_bounds__(128) dx_head_sum_kernel(const float* share, int blocks, int rows, int H, const int32_t* live,
+                                                          const int32_t* n_live, __nv_bfloat16* dh, int64_t ld_dh) {
+  const int row = blockIdx.y, i = (blockIdx.x * 128 + threadIdx.x) * 4;
+  if (row >= __ldg(n_live) || i >= H) return;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+  for (int b = 0; b < blocks; ++b) {
+    const float4 q = __ldcs(reinterpret_cast<const float4*>(share + ((int64_t)b * rows + row) * H + i));
+    s = make_float4(s.x + q.x, s.y + q.y, s.z + q.z, s.w + q.w);
+  }
+  *reinterpret_cast<uint2*>(dh + (int64_t)__ldg(live + row) * ld_dh + i) = make_uint2(bf16_pair(s.x, s.y), bf16_pair(s.z, s.w));
+}
+
 // ---- workspace -----------------------------------------------------------------------------------------------------
 constexpr size_t kPieceBest = size_t(256) << 20;   // bytes of dz of a piece with which more would gain nothing
+constexpr size_t kKeepMost = size_t(64) << 20;     // bytes of logits that are kept (half of L2)
 
-struct HeadSpace {
-  size_t live, n_live, part, target_logit, lse, row_loss, dh_acc, dz, fixed;
-  int pitch;
+constexpr int kFewest = 32768;                     // rows up to which a CTA per row (and block) will do
+
+struct HeadPlan {
+  bool keep;                 // logits are kept
+  int tiles;                 // of the first pass, along the vocabulary
+  int piece;                 // words of a piece (a multiple of 256)
+  int blocks, block;         // blocks of a piece whose shares of dh are summed apart (1: the piece), words of a block
+  size_t live, n_live, rows, part, target_logit, lse, row_loss, dh_acc, logits, share, dz, bytes;
+  int pitch, width;          // words of a tile of the first pass
+  int64_t ld_logits;
 };
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-HeadSpace head_space(int N, int V, int H, bool grad) {
-  HeadSpace s;
-  s.pitch = (N + 31) / 32 * 32;
+// `space`: bytes there are (0: as many as are of use)
+HeadPlan head_plan(const int sm_count, int N, int V, int H, bool grad, size_t space) {
+  HeadPlan s = {};
+  const int64_t words = ((int64_t)V + 255) / 256 * 256;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
     at += up256(bytes);
     return here;
   };
+  s.pitch = (N + 31) / 32 * 32;
   s.n_live = take(8);
   s.live = take((size_t)N * 4);
   s.target_logit = take((size_t)N * 4);
   s.lse = take((size_t)N * 4);
   s.row_loss = take((size_t)N * 4);
-  s.part = take((size_t)((V + 255) / 256) * 2 * s.pitch * sizeof(float2));
-  s.dh_acc = take(grad ? (size_t)N * H * 4 : 0);
-  s.dz = at;
-  s.fixed = at;
-  return s;
+  s.rows = take((size_t)N * H * 2);
+  // Few rows: the width with which the tiles fill the GPU best (the last round is rarely full: 400 tiles of 256 words are 2.7
+  // rounds of 148 SMs, 427 of 240 are 2.9).  More rows: narrower tiles would fetch the rows more often than they save.
+  s.width = 256;
+  if (N <= 128) {
+    int64_t best = 0;
+    for (int w = 256; w >= 128; w -= 16) {
+      const int64_t cost = ((V + w - 1) / w + sm_count - 1) / sm_count * w;
+      if (best == 0 || cost < best) {
+        best = cost;
+        s.width = w;
+      }
+    }
+  }
+  s.tiles = (V + s.width - 1) / s.width;
+  s.part = take((size_t)s.tiles * 2 * s.pitch * sizeof(float2));
+  s.blocks = 1;
+  s.piece = s.block = (int)words;
+  s.bytes = at;
+  if (!grad) return s;
+  const size_t fixed = at, column = (size_t)N * 2;
+  // words of a piece: all of them, or as many as the space allows, in pieces of equal length
+  s.keep = (size_t)N * words * 4 <= kKeepMost && N <= kFewest && space != 1;
+  int64_t piece = (int64_t)(kPieceBest / column / 256 * 256);
+  if (piece < 256 || space == 1) piece = 256;
+  for (bool lean = space == 1;; lean = true) {
+    // (lean: no logits kept, no shares; then as many words as are left room for)
+    at = fixed;
+    if (lean) {
+      s.keep = false;
+      const size_t rest = up256((size_t)N * H * 4);
+      piece = space > fixed + rest ? (int64_t)((space - fixed - rest) / column / 256 * 256) : 256;
+      if (piece < 256) piece = 256;
+    }
+    if (piece > words) piece = words;
+    const int64_t pieces = (words + piece - 1) / piece;
+    piece = (words / 256 + pieces - 1) / pieces * 256;
+    s.blocks = 1;
+    s.block = (int)piece;
+    if (!lean && N <= kFewest) {
+      // dh has few tiles where there are few rows, and rarely a multiple of what runs at a time: cut a piece's words into as many
+      // blocks as fill the GPU best, their shares of dh summed apart.  Rates in words and bytes per microsecond: a pair of CTAs
+      // multiplies 256 x 256 x 64 in a third of a microsecond; few rows wait for the head's bytes instead.
+      const bool few = N <= 32;
+      const int64_t tiles = ((H + (few ? 127 : 255)) / (few ? 128 : 256)) * (int64_t)((N + (few ? 63 : 255)) / (few ? 64 : 256));
+      const int64_t units = few ? sm_count : sm_count / 2;
+      const double wave = few ? (double)piece * 256.0 * units / 6e6 : (double)piece / 64.0 * 0.33;
+      double least = 0.0;
+      for (int b = 1; b <= 32; ++b) {
+        const int block = (int)((piece / 256 + b - 1) / b) * 256;
+        const int n = (int)((piece + block - 1) / block);
+        const double cost = (double)pieces * (double)((n * tiles + units - 1) / units) * wave / n +
+                            (n > 1 ? n * (double)N * H * 8.0 / 6e6 + 4.0 : 0.0);
+        if (b == 1 || cost < least) {
+          least = cost;
+          s.blocks = n;
+          s.block = block;
+        }
+      }
+    }
+    s.piece = (int)piece;
+    if (s.keep && pieces > 1) s.keep = false;
+    s.ld_logits = words;
+    if (s.keep) s.logits = take((size_t)N * words * 4);
+    if (s.blocks > 1) s.share = take((size_t)s.blocks * N * H * 4);
+    else if (pieces > 1 || lean) s.dh_acc = take((size_t)N * H * 4);
+    s.dz = take(column * piece);
+    s.bytes = at;
+    if (lean || space == 0 || space >= s.bytes) return s;
+  }
 }
 
 template <class Epilogue>
@@ -237,26 +402,23 @@ cudaError_t launch_head(dx_ctx* ctx, const MmMaps& m, const MmParams& p, cudaStr
   // up to 128 rows: a pair of CTAs would multiply 128 rows of nothing
   const bool few = p.n_rows <= 128;
   const long long lanes = few ? 128 : 256;
-  const long long tiles = ((p.n_rows + lanes - 1) / lanes) * ((p.columns + 255) / 256);
-  return few ? mm_launch<kHead, true, 1, 256, 4, Epilogue>(ctx, m, p, tiles, st)
-             : mm_launch<kHead, true, 2, 256, 6, Epilogue>(ctx, m, p, tiles, st);
+  const int width = p.tile_width ? p.tile_width : 256;
+  const long long tiles = ((p.n_rows + lanes - 1) / lanes) * ((p.columns + width - 1) / width);
+  return few ? mm_launch<kHead, false, 1, 256, 4, Epilogue>(ctx, m, p, tiles, st)
+             : mm_launch<kHead, false, 2, 256, 6, Epilogue>(ctx, m, p, tiles, st);
 }
 
 }  // namespace
 
-void dx_head_loss_workspace(int N, int V, int H, int grad, size_t* least, size_t* best) {
-  const HeadSpace s = head_space(N, V, H, grad != 0);
-  const size_t column = (size_t)N * 2, all = ((size_t)V + 255) / 256 * 256;
-  *least = s.fixed + (grad ? column * 256 : 0);
-  size_t want = kPieceBest / column / 256 * 256;
-  if (want < 256) want = 256;
-  if (want > all) want = all;
-  *best = s.fixed + (grad ? column * want : 0);
+void dx_head_loss_workspace(int sm_count, int N, int V, int H, int grad, size_t* least, size_t* best) {
+  *best = head_plan(sm_count, N, V, H, grad != 0, 0).bytes;
+  *least = head_plan(sm_count, N, V, H, grad != 0, 1).bytes;
+  if (*best < *least) *best = *least;
 }
 
 cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t st, int* n_launches) {
   const bool grad = a.dh != nullptr || a.dW != nullptr;
-  const HeadSpace s = head_space(a.N, a.V, a.H, grad);
+  const HeadPlan s = head_plan(ctx->sm_count, a.N, a.V, a.H, grad, a.workspace_bytes);
   unsigned char* ws = reinterpret_cast<unsigned char*>(a.workspace);
   int32_t* live = reinterpret_cast<int32_t*>(ws + s.live);
   int32_t* n_live = reinterpret_cast<int32_t*>(ws + s.n_live);
@@ -265,21 +427,33 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   float* lse = reinterpret_cast<float*>(ws + s.lse);
   float* row_loss = reinterpret_cast<float*>(ws + s.row_loss);
   float* dh_acc = reinterpret_cast<float*>(ws + s.dh_acc);
-  const int tiles = (a.V + 255) / 256;
+  float* logits = reinterpret_cast<float*>(ws + s.logits);
+  float* share = reinterpret_cast<float*>(ws + s.share);
+  __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + s.dz);
+  __nv_bfloat16* dh = reinterpret_cast<__nv_bfloat16*>(a.dh);
+  __nv_bfloat16* rows = reinterpret_cast<__nv_bfloat16*>(ws + s.rows);
   int n = 0;
+  cudaError_t e = cudaSuccess;
+  auto launched = [&](cudaError_t err) {
+    e = err;
+    if (e == cudaSuccess) ++n;
+    *n_launches = n;
+    return e == cudaSuccess;
+  };
 
   MmMaps m = {};
-  if (!dx_matrix_map(&m.b, a.W, a.V, a.H, a.ldw, 128)) return cudaErrorInvalidValue;
+  // (few rows: copies of no more rows than that; what else the lanes' place in a stage holds meets no row that counts)
+  const int box = a.N <= 32 ? 32 : 128;
+  if (!dx_matrix_map(&m.a, rows, a.N, a.H, a.H, box) || !dx_matrix_map(&m.b, a.W, a.V, a.H, a.ldw, 128))
+    return cudaErrorInvalidValue;
   MmParams p = {};
   p.n_groups = 1;
   p.n_rows = a.N;
   p.n_live = n_live + 1;
   p.columns = a.V;
   p.kdim = a.H;
-  p.a_src = a.h;
-  p.a_ld = a.ldh;
-  p.a_rows = a.N;
-  p.a_index = live;
+  p.live = live;
+  p.a_box = (uint32_t)box;
   p.targets = a.targets;
   p.row_weight = a.row_weight;
   p.part = part;
@@ -287,88 +461,94 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   p.target_logit = target_logit;
   p.lse = lse;
   p.row_loss = row_loss;
+  p.logits = logits;
+  p.ld_logits = s.ld_logits;
   p.dev_status = ctx->dev_status;
   p.wait_limit = ctx->wait_limit;
 
   dx_head_rows_kernel<<<1, 1024, 0, st>>>(a.targets, a.row_weight, a.N, a.V, live, n_live, a.loss, ctx->dev_status);
-  cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) { ++n; e = launch_head<RowSums>(ctx, m, p, st); }
-  if (e == cudaSuccess) {
-    ++n;
-    dx_head_join_kernel<<<(a.N + 31) / 32, 256, 0, st>>>(part, s.pitch, 2 * tiles, live, n_live + 1, target_logit, a.loss, lse,
-                                                         row_loss, a.targets, a.row_weight, a.N, a.V, a.H,
-                                                         reinterpret_cast<__nv_bfloat16*>(a.dh), a.ld_dh);
-    e = cudaGetLastError();
-    if (e == cudaSuccess) ++n;
-  }
-  if (grad && e == cudaSuccess) {
-    void* dz = ws + s.dz;
-    const size_t column = (size_t)a.N * 2;
-    long long piece = (long long)((a.workspace_bytes - s.fixed) / column / 256 * 256);
-    if (piece > (long long)tiles * 256) piece = (long long)tiles * 256;
-    // (pieces of equal length)
-    const int pieces = (int)((tiles * 256LL + piece - 1) / piece);
-    piece = ((tiles + pieces - 1) / pieces) * 256LL;
-    for (int64_t v0 = 0; v0 < a.V && e == cudaSuccess; v0 += piece) {
-      const int len = (int)(a.V - v0 < piece ? a.V - v0 : piece);
-      const bool first = v0 == 0, last = v0 + len == a.V;
+  if (!launched(cudaGetLastError())) return e;
+  dx_head_pack_kernel<<<(a.N + 3) / 4, 256, 0, st>>>(reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, rows);
+  if (!launched(cudaGetLastError())) return e;
+  p.tile_width = s.width;
+  if (!launched(s.keep ? launch_head<RowSums<true>>(ctx, m, p, st) : launch_head<RowSums<false>>(ctx, m, p, st))) return e;
+  p.tile_width = 0;
+  dx_head_join_kernel<<<(a.N + 31) / 32, 1024, 0, st>>>(part, s.pitch, 2 * s.tiles, live, n_live + 1, target_logit, a.loss, lse,
+                                                       row_loss, a.targets, a.row_weight, a.N, a.V, a.H, dh, a.ld_dh);
+  if (!launched(cudaGetLastError()) || !grad) return e;
+
+  for (int64_t v0 = 0; v0 < a.V; v0 += s.piece) {
+    const int len = (int)(a.V - v0 < s.piece ? a.V - v0 : s.piece);
+    const bool first = v0 == 0, last = v0 + len == a.V;
+    if (s.keep) {
+      dx_head_dz_kernel<<<dim3((a.V + 2047) / 2048, a.N), 256, 0, st>>>(logits, s.ld_logits, a.V, live, n_live + 1, a.targets,
+                                                                        a.row_weight, lse, row_loss, dz, a.N);
+      if (!launched(cudaGetLastError())) return e;
+    } else {
       MmParams q = p;
       q.columns = len;
       q.column0 = (int)v0;
       q.out = dz;
-      q.ld = piece;
-      e = launch_head<StoreDz>(ctx, m, q, st);
-      if (e != cudaSuccess) break;
-      ++n;
-      const unsigned char* W = reinterpret_cast<const unsigned char*>(a.W) + v0 * a.ldw * 2;
-      if (a.dh) {
-        DxGroupedMm g = {};
-        g.x = dz;
-        g.x_rows = a.N;
-        g.ldx = piece;
-        g.w = W;
-        g.n_groups = 1;
-        g.n = len;
-        g.k = a.H;
-        g.transposed = 1;
-        g.ldw = a.ldw;
-        g.w_stride = (int64_t)len * a.ldw;
-        g.offsets = n_live;
-        g.n_rows = a.N;
-        g.gather_div = 1;
+      q.panel = a.N;
+      if (!launched(launch_head<StoreDz>(ctx, m, q, st))) return e;
+    }
+    if (a.dh) {
+      DxGroupedMm g = {};
+      g.x = dz;
+      g.x_rows = a.N;
+      g.ldx = kPanel;
+      g.w = reinterpret_cast<const unsigned char*>(a.W) + v0 * a.ldw * 2;
+      g.n_groups = s.blocks;
+      g.n = s.block;
+      g.k = a.H;
+      g.transposed = 1;
+      g.ldw = a.ldw;
+      g.w_stride = (int64_t)len * a.ldw;
+      g.n_rows = s.blocks * a.N;
+      g.gather_div = 1;
+      g.w_rows = len;
+      g.group_rows = a.N;
+      g.n_live = n_live + 1;
+      if (s.blocks > 1) {
+        g.y = share;
+        g.y_fp32 = 1;
+        g.y_rows = g.n_rows;
+        g.ldy = a.H;
+        g.addend = first ? nullptr : share;
+      } else {
         g.scatter = live;
         g.y = last ? a.dh : (void*)dh_acc;
         g.y_fp32 = last ? 0 : 1;
         g.y_rows = a.N;
         g.ldy = last ? a.ld_dh : a.H;
         g.addend = first ? nullptr : dh_acc;
-        e = dx_launch_grouped_mm(ctx, g, st);
-        if (e != cudaSuccess) break;
-        ++n;
       }
-      if (a.dW) {
-        DxGroupedDw g = {};
-        g.dy = dz;
-        g.dy_rows = a.N;
-        g.ld_dy = piece;
-        g.x = a.h;
-        g.x_rows = a.N;
-        g.ldx = a.ldh;
-        g.n_groups = 1;
-        g.n = len;
-        g.k = a.H;
-        g.offsets = n_live;
-        g.n_rows = a.N;
-        g.gather_x = live;
-        g.dy_div = g.x_div = 1;
-        g.dw = reinterpret_cast<unsigned char*>(a.dW) + v0 * a.ld_dW * 2;
-        g.ld_dw = a.ld_dW;
-        g.dw_stride = (int64_t)len * a.ld_dW;
-        e = dx_launch_grouped_dw(ctx, g, st);
-        if (e == cudaSuccess) ++n;
+      if (!launched(dx_launch_grouped_mm(ctx, g, st))) return e;
+      if (s.blocks > 1 && last) {
+        dx_head_sum_kernel<<<dim3((a.H + 511) / 512, a.N), 128, 0, st>>>(share, s.blocks, a.N, a.H, live, n_live + 1, dh, a.ld_dh);
+        if (!launched(cudaGetLastError())) return e;
       }
     }
+    if (a.dW) {
+      DxGroupedDw g = {};
+      g.dy = dz;
+      g.dy_rows = a.N;
+      g.ld_dy = kPanel;
+      g.dy_panels = 1;
+      g.x = rows;
+      g.x_rows = a.N;
+      g.ldx = a.H;
+      g.n_groups = 1;
+      g.n = len;
+      g.k = a.H;
+      g.offsets = n_live;
+      g.n_rows = a.N;
+      g.dy_div = g.x_div = 1;
+      g.dw = reinterpret_cast<unsigned char*>(a.dW) + v0 * a.ld_dW * 2;
+      g.ld_dw = a.ld_dW;
+      g.dw_stride = (int64_t)len * a.ld_dW;
+      if (!launched(dx_launch_grouped_dw(ctx, g, st))) return e;
+    }
   }
-  *n_launches = n;
   return e;
 }

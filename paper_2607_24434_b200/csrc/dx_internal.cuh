@@ -295,6 +295,10 @@ struct DxGroupedMm {
   int y_fp32, y_rows;
   int64_t ldy;
   const float* addend;       // fp32 [y_rows][columns of y], added in front of the rounding (transposed only)
+  // one matrix of w_rows rows cut into groups of n rows (a multiple of 256; the last one shorter), every group with the same
+  // number *n_live of sorted rows, group_rows apart; x is then [w_rows / 256][group_rows][256] (offsets are not used; transposed)
+  int w_rows, group_rows;
+  const int32_t* n_live;
 };
 struct DxGroupedDw {
   const void* dy;            // bf16 [dy_rows][ld_dy], n columns
@@ -311,6 +315,7 @@ struct DxGroupedDw {
   void* dw;                  // [n_groups][n][ld_dw]
   int dw_fp32;
   int64_t ld_dw, dw_stride;
+  int dy_panels;             // dy is [n / 256][dy_rows][256]
 };
 cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t st);
 cudaError_t dx_launch_grouped_swiglu(dx_ctx* ctx, const DxGroupedMm& a, void* gate_up, int64_t ld_gate_up, cudaStream_t st);
@@ -340,7 +345,7 @@ struct DxHeadLoss {
   size_t workspace_bytes;
 };
 // bytes of workspace the call needs at least, and those with which it runs in as few pieces as are of any use
-void dx_head_loss_workspace(int N, int V, int H, int grad, size_t* least, size_t* best);
+void dx_head_loss_workspace(int sm_count, int N, int V, int H, int grad, size_t* least, size_t* best);
 cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t st, int* n_launches);
 cudaError_t dx_experts_prepare(dx_ctx* ctx);   // opt-in shared memory attributes, once per context
 

@@ -35,6 +35,7 @@ __host__ __device__ constexpr int mm_threads(bool gather) { return gather ? 512 
 constexpr int kMmK = 64;                    // contraction elements of a stage: 128 bytes of a row
 constexpr int kMmA = 128 * kMmK * 2;        // bytes of a CTA's 128 rows of A in a stage
 constexpr int kMmMaxStages = 8;
+constexpr int kPanel = 256;                 // columns of a panel: a tile's, so that a tile's rows lie close together
 
 // ---- PTX ---------------------------------------------------------------------------------------------------------
 // In a pair, every copy reports to the FIRST CTA's barrier: its address is the local one with the CTA bit cleared.
@@ -342,8 +343,17 @@ struct MmParams {
   void* act_w;
   int64_t ld_act;
   float* partial;                // [warps of lanes][n_rows] shares of the pair weights' gradients
+  // Groups of *n_live rows each, group_rows apart, instead of offsets; their matrices follow one another in one (a_step rows each),
+  // and the rows' elements along all of them stand in panels of kPanel columns, one below the other, group_rows rows each.
+  const int32_t* n_live;         // (loss) rows that count
+  int group_rows;
+  int a_step;
+  int b_panel;                   // (products over rows) rows of a panel of B (0: no panels)
   // loss
-  const int32_t* n_live;         // rows that count
+  float* logits;                 // [n_live][ld_logits], kept where that is little
+  int64_t ld_logits;
+  int panel;                     // rows of a panel of dz
+  const int32_t* live;           // the rows that count
   const int32_t* targets;        // [..] by original row
   const float* row_weight;
   float2* part;                  // [column tiles][pitch] (maximum, sum) of a tile
@@ -352,6 +362,8 @@ struct MmParams {
   const float* lse;              // [n_live]
   const float* row_loss;         // [n_live]
   int column0;                   // first column's word
+  int tile_width;                // columns of a tile (0: BN)
+  uint32_t a_box;                // rows of a copy of A
   int32_t* dev_status;
   uint32_t wait_limit;
 };
@@ -362,7 +374,7 @@ enum MmForm {
   kRowsT,     // lanes: columns of W_e (MN-major); columns: sorted rows
   kSwiglu,    // as kRows, the lanes eight gate rows and eight up rows in turns
   kOuter,     // lanes, columns: columns of two matrices of rows (both MN-major); the contraction goes over a group's rows
-  kHead       // lanes: live rows (gathered, K-major); columns: rows of W
+  kHead       // lanes: rows (K-major); columns: rows of W
 };
 __host__ __device__ constexpr bool mm_a_mn(int form) { return form == kRowsT || form == kOuter; }
 __host__ __device__ constexpr bool mm_b_mn(int form) { return form == kOuter; }
@@ -385,7 +397,7 @@ struct MmTile {
   int m0;         // first lane's index (of the tile, not of the CTA)
   int n0;         // first column's index; for rows as columns: the sorted row
   int ncols;      // columns that exist
-  int row0, rows; // (contraction over rows) the group's rows
+  int row0, rows; // (contraction over rows) the group's rows; (kHead) number of the column tile, rows that count
   int kblocks;
   __device__ __forceinline__ MmTile uniform_copy() const {
     return {uniform(e), uniform(m0), uniform(n0), uniform(ncols), uniform(row0), uniform(rows), uniform(kblocks)};
@@ -396,11 +408,12 @@ template <int FORM, int CG, int BN>
 struct MmSchedule {
   const MmParams& p;
   const MmShared* s;
-  int m_tiles, n_tiles, e;
+  int m_tiles, n_tiles, width, e;
   __device__ MmSchedule(const MmParams& p_, const MmShared* s_) : p(p_), s(s_), e(0) {
     const int lanes = FORM == kHead ? s->cnt[0] : p.lanes;
     m_tiles = (lanes + 128 * CG - 1) / (128 * CG);
-    n_tiles = (p.columns + BN - 1) / BN;
+    width = FORM == kHead && p.tile_width ? p.tile_width : BN;
+    n_tiles = (p.columns + width - 1) / width;
   }
   // (tiles are asked for in ascending order)
   __device__ __forceinline__ MmTile get(int t) {
@@ -420,9 +433,9 @@ struct MmSchedule {
       const int nt = t / m_tiles;
       r.e = 0;
       r.m0 = (t - nt * m_tiles) * 128 * CG;
-      r.n0 = nt * BN;
-      r.ncols = min(BN, p.columns - r.n0);
-      r.row0 = 0;
+      r.n0 = nt * width;
+      r.ncols = min(width, p.columns - r.n0);
+      r.row0 = nt;
       r.rows = s->cnt[0];
       r.kblocks = (p.kdim + kMmK - 1) / kMmK;
     } else {
@@ -437,7 +450,7 @@ struct MmSchedule {
       r.ncols = min(width, cnt - j * width);
       r.row0 = r.n0;
       r.rows = r.ncols;
-      r.kblocks = (p.kdim + kMmK - 1) / kMmK;
+      r.kblocks = ((p.a_step ? min(p.a_step, p.kdim - e * p.a_step) : p.kdim) + kMmK - 1) / kMmK;
     }
     return r;
   }
@@ -485,8 +498,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     mbar_init(smem_u32(&s->drained), 1);
     s->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (FORM != kHead) tma_prefetch_map(&maps.a);
-    if (!GATHER || FORM == kHead || FORM == kOuter) tma_prefetch_map(&maps.b);
+    tma_prefetch_map(&maps.a);
+    if (!GATHER || FORM == kOuter) tma_prefetch_map(&maps.b);
   }
   if (warp == kWarpMma) mm_tmem_alloc<CG>(smem_u32(&s->tmem_base), kTmemCols);
   dx_pdl_wait();
@@ -499,6 +512,9 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       if (e < p.n_groups) {
         if (FORM == kHead) {
           hi = __ldg(p.n_live);
+        } else if (p.n_live) {
+          lo = e * p.group_rows;
+          hi = lo + __ldg(p.n_live);
         } else {
           lo = __ldg(p.offsets + e);
           hi = __ldg(p.offsets + e + 1);
@@ -534,7 +550,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   if (warp == kWarpA || (kTwo && warp == kWarpB)) {
     // ------------------------------------------------------------------------------------------------------ copies
     // (the one of them where only one operand comes by tensor map)
-    const bool for_a = FORM != kHead && warp == kWarpA, for_b = FORM == kHead || warp == kWarpB;
+    const bool for_a = warp == kWarpA, for_b = warp == kWarpB;
     uint32_t slot = 0, phase = 0, issued = 0;
     bool alive = true;
     for (int t = unit; t < total && alive; t += n_units) {
@@ -555,30 +571,42 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         const uint32_t bar = smem_u32(&s->full[slot]);
         const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
         if (elect_one()) {
-          if (rank == 0) mbar_arrive_expect_tx(bar, here ? (for_a ? (uint32_t)kMmA : nb * box) * CG : 0u);
+          if (rank == 0) mbar_arrive_expect_tx(bar, here ? (for_a ? (FORM == kHead ? p.a_box * 128u : (uint32_t)kMmA) : nb * box) * CG : 0u);
           if (here && for_a) {
             if constexpr (FORM == kRows) {
               tma3<CG>(da, &maps.a, k0, m0, tile.e, bar);
             } else if constexpr (FORM == kSwiglu) {
               tma5<CG>(da, &maps.a, k0, 0, 0, m0 / 16, tile.e, bar);
             } else if constexpr (FORM == kRowsT) {
-              tma3<CG>(da, &maps.a, m0, k0, tile.e, bar);
-              tma3<CG>(da + 8192u, &maps.a, m0 + 64, k0, tile.e, bar);
+              const int y = tile.e * p.a_step + k0, z = p.a_step ? 0 : tile.e;
+              tma3<CG>(da, &maps.a, m0, y, z, bar);
+              tma3<CG>(da + 8192u, &maps.a, m0 + 64, y, z, bar);
             } else if constexpr (FORM == kOuter) {
               tma2<CG>(da, &maps.a, m0, tile.row0 + k0, bar);
               tma2<CG>(da + 8192u, &maps.a, m0 + 64, tile.row0 + k0, bar);
+            } else {
+              tma2<CG>(da, &maps.a, k0, m0, bar);
             }
           }
           if (here && for_b) {
             if constexpr (FORM == kOuter) {
-              for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 8192u, &maps.b, n0 + 64 * j, tile.row0 + k0, bar);
+              const int x = p.b_panel ? n0 % kPanel : n0, y = p.b_panel ? n0 / kPanel * p.b_panel : 0;
+              for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 8192u, &maps.b, x + 64 * j, y + tile.row0 + k0, bar);
             } else if constexpr (FORM == kHead) {
 #pragma unroll
               for (int j = 0; j < kHalf / 128; ++j) tma2<CG>(db + j * 16384u, &maps.b, k0, p.column0 + n0 + 128 * j, bar);
-            } else if (big) {
-              for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 16384u, &maps.b, k0, n0 + 128 * j, bar);
             } else {
-              for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 4096u, &maps.b_few, k0, n0 + 32 * j, bar);
+              int x = k0, y = n0;
+              if (FORM == kRowsT && p.a_step) {
+                const int at = tile.e * p.a_step + k0;
+                x = at % kPanel;
+                y += (at / kPanel - tile.e) * p.group_rows;
+              }
+              if (big) {
+                for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 16384u, &maps.b, x, y + 128 * j, bar);
+              } else {
+                for (int j = 0; j < nb; ++j) tma2<CG>(db + j * 4096u, &maps.b_few, x, y + 32 * j, bar);
+              }
             }
           }
         }
@@ -605,15 +633,15 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     // where row 4 i + sub's piece goes: rows of one i parity share their place in the swizzle
     const uint32_t place[2] = {(uint32_t)(sub * 128 + ((piece ^ sub) << 4)), (uint32_t)(sub * 128 + ((piece ^ (4 + sub)) << 4))};
     // (what a copy of no bytes names as its source)
-    const unsigned char* zeros = reinterpret_cast<const unsigned char*>(FORM == kHead ? p.a_src : p.b_src);
+    const unsigned char* zeros = reinterpret_cast<const unsigned char*>(p.b_src);
     uint32_t base = 0;              // stages in front of the tile
     bool alive = true;
     for (int t = unit; t < total && alive; t += n_units) {
       const MmTile tile = schedule.get(t).uniform_copy();
       const int half = mm_width<CG>(tile.ncols) / CG, m0 = tile.m0 + (int)rank * 128;
       const int n0 = tile.n0 + (int)rank * half;
-      constexpr int kRegs = FORM == kHead ? 4 : FORM == kOuter ? 2 : (kHalf + 31) / 32;
-      const int here = FORM == kHead ? min(128, tile.rows - m0) : min(half, tile.ncols - (int)rank * half);  // rows as lanes / columns
+      constexpr int kRegs = FORM == kOuter ? 2 : (kHalf + 31) / 32;
+      const int here = min(half, tile.ncols - (int)rank * half);      // rows as columns
       // what this lane has looked up: a row's place in its matrix, in pieces of 16 bytes, and which lanes' rows exist
       uint32_t at_a[FORM == kOuter ? 2 : 1], at_b[kRegs], ok_a[FORM == kOuter ? 2 : 1], ok_b[kRegs];
       auto resolve = [&](int q, bool in, bool indexed, MmDiv div, int n_rows, int64_t ld, uint32_t& at, uint32_t& ok) {
@@ -639,14 +667,13 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         }
       };
       if constexpr (FORM != kOuter) {
-        const int32_t* index = FORM == kHead ? p.a_index + m0 : p.b_index + n0;
+        const int32_t* index = p.b_index + n0;
         int q[kRegs];
 #pragma unroll
         for (int j = 0; j < kRegs; ++j) q[j] = 32 * j + lane < here ? __ldg(index + 32 * j + lane) : 0;
 #pragma unroll
         for (int j = 0; j < kRegs; ++j)
-          resolve(q[j], 32 * j + lane < here, true, FORM == kHead ? MmDiv{0u, 0u} : p.b_div, FORM == kHead ? p.a_rows : p.b_rows,
-                  FORM == kHead ? p.a_ld : p.b_ld, at_b[j], ok_b[j]);
+          resolve(q[j], 32 * j + lane < here, true, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
       }
       // (products over rows: the rows of the warp's next stage are looked up a turn ahead)
       int next_a[2], next_b[2];
@@ -655,8 +682,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         for (int j = 0; j < 2; ++j) {
           const int r = k0 + 32 * j + lane;
           const bool in = r < tile.rows;
-          next_a[j] = in && p.a_index ? __ldg(p.a_index + tile.row0 + r) : tile.row0 + r;
-          next_b[j] = in && p.b_index ? __ldg(p.b_index + tile.row0 + r) : tile.row0 + r;
+          next_a[j] = in && p.a_index ? __ldg(p.a_index + tile.row0 + r) : 0;
+          next_b[j] = in && p.b_index ? __ldg(p.b_index + tile.row0 + r) : 0;
         }
       };
       const int first = (int)((uint32_t)(g - (int)base) & 3u);
@@ -670,10 +697,11 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
           if (do_a || do_b) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const bool in = k0 + 32 * j + lane < tile.rows;
-              resolve(next_a[j], in, p.a_index != nullptr, p.a_div, p.a_rows, p.a_ld, at_a[FORM == kOuter ? j : 0],
+              const int r = k0 + 32 * j + lane;
+              const bool in = r < tile.rows;
+              resolve(p.a_index ? next_a[j] : tile.row0 + r, in, p.a_index != nullptr, p.a_div, p.a_rows, p.a_ld, at_a[FORM == kOuter ? j : 0],
                       ok_a[FORM == kOuter ? j : 0]);
-              resolve(next_b[j], in, p.b_index != nullptr, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
+              resolve(p.b_index ? next_b[j] : tile.row0 + r, in, p.b_index != nullptr, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
             }
             ask(k0 + 4 * kMmK);
           }
@@ -694,7 +722,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             }
           }
           if (do_b) {
-            const unsigned char* from = reinterpret_cast<const unsigned char*>(p.b_src) + 2 * (int64_t)(n0 + 8 * piece);
+            const int64_t x = p.b_panel ? (int64_t)(n0 / kPanel) * p.b_panel * kPanel + n0 % kPanel : n0;
+            const unsigned char* from = reinterpret_cast<const unsigned char*>(p.b_src) + 2 * (x + 8 * piece);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               copy_rows(db + j * 4096u, from, at_b[j], ok_b[j], n0 + 8 * piece < p.columns, 0);
@@ -707,7 +736,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
           const unsigned char* from = zeros + 2 * (int64_t)(k0 + 8 * piece);
 #pragma unroll
           for (int j = 0; j < kRegs; ++j)
-            if (32 * j < here) copy_rows((FORM == kHead ? da : db) + j * 4096u, from, at_b[j], ok_b[j], in, 0);
+            if (32 * j < here) copy_rows(db + j * 4096u, from, at_b[j], ok_b[j], in, 0);
         }
         asm volatile("cp.async.wait_all;\n\tfence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -780,9 +809,10 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       tc_fence_after();
       const uint32_t base = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)buf * kAccCols;
       int c = kCols * share;
+      const int end = (tile.ncols + Epilogue::kRound - 1) / Epilogue::kRound * Epilogue::kRound;
       do {
-        if (c < tile.ncols) epi.load(base + (uint32_t)c, v);
-        if (c + 2 * kCols >= tile.ncols) {     // the accumulator may be written again
+        if (c < end) epi.load(base + (uint32_t)c, v);
+        if (c + 2 * kCols >= end) {            // the accumulator may be written again
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -790,9 +820,9 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             else mbar_arrive(smem_u32(&s->acc_empty[buf]));
           }
         }
-        if (c < tile.ncols) epi.chunk(tile, lane0, c, v);
+        if (c < end) epi.chunk(tile, lane0, c, v);
         c += 2 * kCols;
-      } while (c < tile.ncols);
+      } while (c < end);
       epi.end(tile);
       ++turn;
     }
