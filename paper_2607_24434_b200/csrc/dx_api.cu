@@ -1037,6 +1037,10 @@ extern "C" dx_status moe_grouped_mm_dw(dx_ctx* ctx, const dx_grouped_desc* desc,
   const Range out = groups_range(desc, dw, elem);
   if (overlap(out, rows_range(x, x_rows, desc->k, ldx, 2)) || overlap(out, rows_range(dy, dy_rows, desc->n, ld_dy, 2)))
     return DX_ERR_INVALID_ARG;
+  if (desc->n_rows > 0) {
+    if (!offsets) return DX_ERR_INVALID_ARG;
+    if (dy_rows < (gather_dy ? 1 : desc->n_rows) || x_rows < (gather_x ? 1 : desc->n_rows)) return DX_ERR_SHAPE;
+  }
   DeviceScope scope(ctx->device);
   DX_CUDA(ctx, scope.err);
   if (desc->n_rows == 0) {   // every group is empty
@@ -1045,8 +1049,6 @@ extern "C" dx_status moe_grouped_mm_dw(dx_ctx* ctx, const dx_grouped_desc* desc,
                                      desc->ld_w * elem, 0, desc->k * elem, desc->n, (cudaStream_t)stream));
     return DX_OK;
   }
-  if (!offsets) return DX_ERR_INVALID_ARG;
-  if (dy_rows < (gather_dy ? 1 : desc->n_rows) || x_rows < (gather_x ? 1 : desc->n_rows)) return DX_ERR_SHAPE;
   DxGroupedDw a = {};
   a.dy = dy; a.dy_rows = dy_rows; a.ld_dy = ld_dy; a.gather_dy = gather_dy; a.dy_div = dy_div;
   a.x = x; a.x_rows = x_rows; a.ldx = ldx; a.gather_x = gather_x; a.x_div = x_div;
@@ -1228,15 +1230,17 @@ extern "C" dx_status spec_head_loss(dx_ctx* ctx, const void* h, int32_t N, int64
   for (const Range& o : out)
     for (const Range& i : in)
       if (overlap(o, i)) return DX_ERR_INVALID_ARG;
+  size_t least = 0, best = 0;
+  if (N > 0) {
+    dx_head_loss_workspace(ctx->sm_count, N, V, H, dh || dW, &least, &best);
+    if (!targets || !workspace || (uintptr_t)workspace % 256 || workspace_bytes < least) return DX_ERR_INVALID_ARG;
+  }
   DeviceScope scope(ctx->device);
   DX_CUDA(ctx, scope.err);
   if (N == 0) {
     if (dW) DX_CUDA(ctx, cudaMemset2DAsync(dW, ld_dW * 2, 0, (size_t)H * 2, V, (cudaStream_t)stream));
     return DX_OK;
   }
-  size_t least = 0, best = 0;
-  dx_head_loss_workspace(ctx->sm_count, N, V, H, dh || dW, &least, &best);
-  if (!targets || !workspace || (uintptr_t)workspace % 256 || workspace_bytes < least) return DX_ERR_INVALID_ARG;
   DxHeadLoss a = {};
   a.h = h; a.ldh = ldh; a.W = W_lm; a.ldw = ldw; a.N = N; a.V = V; a.H = H;
   a.targets = targets; a.row_weight = row_weight; a.loss = loss;

@@ -382,11 +382,11 @@ namespace {
 
 // Few rows per group: the weights' bytes are the time, so tiles are small (128 lanes: twice as many CTAs have one, and eight
 // stages of 24 KB keep 128 KB of weights in flight per SM).  Otherwise pairs of CTAs with 256 lanes x 256 columns.
-bool few_rows(const dx_ctx* ctx, int64_t rows, int groups) { return rows <= 32 * (int64_t)groups; }
+bool few_rows(int64_t rows, int groups) { return rows <= 32 * (int64_t)groups; }
 
 template <int FORM, class Epilogue>
 cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cudaStream_t st) {
-  const bool few = few_rows(ctx, p.n_rows, p.n_groups);
+  const bool few = few_rows(p.n_rows, p.n_groups);
   const long long lanes = few ? 128 : 256, bn = few ? 64 : 256;
   // (every group may end in a tile that is not full)
   const long long most = ((p.lanes + lanes - 1) / lanes) *

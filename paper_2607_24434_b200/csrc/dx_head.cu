@@ -163,10 +163,12 @@ __global__ void __launch_bounds__(1024) dx_head_join_kernel(const float2* part, 
                                                            float* lse, float* row_loss, const int32_t* targets,
                                                            const float* row_weight, int N, int V, int H,
                                                            __nv_bfloat16* dh, int64_t ld_dh) {
-  __shared__ float tops[32][33], sums[32][33];
+  __shared__ float tops[32][32];
+  __shared__ double sums[32][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
   const int n_live = __ldg(n_live_at);
-  float top = -INFINITY, sum = 0.0f;
+  float top = -INFINITY;
+  double sum = 0.0;        // (hundreds of tiles: their additions would be the largest error of the loss)
   if (row < n_live) {
     for (int i = warp; i < tiles; i += 256) {     // (eight of them under way at a time)
       float2 q[8];
@@ -191,10 +193,10 @@ __global__ void __launch_bounds__(1024) dx_head_join_kernel(const float2* part, 
 #pragma unroll
     for (int w = 1; w < 32; ++w) m = fmaxf(m, tops[w][lane]);
     const float from = m == -INFINITY ? 0.0f : m;
-    float s = 0.0f;
+    double s = 0.0;
 #pragma unroll
     for (int w = 0; w < 32; ++w) s += sums[w][lane] * ex2((tops[w][lane] - from) * kLog2e);
-    const double log_sum = log((double)s);
+    const double log_sum = log(s);
     const float l = (float)(((double)m - (double)target_logit[row]) + log_sum);
     if (loss) loss[live[row]] = l;
     lse[row] = (float)((double)m + log_sum);
@@ -310,8 +312,9 @@ struct HeadPlan {
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // `space`: bytes there are (0: as many as are of use)
-HeadPlan head_plan(const int sm_count, int N, int V, int H, bool grad, size_t space) {
+HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
   HeadPlan s = {};
+  if (sm_count < 2) sm_count = 2;
   const int64_t words = ((int64_t)V + 255) / 256 * 256;
   size_t at = 0;
   auto take = [&](size_t bytes) {

@@ -35,6 +35,7 @@ __host__ __device__ constexpr int mm_threads(bool gather) { return gather ? 512 
 constexpr int kMmK = 64;                    // contraction elements of a stage: 128 bytes of a row
 constexpr int kMmA = 128 * kMmK * 2;        // bytes of a CTA's 128 rows of A in a stage
 constexpr int kMmMaxStages = 8;
+constexpr uint32_t kDrainPolls = 1u << 16;  // of a barrier that may never complete, after something gave up
 constexpr int kPanel = 256;                 // columns of a panel: a tile's, so that a tile's rows lie close together
 
 // ---- PTX ---------------------------------------------------------------------------------------------------------
@@ -615,14 +616,19 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         if (++slot == STAGES) { slot = 0; phase ^= 1u; }
       }
     }
-    if (rank == 0 && warp == kWarpA && lane == 0 && *abort_flag) {
-      // something gave up: no copy may still be landing when the shared memory is released
-      const uint32_t back = issued < STAGES ? issued : STAGES;
-      for (uint32_t k = 1; k <= back; ++k) {
-        const uint32_t j = issued - k;
-        for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
-          if (mbar_try_wait(smem_u32(&s->full[j % STAGES]), (j / STAGES) & 1u)) break;
+    if (*abort_flag) {
+      // Something gave up: no copy may still be landing when the shared memory (and in a pair the first CTA's barriers) is
+      // released.  Stages that both operands were asked for complete on their barriers; for one that only one operand was asked
+      // for there is nothing to wait on, so the rest is time, a thousand times what a copy takes.
+      if (rank == 0 && warp == kWarpA) {
+        const uint32_t back = issued < STAGES ? issued : STAGES;
+        for (uint32_t k = 1; k <= back; ++k) {
+          const uint32_t j = issued - k;
+          for (uint32_t spin = 0; spin < kDrainPolls; ++spin)
+            if (mbar_try_wait(smem_u32(&s->full[j % STAGES]), (j / STAGES) & 1u)) break;
+        }
       }
+      for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
   } else if (GATHER && warp >= kWarpGather) {
     // ----------------------------------------------------------------------------------------------- gathered rows
