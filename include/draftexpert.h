@@ -128,7 +128,7 @@ dx_status dx_last_device_status(dx_ctx* ctx, void* stream, int32_t* dev_status_o
 dx_status dx_set_activation_split(dx_ctx* ctx, int32_t on);
 /* Which kernels are launched so that they may begin while the kernel in front of them on the stream drains
  * (programmatic stream serialization): bit 0 the routing kernel and the second kernel of moe_route_tokens, bit 1 the
- * expert kernels, bit 2 the greedy-accept kernels.  Default 3.  0 gives plain stream order everywhere; results never
+ * expert kernels (and those of moe_grouped_*, moe_combine_* and spec_head_loss), bit 2 the greedy-accept kernels.  Default 3.  0 gives plain stream order everywhere; results never
  * depend on the mask. */
 dx_status dx_set_launch_overlap(dx_ctx* ctx, int32_t mask);
 /* Every wait inside a kernel (for a word another kernel publishes, for a copy into shared memory, for the other CTAs

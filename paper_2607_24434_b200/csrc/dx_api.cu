@@ -1171,7 +1171,7 @@ extern "C" dx_status moe_combine_tokens(dx_ctx* ctx, const void* z, int32_t z_dt
     return DX_ERR_INVALID_ARG;
   DeviceScope scope(ctx->device);
   DX_CUDA(ctx, scope.err);
-  DX_CUDA(ctx, dx_launch_combine(z, z32, ldz, topk_w, N, top_k, H, y, y32, ldy, (cudaStream_t)stream));
+  DX_CUDA(ctx, dx_launch_combine(ctx, z, z32, ldz, topk_w, N, top_k, H, y, y32, ldy, (cudaStream_t)stream));
   ctx->launches++;
   return DX_OK;
 }
@@ -1194,7 +1194,7 @@ extern "C" dx_status moe_combine_tokens_backward(dx_ctx* ctx, const void* dy, in
     return DX_ERR_INVALID_ARG;
   DeviceScope scope(ctx->device);
   DX_CUDA(ctx, scope.err);
-  DX_CUDA(ctx, dx_launch_combine_grad(dy, z, dtype == DX_DTYPE_FP32, ld_dy, ldz, topk_w, N, top_k, H, dz, ld_dz, d_topk_w,
+  DX_CUDA(ctx, dx_launch_combine_grad(ctx, dy, z, dtype == DX_DTYPE_FP32, ld_dy, ldz, topk_w, N, top_k, H, dz, ld_dz, d_topk_w,
                                       (cudaStream_t)stream));
   ctx->launches++;
   return DX_OK;

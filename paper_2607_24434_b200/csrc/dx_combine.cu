@@ -50,6 +50,8 @@ template <class Tz, class Ty, int K>
 __global__ void __launch_bounds__(256) dx_combine_kernel(const Tz* z, int64_t ldz, const float* w, int n_tokens, int pieces,
                                                          Ty* y, int64_t ldy) {
   constexpr int kN = Piece<Tz>::kN;
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int t = blockIdx.x * blockDim.y + threadIdx.y;
   if (t >= n_tokens) return;
   float weight[K];
@@ -81,6 +83,8 @@ __global__ void __launch_bounds__(256) dx_combine_grad_kernel(const T* dy, int64
                                                               float* dw) {
   constexpr int kN = Piece<T>::kN;
   __shared__ float share[8][K];
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = blockIdx.x * (8 / WARPS) + warp / WARPS, part = warp % WARPS;
   float sum[K] = {};
@@ -133,26 +137,25 @@ __global__ void __launch_bounds__(256) dx_combine_grad_kernel(const T* dy, int64
 }
 
 template <class Tz, class Ty, int K>
-cudaError_t combine(const void* z, int64_t ldz, const float* w, int n, int H, void* y, int64_t ldy, cudaStream_t st) {
+cudaError_t combine(bool pdl, const void* z, int64_t ldz, const float* w, int n, int H, void* y, int64_t ldy, cudaStream_t st) {
   const int pieces = H / Piece<Tz>::kN;
   int along = 8;
   while (along < pieces && along < 256) along *= 2;
   const dim3 block(along, 256 / along);
-  dx_combine_kernel<Tz, Ty, K><<<(n + block.y - 1) / block.y, block, 0, st>>>(
-      reinterpret_cast<const Tz*>(z), ldz, w, n, pieces, reinterpret_cast<Ty*>(y), ldy);
-  return cudaGetLastError();
+  return dx_launch_pdl(pdl, dx_combine_kernel<Tz, Ty, K>, dim3((n + block.y - 1) / block.y), block, 0, st, 1,
+                       reinterpret_cast<const Tz*>(z), ldz, w, n, pieces, reinterpret_cast<Ty*>(y), ldy);
 }
 template <class T, int K>
-cudaError_t combine_grad(const void* dy, const void* z, int64_t ld_dy, int64_t ldz, const float* w, int n, int H, void* dz,
+cudaError_t combine_grad(bool pdl, const void* dy, const void* z, int64_t ld_dy, int64_t ldz, const float* w, int n, int H, void* dz,
                          int64_t ld_dz, float* dw, cudaStream_t st) {
   const int pieces = H / Piece<T>::kN;
   const T *d = reinterpret_cast<const T*>(dy), *x = reinterpret_cast<const T*>(z);
   T* o = reinterpret_cast<T*>(dz);
   if (n < 2048 && pieces > 32)
-    dx_combine_grad_kernel<T, K, 8><<<n, 256, 0, st>>>(d, ld_dy, x, ldz, w, n, pieces, o, ld_dz, dw);
-  else
-    dx_combine_grad_kernel<T, K, 1><<<(n + 7) / 8, 256, 0, st>>>(d, ld_dy, x, ldz, w, n, pieces, o, ld_dz, dw);
-  return cudaGetLastError();
+    return dx_launch_pdl(pdl, dx_combine_grad_kernel<T, K, 8>, dim3(n), dim3(256), 0, st, 1, d, ld_dy, x, ldz, w, n, pieces, o,
+                         ld_dz, dw);
+  return dx_launch_pdl(pdl, dx_combine_grad_kernel<T, K, 1>, dim3((n + 7) / 8), dim3(256), 0, st, 1, d, ld_dy, x, ldz, w, n,
+                       pieces, o, ld_dz, dw);
 }
 // f(the number of rows of a token as a constant)
 template <class F>
@@ -172,21 +175,23 @@ static_assert(DX_MAX_TOPK == 8);
 
 }  // namespace
 
-cudaError_t dx_launch_combine(const void* z, int fp32, int64_t ldz, const float* w, int n_tokens, int k, int H, void* y,
+cudaError_t dx_launch_combine(dx_ctx* ctx, const void* z, int fp32, int64_t ldz, const float* w, int n_tokens, int k, int H, void* y,
                               int y_fp32, int64_t ldy, cudaStream_t st) {
+  const bool pdl = (ctx->pdl_mask & DX_PDL_EXPERTS) != 0;
   return with_k(k, [&](auto K) {
     if (fp32)
-      return y_fp32 ? combine<float, float, K.value>(z, ldz, w, n_tokens, H, y, ldy, st)
-                    : combine<float, __nv_bfloat16, K.value>(z, ldz, w, n_tokens, H, y, ldy, st);
-    return y_fp32 ? combine<__nv_bfloat16, float, K.value>(z, ldz, w, n_tokens, H, y, ldy, st)
-                  : combine<__nv_bfloat16, __nv_bfloat16, K.value>(z, ldz, w, n_tokens, H, y, ldy, st);
+      return y_fp32 ? combine<float, float, K.value>(pdl, z, ldz, w, n_tokens, H, y, ldy, st)
+                    : combine<float, __nv_bfloat16, K.value>(pdl, z, ldz, w, n_tokens, H, y, ldy, st);
+    return y_fp32 ? combine<__nv_bfloat16, float, K.value>(pdl, z, ldz, w, n_tokens, H, y, ldy, st)
+                  : combine<__nv_bfloat16, __nv_bfloat16, K.value>(pdl, z, ldz, w, n_tokens, H, y, ldy, st);
   });
 }
 
-cudaError_t dx_launch_combine_grad(const void* dy, const void* z, int fp32, int64_t ld_dy, int64_t ldz, const float* w,
+cudaError_t dx_launch_combine_grad(dx_ctx* ctx, const void* dy, const void* z, int fp32, int64_t ld_dy, int64_t ldz, const float* w,
                                    int n_tokens, int k, int H, void* dz, int64_t ld_dz, float* dw, cudaStream_t st) {
+  const bool pdl = (ctx->pdl_mask & DX_PDL_EXPERTS) != 0;
   return with_k(k, [&](auto K) {
-    return fp32 ? combine_grad<float, K.value>(dy, z, ld_dy, ldz, w, n_tokens, H, dz, ld_dz, dw, st)
-                : combine_grad<__nv_bfloat16, K.value>(dy, z, ld_dy, ldz, w, n_tokens, H, dz, ld_dz, dw, st);
+    return fp32 ? combine_grad<float, K.value>(pdl, dy, z, ld_dy, ldz, w, n_tokens, H, dz, ld_dz, dw, st)
+                : combine_grad<__nv_bfloat16, K.value>(pdl, dy, z, ld_dy, ldz, w, n_tokens, H, dz, ld_dz, dw, st);
   });
 }

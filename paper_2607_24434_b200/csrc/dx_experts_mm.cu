@@ -5,6 +5,8 @@
 // In all of them the LANES of a tile are the contiguous dimension of the output and its COLUMNS the output's rows: weights
 // are the fixed 128 lanes of a CTA, and the ragged number of an expert's rows is the width of the products, which
 // tcgen05.mma takes in steps of 16 -- a group of 5 rows costs 16 columns, not 128.
+#include <limits.h>
+
 #include "dx_mm.cuh"
 
 namespace {
@@ -44,19 +46,10 @@ __device__ __forceinline__ void stage_fp32(uint32_t at, int lane, const Fragment
         sts4(mine + (uint32_t)((8 * n + (q & 1)) * kColumn32 + (16 * h + 8 * (q >> 1)) * 4), x.v[h][4 * n + q]);
 }
 
-// sorted row of a chunk's column `c0 + lane` (-1: none), and the row of the output it goes to
+// sorted row of a chunk's column `c0 + lane` (-1: none)
 __device__ __forceinline__ int sorted_row(const MmTile& t, int c0, int lane) {
   return c0 + lane < t.ncols ? t.n0 + c0 + lane : -1;
 }
-template <int COLS>
-__device__ __forceinline__ int scattered(const MmParams& p, int row, int lane) {
-  if (row < 0 || !p.scatter || lane >= COLS) return row;
-  const int to = __ldg(p.scatter + row);
-  if (to >= 0 && to < p.out_rows) return to;
-  atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
-  return -1;
-}
-
 template <int COLS>
 struct FragmentEpilogue {
   static constexpr int kCols = COLS, kRound = 1;
@@ -70,21 +63,25 @@ struct FragmentEpilogue {
 #pragma unroll
     for (int i = 0; i < COLS / 2; ++i) x.v[0][i] = x.v[1][i] = 0.0f;
   }
-  __device__ __forceinline__ void begin(const MmTile&, int, int) {}
+  __device__ __forceinline__ void begin(const MmTile&, int, int, const MmTile&, bool) {}
   __device__ __forceinline__ void end(const MmTile&) {}
 };
 
 // Staged columns (bf16) to rows `mine` (of lane = column) of a matrix; m: first of the warp's 32 elements in a row.
+// (First all reads, then all writes: a read and the write of what it brought would each wait for the one in front.)
 template <int COLS>
 __device__ __forceinline__ void flush_bf16(const MmParams& p, int lane, uint32_t at, int mine, int m, __nv_bfloat16* out,
                                            int64_t ld) {
   const int piece = lane & 3, x = m + 8 * piece;
+  uint4 u[COLS / 8];
+  int row[COLS / 8];
 #pragma unroll
-  for (int i = 0; i < COLS / 8; ++i) {
-    const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
-    const uint4 u = lds16(at + piece64(column, piece));
-    if (row >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(out + (int64_t)row * ld + x) = u;
-  }
+  for (int i = 0; i < COLS / 8; ++i) u[i] = lds16(at + piece64(8 * i + (lane >> 2), piece));
+#pragma unroll
+  for (int i = 0; i < COLS / 8; ++i) row[i] = __shfl_sync(0xffffffffu, mine, 8 * i + (lane >> 2));
+#pragma unroll
+  for (int i = 0; i < COLS / 8; ++i)
+    if (row[i] >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(out + (int64_t)row[i] * ld + x) = u[i];
 }
 template <class T, bool ADD, int COLS>
 __device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_t at, const Fragments<COLS>& v, int mine, int m,
@@ -97,19 +94,24 @@ __device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_
     stage_fp32(at, lane, v);
     __syncwarp();
     const int x = m + 4 * (lane & 7);
+    uint4 u[COLS / 4];
+    float4 a[COLS / 4];
+    int row[COLS / 4];
+#pragma unroll
+    for (int i = 0; i < COLS / 4; ++i) row[i] = __shfl_sync(0xffffffffu, mine, 4 * i + (lane >> 3));
 #pragma unroll
     for (int i = 0; i < COLS / 4; ++i) {
-      const int column = 4 * i + (lane >> 3), row = __shfl_sync(0xffffffffu, mine, column);
-      const uint4 u = lds16(at + (uint32_t)(column * kColumn32 + (lane & 7) * 16));
-      if (row >= 0 && x < p.lanes) {
-        float4 f = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
-        if constexpr (ADD) {
-          const float4 a = *reinterpret_cast<const float4*>(p.addend + (int64_t)row * p.lanes + x);
-          f = make_float4(f.x + a.x, f.y + a.y, f.z + a.z, f.w + a.w);
-        }
-        *reinterpret_cast<float4*>(out + (int64_t)row * ld + x) = f;
-      }
+      a[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (ADD && row[i] >= 0 && x < p.lanes) a[i] = *reinterpret_cast<const float4*>(p.addend + (int64_t)row[i] * p.lanes + x);
     }
+#pragma unroll
+    for (int i = 0; i < COLS / 4; ++i) u[i] = lds16(at + (uint32_t)((4 * i + (lane >> 3)) * kColumn32 + (lane & 7) * 16));
+#pragma unroll
+    for (int i = 0; i < COLS / 4; ++i)
+      if (row[i] >= 0 && x < p.lanes)
+        *reinterpret_cast<float4*>(out + (int64_t)row[i] * ld + x) =
+            make_float4(__uint_as_float(u[i].x) + a[i].x, __uint_as_float(u[i].y) + a[i].y, __uint_as_float(u[i].z) + a[i].z,
+                        __uint_as_float(u[i].w) + a[i].w);
   } else {      // (summed in fp32, then rounded)
     stage_fp32(at, lane, v);
     __syncwarp();
@@ -143,8 +145,19 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
   using Base = FragmentEpilogue<store_cols<T, ADD>()>;
   static constexpr int kStaging = store_staging<T, ADD>();
   using Base::Base;
+  int next;      // where column `lane` of the next chunk goes (looked up a chunk ahead)
+  __device__ __forceinline__ void look_up(const MmTile& t, int c0) {
+    const int row = this->lane < Base::kCols ? sorted_row(t, c0, this->lane) : -1;
+    next = row >= 0 && this->p.scatter ? __ldg(this->p.scatter + row) : row;
+  }
+  __device__ __forceinline__ void begin(const MmTile& t, int, int c0, const MmTile&, bool) { look_up(t, c0); }
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x) {
-    const int mine = scattered<Base::kCols>(this->p, sorted_row(t, c0, this->lane), this->lane);
+    int mine = next;
+    if (this->p.scatter && this->lane < Base::kCols && sorted_row(t, c0, this->lane) >= 0 && (mine < 0 || mine >= this->p.out_rows)) {
+      atomicExch(this->p.dev_status, (int32_t)DX_DEV_BAD_ROW);
+      mine = -1;
+    }
+    look_up(t, c0 + 2 * Base::kCols);
     store_chunk<T, ADD>(this->p, this->lane, this->at, x, mine, lane0, reinterpret_cast<T*>(this->p.out), this->p.ld);
   }
 };
@@ -170,7 +183,7 @@ struct StoreSwiglu : FragmentEpilogue<32> {
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
     const float(&v)[2][16] = x.v;
     const int n_inter = p.lanes >> 1, i0 = lane0 >> 1;      // the warp's 16 elements
-    const int mine = sorted_row(t, c0, lane);
+    const int left = t.ncols - c0;
     if constexpr (SAVE) {
 #pragma unroll
       for (int n = 0; n < 4; ++n)     // per column: sixteen gates, sixteen ups
@@ -179,12 +192,13 @@ struct StoreSwiglu : FragmentEpilogue<32> {
       __syncwarp();
       const int piece = lane & 3, i = i0 + 8 * (piece & 1);
       __nv_bfloat16* save = reinterpret_cast<__nv_bfloat16*>(p.save) + (piece >> 1) * (int64_t)n_inter + i;
+      save += (int64_t)(t.n0 + c0 + (lane >> 2)) * p.ld_save;
+      uint4 u[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int column = 8 * k + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
-        const uint4 u = lds16(at + piece64(column, piece));
-        if (row >= 0 && i < n_inter) *reinterpret_cast<uint4*>(save + (int64_t)row * p.ld_save) = u;
-      }
+      for (int k = 0; k < 4; ++k) u[k] = lds16(at + piece64(8 * k + (lane >> 2), piece));
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (8 * k + (lane >> 2) < left && i < n_inter) *reinterpret_cast<uint4*>(save + (int64_t)(8 * k) * p.ld_save) = u[k];
       __syncwarp();
     }
     uint32_t a[2][4];
@@ -202,13 +216,16 @@ struct StoreSwiglu : FragmentEpilogue<32> {
     }
     __syncwarp();
     const int h = lane & 1, i = i0 + 8 * h;
+    __nv_bfloat16* act = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)(t.n0 + c0 + (lane >> 1)) * p.ld + i;
+    uint4 u[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int column = 16 * k + (lane >> 1), row = __shfl_sync(0xffffffffu, mine, column);
-      const uint4 u = lds16(at + (uint32_t)(column * 32 + ((h ^ ((column >> 2) & 1)) << 4)));
-      if (row >= 0 && i < n_inter)
-        *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)row * p.ld + i) = u;
+      const int column = 16 * k + (lane >> 1);
+      u[k] = lds16(at + (uint32_t)(column * 32 + ((h ^ ((column >> 2) & 1)) << 4)));
     }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (16 * k + (lane >> 1) < left && i < n_inter) *reinterpret_cast<uint4*>(act + (int64_t)(16 * k) * p.ld) = u[k];
     __syncwarp();
   }
 };
@@ -218,11 +235,11 @@ struct StoreSwiglu : FragmentEpilogue<32> {
 // A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come in 16-byte pieces, a chunk ahead; their
 // place in the staging takes the gradients.
 struct StoreSwigluGrad : FragmentEpilogue<16> {
-  static constexpr int kArea = 16 * 64, kStaging = 3 * kArea;
+  static constexpr int kArea = 16 * 64, kStaging = 3 * kArea + 512;      // (three areas; the weights of 128 columns)
   uint4 gate[2], up[2];
-  float weight;      // of column `lane`
+  const int share;
   __device__ StoreSwigluGrad(const MmParams& p_, int lane_, int share_, uint32_t at_)
-      : FragmentEpilogue<16>(p_, lane_, share_, at_) {}
+      : FragmentEpilogue<16>(p_, lane_, share_, at_), share(share_) {}
   __device__ __forceinline__ void fetch(const MmTile& t, int lane0, int c0) {
     const int x = lane0 + 8 * (lane & 3);
     const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.gate_up) +
@@ -234,19 +251,51 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       gate[i] = in ? __ldcs(g) : make_uint4(0u, 0u, 0u, 0u);
       up[i] = in ? __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * p.ld_gate_up + p.lanes)) : make_uint4(0u, 0u, 0u, 0u);
     }
-    const int mine = lane < 16 ? sorted_row(t, c0, lane) : -1;
-    weight = 0.0f;
-    if (mine >= 0) {
-      const int q = p.b_index ? __ldg(p.b_index + mine) : mine;
-      if (q >= 0 && q < p.n_pairs) weight = p.pair_w ? __ldg(p.pair_w + q) : 1.0f;
-      else atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
+  }
+  // The weights of the warp's share of a tile's columns, all at once.  An index and the weight behind it are two trips to L2, gate
+  // and up one to memory: they are asked for while the tile in front is still being stored.
+  MmTile next;
+  bool more;
+  int q[4];
+  float w4[4];
+  __device__ __forceinline__ void ask_pairs(const MmTile& t) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {        // 16 columns of every 32
+      const int r = sorted_row(t, 32 * (2 * j + (lane >> 4)) + 16 * share, lane & 15);
+      q[j] = r < 0 ? INT_MIN : p.b_index ? __ldg(p.b_index + r) : r;
     }
   }
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int c0) {
-    if (c0 < t.ncols) fetch(t, lane0, c0);
+  __device__ __forceinline__ void ask_weights() {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool in = q[j] >= 0 && q[j] < p.n_pairs;
+      w4[j] = !in ? 0.0f : p.pair_w ? __ldg(p.pair_w + q[j]) : 1.0f;
+      if (!in && q[j] != INT_MIN) atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
+    }
+  }
+  bool first = true;
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int c0, const MmTile& next_, bool more_) {
+    if (first) {
+      ask_pairs(t);
+      if (c0 < t.ncols) fetch(t, lane0, c0);
+      ask_weights();
+      first = false;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sts4(at + 3 * kArea + (uint32_t)(32 * j + lane) * 4, w4[j]);
+    __syncwarp();
+    next = next_;
+    more = more_;
+    if (more) ask_pairs(next);
+    if (c0 >= t.ncols) ask_next(t, lane0);        // (no chunk of this tile is the warp's)
+  }
+  __device__ __forceinline__ void ask_next(const MmTile& t, int lane0) {
+    if (!more) return;
+    ask_weights();
+    if (kCols * share < next.ncols) fetch(next, next.m0 + lane0 - t.m0, kCols * share);
   }
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
-    const int mine = sorted_row(t, c0, lane);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t to = at + piece64(8 * i + (lane >> 2), lane & 3);
@@ -261,14 +310,16 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       const uint32_t from = at + piece64(8 * n + (lane & 7), lane >> 3);
       ldmatrix_t(from, g4[n]);
       ldmatrix_t(from + kArea, u4[n]);
-      const float w0 = __shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3));
-      const float w1 = __shfl_sync(0xffffffffu, weight, 8 * n + 2 * (lane & 3) + 1);
+      const uint32_t from_w = at + 3 * kArea + (uint32_t)((c0 >> 5) * 16 + 8 * n + 2 * (lane & 3)) * 4;
+      float w0, w1;
+      asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(w0), "=f"(w1) : "r"(from_w) : "memory");
       w[n] = f2(w0, w1);
       mask[n] = (w0 != 0.0f ? 0xffffu : 0u) | (w1 != 0.0f ? 0xffff0000u : 0u);
       dw2[n] = f2(0.0f, 0.0f);
     }
     __syncwarp();
     if (c0 + 2 * kCols < t.ncols) fetch(t, lane0, c0 + 2 * kCols);
+    else ask_next(t, lane0);
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -288,24 +339,39 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
         a4[n][j] = bf16_pair(f2_mul(w[n], act)) & mask[n];
         if (lane0 + 8 * j < p.lanes) dw2[n] = f2_fma(d1, act, dw2[n]);
       }
-    float dw[4];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      f2_get(dw2[n], dw[2 * n], dw[2 * n + 1]);
-      if (!(mask[n] & 0xffffu)) dw[2 * n] = 0.0f;
-      if (!(mask[n] >> 16)) dw[2 * n + 1] = 0.0f;
       stage64(at, lane, n, g4[n][0], g4[n][1], g4[n][2], g4[n][3]);
       stage64(at + kArea, lane, n, u4[n][0], u4[n][1], u4[n][2], u4[n][3]);
       stage64(at + 2 * kArea, lane, n, a4[n][0], a4[n][1], a4[n][2], a4[n][3]);
     }
     __syncwarp();
-    __nv_bfloat16* d_gate_up = reinterpret_cast<__nv_bfloat16*>(p.out);
-    flush_bf16<16>(p, lane, at, mine, lane0, d_gate_up, p.ld);
-    flush_bf16<16>(p, lane, at + kArea, mine, lane0, d_gate_up + p.lanes, p.ld);
-    flush_bf16<16>(p, lane, at + 2 * kArea, mine, lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
-    __syncwarp();
+    uint4 out[3][2];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) out[k][i] = lds16(at + k * kArea + piece64(8 * i + (lane >> 2), lane & 3));
+    const int m = lane0 + 8 * (lane & 3);
+    const int64_t row = t.n0 + c0 + (lane >> 2);
+    __nv_bfloat16* d_gate = reinterpret_cast<__nv_bfloat16*>(p.out) + row * p.ld + m;
+    __nv_bfloat16* act_w = reinterpret_cast<__nv_bfloat16*>(p.act_w) + row * p.ld_act + m;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (c0 + 8 * i + (lane >> 2) < t.ncols && m < p.lanes) {
+        *reinterpret_cast<uint4*>(d_gate + (int64_t)(8 * i) * p.ld) = out[0][i];
+        *reinterpret_cast<uint4*>(d_gate + (int64_t)(8 * i) * p.ld + p.lanes) = out[1][i];
+        *reinterpret_cast<uint4*>(act_w + (int64_t)(8 * i) * p.ld_act) = out[2][i];
+      }
+    }
     if (p.partial) {
       // eight threads (t / 4) hold shares of the columns 8 n + 2 (t % 4) + i: folded so that two of them each end with one
+      float dw[4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        f2_get(dw2[n], dw[2 * n], dw[2 * n + 1]);
+        if (!(mask[n] & 0xffffu)) dw[2 * n] = 0.0f;
+        if (!(mask[n] >> 16)) dw[2 * n + 1] = 0.0f;
+      }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int h = 2 >> b, bit = 16 >> b;
@@ -320,6 +386,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       const int k = lane >> 3, column = c0 + 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
       if (!(lane & 4) && column < t.ncols) p.partial[(int64_t)(lane0 >> 5) * p.n_rows + t.n0 + column] = dw[0];
     }
+    __syncwarp();      // (the staging is written again)
   }
 };
 
@@ -327,6 +394,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
 __global__ void __launch_bounds__(256) dx_pair_weight_grad_kernel(const float* partial, int parts, int n_rows,
                                                                   const int32_t* offsets, int n_groups,
                                                                   const int32_t* index, int n_pairs, float* d_pair_w) {
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int r = blockIdx.x * 256 + threadIdx.x;
   const int lo = max(0, __ldg(offsets)), hi = min(n_rows, __ldg(offsets + n_groups));
   if (r < lo || r >= hi) return;
@@ -506,10 +575,9 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   if (e != cudaSuccess || !d_pair_w) return e;
   // (lanes of a tile behind the last are no shares: only warps with lanes that exist wrote theirs)
   const int parts = (a.k + 31) / 32;
-  dx_pair_weight_grad_kernel<<<(a.n_rows + 255) / 256, 256, 0, st>>>(partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather,
-                                                                     n_pairs, d_pair_w);
   *n_launches = 2;
-  return cudaGetLastError();
+  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, dx_pair_weight_grad_kernel, dim3((a.n_rows + 255) / 256), dim3(256), 0,
+                       st, 1, partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather, n_pairs, d_pair_w);
 }
 
 cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t st) {

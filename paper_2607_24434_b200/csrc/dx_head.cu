@@ -31,6 +31,8 @@ __global__ void __launch_bounds__(1024) dx_head_rows_kernel(const int32_t* targe
                                                             int32_t* live, int32_t* n_live, float* loss,
                                                             int32_t* dev_status) {
   __shared__ int sums[32];
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int each = (N + 1023) / 1024, lo = min(N, (int)threadIdx.x * each), hi = min(N, lo + each);
   int count = 0;
@@ -69,6 +71,8 @@ __global__ void __launch_bounds__(1024) dx_head_rows_kernel(const int32_t* targe
 // the listed rows next to each other: four rows per CTA
 __global__ void __launch_bounds__(256) dx_head_pack_kernel(const __nv_bfloat16* h, int64_t ldh, int H, const int32_t* live,
                                                            const int32_t* n_live, __nv_bfloat16* out) {
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= __ldg(n_live)) return;
   const __nv_bfloat16* from = h + (int64_t)__ldg(live + row) * ldh;
@@ -115,7 +119,7 @@ struct RowSums {
   __device__ RowSums(const MmParams& p_, int lane_, int share_, uint32_t) : p(p_), lane(lane_), share(share_) {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int) {
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int, const MmTile&, bool) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
     target = row >= 0 ? __ldg(p.targets + __ldg(p.live + row)) - t.n0 : -1;   // (its place among the tile's columns)
     top = -INFINITY;
@@ -165,6 +169,8 @@ __global__ void __launch_bounds__(1024) dx_head_join_kernel(const float2* part, 
                                                            __nv_bfloat16* dh, int64_t ld_dh) {
   __shared__ float tops[32][32];
   __shared__ double sums[32][32];
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
   const int n_live = __ldg(n_live_at);
   float top = -INFINITY;
@@ -224,7 +230,7 @@ struct StoreDz {
   __device__ StoreDz(const MmParams& p_, int lane_, int share_, uint32_t) : p(p_), lane(lane_), share(share_) {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
-  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int) {
+  __device__ __forceinline__ void begin(const MmTile& t, int lane0, int, const MmTile&, bool) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
     target = -1;
     lse = weight = at_target = 0.0f;
@@ -262,6 +268,8 @@ __global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, in
                                                          const int32_t* n_live, const int32_t* targets,
                                                          const float* row_weight, const float* lse, const float* row_loss,
                                                          __nv_bfloat16* dz, int panel) {
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int row = blockIdx.y, v0 = (blockIdx.x * 256 + threadIdx.x) * 8;
   if (row >= __ldg(n_live) || v0 >= (V + 63) / 64 * 64) return;
   const int r = __ldg(live + row), target = __ldg(targets + r) - v0;
@@ -283,6 +291,8 @@ __global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, in
 // dh of the rows that count: the blocks' shares in order, rounded once
 __global__ void __launch_bounds__(128) dx_head_sum_kernel(const float* share, int blocks, int rows, int H, const int32_t* live,
                                                           const int32_t* n_live, __nv_bfloat16* dh, int64_t ld_dh) {
+  dx_pdl_wait();
+  dx_pdl_trigger();
   const int row = blockIdx.y, i = (blockIdx.x * 128 + threadIdx.x) * 4;
   if (row >= __ldg(n_live) || i >= H) return;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -469,24 +479,24 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   p.dev_status = ctx->dev_status;
   p.wait_limit = ctx->wait_limit;
 
-  dx_head_rows_kernel<<<1, 1024, 0, st>>>(a.targets, a.row_weight, a.N, a.V, live, n_live, a.loss, ctx->dev_status);
-  if (!launched(cudaGetLastError())) return e;
-  dx_head_pack_kernel<<<(a.N + 3) / 4, 256, 0, st>>>(reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, rows);
-  if (!launched(cudaGetLastError())) return e;
+  const bool pdl = (ctx->pdl_mask & DX_PDL_EXPERTS) != 0;
+  if (!launched(dx_launch_pdl(pdl, dx_head_rows_kernel, dim3(1), dim3(1024), 0, st, 1, a.targets, a.row_weight, a.N, a.V, live,
+                              n_live, a.loss, ctx->dev_status))) return e;
+  if (!launched(dx_launch_pdl(pdl, dx_head_pack_kernel, dim3((a.N + 3) / 4), dim3(256), 0, st, 1,
+                              reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, rows))) return e;
   p.tile_width = s.width;
   if (!launched(s.keep ? launch_head<RowSums<true>>(ctx, m, p, st) : launch_head<RowSums<false>>(ctx, m, p, st))) return e;
   p.tile_width = 0;
-  dx_head_join_kernel<<<(a.N + 31) / 32, 1024, 0, st>>>(part, s.pitch, 2 * s.tiles, live, n_live + 1, target_logit, a.loss, lse,
-                                                       row_loss, a.targets, a.row_weight, a.N, a.V, a.H, dh, a.ld_dh);
-  if (!launched(cudaGetLastError()) || !grad) return e;
+  if (!launched(dx_launch_pdl(pdl, dx_head_join_kernel, dim3((a.N + 31) / 32), dim3(1024), 0, st, 1, part, s.pitch, 2 * s.tiles, live,
+                              n_live + 1, target_logit, a.loss, lse, row_loss, a.targets, a.row_weight, a.N, a.V, a.H, dh,
+                              a.ld_dh)) || !grad) return e;
 
   for (int64_t v0 = 0; v0 < a.V; v0 += s.piece) {
     const int len = (int)(a.V - v0 < s.piece ? a.V - v0 : s.piece);
     const bool first = v0 == 0, last = v0 + len == a.V;
     if (s.keep) {
-      dx_head_dz_kernel<<<dim3((a.V + 2047) / 2048, a.N), 256, 0, st>>>(logits, s.ld_logits, a.V, live, n_live + 1, a.targets,
-                                                                        a.row_weight, lse, row_loss, dz, a.N);
-      if (!launched(cudaGetLastError())) return e;
+      if (!launched(dx_launch_pdl(pdl, dx_head_dz_kernel, dim3((a.V + 2047) / 2048, a.N), dim3(256), 0, st, 1, logits, s.ld_logits,
+                                  a.V, live, n_live + 1, a.targets, a.row_weight, lse, row_loss, dz, a.N))) return e;
     } else {
       MmParams q = p;
       q.columns = len;
@@ -528,8 +538,8 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
       }
       if (!launched(dx_launch_grouped_mm(ctx, g, st))) return e;
       if (s.blocks > 1 && last) {
-        dx_head_sum_kernel<<<dim3((a.H + 511) / 512, a.N), 128, 0, st>>>(share, s.blocks, a.N, a.H, live, n_live + 1, dh, a.ld_dh);
-        if (!launched(cudaGetLastError())) return e;
+        if (!launched(dx_launch_pdl(pdl, dx_head_sum_kernel, dim3((a.H + 511) / 512, a.N), dim3(128), 0, st, 1, share, s.blocks, a.N,
+                                    a.H, live, n_live + 1, dh, a.ld_dh))) return e;
       }
     }
     if (a.dW) {

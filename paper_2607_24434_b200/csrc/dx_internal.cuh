@@ -324,9 +324,9 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
                                           const float* pair_w, int n_pairs, void* act_w, int64_t ld_act, float* partial,
                                           float* d_pair_w, cudaStream_t st, int* n_launches);
 cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t st);
-cudaError_t dx_launch_combine(const void* z, int fp32, int64_t ldz, const float* w, int n_tokens, int k, int H, void* y,
+cudaError_t dx_launch_combine(dx_ctx* ctx, const void* z, int fp32, int64_t ldz, const float* w, int n_tokens, int k, int H, void* y,
                               int y_fp32, int64_t ldy, cudaStream_t st);
-cudaError_t dx_launch_combine_grad(const void* dy, const void* z, int fp32, int64_t ld_dy, int64_t ldz, const float* w,
+cudaError_t dx_launch_combine_grad(dx_ctx* ctx, const void* dy, const void* z, int fp32, int64_t ld_dy, int64_t ldz, const float* w,
                                    int n_tokens, int k, int H, void* dz, int64_t ld_dz, float* dw, cudaStream_t st);
 struct DxHeadLoss {
   const void* h;             // bf16 [N][ldh]

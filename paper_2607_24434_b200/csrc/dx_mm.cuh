@@ -441,7 +441,12 @@ struct MmSchedule {
       r.kblocks = (p.kdim + kMmK - 1) / kMmK;
     } else {
       const int nt = t / m_tiles;
-      while (e + 1 < p.n_groups && s->before[e + 1] <= nt) ++e;
+      int last = p.n_groups - 1;                      // (the last group that begins at or before tile nt)
+      while (e < last) {
+        const int mid = (e + last + 1) >> 1;
+        if (s->before[mid] <= nt) e = mid;
+        else last = mid - 1;
+      }
       r.e = e;
       r.m0 = (t - nt * m_tiles) * 128 * CG;
       // a group's rows are split evenly over its tiles
@@ -504,6 +509,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   }
   if (warp == kWarpMma) mm_tmem_alloc<CG>(smem_u32(&s->tmem_base), kTmemCols);
   dx_pdl_wait();
+  dx_pdl_trigger();      // (what follows may take its place on the SMs as they become free; it waits for this grid to end)
   // the groups: rows outside [0, n_rows) and ends in front of their beginnings are cut off and reported
   if (warp == 0) {
     int run = 0;
@@ -800,10 +806,14 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     const int quarter = warp & 3, share = warp >> 2;
     Epilogue epi(p, lane, share, smem_u32(staging) + (uint32_t)warp * Epilogue::kStaging);
     int turn = 0;
+    MmTile next = {};
+    if (unit < total) next = schedule.get(unit);
     for (int t = unit; t < total; t += n_units) {
-      const MmTile tile = schedule.get(t);
+      const MmTile tile = next;
+      const bool more = t + n_units < total;
+      if (more) next = schedule.get(t + n_units);
       const int lane0 = tile.m0 + (int)rank * 128 + 32 * quarter;   // index of the warp's first lane
-      epi.begin(tile, lane0, kCols * share);
+      epi.begin(tile, lane0, kCols * share, next, more);
       typename Epilogue::Values v;
       if (tile.kblocks == 0) {                                       // (an empty group's product over its rows)
         epi.zero(v);
@@ -860,7 +870,7 @@ cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long l
   long long units = ctx->sm_count / CG;
   if (max_tiles < units) units = max_tiles;
   if (units < 1) units = 1;
-  return dx_launch_pdl(false, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(GATHER)), smem,
+  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(GATHER)), smem,
                        st, CG, maps, p);
 }
 
