@@ -964,6 +964,7 @@ dx_status check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld) {
   if (rows < 0 || cols < 1 || ld < cols) return DX_ERR_SHAPE;
   if (cols % 8 || ld % 8) return DX_ERR_UNSUPPORTED;
   if (rows > INT32_MAX || ld > (int64_t(1) << 38) || (rows > 0 && ld > (INT64_MAX / 16) / rows)) return DX_ERR_SHAPE;
+  if (rows * (ld / 8) > UINT32_MAX) return DX_ERR_UNSUPPORTED;      // (a row's place is counted in 16-byte pieces of bf16)
   if (rows > 0 && (!p || (uintptr_t)p % 16)) return DX_ERR_INVALID_ARG;
   return DX_OK;
 }

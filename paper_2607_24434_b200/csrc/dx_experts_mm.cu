@@ -53,12 +53,14 @@ __device__ __forceinline__ int sorted_row(const MmTile& t, int c0, int lane) {
 template <int COLS>
 struct FragmentEpilogue {
   static constexpr int kCols = COLS, kRound = 1;
+  static constexpr bool kBefore = true;
   using Values = Fragments<COLS>;
   const MmParams& p;
   const int lane;
   const uint32_t at;       // the warp's staging
   __device__ FragmentEpilogue(const MmParams& p_, int lane_, int, uint32_t at_) : p(p_), lane(lane_), at(at_) {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld_frag(taddr, x); }
+  __device__ __forceinline__ void arrived(Values& x) { mm_ld_wait(x.v[0], x.v[1]); }
   __device__ __forceinline__ void zero(Values& x) {
 #pragma unroll
     for (int i = 0; i < COLS / 2; ++i) x.v[0][i] = x.v[1][i] = 0.0f;
@@ -151,7 +153,8 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
     next = row >= 0 && this->p.scatter ? __ldg(this->p.scatter + row) : row;
   }
   __device__ __forceinline__ void begin(const MmTile& t, int, int c0, const MmTile&, bool) { look_up(t, c0); }
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x) {
+  template <class Taken>
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x, Taken) {
     int mine = next;
     if (this->p.scatter && this->lane < Base::kCols && sorted_row(t, c0, this->lane) >= 0 && (mine < 0 || mine >= this->p.out_rows)) {
       atomicExch(this->p.dev_status, (int32_t)DX_DEV_BAD_ROW);
@@ -168,7 +171,8 @@ struct StoreOuter : FragmentEpilogue<store_cols<T, false>()> {
   using Base = FragmentEpilogue<store_cols<T, false>()>;
   static constexpr int kStaging = store_staging<T, false>();
   using Base::Base;
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x) {
+  template <class Taken>
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x, Taken) {
     store_chunk<T, false>(this->p, this->lane, this->at, x, sorted_row(t, c0, this->lane), lane0,
                           reinterpret_cast<T*>(this->p.out) + (int64_t)t.e * this->p.group_stride, this->p.ld);
   }
@@ -180,7 +184,8 @@ template <bool SAVE>
 struct StoreSwiglu : FragmentEpilogue<32> {
   static constexpr int kStaging = 32 * 64;
   using FragmentEpilogue<32>::FragmentEpilogue;
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
+  template <class Taken>
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x, Taken) {
     const float(&v)[2][16] = x.v;
     const int n_inter = p.lanes >> 1, i0 = lane0 >> 1;      // the warp's 16 elements
     const int left = t.ncols - c0;
@@ -235,6 +240,7 @@ struct StoreSwiglu : FragmentEpilogue<32> {
 // A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come in 16-byte pieces, a chunk ahead; their
 // place in the staging takes the gradients.
 struct StoreSwigluGrad : FragmentEpilogue<16> {
+  static constexpr bool kBefore = false;      // (no registers for two chunks: this one is waited for where it is needed)
   static constexpr int kArea = 16 * 64, kStaging = 3 * kArea + 512;      // (three areas; the weights of 128 columns)
   uint4 gate[2], up[2];
   const int share;
@@ -295,7 +301,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
     ask_weights();
     if (kCols * share < next.ncols) fetch(next, next.m0 + lane0 - t.m0, kCols * share);
   }
-  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x) {
+  template <class Taken>
+  __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, Values& x, Taken taken) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t to = at + piece64(8 * i + (lane >> 2), lane & 3);
@@ -320,6 +327,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
     __syncwarp();
     if (c0 + 2 * kCols < t.ncols) fetch(t, lane0, c0 + 2 * kCols);
     else ask_next(t, lane0);
+    arrived(x);
+    taken();
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll

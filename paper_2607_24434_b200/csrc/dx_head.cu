@@ -112,6 +112,7 @@ struct RowSums {
   const int lane, share;
   int row, target;
   float top, sum;
+  static constexpr bool kBefore = false;
   static constexpr int kStaging = 0, kCols = 32, kRound = 1;
   struct Values {
     float v[32];
@@ -125,7 +126,9 @@ struct RowSums {
     top = -INFINITY;
     sum = 0.0f;
   }
-  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, Values& x) {
+  template <class Taken>
+  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, Values& x, Taken taken) {
+    taken();
     float(&v)[32] = x.v;
     const int left = t.ncols - c0;
     if (KEEP && row >= 0) store32(p.logits + (int64_t)row * p.ld_logits + t.n0 + c0, v, left);
@@ -223,6 +226,7 @@ struct StoreDz {
   const int lane, share;
   int row, target;
   float lse, weight, at_target;
+  static constexpr bool kBefore = false;
   static constexpr int kStaging = 0, kCols = 32, kRound = 64;   // (the products of the gradients read whole blocks of 64)
   struct Values {
     float v[32];
@@ -243,7 +247,9 @@ struct StoreDz {
     }
   }
   __device__ __forceinline__ void end(const MmTile&) {}
-  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, Values& x) {
+  template <class Taken>
+  __device__ __forceinline__ void chunk(const MmTile& t, int, int c0, Values& x, Taken taken) {
+    taken();
     float(&v)[32] = x.v;
 #pragma unroll
     for (int c = 0; c < 32; ++c) v[c] = weight * ex2((v[c] - lse) * kLog2e);

@@ -148,35 +148,45 @@ template <int COLS>
 struct Fragments {
   float v[2][COLS / 2];
 };
+// (asked for here; the values are there after mm_ld_wait, which therefore names them)
 __device__ __forceinline__ void mm_ld_frag(uint32_t taddr, Fragments<32>& x) {
-  uint32_t r[2][16];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < 2; ++h) {
+    float(&r)[16] = x.v[h];
     asm volatile(
         "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[h][0]), "=r"(r[h][1]), "=r"(r[h][2]), "=r"(r[h][3]), "=r"(r[h][4]), "=r"(r[h][5]), "=r"(r[h][6]),
-          "=r"(r[h][7]), "=r"(r[h][8]), "=r"(r[h][9]), "=r"(r[h][10]), "=r"(r[h][11]), "=r"(r[h][12]), "=r"(r[h][13]),
-          "=r"(r[h][14]), "=r"(r[h][15])
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
+          "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
         : "r"(taddr + (uint32_t)h * (16u << 16)));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x.v[h][i] = __uint_as_float(r[h][i]);
+  }
 }
 __device__ __forceinline__ void mm_ld_frag(uint32_t taddr, Fragments<16>& x) {
-  uint32_t r[2][8];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < 2; ++h) {
+    float(&r)[8] = x.v[h];
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[h][0]), "=r"(r[h][1]), "=r"(r[h][2]), "=r"(r[h][3]), "=r"(r[h][4]), "=r"(r[h][5]), "=r"(r[h][6]),
-                   "=r"(r[h][7])
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
                  : "r"(taddr + (uint32_t)h * (16u << 16)));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x.v[h][i] = __uint_as_float(r[h][i]);
+  }
+}
+template <int N>
+__device__ __forceinline__ void mm_ld_wait(float (&a)[N], float (&b)[N]) {
+  if constexpr (N == 16)
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]), "+f"(a[6]), "+f"(a[7]), "+f"(a[8]),
+                   "+f"(a[9]), "+f"(a[10]), "+f"(a[11]), "+f"(a[12]), "+f"(a[13]), "+f"(a[14]), "+f"(a[15]), "+f"(b[0]),
+                   "+f"(b[1]), "+f"(b[2]), "+f"(b[3]), "+f"(b[4]), "+f"(b[5]), "+f"(b[6]), "+f"(b[7]), "+f"(b[8]), "+f"(b[9]),
+                   "+f"(b[10]), "+f"(b[11]), "+f"(b[12]), "+f"(b[13])
+                 :
+                 : "memory");
+  else
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]), "+f"(a[6]), "+f"(a[7]), "+f"(b[0]),
+                   "+f"(b[1]), "+f"(b[2]), "+f"(b[3]), "+f"(b[4]), "+f"(b[5]), "+f"(b[6]), "+f"(b[7])
+                 :
+                 : "memory");
+  // (an asm statement takes thirty operands: the last two of 32 follow the others through one more)
+  if constexpr (N == 16) asm volatile("" : "+f"(b[14]), "+f"(b[15]), "+f"(a[0]) : : "memory");
 }
 // four 8 x 8 matrices of 16-bit elements, transposed: lanes 8 j .. 8 j + 7 name the rows of matrix j
 __device__ __forceinline__ void stmatrix_t(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -655,7 +665,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       constexpr int kRegs = FORM == kOuter ? 2 : (kHalf + 31) / 32;
       const int here = min(half, tile.ncols - (int)rank * half);      // rows as columns
       // what this lane has looked up: a row's place in its matrix, in pieces of 16 bytes, and which lanes' rows exist
-      uint32_t at_a[FORM == kOuter ? 2 : 1], at_b[kRegs], ok_a[FORM == kOuter ? 2 : 1], ok_b[kRegs];
+      uint32_t at_a[2], at_b[kRegs], ok_a[2], ok_b[kRegs];
       auto resolve = [&](int q, bool in, bool indexed, MmDiv div, int n_rows, int64_t ld, uint32_t& at, uint32_t& ok) {
         const int row = !in ? -1 : indexed ? mm_row(q, div, n_rows, p.dev_status) : q;
         at = (uint32_t)max(row, 0) * (uint32_t)(ld >> 3);
@@ -711,8 +721,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             for (int j = 0; j < 2; ++j) {
               const int r = k0 + 32 * j + lane;
               const bool in = r < tile.rows;
-              resolve(p.a_index ? next_a[j] : tile.row0 + r, in, p.a_index != nullptr, p.a_div, p.a_rows, p.a_ld, at_a[FORM == kOuter ? j : 0],
-                      ok_a[FORM == kOuter ? j : 0]);
+              resolve(p.a_index ? next_a[j] : tile.row0 + r, in, p.a_index != nullptr, p.a_div, p.a_rows, p.a_ld, at_a[j],
+                      ok_a[j]);
               resolve(p.b_index ? next_b[j] : tile.row0 + r, in, p.b_index != nullptr, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
             }
             ask(k0 + 4 * kMmK);
@@ -727,9 +737,9 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             const unsigned char* from = reinterpret_cast<const unsigned char*>(p.a_src) + 2 * (int64_t)(m0 + 8 * piece);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              copy_rows(da + j * 4096u, from, at_a[FORM == kOuter ? j : 0], ok_a[FORM == kOuter ? j : 0],
+              copy_rows(da + j * 4096u, from, at_a[j], ok_a[j],
                         m0 + 8 * piece < p.lanes, 0);
-              copy_rows(da + 8192u + j * 4096u, from, at_a[FORM == kOuter ? j : 0], ok_a[FORM == kOuter ? j : 0],
+              copy_rows(da + 8192u + j * 4096u, from, at_a[j], ok_a[j],
                         m0 + 64 + 8 * piece < p.lanes, 128);
             }
           }
@@ -817,7 +827,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       typename Epilogue::Values v;
       if (tile.kblocks == 0) {                                       // (an empty group's product over its rows)
         epi.zero(v);
-        for (int c = kCols * share; c < tile.ncols; c += 2 * kCols) epi.chunk(tile, lane0, c, v);
+        for (int c = kCols * share; c < tile.ncols; c += 2 * kCols) epi.chunk(tile, lane0, c, v, [] {});
         continue;
       }
       const int buf = turn & 1;
@@ -826,19 +836,33 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       const uint32_t base = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)buf * kAccCols;
       int c = kCols * share;
       const int end = (tile.ncols + Epilogue::kRound - 1) / Epilogue::kRound * Epilogue::kRound;
-      do {
-        if (c < end) epi.load(base + (uint32_t)c, v);
-        if (c + 2 * kCols >= end) {            // the accumulator may be written again
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if constexpr (CG == 2) arrive_at_first(smem_u32(&s->acc_empty[buf]));
-            else mbar_arrive(smem_u32(&s->acc_empty[buf]));
-          }
+      auto taken = [&]() {                     // the accumulator may be written again
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (CG == 2) arrive_at_first(smem_u32(&s->acc_empty[buf]));
+          else mbar_arrive(smem_u32(&s->acc_empty[buf]));
         }
-        if (c < end) epi.chunk(tile, lane0, c, v);
-        c += 2 * kCols;
-      } while (c < end);
+      };
+      if (c >= end) {
+        taken();
+      } else if constexpr (Epilogue::kBefore) {
+        // a chunk is on its way out of tensor memory while the one in front of it is stored
+        typename Epilogue::Values coming;
+        epi.load(base + (uint32_t)c, coming);
+        for (; c < end; c += 2 * kCols) {
+          epi.arrived(coming);
+          v = coming;
+          if (c + 2 * kCols < end) epi.load(base + (uint32_t)(c + 2 * kCols), coming);
+          else taken();
+          epi.chunk(tile, lane0, c, v, [] {});
+        }
+      } else {
+        for (; c < end; c += 2 * kCols) {
+          epi.load(base + (uint32_t)c, v);
+          epi.chunk(tile, lane0, c, v, [&] { if (c + 2 * kCols >= end) taken(); });
+        }
+      }
       epi.end(tile);
       ++turn;
     }
