@@ -13,9 +13,10 @@ namespace {
 
 // ---- out of tensor memory ------------------------------------------------------------------------------------------
 // A warp turns 32 lanes x 32 (16) columns around in shared memory: fragments as the tensor memory gives them (mm_ld_frag),
-// rounded and stored as transposed 8 x 8 matrices -- a column's lanes next to each other -- and read back in 16-byte pieces, so
-// that global memory sees 64 or 128 neighbouring bytes per row.  About 60 instructions for 1024 elements; exchanging them by
-// shuffles took over 200, and the four storing warps, not the products, were what a tile waited for.
+// rounded and stored as transposed 8 x 8 matrices -- a column's lanes next to each other -- in the swizzle of a tensor map, which
+// takes them from there (what the map cannot cut off -- the rows behind a group's last, rows scattered by index -- goes out in
+// 16-byte pieces).  Some 40 instructions for 1024 elements; exchanged by shuffles they took over 200, and the storing warps, not
+// the products, were what a tile waited for.
 
 // bf16: 64 bytes per column, pieces of 16 bytes in an order that keeps the eight columns of a matrix in different banks
 __device__ __forceinline__ uint32_t piece64(int column, int piece) {
@@ -32,18 +33,25 @@ __device__ __forceinline__ void stage_bf16(uint32_t at, int lane, const Fragment
     stage64(at, lane, n, bf16_pair(x.v[0][4 * n], x.v[0][4 * n + 1]), bf16_pair(x.v[0][4 * n + 2], x.v[0][4 * n + 3]),
             bf16_pair(x.v[1][4 * n], x.v[1][4 * n + 1]), bf16_pair(x.v[1][4 * n + 2], x.v[1][4 * n + 3]));
 }
-// fp32: 144 bytes per column
-constexpr int kColumn32 = 144;
+// fp32: 128 bytes per column, pieces of 16 bytes in an order that keeps eight columns in different banks
+__device__ __forceinline__ uint32_t piece128(int column, int piece) {
+  return (uint32_t)(column * 128 + ((piece ^ (column & 7)) << 4));
+}
 template <int COLS>
 __device__ __forceinline__ void stage_fp32(uint32_t at, int lane, const Fragments<COLS>& x) {
-  const uint32_t mine = at + (uint32_t)(2 * (lane & 3) * kColumn32 + (lane >> 2) * 4);
 #pragma unroll
-  for (int n = 0; n < COLS / 8; ++n)
+  for (int odd = 0; odd < 2; ++odd) {
+    // column 8 n + r, lanes 16 h + 8 q + lane / 4: piece 4 h + 2 q + lane / 16, of which only the last part differs by lane
+    const int r = 2 * (lane & 3) + odd;
+    const uint32_t mine = at + piece128(r, lane >> 4) + ((lane >> 2) & 3) * 4;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int n = 0; n < COLS / 8; ++n)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        sts4(mine + (uint32_t)((8 * n + (q & 1)) * kColumn32 + (16 * h + 8 * (q >> 1)) * 4), x.v[h][4 * n + q]);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          sts4((mine ^ (uint32_t)((4 * h + 2 * q) << 4)) + (uint32_t)(n * 1024), x.v[h][4 * n + 2 * q + odd]);
+  }
 }
 
 // sorted row of a chunk's column `c0 + lane` (-1: none)
@@ -56,9 +64,24 @@ struct FragmentEpilogue {
   static constexpr bool kBefore = true;
   using Values = Fragments<COLS>;
   const MmParams& p;
+  const MmMaps& maps;
   const int lane;
   const uint32_t at;       // the warp's staging
-  __device__ FragmentEpilogue(const MmParams& p_, int lane_, int, uint32_t at_) : p(p_), lane(lane_), at(at_) {}
+  __device__ FragmentEpilogue(const MmParams& p_, const MmMaps& maps_, int lane_, int, uint32_t at_, MmFetch)
+      : p(p_), maps(maps_), lane(lane_), at(at_) {}
+  // the boxes that the staging went out in have been read
+  __device__ __forceinline__ void writable() {
+    if (lane == 0) tma_store_read();
+    __syncwarp();
+  }
+  // the staging is what the tensor map's copies are to see
+  __device__ __forceinline__ void written() {
+    proxy_fence();
+    __syncwarp();
+  }
+  __device__ __forceinline__ void finish() {
+    if (lane == 0) tma_store_done();
+  }
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld_frag(taddr, x); }
   __device__ __forceinline__ void arrived(Values& x) { mm_ld_wait(x.v[0], x.v[1]); }
   __device__ __forceinline__ void zero(Values& x) {
@@ -85,16 +108,10 @@ __device__ __forceinline__ void flush_bf16(const MmParams& p, int lane, uint32_t
   for (int i = 0; i < COLS / 8; ++i)
     if (row[i] >= 0 && x < p.lanes) *reinterpret_cast<uint4*>(out + (int64_t)row[i] * ld + x) = u[i];
 }
+// fp32 columns (plus what is to be added) in pieces
 template <class T, bool ADD, int COLS>
-__device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_t at, const Fragments<COLS>& v, int mine, int m,
-                                            T* out, int64_t ld) {
-  if constexpr (sizeof(T) == 2 && !ADD) {
-    stage_bf16(at, lane, v);
-    __syncwarp();
-    flush_bf16<COLS>(p, lane, at, mine, m, out, ld);
-  } else if constexpr (sizeof(T) == 4) {
-    stage_fp32(at, lane, v);
-    __syncwarp();
+__device__ __forceinline__ void flush_fp32(const MmParams& p, int lane, uint32_t at, int mine, int m, T* out, int64_t ld) {
+  if constexpr (sizeof(T) == 4) {
     const int x = m + 4 * (lane & 7);
     uint4 u[COLS / 4];
     float4 a[COLS / 4];
@@ -107,7 +124,7 @@ __device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_
       if (ADD && row[i] >= 0 && x < p.lanes) a[i] = *reinterpret_cast<const float4*>(p.addend + (int64_t)row[i] * p.lanes + x);
     }
 #pragma unroll
-    for (int i = 0; i < COLS / 4; ++i) u[i] = lds16(at + (uint32_t)((4 * i + (lane >> 3)) * kColumn32 + (lane & 7) * 16));
+    for (int i = 0; i < COLS / 4; ++i) u[i] = lds16(at + piece128(4 * i + (lane >> 3), lane & 7));
 #pragma unroll
     for (int i = 0; i < COLS / 4; ++i)
       if (row[i] >= 0 && x < p.lanes)
@@ -115,14 +132,11 @@ __device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_
             make_float4(__uint_as_float(u[i].x) + a[i].x, __uint_as_float(u[i].y) + a[i].y, __uint_as_float(u[i].z) + a[i].z,
                         __uint_as_float(u[i].w) + a[i].w);
   } else {      // (summed in fp32, then rounded)
-    stage_fp32(at, lane, v);
-    __syncwarp();
     const int x = m + 8 * (lane & 3);
 #pragma unroll
     for (int i = 0; i < COLS / 8; ++i) {
       const int column = 8 * i + (lane >> 2), row = __shfl_sync(0xffffffffu, mine, column);
-      const uint32_t src = at + (uint32_t)(column * kColumn32 + (lane & 3) * 32);
-      const uint4 u = lds16(src), w = lds16(src + 16);
+      const uint4 u = lds16(at + piece128(column, 2 * (lane & 3))), w = lds16(at + piece128(column, 2 * (lane & 3) + 1));
       if (row >= 0 && x < p.lanes) {
         const float4* a = reinterpret_cast<const float4*>(p.addend + (int64_t)row * p.lanes + x);
         const float4 a0 = a[0], a1 = a[1];
@@ -134,18 +148,16 @@ __device__ __forceinline__ void store_chunk(const MmParams& p, int lane, uint32_
       }
     }
   }
-  __syncwarp();      // (the staging is written again)
 }
 template <class T, bool ADD>
 constexpr int store_cols() { return sizeof(T) == 2 && !ADD ? 32 : 16; }
-template <class T, bool ADD>
-constexpr int store_staging() { return sizeof(T) == 2 && !ADD ? 32 * 64 : 16 * kColumn32; }
+constexpr int kStoreStaging = 2048;      // 32 columns of 64 bytes, 16 of 128
 
-// out[row of the column][lane] = D (+ addend), rounded once
+// out[row of the column][lane] = D (+ addend), rounded once.  Whole chunks whose rows follow one another go out as a box.
 template <class T, bool ADD>
 struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
   using Base = FragmentEpilogue<store_cols<T, ADD>()>;
-  static constexpr int kStaging = store_staging<T, ADD>();
+  static constexpr int kStaging = kStoreStaging;
   using Base::Base;
   int next;      // where column `lane` of the next chunk goes (looked up a chunk ahead)
   __device__ __forceinline__ void look_up(const MmTile& t, int c0) {
@@ -155,57 +167,81 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
   __device__ __forceinline__ void begin(const MmTile& t, int, int c0, const MmTile&, bool) { look_up(t, c0); }
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x, Taken) {
+    const MmParams& p = this->p;
     int mine = next;
-    if (this->p.scatter && this->lane < Base::kCols && sorted_row(t, c0, this->lane) >= 0 && (mine < 0 || mine >= this->p.out_rows)) {
-      atomicExch(this->p.dev_status, (int32_t)DX_DEV_BAD_ROW);
+    if (p.scatter && this->lane < Base::kCols && sorted_row(t, c0, this->lane) >= 0 && (mine < 0 || mine >= p.out_rows)) {
+      atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
       mine = -1;
     }
     look_up(t, c0 + 2 * Base::kCols);
-    store_chunk<T, ADD>(this->p, this->lane, this->at, x, mine, lane0, reinterpret_cast<T*>(this->p.out), this->p.ld);
+    this->writable();
+    if constexpr (sizeof(T) == 2 && !ADD) stage_bf16(this->at, this->lane, x);
+    else stage_fp32(this->at, this->lane, x);
+    if (!ADD && !p.scatter && c0 + Base::kCols <= t.ncols) {
+      this->written();
+      if (this->lane == 0 && lane0 < p.lanes) {
+        tma_store2(&this->maps.out[0], lane0, t.n0 + c0, this->at);
+        tma_store_commit();
+      }
+    } else {
+      __syncwarp();
+      if constexpr (sizeof(T) == 2 && !ADD)
+        flush_bf16<Base::kCols>(p, this->lane, this->at, mine, lane0, reinterpret_cast<T*>(p.out), p.ld);
+      else
+        flush_fp32<T, ADD, Base::kCols>(p, this->lane, this->at, mine, lane0, reinterpret_cast<T*>(p.out), p.ld);
+      __syncwarp();
+    }
   }
 };
 
-// out of group e: [columns][lanes], element (n, m) = D
+// out of group e: [columns][lanes], element (n, m) = D.  Every chunk is a box: the matrix ends where its columns do.
 template <class T>
 struct StoreOuter : FragmentEpilogue<store_cols<T, false>()> {
   using Base = FragmentEpilogue<store_cols<T, false>()>;
-  static constexpr int kStaging = store_staging<T, false>();
+  static constexpr int kStaging = kStoreStaging;
   using Base::Base;
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x, Taken) {
-    store_chunk<T, false>(this->p, this->lane, this->at, x, sorted_row(t, c0, this->lane), lane0,
-                          reinterpret_cast<T*>(this->p.out) + (int64_t)t.e * this->p.group_stride, this->p.ld);
+    this->writable();
+    if constexpr (sizeof(T) == 2) stage_bf16(this->at, this->lane, x);
+    else stage_fp32(this->at, this->lane, x);
+    this->written();
+    if (this->lane == 0 && lane0 < this->p.lanes) {
+      tma_store3(&this->maps.out[0], lane0, t.n0 + c0, t.e, this->at);
+      tma_store_commit();
+    }
   }
 };
 
 // act = silu(gate) * up from the fp32 products; SAVE: the products themselves, rounded once, for the backward pass.
 // Of 16 lanes the first eight are gate rows, the others the same eight up rows: a thread holds both of an element.
+// 16 elements of a row per warp: 32 bytes per column, the halves in turns so that eight columns meet different banks.
 template <bool SAVE>
 struct StoreSwiglu : FragmentEpilogue<32> {
-  static constexpr int kStaging = 32 * 64;
+  static constexpr int kArea = 32 * 32, kStaging = (SAVE ? 3 : 1) * kArea;
   using FragmentEpilogue<32>::FragmentEpilogue;
+  static __device__ __forceinline__ uint32_t half32(int column, int h) {
+    return (uint32_t)(column * 32 + ((h ^ ((column >> 2) & 1)) << 4));
+  }
+  // matrices: (eight elements h, eight columns n)
+  __device__ __forceinline__ void stage(uint32_t to, const uint32_t (&a)[2][4]) {
+#pragma unroll
+    for (int n = 0; n < 4; n += 2)
+      stmatrix_t(to + half32(8 * (n + (lane >> 4)) + (lane & 7), (lane >> 3) & 1), a[0][n], a[1][n], a[0][n + 1], a[1][n + 1]);
+  }
+  __device__ __forceinline__ void pieces(uint32_t from, const MmTile& t, int c0, int i, __nv_bfloat16* out, int64_t ld) {
+    out += (int64_t)(t.n0 + c0 + (lane >> 1)) * ld + i;
+    uint4 u[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) u[k] = lds16(from + half32(16 * k + (lane >> 1), lane & 1));
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (16 * k + (lane >> 1) < t.ncols - c0 && i < (p.lanes >> 1)) *reinterpret_cast<uint4*>(out + (int64_t)(16 * k) * ld) = u[k];
+  }
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x, Taken) {
     const float(&v)[2][16] = x.v;
     const int n_inter = p.lanes >> 1, i0 = lane0 >> 1;      // the warp's 16 elements
-    const int left = t.ncols - c0;
-    if constexpr (SAVE) {
-#pragma unroll
-      for (int n = 0; n < 4; ++n)     // per column: sixteen gates, sixteen ups
-        stage64(at, lane, n, bf16_pair(v[0][4 * n], v[0][4 * n + 1]), bf16_pair(v[1][4 * n], v[1][4 * n + 1]),
-                bf16_pair(v[0][4 * n + 2], v[0][4 * n + 3]), bf16_pair(v[1][4 * n + 2], v[1][4 * n + 3]));
-      __syncwarp();
-      const int piece = lane & 3, i = i0 + 8 * (piece & 1);
-      __nv_bfloat16* save = reinterpret_cast<__nv_bfloat16*>(p.save) + (piece >> 1) * (int64_t)n_inter + i;
-      save += (int64_t)(t.n0 + c0 + (lane >> 2)) * p.ld_save;
-      uint4 u[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) u[k] = lds16(at + piece64(8 * k + (lane >> 2), piece));
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (8 * k + (lane >> 2) < left && i < n_inter) *reinterpret_cast<uint4*>(save + (int64_t)(8 * k) * p.ld_save) = u[k];
-      __syncwarp();
-    }
     uint32_t a[2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -213,57 +249,71 @@ struct StoreSwiglu : FragmentEpilogue<32> {
       for (int n = 0; n < 4; ++n)
         a[h][n] = bf16_pair(v[h][4 * n] * sigmoid(v[h][4 * n]) * v[h][4 * n + 2],
                             v[h][4 * n + 1] * sigmoid(v[h][4 * n + 1]) * v[h][4 * n + 3]);
-    // 32 bytes per column; matrices: (eight lanes h, eight columns n)
+    writable();
+    stage(at, a);
+    if constexpr (SAVE) {
 #pragma unroll
-    for (int n = 0; n < 4; n += 2) {
-      const int column = 8 * (n + (lane >> 4)) + (lane & 7), h = (lane >> 3) & 1;
-      stmatrix_t(at + (uint32_t)(column * 32 + ((h ^ ((column >> 2) & 1)) << 4)), a[0][n], a[1][n], a[0][n + 1], a[1][n + 1]);
+      for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) a[h][n] = bf16_pair(v[h][4 * n + 2 * g], v[h][4 * n + 2 * g + 1]);
+        stage(at + (1 + g) * kArea, a);
+      }
     }
-    __syncwarp();
-    const int h = lane & 1, i = i0 + 8 * h;
-    __nv_bfloat16* act = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)(t.n0 + c0 + (lane >> 1)) * p.ld + i;
-    uint4 u[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int column = 16 * k + (lane >> 1);
-      u[k] = lds16(at + (uint32_t)(column * 32 + ((h ^ ((column >> 2) & 1)) << 4)));
+    if (c0 + 32 <= t.ncols) {
+      written();
+      if (lane == 0 && i0 < n_inter) {
+        tma_store2(&maps.out[0], i0, t.n0 + c0, at);
+        if constexpr (SAVE) {
+          tma_store2(&maps.out[1], i0, t.n0 + c0, at + kArea);
+          tma_store2(&maps.out[2], i0, t.n0 + c0, at + 2 * kArea);
+        }
+        tma_store_commit();
+      }
+    } else {
+      __syncwarp();
+      const int i = i0 + 8 * (lane & 1);
+      pieces(at, t, c0, i, reinterpret_cast<__nv_bfloat16*>(p.out), p.ld);
+      if constexpr (SAVE) {
+        __nv_bfloat16* save = reinterpret_cast<__nv_bfloat16*>(p.save);
+        pieces(at + kArea, t, c0, i, save, p.ld_save);
+        pieces(at + 2 * kArea, t, c0, i, save + n_inter, p.ld_save);
+      }
+      __syncwarp();
     }
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-      if (16 * k + (lane >> 1) < left && i < n_inter) *reinterpret_cast<uint4*>(act + (int64_t)(16 * k) * p.ld) = u[k];
-    __syncwarp();
   }
 };
 
 // D = W_down^T dy = the gradient of an unweighted act.  With q the row's pair, w its weight, s = sigmoid(gate):
 //   d gate = w D up s (1 + gate (1 - s)),  d up = w D gate s,  act_w = w gate s up,  share of d w = sum over lanes of D gate s up.
-// A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come in 16-byte pieces, a chunk ahead; their
-// place in the staging takes the gradients.
+// A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come as boxes, a chunk ahead; their place in the
+// staging takes the gradients, which go out as boxes.  (In pieces through registers, every element crossed the load/store path
+// six times, and that path, shared with the gathering warps, was the bound: 430 us, 49152 rows x 2048 x 1408.)
 struct StoreSwigluGrad : FragmentEpilogue<16> {
   static constexpr bool kBefore = false;      // (no registers for two chunks: this one is waited for where it is needed)
-  static constexpr int kArea = 16 * 64, kStaging = 3 * kArea + 512;      // (three areas; the weights of 128 columns)
-  uint4 gate[2], up[2];
+  static constexpr int kArea = 16 * 64, kBuffer = 3 * kArea, kStaging = 2 * kBuffer + 512;    // (two chunks; 128 columns' weights)
   const int share;
-  __device__ StoreSwigluGrad(const MmParams& p_, int lane_, int share_, uint32_t at_)
-      : FragmentEpilogue<16>(p_, lane_, share_, at_), share(share_) {}
-  __device__ __forceinline__ void fetch(const MmTile& t, int lane0, int c0) {
-    const int x = lane0 + 8 * (lane & 3);
-    const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.gate_up) +
-                               (int64_t)(t.n0 + c0 + (lane >> 2)) * p.ld_gate_up + x;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const bool in = c0 + 8 * i + (lane >> 2) < t.ncols && x < p.lanes;
-      const uint4* g = reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * p.ld_gate_up);
-      gate[i] = in ? __ldcs(g) : make_uint4(0u, 0u, 0u, 0u);
-      up[i] = in ? __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * p.ld_gate_up + p.lanes)) : make_uint4(0u, 0u, 0u, 0u);
-    }
-  }
-  // The weights of the warp's share of a tile's columns, all at once.  An index and the weight behind it are two trips to L2, gate
-  // and up one to memory: they are asked for while the tile in front is still being stored.
+  const MmFetch own;
+  uint32_t turn = 0;         // chunks so far
+  bool asked = false;        // the next chunk's gate and up are on their way
   MmTile next;
-  bool more;
+  bool more = false, first = true;
   int q[4];
   float w4[4];
+  __device__ StoreSwigluGrad(const MmParams& p_, const MmMaps& maps_, int lane_, int share_, uint32_t at_, MmFetch own_)
+      : FragmentEpilogue<16>(p_, maps_, lane_, share_, at_, own_), share(share_), own(own_) {}
+  // gate and up of chunk number `n`, which is (tile, c0); its buffer has been read
+  __device__ __forceinline__ void fetch(uint32_t n, const MmTile& t, int lane0, int c0) {
+    if (lane == 0) {
+      const uint32_t bar = own.bar + (n & 1u) * 8u, to = at + (n & 1u) * kBuffer;
+      mbar_arrive_expect_tx(bar, 2 * kArea);
+      tma2<1>(to, &maps.in[0], lane0, t.n0 + c0, bar);
+      tma2<1>(to + kArea, &maps.in[1], lane0, t.n0 + c0, bar);
+    }
+  }
+  // The weights of the warp's share of a tile's columns, all at once.  An index and the weight behind it are two trips to L2:
+  // they are asked for while the tile in front is still being stored.
   __device__ __forceinline__ void ask_pairs(const MmTile& t) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {        // 16 columns of every 32
@@ -279,56 +329,65 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       if (!in && q[j] != INT_MIN) atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
     }
   }
-  bool first = true;
   __device__ __forceinline__ void begin(const MmTile& t, int lane0, int c0, const MmTile& next_, bool more_) {
     if (first) {
       ask_pairs(t);
-      if (c0 < t.ncols) fetch(t, lane0, c0);
       ask_weights();
       first = false;
     }
     __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sts4(at + 3 * kArea + (uint32_t)(32 * j + lane) * 4, w4[j]);
+    for (int j = 0; j < 4; ++j) sts4(at + 2 * kBuffer + (uint32_t)(32 * j + lane) * 4, w4[j]);
     __syncwarp();
     next = next_;
     more = more_;
     if (more) ask_pairs(next);
-    if (c0 >= t.ncols) ask_next(t, lane0);        // (no chunk of this tile is the warp's)
+    if (c0 >= t.ncols && more) ask_weights();        // (no chunk of this tile is the warp's)
   }
-  __device__ __forceinline__ void ask_next(const MmTile& t, int lane0) {
-    if (!more) return;
-    ask_weights();
-    if (kCols * share < next.ncols) fetch(next, next.m0 + lane0 - t.m0, kCols * share);
+  __device__ __forceinline__ void finish() {
+    if (asked && lane == 0) {      // (the loop over the tiles ended early: no box may still be landing)
+      for (uint32_t spin = 0; spin < kDrainPolls; ++spin)
+        if (mbar_try_wait(own.bar + (turn & 1u) * 8u, (turn >> 1) & 1u)) break;
+    }
+    FragmentEpilogue<16>::finish();
+  }
+  // the chunk behind (t, c0): into the buffer that the chunk in front of it went out from
+  __device__ __forceinline__ void ask_next(const MmTile& t, int lane0, int c0) {
+    const bool here = c0 + 2 * kCols < t.ncols;
+    if (!here && more) ask_weights();
+    asked = here || (more && kCols * share < next.ncols);
+    if (!asked) return;
+    if (lane == 0) tma_store_read();
+    if (here) fetch(turn + 1, t, lane0, c0 + 2 * kCols);
+    else fetch(turn + 1, next, next.m0 + lane0 - t.m0, kCols * share);
   }
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, Values& x, Taken taken) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t to = at + piece64(8 * i + (lane >> 2), lane & 3);
-      sts16(to, gate[i]);
-      sts16(to + kArea, up[i]);
+    const uint32_t buf = at + (turn & 1u) * kBuffer;
+    if (!asked) {
+      if (lane == 0) tma_store_read();
+      fetch(turn, t, lane0, c0);
     }
-    __syncwarp();
+    ask_next(t, lane0, c0);
+    // (a wait that runs out raises the abort flag, which ends the loop over the tiles; what this chunk holds is undefined then)
+    mm_store_wait(own.bar + (turn & 1u) * 8u, (turn >> 1) & 1u, own.abort_flag, own.limit, lane);
     uint32_t g4[2][4], u4[2][4], a4[2][4], mask[2];
     F2 w[2], dw2[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      const uint32_t from = at + piece64(8 * n + (lane & 7), lane >> 3);
+      const uint32_t from = buf + piece64(8 * n + (lane & 7), lane >> 3);
       ldmatrix_t(from, g4[n]);
       ldmatrix_t(from + kArea, u4[n]);
-      const uint32_t from_w = at + 3 * kArea + (uint32_t)((c0 >> 5) * 16 + 8 * n + 2 * (lane & 3)) * 4;
+      const uint32_t from_w = at + 2 * kBuffer + (uint32_t)((c0 >> 5) * 16 + 8 * n + 2 * (lane & 3)) * 4;
       float w0, w1;
       asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(w0), "=f"(w1) : "r"(from_w) : "memory");
       w[n] = f2(w0, w1);
       mask[n] = (w0 != 0.0f ? 0xffffu : 0u) | (w1 != 0.0f ? 0xffff0000u : 0u);
       dw2[n] = f2(0.0f, 0.0f);
     }
-    __syncwarp();
-    if (c0 + 2 * kCols < t.ncols) fetch(t, lane0, c0 + 2 * kCols);
-    else ask_next(t, lane0);
     arrived(x);
     taken();
+    __syncwarp();
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -350,27 +409,25 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      stage64(at, lane, n, g4[n][0], g4[n][1], g4[n][2], g4[n][3]);
-      stage64(at + kArea, lane, n, u4[n][0], u4[n][1], u4[n][2], u4[n][3]);
-      stage64(at + 2 * kArea, lane, n, a4[n][0], a4[n][1], a4[n][2], a4[n][3]);
+      stage64(buf, lane, n, g4[n][0], g4[n][1], g4[n][2], g4[n][3]);
+      stage64(buf + kArea, lane, n, u4[n][0], u4[n][1], u4[n][2], u4[n][3]);
+      stage64(buf + 2 * kArea, lane, n, a4[n][0], a4[n][1], a4[n][2], a4[n][3]);
     }
-    __syncwarp();
-    uint4 out[3][2];
+    if (c0 + kCols <= t.ncols) {
+      written();
+      if (lane == 0 && lane0 < p.lanes) {
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) out[k][i] = lds16(at + k * kArea + piece64(8 * i + (lane >> 2), lane & 3));
-    const int m = lane0 + 8 * (lane & 3);
-    const int64_t row = t.n0 + c0 + (lane >> 2);
-    __nv_bfloat16* d_gate = reinterpret_cast<__nv_bfloat16*>(p.out) + row * p.ld + m;
-    __nv_bfloat16* act_w = reinterpret_cast<__nv_bfloat16*>(p.act_w) + row * p.ld_act + m;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (c0 + 8 * i + (lane >> 2) < t.ncols && m < p.lanes) {
-        *reinterpret_cast<uint4*>(d_gate + (int64_t)(8 * i) * p.ld) = out[0][i];
-        *reinterpret_cast<uint4*>(d_gate + (int64_t)(8 * i) * p.ld + p.lanes) = out[1][i];
-        *reinterpret_cast<uint4*>(act_w + (int64_t)(8 * i) * p.ld_act) = out[2][i];
+        for (int k = 0; k < 3; ++k) tma_store2(&maps.out[k], lane0, t.n0 + c0, buf + k * kArea);
+        tma_store_commit();
       }
+    } else {
+      __syncwarp();
+      const int mine = sorted_row(t, c0, lane);
+      __nv_bfloat16* d_gate = reinterpret_cast<__nv_bfloat16*>(p.out);
+      flush_bf16<16>(p, lane, buf, mine, lane0, d_gate, p.ld);
+      flush_bf16<16>(p, lane, buf + kArea, mine, lane0, d_gate + p.lanes, p.ld);
+      flush_bf16<16>(p, lane, buf + 2 * kArea, mine, lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
+      written();            // (boxes of the chunk after the next come here)
     }
     if (p.partial) {
       // eight threads (t / 4) hold shares of the columns 8 n + 2 (t % 4) + i: folded so that two of them each end with one
@@ -395,7 +452,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       const int k = lane >> 3, column = c0 + 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
       if (!(lane & 4) && column < t.ncols) p.partial[(int64_t)(lane0 >> 5) * p.n_rows + t.n0 + column] = dw[0];
     }
-    __syncwarp();      // (the staging is written again)
+    ++turn;
   }
 };
 
@@ -450,6 +507,34 @@ bool dx_tensor_map(CUtensorMap* out, const void* base, int rank, const uint64_t*
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool dx_box_map(CUtensorMap* out, const void* base, bool fp32, int rank, const uint64_t* dims, const uint64_t* strides,
+                const uint32_t* box) {
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
+  const uint64_t elem = fp32 ? 4 : 2;
+  cuuint64_t d[3], s[2];
+  cuuint32_t b[3], one[3] = {1, 1, 1};
+  for (int i = 0; i < rank; ++i) {
+    d[i] = dims[i];
+    b[i] = box[i];
+    if (i + 1 < rank) s[i] = strides[i] * elem;
+  }
+  const uint64_t width = box[0] * elem;
+  return encode(out, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+                const_cast<void*>(base), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
+// boxes of `width` x `height` of a matrix
+bool box_map(CUtensorMap* out, const void* base, bool fp32, int64_t rows, int64_t cols, int64_t ld, int width, int height) {
+  const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows}, strides[1] = {(uint64_t)ld};
+  const uint32_t box[2] = {(uint32_t)width, (uint32_t)height};
+  return dx_box_map(out, base, fp32, 2, dims, strides, box);
+}
+}  // namespace
+
 bool dx_matrix_map(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
   const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows}, strides[1] = {(uint64_t)ld};
   const uint32_t box[2] = {64, (uint32_t)box_rows};
@@ -469,11 +554,13 @@ cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cuda
   // (every group may end in a tile that is not full)
   const long long most = ((p.lanes + lanes - 1) / lanes) *
                          ((p.n_rows + bn - 1) / bn + (p.n_groups < p.n_rows ? p.n_groups : p.n_rows));
+  // (stages: as many as the staging leaves room for)
+  constexpr int kFew = Epilogue::kStaging > 4096 ? 6 : 8, kMany = Epilogue::kStaging > 4096 ? 5 : 6;
   if (p.b_index)
-    return few ? mm_launch<FORM, true, 1, 64, 8, Epilogue>(ctx, maps, p, most, st)
-               : mm_launch<FORM, true, 2, 256, 6, Epilogue>(ctx, maps, p, most, st);
-  return few ? mm_launch<FORM, false, 1, 64, 8, Epilogue>(ctx, maps, p, most, st)
-             : mm_launch<FORM, false, 2, 256, 6, Epilogue>(ctx, maps, p, most, st);
+    return few ? mm_launch<FORM, true, 1, 64, kFew, Epilogue>(ctx, maps, p, most, st)
+               : mm_launch<FORM, true, 2, 256, kMany, Epilogue>(ctx, maps, p, most, st);
+  return few ? mm_launch<FORM, false, 1, 64, kFew, Epilogue>(ctx, maps, p, most, st)
+             : mm_launch<FORM, false, 2, 256, kMany, Epilogue>(ctx, maps, p, most, st);
 }
 
 // the rows (columns of D): a tensor map, or the matrix they are gathered from
@@ -523,7 +610,8 @@ cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t
   const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)(a.w_rows ? a.w_rows : a.n), (uint64_t)(a.w_rows ? 1 : a.n_groups)};
   const uint64_t strides[2] = {(uint64_t)a.ldw, (uint64_t)a.w_stride};
   const uint32_t box[3] = {64, a.transposed ? 64u : 128u, 1};
-  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, n_in))
+  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, n_in) ||
+      (!a.scatter && !a.addend && !box_map(&m.out[0], a.y, a.y_fp32, a.y_rows, n_out, a.ldy, 32, a.y_fp32 ? 16 : 32)))
     return cudaErrorInvalidValue;
   if (a.transposed) {
     if (a.addend)
@@ -550,7 +638,11 @@ cudaError_t dx_launch_grouped_swiglu(dx_ctx* ctx, const DxGroupedMm& a, void* ga
   const uint64_t dims[5] = {(uint64_t)a.k, 8, 2, (uint64_t)(n_inter / 8), (uint64_t)a.n_groups};
   const uint64_t strides[4] = {(uint64_t)a.ldw, (uint64_t)(n_inter * a.ldw), (uint64_t)(8 * a.ldw), (uint64_t)a.w_stride};
   const uint32_t box[5] = {64, 8, 2, 8, 1};
-  if (!dx_tensor_map(&m.a, a.w, 5, dims, strides, box) || !rows_source(&m, &p, a, a.k))
+  const __nv_bfloat16* gu = reinterpret_cast<const __nv_bfloat16*>(gate_up);
+  if (!dx_tensor_map(&m.a, a.w, 5, dims, strides, box) || !rows_source(&m, &p, a, a.k) ||
+      !box_map(&m.out[0], a.y, false, a.n_rows, n_inter, a.ldy, 16, 32) ||
+      (gu && !(box_map(&m.out[1], gu, false, a.n_rows, n_inter, ld_gate_up, 16, 32) &&
+               box_map(&m.out[2], gu + n_inter, false, a.n_rows, n_inter, ld_gate_up, 16, 32))))
     return cudaErrorInvalidValue;
   return gate_up ? launch_rows<kSwiglu, StoreSwiglu<true>>(ctx, m, p, st)
                  : launch_rows<kSwiglu, StoreSwiglu<false>>(ctx, m, p, st);
@@ -577,7 +669,13 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)a.n, (uint64_t)a.n_groups};
   const uint64_t strides[2] = {(uint64_t)a.ldw, (uint64_t)a.w_stride};
   const uint32_t box[3] = {64, 64, 1};
-  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, a.n))
+  const __nv_bfloat16 *gu = reinterpret_cast<const __nv_bfloat16*>(gate_up), *d_gu = reinterpret_cast<const __nv_bfloat16*>(a.y);
+  if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, a.n) ||
+      !box_map(&m.in[0], gu, false, a.n_rows, a.k, ld_gate_up, 32, 16) ||
+      !box_map(&m.in[1], gu + a.k, false, a.n_rows, a.k, ld_gate_up, 32, 16) ||
+      !box_map(&m.out[0], d_gu, false, a.n_rows, a.k, a.ldy, 32, 16) ||
+      !box_map(&m.out[1], d_gu + a.k, false, a.n_rows, a.k, a.ldy, 32, 16) ||
+      !box_map(&m.out[2], act_w, false, a.n_rows, a.k, ld_act, 32, 16))
     return cudaErrorInvalidValue;
   cudaError_t e = launch_rows<kRowsT, StoreSwigluGrad>(ctx, m, p, st);
   *n_launches = 1;
@@ -612,6 +710,10 @@ cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t
       !dx_matrix_map(&m.b, a.dy, (int64_t)(a.dy_panels ? (a.n + kPanel - 1) / kPanel : 1) * a.dy_rows,
                      a.dy_panels ? kPanel : a.n, a.ld_dy, 64))
     return cudaErrorInvalidValue;
+  const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)a.n, (uint64_t)a.n_groups};
+  const uint64_t strides[2] = {(uint64_t)a.ld_dw, (uint64_t)a.dw_stride};
+  const uint32_t box[3] = {32, a.dw_fp32 ? 16u : 32u, 1};
+  if (!dx_box_map(&m.out[0], a.dw, a.dw_fp32, 3, dims, strides, box)) return cudaErrorInvalidValue;
   const long long tiles = (long long)a.n_groups * ((a.k + 255) / 256) * ((a.n + 255) / 256);
   return a.dw_fp32 ? mm_launch<kOuter, true, 2, 256, 6, StoreOuter<float>>(ctx, m, p, tiles, st)
                    : mm_launch<kOuter, true, 2, 256, 6, StoreOuter<__nv_bfloat16>>(ctx, m, p, tiles, st);

@@ -117,7 +117,8 @@ struct RowSums {
   struct Values {
     float v[32];
   };
-  __device__ RowSums(const MmParams& p_, int lane_, int share_, uint32_t) : p(p_), lane(lane_), share(share_) {}
+  __device__ RowSums(const MmParams& p_, const MmMaps&, int lane_, int share_, uint32_t, MmFetch) : p(p_), lane(lane_), share(share_) {}
+  __device__ __forceinline__ void finish() {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
   __device__ __forceinline__ void begin(const MmTile& t, int lane0, int, const MmTile&, bool) {
@@ -231,7 +232,8 @@ struct StoreDz {
   struct Values {
     float v[32];
   };
-  __device__ StoreDz(const MmParams& p_, int lane_, int share_, uint32_t) : p(p_), lane(lane_), share(share_) {}
+  __device__ StoreDz(const MmParams& p_, const MmMaps&, int lane_, int share_, uint32_t, MmFetch) : p(p_), lane(lane_), share(share_) {}
+  __device__ __forceinline__ void finish() {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
   __device__ __forceinline__ void begin(const MmTile& t, int lane0, int, const MmTile&, bool) {

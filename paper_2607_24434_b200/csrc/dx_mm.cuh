@@ -73,6 +73,21 @@ __device__ __forceinline__ void tma5(uint32_t dst, const CUtensorMap* map, int x
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+// boxes of shared memory to a matrix (what lies outside it is left out), by one lane; the copies of a group are waited for together
+__device__ __forceinline__ void tma_store2(const CUtensorMap* map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+               : "memory");
+}
+__device__ __forceinline__ void tma_store3(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
+               "r"(z), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// ... have read their shared memory
+__device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// ... are done
+__device__ __forceinline__ void tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -315,6 +330,8 @@ __device__ __forceinline__ bool mm_store_wait(uint32_t bar, uint32_t parity, vol
 struct MmMaps {
   CUtensorMap a, b;       // boxes of rows
   CUtensorMap b_few;      // of fewer rows
+  CUtensorMap out[3];     // outputs that go out in boxes
+  CUtensorMap in[2];      // (SwiGLU gradient) gate and up
 };
 // Division of 0 <= q < 2^31 by a constant d of the launch: q factor >> shift with shift = 31 + ceil(log2 d) and
 // factor = ceil(2^shift / d) < 2^32 (exact: factor d - 2^shift < d <= 2^(shift - 31), so the error stays below 1 / d).  d = 1: factor 0.
@@ -396,6 +413,7 @@ struct __align__(16) MmShared {
   unsigned long long full[kMmMaxStages];
   unsigned long long empty[kMmMaxStages];
   unsigned long long acc_full[2], acc_empty[2], drained;
+  unsigned long long fetched[kMmStoring][2];   // what a storing warp reads beside the accumulators
   uint32_t tmem_base;
   int abort_flag;
   int off[DX_MAX_E + 1];         // first row of a group, and behind it its end where the next begins elsewhere
@@ -471,6 +489,12 @@ struct MmSchedule {
     return r;
   }
 };
+// barriers of a storing warp's own fetches, and what bounds its waits
+struct MmFetch {
+  uint32_t bar;
+  volatile int* abort_flag;
+  uint32_t limit;
+};
 // columns of the products of a tile
 template <int CG>
 __device__ __forceinline__ int mm_width(int ncols) { return (ncols + 16 * CG - 1) / (16 * CG) * (16 * CG); }
@@ -494,8 +518,9 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   constexpr uint32_t kAccCols = BN < 32 ? 32 : BN, kTmemCols = 2 * kAccCols;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  MmShared* s = reinterpret_cast<MmShared*>(ring + (size_t)STAGES * kStage);
-  unsigned char* staging = ring + (size_t)STAGES * kStage + (sizeof(MmShared) + 127) / 128 * 128;
+  unsigned char* staging = ring + (size_t)STAGES * kStage;
+  MmShared* s = reinterpret_cast<MmShared*>(staging + kMmStoring * Epilogue::kStaging);
+  static_assert(Epilogue::kStaging % 512 == 0);
 
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? cta_rank() : 0u;
@@ -512,6 +537,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       mbar_init(smem_u32(&s->acc_empty[i]), kMmStoring * CG);
     }
     mbar_init(smem_u32(&s->drained), 1);
+    for (int i = 0; i < 2 * kMmStoring; ++i) mbar_init(smem_u32(&s->fetched[i >> 1][i & 1]), 1);
     s->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma_prefetch_map(&maps.a);
@@ -814,7 +840,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     // ---------------------------------------------------------------------------------------------- finished tiles
     constexpr int kCols = Epilogue::kCols;      // columns of a chunk
     const int quarter = warp & 3, share = warp >> 2;
-    Epilogue epi(p, lane, share, smem_u32(staging) + (uint32_t)warp * Epilogue::kStaging);
+    Epilogue epi(p, maps, lane, share, smem_u32(staging) + (uint32_t)warp * Epilogue::kStaging,
+                 MmFetch{smem_u32(&s->fetched[warp][0]), abort_flag, p.wait_limit});
     int turn = 0;
     MmTile next = {};
     if (unit < total) next = schedule.get(unit);
@@ -866,6 +893,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       epi.end(tile);
       ++turn;
     }
+    epi.finish();
   }
   __syncwarp();
   tc_fence_before();
@@ -904,5 +932,8 @@ cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long l
 // in elements, strides[i] of dimension i + 1.  Returns false where the driver refuses it.
 bool dx_tensor_map(CUtensorMap* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
                    const uint32_t* box);
+// Tensor map for boxes of box[0] x box[1] elements of fp32 or bf16 in the swizzle of box[0]'s bytes (32, 64 or 128).
+bool dx_box_map(CUtensorMap* out, const void* base, bool fp32, int rank, const uint64_t* dims, const uint64_t* strides,
+                const uint32_t* box);
 // ... of [rows][cols], boxes of 64 columns by box_rows rows (1: for gathered rows)
 bool dx_matrix_map(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
