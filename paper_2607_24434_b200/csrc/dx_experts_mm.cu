@@ -179,7 +179,7 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
     else stage_fp32(this->at, this->lane, x);
     if (!ADD && !p.scatter && c0 + Base::kCols <= t.ncols) {
       this->written();
-      if (this->lane == 0 && lane0 < p.lanes) {
+      if (this->lane == 0) {
         tma_store2(&this->maps.out[0], lane0, t.n0 + c0, this->at);
         tma_store_commit();
       }
@@ -206,7 +206,7 @@ struct StoreOuter : FragmentEpilogue<store_cols<T, false>()> {
     if constexpr (sizeof(T) == 2) stage_bf16(this->at, this->lane, x);
     else stage_fp32(this->at, this->lane, x);
     this->written();
-    if (this->lane == 0 && lane0 < this->p.lanes) {
+    if (this->lane == 0) {
       tma_store3(&this->maps.out[0], lane0, t.n0 + c0, t.e, this->at);
       tma_store_commit();
     }
@@ -263,7 +263,7 @@ struct StoreSwiglu : FragmentEpilogue<32> {
     }
     if (c0 + 32 <= t.ncols) {
       written();
-      if (lane == 0 && i0 < n_inter) {
+      if (lane == 0) {
         tma_store2(&maps.out[0], i0, t.n0 + c0, at);
         if constexpr (SAVE) {
           tma_store2(&maps.out[1], i0, t.n0 + c0, at + kArea);
@@ -292,7 +292,11 @@ struct StoreSwiglu : FragmentEpilogue<32> {
 // six times, and that path, shared with the gathering warps, was the bound: 430 us, 49152 rows x 2048 x 1408.)
 struct StoreSwigluGrad : FragmentEpilogue<16> {
   static constexpr bool kBefore = false;      // (no registers for two chunks: this one is waited for where it is needed)
-  static constexpr int kArea = 16 * 64, kBuffer = 3 * kArea, kStaging = 2 * kBuffer + 512;    // (two chunks; 128 columns' weights)
+  // of a column 64 bytes of gate, then 64 of up; behind the sixteen columns act_w; two chunks; the weights of 128 columns
+  static constexpr int kArea = 16 * 64, kBuffer = 3 * kArea, kStaging = 2 * kBuffer + 512;
+  static __device__ __forceinline__ uint32_t piece2(int column, int up, int piece) {
+    return (uint32_t)(column * 128 + up * 64 + ((piece ^ (column & 3)) << 4));
+  }
   const int share;
   const MmFetch own;
   uint32_t turn = 0;         // chunks so far
@@ -308,8 +312,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
     if (lane == 0) {
       const uint32_t bar = own.bar + (n & 1u) * 8u, to = at + (n & 1u) * kBuffer;
       mbar_arrive_expect_tx(bar, 2 * kArea);
-      tma2<1>(to, &maps.in[0], lane0, t.n0 + c0, bar);
-      tma2<1>(to + kArea, &maps.in[1], lane0, t.n0 + c0, bar);
+      tma3<1>(to, &maps.in, lane0, 0, t.n0 + c0, bar);
     }
   }
   // The weights of the warp's share of a tile's columns, all at once.  An index and the weight behind it are two trips to L2:
@@ -375,9 +378,9 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
     F2 w[2], dw2[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      const uint32_t from = buf + piece64(8 * n + (lane & 7), lane >> 3);
+      const uint32_t from = buf + piece2(8 * n + (lane & 7), 0, lane >> 3);
       ldmatrix_t(from, g4[n]);
-      ldmatrix_t(from + kArea, u4[n]);
+      ldmatrix_t(from + 64, u4[n]);
       const uint32_t from_w = at + 2 * kBuffer + (uint32_t)((c0 >> 5) * 16 + 8 * n + 2 * (lane & 3)) * 4;
       float w0, w1;
       asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(w0), "=f"(w1) : "r"(from_w) : "memory");
@@ -409,24 +412,32 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      stage64(buf, lane, n, g4[n][0], g4[n][1], g4[n][2], g4[n][3]);
-      stage64(buf + kArea, lane, n, u4[n][0], u4[n][1], u4[n][2], u4[n][3]);
+      const uint32_t to = buf + piece2(8 * n + (lane & 7), 0, lane >> 3);
+      stmatrix_t(to, g4[n][0], g4[n][1], g4[n][2], g4[n][3]);
+      stmatrix_t(to + 64, u4[n][0], u4[n][1], u4[n][2], u4[n][3]);
       stage64(buf + 2 * kArea, lane, n, a4[n][0], a4[n][1], a4[n][2], a4[n][3]);
     }
     if (c0 + kCols <= t.ncols) {
       written();
-      if (lane == 0 && lane0 < p.lanes) {
-#pragma unroll
-        for (int k = 0; k < 3; ++k) tma_store2(&maps.out[k], lane0, t.n0 + c0, buf + k * kArea);
+      if (lane == 0) {
+        tma_store3(&maps.out[0], lane0, 0, t.n0 + c0, buf);
+        tma_store2(&maps.out[1], lane0, t.n0 + c0, buf + 2 * kArea);
         tma_store_commit();
       }
     } else {
       __syncwarp();
-      const int mine = sorted_row(t, c0, lane);
-      __nv_bfloat16* d_gate = reinterpret_cast<__nv_bfloat16*>(p.out);
-      flush_bf16<16>(p, lane, buf, mine, lane0, d_gate, p.ld);
-      flush_bf16<16>(p, lane, buf + kArea, mine, lane0, d_gate + p.lanes, p.ld);
-      flush_bf16<16>(p, lane, buf + 2 * kArea, mine, lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
+      const int x = lane0 + 8 * (lane & 3);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int column = 8 * i + (lane >> 2);
+        const uint4 u0 = lds16(buf + piece2(column, 0, lane & 3)), u1 = lds16(buf + piece2(column, 1, lane & 3));
+        if (c0 + column < t.ncols && x < p.lanes) {
+          __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)(t.n0 + c0 + column) * p.ld + x;
+          *reinterpret_cast<uint4*>(to) = u0;
+          *reinterpret_cast<uint4*>(to + p.lanes) = u1;
+        }
+      }
+      flush_bf16<16>(p, lane, buf + 2 * kArea, sorted_row(t, c0, lane), lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
       written();            // (boxes of the chunk after the next come here)
     }
     if (p.partial) {
@@ -532,6 +543,12 @@ bool box_map(CUtensorMap* out, const void* base, bool fp32, int64_t rows, int64_
   const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows}, strides[1] = {(uint64_t)ld};
   const uint32_t box[2] = {(uint32_t)width, (uint32_t)height};
   return dx_box_map(out, base, fp32, 2, dims, strides, box);
+}
+// boxes of 32 columns of both halves (of `cols` each) of sixteen rows
+bool halves_map(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld) {
+  const uint64_t dims[3] = {(uint64_t)cols, 2, (uint64_t)rows}, strides[2] = {(uint64_t)cols, (uint64_t)ld};
+  const uint32_t box[3] = {32, 2, 16};
+  return dx_box_map(out, base, false, 3, dims, strides, box);
 }
 }  // namespace
 
@@ -669,13 +686,9 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)a.n, (uint64_t)a.n_groups};
   const uint64_t strides[2] = {(uint64_t)a.ldw, (uint64_t)a.w_stride};
   const uint32_t box[3] = {64, 64, 1};
-  const __nv_bfloat16 *gu = reinterpret_cast<const __nv_bfloat16*>(gate_up), *d_gu = reinterpret_cast<const __nv_bfloat16*>(a.y);
   if (!dx_tensor_map(&m.a, a.w, 3, dims, strides, box) || !rows_source(&m, &p, a, a.n) ||
-      !box_map(&m.in[0], gu, false, a.n_rows, a.k, ld_gate_up, 32, 16) ||
-      !box_map(&m.in[1], gu + a.k, false, a.n_rows, a.k, ld_gate_up, 32, 16) ||
-      !box_map(&m.out[0], d_gu, false, a.n_rows, a.k, a.ldy, 32, 16) ||
-      !box_map(&m.out[1], d_gu + a.k, false, a.n_rows, a.k, a.ldy, 32, 16) ||
-      !box_map(&m.out[2], act_w, false, a.n_rows, a.k, ld_act, 32, 16))
+      !halves_map(&m.in, gate_up, a.n_rows, a.k, ld_gate_up) || !halves_map(&m.out[0], a.y, a.n_rows, a.k, a.ldy) ||
+      !box_map(&m.out[1], act_w, false, a.n_rows, a.k, ld_act, 32, 16))
     return cudaErrorInvalidValue;
   cudaError_t e = launch_rows<kRowsT, StoreSwigluGrad>(ctx, m, p, st);
   *n_launches = 1;

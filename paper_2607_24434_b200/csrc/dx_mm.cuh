@@ -331,7 +331,7 @@ struct MmMaps {
   CUtensorMap a, b;       // boxes of rows
   CUtensorMap b_few;      // of fewer rows
   CUtensorMap out[3];     // outputs that go out in boxes
-  CUtensorMap in[2];      // (SwiGLU gradient) gate and up
+  CUtensorMap in;         // (SwiGLU gradient) gate and up
 };
 // Division of 0 <= q < 2^31 by a constant d of the launch: q factor >> shift with shift = 31 + ceil(log2 d) and
 // factor = ceil(2^shift / d) < 2^32 (exact: factor d - 2^shift < d <= 2^(shift - 31), so the error stays below 1 / d).  d = 1: factor 0.
@@ -757,7 +757,6 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         if (!mbar_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
         const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
         if constexpr (FORM == kOuter) {
-          static_assert(FORM != kOuter || kHalf == 128);
           // columns x0 + 64 b + 8 piece of a matrix: inside it, or zeros
           if (do_a) {
             const unsigned char* from = reinterpret_cast<const unsigned char*>(p.a_src) + 2 * (int64_t)(m0 + 8 * piece);
@@ -774,8 +773,10 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             const unsigned char* from = reinterpret_cast<const unsigned char*>(p.b_src) + 2 * (x + 8 * piece);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              copy_rows(db + j * 4096u, from, at_b[j], ok_b[j], n0 + 8 * piece < p.columns, 0);
-              if (half > 64) copy_rows(db + 8192u + j * 4096u, from, at_b[j], ok_b[j], n0 + 64 + 8 * piece < p.columns, 128);
+#pragma unroll
+              for (int b = 0; b < kHalf / 64; ++b)
+                if (64 * b < half)
+                  copy_rows(db + b * 8192u + j * 4096u, from, at_b[j], ok_b[j], n0 + 64 * b + 8 * piece < p.columns, 128 * b);
             }
           }
         } else {
@@ -854,7 +855,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       typename Epilogue::Values v;
       if (tile.kblocks == 0) {                                       // (an empty group's product over its rows)
         epi.zero(v);
-        for (int c = kCols * share; c < tile.ncols; c += 2 * kCols) epi.chunk(tile, lane0, c, v, [] {});
+        for (int c = kCols * share; c < tile.ncols && lane0 < p.lanes; c += 2 * kCols) epi.chunk(tile, lane0, c, v, [] {});
         continue;
       }
       const int buf = turn & 1;
@@ -862,7 +863,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       tc_fence_after();
       const uint32_t base = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)buf * kAccCols;
       int c = kCols * share;
-      const int end = (tile.ncols + Epilogue::kRound - 1) / Epilogue::kRound * Epilogue::kRound;
+      const int lanes = FORM == kHead ? tile.rows : p.lanes;
+      const int end = lane0 >= lanes ? 0 : (tile.ncols + Epilogue::kRound - 1) / Epilogue::kRound * Epilogue::kRound;
       auto taken = [&]() {                     // the accumulator may be written again
         tc_fence_before();
         __syncwarp();
