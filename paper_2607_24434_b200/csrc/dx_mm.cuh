@@ -310,6 +310,11 @@ __device__ __forceinline__ void arrive_at_first(uint32_t bar) {
   asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\t"
                "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
 }
+// A whole warp's wait: all lanes go on or none (those behind a lane that gave up would wait for it at their next exchange).
+template <bool PAIR = false>
+__device__ __forceinline__ bool mm_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  return __all_sync(0xffffffffu, PAIR ? pair_wait(bar, parity, abort_flag, limit) : mbar_wait(bar, parity, abort_flag, limit)) != 0;
+}
 // Wait of the warps that store finished tiles: lane 0 polls with pauses, so that their scheduler partitions stay free for
 // the copying and the multiplying warp.
 __device__ __forceinline__ bool mm_store_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit, int lane) {
@@ -610,7 +615,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         // both operands: nothing of another group's rows, not even a NaN, gets in).
         const bool tail = FORM == kOuter && tile.rows - k0 < kMmK;
         const bool here = FORM != kOuter || (!tail && !(for_a ? p.a_index : p.b_index));
-        if (!mbar_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
+        if (!mm_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
         const uint32_t bar = smem_u32(&s->full[slot]);
         const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
         if (elect_one()) {
@@ -754,7 +759,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             ask(k0 + 4 * kMmK);
           }
         }
-        if (!mbar_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
+        if (!mm_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
         const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
         if constexpr (FORM == kOuter) {
           // columns x0 + 64 b + 8 piece of a matrix: inside it, or zeros
@@ -809,12 +814,11 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         if (tile.kblocks == 0) continue;
         const uint32_t idesc = mm_idesc(A_MN, B_MN, 128 * CG, mm_width<CG>(tile.ncols));
         const int buf = turn & 1;
-        if (!mbar_wait(smem_u32(&s->acc_empty[buf]), (uint32_t)((turn >> 1) & 1) ^ 1u, abort_flag, p.wait_limit)) break;
+        if (!mm_wait(smem_u32(&s->acc_empty[buf]), (uint32_t)((turn >> 1) & 1) ^ 1u, abort_flag, p.wait_limit)) break;
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)buf * kAccCols;
         for (int kb = 0; kb < tile.kblocks; ++kb) {
-          if (!(CG == 2 ? pair_wait(smem_u32(&s->full[slot]), phase, abort_flag, p.wait_limit)
-                        : mbar_wait(smem_u32(&s->full[slot]), phase, abort_flag, p.wait_limit))) { alive = false; break; }
+          if (!mm_wait<CG == 2>(smem_u32(&s->full[slot]), phase, abort_flag, p.wait_limit)) { alive = false; break; }
           // (no tcgen05 fence: the stage was written in, or made visible to, the tensor core's proxy; a fence drains the pipe)
           const uint32_t a = ring_a + slot * (uint32_t)(kStage >> 4), b = ring_b + slot * (uint32_t)(kStage >> 4);
           if (elect_one()) {
