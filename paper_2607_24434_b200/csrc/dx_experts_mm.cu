@@ -621,7 +621,7 @@ cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t
   if (a.w_rows) {
     p.n_live = a.n_live;
     p.group_rows = a.group_rows;
-    p.a_step = a.n;
+    p.shared_out = (a.w_rows + kMmK - 1) / kMmK;
     p.kdim = a.w_rows;
   }
   const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)(a.w_rows ? a.w_rows : a.n), (uint64_t)(a.w_rows ? 1 : a.n_groups)};

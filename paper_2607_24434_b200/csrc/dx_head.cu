@@ -12,7 +12,7 @@
 // The second pass over the products costs 2 N V H operations beside the 6 N V H of loss and gradients; what it saves is
 // N V logits in fp32 (they cannot be kept in bf16: a logit of 20 would be off by 0.06, its probability by 6 %).  For few rows
 // -- a verified block -- the logits are little and the head's bytes are the time: there they are kept (kKeepMost), and the
-// vocabulary is cut into blocks whose shares of dh different SMs sum, in fp32, added up in order afterwards (dh alone has no
+// vocabulary is dealt out to blocks whose shares of dh different SMs sum, in fp32, added up in order afterwards (dh alone has no
 // more tiles than H / 128: 16 of 148 SMs at H = 2048).
 #include "dx_mm.cuh"
 
@@ -21,6 +21,7 @@ namespace {
 // ---- 1: which rows count -------------------------------------------------------------------------------------------
 // One CTA, a thread for every 1/1024 of the rows: counted, summed over the CTA, listed.  live[i]: the i-th row that counts; rows
 // that do not have loss 0 (a target outside the vocabulary: NaN).
+constexpr int kListed = 256;      // rows up to which every row's CTA counts those in front of it
 __device__ __forceinline__ bool row_counts(const int32_t* targets, const float* row_weight, int r, int V, bool& bad) {
   const int t = __ldg(targets + r);
   const float w = row_weight ? __ldg(row_weight + r) : 1.0f;
@@ -67,6 +68,32 @@ __global__ void __launch_bounds__(1024) dx_head_rows_kernel(const int32_t* targe
     n_live[0] = 0;        // (offsets of the one group that the products of the gradients see)
     n_live[1] = all;
   }
+}
+// Few rows (a thread for each): a CTA per row counts those in front of its own and does both.  One launch instead of two and
+// no list to wait for.
+__global__ void __launch_bounds__(kListed) dx_head_few_kernel(const int32_t* targets, const float* row_weight, int N, int V,
+                                                              const __nv_bfloat16* h, int64_t ldh, int H, int32_t* live,
+                                                              int32_t* n_live, float* loss, __nv_bfloat16* out,
+                                                              int32_t* dev_status) {
+  dx_pdl_wait();
+  dx_pdl_trigger();
+  const int mine = blockIdx.x, r = threadIdx.x;
+  bool bad = false, own_bad;
+  const bool in_front = r < mine && row_counts(targets, row_weight, r, V, bad);
+  const int at = __syncthreads_count(in_front);
+  const bool in = row_counts(targets, row_weight, mine, V, own_bad);
+  if (r == 0) {
+    if (own_bad) atomicExch(dev_status, (int32_t)DX_DEV_BAD_TOKEN);
+    if (!in && loss) loss[mine] = own_bad ? __int_as_float(0x7fffffff) : 0.0f;
+    if (in) live[at] = mine;
+    if (mine == N - 1) {
+      n_live[0] = 0;
+      n_live[1] = at + (in ? 1 : 0);
+    }
+  }
+  if (!in) return;
+  for (int i = r * 8; i < H; i += kListed * 8)
+    *reinterpret_cast<uint4*>(out + (int64_t)at * H + i) = __ldg(reinterpret_cast<const uint4*>(h + mine * ldh + i));
 }
 // the listed rows next to each other: four rows per CTA
 __global__ void __launch_bounds__(256) dx_head_pack_kernel(const __nv_bfloat16* h, int64_t ldh, int H, const int32_t* live,
@@ -158,7 +185,7 @@ struct RowSums {
     top = m;
   }
   __device__ __forceinline__ void end(const MmTile& t) {
-    if (row >= 0) p.part[(int64_t)(t.row0 * 2 + share) * p.part_pitch + row] = make_float2(top, sum);
+    if (row >= 0) p.part[(t.row0 * 2 + share) * p.part_half + row * p.part_row] = make_float2(top, sum);
   }
 };
 
@@ -271,24 +298,82 @@ struct StoreDz {
   }
 };
 
-// ... from logits that were kept: eight per thread, rows in blockIdx.y
-__global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, int64_t ld_logits, int V, const int32_t* live,
+// Little work (N V): a CTA joins the tiles of one row (blockIdx.y) ...
+// ... and, where the logits were kept, goes on to eight elements of dz per thread; all CTAs of a row join it in the same order (a
+// kernel for that, between this one and the products, took 8 us where this takes 2).
+__global__ void __launch_bounds__(256) dx_head_row_kernel(const float* logits, int64_t ld_logits, int V, const int32_t* live,
                                                          const int32_t* n_live, const int32_t* targets,
-                                                         const float* row_weight, const float* lse, const float* row_loss,
-                                                         __nv_bfloat16* dz, int panel) {
+                                                         const float* row_weight, const float2* part, int halves,
+                                                         const float* target_logit, float* loss, float* lses, float* row_losses,
+                                                         __nv_bfloat16* dz, int panel, int H, __nv_bfloat16* dh, int64_t ld_dh) {
+  __shared__ float tops[8], row_loss_at, lse_at;
+  __shared__ double sums[8];
   dx_pdl_wait();
   dx_pdl_trigger();
-  const int row = blockIdx.y, v0 = (blockIdx.x * 256 + threadIdx.x) * 8;
-  if (row >= __ldg(n_live) || v0 >= (V + 63) / 64 * 64) return;
+  const int row = blockIdx.y, v0 = (blockIdx.x * 256 + threadIdx.x) * 8, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x == 0 && dh) {          // (of the rows as they were given)
+    bool bad;
+    if (!row_counts(targets, row_weight, row, V, bad))
+      for (int i = threadIdx.x; i < H / 8; i += 256) *reinterpret_cast<uint4*>(dh + row * ld_dh + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  if (row >= __ldg(n_live)) return;
   const int r = __ldg(live + row), target = __ldg(targets + r) - v0;
-  const float weight = row_weight ? __ldg(row_weight + r) : 1.0f, l = __ldg(lse + row);
-  const float4 a = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0);
-  const float4 b = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0 + 4);
-  float z[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  const float at_target = target >= 0 && target < 8 ? weight * expm1f(-__ldg(row_loss + row)) : 0.0f;
+  const float weight = row_weight ? __ldg(row_weight + r) : 1.0f, z_target = __ldg(target_logit + row);
+  float z[8];
+  const bool here = logits && v0 < (V + 63) / 64 * 64;
+  if (here) {
+    const float4 a = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0);
+    const float4 b = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0 + 4);
+    z[0] = a.x; z[1] = a.y; z[2] = a.z; z[3] = a.w; z[4] = b.x; z[5] = b.y; z[6] = b.z; z[7] = b.w;
+  }
+  part += (int64_t)row * halves;
+  float top = -INFINITY;
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < halves; i += 1024) {
+    float2 q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = i + 256 * j < halves ? __ldg(part + i + 256 * j) : make_float2(-INFINITY, 0.0f);
+    const float m = fmaxf(top, fmaxf(fmaxf(q[0].x, q[1].x), fmaxf(q[2].x, q[3].x))), from = m == -INFINITY ? 0.0f : m;
+    sum *= ex2((top - from) * kLog2e);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += q[j].y * ex2((q[j].x - from) * kLog2e);
+    top = m;
+  }
+  float m = top;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (lane == 0) tops[warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) m = fmaxf(m, tops[w]);
+  const float from = m == -INFINITY ? 0.0f : m;
+  sum *= ex2((top - from) * kLog2e);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0) sums[warp] = sum;
+  __syncthreads();
+  if (warp == 0) {
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) sum += sums[w];
+    const double log_sum = log(sum);
+    if (lane == 0) {
+      row_loss_at = (float)(((double)m - (double)z_target) + log_sum);
+      lse_at = (float)((double)m + log_sum);
+      if (blockIdx.x == 0) {
+        if (loss) loss[r] = row_loss_at;
+        lses[row] = lse_at;
+        row_losses[row] = row_loss_at;
+      }
+    }
+  }
+  __syncthreads();
+  if (!here) return;
+  const float row_loss = row_loss_at, lse = lse_at;
+  const float at_target = target >= 0 && target < 8 ? weight * expm1f(-row_loss) : 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    z[i] = weight * ex2((z[i] - l) * kLog2e);
+    z[i] = weight * ex2((z[i] - lse) * kLog2e);
     if (i == target) z[i] = at_target;
     if (v0 + i >= V) z[i] = 0.0f;
   }
@@ -319,12 +404,13 @@ constexpr size_t kKeepMost = size_t(64) << 20;     // bytes of logits that are k
 constexpr int kFewest = 32768;                     // rows up to which a CTA per row (and block) will do
 
 struct HeadPlan {
+  bool by_row;               // a CTA or more for each row joins its tiles
   bool keep;                 // logits are kept
   int tiles;                 // of the first pass, along the vocabulary
   int piece;                 // words of a piece (a multiple of 256)
-  int blocks, block;         // blocks of a piece whose shares of dh are summed apart (1: the piece), words of a block
+  int blocks;                // shares of dh that are summed apart
   size_t live, n_live, rows, part, target_logit, lse, row_loss, dh_acc, logits, share, dz, bytes;
-  int pitch, width;          // words of a tile of the first pass
+  int pitch, width;          // rows of a half tile's sums (where they are joined by themselves), words of a tile of the first pass
   int64_t ld_logits;
 };
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -362,13 +448,14 @@ HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
   }
   s.tiles = (V + s.width - 1) / s.width;
   s.part = take((size_t)s.tiles * 2 * s.pitch * sizeof(float2));
+  s.by_row = (size_t)N * words * 4 <= kKeepMost && N <= kFewest;
   s.blocks = 1;
-  s.piece = s.block = (int)words;
+  s.piece = (int)words;
   s.bytes = at;
   if (!grad) return s;
   const size_t fixed = at, column = (size_t)N * 2;
   // words of a piece: all of them, or as many as the space allows, in pieces of equal length
-  s.keep = (size_t)N * words * 4 <= kKeepMost && N <= kFewest && space != 1;
+  s.keep = s.by_row && space != 1;
   int64_t piece = (int64_t)(kPieceBest / column / 256 * 256);
   if (piece < 256 || space == 1) piece = 256;
   for (bool lean = space == 1;; lean = true) {
@@ -384,25 +471,21 @@ HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
     const int64_t pieces = (words + piece - 1) / piece;
     piece = (words / 256 + pieces - 1) / pieces * 256;
     s.blocks = 1;
-    s.block = (int)piece;
     if (!lean && N <= kFewest) {
-      // dh has few tiles where there are few rows, and rarely a multiple of what runs at a time: cut a piece's words into as many
-      // blocks as fill the GPU best, their shares of dh summed apart.  Rates in words and bytes per microsecond: a pair of CTAs
+      // dh has few tiles where there are few rows, and rarely a multiple of what runs at a time: a piece's words are dealt out to as
+      // many blocks as fill the GPU best, their shares of dh summed apart.  Rates in words and bytes per microsecond: a pair of CTAs
       // multiplies 256 x 256 x 64 in a third of a microsecond; few rows wait for the head's bytes instead.
       const bool few = N <= 32;
       const int64_t tiles = ((H + (few ? 127 : 255)) / (few ? 128 : 256)) * (int64_t)((N + (few ? 63 : 255)) / (few ? 64 : 256));
       const int64_t units = few ? sm_count : sm_count / 2;
       const double wave = few ? (double)piece * 256.0 * units / 6e6 : (double)piece / 64.0 * 0.33;
       double least = 0.0;
-      for (int b = 1; b <= 32; ++b) {
-        const int block = (int)((piece / 256 + b - 1) / b) * 256;
-        const int n = (int)((piece + block - 1) / block);
+      for (int n = 1; n <= 32 && n <= piece / 256; ++n) {
         const double cost = (double)pieces * (double)((n * tiles + units - 1) / units) * wave / n +
                             (n > 1 ? n * (double)N * H * 8.0 / 6e6 + 4.0 : 0.0);
-        if (b == 1 || cost < least) {
+        if (n == 1 || cost < least) {
           least = cost;
           s.blocks = n;
-          s.block = block;
         }
       }
     }
@@ -478,7 +561,8 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   p.targets = a.targets;
   p.row_weight = a.row_weight;
   p.part = part;
-  p.part_pitch = s.pitch;
+  p.part_half = s.by_row ? 1 : s.pitch;
+  p.part_row = s.by_row ? 2 * s.tiles : 1;
   p.target_logit = target_logit;
   p.lse = lse;
   p.row_loss = row_loss;
@@ -488,24 +572,33 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   p.wait_limit = ctx->wait_limit;
 
   const bool pdl = (ctx->pdl_mask & DX_PDL_EXPERTS) != 0;
-  if (!launched(dx_launch_pdl(pdl, dx_head_rows_kernel, dim3(1), dim3(1024), 0, st, 1, a.targets, a.row_weight, a.N, a.V, live,
-                              n_live, a.loss, ctx->dev_status))) return e;
-  if (!launched(dx_launch_pdl(pdl, dx_head_pack_kernel, dim3((a.N + 3) / 4), dim3(256), 0, st, 1,
-                              reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, rows))) return e;
+  if (a.N <= kListed) {
+    if (!launched(dx_launch_pdl(pdl, dx_head_few_kernel, dim3(a.N), dim3(kListed), 0, st, 1, a.targets, a.row_weight, a.N, a.V,
+                                reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live, a.loss, rows,
+                                ctx->dev_status))) return e;
+  } else {
+    if (!launched(dx_launch_pdl(pdl, dx_head_rows_kernel, dim3(1), dim3(1024), 0, st, 1, a.targets, a.row_weight, a.N, a.V, live,
+                                n_live, a.loss, ctx->dev_status))) return e;
+    if (!launched(dx_launch_pdl(pdl, dx_head_pack_kernel, dim3((a.N + 3) / 4), dim3(256), 0, st, 1,
+                                reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, rows))) return e;
+  }
   p.tile_width = s.width;
   if (!launched(s.keep ? launch_head<RowSums<true>>(ctx, m, p, st) : launch_head<RowSums<false>>(ctx, m, p, st))) return e;
   p.tile_width = 0;
-  if (!launched(dx_launch_pdl(pdl, dx_head_join_kernel, dim3((a.N + 31) / 32), dim3(1024), 0, st, 1, part, s.pitch, 2 * s.tiles, live,
+  if (s.by_row) {
+    // (logits that are kept become dz in the same launch)
+    if (!launched(dx_launch_pdl(pdl, dx_head_row_kernel, dim3(s.keep ? (a.V + 2047) / 2048 : 1, a.N), dim3(256), 0, st, 1,
+                                s.keep ? logits : nullptr, s.ld_logits, a.V, live, n_live + 1, a.targets, a.row_weight, part,
+                                2 * s.tiles, target_logit, a.loss, lse, row_loss, dz, a.N, a.H, dh, a.ld_dh))) return e;
+  } else if (!launched(dx_launch_pdl(pdl, dx_head_join_kernel, dim3((a.N + 31) / 32), dim3(1024), 0, st, 1, part, s.pitch, 2 * s.tiles, live,
                               n_live + 1, target_logit, a.loss, lse, row_loss, a.targets, a.row_weight, a.N, a.V, a.H, dh,
-                              a.ld_dh)) || !grad) return e;
+                              a.ld_dh))) return e;
+  if (!grad) return e;
 
   for (int64_t v0 = 0; v0 < a.V; v0 += s.piece) {
     const int len = (int)(a.V - v0 < s.piece ? a.V - v0 : s.piece);
     const bool first = v0 == 0, last = v0 + len == a.V;
-    if (s.keep) {
-      if (!launched(dx_launch_pdl(pdl, dx_head_dz_kernel, dim3((a.V + 2047) / 2048, a.N), dim3(256), 0, st, 1, logits, s.ld_logits,
-                                  a.V, live, n_live + 1, a.targets, a.row_weight, lse, row_loss, dz, a.N))) return e;
-    } else {
+    if (!s.keep) {
       MmParams q = p;
       q.columns = len;
       q.column0 = (int)v0;
@@ -520,7 +613,7 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
       g.ldx = kPanel;
       g.w = reinterpret_cast<const unsigned char*>(a.W) + v0 * a.ldw * 2;
       g.n_groups = s.blocks;
-      g.n = s.block;
+      g.n = len;
       g.k = a.H;
       g.transposed = 1;
       g.ldw = a.ldw;

@@ -295,8 +295,8 @@ struct DxGroupedMm {
   int y_fp32, y_rows;
   int64_t ldy;
   const float* addend;       // fp32 [y_rows][columns of y], added in front of the rounding (transposed only)
-  // one matrix of w_rows rows cut into groups of n rows (a multiple of 256; the last one shorter), every group with the same
-  // number *n_live of sorted rows, group_rows apart; x is then [w_rows / 256][group_rows][256] (offsets are not used; transposed)
+  // one matrix of w_rows rows whose contraction the groups share out, every group with the same number *n_live of sorted rows,
+  // group_rows apart; x is then [w_rows / 256][group_rows][256] (offsets are not used; transposed)
   int w_rows, group_rows;
   const int32_t* n_live;
 };

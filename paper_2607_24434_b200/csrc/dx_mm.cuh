@@ -36,6 +36,7 @@ constexpr int kMmK = 64;                    // contraction elements of a stage: 
 constexpr int kMmA = 128 * kMmK * 2;        // bytes of a CTA's 128 rows of A in a stage
 constexpr int kMmMaxStages = 8;
 constexpr uint32_t kDrainPolls = 1u << 16;  // of a barrier that may never complete, after something gave up
+constexpr int kDealt = 4;                   // (a panel's)
 constexpr int kPanel = 256;                 // columns of a panel: a tile's, so that a tile's rows lie close together
 
 // ---- PTX ---------------------------------------------------------------------------------------------------------
@@ -376,11 +377,12 @@ struct MmParams {
   void* act_w;
   int64_t ld_act;
   float* partial;                // [warps of lanes][n_rows] shares of the pair weights' gradients
-  // Groups of *n_live rows each, group_rows apart, instead of offsets; their matrices follow one another in one (a_step rows each),
-  // and the rows' elements along all of them stand in panels of kPanel columns, one below the other, group_rows rows each.
+  // Groups of *n_live rows each, group_rows apart, instead of offsets, that share out one product's contraction: kDealt blocks of
+  // kMmK rows of the one matrix in turns, from its end (which was read last) to its beginning.  The rows' elements stand in panels
+  // of kPanel columns, one below the other, group_rows rows each.
   const int32_t* n_live;         // (loss) rows that count
   int group_rows;
-  int a_step;
+  int shared_out;                // blocks of kMmK rows of the matrix (0: a matrix per group)
   int b_panel;                   // (products over rows) rows of a panel of B (0: no panels)
   // loss
   float* logits;                 // [n_live][ld_logits], kept where that is little
@@ -389,8 +391,8 @@ struct MmParams {
   const int32_t* live;           // the rows that count
   const int32_t* targets;        // [..] by original row
   const float* row_weight;
-  float2* part;                  // [column tiles][pitch] (maximum, sum) of a tile
-  int part_pitch;
+  float2* part;                  // (maximum, sum) of halves of column tiles
+  int64_t part_half, part_row;   // from one half, one row to the next
   float* target_logit;           // [n_live]
   const float* lse;              // [n_live]
   const float* row_loss;         // [n_live]
@@ -489,7 +491,12 @@ struct MmSchedule {
       r.ncols = min(width, cnt - j * width);
       r.row0 = r.n0;
       r.rows = r.ncols;
-      r.kblocks = ((p.a_step ? min(p.a_step, p.kdim - e * p.a_step) : p.kdim) + kMmK - 1) / kMmK;
+      if (p.shared_out) {
+        const int turn = kDealt * p.n_groups, turns = p.shared_out / turn;
+        r.kblocks = turns * kDealt + min(max(p.shared_out - turns * turn - kDealt * e, 0), kDealt);
+      } else {
+        r.kblocks = (p.kdim + kMmK - 1) / kMmK;
+      }
     }
     return r;
   }
@@ -601,6 +608,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     const bool for_a = warp == kWarpA, for_b = warp == kWarpB;
     uint32_t slot = 0, phase = 0, issued = 0;
     bool alive = true;
+    auto shared_row = [&](int e, int kb) { return (p.shared_out - 1 - (kb / kDealt * p.n_groups + e) * kDealt - kb % kDealt) * kMmK; };
     for (int t = unit; t < total && alive; t += n_units) {
       const MmTile tile = schedule.get(t).uniform_copy();
       const int half = mm_width<CG>(tile.ncols) / CG, m0 = tile.m0 + (int)rank * 128;
@@ -626,7 +634,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
             } else if constexpr (FORM == kSwiglu) {
               tma5<CG>(da, &maps.a, k0, 0, 0, m0 / 16, tile.e, bar);
             } else if constexpr (FORM == kRowsT) {
-              const int y = tile.e * p.a_step + k0, z = p.a_step ? 0 : tile.e;
+              const int y = p.shared_out ? shared_row(tile.e, kb) : k0, z = p.shared_out ? 0 : tile.e;
               tma3<CG>(da, &maps.a, m0, y, z, bar);
               tma3<CG>(da + 8192u, &maps.a, m0 + 64, y, z, bar);
             } else if constexpr (FORM == kOuter) {
@@ -645,8 +653,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
               for (int j = 0; j < kHalf / 128; ++j) tma2<CG>(db + j * 16384u, &maps.b, k0, p.column0 + n0 + 128 * j, bar);
             } else {
               int x = k0, y = n0;
-              if (FORM == kRowsT && p.a_step) {
-                const int at = tile.e * p.a_step + k0;
+              if (FORM == kRowsT && p.shared_out) {
+                const int at = shared_row(tile.e, kb);
                 x = at % kPanel;
                 y += (at / kPanel - tile.e) * p.group_rows;
               }

@@ -257,3 +257,22 @@ def test_training_step_of_a_routed_layer(dx):
     assert float((head["loss"].double() - loss.detach()).abs().max()) <= 0.02 * float(loss.detach().max())
     for name, have, ref in zip(("x", "router", "gate/up", "down", "head"), (d_x, dW_r, dW_gu, dW_d, head["dW"]), want):
         assert float((have.double() - ref).norm()) <= 0.02 * float(ref.norm()), name
+
+
+def test_a_short_last_piece_leaves_no_block_without_an_end(dx):
+    """Many rows, a short hidden row: dz is made in pieces of the vocabulary, the last one shorter, and a piece's words are dealt
+    out to many blocks; a block of the last piece that got no words at all would wait for products that nobody issues."""
+    binding, ctx = dx
+    h, W, t, _ = problem(11, 8192, 34816, 64, False)
+    out = binding.spec_head_loss(ctx, h, W, t)
+    assert ctx.device_status() == 0
+    rows = slice(0, 8192, 97)
+    check(h[rows], W, t[rows], None, {key: value[rows] for key, value in out.items()})
+
+
+@pytest.mark.parametrize("N", [255, 256, 257])
+def test_rows_listed_by_their_own_blocks_or_by_one(dx, N):
+    binding, ctx = dx
+    h, W, t, w = problem(N, N, 1200, 72)
+    h[(t < 0) | (w == 0)] = NAN
+    check(h, W, t, w, binding.spec_head_loss(ctx, h, W, t, row_weight=w, grad_weight=True))
