@@ -315,6 +315,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       tma3<1>(to, &maps.in, lane0, 0, t.n0 + c0, bar);
     }
   }
+  // whether any chunk of a tile is the warp's
+  __device__ __forceinline__ bool chunks(const MmTile& t, int lane0, int c0) const { return lane0 < p.lanes && c0 < t.ncols; }
   // The weights of the warp's share of a tile's columns, all at once.  An index and the weight behind it are two trips to L2:
   // they are asked for while the tile in front is still being stored.
   __device__ __forceinline__ void ask_pairs(const MmTile& t) {
@@ -345,7 +347,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
     next = next_;
     more = more_;
     if (more) ask_pairs(next);
-    if (c0 >= t.ncols && more) ask_weights();        // (no chunk of this tile is the warp's)
+    if (!chunks(t, lane0, c0) && more) ask_weights();        // (the last chunk does it otherwise)
   }
   __device__ __forceinline__ void finish() {
     if (asked && lane == 0) {      // (the loop over the tiles ended early: no box may still be landing)
@@ -358,11 +360,12 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
   __device__ __forceinline__ void ask_next(const MmTile& t, int lane0, int c0) {
     const bool here = c0 + 2 * kCols < t.ncols;
     if (!here && more) ask_weights();
-    asked = here || (more && kCols * share < next.ncols);
+    const int next0 = next.m0 + lane0 - t.m0;
+    asked = here || (more && chunks(next, next0, kCols * share));
     if (!asked) return;
     if (lane == 0) tma_store_read();
     if (here) fetch(turn + 1, t, lane0, c0 + 2 * kCols);
-    else fetch(turn + 1, next, next.m0 + lane0 - t.m0, kCols * share);
+    else fetch(turn + 1, next, next0, kCols * share);
   }
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, Values& x, Taken taken) {

@@ -167,7 +167,8 @@ def routed(g, N, k, E):
 
 
 @pytest.mark.parametrize("N,k,E,H,I", [(1, 2, 5, 64, 8), (7, 3, 9, 136, 40), (40, 8, 8, 264, 136), (333, 2, 3, 520, 200),
-                                       (1000, 6, 64, 256, 352)])
+                                       (1000, 6, 64, 256, 352), (1500, 4, 64, 64, 600), (1000, 6, 64, 64, 1416),
+                                       (300, 8, 100, 64, 328)])     # (the last three: tiles of no lanes between others)
 def test_swiglu_forward_and_backward(dx, N, k, E, H, I):
     """act and gate_up from the same fp32 products; the gradients from what was kept.  sigmoid is good to 2^-20 relative: 1 +
     ex2 and rcp 2^-22 each, the argument's rounding 2^-24 |x| with |x| below 8."""
