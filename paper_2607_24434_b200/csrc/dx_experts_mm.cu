@@ -564,23 +564,28 @@ bool dx_matrix_map(CUtensorMap* out, const void* base, int64_t rows, int64_t col
 namespace {
 
 // Few rows per group: the weights' bytes are the time, so tiles are small (128 lanes: twice as many CTAs have one, and eight
-// stages of 24 KB keep 128 KB of weights in flight per SM).  Otherwise pairs of CTAs with 256 lanes x 256 columns.
-bool few_rows(int64_t rows, int groups) { return rows <= 32 * (int64_t)groups; }
-
-template <int FORM, class Epilogue>
+// stages of 24 KB keep 128 KB of weights in flight per SM).  Some rows, and matrices whose rows are the contraction: 128 lanes
+// with 128 columns (64 groups of 64 rows x 2048 x 1408: 67.5 us, in pairs 73.7; its SwiGLU gradient 92, in pairs 98; of 128 rows 88
+// and 135, in pairs 80 and 119.  The other forms lose with it at 40 rows already: SwiGLU 137 us, in pairs 133).  Otherwise pairs
+// of CTAs with 256 lanes x 256 columns.
+template <int FORM, bool GATHER, class Epilogue>
 cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cudaStream_t st) {
-  const bool few = few_rows(p.n_rows, p.n_groups);
-  const long long lanes = few ? 128 : 256, bn = few ? 64 : 256;
+  const bool few = p.n_rows <= kFewRows * (int64_t)p.n_groups;
+  const bool some = FORM == kRowsT && !few && p.n_rows <= kSomeRows * (int64_t)p.n_groups;
+  const long long lanes = few || some ? 128 : 256, bn = few ? 64 : some ? 128 : 256;
   // (every group may end in a tile that is not full)
   const long long most = ((p.lanes + lanes - 1) / lanes) *
                          ((p.n_rows + bn - 1) / bn + (p.n_groups < p.n_rows ? p.n_groups : p.n_rows));
   // (stages: as many as the staging leaves room for)
   constexpr int kFew = Epilogue::kStaging > 4096 ? 6 : 8, kMany = Epilogue::kStaging > 4096 ? 5 : 6;
-  if (p.b_index)
-    return few ? mm_launch<FORM, true, 1, 64, kFew, Epilogue>(ctx, maps, p, most, st)
-               : mm_launch<FORM, true, 2, 256, kMany, Epilogue>(ctx, maps, p, most, st);
-  return few ? mm_launch<FORM, false, 1, 64, kFew, Epilogue>(ctx, maps, p, most, st)
-             : mm_launch<FORM, false, 2, 256, kMany, Epilogue>(ctx, maps, p, most, st);
+  if (few) return mm_launch<FORM, GATHER, 1, 64, kFew, Epilogue>(ctx, maps, p, most, st);
+  if constexpr (FORM == kRowsT)
+    if (some) return mm_launch<FORM, GATHER, 1, 128, kMany, Epilogue>(ctx, maps, p, most, st);
+  return mm_launch<FORM, GATHER, 2, 256, kMany, Epilogue>(ctx, maps, p, most, st);
+}
+template <int FORM, class Epilogue>
+cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cudaStream_t st) {
+  return p.b_index ? launch_rows<FORM, true, Epilogue>(ctx, maps, p, st) : launch_rows<FORM, false, Epilogue>(ctx, maps, p, st);
 }
 
 // the rows (columns of D): a tensor map, or the matrix they are gathered from

@@ -475,8 +475,8 @@ HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
       // dh has few tiles where there are few rows, and rarely a multiple of what runs at a time: a piece's words are dealt out to as
       // many blocks as fill the GPU best, their shares of dh summed apart.  Rates in words and bytes per microsecond: a pair of CTAs
       // multiplies 256 x 256 x 64 in a third of a microsecond; few rows wait for the head's bytes instead.
-      const bool few = N <= 32;
-      const int64_t tiles = ((H + (few ? 127 : 255)) / (few ? 128 : 256)) * (int64_t)((N + (few ? 63 : 255)) / (few ? 64 : 256));
+      const bool few = N <= kSomeRows;          // (one tile of them)
+      const int64_t tiles = few ? (H + 127) / 128 : ((H + 255) / 256) * (int64_t)((N + 255) / 256);
       const int64_t units = few ? sm_count : sm_count / 2;
       const double wave = few ? (double)piece * 256.0 * units / 6e6 : (double)piece / 64.0 * 0.33;
       double least = 0.0;
