@@ -456,3 +456,60 @@ def test_refusals(dx):
     with pytest.raises(binding.DxError) as err:
         binding.moe_combine_tokens(ctx, x.repeat(9, 1)[:9], None, top_k=9)
     assert err.value.status == 8
+
+
+@pytest.mark.parametrize("E,mean", [(256, 9), (150, 60), (70, 200)])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_many_tiles_one_after_another(dx, E, mean, transposed):
+    """Each block of the grid has several tiles, full ones and others, of groups of very different lengths, empty ones among them."""
+    binding, ctx = dx
+    g = rng(E + mean)
+    counts = (torch.rand(E, generator=g, device="cuda") ** 2 * 3 * mean).int().tolist()
+    counts[3] = counts[E - 2] = 0
+    n, k, P = 328, 264, sum(counts)
+    n_in, n_out = (n, k) if transposed else (k, n)
+    off = offsets_of(counts)
+    w, source = draw(g, E, n, k, scale=0.2), draw(g, 501, n_in)
+    index = torch.randint(0, 1002, (P,), generator=g, device="cuda", dtype=torch.int32)
+    to = torch.randperm(P, generator=g, device="cuda").to(torch.int32)
+    rows = source[(index // 2).long()]
+    want, size = (torch.zeros((P, n_out), dtype=torch.float64, device="cuda") for _ in range(2))
+    for e, here in groups(counts):
+        m = w[e].double() if transposed else w[e].double().t()
+        want[here], size[here] = rows[here].double() @ m, rows[here].double().abs() @ m.abs()
+    for dtype in (BF16, F32):
+        y = binding.moe_grouped_mm(ctx, source, w, off, transposed=transposed, gather=index, gather_div=2, scatter=to, out_dtype=dtype)
+        check(y[to.long()], want, size, n_in)
+        z = binding.moe_grouped_mm(ctx, rows, w, off, transposed=transposed, out_dtype=dtype)
+        assert torch.equal(z, y[to.long()])
+    if transposed:
+        return
+    dy = draw(g, P, n)
+    dw, dw_size = (torch.zeros((E, n, k), dtype=torch.float64, device="cuda") for _ in range(2))
+    for e, here in groups(counts):
+        a, b = dy[here].double(), rows[here].double()
+        dw[e], dw_size[e] = a.t() @ b, a.abs().t() @ b.abs()
+    got = binding.moe_grouped_mm_dw(ctx, dy, source, off, gather_x=index, x_div=2, out_dtype=F32)
+    check(got, dw, dw_size, max(counts))
+
+
+def test_results_do_not_depend_on_the_overlap_of_launches(dx):
+    """A chain of calls, each reading what the one in front wrote, with and without launches that start early: the same bits."""
+    binding, ctx = dx
+    g = rng(77)
+    E, H, I, N, k = 16, 264, 136, 130, 3
+    perm, counts = routed(g, N, k, E)
+    off, x = offsets_of(counts), draw(g, N, H)
+    wg, wd = draw(g, E, 2 * I, H, scale=0.1), draw(g, E, H, I, scale=0.1)
+    topk_w = torch.rand((N, k), generator=g, device="cuda")
+
+    def chain():
+        act = binding.moe_grouped_swiglu(ctx, x, wg, off, gather=perm, gather_div=k)["act"]
+        y = binding.moe_grouped_mm(ctx, act, wd, off, scatter=perm)
+        return act, y, binding.moe_combine_tokens(ctx, y, topk_w)
+
+    ctx.set_launch_overlap(0)
+    plain = chain()
+    ctx.set_launch_overlap(3)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(chain(), plain))
