@@ -128,8 +128,8 @@ dx_status dx_last_device_status(dx_ctx* ctx, void* stream, int32_t* dev_status_o
 dx_status dx_set_activation_split(dx_ctx* ctx, int32_t on);
 /* Which kernels are launched so that they may begin while the kernel in front of them on the stream drains
  * (programmatic stream serialization): bit 0 the routing kernel and the second kernel of moe_route_tokens, bit 1 the
- * expert kernels (and those of moe_grouped_*, moe_combine_* and spec_head_loss), bit 2 the greedy-accept kernels.  Default 3.  0 gives plain stream order everywhere; results never
- * depend on the mask. */
+ * expert kernels (and those of moe_grouped_*, moe_combine_* and spec_head_loss), bit 2 the greedy-accept kernels.
+ * Default 3.  0 gives plain stream order everywhere; results never depend on the mask. */
 dx_status dx_set_launch_overlap(dx_ctx* ctx, int32_t mask);
 /* Every wait inside a kernel (for a word another kernel publishes, for a copy into shared memory, for the other CTAs
  * of a cooperative launch) polls at most `polls` times, then records DX_DEV_WAIT_EXPIRED in the device status word and
@@ -481,7 +481,9 @@ dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, cons
  * capturable, the context's GPU need not be current); calls use no scratch of the context, so graphs of one context may
  * overlap.  The products run on the 5th-generation tensor cores: operands bf16, accumulators fp32, every output rounded
  * once (fp32: not at all).  Every matrix has a 16-byte aligned address, a row pitch (in elements) and sizes that are multiples
- * of 8; n_groups <= 256, otherwise any size.  (DX_ERR_UNSUPPORTED; outputs that overlap inputs: DX_ERR_INVALID_ARG.)
+ * of 8; n_groups <= 256, otherwise any size up to 2^35 elements from a matrix's first row to its last.  (DX_ERR_UNSUPPORTED
+ * beyond.)  Outputs must not overlap inputs or one another; of a matrix counts everything between its first and its last element,
+ * what lies between its rows too (DX_ERR_INVALID_ARG).
  *
  * Groups.  Sorted row r belongs to group e iff offsets[e] <= r < offsets[e+1] (offsets [n_groups+1], ascending, within
  * 0 .. n_rows; values outside are cut off and reported as DX_DEV_BAD_OFFSETS).  Groups may be empty; rows outside every group

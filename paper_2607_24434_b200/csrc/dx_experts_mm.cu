@@ -673,7 +673,7 @@ cudaError_t dx_launch_grouped_swiglu(dx_ctx* ctx, const DxGroupedMm& a, void* ga
                  : launch_rows<kSwiglu, StoreSwiglu<false>>(ctx, m, p, st);
 }
 
-int dx_swiglu_grad_parts(int n_inter) { return (n_inter + 255) / 256 * 8; }
+int dx_swiglu_grad_parts(int n_inter) { return (int)(((int64_t)n_inter + 255) / 256 * 8); }
 
 cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, const void* gate_up, int64_t ld_gate_up,
                                           const float* pair_w, int n_pairs, void* act_w, int64_t ld_act, float* partial,

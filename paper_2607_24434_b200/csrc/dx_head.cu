@@ -401,6 +401,7 @@ __global__ void __launch_bounds__(128) dx_head_sum_kernel(const float* share, in
 constexpr size_t kPieceBest = size_t(256) << 20;   // bytes of dz of a piece with which more would gain nothing
 constexpr size_t kKeepMost = size_t(64) << 20;     // bytes of logits that are kept (half of L2)
 
+constexpr int kByRow = 1 << 21;                    // words up to which every CTA of a row joins its tiles (V^2 / 2^18 pairs are read)
 constexpr int kFewest = 32768;                     // rows up to which a CTA per row (and block) will do
 
 struct HeadPlan {
@@ -448,7 +449,7 @@ HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
   }
   s.tiles = (V + s.width - 1) / s.width;
   s.part = take((size_t)s.tiles * 2 * s.pitch * sizeof(float2));
-  s.by_row = (size_t)N * words * 4 <= kKeepMost && N <= kFewest;
+  s.by_row = (size_t)N * words * 4 <= kKeepMost && words <= kByRow && N <= kFewest;
   s.blocks = 1;
   s.piece = (int)words;
   s.bytes = at;

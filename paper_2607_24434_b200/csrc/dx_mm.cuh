@@ -872,7 +872,10 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         continue;
       }
       const int buf = turn & 1;
-      if (!mm_store_wait(smem_u32(&s->acc_full[buf]), (uint32_t)(turn >> 1) & 1u, abort_flag, p.wait_limit, lane)) break;
+      // (the wait lasts as long as the tile's products: a limit for every 16384 blocks of the contraction, some 5 ms)
+      const uint64_t limit = (uint64_t)p.wait_limit * (1u + ((uint32_t)tile.kblocks >> 14));
+      if (!mm_store_wait(smem_u32(&s->acc_full[buf]), (uint32_t)(turn >> 1) & 1u, abort_flag,
+                         (uint32_t)(limit < UINT32_MAX ? limit : UINT32_MAX), lane)) break;
       tc_fence_after();
       const uint32_t base = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)buf * kAccCols;
       int c = kCols * share;

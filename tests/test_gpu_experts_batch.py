@@ -513,3 +513,14 @@ def test_results_do_not_depend_on_the_overlap_of_launches(dx):
     ctx.set_launch_overlap(3)
     for _ in range(20):
         assert all(torch.equal(a, b) for a, b in zip(chain(), plain))
+
+
+def test_a_long_contraction_is_no_wait_that_ran_out(dx):
+    """One group of two million rows: its only tile's products take several times as long as the context lets a kernel wait."""
+    binding, ctx = dx
+    ctx.set_wait_limit(1 << 15)
+    g, P = rng(5), (1 << 21) + 5
+    dy, x = draw(g, P, 8), draw(g, P, 16)
+    got = binding.moe_grouped_mm_dw(ctx, dy, x, offsets_of([P]), out_dtype=F32)
+    assert ctx.device_status() == 0
+    check(got[0], dy.double().t() @ x.double(), dy.double().abs().t() @ x.double().abs(), P)
