@@ -1101,8 +1101,8 @@ def spec_head_loss(ctx: Context, h: torch.Tensor, W_lm: torch.Tensor, targets: t
                    row_weight: Optional[torch.Tensor] = None, grad: bool = True, grad_weight: bool = False,
                    workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None
                    ) -> Dict[str, torch.Tensor]:
-    """Cross entropy of hidden rows h [N, H] against W_lm [V, H] (both bfloat16) at ``targets`` [N] (int32, -1 = none) without
-    the logits: ``loss`` [N], with ``grad`` ``dh`` [N, H] and with ``grad_weight`` ``dW`` [V, H], both times ``row_weight``.
+    """Cross entropy of hidden rows h [N, H] against W_lm [V, H] (both bfloat16) at ``targets`` [N] (int32, -1 =
+    none): ``loss`` [N], with ``grad`` ``dh`` [N, H] and with ``grad_weight`` ``dW`` [V, H], both times ``row_weight``.
     ``workspace``: a uint8 tensor of at least the library's least size (one of the size it asks for is made otherwise)."""
     ldh, ldw = _operand(ctx, h, "h"), _operand(ctx, W_lm, "W_lm", h.shape[1])
     (N, H), V = h.shape, W_lm.shape[0]
@@ -1136,7 +1136,7 @@ def spec_head_loss(ctx: Context, h: torch.Tensor, W_lm: torch.Tensor, targets: t
 
 
 def spec_head_loss_workspace(ctx: Context, N: int, V: int, H: int, grad: bool = True) -> Tuple[int, int]:
-    """Bytes of workspace ``spec_head_loss`` needs at least, and bytes with which it takes as few pieces as are of use."""
+    """Bytes of workspace ``spec_head_loss`` needs at least, and bytes that are of use (a third size in between works, too)."""
     least, best = C.c_size_t(0), C.c_size_t(0)
     _check(ctx.lib.spec_head_loss_workspace(ctx.handle, N, V, H, 1 if grad else 0, C.byref(least), C.byref(best)),
            "spec_head_loss_workspace")

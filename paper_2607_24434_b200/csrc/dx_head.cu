@@ -1,18 +1,19 @@
 // Cross entropy of hidden rows against a vocabulary (spec_head_loss): with z = W h, per row
 //     loss = log sum_v exp(z_v) - z_target,      dz = weight * (softmax(z) - 1_target),      dh = W^T dz,     dW = dz^T h
-// in pieces of the vocabulary; logits exist as tiles in tensor memory only.
+// with dz in pieces of the vocabulary, and the logits kept only where that is worth their bytes.
 //
 //   1. the rows that count (a target, a weight other than 0) are listed in order and copied next to each other: the others cost
 //      nothing below, whatever they hold
 //   2. products of the listed rows with the whole vocabulary; of every tile a row keeps (maximum, sum of exponentials) and,
 //      where the tile holds it, the target's logit
 //   3. the tiles' pairs are joined: loss, log of the sum
-//   4. (gradients) for each piece of the vocabulary the products once more, now straight to dz (rounded to bf16 once), then
+//   4. (gradients) for each piece of the vocabulary dz, rounded to bf16 once, from kept logits or from the products once more, then
 //      dh += dz W and dW = dz^T h as products of the kernel of the grouped experts with one group
-// The second pass over the products costs 2 N V H operations beside the 6 N V H of loss and gradients; what it saves is
-// N V logits in fp32 (they cannot be kept in bf16: a logit of 20 would be off by 0.06, its probability by 6 %).  For few rows
-// -- a verified block -- the logits are little and the head's bytes are the time: there they are kept (kKeepMost), and the
-// vocabulary is dealt out to blocks whose shares of dh different SMs sum, in fp32, added up in order afterwards (dh alone has no
+// A second pass over the products costs 2 N V H operations beside the 6 N V H of loss and gradients; what it saves is N V logits
+// in fp32 (they cannot be kept in bf16: a logit of 20 would be off by 0.06, its probability by 6 %), which cross to memory and
+// back at some 5.5 TB/s.  So long hidden rows keep them where there is room (4096 rows, 102400 words, H = 2048: all gradients
+// 4.30 ms, recomputed 5.11; 32768 words: H = 2048 1.40 ms, recomputed 1.61, H = 1024 0.87, recomputed 0.81).  For few rows
+// -- a verified block -- the logits are little and the head's bytes are the time: there they are always kept, and the vocabulary is dealt out to blocks whose shares of dh different SMs sum, in fp32, added up in order afterwards (dh alone has no
 // more tiles than H / 128: 16 of 148 SMs at H = 2048).
 #include "dx_mm.cuh"
 
@@ -298,6 +299,33 @@ struct StoreDz {
   }
 };
 
+// ... from logits that were kept, eight words of a row (lse, row_loss of that row; target: its place among the eight)
+__device__ __forceinline__ uint4 dz_of(const float* logits, float weight, float lse, float row_loss, int target, int left) {
+  float z[8];
+  asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(z[0]), "=f"(z[1]), "=f"(z[2]), "=f"(z[3]), "=f"(z[4]), "=f"(z[5]), "=f"(z[6]), "=f"(z[7]) : "l"(logits));
+  const float at_target = target >= 0 && target < 8 ? weight * expm1f(-row_loss) : 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    z[i] = weight * ex2((z[i] - lse) * kLog2e);
+    if (i == target) z[i] = at_target;
+    if (i >= left) z[i] = 0.0f;
+  }
+  return make_uint4(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]), bf16_pair(z[4], z[5]), bf16_pair(z[6], z[7]));
+}
+// words v0 .. v0 + len of all rows (blockIdx.x): dz of a piece
+__global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, int64_t ld_logits, int v0, int len, const int32_t* live,
+                                                         const int32_t* n_live, const int32_t* targets, const float* row_weight,
+                                                         const float* lse, const float* row_loss, __nv_bfloat16* dz, int panel) {
+  dx_pdl_wait();
+  dx_pdl_trigger();
+  const int row = blockIdx.x, v = (blockIdx.y * 256 + threadIdx.x) * 8;
+  if (row >= __ldg(n_live) || v >= (len + 63) / 64 * 64) return;
+  const int r = __ldg(live + row);
+  *reinterpret_cast<uint4*>(dz + ((int64_t)(v / kPanel) * panel + row) * kPanel + v % kPanel) =
+      dz_of(logits + row * ld_logits + v0 + v, row_weight ? __ldg(row_weight + r) : 1.0f, __ldg(lse + row), __ldg(row_loss + row),
+            __ldg(targets + r) - v0 - v, len - v);
+}
 // Little work (N V): a CTA joins the tiles of one row (blockIdx.y) ...
 // ... and, where the logits were kept, goes on to eight elements of dz per thread; all CTAs of a row join it in the same order (a
 // kernel for that, between this one and the products, took 8 us where this takes 2).
@@ -319,13 +347,7 @@ __global__ void __launch_bounds__(256) dx_head_row_kernel(const float* logits, i
   if (row >= __ldg(n_live)) return;
   const int r = __ldg(live + row), target = __ldg(targets + r) - v0;
   const float weight = row_weight ? __ldg(row_weight + r) : 1.0f, z_target = __ldg(target_logit + row);
-  float z[8];
   const bool here = logits && v0 < (V + 63) / 64 * 64;
-  if (here) {
-    const float4 a = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0);
-    const float4 b = *reinterpret_cast<const float4*>(logits + row * ld_logits + v0 + 4);
-    z[0] = a.x; z[1] = a.y; z[2] = a.z; z[3] = a.w; z[4] = b.x; z[5] = b.y; z[6] = b.z; z[7] = b.w;
-  }
   part += (int64_t)row * halves;
   float top = -INFINITY;
   double sum = 0.0;
@@ -369,16 +391,8 @@ __global__ void __launch_bounds__(256) dx_head_row_kernel(const float* logits, i
   }
   __syncthreads();
   if (!here) return;
-  const float row_loss = row_loss_at, lse = lse_at;
-  const float at_target = target >= 0 && target < 8 ? weight * expm1f(-row_loss) : 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    z[i] = weight * ex2((z[i] - lse) * kLog2e);
-    if (i == target) z[i] = at_target;
-    if (v0 + i >= V) z[i] = 0.0f;
-  }
   *reinterpret_cast<uint4*>(dz + ((int64_t)(v0 / kPanel) * panel + row) * kPanel + v0 % kPanel) =
-      make_uint4(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]), bf16_pair(z[4], z[5]), bf16_pair(z[6], z[7]));
+      dz_of(logits + row * ld_logits + v0, weight, lse_at, row_loss_at, target, V - v0);
 }
 
 // dh of the rows that count: the blocks' shares in order, rounded once
@@ -399,7 +413,10 @@ __global__ void __launch_bounds__(128) dx_head_sum_kernel(const float* share, in
 
 // ---- workspace -----------------------------------------------------------------------------------------------------
 constexpr size_t kPieceBest = size_t(256) << 20;   // bytes of dz of a piece with which more would gain nothing
-constexpr size_t kKeepMost = size_t(64) << 20;     // bytes of logits that are kept (half of L2)
+// Logits are kept where there are few (half of L2), and, up to 2 GB, where hidden rows are so long that a logit's second product
+// takes longer than its way to memory and back (measured above: the two meet a little above H = 1024).
+constexpr size_t kKeepFew = size_t(64) << 20, kKeepMost = size_t(2) << 30;
+constexpr int kKeepFrom = 1280;
 
 constexpr int kByRow = 1 << 21;                    // words up to which every CTA of a row joins its tiles (V^2 / 2^18 pairs are read)
 constexpr int kFewest = 32768;                     // rows up to which a CTA per row (and block) will do
@@ -449,21 +466,23 @@ HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
   }
   s.tiles = (V + s.width - 1) / s.width;
   s.part = take((size_t)s.tiles * 2 * s.pitch * sizeof(float2));
-  s.by_row = (size_t)N * words * 4 <= kKeepMost && words <= kByRow && N <= kFewest;
+  s.by_row = (size_t)N * words * 4 <= kKeepFew && words <= kByRow && N <= kFewest;
   s.blocks = 1;
   s.piece = (int)words;
   s.bytes = at;
   if (!grad) return s;
   const size_t fixed = at, column = (size_t)N * 2;
   // words of a piece: all of them, or as many as the space allows, in pieces of equal length
-  s.keep = s.by_row && space != 1;
   int64_t piece = (int64_t)(kPieceBest / column / 256 * 256);
   if (piece < 256 || space == 1) piece = 256;
-  for (bool lean = space == 1;; lean = true) {
-    // (lean: no logits kept, no shares; then as many words as are left room for)
+  const size_t kept = (size_t)N * words * 4;
+  const bool worth = s.by_row || (H >= kKeepFrom && kept <= kKeepMost);
+  for (int level = space == 1 ? 2 : worth ? 0 : 1;; ++level) {
+    // (0: the logits are kept; 1: they are not; 2: nor shares of dh, and as many words as are left room for)
+    const bool lean = level == 2;
     at = fixed;
+    s.keep = level == 0;
     if (lean) {
-      s.keep = false;
       const size_t rest = up256((size_t)N * H * 4);
       piece = space > fixed + rest ? (int64_t)((space - fixed - rest) / column / 256 * 256) : 256;
       if (piece < 256) piece = 256;
@@ -491,9 +510,8 @@ HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
       }
     }
     s.piece = (int)piece;
-    if (s.keep && pieces > 1) s.keep = false;
     s.ld_logits = words;
-    if (s.keep) s.logits = take((size_t)N * words * 4);
+    if (s.keep) s.logits = take(kept);
     if (s.blocks > 1) s.share = take((size_t)s.blocks * N * H * 4);
     else if (pieces > 1 || lean) s.dh_acc = take((size_t)N * H * 4);
     s.dz = take(column * piece);
@@ -599,7 +617,10 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   for (int64_t v0 = 0; v0 < a.V; v0 += s.piece) {
     const int len = (int)(a.V - v0 < s.piece ? a.V - v0 : s.piece);
     const bool first = v0 == 0, last = v0 + len == a.V;
-    if (!s.keep) {
+    if (s.keep && !s.by_row) {
+      if (!launched(dx_launch_pdl(pdl, dx_head_dz_kernel, dim3(a.N, (len + 2047) / 2048), dim3(256), 0, st, 1, logits, s.ld_logits,
+                                  (int)v0, len, live, n_live + 1, a.targets, a.row_weight, lse, row_loss, dz, a.N))) return e;
+    } else if (!s.keep) {
       MmParams q = p;
       q.columns = len;
       q.column0 = (int)v0;

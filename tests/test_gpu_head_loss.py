@@ -276,3 +276,28 @@ def test_rows_listed_by_their_own_blocks_or_by_one(dx, N):
     h, W, t, w = problem(N, N, 1200, 72)
     h[(t < 0) | (w == 0)] = NAN
     check(h, W, t, w, binding.spec_head_loss(ctx, h, W, t, row_weight=w, grad_weight=True))
+
+
+@pytest.mark.parametrize("N,V", [(400, 50003), (2800, 50003)])
+def test_kept_and_recomputed_logits_give_the_same_bits(dx, N, V):
+    """Long hidden rows and enough workspace: the logits are kept, in one piece of dz or several; without their bytes the products
+    are computed twice."""
+    binding, ctx = dx
+    H = 1288
+    h, W, t, w = problem(N, N, V, H)
+    h[(t < 0) | (w == 0)] = NAN
+    kept = binding.spec_head_loss(ctx, h, W, t, row_weight=w, grad_weight=True)
+    check(h, W, t, w, kept)
+    _, best = binding.spec_head_loss_workspace(ctx, N, V, H)
+    less = torch.full((best - N * 50176 * 4,), 0xFF, dtype=torch.uint8, device="cuda")
+    twice = binding.spec_head_loss(ctx, h, W, t, row_weight=w, grad_weight=True, workspace=less)
+    assert all(torch.equal(kept[key], twice[key]) for key in kept)
+    check(h, W, t, w, binding.spec_head_loss(ctx, h, W, t, row_weight=w, grad_weight=True, workspace=less[:-4096]))
+
+
+@pytest.mark.parametrize("N,V,H", [(70, 40009, 1032), (64, 9001, 2048), (600, 12007, 2048)])
+def test_larger_heads(dx, N, V, H):
+    binding, ctx = dx
+    h, W, t, w = problem(N, N, V, H)
+    h[(t < 0) | (w == 0)] = NAN
+    check(h, W, t, w, binding.spec_head_loss(ctx, h, W, t, row_weight=w, grad_weight=True))
