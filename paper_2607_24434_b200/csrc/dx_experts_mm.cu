@@ -482,8 +482,8 @@ __global__ void __launch_bounds__(256) dx_pair_weight_grad_kernel(const float* p
   const int q = index ? __ldg(index + r) : r;
   if (q < 0 || q >= n_pairs) return;
   float sum = 0.0f;
-#pragma unroll 8
-  for (int i = 0; i < parts; ++i) sum += __ldg(partial + (int64_t)i * n_rows + r);
+#pragma unroll 16
+  for (int i = 0; i < parts; ++i) sum += __ldg(partial + (int64_t)i * n_rows + r);      // (16 on their way at a time)
   d_pair_w[q] = sum;
 }
 
@@ -564,13 +564,15 @@ bool dx_matrix_map(CUtensorMap* out, const void* base, int64_t rows, int64_t col
 namespace {
 
 // Few rows per group: the weights' bytes are the time, so tiles are small (128 lanes: twice as many CTAs have one, and eight
-// stages of 24 KB keep 128 KB of weights in flight per SM).  Some rows, and matrices whose rows are the contraction: 128 lanes
-// with 128 columns (64 groups of 64 rows x 2048 x 1408: 67.5 us, in pairs 73.7; its SwiGLU gradient 92, in pairs 98; of 128 rows 88
-// and 135, in pairs 80 and 119.  The other forms lose with it at 40 rows already: SwiGLU 137 us, in pairs 133).  Otherwise pairs
-// of CTAs with 256 lanes x 256 columns.
+// stages of 24 KB keep 128 KB of weights in flight per SM).  That pays up to 32 rows where the matrices' rows are the contraction
+// (64 groups of 24 rows x 2048 x 1408: 66.3 us, in pairs 71.8; its SwiGLU gradient 76.9, in pairs 85.0), otherwise for a handful
+// (one row: SwiGLU 84 us, in pairs 86; 24 rows 133, in pairs 130).  Some rows, and matrices whose rows are the contraction: 128
+// lanes with 128 columns (64 rows 67.5 us, in pairs 73.7; SwiGLU gradient 92, in pairs 98; 128 rows 88 and 135, in pairs 80 and
+// 119.  The other forms lose with it at 40 rows already: SwiGLU 137 us, in pairs 133).  Otherwise pairs of CTAs with 256 lanes x
+// 256 columns.
 template <int FORM, bool GATHER, class Epilogue>
 cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cudaStream_t st) {
-  const bool few = p.n_rows <= kFewRows * (int64_t)p.n_groups;
+  const bool few = p.n_rows <= (FORM == kRowsT ? kFewRows : kFewestRows) * (int64_t)p.n_groups;
   const bool some = FORM == kRowsT && !few && p.n_rows <= kSomeRows * (int64_t)p.n_groups;
   const long long lanes = few || some ? 128 : 256, bn = few ? 64 : some ? 128 : 256;
   // (every group may end in a tile that is not full)

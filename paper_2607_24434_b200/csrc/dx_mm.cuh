@@ -37,7 +37,8 @@ constexpr int kMmA = 128 * kMmK * 2;        // bytes of a CTA's 128 rows of A in
 constexpr int kMmMaxStages = 8;
 constexpr uint32_t kDrainPolls = 1u << 16;  // of a barrier that may never complete, after something gave up
 constexpr int kDealt = 4;                   // (a panel's)
-constexpr int kFewRows = 32, kSomeRows = 96;   // per group, up to which tiles are of 64 and (products with transposed matrices) 128 columns
+// rows per group up to which tiles have 64 columns, and, products with transposed matrices, 64 and 128
+constexpr int kFewestRows = 8, kFewRows = 32, kSomeRows = 96;
 constexpr int kPanel = 256;                 // columns of a panel: a tile's, so that a tile's rows lie close together
 
 // ---- PTX ---------------------------------------------------------------------------------------------------------
