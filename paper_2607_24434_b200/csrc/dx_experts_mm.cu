@@ -5,6 +5,13 @@
 // In all of them the LANES of a tile are the contiguous dimension of the output and its COLUMNS the output's rows: weights
 // are the fixed 128 lanes of a CTA, and the ragged number of an expert's rows is the width of the products, which
 // tcgen05.mma takes in steps of 16 -- a group of 5 rows costs 16 columns, not 128.
+//
+// Bounds and measurements, 64 experts of which a token takes six, H = 2048, I = 1408.  One token: the weights' bytes (34.6 MB; 5.4 us
+// at the copy rate) behind a chain of launch, offsets and first stage: 11.3 us, SwiGLU (69 MB) 15.8.  700 tokens, SwiGLU gradient:
+// 370 MB of weights, 97 us.  16384 tokens: the products (669 us at the burst rate) under the power cap, as a dense product of their
+// size: 914 to 1011 us, SwiGLU that keeps its products 1006 to 1072.  Weight gradients: of many rows the products and 1.5 GB of fp32
+// results through the same path out of the SM (8192 tokens 636 to 678 us, 335 by the products alone), of few the results (64 rows per
+// group 5.0 TB/s in fp32, 5.2 in bf16; a plain fill writes 3.9).
 #include <limits.h>
 
 #include "dx_mm.cuh"
@@ -289,7 +296,8 @@ struct StoreSwiglu : FragmentEpilogue<32> {
 //   d gate = w D up s (1 + gate (1 - s)),  d up = w D gate s,  act_w = w gate s up,  share of d w = sum over lanes of D gate s up.
 // A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come as boxes, a chunk ahead; their place in the
 // staging takes the gradients, which go out as boxes.  (In pieces through registers, every element crossed the load/store path
-// six times, and that path, shared with the gathering warps, was the bound: 430 us, 49152 rows x 2048 x 1408.)
+// six times, and that path, shared with the gathering warps, was the bound: 430 us, 49152 rows x 2048 x 1408, now 347.  What bounds
+// it now is the storing warps' arithmetic, some 40 instructions for 32 elements beside their way in and out.)
 struct StoreSwigluGrad : FragmentEpilogue<16> {
   static constexpr bool kBefore = false;      // (no registers for two chunks: this one is waited for where it is needed)
   // of a column 64 bytes of gate, then 64 of up; behind the sixteen columns act_w; two chunks; the weights of 128 columns
