@@ -144,7 +144,7 @@ struct RowSums {
   int row, target;
   float top, sum;
   static constexpr bool kBefore = false;
-  static constexpr int kStaging = 0, kCols = 32, kRound = 1;
+  static constexpr int kStaging = 0, kCols = 32, kRound = 1, kGathering = 0;
   struct Values {
     float v[32];
   };
@@ -259,7 +259,7 @@ struct StoreDz {
   int row, target;
   float lse, weight, at_target;
   static constexpr bool kBefore = false;
-  static constexpr int kStaging = 0, kCols = 32, kRound = 64;   // (the products of the gradients read whole blocks of 64)
+  static constexpr int kStaging = 0, kCols = 32, kGathering = 0, kRound = 64;   // (the products of the gradients read whole blocks of 64)
   struct Values {
     float v[32];
   };

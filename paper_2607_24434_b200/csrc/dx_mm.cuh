@@ -10,14 +10,14 @@
 // rows of 128 bytes in the 128-byte swizzle that tcgen05.mma reads.  Either operand may be "K-major" (its rows lie along
 // the contraction) or "MN-major" (its rows lie across it: a box holds 64 contraction rows of 64 lanes or columns), so
 // that transposed weights and products over the rows themselves need no transposed copy.  Rows gathered by index come in
-// 16-byte pieces (cp.async) from four warps of their own, which write the same swizzle; an index outside the matrix reads
+// 16-byte pieces (cp.async) from four to six warps of their own, which write the same swizzle; an index outside the matrix reads
 // zeros.  (Tensor-map copies of four gathered rows took 85 to 120 clocks each, whoever issued them: 2.8 to 3.8 ms where rows
 // in place take 1.0 ms, 98304 rows x 2048 x 2816.)
 //
 // Warps: 0-7 take finished tiles out of tensor memory (lanes 32 (w % 4) .. + 31, every other chunk of columns), 8 asks for A and
 // 10 for B (one of them where only one operand comes by tensor map), 9 owns the tensor memory and issues the products (in a pair
-// only the first CTA's), 12-15 gather.  Two accumulators take turns, so a tile
-// is stored while the next one is multiplied.  Every wait is bounded; one that runs out raises the CTA's abort flag,
+// only the first CTA's), those from 12 on gather.  Two accumulators take turns, so a tile is stored while the next one is
+// multiplied.  Every wait is bounded; one that runs out raises the CTA's abort flag,
 // after which nothing more is copied or multiplied, copies and products in flight are waited for (bounded), tensor
 // memory is freed and DX_DEV_WAIT_EXPIRED stands in the status word.
 #pragma once
@@ -31,7 +31,7 @@ namespace {
 
 constexpr int kMmStoring = 8;               // storing warps: two for each quarter of the tile's lanes, which share its columns
 enum { kWarpA = 8, kWarpMma = 9, kWarpB = 10, kWarpGather = 12 };
-__host__ __device__ constexpr int mm_threads(bool gather) { return gather ? 512 : 352; }
+__host__ __device__ constexpr int mm_threads(int gathering) { return gathering ? 32 * (kWarpGather + gathering) : 352; }
 constexpr int kMmK = 64;                    // contraction elements of a stage: 128 bytes of a row
 constexpr int kMmA = 128 * kMmK * 2;        // bytes of a CTA's 128 rows of A in a stage
 constexpr int kMmMaxStages = 8;
@@ -523,7 +523,7 @@ __device__ __forceinline__ int mm_row(int q, MmDiv div, int n_rows, int32_t* dev
 }
 
 template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
-__global__ void __launch_bounds__(mm_threads(GATHER), 1)
+__global__ void __launch_bounds__(mm_threads(GATHER ? Epilogue::kGathering : 0), 1)
 dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmParams p) {
   constexpr int kHalf = BN / CG;                       // columns whose rows a CTA fetches
   constexpr int kB = (kHalf < 32 ? 32 : kHalf) * kMmK * 2;
@@ -689,9 +689,14 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     }
   } else if (GATHER && warp >= kWarpGather) {
     // ----------------------------------------------------------------------------------------------- gathered rows
-    // Each of the four warps does every fourth stage by itself: its fixed costs (waiting for the slot, for the pieces to land,
-    // making them visible to the tensor core) are spread over the time of four stages.  Eight lanes bring 128 bytes of a row,
+    // Each of the four or six warps does every fourth or sixth stage by itself: its fixed costs (waiting for the slot, for the
+    // pieces to land, making them visible to the tensor core) are spread over the time of as many stages.  A stage takes a warp
+    // some 2800 clocks, most of them to issue the copies, and its products 512: with four warps they wait for it.  Eight lanes bring 128 bytes of a row,
     // the warp four rows at a time: row 4 i + lane / 8; lane l looks up rows l, l + 32, ...
+    // (A warp asks for a slot when it has filled the one kGathering stages in front.  That one's own slot was empty then, so no
+    // slot is more than one turn behind what is asked of it: its barrier's phase tells turns apart.)
+    constexpr uint32_t kGathering = Epilogue::kGathering;
+    static_assert(kGathering <= STAGES);
     const int g = warp - kWarpGather, sub = lane >> 3, piece = lane & 7;
     // where row 4 i + sub's piece goes: rows of one i parity share their place in the swizzle
     const uint32_t place[2] = {(uint32_t)(sub * 128 + ((piece ^ sub) << 4)), (uint32_t)(sub * 128 + ((piece ^ (4 + sub)) << 4))};
@@ -749,9 +754,9 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
           next_b[j] = in && p.b_index ? __ldg(p.b_index + tile.row0 + r) : 0;
         }
       };
-      const int first = (int)((uint32_t)(g - (int)base) & 3u);
+      const int first = (int)((uint32_t)g + kGathering - base % kGathering) % (int)kGathering;
       if constexpr (FORM == kOuter) ask(first * kMmK);
-      for (int kb = first; kb < tile.kblocks; kb += 4) {
+      for (int kb = first; kb < tile.kblocks; kb += (int)kGathering) {
         const int k0 = kb * kMmK;
         const uint32_t n = base + (uint32_t)kb, slot = n % STAGES, phase = (n / STAGES) & 1u;
         const bool tail = FORM == kOuter && tile.rows - k0 < kMmK;
@@ -766,7 +771,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
                       ok_a[j]);
               resolve(p.b_index ? next_b[j] : tile.row0 + r, in, p.b_index != nullptr, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
             }
-            ask(k0 + 4 * kMmK);
+            ask(k0 + (int)kGathering * kMmK);
           }
         }
         if (!mm_wait(smem_u32(&s->empty[slot]), phase ^ 1u, abort_flag, p.wait_limit)) { alive = false; break; }
@@ -941,7 +946,7 @@ cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long l
   long long units = ctx->sm_count / CG;
   if (max_tiles < units) units = max_tiles;
   if (units < 1) units = 1;
-  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(GATHER)), smem,
+  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(GATHER ? Epilogue::kGathering : 0)), smem,
                        st, CG, maps, p);
 }
 
