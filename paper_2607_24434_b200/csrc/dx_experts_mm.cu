@@ -9,8 +9,8 @@
 // Bounds and measurements, 64 experts of which a token takes six, H = 2048, I = 1408.  One token: the weights' bytes (34.6 MB; 5.4 us
 // at the copy rate) behind a chain of launch, offsets and first stage: 11.3 us, SwiGLU (69 MB) 15.8.  700 tokens, SwiGLU gradient:
 // 370 MB of weights, 97 us.  16384 tokens: the products (669 us at the burst rate) under the power cap, as a dense product of their
-// size: 914 to 1011 us, SwiGLU that keeps its products 1006 to 1072.  Weight gradients: of many rows the products and 1.5 GB of fp32
-// results through the same path out of the SM (8192 tokens 636 to 678 us, 335 by the products alone), of few the results (64 rows per
+// size: 914 to 1011 us, SwiGLU that keeps its products 1010 to 1083.  Weight gradients: of many rows the products and 1.5 GB of fp32
+// results through the same path out of the SM (8192 tokens 626 to 665 us, 335 by the products alone), of few the results (64 rows per
 // group 5.0 TB/s in fp32, 5.2 in bf16; a plain fill writes 3.9).
 #include <limits.h>
 
