@@ -10,7 +10,7 @@
 // at the copy rate) behind a chain of launch, offsets and first stage: 11.3 us, SwiGLU (69 MB) 15.8.  700 tokens, SwiGLU gradient:
 // 370 MB of weights, 97 us.  16384 tokens: the products (669 us at the burst rate) under the power cap, as a dense product of their
 // size: 914 to 1011 us, SwiGLU that keeps its products 1010 to 1083.  Weight gradients: of many rows the products and 1.5 GB of fp32
-// results through the same path out of the SM (8192 tokens 626 to 665 us, 335 by the products alone), of few the results (64 rows per
+// results through the same path out of the SM (8192 tokens 611 to 665 us, 335 by the products alone), of few the results (64 rows per
 // group 5.0 TB/s in fp32, 5.2 in bf16; a plain fill writes 3.9).
 #include <limits.h>
 
@@ -204,10 +204,10 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
 };
 
 // out of group e: [columns][lanes], element (n, m) = D.  Every chunk is a box: the matrix ends where its columns do.
-template <class T>
+template <class T, int GATHERING>
 struct StoreOuter : FragmentEpilogue<store_cols<T, false>()> {
   using Base = FragmentEpilogue<store_cols<T, false>()>;
-  static constexpr int kStaging = kStoreStaging, kGathering = 6;
+  static constexpr int kStaging = kStoreStaging, kGathering = GATHERING;
   using Base::Base;
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const typename Base::Values& x, Taken) {
@@ -747,7 +747,16 @@ cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t
   const uint64_t strides[2] = {(uint64_t)a.ld_dw, (uint64_t)a.dw_stride};
   const uint32_t box[3] = {32, a.dw_fp32 ? 16u : 32u, 1};
   if (!dx_box_map(&m.out[0], a.dw, a.dw_fp32, 3, dims, strides, box)) return cudaErrorInvalidValue;
+  // Few rows per group, and one, three or five times 128 lanes: pairs would spend a sixth or more of their tiles on lanes that do not
+  // exist, so CTAs work by themselves (130 groups of five rows, 1000 x 520 bf16: 46 us, in pairs 52; 256 of two, 640 x 384 fp32: 57,
+  // in pairs 65.  Where pairs have no such lanes they are faster: 64 of five, 1408 x 2048 bf16 89 us, by themselves 105).
+  const int blocks = (a.k + 127) / 128;
+  if (a.n_rows <= 64 * (int64_t)a.n_groups && blocks % 2 && blocks <= 5) {
+    const long long tiles = (long long)a.n_groups * blocks * ((a.n + 255) / 256);
+    return a.dw_fp32 ? mm_launch<kOuter, true, 1, 256, 4, StoreOuter<float, 4>>(ctx, m, p, tiles, st)
+                     : mm_launch<kOuter, true, 1, 256, 4, StoreOuter<__nv_bfloat16, 4>>(ctx, m, p, tiles, st);
+  }
   const long long tiles = (long long)a.n_groups * ((a.k + 255) / 256) * ((a.n + 255) / 256);
-  return a.dw_fp32 ? mm_launch<kOuter, true, 2, 256, 6, StoreOuter<float>>(ctx, m, p, tiles, st)
-                   : mm_launch<kOuter, true, 2, 256, 6, StoreOuter<__nv_bfloat16>>(ctx, m, p, tiles, st);
+  return a.dw_fp32 ? mm_launch<kOuter, true, 2, 256, 6, StoreOuter<float, 6>>(ctx, m, p, tiles, st)
+                   : mm_launch<kOuter, true, 2, 256, 6, StoreOuter<__nv_bfloat16, 6>>(ctx, m, p, tiles, st);
 }
