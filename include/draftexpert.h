@@ -502,7 +502,8 @@ dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, cons
  *   down matrix, dy the gradient of the tokens' sums; sorted row r is pair q = gather[r] (NULL: r), its dy row q / gather_div, its
  *   weight pair_w[q] (NULL: 1).  With a = W_e^T dy, s = sigmoid(g):  d_gate_up[r] = (w a u s (1 + g (1 - s)), w a g s),
  *   act_w[r] = w silu(g) u -- with moe_grouped_mm_dw the gradient of W_e: sum of dy act_w^T -- and
- *   d_pair_w[q] = <a, silu(g) u> (may be NULL; pairs that no row stands for are not written).  A pair of weight 0 is taken out: all
+ *   d_pair_w[q] = <a, silu(g) u> (may be NULL; pairs that no row stands for are not written, a pair that several rows stand for gets
+ *   what one of them gives: a permutation has neither).  A pair of weight 0 is taken out, its row is not looked at: all
  *   of its gradients are 0.  workspace: moe_grouped_swiglu_backward_workspace bytes (0 without d_pair_w), 16-byte aligned.
  * moe_combine_tokens: y[t] = sum_j w[t, j] z[t k + j], rows fp32 or bf16 (each of z, y), k <= 8, sums in fp32; w NULL: all 1.  A
  *   weight of 0 takes its row out (it is not read).  moe_combine_tokens_backward: dz[t k + j] = w[t, j] dy[t] and

@@ -1000,9 +1000,8 @@ def moe_grouped_swiglu_backward(ctx: Context, dy: torch.Tensor, w_down: torch.Te
         out = {"d_gate_up": torch.empty(rows, 2 * d.k, dtype=bf16, device=device),
                "act_w": torch.empty(rows, d.k, dtype=bf16, device=device)}
         if topk_w is not None:
-            # (a permutation writes every pair; fewer rows than pairs leave some out)
-            make = torch.empty_like if topk_w.numel() == rows else torch.zeros_like
-            out["d_topk_w"] = make(topk_w)
+            # (as many rows as pairs need not be all of them: rows outside every group have none written)
+            out["d_topk_w"] = torch.zeros_like(topk_w)
         ld_d, ld_act = 2 * d.k, d.k
     else:
         ld_d, ld_act = _operand(ctx, out["d_gate_up"], "d_gate_up", 2 * d.k), _operand(ctx, out["act_w"], "act_w", d.k)
