@@ -983,9 +983,9 @@ def moe_grouped_swiglu_backward(ctx: Context, dy: torch.Tensor, w_down: torch.Te
     """Backward through w_down [E, H, I] and the SwiGLU in front of it, from the gradient ``dy`` of the tokens' sums:
     ``d_gate_up`` [rows, 2 I], ``act_w`` [rows, I] (the weighted SwiGLU outputs, the other factor of w_down's gradient) and, with
     ``topk_w`` (any shape, indexed by pair = gather[r]), ``d_topk_w`` in its shape (pairs without a row keep what ``out`` held, or
-    0)."""
+    0).  Sorted row r takes row pair // gather_div of ``dy``; without ``gather`` it is pair r."""
     _index(ctx, gather, "gather")
-    rows = dy.shape[0] if gather is None else gather.shape[0]
+    rows = dy.shape[0] * gather_div if gather is None else gather.shape[0]
     d = _groups(ctx, w_down, "w_down", rows)
     if w_down.dtype is not torch.bfloat16:
         raise ValueError(f"w_down: bfloat16 is expected, not {w_down.dtype}")
@@ -1021,7 +1021,6 @@ def moe_grouped_swiglu_backward(ctx: Context, dy: torch.Tensor, w_down: torch.Te
         space = torch.empty(n_space, dtype=torch.uint8, device=dy.device)
     _check(ctx.lib.moe_grouped_swiglu_backward(ctx.handle, C.byref(d), _ptr(dy), dy.shape[0], ld_dy, _ptr(w_down),
                                                _ptr(gate_up), ld_gu, _ptr(topk_w),
-                                               rows if topk_w is None and gather is None else
                                                dy.shape[0] * gather_div if topk_w is None else topk_w.numel(),
                                                _ptr(offsets), _ptr(gather), gather_div, _ptr(out["d_gate_up"]), ld_d,
                                                _ptr(out["act_w"]), ld_act, _ptr(d_w), _ptr(space), n_space,

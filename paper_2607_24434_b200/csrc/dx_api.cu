@@ -1018,7 +1018,7 @@ extern "C" dx_status moe_grouped_mm(dx_ctx* ctx, const dx_grouped_desc* desc, co
   a.x = x; a.x_rows = x_rows; a.ldx = ldx;
   a.w = w; a.n_groups = desc->n_groups; a.n = desc->n; a.k = desc->k; a.ldw = desc->ld_w; a.w_stride = desc->stride_w;
   a.transposed = transposed;
-  a.offsets = offsets; a.n_rows = desc->n_rows; a.gather = gather; a.gather_div = gather_div; a.scatter = scatter;
+  a.offsets = offsets; a.n_rows = desc->n_rows; a.gather = gather; a.gather_div = gather ? gather_div : 1; a.scatter = scatter;
   a.y = y; a.y_fp32 = y_dtype == DX_DTYPE_FP32; a.y_rows = y_rows; a.ldy = ldy;
   DX_CUDA(ctx, dx_launch_grouped_mm(ctx, a, (cudaStream_t)stream));
   ctx->launches++;
@@ -1088,7 +1088,7 @@ extern "C" dx_status moe_grouped_swiglu(dx_ctx* ctx, const dx_grouped_desc* desc
   DxGroupedMm a = {};
   a.x = x; a.x_rows = x_rows; a.ldx = ldx;
   a.w = w_gate_up; a.n_groups = desc->n_groups; a.n = desc->n; a.k = desc->k; a.ldw = desc->ld_w; a.w_stride = desc->stride_w;
-  a.offsets = offsets; a.n_rows = P; a.gather = gather; a.gather_div = gather_div;
+  a.offsets = offsets; a.n_rows = P; a.gather = gather; a.gather_div = gather ? gather_div : 1;
   a.y = act; a.y_rows = P; a.ldy = ld_act;
   DX_CUDA(ctx, dx_launch_grouped_swiglu(ctx, a, gate_up, ld_gate_up, (cudaStream_t)stream));
   ctx->launches++;
@@ -1120,7 +1120,7 @@ extern "C" dx_status moe_grouped_swiglu_backward(dx_ctx* ctx, const dx_grouped_d
   if (s != DX_OK) return s;
   if (P == 0) return DX_OK;
   if (!offsets) return DX_ERR_INVALID_ARG;
-  if (dy_rows < (gather ? 1 : P) || n_pairs < (gather ? 1 : P)) return DX_ERR_SHAPE;
+  if (dy_rows < (gather ? 1 : (P - 1) / gather_div + 1) || n_pairs < (gather ? 1 : P)) return DX_ERR_SHAPE;
   if (d_pair_w) {
     size_t need = 0;
     moe_grouped_swiglu_backward_workspace(desc, &need);

@@ -597,7 +597,8 @@ cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cuda
 }
 template <int FORM, class Epilogue>
 cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cudaStream_t st) {
-  return p.b_index ? launch_rows<FORM, true, Epilogue>(ctx, maps, p, st) : launch_rows<FORM, false, Epilogue>(ctx, maps, p, st);
+  return p.b_index || p.b_div.factor != 0u ? launch_rows<FORM, true, Epilogue>(ctx, maps, p, st)
+                                           : launch_rows<FORM, false, Epilogue>(ctx, maps, p, st);
 }
 
 // the rows (columns of D): a tensor map, or the matrix they are gathered from
@@ -612,7 +613,7 @@ bool rows_source(MmMaps* m, MmParams* p, const DxGroupedMm& a, int cols) {
     rows = (int64_t)((a.w_rows + kPanel - 1) / kPanel) * a.group_rows;
     cols = kPanel;
   }
-  return a.gather || (dx_matrix_map(&m->b, a.x, rows, cols, a.ldx, 128) && dx_matrix_map(&m->b_few, a.x, rows, cols, a.ldx, 32));
+  return a.gather || a.gather_div > 1 || (dx_matrix_map(&m->b, a.x, rows, cols, a.ldx, 128) && dx_matrix_map(&m->b_few, a.x, rows, cols, a.ldx, 32));
 }
 
 MmParams base_params(const dx_ctx* ctx, const int32_t* offsets, int groups, int rows) {

@@ -288,7 +288,7 @@ struct DxGroupedMm {
   int64_t ldw, w_stride;
   const int32_t* offsets;    // [n_groups + 1]
   int n_rows;                // of the sorted order
-  const int32_t* gather;     // sorted row -> gather / gather_div = row of x (null: itself)
+  const int32_t* gather;     // sorted row r -> gather[r] / gather_div = row of x (null: r / gather_div)
   int gather_div;
   const int32_t* scatter;    // sorted row -> row of y (null: itself)
   void* y;

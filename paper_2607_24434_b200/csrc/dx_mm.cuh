@@ -359,7 +359,7 @@ struct MmParams {
   int a_rows, b_rows;            // reads zeros
   int64_t a_ld, b_ld;
   const int32_t* offsets;        // [n_groups + 1]
-  const int32_t* a_index;        // sorted row -> index / a_div = row of A's matrix (null: the row itself)
+  const int32_t* a_index;        // sorted row -> index / a_div = row of A's matrix (null: the row itself; rows as columns: row / b_div)
   const int32_t* b_index;
   MmDiv a_div, b_div;
   // output: element (row of column n, lane m) at out + row * ld + m
@@ -735,10 +735,10 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         }
       };
       if constexpr (FORM != kOuter) {
-        const int32_t* index = p.b_index + n0;
         int q[kRegs];
 #pragma unroll
-        for (int j = 0; j < kRegs; ++j) q[j] = 32 * j + lane < here ? __ldg(index + 32 * j + lane) : 0;
+        for (int j = 0; j < kRegs; ++j)
+          q[j] = 32 * j + lane >= here ? 0 : p.b_index ? __ldg(p.b_index + n0 + 32 * j + lane) : n0 + 32 * j + lane;
 #pragma unroll
         for (int j = 0; j < kRegs; ++j)
           resolve(q[j], 32 * j + lane < here, true, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);

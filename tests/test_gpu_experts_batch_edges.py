@@ -1,5 +1,5 @@
 """Calls of the batch experts' operators that their own tests leave out: rows outside every group, rows that name a pair twice or
-none at all."""
+none at all, indexes that are not given."""
 import pytest
 import torch
 
@@ -87,3 +87,33 @@ def test_gates_without_a_row_have_gradient_zero(dx, first, each, index):
     assert ctx.device_status() == (BAD_ROW if index == "bad" else 0)
     kept = kept.reshape(-1)
     assert bool((kept[~has_row] == 7.0).all()) and torch.equal(kept[alone], got[alone])
+
+
+@pytest.mark.parametrize("counts", [[1, 0, 3], [17, 40, 0, 83], [300, 0, 500]])
+@pytest.mark.parametrize("k", [1, 2, 6])
+def test_pairs_in_order_take_their_tokens_gradient(dx, counts, k):
+    """Without ``gather`` sorted row r is pair r and takes row r // gather_div of dy: what the indexes 0, 1, 2, ... give."""
+    binding, ctx = dx
+    g = rng(k)
+    P = (sum(counts) + k - 1) // k * k
+    N, E, H, I = P // k, len(counts), 264, 136
+    off = [0]
+    for c in counts:
+        off.append(off[-1] + c)
+    off = ints(*off)
+    dy, wd, gate_up = draw(g, N, H), draw(g, E, H, I, scale=0.1), draw(g, P, 2 * I)
+    topk_w = torch.rand((N, k), generator=g, device="cuda") + 0.1
+    order = torch.arange(P, dtype=torch.int32, device="cuda")
+    rows = slice(0, sum(counts))
+    for w in (topk_w, None):
+        plain = binding.moe_grouped_swiglu_backward(ctx, dy, wd, gate_up, w, off, gather_div=k)
+        named = binding.moe_grouped_swiglu_backward(ctx, dy, wd, gate_up, w, off, gather=order, gather_div=k)
+        assert plain.keys() == named.keys() and all(torch.equal(plain[n][rows], named[n][rows]) for n in ("d_gate_up", "act_w"))
+        assert w is None or torch.equal(plain["d_topk_w"], named["d_topk_w"])
+    with pytest.raises(ValueError):
+        binding.moe_grouped_swiglu_backward(ctx, dy, wd, gate_up[:-1], topk_w, off, gather_div=k)
+    # the forward products' rows are their own: gather_div belongs to gather there
+    x, w = draw(g, P, H), draw(g, E, 2 * I, H, scale=0.1)
+    assert torch.equal(binding.moe_grouped_mm(ctx, x, w, off, gather_div=k)[rows], binding.moe_grouped_mm(ctx, x, w, off)[rows])
+    assert torch.equal(binding.moe_grouped_swiglu(ctx, x, w, off, gather_div=k)["act"][rows],
+                       binding.moe_grouped_swiglu(ctx, x, w, off)["act"][rows])
