@@ -511,8 +511,9 @@ dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, cons
  *
  * spec_head_loss: for rows h [N, H] bf16 and a head W [V, H] bf16, with z = W h[t]:  loss[t] = log sum_v exp(z_v) - z_target,
  *   dh [N, H] = row_weight[t] * dloss/dh and dW [V, H] = sum_t row_weight[t] * dloss/dW, bf16 (each may be NULL, not all three).
- *   targets [N]: -1 (no token) and rows of weight 0 have loss 0 and no part in the gradients, whatever h holds (they are left
- *   out: a padded batch costs its real rows); another id outside [0, V) gives loss NaN, no gradient, DX_DEV_BAD_TOKEN.  The
+ *   targets [N]: -1 (no token) and rows of weight 0 (whatever their target) have loss 0 and no part in the gradients, whatever h
+ *   holds (they are left out: a padded batch costs its real rows); another id outside [0, V) gives loss NaN, no gradient,
+ *   DX_DEV_BAD_TOKEN.  The
  *   gradients work through the vocabulary piece by piece, a piece's dz in bf16 (each element rounded once), from logits kept in
  *   fp32 (N V of them, where that pays and the workspace has room) or computed a second time; dz is the same either way.  Any V.
  *   workspace (256-byte aligned): spec_head_loss_workspace says how many bytes are needed at least, and how many are of use;

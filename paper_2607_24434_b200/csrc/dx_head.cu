@@ -24,13 +24,13 @@ namespace {
 
 // ---- 1: which rows count -------------------------------------------------------------------------------------------
 // One CTA, a thread for every 1/1024 of the rows: counted, summed over the CTA, listed.  live[i]: the i-th row that counts; rows
-// that do not have loss 0 (a target outside the vocabulary: NaN).
+// that do not have loss 0 (a target outside the vocabulary, and a weight other than 0: NaN).
 constexpr int kListed = 256;      // rows up to which every row's CTA counts those in front of it
 __device__ __forceinline__ bool row_counts(const int32_t* targets, const float* row_weight, int r, int V, bool& bad) {
   const int t = __ldg(targets + r);
   const float w = row_weight ? __ldg(row_weight + r) : 1.0f;
-  bad = t < -1 || t >= V;
-  return t >= 0 && !bad && w != 0.0f;
+  bad = (t < -1 || t >= V) && w != 0.0f;      // (what a row of weight 0 has for a target does not matter)
+  return t >= 0 && t < V && w != 0.0f;
 }
 __global__ void __launch_bounds__(1024) dx_head_rows_kernel(const int32_t* targets, const float* row_weight, int N, int V,
                                                             int32_t* live, int32_t* n_live, float* loss,
