@@ -311,6 +311,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
   const MmFetch own;
   uint32_t turn = 0;         // chunks so far
   bool asked = false;        // the next chunk's gate and up are on their way
+  bool gone = false;         // a chunk's did not come in time: nothing more is asked for
   MmTile next;
   bool more = false, first = true;
   int q[4];
@@ -360,9 +361,11 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
     if (!chunks(t, lane0, c0) && more) ask_weights();        // (the last chunk does it otherwise)
   }
   __device__ __forceinline__ void finish() {
-    if (asked && lane == 0) {      // (the loop over the tiles ended early: no box may still be landing)
-      for (uint32_t spin = 0; spin < kDrainPolls; ++spin)
-        if (mbar_try_wait(own.bar + (turn & 1u) * 8u, (turn >> 1) & 1u)) break;
+    if (lane == 0) {               // (the loop over the tiles ended early: no box may still be landing)
+      const uint32_t end = turn + (gone ? 1u : 0u) + (asked ? 1u : 0u);
+      for (uint32_t n = turn; n < end; ++n)
+        for (uint32_t spin = 0; spin < kDrainPolls; ++spin)
+          if (mbar_try_wait(own.bar + (n & 1u) * 8u, (n >> 1) & 1u)) break;
     }
     FragmentEpilogue<16>::finish();
   }
@@ -379,14 +382,25 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
   }
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, Values& x, Taken taken) {
+    if (gone) {
+      arrived(x);
+      taken();
+      return;
+    }
     const uint32_t buf = at + (turn & 1u) * kBuffer;
     if (!asked) {
       if (lane == 0) tma_store_read();
       fetch(turn, t, lane0, c0);
     }
     ask_next(t, lane0, c0);
-    // (a wait that runs out raises the abort flag, which ends the loop over the tiles; what this chunk holds is undefined then)
-    mm_store_wait(own.bar + (turn & 1u) * 8u, (turn >> 1) & 1u, own.abort_flag, own.limit, lane);
+    // (a wait that runs out raises the abort flag, which ends the loop over the tiles.  No barrier is armed again while its box may
+    // still be landing, so this warp asks for none from here on.)
+    if (!mm_store_wait(own.bar + (turn & 1u) * 8u, (turn >> 1) & 1u, own.abort_flag, own.limit, lane)) {
+      gone = true;
+      arrived(x);
+      taken();
+      return;
+    }
     uint32_t g4[2][4], u4[2][4], a4[2][4], mask[2];
     F2 w[2], dw2[2];
 #pragma unroll

@@ -18,7 +18,8 @@
 // 10 for B (one of them where only one operand comes by tensor map), 9 owns the tensor memory and issues the products (in a pair
 // only the first CTA's), those from 12 on gather.  Two accumulators take turns, so a tile is stored while the next one is
 // multiplied.  Every wait is bounded; one that runs out raises the CTA's abort flag,
-// after which nothing more is copied or multiplied, copies and products in flight are waited for (bounded), tensor
+// after which nothing more is copied or multiplied.  When all warps of the CTA have come to their ends, copies and products in
+// flight are waited for (bounded; a warp that issued its last ones may have been done long before another one gave up), tensor
 // memory is freed and DX_DEV_WAIT_EXPIRED stands in the status word.
 #pragma once
 
@@ -603,12 +604,13 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   const int total = FORM == kOuter ? p.n_groups * schedule.m_tiles * schedule.n_tiles
                     : FORM == kHead ? schedule.m_tiles * schedule.n_tiles
                                     : s->before[p.n_groups] * schedule.m_tiles;
+  uint32_t issued = 0;      // (copying warps) stages asked for
 
   if (warp == kWarpA || (kTwo && warp == kWarpB)) {
     // ------------------------------------------------------------------------------------------------------ copies
     // (the one of them where only one operand comes by tensor map)
     const bool for_a = warp == kWarpA, for_b = warp == kWarpB;
-    uint32_t slot = 0, phase = 0, issued = 0;
+    uint32_t slot = 0, phase = 0;
     bool alive = true;
     auto shared_row = [&](int e, int kb) { return (p.shared_out - 1 - (kb / kDealt * p.n_groups + e) * kDealt - kb % kDealt) * kMmK; };
     for (int t = unit; t < total && alive; t += n_units) {
@@ -672,20 +674,6 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         ++issued;
         if (++slot == STAGES) { slot = 0; phase ^= 1u; }
       }
-    }
-    if (*abort_flag) {
-      // Something gave up: no copy may still be landing when the shared memory (and in a pair the first CTA's barriers) is
-      // released.  Stages that both operands were asked for complete on their barriers; for one that only one operand was asked
-      // for there is nothing to wait on, so the rest is time, a thousand times what a copy takes.
-      if (rank == 0 && warp == kWarpA) {
-        const uint32_t back = issued < STAGES ? issued : STAGES;
-        for (uint32_t k = 1; k <= back; ++k) {
-          const uint32_t j = issued - k;
-          for (uint32_t spin = 0; spin < kDrainPolls; ++spin)
-            if (mbar_try_wait(smem_u32(&s->full[j % STAGES]), (j / STAGES) & 1u)) break;
-        }
-      }
-      for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     }
   } else if (GATHER && warp >= kWarpGather) {
     // ----------------------------------------------------------------------------------------------- gathered rows
@@ -850,11 +838,6 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         if (!alive) break;
         ++turn;
       }
-      if (*abort_flag && lane == 0) {
-        mm_commit<CG>(smem_u32(&s->drained));
-        for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
-          if (mbar_try_wait(smem_u32(&s->drained), 0)) break;
-      }
     }
   } else if (warp < kMmStoring) {
     // ---------------------------------------------------------------------------------------------- finished tiles
@@ -921,8 +904,32 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   }
   __syncwarp();
   tc_fence_before();
+  __syncthreads();          // (nobody of this CTA issues anything more, or gives up)
+  if (*abort_flag) {
+    // Neither a copy nor a product may be on its way when the shared memory, the tensor memory and in a pair the first CTA's
+    // barriers are released.  (The other CTA of a pair waits at pair_sync.  If only that one gave up, all products of this one are
+    // done: each of its tiles was stored.)
+    if (warp == kWarpMma && rank == 0) {
+      if (elect_one()) mm_commit<CG>(smem_u32(&s->drained));      // (by the lane that issued the products)
+      __syncwarp();
+      for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
+        if (mbar_try_wait(smem_u32(&s->drained), 0)) break;
+    } else if (warp == kWarpA || (kTwo && warp == kWarpB)) {
+      // Stages that both operands were asked for complete on their barriers; for one that only one operand was asked for, or a box
+      // of a storing warp, there is nothing to wait on, so the rest is time, a thousand times what a copy takes.
+      if (rank == 0 && warp == kWarpA) {
+        const uint32_t back = issued < STAGES ? issued : STAGES;
+        for (uint32_t k = 1; k <= back; ++k) {
+          const uint32_t j = issued - k;
+          for (uint32_t spin = 0; spin < kDrainPolls; ++spin)
+            if (mbar_try_wait(smem_u32(&s->full[j % STAGES]), (j / STAGES) & 1u)) break;
+        }
+      }
+      for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    }
+    __syncwarp();
+  }
   if constexpr (CG == 2) pair_sync();
-  else __syncthreads();
   tc_fence_after();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.dev_status, (int32_t)DX_DEV_WAIT_EXPIRED);
   if (warp == kWarpMma) mm_tmem_free<CG>(tmem, kTmemCols);
