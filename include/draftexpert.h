@@ -479,9 +479,11 @@ dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, cons
  * the vocabulary, and the gradients of all of them -- from a loss back to the d_topk_w that moe_route_tokens_backward takes.
  * Conventions of the section above hold (any number of rows, same results on every run, no device memory but the caller's,
  * capturable, the context's GPU need not be current); calls use no scratch of the context, so graphs of one context may
- * overlap.  The products run on the 5th-generation tensor cores: operands bf16, accumulators fp32 (whose additions truncate:
- * n terms of one sign may come out n 2^-26 of their sum short), every output rounded once (fp32: not at all).  Every matrix has a 16-byte aligned address, a row pitch (in elements) and sizes that are multiples
- * of 8; n_groups <= 256, otherwise any size up to 2^35 elements from a matrix's first row to its last.  (DX_ERR_UNSUPPORTED
+ * overlap.  The products run on the 5th-generation tensor cores: operands bf16, accumulators fp32, every output rounded once
+ * (fp32: not at all).  The tensor cores' additions truncate: up to 4096 terms of one sign may come out 1e-5 of their sum short
+ * (random signs: 4e-6 of the root mean square).  Longer contractions are summed in sections of 4096 terms -- where the result is
+ * rounded to bf16, of 32768, 2e-4 short -- which are added up rounded to nearest, so that no more is lost however long they are.
+ * Every matrix has a 16-byte aligned address, a row pitch (in elements) and sizes that are multiples of 8; n_groups <= 256, otherwise any size up to 2^35 elements from a matrix's first row to its last.  (DX_ERR_UNSUPPORTED
  * beyond.)  Outputs must not overlap inputs or one another; of a matrix counts everything between its first and its last element,
  * what lies between its rows too (DX_ERR_INVALID_ARG).
  *

@@ -637,6 +637,7 @@ MmParams base_params(const dx_ctx* ctx, const int32_t* offsets, int groups, int 
   p.n_rows = rows;
   p.dev_status = ctx->dev_status;
   p.wait_limit = ctx->wait_limit;
+  p.section = kSectionBf16;
   return p;
 }
 
@@ -653,6 +654,7 @@ cudaError_t dx_launch_grouped_mm(dx_ctx* ctx, const DxGroupedMm& a, cudaStream_t
   p.scatter = a.scatter;
   p.out_rows = a.y_rows;
   p.addend = a.addend;
+  if (a.y_fp32 && !a.w_rows) p.section = kSectionFp32;      // (shares of the loss's gradient end in bf16)
   if (a.w_rows) {
     p.n_live = a.n_live;
     p.group_rows = a.group_rows;
@@ -718,6 +720,7 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   p.act_w = act_w;
   p.ld_act = ld_act;
   p.partial = d_pair_w ? partial : nullptr;
+  if (d_pair_w) p.section = kSectionFp32;
   const uint64_t dims[3] = {(uint64_t)a.k, (uint64_t)a.n, (uint64_t)a.n_groups};
   const uint64_t strides[2] = {(uint64_t)a.ldw, (uint64_t)a.w_stride};
   const uint32_t box[3] = {64, 64, 1};
@@ -753,6 +756,7 @@ cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t
   p.out = a.dw;
   p.ld = a.ld_dw;
   p.group_stride = a.dw_stride;
+  if (a.dw_fp32) p.section = kSectionFp32;
   if (a.dy_panels) p.b_panel = a.dy_rows;
   if (!dx_matrix_map(&m.a, a.x, a.x_rows, a.k, a.ldx, 64) ||
       !dx_matrix_map(&m.b, a.dy, (int64_t)(a.dy_panels ? (a.n + kPanel - 1) / kPanel : 1) * a.dy_rows,

@@ -592,6 +592,7 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
   p.ld_logits = s.ld_logits;
   p.dev_status = ctx->dev_status;
   p.wait_limit = ctx->wait_limit;
+  p.section = kSectionFp32;
 
   const bool pdl = (ctx->pdl_mask & DX_PDL_EXPERTS) != 0;
   if (a.N <= kListed) {

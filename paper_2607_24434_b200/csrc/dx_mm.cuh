@@ -41,6 +41,14 @@ constexpr int kDealt = 4;                   // (a panel's)
 // rows per group up to which tiles have 64 columns, and, products with transposed matrices, 64 and 128
 constexpr int kFewestRows = 8, kFewRows = 32, kSomeRows = 96;
 constexpr int kPanel = 256;                 // columns of a panel: a tile's, so that a tile's rows lie close together
+// The tensor cores' additions to an accumulator truncate, so what is lost grows with their number: of one group's fp32 weight
+// gradient 7e-7 of its rms after 768 rows, 4e-6 after 4096, 1e-4 after 98304, 1.2e-3 after 2^20 (operands of one sign: 5e-7,
+// 7e-6, 6e-4, 7e-3).  So a long contraction goes in sections, each from zero, which the storing warps add up in fp32, rounded to
+// nearest: 4e-6 (7e-6) from 4096 rows on.  Blocks of kMmK of a section: 4096 terms where the result leaves in fp32; where it is
+// rounded to bf16, 32768, which lose a tenth of that rounding's half step.  A section's end costs the tensor core the time of the
+// addition, some 1700 clocks beside the 33000 that 64 blocks of a pair take: fp32 gradient of 2816 x 2048 over 98304 rows in one
+// group 1025 -> 1070 us, in eight 805 -> 808; products of 4096 x 4096 x 16384 396 -> 419 us.
+constexpr int kSectionFp32 = 64, kSectionBf16 = 512;
 
 // ---- PTX ---------------------------------------------------------------------------------------------------------
 // In a pair, every copy reports to the FIRST CTA's barrier: its address is the local one with the CTA bit cleared.
@@ -147,6 +155,22 @@ __device__ __forceinline__ void mm_tmem_free(uint32_t base, uint32_t columns) {
   else
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
 }
+// 32 lanes x 16 columns, a lane per thread
+__device__ __forceinline__ void mm_ld16(uint32_t taddr, float (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+        "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void mm_st16(uint32_t taddr, const float (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"f"(r[0]), "f"(r[1]),
+      "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]),
+      "f"(r[13]), "f"(r[14]), "f"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void mm_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void mm_ld32(uint32_t taddr, float (&v)[32]) {
   uint32_t r[32];
   asm volatile(
@@ -206,6 +230,13 @@ __device__ __forceinline__ void mm_ld_wait(float (&a)[N], float (&b)[N]) {
                  : "memory");
   // (an asm statement takes thirty operands: the last two of 32 follow the others through one more)
   if constexpr (N == 16) asm volatile("" : "+f"(b[14]), "+f"(b[15]), "+f"(a[0]) : : "memory");
+}
+__device__ __forceinline__ void mm_ld_wait(float (&a)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]), "+f"(a[6]), "+f"(a[7]), "+f"(a[8]),
+                 "+f"(a[9]), "+f"(a[10]), "+f"(a[11]), "+f"(a[12]), "+f"(a[13]), "+f"(a[14]), "+f"(a[15])
+               :
+               : "memory");
 }
 // four 8 x 8 matrices of 16-bit elements, transposed: lanes 8 j .. 8 j + 7 name the rows of matrix j
 __device__ __forceinline__ void stmatrix_t(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -402,6 +433,7 @@ struct MmParams {
   int column0;                   // first column's word
   int tile_width;                // columns of a tile (0: BN)
   uint32_t a_box;                // rows of a copy of A
+  int section;                   // blocks of the contraction that one accumulator takes
   int32_t* dev_status;
   uint32_t wait_limit;
 };
@@ -523,7 +555,8 @@ __device__ __forceinline__ int mm_row(int q, MmDiv div, int n_rows, int32_t* dev
   return -1;
 }
 
-template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
+// LONG: some tile's contraction may go in sections
+template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue, bool LONG>
 __global__ void __launch_bounds__(mm_threads(GATHER ? Epilogue::kGathering : 0), 1)
 dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmParams p) {
   constexpr int kHalf = BN / CG;                       // columns whose rows a CTA fetches
@@ -810,17 +843,31 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     if (rank == 0) {
       uint32_t slot = 0, phase = 0;
       int turn = 0;
+      uint32_t parity = 0, held = 0;      // (LONG) bit b: of accumulator b's next turn; the accumulator whose turn it is
       bool alive = true;
       const uint32_t ring_a = mm_desc_lo(smem_u32(ring), A_MN), ring_b = mm_desc_lo(smem_u32(ring) + kMmA, B_MN);
       for (int t = unit; t < total && alive; t += n_units) {
         const MmTile tile = schedule.get(t).uniform_copy();
         if (tile.kblocks == 0) continue;
         const uint32_t idesc = mm_idesc(A_MN, B_MN, 128 * CG, mm_width<CG>(tile.ncols));
-        const int buf = turn & 1;
-        if (!mm_wait(smem_u32(&s->acc_empty[buf]), (uint32_t)((turn >> 1) & 1) ^ 1u, abort_flag, p.wait_limit)) break;
-        tc_fence_after();
-        const uint32_t d = tmem + (uint32_t)buf * kAccCols;
+        const uint32_t buf = LONG ? held : (uint32_t)turn & 1u;
+        // (a long contraction's sections take turns on one accumulator; the other one holds their sum)
+        auto empty = [&] {
+          const uint32_t odd = LONG ? (parity >> buf) & 1u : (uint32_t)(turn >> 1) & 1u;
+          if (!mm_wait(smem_u32(&s->acc_empty[buf]), odd ^ 1u, abort_flag, p.wait_limit)) return false;
+          tc_fence_after();
+          if (LONG) parity ^= 1u << buf;
+          return true;
+        };
+        int begin = 0, end = LONG ? min(p.section, tile.kblocks) : tile.kblocks;
+        if (!empty()) break;
+        const uint32_t d = tmem + buf * kAccCols;
         for (int kb = 0; kb < tile.kblocks; ++kb) {
+          if (LONG && kb == end) {
+            if (!empty()) { alive = false; break; }
+            begin = end;
+            end = min(end + p.section, tile.kblocks);
+          }
           if (!mm_wait<CG == 2>(smem_u32(&s->full[slot]), phase, abort_flag, p.wait_limit)) { alive = false; break; }
           // (no tcgen05 fence: the stage was written in, or made visible to, the tensor core's proxy; a fence drains the pipe)
           const uint32_t a = ring_a + slot * (uint32_t)(kStage >> 4), b = ring_b + slot * (uint32_t)(kStage >> 4);
@@ -828,15 +875,20 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               mm_mma<CG>(d, a + (uint32_t)(i * (A_MN ? 128 : 2)), b + (uint32_t)(i * (B_MN ? 128 : 2)), idesc,
-                         (kb | i) != 0 ? 1u : 0u);
+                         (kb != begin) | (i != 0) ? 1u : 0u);
             mm_commit<CG>(smem_u32(&s->empty[slot]));
-            if (kb + 1 == tile.kblocks) mm_commit<CG>(smem_u32(&s->acc_full[buf]));
+            if (kb + 1 == end) mm_commit<CG>(smem_u32(&s->acc_full[buf]));
           }
           __syncwarp();
           if (++slot == STAGES) { slot = 0; phase ^= 1u; }
         }
         if (!alive) break;
         ++turn;
+        if constexpr (LONG) {
+          // (the accumulator that holds a sum is handed back like one that held products)
+          if (tile.kblocks > p.section) parity ^= 2u >> buf;
+          else held ^= 1u;
+        }
       }
     }
   } else if (warp < kMmStoring) {
@@ -846,6 +898,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     Epilogue epi(p, maps, lane, share, smem_u32(staging) + (uint32_t)warp * Epilogue::kStaging,
                  MmFetch{smem_u32(&s->fetched[warp][0]), abort_flag, p.wait_limit});
     int turn = 0;
+    uint32_t parity = 0, held = 0;              // (LONG) as the products'
     MmTile next = {};
     if (unit < total) next = schedule.get(unit);
     for (int t = unit; t < total; t += n_units) {
@@ -860,24 +913,61 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         for (int c = kCols * share; c < tile.ncols && lane0 < p.lanes; c += 2 * kCols) epi.chunk(tile, lane0, c, v, [] {});
         continue;
       }
-      const int buf = turn & 1;
-      // (the wait lasts as long as the tile's products: a limit for every 16384 blocks of the contraction, some 5 ms)
-      const uint64_t limit = (uint64_t)p.wait_limit * (1u + ((uint32_t)tile.kblocks >> 14));
-      if (!mm_store_wait(smem_u32(&s->acc_full[buf]), (uint32_t)(turn >> 1) & 1u, abort_flag,
-                         (uint32_t)(limit < UINT32_MAX ? limit : UINT32_MAX), lane)) break;
-      tc_fence_after();
-      const uint32_t base = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)buf * kAccCols;
-      int c = kCols * share;
       const int lanes = FORM == kHead ? tile.rows : p.lanes;
       const int end = lane0 >= lanes ? 0 : (tile.ncols + Epilogue::kRound - 1) / Epilogue::kRound * Epilogue::kRound;
-      auto taken = [&]() {                     // the accumulator may be written again
+      const uint32_t quarters = tmem + ((uint32_t)(32 * quarter) << 16);
+      const uint32_t buf = LONG ? held : (uint32_t)turn & 1u;
+      uint32_t from = buf;                     // the accumulator that the tile is taken from
+      auto taken = [&]() {                     // it may be written again
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if constexpr (CG == 2) arrive_at_first(smem_u32(&s->acc_empty[buf]));
-          else mbar_arrive(smem_u32(&s->acc_empty[buf]));
+          if constexpr (CG == 2) arrive_at_first(smem_u32(&s->acc_empty[from]));
+          else mbar_arrive(smem_u32(&s->acc_empty[from]));
         }
       };
+      auto full = [&] {
+        const uint32_t odd = LONG ? (parity >> buf) & 1u : (uint32_t)(turn >> 1) & 1u;
+        if (!mm_store_wait(smem_u32(&s->acc_full[buf]), odd, abort_flag, p.wait_limit, lane)) return false;
+        tc_fence_after();
+        if (LONG) parity ^= 1u << buf;
+        return true;
+      };
+      if (!full()) break;
+      bool alive = true;
+      for (int kb = 0; LONG && tile.kblocks > p.section; kb += p.section) {
+        // A section of a long contraction: this warp's part of it is added to its part of the other accumulator.  That one is free of
+        // products: its last ones were taken out, by this warp too, before this tile, and are handed back after it.
+        const uint32_t part = quarters + buf * kAccCols, sum = quarters + (buf ^ 1u) * kAccCols;
+#pragma unroll 1
+        for (int c0 = kCols * share; c0 < end; c0 += 2 * kCols) {
+#pragma unroll 1
+          for (int i = 0; i < kCols; i += 16) {
+            float x[16], y[16];
+            mm_ld16(part + (uint32_t)(c0 + i), x);
+            if (kb > 0) {
+              mm_ld16(sum + (uint32_t)(c0 + i), y);
+              mm_ld_wait(x, y);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) x[j] += y[j];
+              mm_st16(sum + (uint32_t)(c0 + i), x);
+            } else {
+              mm_ld_wait(x);
+              mm_st16(sum + (uint32_t)(c0 + i), x);
+            }
+          }
+        }
+        mm_st_wait();
+        taken();
+        if (kb + p.section >= tile.kblocks) {
+          from = buf ^ 1u;
+          break;
+        }
+        if (!full()) { alive = false; break; }
+      }
+      if (!alive) break;
+      const uint32_t base = quarters + from * kAccCols;
+      int c = kCols * share;
       if (c >= end) {
         taken();
       } else if constexpr (Epilogue::kBefore) {
@@ -899,6 +989,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       }
       epi.end(tile);
       ++turn;
+      if (LONG && from == buf) held ^= 1u;
     }
     epi.finish();
   }
@@ -943,9 +1034,9 @@ constexpr size_t mm_smem() {
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
-template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
+template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue, bool LONG>
 cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long long max_tiles, cudaStream_t st) {
-  auto kernel = dx_mm_kernel<FORM, GATHER, CG, BN, STAGES, Epilogue>;
+  auto kernel = dx_mm_kernel<FORM, GATHER, CG, BN, STAGES, Epilogue, LONG>;
   constexpr size_t smem = mm_smem<CG, BN, STAGES, Epilogue>();
   static_assert(smem <= 227 * 1024);
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -955,6 +1046,14 @@ cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long l
   if (units < 1) units = 1;
   return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(GATHER ? Epilogue::kGathering : 0)), smem,
                        st, CG, maps, p);
+}
+// (a kernel of its own for long contractions: the code for their sections costs the gathering forms registers, 5 % of SwiGLU of 98304
+// gathered rows)
+template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
+cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long long max_tiles, cudaStream_t st) {
+  const int most = ((FORM == kOuter ? p.n_rows : p.kdim) - 1) / kMmK + 1;      // blocks of a tile's contraction
+  return most > p.section ? mm_launch<FORM, GATHER, CG, BN, STAGES, Epilogue, true>(ctx, maps, p, max_tiles, st)
+                          : mm_launch<FORM, GATHER, CG, BN, STAGES, Epilogue, false>(ctx, maps, p, max_tiles, st);
 }
 
 }  // namespace

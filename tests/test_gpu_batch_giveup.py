@@ -59,7 +59,8 @@ CALLS = {
     "pairs": (grouped, 300, False, False, BF16), "pairs_gathered": (grouped, 300, False, True, F32),
     "pairs_transposed": (grouped, 300, True, True, BF16), "few": (grouped, 2, False, False, F32),
     "few_gathered": (grouped, 20, True, True, BF16), "some": (grouped, 50, True, False, BF16),
-    "dw": (gradient, 3000, 1024, False), "dw_gathered": (gradient, 3000, 1024, True), "dw_single": (gradient, 60, 640, True),
+    "dw": (gradient, 1000, 1024, False), "dw_gathered": (gradient, 1000, 1024, True), "dw_single": (gradient, 60, 640, True),
+    "dw_long": (gradient, 13000, 1024, False), "dw_long_gathered": (gradient, 13000, 1024, True),
     "swiglu": (swiglu, 300, False, False), "swiglu_few": (swiglu, 4, False, True),
     "swiglu_grad": (swiglu, 300, True, False), "swiglu_grad_gathered": (swiglu, 300, True, True),
     "swiglu_grad_some": (swiglu, 50, True, True), "swiglu_grad_few": (swiglu, 8, True, False),

@@ -117,3 +117,144 @@ def test_pairs_in_order_take_their_tokens_gradient(dx, counts, k):
     assert torch.equal(binding.moe_grouped_mm(ctx, x, w, off, gather_div=k)[rows], binding.moe_grouped_mm(ctx, x, w, off)[rows])
     assert torch.equal(binding.moe_grouped_swiglu(ctx, x, w, off, gather_div=k)["act"][rows],
                        binding.moe_grouped_swiglu(ctx, x, w, off)["act"][rows])
+
+
+# ---- long contractions ----------------------------------------------------------------------------------------------------
+# The tensor cores' additions truncate, so a contraction goes in sections of 4096 terms (results in fp32) or 32768 (in bf16) whose
+# sums are added up rounded to nearest.  A section's error is that of the other tests, (2 n / 16 + 2) 2^-23 of the sum of absolute
+# values for n terms, and each of S additions is off by at most half a step, 2^-24 of it.
+def long_bound(terms, section):
+    n = min(terms, section)
+    return (2 * n / 16 + 2) * 2.0 ** -23 + -(-terms // section) * 2.0 ** -24
+
+
+def whole(g, *shape, some=1.0):
+    """-2, -1, 1, 2, and zeros for all but ``some`` of the elements: sums of their products are exact in fp32 below 2^24."""
+    x = torch.randint(1, 3, shape, generator=g, device="cuda") * (1 - 2 * torch.randint(0, 2, shape, generator=g, device="cuda"))
+    return (x * (torch.rand(shape, generator=g, device="cuda") < some)).to(BF16)
+
+
+LENGTHS = [[4096, 4097, 0, 8191, 8192, 8193, 5], [12345, 1, 0, 64, 20000], [63, 4159, 4160, 4161, 300, 16389, 0, 0, 700, 4096, 9000, 30]]
+
+
+@pytest.mark.parametrize("counts", LENGTHS)
+@pytest.mark.parametrize("n,k", [(264, 136), (40, 520), (776, 1288)])
+def test_gradients_of_long_groups_are_exact_where_their_sums_are(dx, counts, n, k):
+    """Long and short groups, empty ones between them, on few and on many tiles: every term is there once."""
+    binding, ctx = dx
+    g = rng(n + sum(counts))
+    P, E = sum(counts), len(counts)
+    off = [0]
+    for c in counts:
+        off.append(off[-1] + c)
+    dy, x = whole(g, P, n), whole(g, P, k)
+    want = torch.stack([dy[a:b].double().t() @ x[a:b].double() for a, b in zip(off, off[1:])])
+    off = ints(*off)
+    assert torch.equal(binding.moe_grouped_mm_dw(ctx, dy, x, off, out_dtype=F32).double(), want)
+    order = torch.randperm(P, generator=g, device="cuda")
+    put = lambda t: torch.empty_like(t).index_copy_(0, order, t)  # noqa: E731
+    named = order.to(torch.int32)
+    assert torch.equal(binding.moe_grouped_mm_dw(ctx, put(dy), put(x), off, gather_dy=named, gather_x=named, out_dtype=F32).double(), want)
+
+
+def test_gradients_of_long_groups_in_bf16(dx):
+    """Sums of at most 256, which bf16 holds; sections of 32768 rows."""
+    binding, ctx = dx
+    g = rng(8)
+    counts = [32768, 40000, 7, 0, 98310, 32769]
+    off = [0]
+    for c in counts:
+        off.append(off[-1] + c)
+    dy, x = whole(g, off[-1], 136, some=0.02), whole(g, off[-1], 264, some=0.02)
+    want = torch.stack([dy[a:b].double().t() @ x[a:b].double() for a, b in zip(off, off[1:])])
+    assert float(want.abs().max()) <= 256
+    assert torch.equal(binding.moe_grouped_mm_dw(ctx, dy, x, ints(*off)).double(), want)
+
+
+@pytest.mark.parametrize("counts", [[3, 0, 1], [40, 50, 0, 33], [300, 5, 513, 0, 700]])
+@pytest.mark.parametrize("K", [4096, 4104, 8192, 8256, 12296])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_products_of_long_rows_are_exact_where_their_sums_are(dx, counts, K, transposed):
+    binding, ctx = dx
+    g = rng(K)
+    P, E, n = sum(counts), len(counts), 520
+    off = [0]
+    for c in counts:
+        off.append(off[-1] + c)
+    w = whole(g, E, K, n) if transposed else whole(g, E, n, K)
+    x = whole(g, P, K)
+    want = torch.cat([x[a:b].double() @ (w[e].double() if transposed else w[e].double().t()) for e, (a, b) in enumerate(zip(off, off[1:]))])
+    off = ints(*off)
+    assert torch.equal(binding.moe_grouped_mm(ctx, x, w, off, transposed=transposed, out_dtype=F32).double(), want)
+    order = torch.randperm(P, generator=g, device="cuda").to(torch.int32)
+    to = torch.randperm(P, generator=g, device="cuda").to(torch.int32)
+    y = binding.moe_grouped_mm(ctx, torch.empty_like(x).index_copy_(0, order.long(), x), w, off, transposed=transposed, gather=order,
+                               scatter=to, out_dtype=F32)
+    assert torch.equal(y[to.long()].double(), want)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("rows", [3, 40, 300])
+def test_products_of_very_long_rows_in_bf16(dx, transposed, rows):
+    binding, ctx = dx
+    g = rng(rows)
+    K = 65544
+    w = whole(g, 2, K, 136, some=0.03) if transposed else whole(g, 2, 136, K, some=0.03)
+    x = whole(g, 2 * rows, K, some=0.03)
+    want = torch.cat([x[e * rows:(e + 1) * rows].double() @ (w[e].double() if transposed else w[e].double().t()) for e in range(2)])
+    assert float(want.abs().max()) <= 256
+    assert torch.equal(binding.moe_grouped_mm(ctx, x, w, ints(0, rows, 2 * rows), transposed=transposed).double(), want)
+
+
+def test_one_tile_of_two_million_rows(dx):
+    """As long as the other tests' longest, with a limit on waits that is a fraction of the products' time; every one of the terms
+    shows in a sum that is exact."""
+    binding, ctx = dx
+    ctx.set_wait_limit(1 << 15)
+    g, P = rng(5), (1 << 21) + 5
+    dy, x = whole(g, P, 8), whole(g, P, 16)
+    got = binding.moe_grouped_mm_dw(ctx, dy, x, ints(0, P), out_dtype=F32)
+    assert ctx.device_status() == 0
+    assert torch.equal(got[0].double(), dy.double().t() @ x.double())
+
+
+@pytest.mark.parametrize("dtype,P", [(F32, 98309), (F32, 400000), (BF16, 1 << 20)])
+def test_sums_of_one_sign_do_not_drift(dx, dtype, P):
+    """A weight gradient over one long group whose terms are all positive: what truncation takes away does not grow with the rows."""
+    binding, ctx = dx
+    g = rng(9)
+    dy, x = draw(g, P, 64).abs() + 1, draw(g, P, 72).abs() + 1
+    want = dy.double().t() @ x.double()
+    got = binding.moe_grouped_mm_dw(ctx, dy, x, ints(0, P), out_dtype=dtype)[0].double()
+    bound = long_bound(P, 4096) if dtype is F32 else long_bound(P, 32768) + 2.0 ** -8
+    assert float(((got - want).abs() / want).max()) <= bound
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_products_of_one_sign_do_not_drift(dx, transposed):
+    binding, ctx = dx
+    g, K = rng(10), 65536
+    x = draw(g, 90, K).abs() + 1
+    w = draw(g, 1, *((K, 64) if transposed else (64, K))).abs() + 1
+    want = x.double() @ (w[0].double() if transposed else w[0].double().t())
+    got = binding.moe_grouped_mm(ctx, x, w, ints(0, 90), transposed=transposed, out_dtype=F32).double()
+    assert float(((got - want).abs() / want).max()) <= long_bound(K, 4096)
+
+
+@pytest.mark.parametrize("rows", [4, 60, 300])
+def test_gates_gradients_through_long_rows(dx, rows):
+    """d_topk_w = <W^T dy, act> with all terms positive: what the products are off by, what 32-bit sums over I are, and 2^-18 for the
+    sigmoid and the activation (as the other tests of it allow)."""
+    binding, ctx = dx
+    g, H, I = rng(rows), 65536, 40
+    dy, wd = draw(g, rows, H).abs() + 1, draw(g, 1, H, I).abs() + 1
+    gate_up = draw(g, rows, 2 * I).abs() + 1
+    topk_w = torch.rand((rows,), generator=g, device="cuda") + 0.5
+    got = binding.moe_grouped_swiglu_backward(ctx, dy, wd, gate_up, topk_w, ints(0, rows))
+    gate, up = gate_up.double().chunk(2, dim=1)
+    a, s = dy.double() @ wd[0].double(), torch.sigmoid(gate)
+    want = (a * gate * s * up).sum(1)
+    bound = long_bound(H, 4096) + I * 2.0 ** -23 + 2.0 ** -18
+    assert float(((got["d_topk_w"].double() - want).abs() / want).max()) <= bound
+    d_up = topk_w.double()[:, None] * a * gate * s
+    assert float(((got["d_gate_up"][:, I:].double() - d_up).abs() / d_up).max()) <= bound + 2.0 ** -8
