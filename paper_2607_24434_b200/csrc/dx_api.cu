@@ -1201,10 +1201,18 @@ extern "C" dx_status moe_combine_tokens_backward(dx_ctx* ctx, const void* dy, in
   return DX_OK;
 }
 
+namespace {
+// (tiles, pieces and rows are numbered in 32 bits)
+bool head_countable(int32_t N, int32_t V) {
+  return ((int64_t)N / 128 + 1) * ((int64_t)V / 256 + 1) <= INT32_MAX && V <= INT32_MAX - 512 && N <= INT32_MAX - 2048;
+}
+}  // namespace
+
 extern "C" dx_status spec_head_loss_workspace(dx_ctx* ctx, int32_t N, int32_t V, int32_t H, int32_t grad, size_t* least_out,
                                               size_t* best_out) {
   if (!ctx || !least_out || !best_out) return DX_ERR_INVALID_ARG;
   if (N < 0 || V < 1 || H < 1) return DX_ERR_SHAPE;
+  if (!head_countable(N, V)) return DX_ERR_UNSUPPORTED;
   *least_out = *best_out = 0;
   if (N > 0) dx_head_loss_workspace(ctx->sm_count, N, V, H, grad, least_out, best_out);
   return DX_OK;
@@ -1221,9 +1229,7 @@ extern "C" dx_status spec_head_loss(dx_ctx* ctx, const void* h, int32_t N, int64
   if (s == DX_OK && dh) s = check_matrix(dh, N, H, ld_dh);
   if (s == DX_OK && dW) s = check_matrix(dW, V, H, ld_dW);
   if (s != DX_OK) return s;
-  // (tiles and pieces are numbered in 32 bits)
-  if (((int64_t)N / 128 + 1) * ((int64_t)V / 256 + 1) > INT32_MAX || V > INT32_MAX - 512 || N > INT32_MAX - 2048)
-    return DX_ERR_UNSUPPORTED;
+  if (!head_countable(N, V)) return DX_ERR_UNSUPPORTED;
   if (!loss && !dh && !dW) return DX_ERR_INVALID_ARG;
   const Range in[2] = {rows_range(h, N, H, ldh, 2), rows_range(W_lm, V, H, ldw, 2)};
   const Range out[2] = {rows_range(dh, dh ? N : 0, H, ld_dh, 2), rows_range(dW, dW ? V : 0, H, ld_dW, 2)};
