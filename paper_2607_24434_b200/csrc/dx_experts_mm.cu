@@ -171,7 +171,7 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
   int next;      // where column `lane` of the next chunk goes (looked up a chunk ahead)
   __device__ __forceinline__ void look_up(const MmTile& t, int c0) {
     const int row = this->lane < Base::kCols ? sorted_row(t, c0, this->lane) : -1;
-    next = row >= 0 && this->p.scatter ? __ldg(this->p.scatter + row) : row;
+    next = row >= 0 && this->p.scatter && DX_BOUNDS(row < this->p.n_rows, this->p.dev_status) ? __ldg(this->p.scatter + row) : row;
   }
   __device__ __forceinline__ void begin(const MmTile& t, int, int c0, const MmTile&, bool) { look_up(t, c0); }
   template <class Taken>
@@ -182,6 +182,7 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
       atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_ROW);
       mine = -1;
     }
+    if (!DX_BOUNDS(mine < this->p.out_rows, p.dev_status)) mine = -1;
     look_up(t, c0 + 2 * Base::kCols);
     this->writable();
     if constexpr (sizeof(T) == 2 && !ADD) stage_bf16(this->at, this->lane, x);
@@ -245,7 +246,9 @@ struct StoreSwiglu : FragmentEpilogue<32> {
     for (int k = 0; k < 2; ++k) u[k] = lds16(from + half32(16 * k + (lane >> 1), lane & 1));
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-      if (16 * k + (lane >> 1) < t.ncols - c0 && i < (p.lanes >> 1)) *reinterpret_cast<uint4*>(out + (int64_t)(16 * k) * ld) = u[k];
+      if (16 * k + (lane >> 1) < t.ncols - c0 && i < (p.lanes >> 1) &&
+          DX_BOUNDS(t.n0 + c0 + 16 * k + (lane >> 1) < p.n_rows, p.dev_status))
+        *reinterpret_cast<uint4*>(out + (int64_t)(16 * k) * ld) = u[k];
   }
   template <class Taken>
   __device__ __forceinline__ void chunk(const MmTile& t, int lane0, int c0, const Values& x, Taken) {
@@ -334,7 +337,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {        // 16 columns of every 32
       const int r = sorted_row(t, 32 * (2 * j + (lane >> 4)) + 16 * share, lane & 15);
-      q[j] = r < 0 ? INT_MIN : p.b_index ? __ldg(p.b_index + r) : r;
+      q[j] = r < 0 || !DX_BOUNDS(r < p.n_rows, p.dev_status) ? INT_MIN : p.b_index ? __ldg(p.b_index + r) : r;
     }
   }
   __device__ __forceinline__ void ask_weights() {
@@ -458,7 +461,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       for (int i = 0; i < 2; ++i) {
         const int column = 8 * i + (lane >> 2);
         const uint4 u0 = lds16(buf + piece2(column, 0, lane & 3)), u1 = lds16(buf + piece2(column, 1, lane & 3));
-        if (c0 + column < t.ncols && x < p.lanes) {
+        if (c0 + column < t.ncols && x < p.lanes && DX_BOUNDS(t.n0 + c0 + column < p.n_rows, p.dev_status)) {
           __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.out) + (int64_t)(t.n0 + c0 + column) * p.ld + x;
           *reinterpret_cast<uint4*>(to) = u0;
           *reinterpret_cast<uint4*>(to + p.lanes) = u1;
@@ -488,7 +491,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       }
       dw[0] += __shfl_xor_sync(0xffffffffu, dw[0], 4);
       const int k = lane >> 3, column = c0 + 8 * (k >> 1) + 2 * (lane & 3) + (k & 1);
-      if (!(lane & 4) && column < t.ncols) p.partial[(int64_t)(lane0 >> 5) * p.n_rows + t.n0 + column] = dw[0];
+      if (!(lane & 4) && column < t.ncols && DX_BOUNDS(t.n0 + column < p.n_rows && lane0 < p.lanes, p.dev_status))
+        p.partial[(int64_t)(lane0 >> 5) * p.n_rows + t.n0 + column] = dw[0];
     }
     ++turn;
   }
@@ -497,12 +501,13 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
 // d pair_w[q] = sum of the shares, in order
 __global__ void __launch_bounds__(256) dx_pair_weight_grad_kernel(const float* partial, int parts, int n_rows,
                                                                   const int32_t* offsets, int n_groups,
-                                                                  const int32_t* index, int n_pairs, float* d_pair_w) {
+                                                                  const int32_t* index, int n_pairs, float* d_pair_w,
+                                                                  int32_t* dev_status) {
   dx_pdl_wait();
   dx_pdl_trigger();
   const int r = blockIdx.x * 256 + threadIdx.x;
   const int lo = max(0, __ldg(offsets)), hi = min(n_rows, __ldg(offsets + n_groups));
-  if (r < lo || r >= hi) return;
+  if (r < lo || r >= hi || !DX_BOUNDS(r < n_rows, dev_status)) return;
   const int q = index ? __ldg(index + r) : r;
   if (q < 0 || q >= n_pairs) return;
   float sum = 0.0f;
@@ -735,7 +740,8 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   const int parts = (a.k + 31) / 32;
   *n_launches = 2;
   return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, dx_pair_weight_grad_kernel, dim3((a.n_rows + 255) / 256), dim3(256), 0,
-                       st, 1, partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather, n_pairs, d_pair_w);
+                       st, 1, partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather, n_pairs, d_pair_w,
+                       ctx->dev_status);
 }
 
 cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t st) {

@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(1024) dx_head_rows_kernel(const int32_t* targe
 #pragma unroll 4
   for (int r = lo; r < hi; ++r) {
     bool bad;
-    if (row_counts(targets, row_weight, r, V, bad)) live[at++] = r;
+    if (row_counts(targets, row_weight, r, V, bad) && DX_BOUNDS(at < N, dev_status)) live[at++] = r;
   }
   if (threadIdx.x == 0) {
     n_live[0] = 0;        // (offsets of the one group that the products of the gradients see)
@@ -89,23 +89,24 @@ __global__ void __launch_bounds__(kListed) dx_head_few_kernel(const int32_t* tar
   if (r == 0) {
     if (own_bad) atomicExch(dev_status, (int32_t)DX_DEV_BAD_TOKEN);
     if (!in && loss) loss[mine] = own_bad ? __int_as_float(0x7fffffff) : 0.0f;
-    if (in) live[at] = mine;
+    if (in && DX_BOUNDS(at < N, dev_status)) live[at] = mine;
     if (mine == N - 1) {
       n_live[0] = 0;
       n_live[1] = at + (in ? 1 : 0);
     }
   }
-  if (!in) return;
+  if (!in || !DX_BOUNDS(at < N, dev_status)) return;
   for (int i = r * 8; i < H; i += kListed * 8)
     *reinterpret_cast<uint4*>(out + (int64_t)at * H + i) = __ldg(reinterpret_cast<const uint4*>(h + mine * ldh + i));
 }
 // the listed rows next to each other: four rows per CTA
 __global__ void __launch_bounds__(256) dx_head_pack_kernel(const __nv_bfloat16* h, int64_t ldh, int H, const int32_t* live,
-                                                           const int32_t* n_live, __nv_bfloat16* out) {
+                                                           const int32_t* n_live, int N, __nv_bfloat16* out,
+                                                           int32_t* dev_status) {
   dx_pdl_wait();
   dx_pdl_trigger();
   const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= __ldg(n_live)) return;
+  if (row >= __ldg(n_live) || !DX_BOUNDS(row < N && live[row] >= 0 && live[row] < N, dev_status)) return;
   const __nv_bfloat16* from = h + (int64_t)__ldg(live + row) * ldh;
   for (int i = (threadIdx.x & 63) * 8; i < H; i += 512)
     *reinterpret_cast<uint4*>(out + (int64_t)row * H + i) = __ldg(reinterpret_cast<const uint4*>(from + i));
@@ -154,6 +155,7 @@ struct RowSums {
   __device__ __forceinline__ void zero(Values&) {}
   __device__ __forceinline__ void begin(const MmTile& t, int lane0, int, const MmTile&, bool) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
+    if (!DX_BOUNDS(row < p.n_rows, p.dev_status)) row = -1;
     target = row >= 0 ? __ldg(p.targets + __ldg(p.live + row)) - t.n0 : -1;   // (its place among the tile's columns)
     top = -INFINITY;
     sum = 0.0f;
@@ -163,7 +165,7 @@ struct RowSums {
     taken();
     float(&v)[32] = x.v;
     const int left = t.ncols - c0;
-    if (KEEP && row >= 0) store32(p.logits + (int64_t)row * p.ld_logits + t.n0 + c0, v, left);
+    if (KEEP && row >= 0 && DX_BOUNDS(t.n0 + c0 + (left < 32 ? (left + 7) / 8 * 8 : 32) <= p.ld_logits, p.dev_status)) store32(p.logits + (int64_t)row * p.ld_logits + t.n0 + c0, v, left);
     if (left < 32) {
 #pragma unroll
       for (int c = 0; c < 32; ++c)
@@ -201,7 +203,7 @@ __global__ void __launch_bounds__(1024) dx_head_join_kernel(const float2* part, 
                                                            const int32_t* n_live_at, const float* target_logit, float* loss,
                                                            float* lse, float* row_loss, const int32_t* targets,
                                                            const float* row_weight, int N, int V, int H,
-                                                           __nv_bfloat16* dh, int64_t ld_dh) {
+                                                           __nv_bfloat16* dh, int64_t ld_dh, int32_t* dev_status) {
   __shared__ float tops[32][32];
   __shared__ double sums[32][32];
   dx_pdl_wait();
@@ -229,7 +231,7 @@ __global__ void __launch_bounds__(1024) dx_head_join_kernel(const float2* part, 
   tops[warp][lane] = top;
   sums[warp][lane] = sum;
   __syncthreads();
-  if (warp == 0 && row < n_live) {
+  if (warp == 0 && row < n_live && DX_BOUNDS(row < N && live[row] >= 0 && live[row] < N, dev_status)) {
     float m = tops[0][lane];
 #pragma unroll
     for (int w = 1; w < 32; ++w) m = fmaxf(m, tops[w][lane]);
@@ -269,6 +271,7 @@ struct StoreDz {
   __device__ __forceinline__ void zero(Values&) {}
   __device__ __forceinline__ void begin(const MmTile& t, int lane0, int, const MmTile&, bool) {
     row = lane0 + lane < t.rows ? lane0 + lane : -1;
+    if (!DX_BOUNDS(row < p.n_rows, p.dev_status)) row = -1;
     target = -1;
     lse = weight = at_target = 0.0f;
     if (row >= 0) {
@@ -297,7 +300,7 @@ struct StoreDz {
       for (int c = 0; c < 32; ++c)
         if (c >= t.ncols - c0) v[c] = 0.0f;
     }
-    if (row < 0) return;
+    if (row < 0 || !DX_BOUNDS(row < p.panel && t.n0 % kPanel == 0 && c0 + 32 <= kPanel, p.dev_status)) return;
     store32(reinterpret_cast<__nv_bfloat16*>(p.out) + ((int64_t)(t.n0 / kPanel) * p.panel + row) * kPanel + c0, v);
   }
 };
@@ -319,11 +322,14 @@ __device__ __forceinline__ uint4 dz_of(const float* logits, float weight, float 
 // words v0 .. v0 + len of all rows (blockIdx.x): dz of a piece
 __global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, int64_t ld_logits, int v0, int len, const int32_t* live,
                                                          const int32_t* n_live, const int32_t* targets, const float* row_weight,
-                                                         const float* lse, const float* row_loss, __nv_bfloat16* dz, int panel) {
+                                                         const float* lse, const float* row_loss, __nv_bfloat16* dz, int panel,
+                                                         int32_t* dev_status) {
   dx_pdl_wait();
   dx_pdl_trigger();
   const int row = blockIdx.x, v = (blockIdx.y * 256 + threadIdx.x) * 8;
-  if (row >= __ldg(n_live) || v >= (len + 63) / 64 * 64) return;
+  if (row >= __ldg(n_live) || v >= (len + 63) / 64 * 64 ||
+      !DX_BOUNDS(row < panel && live[row] >= 0 && live[row] < panel && v0 + v + 8 <= ld_logits, dev_status))
+    return;
   const int r = __ldg(live + row);
   *reinterpret_cast<uint4*>(dz + ((int64_t)(v / kPanel) * panel + row) * kPanel + v % kPanel) =
       dz_of(logits + row * ld_logits + v0 + v, row_weight ? __ldg(row_weight + r) : 1.0f, __ldg(lse + row), __ldg(row_loss + row),
@@ -336,7 +342,8 @@ __global__ void __launch_bounds__(256) dx_head_row_kernel(const float* logits, i
                                                          const int32_t* n_live, const int32_t* targets,
                                                          const float* row_weight, const float2* part, int halves,
                                                          const float* target_logit, float* loss, float* lses, float* row_losses,
-                                                         __nv_bfloat16* dz, int panel, int H, __nv_bfloat16* dh, int64_t ld_dh) {
+                                                         __nv_bfloat16* dz, int panel, int H, __nv_bfloat16* dh, int64_t ld_dh,
+                                                         int32_t* dev_status) {
   __shared__ float tops[8], row_loss_at, lse_at;
   __shared__ double sums[8];
   dx_pdl_wait();
@@ -347,7 +354,7 @@ __global__ void __launch_bounds__(256) dx_head_row_kernel(const float* logits, i
     if (!row_counts(targets, row_weight, row, V, bad))
       for (int i = threadIdx.x; i < H / 8; i += 256) *reinterpret_cast<uint4*>(dh + row * ld_dh + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
   }
-  if (row >= __ldg(n_live)) return;
+  if (row >= __ldg(n_live) || !DX_BOUNDS(row < panel && live[row] >= 0 && live[row] < panel, dev_status)) return;
   const int r = __ldg(live + row), target = __ldg(targets + r) - v0;
   const float weight = row_weight ? __ldg(row_weight + r) : 1.0f, z_target = __ldg(target_logit + row);
   const bool here = logits && v0 < (V + 63) / 64 * 64;
@@ -393,18 +400,19 @@ __global__ void __launch_bounds__(256) dx_head_row_kernel(const float* logits, i
     }
   }
   __syncthreads();
-  if (!here) return;
+  if (!here || !DX_BOUNDS(v0 + 8 <= ld_logits, dev_status)) return;
   *reinterpret_cast<uint4*>(dz + ((int64_t)(v0 / kPanel) * panel + row) * kPanel + v0 % kPanel) =
       dz_of(logits + row * ld_logits + v0, weight, lse_at, row_loss_at, target, V - v0);
 }
 
 // dh of the rows that count: the blocks' shares in order, rounded once
 __global__ void __launch_bounds__(128) dx_head_sum_kernel(const float* share, int blocks, int rows, int H, const int32_t* live,
-                                                          const int32_t* n_live, __nv_bfloat16* dh, int64_t ld_dh) {
+                                                          const int32_t* n_live, __nv_bfloat16* dh, int64_t ld_dh,
+                                                          int32_t* dev_status) {
   dx_pdl_wait();
   dx_pdl_trigger();
   const int row = blockIdx.y, i = (blockIdx.x * 128 + threadIdx.x) * 4;
-  if (row >= __ldg(n_live) || i >= H) return;
+  if (row >= __ldg(n_live) || i >= H || !DX_BOUNDS(row < rows && live[row] >= 0 && live[row] < rows, dev_status)) return;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
   for (int b = 0; b < blocks; ++b) {
@@ -603,7 +611,7 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
     if (!launched(dx_launch_pdl(pdl, dx_head_rows_kernel, dim3(1), dim3(1024), 0, st, 1, a.targets, a.row_weight, a.N, a.V, live,
                                 n_live, a.loss, ctx->dev_status))) return e;
     if (!launched(dx_launch_pdl(pdl, dx_head_pack_kernel, dim3((a.N + 3) / 4), dim3(256), 0, st, 1,
-                                reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, rows))) return e;
+                                reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, a.N, rows, ctx->dev_status))) return e;
   }
   p.tile_width = s.width;
   if (!launched(s.keep ? launch_head<RowSums<true>>(ctx, m, p, st) : launch_head<RowSums<false>>(ctx, m, p, st))) return e;
@@ -612,10 +620,11 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
     // (logits that are kept become dz in the same launch)
     if (!launched(dx_launch_pdl(pdl, dx_head_row_kernel, dim3(s.keep ? (a.V + 2047) / 2048 : 1, a.N), dim3(256), 0, st, 1,
                                 s.keep ? logits : nullptr, s.ld_logits, a.V, live, n_live + 1, a.targets, a.row_weight, part,
-                                2 * s.tiles, target_logit, a.loss, lse, row_loss, dz, a.N, a.H, dh, a.ld_dh))) return e;
+                                2 * s.tiles, target_logit, a.loss, lse, row_loss, dz, a.N, a.H, dh, a.ld_dh,
+                                ctx->dev_status))) return e;
   } else if (!launched(dx_launch_pdl(pdl, dx_head_join_kernel, dim3((a.N + 31) / 32), dim3(1024), 0, st, 1, part, s.pitch, 2 * s.tiles, live,
                               n_live + 1, target_logit, a.loss, lse, row_loss, a.targets, a.row_weight, a.N, a.V, a.H, dh,
-                              a.ld_dh))) return e;
+                              a.ld_dh, ctx->dev_status))) return e;
   if (!grad) return e;
 
   for (int64_t v0 = 0; v0 < a.V; v0 += s.piece) {
@@ -623,7 +632,8 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
     const bool first = v0 == 0, last = v0 + len == a.V;
     if (s.keep && !s.by_row) {
       if (!launched(dx_launch_pdl(pdl, dx_head_dz_kernel, dim3(a.N, (len + 2047) / 2048), dim3(256), 0, st, 1, logits, s.ld_logits,
-                                  (int)v0, len, live, n_live + 1, a.targets, a.row_weight, lse, row_loss, dz, a.N))) return e;
+                                  (int)v0, len, live, n_live + 1, a.targets, a.row_weight, lse, row_loss, dz, a.N,
+                                  ctx->dev_status))) return e;
     } else if (!s.keep) {
       MmParams q = p;
       q.columns = len;
@@ -666,7 +676,7 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
       if (!launched(dx_launch_grouped_mm(ctx, g, st))) return e;
       if (s.blocks > 1 && last) {
         if (!launched(dx_launch_pdl(pdl, dx_head_sum_kernel, dim3((a.H + 511) / 512, a.N), dim3(128), 0, st, 1, share, s.blocks, a.N,
-                                    a.H, live, n_live + 1, dh, a.ld_dh))) return e;
+                                    a.H, live, n_live + 1, dh, a.ld_dh, ctx->dev_status))) return e;
       }
     }
     if (a.dW) {

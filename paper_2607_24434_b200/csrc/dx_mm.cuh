@@ -614,8 +614,10 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         if (a != lo || b != hi) atomicExch(p.dev_status, (int32_t)DX_DEV_BAD_OFFSETS);
         lo = a;
         hi = b;
-        s->off[e] = lo;
-        s->cnt[e] = hi - lo;
+        if (DX_BOUNDS(e < DX_MAX_E, p.dev_status)) {
+          s->off[e] = lo;
+          s->cnt[e] = hi - lo;
+        }
       }
       int tiles = (hi - lo + BN - 1) / BN, sum = tiles;
 #pragma unroll
@@ -623,7 +625,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         const int o = __shfl_up_sync(0xffffffffu, sum, d);
         if (lane >= d) sum += o;
       }
-      if (e < p.n_groups) s->before[e] = run + sum - tiles;
+      if (e < p.n_groups && DX_BOUNDS(e < DX_MAX_E, p.dev_status)) s->before[e] = run + sum - tiles;
       run += __shfl_sync(0xffffffffu, sum, 31);
     }
     if (lane == 0) s->before[p.n_groups] = run;
@@ -734,7 +736,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       // what this lane has looked up: a row's place in its matrix, in pieces of 16 bytes, and which lanes' rows exist
       uint32_t at_a[2], at_b[kRegs], ok_a[2], ok_b[kRegs];
       auto resolve = [&](int q, bool in, bool indexed, MmDiv div, int n_rows, int64_t ld, uint32_t& at, uint32_t& ok) {
-        const int row = !in ? -1 : indexed ? mm_row(q, div, n_rows, p.dev_status) : q;
+        int row = !in ? -1 : indexed ? mm_row(q, div, n_rows, p.dev_status) : q;
+        if (in && !indexed && !DX_BOUNDS(q >= 0 && q < n_rows, p.dev_status)) row = -1;
         at = (uint32_t)max(row, 0) * (uint32_t)(ld >> 3);
         ok = __ballot_sync(0xffffffffu, row >= 0);
       };
@@ -759,7 +762,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         int q[kRegs];
 #pragma unroll
         for (int j = 0; j < kRegs; ++j)
-          q[j] = 32 * j + lane >= here ? 0 : p.b_index ? __ldg(p.b_index + n0 + 32 * j + lane) : n0 + 32 * j + lane;
+          q[j] = 32 * j + lane >= here || !DX_BOUNDS(n0 >= 0 && n0 + 32 * j + lane < p.n_rows, p.dev_status) ? 0
+                 : p.b_index ? __ldg(p.b_index + n0 + 32 * j + lane) : n0 + 32 * j + lane;
 #pragma unroll
         for (int j = 0; j < kRegs; ++j)
           resolve(q[j], 32 * j + lane < here, true, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
@@ -770,7 +774,7 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int r = k0 + 32 * j + lane;
-          const bool in = r < tile.rows;
+          const bool in = r < tile.rows && DX_BOUNDS(tile.row0 >= 0 && tile.row0 + r < p.n_rows, p.dev_status);
           next_a[j] = in && p.a_index ? __ldg(p.a_index + tile.row0 + r) : 0;
           next_b[j] = in && p.b_index ? __ldg(p.b_index + tile.row0 + r) : 0;
         }
@@ -906,6 +910,12 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       const bool more = t + n_units < total;
       if (more) next = schedule.get(t + n_units);
       const int lane0 = tile.m0 + (int)rank * 128 + 32 * quarter;   // index of the warp's first lane
+      // (what everything the epilogues store is placed by)
+      if (!DX_BOUNDS(tile.e >= 0 && tile.e < p.n_groups && tile.m0 >= 0 && tile.n0 >= 0 && tile.ncols > 0 && tile.ncols <= BN &&
+                         tile.n0 + tile.ncols <= (FORM == kOuter || FORM == kHead ? p.columns : p.n_rows) &&
+                         tile.row0 >= 0 && tile.rows >= 0 && (FORM != kOuter || tile.row0 + tile.rows <= p.n_rows),
+                     p.dev_status))
+        break;
       epi.begin(tile, lane0, kCols * share, next, more);
       typename Epilogue::Values v;
       if (tile.kblocks == 0) {                                       // (an empty group's product over its rows)
