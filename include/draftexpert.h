@@ -505,11 +505,12 @@ dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, cons
  *   weight pair_w[q] (NULL: 1).  With a = W_e^T dy, s = sigmoid(g):  d_gate_up[r] = (w a u s (1 + g (1 - s)), w a g s),
  *   act_w[r] = w silu(g) u -- with moe_grouped_mm_dw the gradient of W_e: sum of dy act_w^T -- and
  *   d_pair_w[q] = <a, silu(g) u> (may be NULL; pairs that no row stands for are not written, a pair that several rows stand for gets
- *   what one of them gives: a permutation has neither).  A pair of weight 0 is taken out, its row is not looked at: all
- *   of its gradients are 0.  workspace: moe_grouped_swiglu_backward_workspace bytes (0 without d_pair_w), 16-byte aligned.
+ *   what one of them gives: a permutation has neither).  A pair of weight 0 is taken out and its row may hold anything: d_gate_up and
+ *   act_w are 0 there, d_pair_w is 0 where the row makes no finite number of it.  workspace: moe_grouped_swiglu_backward_workspace bytes (0 without d_pair_w), 16-byte aligned.
  * moe_combine_tokens: y[t] = sum_j w[t, j] z[t k + j], rows fp32 or bf16 (each of z, y), k <= 8, sums in fp32; w NULL: all 1.  A
- *   weight of 0 takes its row out (it is not read).  moe_combine_tokens_backward: dz[t k + j] = w[t, j] dy[t] and
- *   dw[t, j] = <z[t k + j], dy[t]> (either may be NULL; both 0 where the weight is 0), all rows of one type.
+ *   weight of 0 takes its row out (it is not read, and may hold anything).  moe_combine_tokens_backward: dz[t k + j] = w[t, j] dy[t]
+ *   (0 where the weight is 0) and dw[t, j] = <z[t k + j], dy[t]> (where the weight is 0 and that is no finite number: 0); either may
+ *   be NULL; all rows of one type.
  *
  * spec_head_loss: for rows h [N, H] bf16 and a head W [V, H] bf16, with z = W h[t]:  loss[t] = log sum_v exp(z_v) - z_target,
  *   dh [N, H] = row_weight[t] * dloss/dh and dW [V, H] = sum_t row_weight[t] * dloss/dW, bf16 (each may be NULL, not all three).

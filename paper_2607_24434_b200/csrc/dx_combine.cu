@@ -98,15 +98,13 @@ __global__ void __launch_bounds__(256) dx_combine_grad_kernel(const T* dy, int64
       d.load(dy + (int64_t)t * ld_dy + kN * i);
       if (dw) {
 #pragma unroll
-        for (int j = 0; j < K; ++j)
-          if (weight[j] != 0.0f) x[j].load(z + ((int64_t)t * K + j) * ldz + kN * i);
+        for (int j = 0; j < K; ++j) x[j].load(z + ((int64_t)t * K + j) * ldz + kN * i);
       }
       float g[kN];
       d.get(g);
 #pragma unroll
       for (int j = 0; j < K; ++j) {
-        const bool on = weight[j] != 0.0f;
-        if (dw && on) {
+        if (dw) {
           float v[kN];
           x[j].get(v);
 #pragma unroll
@@ -115,7 +113,7 @@ __global__ void __launch_bounds__(256) dx_combine_grad_kernel(const T* dy, int64
         if (dz) {
           float o[kN];
 #pragma unroll
-          for (int q = 0; q < kN; ++q) o[q] = on ? weight[j] * g[q] : 0.0f;
+          for (int q = 0; q < kN; ++q) o[q] = weight[j] != 0.0f ? weight[j] * g[q] : 0.0f;
           put(dz + ((int64_t)t * K + j) * ld_dz + kN * i, o);
         }
       }
@@ -133,7 +131,8 @@ __global__ void __launch_bounds__(256) dx_combine_grad_kernel(const T* dy, int64
   if (part == 0 && lane < K && t < n_tokens) {
     float s = share[warp][lane];
     for (int i = 1; i < WARPS; ++i) s += share[warp + i][lane];
-    dw[(int64_t)t * K + lane] = s;
+    const int64_t q = (int64_t)t * K + lane;
+    dw[q] = isfinite(s) || weight_of(w, q) != 0.0f ? s : 0.0f;      // (a row that was taken out may hold anything)
   }
 }
 

@@ -299,7 +299,7 @@ struct StoreSwiglu : FragmentEpilogue<32> {
 
 // D = W_down^T dy = the gradient of an unweighted act.  With q the row's pair, w its weight, s = sigmoid(gate):
 //   d gate = w D up s (1 + gate (1 - s)),  d up = w D gate s,  act_w = w gate s up,  share of d w = sum over lanes of D gate s up.
-// A pair of weight 0 contributes nothing, whatever its rows hold.  gate and up come as boxes, a chunk ahead; their place in the
+// The rows of a pair of weight 0 get zeros, whatever they hold.  gate and up come as boxes, a chunk ahead; their place in the
 // staging takes the gradients, which go out as boxes.  (In pieces through registers, every element crossed the load/store path
 // six times, and that path, shared with the gathering warps, was the bound: 430 us, 49152 rows x 2048 x 1408, now 347.  What bounds
 // it now is the storing warps' arithmetic, some 40 instructions for 32 elements beside their way in and out.)
@@ -474,11 +474,7 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       // eight threads (t / 4) hold shares of the columns 8 n + 2 (t % 4) + i: folded so that two of them each end with one
       float dw[4];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        f2_get(dw2[n], dw[2 * n], dw[2 * n + 1]);
-        if (!(mask[n] & 0xffffu)) dw[2 * n] = 0.0f;
-        if (!(mask[n] >> 16)) dw[2 * n + 1] = 0.0f;
-      }
+      for (int n = 0; n < 2; ++n) f2_get(dw2[n], dw[2 * n], dw[2 * n + 1]);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const int h = 2 >> b, bit = 16 >> b;
@@ -498,10 +494,12 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
   }
 };
 
-// d pair_w[q] = sum of the shares, in order
+// d pair_w[q] = sum of the shares, in order.  The row of a pair of weight 0 was taken out and may hold anything: where that makes no
+// finite number, 0.
 __global__ void __launch_bounds__(256) dx_pair_weight_grad_kernel(const float* partial, int parts, int n_rows,
                                                                   const int32_t* offsets, int n_groups,
-                                                                  const int32_t* index, int n_pairs, float* d_pair_w,
+                                                                  const int32_t* index, const float* pair_w, int n_pairs,
+                                                                  float* d_pair_w,
                                                                   int32_t* dev_status) {
   dx_pdl_wait();
   dx_pdl_trigger();
@@ -513,7 +511,7 @@ __global__ void __launch_bounds__(256) dx_pair_weight_grad_kernel(const float* p
   float sum = 0.0f;
 #pragma unroll 16
   for (int i = 0; i < parts; ++i) sum += __ldg(partial + (int64_t)i * n_rows + r);      // (16 on their way at a time)
-  d_pair_w[q] = sum;
+  d_pair_w[q] = isfinite(sum) || !pair_w || __ldg(pair_w + q) != 0.0f ? sum : 0.0f;
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -740,7 +738,7 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   const int parts = (a.k + 31) / 32;
   *n_launches = 2;
   return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, dx_pair_weight_grad_kernel, dim3((a.n_rows + 255) / 256), dim3(256), 0,
-                       st, 1, partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather, n_pairs, d_pair_w,
+                       st, 1, partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather, pair_w, n_pairs, d_pair_w,
                        ctx->dev_status);
 }
 

@@ -258,3 +258,63 @@ def test_gates_gradients_through_long_rows(dx, rows):
     assert float(((got["d_topk_w"].double() - want).abs() / want).max()) <= bound
     d_up = topk_w.double()[:, None] * a * gate * s
     assert float(((got["d_gate_up"][:, I:].double() - d_up).abs() / d_up).max()) <= bound + 2.0 ** -8
+
+
+# ---- weights of exactly 0 --------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,k,H", [(5, 3, 64), (40, 8, 1000), (2500, 2, 264)])
+def test_gradient_of_a_weight_of_zero(dx, dtype, N, k, H):
+    """y is linear in the weights: the slope is <z, dy> at 0 as anywhere (sums of H products in fp32, each addition half a step).  A
+    row that was taken out and holds NaN or infinities has slope 0, and so has its dz."""
+    binding, ctx = dx
+    g = rng(N)
+    z = torch.randn((N * k, H), generator=g, device="cuda").to(dtype)
+    dy = torch.randn((N, H), generator=g, device="cuda").to(dtype)
+    w = torch.randn((N, k), generator=g, device="cuda")
+    zero = torch.rand((N, k), generator=g, device="cuda") < 0.4
+    w[zero] = 0.0
+    w[0, 0] = -0.0
+    zero[0, 0] = True
+    want = (z.double().view(N, k, H) * dy.double()[:, None]).sum(2)
+    size = (z.double().view(N, k, H) * dy.double()[:, None]).abs().sum(2)
+    back = binding.moe_combine_tokens_backward(ctx, dy, z, w)
+    assert bool(((back["d_topk_w"].double() - want).abs() <= (H / 8 + 16) * 2.0 ** -24 * size).all())
+    assert not back["dz"][zero.reshape(-1)].any()
+    out = torch.where(zero.reshape(-1, 1), float("inf"), z.float()).to(dtype)
+    out[::2] = torch.where(zero.reshape(-1, 1)[::2], NAN, out[::2].float()).to(dtype)
+    gone = binding.moe_combine_tokens_backward(ctx, dy, out, w)
+    assert not gone["d_topk_w"][zero].any() and torch.equal(gone["d_topk_w"][~zero], back["d_topk_w"][~zero])
+    assert torch.equal(gone["dz"], back["dz"])
+    # a row that counts and holds NaN shows it
+    out[k - 1] = NAN
+    w[0, k - 1] = 0.5
+    assert bool(binding.moe_combine_tokens_backward(ctx, dy, out, w)["d_topk_w"][0, k - 1].isnan())
+
+
+@pytest.mark.parametrize("rows", [3, 50, 300])
+def test_gradient_of_a_gate_of_zero(dx, rows):
+    """d_topk_w does not depend on the gate: a gate of 0 gets what it gets with any other, bit for bit, and 0 where its row holds
+    NaN or infinities; d_gate_up and act_w are zeros either way."""
+    binding, ctx = dx
+    g = rng(rows)
+    E, k, H, I = 3, 2, 264, 136
+    P = E * rows // k * k
+    off = ints(0, rows, 2 * rows, P)
+    perm = torch.randperm(P, generator=g, device="cuda").to(torch.int32)
+    dy, wd, gate_up = draw(g, P // k, H), draw(g, E, H, I, scale=0.1), draw(g, P, 2 * I)
+    w = torch.rand((P // k, k), generator=g, device="cuda") + 0.1
+    call = lambda gu, w: binding.moe_grouped_swiglu_backward(ctx, dy, wd, gu, w, off, gather=perm, gather_div=k)  # noqa: E731
+    full = call(gate_up, w)
+    zero = torch.rand((P // k, k), generator=g, device="cuda") < 0.4
+    zero[0, 0] = True
+    of_row = zero.reshape(-1)[perm.long()]
+    some = call(gate_up, w.masked_fill(zero, 0.0))
+    assert bool(full["d_topk_w"][zero].any()) and torch.equal(some["d_topk_w"], full["d_topk_w"])
+    for value in (NAN, float("inf")):
+        gone = call(gate_up.masked_fill(of_row[:, None], value), w.masked_fill(zero, 0.0))
+        assert not gone["d_topk_w"][zero].any() and torch.equal(gone["d_topk_w"][~zero], full["d_topk_w"][~zero])
+        for n in ("d_gate_up", "act_w"):
+            assert not gone[n][of_row].any() and not some[n][of_row].any()
+            assert torch.equal(gone[n][~of_row], full[n][~of_row]) and torch.equal(some[n][~of_row], full[n][~of_row])
+    # a gate that counts shows what its row holds
+    assert bool(call(gate_up.masked_fill(of_row[:, None], NAN), w)["d_topk_w"][zero].isnan().all())
