@@ -475,52 +475,54 @@ dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, cons
 
 /* ---- whole batches of tokens: the experts, their combination, the loss --------------------------------------------------
  * The other half of a training or scoring pass over a batch: the experts' products for rows sorted by expert (what
- * moe_route_tokens returns in offsets / perm), the weighted sum of a token's experts, the cross entropy of hidden rows against
- * the vocabulary, and the gradients of all of them -- from a loss back to the d_topk_w that moe_route_tokens_backward takes.
- * Conventions of the section above hold (any number of rows, same results on every run, no device memory but the caller's,
- * capturable, the context's GPU need not be current); calls use no scratch of the context, so graphs of one context may
- * overlap.  The products run on the 5th-generation tensor cores: operands bf16, accumulators fp32, every output rounded once
- * (fp32: not at all).  The tensor cores' additions truncate: up to 4096 terms of one sign may come out 1e-5 of their sum short
- * (random signs: 4e-6 of the root mean square).  Longer contractions are summed in sections of 4096 terms -- where the result is
- * rounded to bf16, of 32768, 2e-4 short -- which are added up rounded to nearest, so that no more is lost however long they are.
- * Every matrix has a 16-byte aligned address, a row pitch (in elements) and sizes that are multiples of 8; n_groups <= 256, otherwise any size up to 2^35 elements from a matrix's first row to its last.  (DX_ERR_UNSUPPORTED
- * beyond.)  Outputs must not overlap inputs or one another; of a matrix counts everything between its first and its last element,
- * what lies between its rows too (DX_ERR_INVALID_ARG).
+ * moe_route_tokens returns in offsets / perm), the weighted sum of a token's experts, the cross entropy of hidden rows
+ * against the vocabulary, and the gradients of all of them -- from a loss back to the d_topk_w that moe_route_tokens_backward
+ * takes. Conventions of the section above hold (any number of rows, same results on every run, no device memory but the
+ * caller's, capturable, the context's GPU need not be current); calls use no scratch of the context, so graphs of one context
+ * may overlap.  The products run on the 5th-generation tensor cores: operands bf16, accumulators fp32, every output rounded
+ * once (fp32: not at all).  The tensor cores' additions truncate: up to 4096 terms of one sign may come out 1e-5 of their sum
+ * short (random signs: 4e-6 of the root mean square).  Longer contractions are summed in sections of 4096 terms -- where the
+ * result is rounded to bf16, of 32768, 2e-4 short -- which are added up rounded to nearest, so that no more is lost however
+ * long they are. Every matrix has a 16-byte aligned address, a row pitch (in elements) and sizes that are multiples of 8;
+ * n_groups <= 256, otherwise any size up to 2^35 elements from a matrix's first row to its last.  (DX_ERR_UNSUPPORTED
+ * beyond.)  Outputs must not overlap inputs or one another, nor the workspace anything; matrices that do are refused
+ * (DX_ERR_INVALID_ARG; of a matrix counts everything between its first and its last element, what lies between its rows too).
  *
- * Groups.  Sorted row r belongs to group e iff offsets[e] <= r < offsets[e+1] (offsets [n_groups+1], ascending, within
- * 0 .. n_rows; values outside are cut off and reported as DX_DEV_BAD_OFFSETS).  Groups may be empty; rows outside every group
- * are neither computed nor written.  gather [n_rows] / gather_div: sorted row r takes row gather[r] / gather_div of its
- * matrix (a token's row, from the pair perm[r] = token * k + choice; NULL: row r); scatter [n_rows]: the output of sorted row r is
- * written to row scatter[r] (NULL: r; no row twice).  An index outside its matrix reads zeros / writes nothing and is reported as
- * DX_DEV_BAD_ROW.  Rows of other groups never matter, whatever they hold.
+ * Groups.  Sorted row r belongs to group e iff offsets[e] <= r < offsets[e+1] (offsets [n_groups+1], ascending, within 0 ..
+ * n_rows; values outside are cut off and reported as DX_DEV_BAD_OFFSETS).  Groups may be empty; rows outside every group are
+ * neither computed nor written.  gather [n_rows] / gather_div: sorted row r takes row gather[r] / gather_div of its matrix (a
+ * token's row, from the pair perm[r] = token * k + choice; NULL: row r); scatter [n_rows]: the output of sorted row r is
+ * written to row scatter[r] (NULL: r; no row twice).  An index outside its matrix reads zeros / writes nothing and is
+ * reported as DX_DEV_BAD_ROW.  Rows of other groups never matter, whatever they hold.
  *
- * moe_grouped_mm: y[scatter(r)] = W_e x[gather(r)], or W_e^T x (transposed = 1), W_e [n, k] row-major.  y_dtype DX_DTYPE_BF16 /
- *   DX_DTYPE_FP32.  One group is a plain product.
- * moe_grouped_mm_dw: dW_e [n, k] = sum over the group's rows of dy[gather_dy(r)] x[gather_x(r)]^T: the gradient of W_e.  Written
- *   whole, zeros for an empty group.  dw_dtype as above; ld_w / stride_w of the description are dW's.
+ * moe_grouped_mm: y[scatter(r)] = W_e x[gather(r)], or W_e^T x (transposed = 1), W_e [n, k] row-major.  y_dtype DX_DTYPE_BF16
+ *   / DX_DTYPE_FP32.  One group is a plain product.
+ * moe_grouped_mm_dw: dW_e [n, k] = sum over the group's rows of dy[gather_dy(r)] x[gather_x(r)]^T: the gradient of W_e.
+ *   Written whole, zeros for an empty group.  dw_dtype as above; ld_w / stride_w of the description are dW's.
  * moe_grouped_swiglu: W_e [n = 2 I, k = H], I gate rows, then I up rows: act[r] = silu(g) * u with (g, u) = W_e x[gather(r)],
- *   from the fp32 products, [n_rows, I] bf16; gate_up [n_rows, 2 I] bf16 receives g and u for the backward pass (may be NULL).
+ *   from the fp32 products, [n_rows, I] bf16; gate_up [n_rows, 2 I] bf16 receives g and u for the backward pass (may be
+ *   NULL).
  * moe_grouped_swiglu_backward: through the down product of each row and the SwiGLU in front of it.  W_e [n = H, k = I] is the
- *   down matrix, dy the gradient of the tokens' sums; sorted row r is pair q = gather[r] (NULL: r), its dy row q / gather_div, its
- *   weight pair_w[q] (NULL: 1).  With a = W_e^T dy, s = sigmoid(g):  d_gate_up[r] = (w a u s (1 + g (1 - s)), w a g s),
- *   act_w[r] = w silu(g) u -- with moe_grouped_mm_dw the gradient of W_e: sum of dy act_w^T -- and
- *   d_pair_w[q] = <a, silu(g) u> (may be NULL; pairs that no row stands for are not written, a pair that several rows stand for gets
- *   what one of them gives: a permutation has neither).  A pair of weight 0 is taken out and its row may hold anything: d_gate_up and
- *   act_w are 0 there, d_pair_w is 0 where the row makes no finite number of it.  workspace: moe_grouped_swiglu_backward_workspace bytes (0 without d_pair_w), 16-byte aligned.
- * moe_combine_tokens: y[t] = sum_j w[t, j] z[t k + j], rows fp32 or bf16 (each of z, y), k <= 8, sums in fp32; w NULL: all 1.  A
- *   weight of 0 takes its row out (it is not read, and may hold anything).  moe_combine_tokens_backward: dz[t k + j] = w[t, j] dy[t]
- *   (0 where the weight is 0) and dw[t, j] = <z[t k + j], dy[t]> (where the weight is 0 and that is no finite number: 0); either may
- *   be NULL; all rows of one type.
+ *   down matrix, dy the gradient of the tokens' sums; sorted row r is pair q = gather[r] (NULL: r), its dy row q /
+ *   gather_div, its weight pair_w[q] (NULL: 1).  With a = W_e^T dy, s = sigmoid(g):  d_gate_up[r] = (w a u s (1 + g (1 - s)),
+ *   w a g s), act_w[r] = w silu(g) u -- with moe_grouped_mm_dw the gradient of W_e: sum of dy act_w^T -- and d_pair_w[q] =
+ *   <a, silu(g) u> (may be NULL; pairs that no row stands for are not written, a pair that several rows stand for gets what
+ *   one of them gives: a permutation has neither).  A pair of weight 0 is taken out and its row may hold anything: d_gate_up
+ *   and act_w are 0 there, d_pair_w is 0 where the row makes no finite number of it.  workspace:
+ *   moe_grouped_swiglu_backward_workspace bytes (0 without d_pair_w), 16-byte aligned.
+ * moe_combine_tokens: y[t] = sum_j w[t, j] z[t k + j], rows fp32 or bf16 (each of z, y), k <= 8, sums in fp32; w NULL: all 1.
+ *   A weight of 0 takes its row out (it is not read, and may hold anything).  moe_combine_tokens_backward: dz[t k + j] = w[t,
+ *   j] dy[t] (0 where the weight is 0) and dw[t, j] = <z[t k + j], dy[t]> (where the weight is 0 and that is no finite
+ *   number: 0); either may be NULL; all rows of one type.
  *
  * spec_head_loss: for rows h [N, H] bf16 and a head W [V, H] bf16, with z = W h[t]:  loss[t] = log sum_v exp(z_v) - z_target,
- *   dh [N, H] = row_weight[t] * dloss/dh and dW [V, H] = sum_t row_weight[t] * dloss/dW, bf16 (each may be NULL, not all three).
- *   targets [N]: -1 (no token) and rows of weight 0 (whatever their target) have loss 0 and no part in the gradients, whatever h
- *   holds (they are left out: a padded batch costs its real rows); another id outside [0, V) gives loss NaN, no gradient,
- *   DX_DEV_BAD_TOKEN.  The
- *   gradients work through the vocabulary piece by piece, a piece's dz in bf16 (each element rounded once), from logits kept in
- *   fp32 (N V of them, where that pays and the workspace has room) or computed a second time; dz is the same either way.  Any V.
- *   workspace (256-byte aligned): spec_head_loss_workspace says how many bytes are needed at least, and how many are of use;
- *   anything between works. */
+ *   dh [N, H] = row_weight[t] * dloss/dh and dW [V, H] = sum_t row_weight[t] * dloss/dW, bf16 (each may be NULL, not all
+ *   three). targets [N]: -1 (no token) and rows of weight 0 (whatever their target) have loss 0 and no part in the gradients,
+ *   whatever h holds (they are left out: a padded batch costs its real rows); another id outside [0, V) gives loss NaN, no
+ *   gradient, DX_DEV_BAD_TOKEN.  The gradients work through the vocabulary piece by piece, a piece's dz in bf16 (each element
+ *   rounded once), from logits kept in fp32 (N V of them, where that pays and the workspace has room) or computed a second
+ *   time; dz is the same either way.  Any V. workspace (256-byte aligned): spec_head_loss_workspace says how many bytes are
+ *   needed at least, and how many are of use; anything between works. */
 typedef struct {
   int32_t n_groups;      /* E, 1 .. 256 */
   int32_t n_rows;        /* sorted rows */

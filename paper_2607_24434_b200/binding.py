@@ -984,7 +984,8 @@ def moe_grouped_swiglu_backward(ctx: Context, dy: torch.Tensor, w_down: torch.Te
     ``d_gate_up`` [rows, 2 I], ``act_w`` [rows, I] (the weighted SwiGLU outputs, the other factor of w_down's gradient) and, with
     ``topk_w`` (any shape, indexed by pair = gather[r]), ``d_topk_w`` in its shape (pairs without a row keep what ``out`` held, or
     0).  Sorted row r takes row pair // gather_div of ``dy``; without ``gather`` it is pair r.  The row of a
-    pair of weight 0 may hold anything: zeros in ``d_gate_up`` and ``act_w``, and in ``d_topk_w`` where it makes no finite number."""
+    pair of weight 0 may hold anything: zeros in ``d_gate_up`` and ``act_w``, and in ``d_topk_w`` where it makes no finite
+    number."""
     _index(ctx, gather, "gather")
     rows = dy.shape[0] * gather_div if gather is None else gather.shape[0]
     d = _groups(ctx, w_down, "w_down", rows)
@@ -1066,8 +1067,8 @@ def moe_combine_tokens_backward(ctx: Context, dy: torch.Tensor, z: Optional[torc
                                 top_k: Optional[int] = None, out: Optional[Dict[str, torch.Tensor]] = None
                                 ) -> Dict[str, torch.Tensor]:
     """Gradients of ``moe_combine_tokens``: ``dz`` [N * k, H] = topk_w dy and, with ``topk_w``, ``d_topk_w`` [N, k] = <z, dy> (z
-    and dy of one type; z is not needed without ``d_topk_w``).  The row of a weight of 0 may hold anything: where that makes no finite
-    number of its ``d_topk_w``, 0."""
+    and dy of one type; z is not needed without ``d_topk_w``).  The row of a weight of 0 may hold anything: where that makes no
+    finite number of its ``d_topk_w``, 0."""
     dt, ld_dy = _matrix(ctx, dy, "dy")
     N, H = dy.shape
     k = topk_w.shape[1] if topk_w is not None and topk_w.dim() == 2 else top_k

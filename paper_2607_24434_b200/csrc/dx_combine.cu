@@ -1,8 +1,9 @@
 // The weighted sum of a token's experts and its gradient (moe_combine_tokens, moe_combine_tokens_backward):
 //     y[t] = sum_j w[t, j] z[t k + j];      dz[t k + j] = w[t, j] dy[t],   dw[t, j] = <z[t k + j], dy[t]>
-// Rows of k neighbours in fp32 or bf16, sums in fp32 in the order of j, rounded once.  Bound by the rows' bytes: every
-// element is touched once, in 16-byte vectors, the k rows of a token by the same threads with all loads in flight.  16384 tokens x 6
-// x 2048 bf16: 75 us, 97 % of the copy rate; the gradient of 4999 x 4 x 1000 fp32, of which nearly half is written: 38 us, 73 %.
+// Rows of k neighbours in fp32 or bf16, sums in fp32 in the order of j, rounded once.  Bound by the rows' bytes: every element is
+// touched once, in 16-byte vectors, the k rows of a token by the same threads with all loads in flight.  16384 tokens x 6 x 2048
+// bf16: 73 to 75 us, 97 to 100 % of the copy rate.  The gradient of 4999 x 4 x 1000 fp32, of which nearly half is written: 36.5
+// to 37.2 us, 76 % (with the loads of each row behind its own weight's test, 41.8).
 #include <type_traits>
 
 #include "dx_internal.cuh"
@@ -146,8 +147,8 @@ cudaError_t combine(bool pdl, const void* z, int64_t ldz, const float* w, int n,
                        reinterpret_cast<const Tz*>(z), ldz, w, n, pieces, reinterpret_cast<Ty*>(y), ldy);
 }
 template <class T, int K>
-cudaError_t combine_grad(bool pdl, const void* dy, const void* z, int64_t ld_dy, int64_t ldz, const float* w, int n, int H, void* dz,
-                         int64_t ld_dz, float* dw, cudaStream_t st) {
+cudaError_t combine_grad(bool pdl, const void* dy, const void* z, int64_t ld_dy, int64_t ldz, const float* w, int n, int H,
+                         void* dz, int64_t ld_dz, float* dw, cudaStream_t st) {
   const int pieces = H / Piece<T>::kN;
   const T *d = reinterpret_cast<const T*>(dy), *x = reinterpret_cast<const T*>(z);
   T* o = reinterpret_cast<T*>(dz);
@@ -175,8 +176,8 @@ static_assert(DX_MAX_TOPK == 8);
 
 }  // namespace
 
-cudaError_t dx_launch_combine(dx_ctx* ctx, const void* z, int fp32, int64_t ldz, const float* w, int n_tokens, int k, int H, void* y,
-                              int y_fp32, int64_t ldy, cudaStream_t st) {
+cudaError_t dx_launch_combine(dx_ctx* ctx, const void* z, int fp32, int64_t ldz, const float* w, int n_tokens, int k, int H,
+                              void* y, int y_fp32, int64_t ldy, cudaStream_t st) {
   const bool pdl = (ctx->pdl_mask & DX_PDL_EXPERTS) != 0;
   return with_k(k, [&](auto K) {
     if (fp32)
@@ -187,8 +188,9 @@ cudaError_t dx_launch_combine(dx_ctx* ctx, const void* z, int fp32, int64_t ldz,
   });
 }
 
-cudaError_t dx_launch_combine_grad(dx_ctx* ctx, const void* dy, const void* z, int fp32, int64_t ld_dy, int64_t ldz, const float* w,
-                                   int n_tokens, int k, int H, void* dz, int64_t ld_dz, float* dw, cudaStream_t st) {
+cudaError_t dx_launch_combine_grad(dx_ctx* ctx, const void* dy, const void* z, int fp32, int64_t ld_dy, int64_t ldz,
+                                   const float* w, int n_tokens, int k, int H, void* dz, int64_t ld_dz, float* dw,
+                                   cudaStream_t st) {
   const bool pdl = (ctx->pdl_mask & DX_PDL_EXPERTS) != 0;
   return with_k(k, [&](auto K) {
     return fp32 ? combine_grad<float, K.value>(pdl, dy, z, ld_dy, ldz, w, n_tokens, H, dz, ld_dz, dw, st)

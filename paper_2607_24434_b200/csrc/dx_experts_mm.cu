@@ -6,12 +6,13 @@
 // are the fixed 128 lanes of a CTA, and the ragged number of an expert's rows is the width of the products, which
 // tcgen05.mma takes in steps of 16 -- a group of 5 rows costs 16 columns, not 128.
 //
-// Bounds and measurements, 64 experts of which a token takes six, H = 2048, I = 1408.  One token: the weights' bytes (34.6 MB; 5.4 us
-// at the copy rate) behind a chain of launch, offsets and first stage: 11.3 us, SwiGLU (69 MB) 15.8.  700 tokens, SwiGLU gradient:
-// 370 MB of weights, 97 us.  16384 tokens: the products (669 us at the burst rate) under the power cap, as a dense product of their
-// size: 914 to 1011 us, SwiGLU that keeps its products 1010 to 1083.  Weight gradients: of many rows the products and 1.5 GB of fp32
-// results through the same path out of the SM (8192 tokens 611 to 665 us, 335 by the products alone), of few the results (64 rows per
-// group 5.0 TB/s in fp32, 5.2 in bf16; a plain fill writes 3.9).
+// Bounds and measurements, 64 experts of which a token takes six, H = 2048, I = 1408, calls one after the other.  One token:
+// the weights' bytes (34.6 MB, 5.4 us at the copy rate) fetched by 96 CTAs of 148 SMs behind a chain of launch, offsets and
+// first stage: 12.2 us; SwiGLU (69 MB, 132 CTAs) 16.5.  700 tokens, SwiGLU gradient: 370 MB of weights, 98 us with the gates'
+// sums.  16384 tokens: the products (669 us at the burst rate, 813 at the sustained one) under the power cap, W^T x 940 to 1015
+// us, SwiGLU that keeps its products 993 to 1052.  Weight gradients of many rows: 1.5 GB of fp32 results, gathered rows and
+// operands through the SMs' path to L2, which is 74 % busy, the tensor pipe 45 % (8192 tokens 619 to 676 us, 335 by the
+// products alone); of few rows the results (64 rows per group 4.9 TB/s in fp32, 4.7 in bf16).
 #include <limits.h>
 
 #include "dx_mm.cuh"
@@ -67,8 +68,9 @@ __device__ __forceinline__ int sorted_row(const MmTile& t, int c0, int lane) {
 }
 template <int COLS>
 struct FragmentEpilogue {
-  // Warps that gather: as many as the ring has stages, six, where 96 registers do (20 warps; SwiGLU of 98304 gathered rows 902 us
-  // with four of them, 856 with six, the weight gradient of 49152 in fp32 663 and 564), four where 128 are needed.
+  // Warps that gather: as many as the ring has stages, six, where 96 registers do (20 warps; of 98304 gathered rows SwiGLU that
+  // keeps its products 922 us with four of them, 897 with six; of 49152 the weight gradient in fp32 591 and 567, in bf16 477 and
+  // 454, W x 451 and 435: in turns, in bursts of 80 ms), four where 128 are needed.
   static constexpr int kCols = COLS, kRound = 1, kGathering = 4;
   static constexpr bool kBefore = true;
   using Values = Fragments<COLS>;
@@ -171,7 +173,8 @@ struct StoreRows : FragmentEpilogue<store_cols<T, ADD>()> {
   int next;      // where column `lane` of the next chunk goes (looked up a chunk ahead)
   __device__ __forceinline__ void look_up(const MmTile& t, int c0) {
     const int row = this->lane < Base::kCols ? sorted_row(t, c0, this->lane) : -1;
-    next = row >= 0 && this->p.scatter && DX_BOUNDS(row < this->p.n_rows, this->p.dev_status) ? __ldg(this->p.scatter + row) : row;
+    const bool look = row >= 0 && this->p.scatter && DX_BOUNDS(row < this->p.n_rows, this->p.dev_status);
+    next = look ? __ldg(this->p.scatter + row) : row;
   }
   __device__ __forceinline__ void begin(const MmTile& t, int, int c0, const MmTile&, bool) { look_up(t, c0); }
   template <class Taken>
@@ -298,11 +301,14 @@ struct StoreSwiglu : FragmentEpilogue<32> {
 };
 
 // D = W_down^T dy = the gradient of an unweighted act.  With q the row's pair, w its weight, s = sigmoid(gate):
-//   d gate = w D up s (1 + gate (1 - s)),  d up = w D gate s,  act_w = w gate s up,  share of d w = sum over lanes of D gate s up.
+//   d gate = w D up s (1 + gate (1 - s)),  d up = w D gate s,  act_w = w gate s up,
+//   share of d w = sum over lanes of D gate s up.
 // The rows of a pair of weight 0 get zeros, whatever they hold.  gate and up come as boxes, a chunk ahead; their place in the
 // staging takes the gradients, which go out as boxes.  (In pieces through registers, every element crossed the load/store path
-// six times, and that path, shared with the gathering warps, was the bound: 430 us, 49152 rows x 2048 x 1408, now 347.  What bounds
-// it now is the storing warps' arithmetic, some 40 instructions for 32 elements beside their way in and out.)
+// six times: 458 us, 49152 rows x 2048 x 1408, where boxes took 423 in the same run; 396 to 419 now.)  Nothing is at its limit
+// there -- an instruction in 38 % of the cycles, tensor pipe 47 %, DRAM 50 %, path to L2 40 %: what bounds it is the chain of
+// each chunk -- its products' way out of tensor memory, exponential and reciprocal, stores, fence, box -- with two storing
+// warps per scheduler and no registers to have two chunks under way.
 struct StoreSwigluGrad : FragmentEpilogue<16> {
   static constexpr bool kBefore = false;      // (no registers for two chunks: this one is waited for where it is needed)
   // of a column 64 bytes of gate, then 64 of up; behind the sixteen columns act_w; two chunks; the weights of 128 columns
@@ -396,8 +402,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
       fetch(turn, t, lane0, c0);
     }
     ask_next(t, lane0, c0);
-    // (a wait that runs out raises the abort flag, which ends the loop over the tiles.  No barrier is armed again while its box may
-    // still be landing, so this warp asks for none from here on.)
+    // (a wait that runs out raises the abort flag, which ends the loop over the tiles.  No barrier is armed again while its box
+    // may still be landing, so this warp asks for none from here on.)
     if (!mm_store_wait(own.bar + (turn & 1u) * 8u, (turn >> 1) & 1u, own.abort_flag, own.limit, lane)) {
       gone = true;
       arrived(x);
@@ -467,7 +473,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
           *reinterpret_cast<uint4*>(to + p.lanes) = u1;
         }
       }
-      flush_bf16<16>(p, lane, buf + 2 * kArea, sorted_row(t, c0, lane), lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w), p.ld_act);
+      flush_bf16<16>(p, lane, buf + 2 * kArea, sorted_row(t, c0, lane), lane0, reinterpret_cast<__nv_bfloat16*>(p.act_w),
+                     p.ld_act);
       written();            // (boxes of the chunk after the next come here)
     }
     if (p.partial) {
@@ -494,8 +501,8 @@ struct StoreSwigluGrad : FragmentEpilogue<16> {
   }
 };
 
-// d pair_w[q] = sum of the shares, in order.  The row of a pair of weight 0 was taken out and may hold anything: where that makes no
-// finite number, 0.
+// d pair_w[q] = sum of the shares, in order.  The row of a pair of weight 0 was taken out and may hold anything: where that makes
+// no finite number, 0.
 __global__ void __launch_bounds__(256) dx_pair_weight_grad_kernel(const float* partial, int parts, int n_rows,
                                                                   const int32_t* offsets, int n_groups,
                                                                   const int32_t* index, const float* pair_w, int n_pairs,
@@ -592,11 +599,12 @@ namespace {
 
 // Few rows per group: the weights' bytes are the time, so tiles are small (128 lanes: twice as many CTAs have one, and eight
 // stages of 24 KB keep 128 KB of weights in flight per SM).  That pays up to 32 rows where the matrices' rows are the contraction
-// (64 groups of 24 rows x 2048 x 1408: 66.3 us, in pairs 71.8; its SwiGLU gradient 76.9, in pairs 85.0), otherwise for a handful
-// (one row: SwiGLU 84 us, in pairs 86; 24 rows 133, in pairs 130).  Some rows, and matrices whose rows are the contraction: 128
-// lanes with 128 columns (64 rows 67.5 us, in pairs 73.7; SwiGLU gradient 92, in pairs 98; 128 rows 88 and 135, in pairs 80 and
-// 119.  The other forms lose with it at 40 rows already: SwiGLU 137 us, in pairs 133).  Otherwise pairs of CTAs with 256 lanes x
-// 256 columns.
+// (64 groups of 24 rows x 2048 x 1408: 61.8 us, in pairs 67.8; its SwiGLU gradient 77.5, in pairs 86.4), otherwise for a handful
+// (SwiGLU of one row 116.5 us, in pairs 117.7, of eight 118.3 and 119.6, of 40 123.4 and 123.0; W x of 24 64.2 and 63.3).  Some
+// rows, and matrices whose rows are the contraction: 128 lanes with 128 columns (96 rows 67 us, in pairs 73; SwiGLU gradient 95,
+// in pairs 103.  128 rows in every group 71 and 76, but 128 in the mean, as routing deals them out, 82 and 78, its SwiGLU
+// gradient 123 and 115: groups of 129 rows take two tiles.  The other forms lose with it at 40 rows already: SwiGLU 137 us, in
+// pairs 133).  Otherwise pairs of CTAs with 256 lanes x 256 columns.
 template <int FORM, bool GATHER, class Epilogue>
 cudaError_t launch_rows(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, cudaStream_t st) {
   const bool few = p.n_rows <= (FORM == kRowsT ? kFewRows : kFewestRows) * (int64_t)p.n_groups;
@@ -630,7 +638,8 @@ bool rows_source(MmMaps* m, MmParams* p, const DxGroupedMm& a, int cols) {
     rows = (int64_t)((a.w_rows + kPanel - 1) / kPanel) * a.group_rows;
     cols = kPanel;
   }
-  return a.gather || a.gather_div > 1 || (dx_matrix_map(&m->b, a.x, rows, cols, a.ldx, 128) && dx_matrix_map(&m->b_few, a.x, rows, cols, a.ldx, 32));
+  return a.gather || a.gather_div > 1 ||
+         (dx_matrix_map(&m->b, a.x, rows, cols, a.ldx, 128) && dx_matrix_map(&m->b_few, a.x, rows, cols, a.ldx, 32));
 }
 
 MmParams base_params(const dx_ctx* ctx, const int32_t* offsets, int groups, int rows) {
@@ -716,8 +725,6 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   p.kdim = a.n;
   p.out = a.y;
   p.ld = a.ldy;
-  p.gate_up = gate_up;
-  p.ld_gate_up = ld_gate_up;
   p.pair_w = pair_w;
   p.n_pairs = n_pairs;
   p.act_w = act_w;
@@ -737,8 +744,8 @@ cudaError_t dx_launch_grouped_swiglu_grad(dx_ctx* ctx, const DxGroupedMm& a, con
   // (lanes of a tile behind the last are no shares: only warps with lanes that exist wrote theirs)
   const int parts = (a.k + 31) / 32;
   *n_launches = 2;
-  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, dx_pair_weight_grad_kernel, dim3((a.n_rows + 255) / 256), dim3(256), 0,
-                       st, 1, partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather, pair_w, n_pairs, d_pair_w,
+  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, dx_pair_weight_grad_kernel, dim3((a.n_rows + 255) / 256),
+                       dim3(256), 0, st, 1, partial, parts, a.n_rows, a.offsets, a.n_groups, a.gather, pair_w, n_pairs, d_pair_w,
                        ctx->dev_status);
 }
 
@@ -759,7 +766,6 @@ cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t
   p.b_div = mm_div(a.dy_div);
   p.out = a.dw;
   p.ld = a.ld_dw;
-  p.group_stride = a.dw_stride;
   if (a.dw_fp32) p.section = kSectionFp32;
   if (a.dy_panels) p.b_panel = a.dy_rows;
   if (!dx_matrix_map(&m.a, a.x, a.x_rows, a.k, a.ldx, 64) ||
@@ -770,9 +776,10 @@ cudaError_t dx_launch_grouped_dw(dx_ctx* ctx, const DxGroupedDw& a, cudaStream_t
   const uint64_t strides[2] = {(uint64_t)a.ld_dw, (uint64_t)a.dw_stride};
   const uint32_t box[3] = {32, a.dw_fp32 ? 16u : 32u, 1};
   if (!dx_box_map(&m.out[0], a.dw, a.dw_fp32, 3, dims, strides, box)) return cudaErrorInvalidValue;
-  // Few rows per group, and one, three or five times 128 lanes: pairs would spend a sixth or more of their tiles on lanes that do not
-  // exist, so CTAs work by themselves (130 groups of five rows, 1000 x 520 bf16: 46 us, in pairs 52; 256 of two, 640 x 384 fp32: 57,
-  // in pairs 65.  Where pairs have no such lanes they are faster: 64 of five, 1408 x 2048 bf16 89 us, by themselves 105).
+  // Few rows per group, and one, three or five times 128 lanes: pairs would spend a sixth or more of their tiles on lanes that
+  // do not exist, so CTAs work by themselves (130 groups of five rows, 1000 x 520 bf16: 45 us, in pairs 52; 256 of two, 640 x
+  // 384 fp32: 55, in pairs 64.  Where pairs have no such lanes they are faster: 64 of five, 1408 x 2048 bf16 86 us, by
+  // themselves 105).
   const int blocks = (a.k + 127) / 128;
   if (a.n_rows <= 64 * (int64_t)a.n_groups && blocks % 2 && blocks <= 5) {
     const long long tiles = (long long)a.n_groups * blocks * ((a.n + 255) / 256);

@@ -7,17 +7,22 @@
 //   2. products of the listed rows with the whole vocabulary; of every tile a row keeps (maximum, sum of exponentials) and,
 //      where the tile holds it, the target's logit
 //   3. the tiles' pairs are joined: loss, log of the sum
-//   4. (gradients) for each piece of the vocabulary dz, rounded to bf16 once, from kept logits or from the products once more, then
-//      dh += dz W and dW = dz^T h as products of the kernel of the grouped experts with one group
+//   4. (gradients) for each piece of the vocabulary dz, from kept logits or from the products once more, then dh += dz W and
+//      dW = dz^T h as products of the kernel of the grouped experts with one group
+// dz is rounded to bf16 once: it is the tensor cores' operand, and carried in two parts (a bf16 value and what it leaves) both
+// gradients' products would double, 2.2 of the 3.6 ms of 4096 rows.  The rounding is what dh and dW are off by beside their own:
+// 1.9e-3 to 2.6e-3 of their rms against 64 bits where the output's rounding alone is 1.7e-3.
 // A second pass over the products costs 2 N V H operations beside the 6 N V H of loss and gradients; what it saves is N V logits
 // in fp32 (they cannot be kept in bf16: a logit of 20 would be off by 0.06, its probability by 6 %), which cross to memory and
 // back at some 5.5 TB/s.  So long hidden rows keep them where there is room (4096 rows, 102400 words, H = 2048: all gradients
-// 4.30 ms, recomputed 5.11; 32768 words: H = 2048 1.40 ms, recomputed 1.61, H = 1024 0.87, recomputed 0.81).  For few rows
-// -- a verified block -- the logits are little and the head's bytes are the time: there they are always kept, and the vocabulary is dealt out to blocks whose shares of dh different SMs sum, in fp32, added up in order afterwards (dh alone has no
-// more tiles than H / 128: 16 of 148 SMs at H = 2048).
+// 4.11 ms, recomputed 4.73; 32768 words: H = 2048 1.30 ms, recomputed 1.47, H = 1024 0.87, recomputed 0.81; 256 rows, 102400
+// words, H = 4096: 0.64, recomputed 0.81).  For few rows -- a verified block -- the logits are little and the head's bytes are
+// the time: there they are always kept, and the vocabulary is dealt out to blocks whose shares of dh different SMs sum, in fp32,
+// added up in order afterwards (dh alone has no more tiles than H / 128: 16 of 148 SMs at H = 2048).
 //
-// 16 rows x 102400 words x 2048: 144 us with dh, of which the head's two ways from memory are 130; the loss alone 78 (65).  4096 rows
-// (a quarter of them padding) with both gradients 3.64 ms, the three products 2.8 at the rate that the power cap allows.
+// 16 rows x 102400 words x 2048: 147 to 159 us with dh, of which the head's two ways from memory are 130; the loss alone 76 (65).
+// 4096 rows (a quarter of them padding) with both gradients 3.60 to 3.73 ms, the three products 2.8 at the rate that the power
+// cap allows; 4096 rows, loss alone 1.10 ms.
 #include "dx_mm.cuh"
 
 namespace {
@@ -114,8 +119,8 @@ __global__ void __launch_bounds__(256) dx_head_pack_kernel(const __nv_bfloat16* 
 
 // 32 bytes of a row per store: a thread has a row of its own, and less than a sector would be written twice
 __device__ __forceinline__ void store_sector(void* at, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-               "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 __device__ __forceinline__ void store32(float* at, const float (&v)[32], int n) {   // (n: whole sectors of them)
 #pragma unroll
@@ -137,7 +142,7 @@ __device__ __forceinline__ void store32(__nv_bfloat16* at, const float (&v)[32])
   }
 }
 
-// ---- 2: (maximum, sum) of a half of a tile's columns (every other 32), a row per thread ---------------------------------------------------------
+// ---- 2: (maximum, sum) of a half of a tile's columns (every other 32), a row per thread ----------------------------------
 template <bool KEEP>
 struct RowSums {
   const MmParams& p;
@@ -149,7 +154,8 @@ struct RowSums {
   struct Values {
     float v[32];
   };
-  __device__ RowSums(const MmParams& p_, const MmMaps&, int lane_, int share_, uint32_t, MmFetch) : p(p_), lane(lane_), share(share_) {}
+  __device__ RowSums(const MmParams& p_, const MmMaps&, int lane_, int share_, uint32_t, MmFetch)
+      : p(p_), lane(lane_), share(share_) {}
   __device__ __forceinline__ void finish() {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
@@ -165,7 +171,8 @@ struct RowSums {
     taken();
     float(&v)[32] = x.v;
     const int left = t.ncols - c0;
-    if (KEEP && row >= 0 && DX_BOUNDS(t.n0 + c0 + (left < 32 ? (left + 7) / 8 * 8 : 32) <= p.ld_logits, p.dev_status)) store32(p.logits + (int64_t)row * p.ld_logits + t.n0 + c0, v, left);
+    if (KEEP && row >= 0 && DX_BOUNDS(t.n0 + c0 + (left < 32 ? (left + 7) / 8 * 8 : 32) <= p.ld_logits, p.dev_status))
+      store32(p.logits + (int64_t)row * p.ld_logits + t.n0 + c0, v, left);
     if (left < 32) {
 #pragma unroll
       for (int c = 0; c < 32; ++c)
@@ -261,11 +268,13 @@ struct StoreDz {
   int row, target;
   float lse, weight, at_target;
   static constexpr bool kBefore = false;
-  static constexpr int kStaging = 0, kCols = 32, kGathering = 0, kRound = 64;   // (the products of the gradients read whole blocks of 64)
+  static constexpr int kStaging = 0, kCols = 32, kGathering = 0;
+  static constexpr int kRound = 64;      // (the products of the gradients read whole blocks of 64)
   struct Values {
     float v[32];
   };
-  __device__ StoreDz(const MmParams& p_, const MmMaps&, int lane_, int share_, uint32_t, MmFetch) : p(p_), lane(lane_), share(share_) {}
+  __device__ StoreDz(const MmParams& p_, const MmMaps&, int lane_, int share_, uint32_t, MmFetch)
+      : p(p_), lane(lane_), share(share_) {}
   __device__ __forceinline__ void finish() {}
   __device__ __forceinline__ void load(uint32_t taddr, Values& x) { mm_ld32(taddr, x.v); }
   __device__ __forceinline__ void zero(Values&) {}
@@ -320,8 +329,9 @@ __device__ __forceinline__ uint4 dz_of(const float* logits, float weight, float 
   return make_uint4(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]), bf16_pair(z[4], z[5]), bf16_pair(z[6], z[7]));
 }
 // words v0 .. v0 + len of all rows (blockIdx.x): dz of a piece
-__global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, int64_t ld_logits, int v0, int len, const int32_t* live,
-                                                         const int32_t* n_live, const int32_t* targets, const float* row_weight,
+__global__ void __launch_bounds__(256) dx_head_dz_kernel(const float* logits, int64_t ld_logits, int v0, int len,
+                                                         const int32_t* live, const int32_t* n_live,
+                                                         const int32_t* targets, const float* row_weight,
                                                          const float* lse, const float* row_loss, __nv_bfloat16* dz, int panel,
                                                          int32_t* dev_status) {
   dx_pdl_wait();
@@ -352,7 +362,8 @@ __global__ void __launch_bounds__(256) dx_head_row_kernel(const float* logits, i
   if (blockIdx.x == 0 && dh) {          // (of the rows as they were given)
     bool bad;
     if (!row_counts(targets, row_weight, row, V, bad))
-      for (int i = threadIdx.x; i < H / 8; i += 256) *reinterpret_cast<uint4*>(dh + row * ld_dh + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
+      for (int i = threadIdx.x; i < H / 8; i += 256)
+        *reinterpret_cast<uint4*>(dh + row * ld_dh + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
   }
   if (row >= __ldg(n_live) || !DX_BOUNDS(row < panel && live[row] >= 0 && live[row] < panel, dev_status)) return;
   const int r = __ldg(live + row), target = __ldg(targets + r) - v0;
@@ -429,8 +440,8 @@ constexpr size_t kPieceBest = size_t(256) << 20;   // bytes of dz of a piece wit
 constexpr size_t kKeepFew = size_t(64) << 20, kKeepMost = size_t(2) << 30;
 constexpr int kKeepFrom = 1280;
 
-constexpr int kByRow = 1 << 21;                    // words up to which every CTA of a row joins its tiles (V^2 / 2^18 pairs are read)
-constexpr int kFewest = 32768;                     // rows up to which a CTA per row (and block) will do
+constexpr int kByRow = 1 << 21;      // words up to which every CTA of a row joins its tiles (V^2 / 2^18 pairs are read)
+constexpr int kFewest = 32768;       // rows up to which a CTA per row (and block) will do
 
 struct HeadPlan {
   bool by_row;               // a CTA or more for each row joins its tiles
@@ -439,7 +450,8 @@ struct HeadPlan {
   int piece;                 // words of a piece (a multiple of 256)
   int blocks;                // shares of dh that are summed apart
   size_t live, n_live, rows, part, target_logit, lse, row_loss, dh_acc, logits, share, dz, bytes;
-  int pitch, width;          // rows of a half tile's sums (where they are joined by themselves), words of a tile of the first pass
+  int pitch;                 // rows of a half tile's sums (where they are joined by themselves)
+  int width;                 // words of a tile of the first pass
   int64_t ld_logits;
 };
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -503,9 +515,9 @@ HeadPlan head_plan(int sm_count, int N, int V, int H, bool grad, size_t space) {
     piece = (words / 256 + pieces - 1) / pieces * 256;
     s.blocks = 1;
     if (!lean && N <= kFewest) {
-      // dh has few tiles where there are few rows, and rarely a multiple of what runs at a time: a piece's words are dealt out to as
-      // many blocks as fill the GPU best, their shares of dh summed apart.  Rates in words and bytes per microsecond: a pair of CTAs
-      // multiplies 256 x 256 x 64 in a third of a microsecond; few rows wait for the head's bytes instead.
+      // dh has few tiles where there are few rows, and rarely a multiple of what runs at a time: a piece's words are dealt out
+      // to as many blocks as fill the GPU best, their shares of dh summed apart.  Rates in words and bytes per microsecond: a
+      // pair of CTAs multiplies 256 x 256 x 64 in a third of a microsecond; few rows wait for the head's bytes instead.
       const bool few = N <= kSomeRows;          // (one tile of them)
       const int64_t tiles = few ? (H + 127) / 128 : ((H + 255) / 256) * (int64_t)((N + 255) / 256);
       const int64_t units = few ? sm_count : sm_count / 2;
@@ -611,7 +623,8 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
     if (!launched(dx_launch_pdl(pdl, dx_head_rows_kernel, dim3(1), dim3(1024), 0, st, 1, a.targets, a.row_weight, a.N, a.V, live,
                                 n_live, a.loss, ctx->dev_status))) return e;
     if (!launched(dx_launch_pdl(pdl, dx_head_pack_kernel, dim3((a.N + 3) / 4), dim3(256), 0, st, 1,
-                                reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, a.N, rows, ctx->dev_status))) return e;
+                                reinterpret_cast<const __nv_bfloat16*>(a.h), a.ldh, a.H, live, n_live + 1, a.N, rows,
+                                ctx->dev_status))) return e;
   }
   p.tile_width = s.width;
   if (!launched(s.keep ? launch_head<RowSums<true>>(ctx, m, p, st) : launch_head<RowSums<false>>(ctx, m, p, st))) return e;
@@ -622,17 +635,17 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
                                 s.keep ? logits : nullptr, s.ld_logits, a.V, live, n_live + 1, a.targets, a.row_weight, part,
                                 2 * s.tiles, target_logit, a.loss, lse, row_loss, dz, a.N, a.H, dh, a.ld_dh,
                                 ctx->dev_status))) return e;
-  } else if (!launched(dx_launch_pdl(pdl, dx_head_join_kernel, dim3((a.N + 31) / 32), dim3(1024), 0, st, 1, part, s.pitch, 2 * s.tiles, live,
-                              n_live + 1, target_logit, a.loss, lse, row_loss, a.targets, a.row_weight, a.N, a.V, a.H, dh,
-                              a.ld_dh, ctx->dev_status))) return e;
+  } else if (!launched(dx_launch_pdl(pdl, dx_head_join_kernel, dim3((a.N + 31) / 32), dim3(1024), 0, st, 1, part, s.pitch,
+                              2 * s.tiles, live, n_live + 1, target_logit, a.loss, lse, row_loss, a.targets, a.row_weight,
+                              a.N, a.V, a.H, dh, a.ld_dh, ctx->dev_status))) return e;
   if (!grad) return e;
 
   for (int64_t v0 = 0; v0 < a.V; v0 += s.piece) {
     const int len = (int)(a.V - v0 < s.piece ? a.V - v0 : s.piece);
     const bool first = v0 == 0, last = v0 + len == a.V;
     if (s.keep && !s.by_row) {
-      if (!launched(dx_launch_pdl(pdl, dx_head_dz_kernel, dim3(a.N, (len + 2047) / 2048), dim3(256), 0, st, 1, logits, s.ld_logits,
-                                  (int)v0, len, live, n_live + 1, a.targets, a.row_weight, lse, row_loss, dz, a.N,
+      if (!launched(dx_launch_pdl(pdl, dx_head_dz_kernel, dim3(a.N, (len + 2047) / 2048), dim3(256), 0, st, 1, logits,
+                                  s.ld_logits, (int)v0, len, live, n_live + 1, a.targets, a.row_weight, lse, row_loss, dz, a.N,
                                   ctx->dev_status))) return e;
     } else if (!s.keep) {
       MmParams q = p;
@@ -675,8 +688,8 @@ cudaError_t dx_launch_head_loss(dx_ctx* ctx, const DxHeadLoss& a, cudaStream_t s
       }
       if (!launched(dx_launch_grouped_mm(ctx, g, st))) return e;
       if (s.blocks > 1 && last) {
-        if (!launched(dx_launch_pdl(pdl, dx_head_sum_kernel, dim3((a.H + 511) / 512, a.N), dim3(128), 0, st, 1, share, s.blocks, a.N,
-                                    a.H, live, n_live + 1, dh, a.ld_dh, ctx->dev_status))) return e;
+        if (!launched(dx_launch_pdl(pdl, dx_head_sum_kernel, dim3((a.H + 511) / 512, a.N), dim3(128), 0, st, 1, share,
+                                    s.blocks, a.N, a.H, live, n_live + 1, dh, a.ld_dh, ctx->dev_status))) return e;
       }
     }
     if (a.dW) {

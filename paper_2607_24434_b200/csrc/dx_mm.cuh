@@ -17,10 +17,12 @@
 // Warps: 0-7 take finished tiles out of tensor memory (lanes 32 (w % 4) .. + 31, every other chunk of columns), 8 asks for A and
 // 10 for B (one of them where only one operand comes by tensor map), 9 owns the tensor memory and issues the products (in a pair
 // only the first CTA's), those from 12 on gather.  Two accumulators take turns, so a tile is stored while the next one is
-// multiplied.  Every wait is bounded; one that runs out raises the CTA's abort flag,
-// after which nothing more is copied or multiplied.  When all warps of the CTA have come to their ends, copies and products in
-// flight are waited for (bounded; a warp that issued its last ones may have been done long before another one gave up), tensor
-// memory is freed and DX_DEV_WAIT_EXPIRED stands in the status word.
+// multiplied; of a contraction longer than a section (below) one takes the sections and the other holds their sum.
+//
+// Every wait is bounded; one that runs out raises the CTA's abort flag, after which nothing more is copied or multiplied.  When
+// all warps of the CTA have come to their ends, copies and products in flight are waited for (bounded; a warp that issued its
+// last ones may have been done long before another one gave up), tensor memory is freed and DX_DEV_WAIT_EXPIRED stands in the
+// status word.
 #pragma once
 
 #include <cuda.h>
@@ -57,38 +59,45 @@ constexpr uint32_t kFirstCta = 0xFEFFFFFFu;
 template <int CG>
 __device__ __forceinline__ void tma2(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   if constexpr (CG == 2)
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar & kFirstCta) : "memory");
   else
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 template <int CG>
 __device__ __forceinline__ void tma3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   if constexpr (CG == 2)
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar & kFirstCta) : "memory");
   else
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 template <int CG>
 __device__ __forceinline__ void tma5(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int u, int v, uint32_t bar) {
   if constexpr (CG == 2)
-    asm volatile("cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+    asm volatile("cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar & kFirstCta) : "memory");
   else
-    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar) : "memory");
 }
 // 16 bytes, or (bytes = 0) zeros
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-// boxes of shared memory to a matrix (what lies outside it is left out), by one lane; the copies of a group are waited for together
+// boxes of shared memory to a matrix (what lies outside it is left out), by one lane; the copies of a group are waited for
+// together
 __device__ __forceinline__ void tma_store2(const CUtensorMap* map, int x, int y, uint32_t src) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
-               : "memory");
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y),
+               "r"(src) : "memory");
 }
 __device__ __forceinline__ void tma_store3(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
@@ -121,11 +130,13 @@ __host__ __device__ constexpr uint32_t mm_idesc(bool a_mn, bool b_mn, int lanes,
 template <int CG>
 __device__ __forceinline__ void mm_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   if constexpr (CG == 2)
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
                  "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
                  ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
   else
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\tsetp.ne.b32 p, %4, 0;\n\t"
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
                  ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(kDescHi) : "memory");
 }
@@ -165,9 +176,9 @@ __device__ __forceinline__ void mm_ld16(uint32_t taddr, float (&r)[16]) {
 }
 __device__ __forceinline__ void mm_st16(uint32_t taddr, const float (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"f"(r[0]), "f"(r[1]),
-      "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]),
-      "f"(r[13]), "f"(r[14]), "f"(r[15]), "r"(taddr)
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"f"(r[0]),
+      "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]),
+      "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "r"(taddr)
       : "memory");
 }
 __device__ __forceinline__ void mm_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -330,7 +341,8 @@ __device__ __forceinline__ void pair_sync() {
 __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
   for (uint32_t it = 0; it <= limit; ++it) {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     if (ok) return true;
     if ((it & 63u) == 63u && *abort_flag) return false;
@@ -348,7 +360,8 @@ __device__ __forceinline__ void arrive_at_first(uint32_t bar) {
 // A whole warp's wait: all lanes go on or none (those behind a lane that gave up would wait for it at their next exchange).
 template <bool PAIR = false>
 __device__ __forceinline__ bool mm_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
-  return __all_sync(0xffffffffu, PAIR ? pair_wait(bar, parity, abort_flag, limit) : mbar_wait(bar, parity, abort_flag, limit)) != 0;
+  const bool mine = PAIR ? pair_wait(bar, parity, abort_flag, limit) : mbar_wait(bar, parity, abort_flag, limit);
+  return __all_sync(0xffffffffu, mine) != 0;
 }
 // Wait of the warps that store finished tiles: lane 0 polls with pauses, so that their scheduler partitions stay free for
 // the copying and the multiplying warp.
@@ -374,7 +387,8 @@ struct MmMaps {
   CUtensorMap in;         // (SwiGLU gradient) gate and up
 };
 // Division of 0 <= q < 2^31 by a constant d of the launch: q factor >> shift with shift = 31 + ceil(log2 d) and
-// factor = ceil(2^shift / d) < 2^32 (exact: factor d - 2^shift < d <= 2^(shift - 31), so the error stays below 1 / d).  d = 1: factor 0.
+// factor = ceil(2^shift / d) < 2^32 (exact: factor d - 2^shift < d <= 2^(shift - 31), so the error stays below 1 / d).
+// d = 1: factor 0.
 struct MmDiv {
   uint32_t factor, shift;
 };
@@ -391,29 +405,26 @@ struct MmParams {
   int a_rows, b_rows;            // reads zeros
   int64_t a_ld, b_ld;
   const int32_t* offsets;        // [n_groups + 1]
-  const int32_t* a_index;        // sorted row -> index / a_div = row of A's matrix (null: the row itself; rows as columns: row / b_div)
-  const int32_t* b_index;
+  const int32_t* a_index;        // sorted row -> index / a_div = row of A's matrix (null: the row itself)
+  const int32_t* b_index;        // ... / b_div = row of B's (null: the row itself; rows as columns: row / b_div)
   MmDiv a_div, b_div;
   // output: element (row of column n, lane m) at out + row * ld + m
   void* out;
   int64_t ld;
-  int64_t group_stride;          // elements between the groups' outputs (products over rows)
   const int32_t* scatter;        // sorted row -> row of out (null: itself)
   int out_rows;
   const float* addend;           // fp32, added to the products, laid out like out
   // SwiGLU
   void* save;                    // [n_rows, 2 I] gate and up products
   int64_t ld_save;
-  const void* gate_up;
-  int64_t ld_gate_up;
   const float* pair_w;           // weight of pair q
   int n_pairs;
   void* act_w;
   int64_t ld_act;
   float* partial;                // [warps of lanes][n_rows] shares of the pair weights' gradients
   // Groups of *n_live rows each, group_rows apart, instead of offsets, that share out one product's contraction: kDealt blocks of
-  // kMmK rows of the one matrix in turns, from its end (which was read last) to its beginning.  The rows' elements stand in panels
-  // of kPanel columns, one below the other, group_rows rows each.
+  // kMmK rows of the one matrix in turns, from its end (which was read last) to its beginning.  The rows' elements stand in
+  // panels of kPanel columns, one below the other, group_rows rows each.
   const int32_t* n_live;         // (loss) rows that count
   int group_rows;
   int shared_out;                // blocks of kMmK rows of the matrix (0: a matrix per group)
@@ -458,8 +469,7 @@ struct __align__(16) MmShared {
   unsigned long long fetched[kMmStoring][2];   // what a storing warp reads beside the accumulators
   uint32_t tmem_base;
   int abort_flag;
-  int off[DX_MAX_E + 1];         // first row of a group, and behind it its end where the next begins elsewhere
-  int cnt[DX_MAX_E];
+  int off[DX_MAX_E], cnt[DX_MAX_E];      // a group's first row, its rows
   int before[DX_MAX_E + 1];      // row tiles in front of a group
 };
 
@@ -647,14 +657,17 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     const bool for_a = warp == kWarpA, for_b = warp == kWarpB;
     uint32_t slot = 0, phase = 0;
     bool alive = true;
-    auto shared_row = [&](int e, int kb) { return (p.shared_out - 1 - (kb / kDealt * p.n_groups + e) * kDealt - kb % kDealt) * kMmK; };
+    auto shared_row = [&](int e, int kb) {
+      return (p.shared_out - 1 - (kb / kDealt * p.n_groups + e) * kDealt - kb % kDealt) * kMmK;
+    };
     for (int t = unit; t < total && alive; t += n_units) {
       const MmTile tile = schedule.get(t).uniform_copy();
       const int half = mm_width<CG>(tile.ncols) / CG, m0 = tile.m0 + (int)rank * 128;
       const int n0 = tile.n0 + (int)rank * half;
       // rows as columns: copies of 128 rows, or of 32 where those would bring twice what is needed
       const bool big = FORM == kHead || (kHalf >= 128 && half > 64);
-      const int nb = FORM == kOuter ? (half + 63) / 64 : FORM == kHead ? kHalf / 128 : big ? (half + 127) / 128 : (half + 31) / 32;
+      const int nb = FORM == kOuter ? (half + 63) / 64
+                     : FORM == kHead ? kHalf / 128 : big ? (half + 127) / 128 : (half + 31) / 32;
       const uint32_t box = FORM == kOuter ? 8192u : big ? 16384u : 4096u;   // bytes of a copy of B
       for (int kb = 0; kb < tile.kblocks; ++kb) {
         const int k0 = kb * kMmK;
@@ -666,7 +679,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
         const uint32_t bar = smem_u32(&s->full[slot]);
         const uint32_t da = smem_u32(ring + (size_t)slot * kStage), db = da + kMmA;
         if (elect_one()) {
-          if (rank == 0) mbar_arrive_expect_tx(bar, here ? (for_a ? (FORM == kHead ? p.a_box * 128u : (uint32_t)kMmA) : nb * box) * CG : 0u);
+          const uint32_t bytes = for_a ? (FORM == kHead ? p.a_box * 128u : (uint32_t)kMmA) : nb * box;
+          if (rank == 0) mbar_arrive_expect_tx(bar, here ? bytes * CG : 0u);
           if (here && for_a) {
             if constexpr (FORM == kRows) {
               tma3<CG>(da, &maps.a, k0, m0, tile.e, bar);
@@ -714,8 +728,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
     // ----------------------------------------------------------------------------------------------- gathered rows
     // Each of the four or six warps does every fourth or sixth stage by itself: its fixed costs (waiting for the slot, for the
     // pieces to land, making them visible to the tensor core) are spread over the time of as many stages.  A stage takes a warp
-    // some 2800 clocks, most of them to issue the copies, and its products 512: with four warps they wait for it.  Eight lanes bring 128 bytes of a row,
-    // the warp four rows at a time: row 4 i + lane / 8; lane l looks up rows l, l + 32, ...
+    // some 2800 clocks, most of them to issue the copies, and its products 512: with four warps they wait for it.  Eight lanes
+    // bring 128 bytes of a row, the warp four rows at a time: row 4 i + lane / 8; lane l looks up rows l, l + 32, ...
     // (A warp asks for a slot when it has filled the one kGathering stages in front.  That one's own slot was empty then, so no
     // slot is more than one turn behind what is asked of it: its barrier's phase tells turns apart.)
     constexpr uint32_t kGathering = Epilogue::kGathering;
@@ -794,7 +808,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
               const bool in = r < tile.rows;
               resolve(p.a_index ? next_a[j] : tile.row0 + r, in, p.a_index != nullptr, p.a_div, p.a_rows, p.a_ld, at_a[j],
                       ok_a[j]);
-              resolve(p.b_index ? next_b[j] : tile.row0 + r, in, p.b_index != nullptr, p.b_div, p.b_rows, p.b_ld, at_b[j], ok_b[j]);
+              resolve(p.b_index ? next_b[j] : tile.row0 + r, in, p.b_index != nullptr, p.b_div, p.b_rows, p.b_ld, at_b[j],
+                      ok_b[j]);
             }
             ask(k0 + (int)kGathering * kMmK);
           }
@@ -946,8 +961,8 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
       if (!full()) break;
       bool alive = true;
       for (int kb = 0; LONG && tile.kblocks > p.section; kb += p.section) {
-        // A section of a long contraction: this warp's part of it is added to its part of the other accumulator.  That one is free of
-        // products: its last ones were taken out, by this warp too, before this tile, and are handed back after it.
+        // A section of a long contraction: this warp's part of it is added to its part of the other accumulator.  That one is
+        // free of products: its last ones were taken out, by this warp too, before this tile, and it is handed back after it.
         const uint32_t part = quarters + buf * kAccCols, sum = quarters + (buf ^ 1u) * kAccCols;
 #pragma unroll 1
         for (int c0 = kCols * share; c0 < end; c0 += 2 * kCols) {
@@ -1008,16 +1023,16 @@ dx_mm_kernel(const __grid_constant__ MmMaps maps, const __grid_constant__ MmPara
   __syncthreads();          // (nobody of this CTA issues anything more, or gives up)
   if (*abort_flag) {
     // Neither a copy nor a product may be on its way when the shared memory, the tensor memory and in a pair the first CTA's
-    // barriers are released.  (The other CTA of a pair waits at pair_sync.  If only that one gave up, all products of this one are
-    // done: each of its tiles was stored.)
+    // barriers are released.  (The other CTA of a pair waits at pair_sync.  If only that one gave up, all products of this one
+    // are done: each of its tiles was stored.)
     if (warp == kWarpMma && rank == 0) {
       if (elect_one()) mm_commit<CG>(smem_u32(&s->drained));      // (by the lane that issued the products)
       __syncwarp();
       for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
         if (mbar_try_wait(smem_u32(&s->drained), 0)) break;
     } else if (warp == kWarpA || (kTwo && warp == kWarpB)) {
-      // Stages that both operands were asked for complete on their barriers; for one that only one operand was asked for, or a box
-      // of a storing warp, there is nothing to wait on, so the rest is time, a thousand times what a copy takes.
+      // Stages that both operands were asked for complete on their barriers; for one that only one operand was asked for, or a
+      // box of a storing warp, there is nothing to wait on, so the rest is time, a thousand times what a copy takes.
       if (rank == 0 && warp == kWarpA) {
         const uint32_t back = issued < STAGES ? issued : STAGES;
         for (uint32_t k = 1; k <= back; ++k) {
@@ -1054,11 +1069,11 @@ cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long l
   long long units = ctx->sm_count / CG;
   if (max_tiles < units) units = max_tiles;
   if (units < 1) units = 1;
-  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, kernel, dim3((unsigned)(units * CG)), dim3(mm_threads(GATHER ? Epilogue::kGathering : 0)), smem,
-                       st, CG, maps, p);
+  return dx_launch_pdl((ctx->pdl_mask & DX_PDL_EXPERTS) != 0, kernel, dim3((unsigned)(units * CG)),
+                       dim3(mm_threads(GATHER ? Epilogue::kGathering : 0)), smem, st, CG, maps, p);
 }
-// (a kernel of its own for long contractions: the code for their sections costs the gathering forms registers, 5 % of SwiGLU of 98304
-// gathered rows)
+// A kernel of its own for long contractions: in one for both, the code for their sections cost SwiGLU of 98304 gathered rows 5 %
+// (867 -> 916 us: registers) and weight gradients of five rows per group as much (47.2 -> 49.5 us).
 template <int FORM, bool GATHER, int CG, int BN, int STAGES, class Epilogue>
 cudaError_t mm_launch(dx_ctx* ctx, const MmMaps& maps, const MmParams& p, long long max_tiles, cudaStream_t st) {
   const int most = ((FORM == kOuter ? p.n_rows : p.kdim) - 1) / kMmK + 1;      // blocks of a tile's contraction
@@ -1075,5 +1090,5 @@ bool dx_tensor_map(CUtensorMap* out, const void* base, int rank, const uint64_t*
 // Tensor map for boxes of box[0] x box[1] elements of fp32 or bf16 in the swizzle of box[0]'s bytes (32, 64 or 128).
 bool dx_box_map(CUtensorMap* out, const void* base, bool fp32, int rank, const uint64_t* dims, const uint64_t* strides,
                 const uint32_t* box);
-// ... of [rows][cols], boxes of 64 columns by box_rows rows (1: for gathered rows)
+// ... of [rows][cols], boxes of 64 columns by box_rows rows
 bool dx_matrix_map(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
