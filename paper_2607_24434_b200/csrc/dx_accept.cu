@@ -350,15 +350,15 @@ __global__ void __launch_bounds__(kRingThreads, 1) dx_accept_ring_kernel(AcceptP
           bulk_g2s(smem_u32(ring + (size_t)slot * TILE + (size_t)r * STRIDE), Wb + ((size_t)tile * 16 + r) * ROW, ROW, fb, pol);
         if (++slot == (uint32_t)kRingSlots) { slot = 0; phase ^= 1u; }
       }
-      if (*abort_flag) {
-        // something gave up: no copy may still be landing in this CTA's shared memory when it is released
+      if (ring_drains(abort_flag, wait_limit)) {
+        // no copy may still be landing in this CTA's shared memory when it is released
         const uint32_t n_back = issued < (uint32_t)kRingSlots ? issued : (uint32_t)kRingSlots;
         for (uint32_t k = 1; k <= n_back; ++k) {
           const uint32_t j = issued - k, s = j % (uint32_t)kRingSlots, ph = (j / (uint32_t)kRingSlots) & 1u;
           for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
             if (mbar_try_wait(smem_u32(&hdr->full[s]), ph)) break;
         }
-        if (p.dev_status) atomicExch(p.dev_status, (int32_t)DX_DEV_WAIT_EXPIRED);
+        if (*abort_flag && p.dev_status) atomicExch(p.dev_status, (int32_t)DX_DEV_WAIT_EXPIRED);
       }
     }
     __syncwarp();

@@ -216,15 +216,15 @@ __global__ void __launch_bounds__(kStackThreads, 1) dx_draft_stack_kernel(DxStac
       }
       __syncwarp();
     }
-    if (lane == 0 && *abort_flag) {
-      // something gave up: make sure no copy is still landing in this CTA's shared memory before it is released
+    if (lane == 0 && ring_drains(abort_flag, p.wait_limit)) {
+      // make sure no copy is still landing in this CTA's shared memory before it is released
       const uint32_t n_back = it < (uint32_t)n_slots ? it : (uint32_t)n_slots;
       for (uint32_t k = 1; k <= n_back; ++k) {
         const uint32_t j = it - k, s = j % (uint32_t)n_slots, ph = (j / (uint32_t)n_slots) & 1u;
         for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
           if (mbar_try_wait(smem_u32(&hdr->full[s]), ph)) break;
       }
-      atomicExch(p.dev_status, DX_DEV_WAIT_EXPIRED);
+      if (*abort_flag) atomicExch(p.dev_status, DX_DEV_WAIT_EXPIRED);
     }
     return;
   }

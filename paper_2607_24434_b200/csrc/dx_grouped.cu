@@ -266,8 +266,8 @@ __global__ void __launch_bounds__(kThreads, 1) dx_experts_bf16_kernel(DxExpertPa
     asm volatile("bar.arrive 2, 288;" ::: "memory");
     if (lane == 0) {
       issue(e_lo, e_hi, u_lo, u_hi);
-      if (*abort_flag) {
-        // something gave up: make sure no copy is still landing in this CTA's
+      if (ring_drains(abort_flag, p.wait_limit)) {
+        // make sure no copy is still landing in this CTA's
         // shared memory before it is released (bounded, ignores the flag; the copies themselves take
         // microseconds, so this uses the library's default limit whatever the context's limit is)
         const uint32_t n_back = it < (uint32_t)n_slots ? it : (uint32_t)n_slots;
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) dx_experts_bf16_kernel(DxExpertPa
           for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
             if (mbar_try_wait(smem_u32(&hdr->full[s]), ph)) break;
         }
-        atomicExch(p.dev_status, DX_DEV_WAIT_EXPIRED);
+        if (*abort_flag) atomicExch(p.dev_status, DX_DEV_WAIT_EXPIRED);
       }
     }
     return;

@@ -55,6 +55,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   *abort_flag = 1;
   return false;
 }
+// Whether the copy thread of a ring, having issued its last copy, waits for what is still in flight before it is done: where
+// something gave up, and where the limit is short enough for a consumer to give up on a copy that is still going to land (by then
+// this thread would be gone, and the shared memory released under the copy).  Within the default limit every copy lands.
+__device__ __forceinline__ bool ring_drains(const volatile int* abort_flag, uint32_t limit) {
+  return *abort_flag || limit < DX_WAIT_LIMIT_DEFAULT;
+}
 // Expert weights are read exactly once per launch: mark them evict-first in L2 so that they do not push out
 // what is reused (block rows, router matrix, work list, output rows).
 __device__ __forceinline__ uint64_t l2_evict_first_policy() {

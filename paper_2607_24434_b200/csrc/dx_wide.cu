@@ -406,15 +406,15 @@ __global__ void __launch_bounds__(kWideThreads, 1) dx_experts_wide_kernel(DxExpe
       mbar_arrive(smem_u32(&hdr->list_ready));   // (release: everything written above is visible to who waits)
       if (!paired) dx_pdl_trigger();   // what follows on the stream may be scheduled (it waits for this grid to end)
       stream(n_a, np);
-      if (*abort_flag) {
-        // something gave up: no copy may still be landing when the CTA's shared memory is released
+      if (ring_drains(abort_flag, p.wait_limit)) {
+        // no copy may still be landing when the CTA's shared memory is released
         const uint32_t n_back = it < (uint32_t)n_stages ? it : (uint32_t)n_stages;
         for (uint32_t k = 1; k <= n_back; ++k) {
           const uint32_t j = it - k, s = j % (uint32_t)n_stages, ph = (j / (uint32_t)n_stages) & 1u;
           for (uint32_t spin = 0; spin < DX_WAIT_LIMIT_DEFAULT; ++spin)
             if (mbar_try_wait(smem_u32(&hdr->full[s]), ph)) break;
         }
-        atomicExch(p.dev_status, DX_DEV_WAIT_EXPIRED);
+        if (*abort_flag) atomicExch(p.dev_status, DX_DEV_WAIT_EXPIRED);
       }
     }
   } else if (warp == 5) {
