@@ -484,8 +484,8 @@ dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc* desc, cons
  * short (random signs: 4e-6 of the root mean square).  Longer contractions are summed in sections of 4096 terms -- where the
  * result is rounded to bf16, of 32768, 2e-4 short -- which are added up rounded to nearest, so that no more is lost however
  * long they are. Every matrix has a 16-byte aligned address, a row pitch (in elements) and sizes that are multiples of 8;
- * n_groups <= 256, otherwise any size up to 2^35 elements from a matrix's first row to its last.  (DX_ERR_UNSUPPORTED
- * beyond.)  Outputs must not overlap inputs or one another, nor the workspace anything; matrices that do are refused
+ * n_groups <= 256, otherwise any size up to 2^31 - 2049 rows or columns and 2^35 elements from a matrix's first row to its
+ * last.  (DX_ERR_UNSUPPORTED beyond.)  Outputs must not overlap inputs or one another, nor the workspace anything; matrices that do are refused
  * (DX_ERR_INVALID_ARG; of a matrix counts everything between its first and its last element, what lies between its rows too).
  *
  * Groups.  Sorted row r belongs to group e iff offsets[e] <= r < offsets[e+1] (offsets [n_groups+1], ascending, within 0 ..

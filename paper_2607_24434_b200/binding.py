@@ -1023,7 +1023,7 @@ def moe_grouped_swiglu_backward(ctx: Context, dy: torch.Tensor, w_down: torch.Te
         space = torch.empty(n_space, dtype=torch.uint8, device=dy.device)
     _check(ctx.lib.moe_grouped_swiglu_backward(ctx.handle, C.byref(d), _ptr(dy), dy.shape[0], ld_dy, _ptr(w_down),
                                                _ptr(gate_up), ld_gu, _ptr(topk_w),
-                                               dy.shape[0] * gather_div if topk_w is None else topk_w.numel(),
+                                               min(2 ** 31 - 1, dy.shape[0] * gather_div if topk_w is None else topk_w.numel()),
                                                _ptr(offsets), _ptr(gather), gather_div, _ptr(out["d_gate_up"]), ld_d,
                                                _ptr(out["act_w"]), ld_act, _ptr(d_w), _ptr(space), n_space,
                                                _ctx_stream(ctx)), "moe_grouped_swiglu_backward")

@@ -959,6 +959,8 @@ extern "C" dx_status moe_route_tokens_backward(dx_ctx* ctx, const dx_route_desc*
 // ---- whole batches of tokens: the experts, their combination, the loss -------------------------------------------------
 namespace {
 
+constexpr int32_t kMostRows = INT32_MAX - 2048;      // (what 32 bits count, less the largest step that is added to it)
+
 // a matrix of the tensor-core products: address, pitch and width in whole 16-byte vectors of bf16 (8 elements)
 dx_status check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld) {
   if (rows < 0 || cols < 1 || ld < cols) return DX_ERR_SHAPE;
@@ -983,7 +985,8 @@ dx_status check_groups(const dx_grouped_desc* d, const void* w) {
   if (d->ld_w > (int64_t(1) << 36) || d->stride_w < (int64_t)(d->n - 1) * d->ld_w + d->k ||
       d->stride_w > (int64_t(1) << 38)) return DX_ERR_SHAPE;
   if (d->n_groups > DX_MAX_E || d->n % 8 || d->k % 8 || d->ld_w % 8 || d->stride_w % 8) return DX_ERR_UNSUPPORTED;
-  // (tiles are numbered in 32 bits)
+  // (rows, columns and tiles are numbered in 32 bits, up to a tile behind the last)
+  if (d->n_rows > kMostRows || d->n > kMostRows || d->k > kMostRows) return DX_ERR_UNSUPPORTED;
   const int64_t a = (d->n + 63) / 64, b = (d->k + 63) / 64, rows = d->n_rows / 64 + d->n_groups;
   const int64_t most = a > b ? a : b;
   if (a * b > INT32_MAX / d->n_groups || rows * most > INT32_MAX) return DX_ERR_UNSUPPORTED;
@@ -1152,7 +1155,7 @@ namespace {
 dx_status check_combine(const dx_ctx* ctx, int32_t N, int32_t k, int32_t H) {
   if (!ctx) return DX_ERR_INVALID_ARG;
   if (N < 0 || k < 1 || H < 1) return DX_ERR_SHAPE;
-  if (k > DX_MAX_TOPK || (int64_t)N * k > INT32_MAX) return DX_ERR_UNSUPPORTED;
+  if (k > DX_MAX_TOPK || (int64_t)N * k > kMostRows || H > kMostRows) return DX_ERR_UNSUPPORTED;
   return DX_OK;
 }
 }  // namespace
@@ -1203,8 +1206,8 @@ extern "C" dx_status moe_combine_tokens_backward(dx_ctx* ctx, const void* dy, in
 
 namespace {
 // (tiles, pieces and rows are numbered in 32 bits)
-bool head_countable(int32_t N, int32_t V) {
-  return ((int64_t)N / 128 + 1) * ((int64_t)V / 256 + 1) <= INT32_MAX && V <= INT32_MAX - 512 && N <= INT32_MAX - 2048;
+bool head_countable(int32_t N, int32_t V, int32_t H) {
+  return ((int64_t)N / 128 + 1) * ((int64_t)V / 256 + 1) <= INT32_MAX && V <= kMostRows && N <= kMostRows && H <= kMostRows;
 }
 }  // namespace
 
@@ -1212,7 +1215,7 @@ extern "C" dx_status spec_head_loss_workspace(dx_ctx* ctx, int32_t N, int32_t V,
                                               size_t* best_out) {
   if (!ctx || !least_out || !best_out) return DX_ERR_INVALID_ARG;
   if (N < 0 || V < 1 || H < 1) return DX_ERR_SHAPE;
-  if (!head_countable(N, V)) return DX_ERR_UNSUPPORTED;
+  if (!head_countable(N, V, H)) return DX_ERR_UNSUPPORTED;
   *least_out = *best_out = 0;
   if (N > 0) dx_head_loss_workspace(ctx->sm_count, N, V, H, grad, least_out, best_out);
   return DX_OK;
@@ -1229,7 +1232,7 @@ extern "C" dx_status spec_head_loss(dx_ctx* ctx, const void* h, int32_t N, int64
   if (s == DX_OK && dh) s = check_matrix(dh, N, H, ld_dh);
   if (s == DX_OK && dW) s = check_matrix(dW, V, H, ld_dW);
   if (s != DX_OK) return s;
-  if (!head_countable(N, V)) return DX_ERR_UNSUPPORTED;
+  if (!head_countable(N, V, H)) return DX_ERR_UNSUPPORTED;
   if (!loss && !dh && !dW) return DX_ERR_INVALID_ARG;
   const Range in[2] = {rows_range(h, N, H, ldh, 2), rows_range(W_lm, V, H, ldw, 2)};
   const Range out[2] = {rows_range(dh, dh ? N : 0, H, ld_dh, 2), rows_range(dW, dW ? V : 0, H, ld_dW, 2)};

@@ -64,3 +64,29 @@ def test_workspace_refuses_what_the_loss_refuses(lib):
     assert ask(1 << 24, 100, 64) == 0 and a.value > (1 << 24) * 128 and ask(10, 1 << 24, 64) == 0
     call = lambda N, V: L.spec_head_loss(ctx, A, N, 64, B, V, 64, 64, 64, None, 64, None, 64, None, 64, G, 1 << 62, None)  # noqa: E731
     assert call(top, 100) == 8 and call(top - 2047, 100) == 8 and call(10, top) == 8 and call(1 << 29, 1 << 29) == 8 and call(10, 100) == 3
+
+
+def test_sizes_that_32_bits_do_not_count(lib):
+    """Rows, columns and tokens that reach 2^31 with the step of a grid or a tile behind them: refused, not counted past it."""
+    binding, L, ctx, _ = lib
+    top = 2 ** 31 - 8
+    desc = lambda rows=100, n=64, k=32: ctypes.byref(binding.GroupedDesc(1, rows, n, k, k, n * k))  # noqa: E731
+    far = 1 << 45
+
+    def mm(d, x_rows=100, ldx=32, y_rows=100, ldy=64, t=0):
+        return L.moe_grouped_mm(ctx, d, A, x_rows, ldx, far, t, 64, None, 1, None, 2 * far, 1, y_rows, ldy, None)
+
+    assert mm(desc(n=top, k=8), ldx=8, ldy=top, y_rows=1, x_rows=100) in (2, 8)
+    assert mm(desc(rows=1, n=top, k=8), ldx=8, ldy=top) == 8 and mm(desc(rows=1, n=8, k=top), ldx=top, ldy=8, x_rows=1) == 8
+    assert mm(desc(rows=top, n=8, k=8), x_rows=top, ldx=8, y_rows=top, ldy=8) == 8
+    assert mm(desc(rows=1 << 30, n=8, k=8), x_rows=1 << 30, ldx=8, y_rows=1 << 30, ldy=8) == 3
+    dw = lambda d, rows, n, k: L.moe_grouped_mm_dw(ctx, d, A, rows, n, None, 1, far, rows, k, None, 1, 64, 2 * far, 0, None)  # noqa: E731
+    assert dw(desc(top, 8, 8), top, 8, 8) == 8 and dw(desc(1, top, 8), 1, top, 8) == 8 and dw(desc(1, 8, top), 1, 8, top) == 8
+    assert dw(desc(1 << 30, 8, 8), 1 << 30, 8, 8) == 3
+    combine = lambda N, k, H: L.moe_combine_tokens(ctx, A, 1, H, None, N, k, H, far, 1, H, None)  # noqa: E731
+    back = lambda N, k, H: L.moe_combine_tokens_backward(ctx, A, H, far, H, 1, None, N, k, H, 2 * far, H, None, None)  # noqa: E731
+    for call in (combine, back):
+        assert call(2 ** 31 - 1, 1, 8) == 8 and call(2 ** 28, 8, 8) == 8 and call(1, 1, top) == 8 and call(1 << 30, 1, 8) == 3
+    a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    assert L.spec_head_loss_workspace(ctx, 1, 100, top, 1, ctypes.byref(a), ctypes.byref(b)) == 8
+    assert L.spec_head_loss(ctx, A, 1, top, far, 1, top, top, 64, None, 64, None, top, None, top, G, 1 << 62, None) == 8
