@@ -260,6 +260,40 @@ def test_gates_gradients_through_long_rows(dx, rows):
     assert float(((got["d_gate_up"][:, I:].double() - d_up).abs() / d_up).max()) <= bound + 2.0 ** -8
 
 
+def test_long_contractions_repeat_themselves(dx):
+    """Random operands, long and short groups: the same bits in every call, in place and gathered, alone and beside other work."""
+    binding, ctx = dx
+    g = rng(21)
+    off = ints(0, 9000, 9001, 9001, 22000, 22300, 31000)
+    P = 31000
+    dy, x = draw(g, P, 520), draw(g, P, 776)
+    order = torch.randperm(P, generator=g, device="cuda")
+    put = lambda t: torch.empty_like(t).index_copy_(0, order, t)  # noqa: E731
+    dy2, x2, named = put(dy), put(x), order.to(torch.int32)
+    want = binding.moe_grouped_mm_dw(ctx, dy, x, off, out_dtype=F32).clone()
+    ref = torch.stack([dy[a:b].double().t() @ x[a:b].double() for a, b in zip(off.tolist(), off.tolist()[1:])])
+    # (root mean square of the errors: running sums are no larger than the final ones in the mean)
+    for e in range(6):
+        if ref[e].any():
+            assert float((want[e].double() - ref[e]).pow(2).mean().sqrt()) <= long_bound(P, 4096) * float(ref[e].pow(2).mean().sqrt())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            busy = binding.moe_grouped_mm_dw(ctx, x2, dy2, off, gather_dy=named, gather_x=named, out_dtype=F32)
+        assert torch.equal(binding.moe_grouped_mm_dw(ctx, dy, x, off, out_dtype=F32), want)
+        assert torch.equal(binding.moe_grouped_mm_dw(ctx, dy2, x2, off, gather_dy=named, gather_x=named, out_dtype=F32), want)
+    torch.cuda.synchronize()
+    assert float((busy.transpose(1, 2) - want).abs().max()) <= 1e-4 * float(want.abs().max())      # (the transposed product)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = binding.moe_grouped_mm_dw(ctx, dy, x, off, out_dtype=F32)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(held, want)
+    del graph
+
+
 # ---- weights of exactly 0 --------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("N,k,H", [(5, 3, 64), (40, 8, 1000), (2500, 2, 264)])
