@@ -10,7 +10,7 @@
 // the weights' bytes (34.6 MB, 5.4 us at the copy rate) fetched by 96 CTAs of 148 SMs behind a chain of launch, offsets and
 // first stage: 12.2 us; SwiGLU (69 MB, 132 CTAs) 16.5.  700 tokens, SwiGLU gradient: 370 MB of weights, 98 us with the gates'
 // sums.  16384 tokens: the products (669 us at the burst rate, 813 at the sustained one) under the power cap, W^T x 940 to 1015
-// us, SwiGLU that keeps its products 993 to 1052.  Weight gradients of many rows: 1.5 GB of fp32 results, gathered rows and
+// us, SwiGLU that keeps its products 993 to 1060.  Weight gradients of many rows: 1.5 GB of fp32 results, gathered rows and
 // operands through the SMs' path to L2, which is 74 % busy, the tensor pipe 45 % (8192 tokens 619 to 676 us, 335 by the
 // products alone); of few rows the results (64 rows per group 4.9 TB/s in fp32, 4.7 in bf16).
 #include <limits.h>
@@ -305,7 +305,7 @@ struct StoreSwiglu : FragmentEpilogue<32> {
 //   share of d w = sum over lanes of D gate s up.
 // The rows of a pair of weight 0 get zeros, whatever they hold.  gate and up come as boxes, a chunk ahead; their place in the
 // staging takes the gradients, which go out as boxes.  (In pieces through registers, every element crossed the load/store path
-// six times: 458 us, 49152 rows x 2048 x 1408, where boxes took 423 in the same run; 396 to 419 now.)  Nothing is at its limit
+// six times: 458 us, 49152 rows x 2048 x 1408, where boxes took 423 in the same run; 396 to 421 now.)  Nothing is at its limit
 // there -- an instruction in 38 % of the cycles, tensor pipe 47 %, DRAM 50 %, path to L2 40 %: what bounds it is the chain of
 // each chunk -- its products' way out of tensor memory, exponential and reciprocal, stores, fence, box -- with two storing
 // warps per scheduler and no registers to have two chunks under way.

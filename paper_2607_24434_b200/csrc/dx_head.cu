@@ -21,7 +21,7 @@
 // added up in order afterwards (dh alone has no more tiles than H / 128: 16 of 148 SMs at H = 2048).
 //
 // 16 rows x 102400 words x 2048: 147 to 159 us with dh, of which the head's two ways from memory are 130; the loss alone 76 (65).
-// 4096 rows (a quarter of them padding) with both gradients 3.60 to 3.73 ms, the three products 2.8 at the rate that the power
+// 4096 rows (a quarter of them padding) with both gradients 3.60 to 3.80 ms, the three products 2.8 at the rate that the power
 // cap allows; 4096 rows, loss alone 1.10 ms.
 #include "dx_mm.cuh"
 
